@@ -19,7 +19,10 @@
  *     and its gradient (Sec. 2.3, Eq. bracket-loss), and the labelling stage
  *     of the two-stage parser (Sec. 2.1, Eq. label-argmax);
  *   - the span (and label) scores themselves, from boundary representations
- *     by the biaffine scorer (Sec. 2.2, Eq. biaffine).
+ *     by the biaffine scorer (Sec. 2.2, Eq. biaffine), and the scorer's
+ *     backward pass, from the representations or from an 8-bit form of them;
+ *   - log-probabilities of given trees and a clipped policy loss on them with
+ *     its gradient, for training past the gold trees.
  *
  * Conventions
  *   Fence posts.  A sentence of n words has boundaries 0..n; span (i,j),
@@ -94,6 +97,8 @@ enum {
 
 #define CRF_MAX_LEN 1023      /* longest sentence, in words */
 #define CRF_MAX_LABELS 4096   /* most labels per span */
+#define CRF_MAX_TREES 64      /* most candidate trees per sentence */
+#define CRF_MAX_ROW 8192      /* longest activation row held in 8 bits */
 
 /* Plan flags. */
 #define CRF_FORCE_SPILL 0x1u  /* run every sentence on the workspace-chart kernels */
@@ -311,6 +316,103 @@ int crf_biaffine_scores(const crf_plan *plan, const uint16_t *rl, const uint16_t
 int crf_inside_fwd_bwd_cky_noalloc(const crf_plan *plan, const float *scores, const float *grad_logZ,
                                    float *logZ, float *marginals, int32_t *spans, float *best,
                                    void *stream);
+
+/*
+ * Workspaces.  The calls below that take one use it, device memory of the
+ * caller of at least the size that the plan's query gives, 256-byte aligned,
+ * only while they run: calls that may overlap need one each (two graphs that
+ * are replayed side by side too).  The calls still use the plan's own
+ * workspace like the others, so calls on one plan must not overlap.
+ */
+
+/* crf_tree_workspace -- bytes of workspace of crf_tree_logprobs and
+ * crf_policy_loss. */
+int crf_tree_workspace(const crf_plan *plan, int64_t *bytes);
+
+/*
+ * crf_tree_logprobs -- log-probabilities of given trees (Sec. 2.1,
+ * Eq. tree-prob): log p(y|x) = s(x,y) - log Z(x), s(x,y) the sum of the
+ * spans' scores (Eq. tree-score); sums and differences in float64.
+ *   trees       device int32 [B][num_trees][2*(N1-1)-1][2], 8-byte aligned: of
+ *               each tree the first 2n_b-1 rows are its spans (i,j) (what
+ *               crf_cky_decode writes; any order).  Rows that are not spans of
+ *               the sentence (0 <= i < j <= n_b) are skipped; a repeated span
+ *               adds its score again.
+ *   num_trees   G, 1 <= G <= CRF_MAX_TREES.
+ *   counts      device int32[B]: the first counts[b] trees of sentence b are
+ *               there (clamped to 0..G), or NULL: all of them.
+ *   logp        device float32 [B][G]: log p of the trees that are there; the
+ *               others' entries are left as they were.
+ *   logZ        device float32 [B], or NULL: log Z(x_b).
+ * Unlabelled plans only (CRF_EUNSUPPORTED otherwise).
+ */
+int crf_tree_logprobs(const crf_plan *plan, const float *scores, const int32_t *trees, int32_t num_trees,
+                      const int32_t *counts, float *logp, float *logZ, void *workspace, int64_t workspace_bytes,
+                      void *stream);
+
+/*
+ * crf_tree_logprobs_bwd -- the gradient of sum_g u_g log p(y_g|x_b) with
+ * respect to the scores, u = grad_logp:
+ *   sum_{g: (i,j) in y_g} u_g - (sum_g u_g) p((i,j)|x_b).
+ *   trees, num_trees, counts: as crf_tree_logprobs; a repeated span counts
+ *               once.
+ *   grad_logp   device float32 [B][G]; the entries of trees that are not there
+ *               are not read.
+ *   grad_scores device float32, layout of scores (must not alias scores):
+ *               valid cells only.
+ * Unlabelled plans only (CRF_EUNSUPPORTED otherwise).  Needs no workspace.
+ */
+int crf_tree_logprobs_bwd(const crf_plan *plan, const float *scores, const int32_t *trees, int32_t num_trees,
+                          const int32_t *counts, const float *grad_logp, float *grad_scores, void *stream);
+
+/*
+ * crf_policy_loss -- clipped policy loss of each sentence's trees with a KL
+ * term, and its gradient with respect to the scores.  With A the advantages,
+ * r_g = exp(log p_g - old_g), q_g = ref_g - log p_g and c = counts[b]:
+ *   L_b = 1/c sum_g [ -min(r_g A_g, clip(r_g, 1 - clip_low, 1 + clip_high) A_g)
+ *                     + kl_coef (exp(q_g) - q_g - 1) ],
+ *   dL_b/ds(i,j) = sum_{g: (i,j) in y_g} c_g - (sum_g c_g) p((i,j)|x_b),
+ *   c_g = dL_b/dlog p_g = 1/c [ -r_g A_g [r_g A_g <= clip(r_g) A_g]
+ *                               + kl_coef (1 - exp(q_g)) ].
+ * log p_g - old_g and q_g above 80 are taken as 80.  A sentence without trees
+ * has the loss 0 and the gradient 0.
+ *   trees, num_trees, counts, logp (or NULL): as crf_tree_logprobs; a repeated
+ *               span counts once in the gradient.
+ *   advantages, old_logp  device float32 [B][G].
+ *   ref_logp    device float32 [B][G], or NULL: no KL term (kl_coef is 0).
+ *   clip_low    0 <= clip_low <= 1; clip_high >= 0; kl_coef >= 0.
+ *   grad_loss   device float32[B] upstream gradient dOut/dL_b, or NULL for 1.
+ *   loss        device float32[B]: L_b (not scaled by grad_loss).
+ *   grad_scores device float32, layout of scores (must not alias scores):
+ *               grad_loss[b] dL_b/ds(i,j) on valid cells only.
+ * Unlabelled plans only (CRF_EUNSUPPORTED otherwise).
+ */
+int crf_policy_loss(const crf_plan *plan, const float *scores, const int32_t *trees, int32_t num_trees,
+                    const int32_t *counts, const float *advantages, const float *old_logp, const float *ref_logp,
+                    float clip_low, float clip_high, float kl_coef, const float *grad_loss, float *loss, float *logp,
+                    float *grad_scores, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * crf_pack_rows -- activation rows in 8 bits, for what a backward pass keeps.
+ * Blocks of 32 entries of a row share a power of two: with m the largest
+ * finite magnitude of a block, code = e4m3(x 2^-s) (nearest, ties to even),
+ * s = max(ceil(log2(m / 448)), -127), and the code stands for code 2^s.
+ * Magnitudes from 1.9375 2^127 up are held as 1.875 2^127 (the nearest code
+ * would stand for 2^128).  Infinities and NaN become the code's NaN.
+ *   x       device bf16 bit patterns [B][N1][d], 8-byte aligned; rows past n_b
+ *           are not read.
+ *   d       4 <= d <= CRF_MAX_ROW, a multiple of 4.
+ *   codes   device uint8 [B][N1][dc], dc = d rounded up to a multiple of 32,
+ *           16-byte aligned: e4m3 (no infinities) bit patterns, zeros past d.
+ *   scales  device uint8 [B][N1][dc/32]: s + 127.
+ * Rows past n_b are left as they were.  B, N1 and the lengths are the plan's.
+ */
+int crf_pack_rows(const crf_plan *plan, const uint16_t *x, int32_t d, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* crf_unpack_rows -- the values that packed rows stand for, as bf16 (exact but
+ * for values below 2^-126); rows past n_b are left as they were. */
+int crf_unpack_rows(const crf_plan *plan, const uint8_t *codes, const uint8_t *scales, int32_t d, uint16_t *x,
+                    void *stream);
 
 /* Static description of a status code. */
 const char *crf_status_string(int status);

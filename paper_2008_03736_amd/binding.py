@@ -18,12 +18,17 @@ LIB_PATH = os.path.join(PKG, "libcrfinside.so")
 CRF_OK, CRF_EINVAL, CRF_ENOMEM, CRF_EHIP, CRF_EUNSUPPORTED = 0, 1, 2, 3, 4
 CRF_MAX_LEN = 1023
 CRF_MAX_LABELS = 4096
+CRF_MAX_TREES = 64
+CRF_MAX_ROW = 8192
+ROW_BLOCK = 32          # entries of a packed row that share a power of two
 CRF_FORCE_SPILL = 0x1
 CRF_NO_TEAMS = 0x2
 
 # Every function the C header declares, with its ctypes signature.
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
+_I64 = ctypes.c_int64
+_F32 = ctypes.c_float
 SIGNATURES = {
     "crf_plan_create": (ctypes.c_int, [ctypes.POINTER(_P), _P, _I32, _I32, _I32, ctypes.c_uint32]),
     "crf_plan_destroy": (ctypes.c_int, [_P]),
@@ -39,6 +44,13 @@ SIGNATURES = {
     "crf_cky_decode_labeled": (ctypes.c_int, [_P, _P, _P, _P, _P, _P]),
     "crf_label_spans": (ctypes.c_int, [_P, _P, _I32, _P, _P, _P]),
     "crf_biaffine_scores": (ctypes.c_int, [_P, _P, _P, _P, _I32, _I32, _I32, _P, _P]),
+    "crf_tree_workspace": (ctypes.c_int, [_P, ctypes.POINTER(_I64)]),
+    "crf_tree_logprobs": (ctypes.c_int, [_P, _P, _P, _I32, _P, _P, _P, _P, _I64, _P]),
+    "crf_tree_logprobs_bwd": (ctypes.c_int, [_P, _P, _P, _I32, _P, _P, _P, _P]),
+    "crf_policy_loss": (ctypes.c_int, [_P, _P, _P, _I32, _P, _P, _P, _P, _F32, _F32, _F32, _P, _P, _P, _P, _P, _I64,
+                                       _P]),
+    "crf_pack_rows": (ctypes.c_int, [_P, _P, _I32, _P, _P, _P]),
+    "crf_unpack_rows": (ctypes.c_int, [_P, _P, _P, _I32, _P, _P]),
     "crf_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "crf_last_error": (ctypes.c_char_p, []),
 }
@@ -162,6 +174,37 @@ def crf_label_spans(plan, label_scores, num_labels, spans, labels, stream):
 def crf_biaffine_scores(plan, rl, rr, w, d, ldw, num_labels, scores, stream):
     _check(load().crf_biaffine_scores(plan, rl, rr, w, d, ldw, num_labels, scores, stream),
            "crf_biaffine_scores")
+
+
+def crf_tree_workspace(plan):
+    n = _I64()
+    _check(load().crf_tree_workspace(plan, ctypes.byref(n)), "crf_tree_workspace")
+    return n.value
+
+
+def crf_tree_logprobs(plan, scores, trees, num_trees, counts, logp, logZ, workspace, workspace_bytes, stream):
+    _check(load().crf_tree_logprobs(plan, scores, trees, num_trees, counts, logp, logZ, workspace, workspace_bytes,
+                                    stream), "crf_tree_logprobs")
+
+
+def crf_tree_logprobs_bwd(plan, scores, trees, num_trees, counts, grad_logp, grad_scores, stream):
+    _check(load().crf_tree_logprobs_bwd(plan, scores, trees, num_trees, counts, grad_logp, grad_scores, stream),
+           "crf_tree_logprobs_bwd")
+
+
+def crf_policy_loss(plan, scores, trees, num_trees, counts, advantages, old_logp, ref_logp, clip_low, clip_high,
+                    kl_coef, grad_loss, loss, logp, grad_scores, workspace, workspace_bytes, stream):
+    _check(load().crf_policy_loss(plan, scores, trees, num_trees, counts, advantages, old_logp, ref_logp, clip_low,
+                                  clip_high, kl_coef, grad_loss, loss, logp, grad_scores, workspace, workspace_bytes,
+                                  stream), "crf_policy_loss")
+
+
+def crf_pack_rows(plan, x, d, codes, scales, stream):
+    _check(load().crf_pack_rows(plan, x, d, codes, scales, stream), "crf_pack_rows")
+
+
+def crf_unpack_rows(plan, codes, scales, d, x, stream):
+    _check(load().crf_unpack_rows(plan, codes, scales, d, x, stream), "crf_unpack_rows")
 
 
 def crf_status_string(status):
@@ -419,6 +462,125 @@ class Plan:
                             scores.data_ptr(), _stream_ptr(t, self.device))
         return scores
 
+    def _tensor(self, x, name, shape, dtypes, optional=False):
+        """Pointer of a contiguous tensor of the given shape on the plan's device."""
+        if x is None and optional:
+            return None
+        if tuple(x.shape) != tuple(shape) or x.dtype not in dtypes:
+            raise ValueError(f"{name} must be {' or '.join(str(t) for t in dtypes)} {tuple(shape)}, got "
+                             f"{x.dtype} {tuple(x.shape)}")
+        if x.device != self.device:
+            raise ValueError(f"{name} on {x.device}, plan on {self.device}")
+        if not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return x.data_ptr()
+
+    def _trees(self, trees, counts):
+        """(number of trees, pointers of trees and counts)."""
+        t = self._torch
+        if trees.dim() != 4:
+            raise ValueError("trees must be [B, G, 2 (N1 - 1) - 1, 2]")
+        G, R = int(trees.shape[1]), 2 * (self.n1 - 1) - 1
+        return (G, self._tensor(trees, "trees", (self.B, G, R, 2), (t.int32,)),
+                self._tensor(counts, "counts", (self.B,), (t.int32,), optional=True))
+
+    def _workspace(self, size):
+        return self._torch.empty(max(int(size), 1), dtype=self._torch.uint8, device=self.device)
+
+    def _out(self, x, shape, dtype, zero=False):
+        if x is not None:
+            return x
+        make = self._torch.zeros if zero else self._torch.empty
+        return make(shape, dtype=dtype, device=self.device)
+
+    def tree_logprobs(self, scores, trees, counts=None, logp=None, logZ=None):
+        """Log-probabilities of G trees a sentence (Sec. 2.1, Eq. tree-prob):
+        trees int32 [B, G, 2(N1-1)-1, 2] as cky_decode writes them, counts
+        int32 [B] (how many of them are there; default all).  Returns
+        (logp [B, G], logZ [B]); a fresh logp is 0 where no tree is there."""
+        t = self._torch
+        sp = self._scores(scores)
+        G, tp, cp = self._trees(trees, counts)
+        logp = self._out(logp, (self.B, G), t.float32, zero=counts is not None)
+        logZ = self._out(logZ, (self.B,), t.float32)
+        ws = self._workspace(crf_tree_workspace(self._handle))
+        crf_tree_logprobs(self._handle, sp, tp, G, cp, self._tensor(logp, "logp", (self.B, G), (t.float32,)),
+                          self._vec(logZ, "logZ"), ws.data_ptr(), ws.numel(), _stream_ptr(t, self.device))
+        return logp, logZ
+
+    def tree_logprobs_bwd(self, scores, trees, grad_logp, counts=None, grad_scores=None):
+        """Gradient of sum(grad_logp * logp) with respect to the scores (valid
+        cells only; a fresh buffer is zero-filled)."""
+        t = self._torch
+        sp = self._scores(scores)
+        G, tp, cp = self._trees(trees, counts)
+        up = self._tensor(grad_logp, "grad_logp", (self.B, G), (t.float32,))
+        grad_scores = self._out(grad_scores, scores.shape, t.float32, zero=True)
+        crf_tree_logprobs_bwd(self._handle, sp, tp, G, cp, up,
+                              self._tensor(grad_scores, "grad_scores", scores.shape, (t.float32,)),
+                              _stream_ptr(t, self.device))
+        return grad_scores
+
+    def policy_loss(self, scores, trees, advantages, old_logp, ref_logp=None, counts=None, clip_low=0.2, clip_high=0.2,
+                    kl_coef=0.0, grad_loss=None, loss=None, logp=None, grad_scores=None):
+        """Clipped policy loss of G trees a sentence with a KL term: (loss [B],
+        logp [B, G], gradient shaped like scores).  advantages, old_logp and
+        ref_logp (needed where kl_coef is not 0) are float32 [B, G]; a fresh
+        gradient is zero-filled, a fresh logp 0 where no tree is there."""
+        t = self._torch
+        sp = self._scores(scores)
+        G, tp, cp = self._trees(trees, counts)
+        each = (self.B, G)
+        ins = [self._tensor(x, name, each, (t.float32,), optional=name == "ref_logp")
+               for x, name in ((advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"))]
+        loss = self._out(loss, (self.B,), t.float32)
+        logp = self._out(logp, each, t.float32, zero=counts is not None)
+        grad_scores = self._out(grad_scores, scores.shape, t.float32, zero=True)
+        ws = self._workspace(crf_tree_workspace(self._handle))
+        crf_policy_loss(self._handle, sp, tp, G, cp, *ins, float(clip_low), float(clip_high), float(kl_coef),
+                        self._vec(grad_loss, "grad_loss"), self._vec(loss, "loss"),
+                        self._tensor(logp, "logp", each, (t.float32,)),
+                        self._tensor(grad_scores, "grad_scores", scores.shape, (t.float32,)), ws.data_ptr(), ws.numel(),
+                        _stream_ptr(t, self.device))
+        return loss, logp, grad_scores
+
+    def _bf16(self, x, name, shape):
+        t = self._torch
+        return self._tensor(x, name, shape, (t.bfloat16, t.int16, t.uint16))
+
+    def _packed(self, codes, scales, d):
+        wide = (d + ROW_BLOCK - 1) // ROW_BLOCK * ROW_BLOCK
+        u8 = (self._torch.uint8,)
+        return (self._tensor(codes, "codes", (self.B, self.n1, wide), u8),
+                self._tensor(scales, "scales", (self.B, self.n1, wide // ROW_BLOCK), u8))
+
+    def pack_rows(self, x, codes=None, scales=None):
+        """Rows of bf16 activations [B, N1, d] in 8 bits: (codes uint8
+        [B, N1, dc], e4m3 bit patterns, dc = d rounded up to a multiple of 32;
+        scales uint8 [B, N1, dc/32], the exponent plus 127 of the power of two
+        that 32 codes share).  Rows past a sentence's last fence post are left
+        as they were (zero in fresh buffers)."""
+        t = self._torch
+        if x.dim() != 3:
+            raise ValueError("x must be [B, N1, d]")
+        d = int(x.shape[2])
+        xp = self._bf16(x, "x", (self.B, self.n1, d))
+        wide = (d + ROW_BLOCK - 1) // ROW_BLOCK * ROW_BLOCK
+        codes = self._out(codes, (self.B, self.n1, wide), t.uint8, zero=True)
+        scales = self._out(scales, (self.B, self.n1, wide // ROW_BLOCK), t.uint8, zero=True)
+        crf_pack_rows(self._handle, xp, d, *self._packed(codes, scales, d), _stream_ptr(t, self.device))
+        return codes, scales
+
+    def unpack_rows(self, codes, scales, d, out=None):
+        """The bf16 rows [B, N1, d] that packed ones stand for."""
+        t = self._torch
+        d = int(d)
+        cp, sc = self._packed(codes, scales, d)
+        out = self._out(out, (self.B, self.n1, d), t.bfloat16, zero=True)
+        crf_unpack_rows(self._handle, cp, sc, d, self._bf16(out, "out", (self.B, self.n1, d)),
+                        _stream_ptr(t, self.device))
+        return out
+
     def cky_decode(self, scores, spans=None, best=None):
         """(spans int32 [B, 2(N1-1)-1, 2] preorder padded with -1, best float32 [B])."""
         t = self._torch
@@ -453,3 +615,44 @@ def log_partition(scores, plan):
             return plan.inside_bwd(s, grad_logZ=g)
 
     return _LogZ.apply(scores)
+
+
+def tree_log_prob(scores, trees, plan, counts=None):
+    """Differentiable log-probabilities of given trees (Sec. 2.1,
+    Eq. tree-prob), float32 [B, G]: backward returns, per sentence, the trees'
+    upstream gradients on their spans less their sum times the marginals."""
+    import torch
+
+    class _LogP(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, s):
+            ctx.save_for_backward(s)
+            return plan.tree_logprobs(s, trees, counts=counts)[0]
+
+        @staticmethod
+        def backward(ctx, g):
+            (s,) = ctx.saved_tensors
+            g = g.float().contiguous()   # held by this frame until the call has been enqueued
+            return plan.tree_logprobs_bwd(s, trees, g, counts=counts)
+
+    return _LogP.apply(scores)
+
+
+def policy_loss(scores, trees, advantages, old_logp, plan, **options):
+    """Differentiable clipped policy loss, float32 [B] (Plan.policy_loss's
+    arguments): the gradient is computed with the loss and kept."""
+    import torch
+
+    class _Policy(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, s):
+            loss, _, grad = plan.policy_loss(s, trees, advantages, old_logp, **options)
+            ctx.save_for_backward(grad)
+            return loss
+
+        @staticmethod
+        def backward(ctx, g):
+            (grad,) = ctx.saved_tensors
+            return grad * g[:, None, None]
+
+    return _Policy.apply(scores)

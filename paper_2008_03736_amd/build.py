@@ -10,6 +10,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 SOURCES = [os.path.join(CSRC, "crf_kernels.hip"), os.path.join(CSRC, "crf_biaffine.hip"),
            os.path.join(CSRC, "crf_tile.hip"), os.path.join(CSRC, "crf_plan.cpp")]
+# the fine-tuning operators, linked into the same library
+TRAIN_SOURCES = [os.path.join(CSRC, "crf_trees.hip"), os.path.join(CSRC, "crf_rows.hip"),
+                 os.path.join(CSRC, "crf_train.cpp")]
 LIB = os.path.join(PKG, "libcrfinside.so")
 # microbenchmarks of the ceilings behind the roofline (bench.py --ceilings)
 CEIL_SOURCES = [os.path.join(CSRC, "crf_ceilings.hip")]
@@ -32,8 +35,10 @@ FLAGS = [
 
 
 # Per-kernel register, scratch and LDS use of the last build of LIB (one
-# line per kernel, tab-separated, from the compiler's resource remarks).
+# line per kernel, tab-separated, from the compiler's resource remarks): the
+# kernels of SOURCES and those of TRAIN_SOURCES.
 RESOURCES = os.path.join(PKG, "libcrfinside.resources.tsv")
+TRAIN_RESOURCES = os.path.join(PKG, "libcrfinside.train.resources.tsv")
 RESOURCE_FIELDS = ("VGPRs", "AGPRs", "TotalSGPRs", "ScratchSize [bytes/lane]", "VGPRs Spill", "SGPRs Spill",
                    "Occupancy [waves/SIMD]", "LDS Size [bytes/block]")
 _REMARK = re.compile(r"remark:\s+(Function Name|" + "|".join(re.escape(f) for f in RESOURCE_FIELDS)
@@ -69,10 +74,11 @@ def _write_resources(stderr_text, path):
             f.write("\t".join([d, r["name"]] + [r.get(k, "") for k in RESOURCE_FIELDS]) + "\n")
 
 
-def _compile(sources, lib, verbose, resources=None):
-    """Compile the sources side by side (one object each), then link."""
+def _compile(sources, lib, verbose, resources=()):
+    """Compile the sources side by side (one object each), then link.
+    resources: (path, its sources) of the resource reports to write."""
     flags = [f for f in FLAGS if f != "-shared"]
-    if resources is not None:
+    if resources:
         flags = ["-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics", *flags]
     objs = [f"{lib}.{os.path.basename(src)}.o" for src in sources]
     cmds = [[HIPCC, *flags, "-c", "-o", obj, src] for src, obj in zip(sources, objs)]
@@ -88,8 +94,8 @@ def _compile(sources, lib, verbose, resources=None):
             raise subprocess.CalledProcessError(r.returncode, cmd)
     tmp = lib + ".tmp"
     subprocess.run([HIPCC, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", tmp, *objs], check=True)
-    if resources is not None:
-        _write_resources("\n".join(r.stderr for r in runs), resources)
+    for path, of in resources:
+        _write_resources("\n".join(r.stderr for src, r in zip(sources, runs) if src in of), path)
     os.replace(tmp, lib)
     for obj in objs:
         os.remove(obj)
@@ -97,9 +103,10 @@ def _compile(sources, lib, verbose, resources=None):
 
 def build(verbose: bool = False) -> str:
     """Compile every HIP source: ``libcrfinside.so`` (the CRF library, with
-    its kernels' resource report beside it) and ``libcrfceilings.so``
+    its kernels' resource reports beside it) and ``libcrfceilings.so``
     (ceiling microbenchmarks).  Always recompiles."""
-    _compile(SOURCES, LIB, verbose, resources=RESOURCES)
+    _compile(SOURCES + TRAIN_SOURCES, LIB, verbose,
+             resources=((RESOURCES, SOURCES), (TRAIN_RESOURCES, TRAIN_SOURCES)))
     _compile(CEIL_SOURCES, CEIL_LIB, verbose)
     return LIB
 

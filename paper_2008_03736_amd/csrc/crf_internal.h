@@ -354,6 +354,7 @@ __host__ __device__ inline int masked_reach(int n) {
 // and the largest d whose staged rows fit in LDS beside a chunk of W.
 constexpr int kBiaRows = 64, kBiaCols = 64, kBiaChunk = 32;
 constexpr int kBiaMaxD = 508;
+constexpr int kPostRec = kBiaRows + 2;
 static_assert(kBiaRows == kBiaCols, "packed tiles use their fence posts as both rows and columns");
 
 // Threads per workgroup of the label passes, and floats of a row's label
@@ -479,6 +480,16 @@ struct KernelPlan {
     // (b N1 + fence post, or -1)
     const int32_t *bia_tiles;
     int32_t n_bia_tiles;
+    // every fence post of the batch once, in blocks: kPostRec ints a block
+    // (kBiaRows ids b N1 + fence post or -1, then the first and the last block
+    // that hold posts of its sentences), and where each sentence's n x n cells
+    // start in a compact array of the batch's cells
+    const int32_t *posts;
+    int32_t n_posts;
+    const int64_t *cell_off;
+    // set per launch: log Z in float64 as well (NULL: not wanted), for calls
+    // that subtract it from a tree's score
+    double *z64;
     int64_t lab_sp_off, lab_mu_off;
     // set per labelled inside launch: the label scores [B][N1][N1][L], the
     // per-label marginals out (NULL for the forward pass) and L, for the
@@ -627,5 +638,20 @@ int64_t biaffine_lds_bytes(int d);
 hipError_t set_biaffine_attributes();   // once per plan: the LDS of the largest d
 hipError_t launch_biaffine(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
                            int ldw, int L, float *scores, hipStream_t stream);
+// Log-probabilities of given trees and the clipped policy loss (crf_trees.hip):
+// the inside sweep, then a pass over the trees.  z64: [B] of workspace.
+hipError_t launch_tree_logprobs(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
+                                const int32_t *counts, double *z64, float *logp, float *logZ, hipStream_t stream);
+hipError_t launch_tree_logprobs_bwd(const KernelPlan &p, int max_len, const float *scores, const int32_t *trees, int G,
+                                    const int32_t *counts, const float *grad_logp, float *grad, hipStream_t stream);
+hipError_t launch_policy_loss(const KernelPlan &p, int max_len, const float *scores, const int32_t *trees, int G,
+                              const int32_t *counts, const float *adv, const float *old_logp, const float *ref_logp,
+                              float clip_low, float clip_high, float kl_coef, const float *grad_loss, double *z64,
+                              float *loss, float *logp, float *grad, hipStream_t stream);
+// Activation rows in 8 bits (crf_rows.hip)
+hipError_t launch_pack_rows(const KernelPlan &p, const uint16_t *x, int d, uint8_t *codes, uint8_t *scales,
+                            hipStream_t stream);
+hipError_t launch_unpack_rows(const KernelPlan &p, const uint8_t *codes, const uint8_t *scales, int d, uint16_t *x,
+                              hipStream_t stream);
 
 }  // namespace crf

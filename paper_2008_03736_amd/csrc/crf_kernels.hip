@@ -1302,6 +1302,11 @@ __device__ __forceinline__ bool inside_block_impl(const KernelPlan &p, int block
         for (int sb = tid; sb < nb; sb += NT)
             logZ[sid[sb]] = aborted ? __builtin_bit_cast(float, 0x7fc00000) : (float)log_z(sb);
     }
+    if constexpr (SPILL && !GOLD) if (p.z64 != nullptr && tm.rank == 0) {   // (sentences in LDS: crf_tile.hip)
+        const bool aborted = team_aborted(tm);
+        for (int sb = tid; sb < nb; sb += NT)
+            p.z64[sid[sb]] = aborted ? __builtin_bit_cast(double, 0x7ff8000000000000ll) : log_z(sb);
+    }
     if constexpr (!REV) return true;
 
     if constexpr (GOLD) {

@@ -20,13 +20,16 @@
 #include <vector>
 
 #include "../../include/crf_inside.h"
-#include "crf_internal.h"
+#include "crf_plan.h"
 
 namespace {
 
 thread_local char g_last_error[256] = "";
 
-int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+}  // namespace
+
+namespace crf {
+
 int fail(int code, const char *fmt, ...) {
     va_list ap;
     va_start(ap, fmt);
@@ -44,19 +47,22 @@ int hip_fail(hipError_t e, const char *where) {
     return fail(CRF_EHIP, "%s: %s", where, hipGetErrorString(e));
 }
 
-}  // namespace
+int check_device(const crf_plan *plan) {
+    int dev = -1;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+    if (dev != plan->device)
+        return fail(CRF_EINVAL, "plan was created on device %d, current device is %d",
+                    plan->device, dev);
+    return CRF_OK;
+}
 
-struct crf_plan {
-    int device = -1;
-    int32_t B = 0, n1 = 0, L = 1, max_len = 0;
-    uint32_t flags = 0;
-    std::vector<void *> allocations;
-    crf::KernelPlan kp{};
-    int64_t ws_bytes = 0;          // device workspace owned
-    int64_t scratch_bytes = 0;     // of it, what the no-allocation call needs at least
-    int32_t split_ws_count = 0;    // sentences with CKY split tables in the workspace
-    int32_t workspace_users = 0;   // sentences using the workspace in some call
-};
+}  // namespace crf
+
+using crf::check_device;
+using crf::fail;
+using crf::hip_fail;
+using crf::ok;
 
 namespace {
 
@@ -494,7 +500,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     // room that still holds it, found through lists of open tiles by free
     // rows), longer ones cut into blocks of fence posts with a tile per pair
     // of row block <= column block.
-    std::vector<int32_t> bia;
+    std::vector<int32_t> bia, posts;
     {
         std::vector<std::vector<int32_t>> packed;
         std::vector<std::vector<int32_t>> by_free(crf::kBiaRows + 1);
@@ -532,6 +538,34 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
         for (const auto &ids : packed)
             for (int h = 0; h < 2; ++h)
                 for (int r = 0; r < crf::kBiaRows; ++r) bia.push_back(r < (int)ids.size() ? ids[r] : -1);
+        // The batch's fence posts in blocks of kBiaRows: those of a long
+        // sentence one after the other (each with the first and last of them),
+        // then the packed ones.
+        for (int32_t b : order) {
+            const int n = lengths_host[b];
+            if (n + 1 <= crf::kBiaRows) continue;
+            const int first = (int)(posts.size() / crf::kPostRec);
+            const int nblk = (n + 1 + crf::kBiaRows - 1) / crf::kBiaRows;
+            for (int k = 0; k < nblk; ++k) {
+                for (int r = 0; r < crf::kBiaRows; ++r) {
+                    const int i = k * crf::kBiaRows + r;
+                    posts.push_back(i <= n ? b * n1 + i : -1);
+                }
+                posts.push_back(first);
+                posts.push_back(first + nblk - 1);
+            }
+        }
+        for (const auto &ids : packed) {
+            const int at = (int)(posts.size() / crf::kPostRec);
+            for (int r = 0; r < crf::kBiaRows; ++r) posts.push_back(r < (int)ids.size() ? ids[r] : -1);
+            posts.push_back(at);
+            posts.push_back(at);
+        }
+    }
+    std::vector<int64_t> cell_off(batch);
+    for (int32_t b = 0; b < batch; ++b) {
+        cell_off[b] = p->cells;
+        p->cells += (int64_t)lengths_host[b] * lengths_host[b];
     }
 
     std::vector<int32_t> len(lengths_host, lengths_host + batch);
@@ -590,6 +624,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     const std::vector<int32_t> rec_in = records(si, crf::kKindInside), rec_ck = records(sc, crf::kKindCky);
     kp.n_lab_rows = (int32_t)(lab_rows.size() / 4);
     kp.n_bia_tiles = (int32_t)(bia.size() / (crf::kBiaRows + crf::kBiaCols));
+    kp.n_posts = (int32_t)(posts.size() / crf::kPostRec);
     kp.lab_sp_off = lab_sp_off;
     kp.lab_mu_off = lab_mu_off;
     std::vector<int32_t> rec_mix;
@@ -716,6 +751,8 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
         (e = upload(p, rec_mix, &kp.mix)) != hipSuccess ||
         (e = upload(p, lab_rows, &kp.lab_rows)) != hipSuccess ||
         (e = upload(p, bia, &kp.bia_tiles)) != hipSuccess ||
+        (e = upload(p, posts, &kp.posts)) != hipSuccess ||
+        (e = upload(p, cell_off, &kp.cell_off)) != hipSuccess ||
         (e = upload(p, tile_recs, &kp.tile_io.recs)) != hipSuccess ||
         (e = upload(p, tile_ws_recs, &kp.tile_ws.recs)) != hipSuccess) {
         const int code = (e == hipErrorOutOfMemory) ? CRF_ENOMEM : CRF_EHIP;
@@ -811,16 +848,6 @@ int crf_plan_info(const crf_plan *plan, crf_plan_stats *out) {
     out->fused_queue = 0;
     out->mbr_fused = kp.tile_io.n > 0 ? 1 : 0;
     return ok();
-}
-
-static int check_device(const crf_plan *plan) {
-    int dev = -1;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-    if (dev != plan->device)
-        return fail(CRF_EINVAL, "plan was created on device %d, current device is %d",
-                    plan->device, dev);
-    return CRF_OK;
 }
 
 int crf_inside_fwd(const crf_plan *plan, const float *scores, float *logZ, void *stream) {

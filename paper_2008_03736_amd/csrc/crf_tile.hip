@@ -289,6 +289,7 @@ struct Io_ctx {
     uint32_t mag;        // div_magic(S)
     int part, partd, forced, tab;
     char *tb;
+    bool fine;           // shifts in whole steps of kFineShift (see growth_shift)
     __device__ __forceinline__ int rot(int g) const { return GLOB ? 0 : (g >> 1) & 3; }
     __device__ __forceinline__ int diag(int D) const { return 64 * (D * m - ((D * (D - 1)) >> 1)); }
     __device__ __forceinline__ int rs(int D) const { return GLOB ? 16 * (m - D) : 16; }
@@ -306,8 +307,9 @@ struct Io_ctx {
     }
 };
 template <bool GLOB>
-__device__ __forceinline__ Io_ctx<GLOB> io_ctx(const int32_t *rec, char *lds) {
+__device__ __forceinline__ Io_ctx<GLOB> io_ctx(const int32_t *rec, char *lds, bool fine) {
     Io_ctx<GLOB> c;
+    c.fine = fine;
     c.m = rec[kTrM];
     c.S = GLOB ? 1 : rec[kTrCount];
     c.rpb = rec[kTrPitch] * 64;
@@ -762,6 +764,12 @@ __device__ __forceinline__ Growth tile_growth(const Tile &x, int D) {
 // call for: linear domain, minus the midpoint of the mean and the largest,
 // which keeps the largest values further from float32's limit; log domain,
 // minus the mean.  Left in table `which`; add: on top of what it holds.
+// cx.fine: a multiple of kFineShift, so that shifts add up, and their products
+// with numbers of nodes come out, without rounding.  log Z takes the shift n - 2
+// times off again, so that a shift rounded to float32's own step is 1e-7 n off,
+// more than all the rest (300 words at deviation 2: 3.2e-5 against 2e-6).  The
+// calls that subtract log Z from a tree's score ask for it.
+constexpr float kFineShift = 1.0f / 64.0f;
 template <bool LIN, typename CX>
 __device__ __forceinline__ void growth_shift(const CX &cx, int blocks, int which) {
     const int gl = this_thread() & 15, S = cx.S;
@@ -784,8 +792,11 @@ __device__ __forceinline__ void growth_shift(const CX &cx, int blocks, int which
         if constexpr (LIN) mx = row_max(mx);
         sum = row_sum(sum);
         c = row_sum(c);
-        if (gl == 0)
-            tab<float>(cx, which, sb) = c > 0.f ? (LIN ? -0.5f * (mx + sum / c) : -sum / c) : 0.f;
+        if (gl == 0) {
+            float shift = c > 0.f ? (LIN ? -0.5f * (mx + sum / c) : -sum / c) : 0.f;
+            if (cx.fine) shift = __builtin_rintf(shift * (1.0f / kFineShift)) * kFineShift;
+            tab<float>(cx, which, sb) = shift;
+        }
     }
 }
 
@@ -969,7 +980,7 @@ __device__ __forceinline__ bool tile_inside_impl(const KernelPlan &p, const int3
     typedef Dom<LIN> Dm;
     __shared__ int flags[kFlags];
     const int tid = this_thread(), NT = (int)blockDim.x, N1 = p.n1;
-    const Io_ctx<GLOB> cx = io_ctx<GLOB>(rec, lds);
+    const Io_ctx<GLOB> cx = io_ctx<GLOB>(rec, lds, !GOLD && p.z64 != nullptr);
     const int m = cx.m, S = cx.S;
     for (int sb = tid; sb < S; sb += NT) {
         const int id = rec[kTrHeader + 2 * sb];
@@ -1135,6 +1146,8 @@ __device__ __forceinline__ bool tile_inside_impl(const KernelPlan &p, const int3
     };
     if (logZ != nullptr)
         for (int sb = tid; sb < S; sb += NT) logZ[tab<int>(cx, kTabId, sb)] = (float)log_z(sb);
+    if constexpr (!GOLD) if (p.z64 != nullptr)
+        for (int sb = tid; sb < S; sb += NT) p.z64[tab<int>(cx, kTabId, sb)] = log_z(sb);
     if constexpr (!REV) return true;
 
     if constexpr (GOLD) {
