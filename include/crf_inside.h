@@ -414,6 +414,40 @@ int crf_pack_rows(const crf_plan *plan, const uint16_t *x, int32_t d, uint8_t *c
 int crf_unpack_rows(const crf_plan *plan, const uint8_t *codes, const uint8_t *scales, int32_t d, uint16_t *x,
                     void *stream);
 
+/* crf_biaffine_bwd_workspace -- bytes of workspace of crf_biaffine_bwd and
+ * crf_biaffine_bwd_packed for representations of d dimensions and num_labels
+ * labels. */
+int crf_biaffine_bwd_workspace(const crf_plan *plan, int32_t d, int32_t num_labels, int64_t *bytes);
+
+/*
+ * crf_biaffine_bwd -- the backward pass of crf_biaffine_scores (Sec. 2.2,
+ * Eq. biaffine).  With G_l(i,j) = dL/ds(i,j,l) on 0 <= i < j <= n_b,
+ *   dL/dr^l_i = sum_l sum_j G_l(i,j) W_l r^r_j  (W_l's first d rows),
+ *   dL/dr^r_j = sum_l sum_i G_l(i,j) W_l^T [r^l_i ; 1],
+ *   dL/dW_l   = sum_b sum_{i<j} G_l(i,j) [r^l_i ; 1] r^r_j^T.
+ * Products on the matrix cores with fp32 sums; G_l enters as two bf16 parts.
+ *   rl, rr, w, d, ldw, num_labels: as crf_biaffine_scores.
+ *   grad_scores device float32, the layout of the scores; only cells
+ *               0 <= i < j <= n_b are read.
+ *   grad_rl, grad_rr  device bf16 bit patterns [B][N1][d], 8-byte aligned, or
+ *               NULL: rows 0..n_b are written (the products' inner d x d side
+ *               is rounded to bf16 once).
+ *   grad_w      device float32 [num_labels][d][ldw], 16-byte aligned, or NULL:
+ *               the layout of w; entries a <= d are written.
+ * Sums run in a fixed order: equal calls give equal bits.
+ */
+int crf_biaffine_bwd(const crf_plan *plan, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int32_t d,
+                     int32_t ldw, int32_t num_labels, const float *grad_scores, uint16_t *grad_rl, uint16_t *grad_rr,
+                     float *grad_w, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* crf_biaffine_bwd_packed -- the same from representations in the 8-bit form
+ * of crf_pack_rows (the gradients are those at the values that the codes stand
+ * for). */
+int crf_biaffine_bwd_packed(const crf_plan *plan, const uint8_t *rl_codes, const uint8_t *rl_scales,
+                            const uint8_t *rr_codes, const uint8_t *rr_scales, const uint16_t *w, int32_t d, int32_t ldw,
+                            int32_t num_labels, const float *grad_scores, uint16_t *grad_rl, uint16_t *grad_rr,
+                            float *grad_w, void *workspace, int64_t workspace_bytes, void *stream);
+
 /* Static description of a status code. */
 const char *crf_status_string(int status);
 

@@ -51,6 +51,9 @@ SIGNATURES = {
                                        _P]),
     "crf_pack_rows": (ctypes.c_int, [_P, _P, _I32, _P, _P, _P]),
     "crf_unpack_rows": (ctypes.c_int, [_P, _P, _P, _I32, _P, _P]),
+    "crf_biaffine_bwd_workspace": (ctypes.c_int, [_P, _I32, _I32, ctypes.POINTER(_I64)]),
+    "crf_biaffine_bwd": (ctypes.c_int, [_P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P, _P, _I64, _P]),
+    "crf_biaffine_bwd_packed": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P, _P, _I64, _P]),
     "crf_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "crf_last_error": (ctypes.c_char_p, []),
 }
@@ -205,6 +208,25 @@ def crf_pack_rows(plan, x, d, codes, scales, stream):
 
 def crf_unpack_rows(plan, codes, scales, d, x, stream):
     _check(load().crf_unpack_rows(plan, codes, scales, d, x, stream), "crf_unpack_rows")
+
+
+def crf_biaffine_bwd_workspace(plan, d, num_labels):
+    n = _I64()
+    _check(load().crf_biaffine_bwd_workspace(plan, d, num_labels, ctypes.byref(n)), "crf_biaffine_bwd_workspace")
+    return n.value
+
+
+def crf_biaffine_bwd(plan, rl, rr, w, d, ldw, num_labels, grad_scores, grad_rl, grad_rr, grad_w, workspace,
+                     workspace_bytes, stream):
+    _check(load().crf_biaffine_bwd(plan, rl, rr, w, d, ldw, num_labels, grad_scores, grad_rl, grad_rr, grad_w, workspace,
+                                   workspace_bytes, stream), "crf_biaffine_bwd")
+
+
+def crf_biaffine_bwd_packed(plan, rl_codes, rl_scales, rr_codes, rr_scales, w, d, ldw, num_labels, grad_scores, grad_rl,
+                            grad_rr, grad_w, workspace, workspace_bytes, stream):
+    _check(load().crf_biaffine_bwd_packed(plan, rl_codes, rl_scales, rr_codes, rr_scales, w, d, ldw, num_labels,
+                                          grad_scores, grad_rl, grad_rr, grad_w, workspace, workspace_bytes, stream),
+           "crf_biaffine_bwd_packed")
 
 
 def crf_status_string(status):
@@ -581,6 +603,38 @@ class Plan:
                         _stream_ptr(t, self.device))
         return out
 
+    def biaffine_bwd(self, rl, rr, w, grad_scores, grad_rl=None, grad_rr=None, grad_w=None, need=(True, True, True)):
+        """Backward pass of biaffine_scores (Sec. 2.2, Eq. biaffine) from the
+        gradient of its scores: (grad_rl bf16 [B, N1, d], grad_rr, grad_w
+        float32 shaped like w).  rl and rr: bf16 (or its bit patterns)
+        [B, N1, d], or both what pack_rows gave for them.  need: which of the
+        three to compute (None in the place of the others); rows past a
+        sentence and entries of grad_w past the bias are left as they were
+        (zero in fresh buffers)."""
+        t = self._torch
+        if w.dim() != 3:
+            raise ValueError("w must be [L, d, ldw]")
+        L, d, ldw = (int(x) for x in w.shape)
+        wp = self._bf16(w, "w", w.shape)
+        rows = (self.B, self.n1, d)
+        packed = isinstance(rl, (tuple, list))
+        if packed != isinstance(rr, (tuple, list)):
+            raise ValueError("rl and rr must both be rows or both be packed")
+        ins = (*self._packed(*rl, d), *self._packed(*rr, d)) if packed else (self._bf16(rl, "rl", rows),
+                                                                            self._bf16(rr, "rr", rows))
+        shape = (self.B, self.n1, self.n1) if L == 1 else (self.B, self.n1, self.n1, L)
+        gp = self._tensor(grad_scores, "grad_scores", shape, (t.float32,))
+        out = [self._out(x, s, dt, zero=True) if want else None
+               for x, s, dt, want in ((grad_rl, rows, t.bfloat16, need[0]), (grad_rr, rows, t.bfloat16, need[1]),
+                                      (grad_w, tuple(w.shape), t.float32, need[2]))]
+        types = ((t.bfloat16, t.int16, t.uint16),) * 2 + ((t.float32,),)
+        ptrs = [self._tensor(x, name, s, dt, optional=True)
+                for x, name, s, dt in zip(out, ("grad_rl", "grad_rr", "grad_w"), (rows, rows, w.shape), types)]
+        ws = self._workspace(crf_biaffine_bwd_workspace(self._handle, d, L))
+        call = crf_biaffine_bwd_packed if packed else crf_biaffine_bwd
+        call(self._handle, *ins, wp, d, ldw, L, gp, *ptrs, ws.data_ptr(), ws.numel(), _stream_ptr(t, self.device))
+        return tuple(out)
+
     def cky_decode(self, scores, spans=None, best=None):
         """(spans int32 [B, 2(N1-1)-1, 2] preorder padded with -1, best float32 [B])."""
         t = self._torch
@@ -656,3 +710,39 @@ def policy_loss(scores, trees, advantages, old_logp, plan, **options):
             return grad * g[:, None, None]
 
     return _Policy.apply(scores)
+
+
+def biaffine(rl, rr, w, plan, held="bf16"):
+    """Differentiable span (or label) scores from boundary representations
+    (Sec. 2.2, Eq. biaffine): rl, rr bfloat16 [B, N1, d], w bfloat16
+    [L, d, ldw]; cells that are no spans are 0.  held="8bit": the backward pass
+    keeps the representations in 8 bits (Plan.pack_rows) and gives the
+    gradients at the values those stand for."""
+    import torch
+
+    if held not in ("bf16", "8bit"):
+        raise ValueError('held must be "bf16" or "8bit"')
+
+    class _Biaffine(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, rl, rr, w):
+            L = w.shape[0]
+            shape = (plan.B, plan.n1, plan.n1) if L == 1 else (plan.B, plan.n1, plan.n1, L)
+            scores = torch.zeros(shape, dtype=torch.float32, device=rl.device)
+            plan.biaffine_scores(rl.view(torch.int16), rr.view(torch.int16), w.view(torch.int16), scores=scores)
+            kept = (*plan.pack_rows(rl), *plan.pack_rows(rr)) if held == "8bit" else (rl, rr)
+            ctx.save_for_backward(w, *kept)
+            return scores
+
+        @staticmethod
+        def backward(ctx, g):
+            w, *kept = ctx.saved_tensors
+            rl, rr = (kept[:2], kept[2:]) if held == "8bit" else kept
+            g = g.float().contiguous()   # held by this frame until the call has been enqueued
+            need = ctx.needs_input_grad
+            if not any(need):
+                return None, None, None
+            grads = plan.biaffine_bwd(rl, rr, w, g, need=need)
+            return tuple(x if x is None else x.to(torch.bfloat16) for x in grads)
+
+    return _Biaffine.apply(rl, rr, w)

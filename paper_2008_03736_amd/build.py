@@ -12,6 +12,7 @@ SOURCES = [os.path.join(CSRC, "crf_kernels.hip"), os.path.join(CSRC, "crf_biaffi
            os.path.join(CSRC, "crf_tile.hip"), os.path.join(CSRC, "crf_plan.cpp")]
 # the fine-tuning operators, linked into the same library
 TRAIN_SOURCES = [os.path.join(CSRC, "crf_trees.hip"), os.path.join(CSRC, "crf_rows.hip"),
+                 os.path.join(CSRC, "crf_biaffine_bwd.hip"),
                  os.path.join(CSRC, "crf_train.cpp")]
 LIB = os.path.join(PKG, "libcrfinside.so")
 # microbenchmarks of the ceilings behind the roofline (bench.py --ceilings)

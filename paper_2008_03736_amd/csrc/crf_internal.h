@@ -354,7 +354,7 @@ __host__ __device__ inline int masked_reach(int n) {
 // and the largest d whose staged rows fit in LDS beside a chunk of W.
 constexpr int kBiaRows = 64, kBiaCols = 64, kBiaChunk = 32;
 constexpr int kBiaMaxD = 508;
-constexpr int kPostRec = kBiaRows + 2;
+constexpr int kPostRec = 2 * kBiaRows + 2;
 static_assert(kBiaRows == kBiaCols, "packed tiles use their fence posts as both rows and columns");
 
 // Threads per workgroup of the label passes, and floats of a row's label
@@ -481,12 +481,13 @@ struct KernelPlan {
     const int32_t *bia_tiles;
     int32_t n_bia_tiles;
     // every fence post of the batch once, in blocks: kPostRec ints a block
-    // (kBiaRows ids b N1 + fence post or -1, then the first and the last block
-    // that hold posts of its sentences), and where each sentence's n x n cells
-    // start in a compact array of the batch's cells
+    // (kBiaRows ids b N1 + fence post or -1, the ids b N1 of their sentences'
+    // first posts, then the first and the last block that hold posts of its
+    // sentences), and for each of them where its row's cells are in a compact
+    // array of all sentences' n x n cells: cell (i, j) at post_cells + j
     const int32_t *posts;
     int32_t n_posts;
-    const int64_t *cell_off;
+    const int64_t *post_cells;
     // set per launch: log Z in float64 as well (NULL: not wanted), for calls
     // that subtract it from a tree's score
     double *z64;
@@ -653,5 +654,14 @@ hipError_t launch_pack_rows(const KernelPlan &p, const uint16_t *x, int d, uint8
                             hipStream_t stream);
 hipError_t launch_unpack_rows(const KernelPlan &p, const uint8_t *codes, const uint8_t *scales, int d, uint16_t *x,
                               hipStream_t stream);
+// The biaffine scorer's backward pass (crf_biaffine_bwd.hip): workspace bytes
+// (cells: the plan's), the LDS of its kernels (once per device) and the
+// launches.  rl and rr are bf16 rows, or codes where their scales are given;
+// outputs may be NULL.
+int64_t biaffine_bwd_bytes(const KernelPlan &p, int64_t cells, int d, int L);
+hipError_t set_biaffine_bwd_attributes();
+hipError_t launch_biaffine_bwd(const KernelPlan &p, int64_t cells, const void *rl, const uint8_t *rl_scales, const void *rr,
+                               const uint8_t *rr_scales, const uint16_t *w, int d, int ldw, int L, const float *grad,
+                               uint16_t *grad_rl, uint16_t *grad_rr, float *grad_w, char *ws, hipStream_t stream);
 
 }  // namespace crf

@@ -501,6 +501,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     // rows), longer ones cut into blocks of fence posts with a tile per pair
     // of row block <= column block.
     std::vector<int32_t> bia, posts;
+    std::vector<int64_t> post_cells;
     {
         std::vector<std::vector<int32_t>> packed;
         std::vector<std::vector<int32_t>> by_free(crf::kBiaRows + 1);
@@ -541,31 +542,42 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
         // The batch's fence posts in blocks of kBiaRows: those of a long
         // sentence one after the other (each with the first and last of them),
         // then the packed ones.
+        std::vector<int64_t> cell_off(batch);
+        for (int32_t b = 0; b < batch; ++b) {
+            cell_off[b] = p->cells;
+            p->cells += (int64_t)lengths_host[b] * lengths_host[b];
+        }
+        auto put_block = [&](const int32_t *ids, int count, int first, int last) {
+            const size_t at = posts.size();
+            posts.resize(at + crf::kPostRec, -1);
+            for (int r = 0; r < crf::kBiaRows; ++r) {
+                int64_t cell = 0;
+                if (r < count) {
+                    const int32_t b = ids[r] / n1, i = ids[r] - b * n1;
+                    posts[at + r] = ids[r];
+                    posts[at + crf::kBiaRows + r] = b * n1;
+                    cell = cell_off[b] + (int64_t)i * lengths_host[b] - 1;
+                }
+                post_cells.push_back(cell);
+            }
+            posts[at + 2 * crf::kBiaRows] = first;
+            posts[at + 2 * crf::kBiaRows + 1] = last;
+        };
         for (int32_t b : order) {
             const int n = lengths_host[b];
             if (n + 1 <= crf::kBiaRows) continue;
             const int first = (int)(posts.size() / crf::kPostRec);
             const int nblk = (n + 1 + crf::kBiaRows - 1) / crf::kBiaRows;
-            for (int k = 0; k < nblk; ++k) {
-                for (int r = 0; r < crf::kBiaRows; ++r) {
-                    const int i = k * crf::kBiaRows + r;
-                    posts.push_back(i <= n ? b * n1 + i : -1);
-                }
-                posts.push_back(first);
-                posts.push_back(first + nblk - 1);
-            }
+            std::vector<int32_t> ids(n + 1);
+            for (int i = 0; i <= n; ++i) ids[i] = b * n1 + i;
+            for (int k = 0; k < nblk; ++k)
+                put_block(ids.data() + k * crf::kBiaRows, std::min(crf::kBiaRows, n + 1 - k * crf::kBiaRows), first,
+                          first + nblk - 1);
         }
         for (const auto &ids : packed) {
             const int at = (int)(posts.size() / crf::kPostRec);
-            for (int r = 0; r < crf::kBiaRows; ++r) posts.push_back(r < (int)ids.size() ? ids[r] : -1);
-            posts.push_back(at);
-            posts.push_back(at);
+            put_block(ids.data(), (int)ids.size(), at, at);
         }
-    }
-    std::vector<int64_t> cell_off(batch);
-    for (int32_t b = 0; b < batch; ++b) {
-        cell_off[b] = p->cells;
-        p->cells += (int64_t)lengths_host[b] * lengths_host[b];
     }
 
     std::vector<int32_t> len(lengths_host, lengths_host + batch);
@@ -752,7 +764,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
         (e = upload(p, lab_rows, &kp.lab_rows)) != hipSuccess ||
         (e = upload(p, bia, &kp.bia_tiles)) != hipSuccess ||
         (e = upload(p, posts, &kp.posts)) != hipSuccess ||
-        (e = upload(p, cell_off, &kp.cell_off)) != hipSuccess ||
+        (e = upload(p, post_cells, &kp.post_cells)) != hipSuccess ||
         (e = upload(p, tile_recs, &kp.tile_io.recs)) != hipSuccess ||
         (e = upload(p, tile_ws_recs, &kp.tile_ws.recs)) != hipSuccess) {
         const int code = (e == hipErrorOutOfMemory) ? CRF_ENOMEM : CRF_EHIP;

@@ -17,7 +17,7 @@ struct crf_plan {
     int64_t scratch_bytes = 0;     // of it, what the no-allocation call needs at least
     int32_t split_ws_count = 0;    // sentences with CKY split tables in the workspace
     int32_t workspace_users = 0;   // sentences using the workspace in some call
-    int64_t cells = 0;             // squares of the lengths, summed (see KernelPlan::cell_off)
+    int64_t cells = 0;             // squares of the lengths, summed (see KernelPlan::post_cells)
 };
 
 namespace crf {

@@ -2,6 +2,7 @@
 // checks and launches, as crf_plan.cpp has them for the others.
 #include <hip/hip_runtime_api.h>
 
+#include <atomic>
 #include <cstring>
 
 #include "../../include/crf_inside.h"
@@ -47,6 +48,44 @@ int check_row(int32_t d) {
     if (d < 4 || d > CRF_MAX_ROW || d % 4 != 0)
         return fail(CRF_EINVAL, "d %d is not a multiple of 4 in [4, %d]", d, CRF_MAX_ROW);
     return CRF_OK;
+}
+
+int check_scorer(int32_t d, int32_t ldw, int32_t num_labels) {
+    if (d < 4 || d > crf::kBiaMaxD || d % 4 != 0)
+        return fail(CRF_EINVAL, "d %d is not a multiple of 4 in [4, %d]", d, crf::kBiaMaxD);
+    if (ldw < d + 1 || ldw % 4 != 0) return fail(CRF_EINVAL, "ldw %d < d+1 or not a multiple of 4", ldw);
+    if (num_labels < 1 || num_labels > CRF_MAX_LABELS)
+        return fail(CRF_EINVAL, "num_labels %d outside [1, %d]", num_labels, CRF_MAX_LABELS);
+    return CRF_OK;
+}
+
+// crf_biaffine_bwd and crf_biaffine_bwd_packed once rl and rr are checked.
+int scorer_backward(const crf_plan *plan, const void *rl, const uint8_t *rl_scales, const void *rr,
+                    const uint8_t *rr_scales, const uint16_t *w, int32_t d, int32_t ldw, int32_t num_labels,
+                    const float *grad_scores, uint16_t *grad_rl, uint16_t *grad_rr, float *grad_w, void *workspace,
+                    int64_t workspace_bytes, void *stream, const char *what) {
+    int rc = check_scorer(d, ldw, num_labels);
+    if (rc != CRF_OK) return rc;
+    if (misaligned(grad_rl, 8) || misaligned(grad_rr, 8)) return fail(CRF_EINVAL, "grad_rl/grad_rr must be 8-byte aligned");
+    if (misaligned(grad_w, 16)) return fail(CRF_EINVAL, "grad_w must be 16-byte aligned");
+    const void *ins[] = {rl, rr, rl_scales, rr_scales, w, grad_scores};
+    const void *outs[] = {grad_rl, grad_rr, grad_w};
+    for (const void *o : outs)
+        for (const void *i : ins)
+            if (o != nullptr && o == i) return fail(CRF_EINVAL, "a gradient must not alias an input");
+    if (grad_rl != nullptr && grad_rl == grad_rr) return fail(CRF_EINVAL, "grad_rl and grad_rr must not alias");
+    if ((rc = check_workspace(workspace, workspace_bytes, crf::biaffine_bwd_bytes(plan->kp, plan->cells, d, num_labels))) !=
+            CRF_OK ||
+        (rc = check_device(plan)) != CRF_OK)
+        return rc;
+    // best effort, as for the other kernels: a real shortfall surfaces as a launch error
+    static std::atomic<uint64_t> seen{0};
+    const uint64_t bit = (uint64_t)1 << (plan->device & 63);
+    if (!(seen.fetch_or(bit) & bit) && crf::set_biaffine_bwd_attributes() != hipSuccess) (void)hipGetLastError();
+    const hipError_t e = crf::launch_biaffine_bwd(plan->kp, plan->cells, rl, rl_scales, rr, rr_scales, w, d, ldw, num_labels,
+                                                  grad_scores, grad_rl, grad_rr, grad_w, static_cast<char *>(workspace),
+                                                  static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, what);
 }
 
 }  // namespace
@@ -137,6 +176,41 @@ int crf_unpack_rows(const crf_plan *plan, const uint8_t *codes, const uint8_t *s
     if ((rc = check_device(plan)) != CRF_OK) return rc;
     const hipError_t e = crf::launch_unpack_rows(plan->kp, codes, scales, d, x, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_unpack_rows launch");
+}
+
+int crf_biaffine_bwd_workspace(const crf_plan *plan, int32_t d, int32_t num_labels, int64_t *bytes) {
+    if (plan == nullptr || bytes == nullptr) return fail(CRF_EINVAL, "NULL argument");
+    const int rc = check_scorer(d, (d + 4) / 4 * 4, num_labels);
+    if (rc != CRF_OK) return rc;
+    *bytes = crf::biaffine_bwd_bytes(plan->kp, plan->cells, d, num_labels);
+    return ok();
+}
+
+int crf_biaffine_bwd(const crf_plan *plan, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int32_t d,
+                     int32_t ldw, int32_t num_labels, const float *grad_scores, uint16_t *grad_rl, uint16_t *grad_rr,
+                     float *grad_w, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (plan == nullptr) return fail(CRF_EINVAL, "plan is NULL");
+    if (rl == nullptr || rr == nullptr || w == nullptr || grad_scores == nullptr)
+        return fail(CRF_EINVAL, "rl/rr/w/grad_scores is NULL");
+    if (misaligned(rl, 8) || misaligned(rr, 8) || misaligned(w, 8))
+        return fail(CRF_EINVAL, "rl/rr/w must be 8-byte aligned");
+    return scorer_backward(plan, rl, nullptr, rr, nullptr, w, d, ldw, num_labels, grad_scores, grad_rl, grad_rr, grad_w,
+                           workspace, workspace_bytes, stream, "crf_biaffine_bwd launch");
+}
+
+int crf_biaffine_bwd_packed(const crf_plan *plan, const uint8_t *rl_codes, const uint8_t *rl_scales,
+                            const uint8_t *rr_codes, const uint8_t *rr_scales, const uint16_t *w, int32_t d, int32_t ldw,
+                            int32_t num_labels, const float *grad_scores, uint16_t *grad_rl, uint16_t *grad_rr,
+                            float *grad_w, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (plan == nullptr) return fail(CRF_EINVAL, "plan is NULL");
+    if (rl_codes == nullptr || rl_scales == nullptr || rr_codes == nullptr || rr_scales == nullptr || w == nullptr ||
+        grad_scores == nullptr)
+        return fail(CRF_EINVAL, "rl_codes/rl_scales/rr_codes/rr_scales/w/grad_scores is NULL");
+    if (misaligned(rl_codes, 16) || misaligned(rr_codes, 16))
+        return fail(CRF_EINVAL, "rl_codes/rr_codes must be 16-byte aligned");
+    if (misaligned(w, 8)) return fail(CRF_EINVAL, "w must be 8-byte aligned");
+    return scorer_backward(plan, rl_codes, rl_scales, rr_codes, rr_scales, w, d, ldw, num_labels, grad_scores, grad_rl,
+                           grad_rr, grad_w, workspace, workspace_bytes, stream, "crf_biaffine_bwd_packed launch");
 }
 
 }  // extern "C"

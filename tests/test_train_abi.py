@@ -28,6 +28,9 @@ def test_null_plan(lib):
                                None) == B.CRF_EINVAL
     assert lib.crf_pack_rows(None, P, 100, P, P, None) == B.CRF_EINVAL
     assert lib.crf_unpack_rows(None, P, P, 100, P, None) == B.CRF_EINVAL
+    assert lib.crf_biaffine_bwd_workspace(None, 100, 1, ctypes.byref(n)) == B.CRF_EINVAL
+    assert lib.crf_biaffine_bwd(None, P, P, P, 100, 104, 1, P, Q, Q, None, P, 1 << 20, None) == B.CRF_EINVAL
+    assert lib.crf_biaffine_bwd_packed(None, P, P, P, P, P, 100, 104, 1, P, Q, Q, None, P, 1 << 20, None) == B.CRF_EINVAL
     assert "plan" in B.crf_last_error()
 
 
