@@ -372,6 +372,9 @@ constexpr int kLabelRowChunk = 1024;
 // longer ones to the workspace kernels.
 constexpr int kMaxLenInLds = 141;
 
+// Cells of a stripe of the tree calls' gradient pass.
+constexpr int kTreeCells = 2048;
+
 // A bundle: `count` sentences of identical length `n`, processed together by
 // one workgroup; their ids are order[first .. first+count).
 struct Bundle {
@@ -488,6 +491,11 @@ struct KernelPlan {
     const int32_t *posts;
     int32_t n_posts;
     const int64_t *post_cells;
+    // the tree calls' pass over the trees, longest sentences first: (sentence,
+    // n, first row, rows) of a stripe of rows of at most kTreeCells cells (a
+    // row at least), and the most cells of one
+    const int32_t *tree_recs;
+    int32_t n_tree_recs, tree_cells;
     // set per launch: log Z in float64 as well (NULL: not wanted), for calls
     // that subtract it from a tree's score
     double *z64;
@@ -643,9 +651,9 @@ hipError_t launch_biaffine(const KernelPlan &p, const uint16_t *rl, const uint16
 // the inside sweep, then a pass over the trees.  z64: [B] of workspace.
 hipError_t launch_tree_logprobs(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
                                 const int32_t *counts, double *z64, float *logp, float *logZ, hipStream_t stream);
-hipError_t launch_tree_logprobs_bwd(const KernelPlan &p, int max_len, const float *scores, const int32_t *trees, int G,
+hipError_t launch_tree_logprobs_bwd(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
                                     const int32_t *counts, const float *grad_logp, float *grad, hipStream_t stream);
-hipError_t launch_policy_loss(const KernelPlan &p, int max_len, const float *scores, const int32_t *trees, int G,
+hipError_t launch_policy_loss(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
                               const int32_t *counts, const float *adv, const float *old_logp, const float *ref_logp,
                               float clip_low, float clip_high, float kl_coef, const float *grad_loss, double *z64,
                               float *loss, float *logp, float *grad, hipStream_t stream);

@@ -582,6 +582,16 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
 
     std::vector<int32_t> len(lengths_host, lengths_host + batch);
     crf::KernelPlan &kp = p->kp;
+    // Stripes of rows for the tree calls' pass.
+    std::vector<int32_t> tree_recs;
+    kp.tree_cells = 0;
+    for (int32_t b : order) {
+        const int n = lengths_host[b], rows = std::max(1, std::min(n, crf::kTreeCells / n));
+        kp.tree_cells = std::max(kp.tree_cells, rows * n);
+        for (int i = 0; i < n; i += rows)
+            for (int32_t v : {b, (int32_t)n, (int32_t)i, (int32_t)std::min(rows, n - i)}) tree_recs.push_back(v);
+    }
+    kp.n_tree_recs = (int32_t)(tree_recs.size() / 4);
     kp.B = batch;
     kp.n1 = n1;
     kp.L = num_labels;
@@ -764,6 +774,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
         (e = upload(p, lab_rows, &kp.lab_rows)) != hipSuccess ||
         (e = upload(p, bia, &kp.bia_tiles)) != hipSuccess ||
         (e = upload(p, posts, &kp.posts)) != hipSuccess ||
+        (e = upload(p, tree_recs, &kp.tree_recs)) != hipSuccess ||
         (e = upload(p, post_cells, &kp.post_cells)) != hipSuccess ||
         (e = upload(p, tile_recs, &kp.tile_io.recs)) != hipSuccess ||
         (e = upload(p, tile_ws_recs, &kp.tile_ws.recs)) != hipSuccess) {

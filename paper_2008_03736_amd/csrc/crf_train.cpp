@@ -122,7 +122,7 @@ int crf_tree_logprobs_bwd(const crf_plan *plan, const float *scores, const int32
     if (scores == grad_scores) return fail(CRF_EINVAL, "grad_scores must not alias scores");
     int rc = check_trees(plan, trees, num_trees);
     if (rc != CRF_OK || (rc = check_device(plan)) != CRF_OK) return rc;
-    const hipError_t e = crf::launch_tree_logprobs_bwd(plan->kp, plan->max_len, scores, trees, num_trees, counts,
+    const hipError_t e = crf::launch_tree_logprobs_bwd(plan->kp, scores, trees, num_trees, counts,
                                                        grad_logp, grad_scores, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_tree_logprobs_bwd launch");
 }
@@ -146,7 +146,7 @@ int crf_policy_loss(const crf_plan *plan, const float *scores, const int32_t *tr
     if (rc != CRF_OK || (rc = check_workspace(workspace, workspace_bytes, tree_bytes(plan))) != CRF_OK ||
         (rc = check_device(plan)) != CRF_OK)
         return rc;
-    const hipError_t e = crf::launch_policy_loss(plan->kp, plan->max_len, scores, trees, num_trees, counts, advantages,
+    const hipError_t e = crf::launch_policy_loss(plan->kp, scores, trees, num_trees, counts, advantages,
                                                  old_logp, ref_logp, clip_low, clip_high, kl_coef, grad_loss,
                                                  static_cast<double *>(workspace), loss, logp, grad_scores,
                                                  static_cast<hipStream_t>(stream));

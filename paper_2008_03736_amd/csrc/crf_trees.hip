@@ -15,11 +15,17 @@
 //
 // Two launches: the inside sweep (with the marginals for the loss, which it
 // leaves in the gradient's buffer), then the kernel below, a workgroup per
-// sentence, or per stripe of a long sentence's rows.
+// sentence, or per stripe of at most kTreeCells cells of a long sentence's rows
+// (KernelPlan::tree_recs; each sums the trees anew, which for its few
+// workgroups is cheaper than another launch).
+//
+// The second pass is bound by its chain of memory round trips (rows of the
+// trees, their scores, the cells), so what does not depend on them is loaded
+// first, and stripes are kept small (8 KB of masks) so that eight workgroups
+// share a CU: 4 trees of 5,000 sentences 52.6 us with stripes of 8,192 cells
+// and nothing loaded ahead.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-
-#include <algorithm>
 
 #include "crf_internal.h"
 
@@ -27,17 +33,7 @@ namespace crf {
 namespace {
 
 constexpr int kTreeThreads = 256;
-constexpr int kTreeWords = 8192;   // mask words a workgroup holds (32 KB: five workgroups a CU)
-constexpr int kAhead = 4;          // rows a lane has in flight
-
-// Rows of a sentence of n words in a stripe whose masks of W words a cell fit
-// in kTreeWords (a row holds n cells: columns 1..n), and its stripes.
-__host__ __device__ inline int stripe_rows(int n, int W) { return n * W <= kTreeWords ? kTreeWords / (n * W) : 1; }
-__host__ __device__ inline int stripes(int n, int W) {
-    const int r = stripe_rows(n, W);
-    return (n + r - 1) / r;
-}
-static_assert(CRF_MAX_LEN * 2 <= kTreeWords, "a row of the longest sentence fits, 64 trees");
+constexpr int kAhead = 4;   // rows of a tree, and cells of the gradient, that a lane has in flight
 
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
@@ -78,85 +74,135 @@ constexpr double kMaxLogRatio = 80.0;
 // then summed in the order of the trees.  A span of every tree takes the sum
 // of all coefficients, so that the gradient of a span that every tree must
 // have (p = 1) is exactly zero.
+struct TreeArgs {
+    const int32_t *recs;   // KernelPlan::tree_recs
+    int N1, G, W;
+    const float *scores;
+    const int32_t *trees, *counts;
+    const double *z64;
+    float *logp, *logZ;
+    PolicyArgs p;
+};
+
+// A workgroup a record.  (A wavefront for each sentence of up to 32 words, four
+// a workgroup, was slower for small batches: 8 trees of 200 sentences 19.7 us
+// against 11.4, 4 of 5,000 26.1 against 27.9: the steps that one wavefront takes
+// alone add up.)
 template <TreeMode MODE>
-__global__ __launch_bounds__(kTreeThreads) void tree_kernel(const int32_t *__restrict__ len, int N1, int G, int W,
-                                                            const float *__restrict__ scores,
-                                                            const int32_t *__restrict__ trees,
-                                                            const int32_t *__restrict__ counts,
-                                                            const double *__restrict__ z64, float *__restrict__ logp,
-                                                            float *__restrict__ logZ, PolicyArgs a) {
+__global__ __launch_bounds__(kTreeThreads) void tree_kernel(TreeArgs ta) {
     extern __shared__ __align__(16) uint32_t mask[];
     __shared__ double sums[CRF_MAX_TREES];
     __shared__ float coef[CRF_MAX_TREES + 1];
     constexpr bool GRAD = MODE != kTreeLogp;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int b = blockIdx.x, n = len[b];
-    int i0 = 0, rows = n;
-    if constexpr (GRAD) {
-        const int per = stripe_rows(n, W);
-        i0 = (int)blockIdx.y * per;
-        if (i0 >= n) return;
-        rows = min(per, n - i0);
-        for (int t = tid; t < rows * n * W; t += kTreeThreads) mask[t] = 0u;
-        __syncthreads();
-    }
-    const int cnt = counts ? min(max(counts[b], 0), G) : G;
+    constexpr int NW = kTreeThreads / 64, NT = kTreeThreads;
+    const PolicyArgs &a = ta.p;
+    const int N1 = ta.N1, G = ta.G, W = ta.W;
+    const float *scores = ta.scores;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int4 rec = reinterpret_cast<const int4 *>(ta.recs)[blockIdx.x];
+    const int b = rec.x, n = rec.y, i0 = rec.z, rows = rec.w;
+    if (!GRAD && i0 != 0) return;
+    const int cnt = ta.counts ? min(max(ta.counts[b], 0), G) : G;
     const int R = 2 * (N1 - 1) - 1, own = 2 * n - 1;
     const size_t sent = (size_t)b * N1 * N1;
-    const double z = MODE == kTreeBack ? 0.0 : z64[b];
+    const double z = MODE == kTreeBack ? 0.0 : ta.z64[b];
+    const size_t at = (size_t)b * G + min(lane, G - 1);
+    float adv = 0.f, old = 0.f, ref = 0.f, up = 1.f;
+    if constexpr (MODE == kTreePolicy) {
+        adv = a.adv[at];
+        old = a.old_logp[at];
+        if (a.ref_logp != nullptr) ref = a.ref_logp[at];
+        if (a.grad_loss != nullptr) up = a.grad_loss[b];
+    } else if constexpr (MODE == kTreeBack) {
+        adv = a.grad_logp[at];
+    }
+    const float inv = 1.0f / (float)n;
+    struct Cell {
+        int i, j;
+        bool ok;
+    };
+    auto cell_of = [&](int t) {
+        int r = (int)(((float)t + 0.5f) * inv);   // t / n: t < 2^12, off by one at most
+        r -= r * n > t;
+        r += (r + 1) * n <= t;
+        const int i = i0 + r, j = t - r * n + 1;
+        return Cell{i, j, t < rows * n && j > i};
+    };
+    float p[kAhead];
+    auto load_cells = [&](int t0) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const Cell c = cell_of(t0 + u * NT);
+            p[u] = c.ok ? a.grad[sent + (size_t)c.i * N1 + c.j] : 0.f;
+        }
+    };
+    if constexpr (GRAD) {
+        load_cells(tid);
+        for (int t = tid; t < rows * n * W; t += NT) mask[t] = 0u;
+        __syncthreads();
+    }
 
-    // A wavefront a tree: its spans' scores, a row a lane.
-    for (int g = wave; g < cnt; g += kTreeThreads / 64) {
-        const int2 *t = reinterpret_cast<const int2 *>(trees) + ((size_t)b * G + g) * R;
-        double acc = 0.0;
-        for (int r0 = lane; r0 < own; r0 += 64 * kAhead) {
-            int2 sp[kAhead];
-            float v[kAhead];
+    // A wavefront a tree, its spans' scores 64 rows at a time, kAhead such
+    // pieces (of one tree or several) in flight.
+    const int pieces = (own + 63) >> 6, mine = (cnt - wave + NW - 1) / NW;
+    int g = wave, c = 0;   // the tree and piece that are summed next
+    double acc = 0.0;
+    for (int at0 = 0; at0 < mine * pieces; at0 += kAhead) {
+        int2 sp[kAhead];
+        float v[kAhead];
+        int gu = g, cu = c;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                sp[u] = t[min(r0 + 64 * u, own - 1)];
-                if (r0 + 64 * u >= own || !(0 <= sp[u].x && sp[u].x < sp[u].y && sp[u].y <= n)) sp[u].x = -1;
-            }
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = 64 * cu + lane;
+            const bool in = gu < cnt && r < own;
+            sp[u] = reinterpret_cast<const int2 *>(ta.trees)[((size_t)b * G + (in ? gu : 0)) * R + (in ? r : 0)];
+            if (!(in && 0 <= sp[u].x && sp[u].x < sp[u].y && sp[u].y <= n)) sp[u].x = -1;
+            if (++cu == pieces) cu = 0, gu += NW;
+        }
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) v[u] = sp[u].x >= 0 ? scores[sent + (size_t)sp[u].x * N1 + sp[u].y] : 0.f;
+        for (int u = 0; u < kAhead; ++u) v[u] = sp[u].x >= 0 ? scores[sent + (size_t)sp[u].x * N1 + sp[u].y] : 0.f;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const bool forced = sp[u].y == sp[u].x + 1 || (sp[u].x == 0 && sp[u].y == n);
-                acc += (double)v[u] * (forced ? 1.0 : kChartScore);
-                if constexpr (GRAD)
-                    if (sp[u].x >= i0 && sp[u].x < i0 + rows)
-                        atomicOr(&mask[((sp[u].x - i0) * n + sp[u].y - 1) * W + (g >> 5)], 1u << (g & 31));
+        for (int u = 0; u < kAhead; ++u) {
+            if (g >= cnt) break;
+            const bool forced = sp[u].y == sp[u].x + 1 || (sp[u].x == 0 && sp[u].y == n);
+            acc += (double)v[u] * (forced ? 1.0 : kChartScore);
+            if constexpr (GRAD)
+                if (sp[u].x >= i0 && sp[u].x < i0 + rows)
+                    atomicOr(&mask[((sp[u].x - i0) * n + sp[u].y - 1) * W + (g >> 5)], 1u << (g & 31));
+            if (++c == pieces) {
+                acc = wave_sum(acc);
+                if (lane == 0) sums[g] = acc;
+                acc = 0.0;
+                c = 0;
+                g += NW;
             }
         }
-        acc = wave_sum(acc);
-        if (lane == 0) sums[g] = acc;
     }
     __syncthreads();
 
     // The trees' terms, a lane each (G <= 64).
     if (wave == 0) {
         const bool here = lane < cnt;
-        const size_t at = (size_t)b * G + lane;
         const double lp = here ? sums[lane] - z : 0.0;
-        if (!GRAD || blockIdx.y == 0)
-            if (here && logp != nullptr) logp[at] = (float)lp;
+        if (i0 == 0)
+            if (here && ta.logp != nullptr) ta.logp[at] = (float)lp;
         if constexpr (MODE == kTreeLogp) {
-            if (lane == 0 && logZ != nullptr) logZ[b] = (float)z;
+            if (lane == 0 && ta.logZ != nullptr) ta.logZ[b] = (float)z;
         } else if constexpr (MODE == kTreeBack) {
-            const float c = here ? a.grad_logp[at] : 0.f;
+            const float c = here ? adv : 0.f;
             const double all = wave_sum((double)c);
             if (here) coef[lane] = c;
             if (lane == 0) coef[CRF_MAX_TREES] = (float)all;
         } else {
             double term = 0.0, c = 0.0;
             if (here) {
-                const double A = a.adv[at], r = exp(fmin(lp - (double)a.old_logp[at], kMaxLogRatio));
+                const double A = adv, r = exp(fmin(lp - (double)old, kMaxLogRatio));
                 const double kept = fmin(fmax(r, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high);
                 const bool free = r * A <= kept * A;
                 term = -(free ? r : kept) * A;
                 c = free ? -r * A : 0.0;
                 if (a.ref_logp != nullptr) {
-                    const double q = fmin((double)a.ref_logp[at] - lp, kMaxLogRatio), e = expm1(q);
+                    const double q = fmin((double)ref - lp, kMaxLogRatio), e = expm1(q);
                     term += (double)a.kl_coef * (e - q);
                     c -= (double)a.kl_coef * e;
                 }
@@ -166,7 +212,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_kernel(const int32_t *__res
             if (here) coef[lane] = (float)(c * share);
             if (lane == 0) {
                 coef[CRF_MAX_TREES] = (float)all;
-                if (blockIdx.y == 0) a.loss[b] = (float)total;
+                if (i0 == 0) a.loss[b] = (float)total;
             }
         }
     }
@@ -174,24 +220,24 @@ __global__ __launch_bounds__(kTreeThreads) void tree_kernel(const int32_t *__res
     __syncthreads();
 
     // The cells of the stripe.
-    const float all = coef[CRF_MAX_TREES], gl = a.grad_loss ? a.grad_loss[b] : 1.0f;
-    const float inv = 1.0f / (float)n;
+    const float all = coef[CRF_MAX_TREES];
     const uint32_t full[2] = {cnt >= 32 ? ~0u : (1u << cnt) - 1u, cnt >= 64 ? ~0u : cnt > 32 ? (1u << (cnt - 32)) - 1u : 0u};
-    for (int t = tid; t < rows * n; t += kTreeThreads) {
-        int r = (int)(((float)t + 0.5f) * inv);   // t / n: t < 2^13, off by one at most
-        r -= r * n > t;
-        r += (r + 1) * n <= t;
-        const int i = i0 + r, j = t - r * n + 1;
-        if (j <= i) continue;
-        float sum = 0.f;
-        bool every = cnt > 0;
-        for (int w = 0; w < W; ++w) {
-            uint32_t m = mask[t * W + w];
-            every = every && m == full[w];
-            for (; m != 0; m &= m - 1) sum += coef[32 * w + __builtin_ctz(m)];
+    for (int t0 = tid; t0 < rows * n; t0 += kAhead * NT) {
+        if (t0 != tid) load_cells(t0);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int t = t0 + u * NT;
+            const Cell c = cell_of(t);
+            if (!c.ok) continue;
+            float sum = 0.f;
+            bool every = cnt > 0;
+            for (int w = 0; w < W; ++w) {
+                uint32_t m = mask[t * W + w];
+                every = every && m == full[w];
+                for (; m != 0; m &= m - 1) sum += coef[32 * w + __builtin_ctz(m)];
+            }
+            a.grad[sent + (size_t)c.i * N1 + c.j] = up * ((every ? all : sum) - all * p[u]);
         }
-        float *cell = a.grad + sent + (size_t)i * N1 + j;
-        *cell = gl * ((every ? all : sum) - all * *cell);
     }
 }
 
@@ -203,47 +249,39 @@ static hipError_t sweep(const KernelPlan &p, const float *scores, double *z64, f
     return launch_inside(q, scores, nullptr, nullptr, marg, stream);
 }
 
-hipError_t launch_tree_logprobs(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
-                                const int32_t *counts, double *z64, float *logp, float *logZ, hipStream_t stream) {
-    const hipError_t e = sweep(p, scores, z64, nullptr, stream);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(tree_kernel<kTreeLogp>, dim3(p.B), dim3(kTreeThreads), 0, stream, p.len, p.n1, G, 1, scores, trees,
-                       counts, z64, logp, logZ, PolicyArgs{});
-    return hipGetLastError();
-}
-
-static hipError_t launch_gradient(void (*kernel)(const int32_t *, int, int, int, const float *, const int32_t *,
-                                                 const int32_t *, const double *, float *, float *, PolicyArgs),
-                                  const KernelPlan &p, int max_len, const float *scores, const int32_t *trees, int G,
-                                  const int32_t *counts, double *z64, float *logp, const PolicyArgs &a,
-                                  hipStream_t stream) {
+// The sweep, then the pass over the trees.
+template <TreeMode MODE>
+static hipError_t launch_trees(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
+                               const int32_t *counts, double *z64, float *logp, float *logZ, const PolicyArgs &a,
+                               hipStream_t stream) {
     const hipError_t e = sweep(p, scores, z64, a.grad, stream);
     if (e != hipSuccess) return e;
     const int W = (G + 31) / 32;
-    int most = 1, words = 0;
-    for (int n = 1; n <= max_len; ++n) {
-        most = std::max(most, stripes(n, W));
-        words = std::max(words, std::min(n, stripe_rows(n, W)) * n * W);
-    }
-    hipLaunchKernelGGL(kernel, dim3(p.B, most), dim3(kTreeThreads), (size_t)words * 4, stream, p.len, p.n1, G, W, scores,
-                       trees, counts, z64, logp, nullptr, a);
+    const TreeArgs ta{p.tree_recs, p.n1, G, W, scores, trees, counts, z64, logp, logZ, a};
+    hipLaunchKernelGGL(tree_kernel<MODE>, dim3(p.n_tree_recs), dim3(kTreeThreads),
+                       MODE == kTreeLogp ? 0 : (size_t)p.tree_cells * W * 4, stream, ta);
     return hipGetLastError();
 }
 
-hipError_t launch_tree_logprobs_bwd(const KernelPlan &p, int max_len, const float *scores, const int32_t *trees, int G,
+hipError_t launch_tree_logprobs(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
+                                const int32_t *counts, double *z64, float *logp, float *logZ, hipStream_t stream) {
+    return launch_trees<kTreeLogp>(p, scores, trees, G, counts, z64, logp, logZ, PolicyArgs{}, stream);
+}
+
+hipError_t launch_tree_logprobs_bwd(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
                                     const int32_t *counts, const float *grad_logp, float *grad, hipStream_t stream) {
     PolicyArgs a{};
     a.grad_logp = grad_logp;
     a.grad = grad;
-    return launch_gradient(tree_kernel<kTreeBack>, p, max_len, scores, trees, G, counts, nullptr, nullptr, a, stream);
+    return launch_trees<kTreeBack>(p, scores, trees, G, counts, nullptr, nullptr, nullptr, a, stream);
 }
 
-hipError_t launch_policy_loss(const KernelPlan &p, int max_len, const float *scores, const int32_t *trees, int G,
+hipError_t launch_policy_loss(const KernelPlan &p, const float *scores, const int32_t *trees, int G,
                               const int32_t *counts, const float *adv, const float *old_logp, const float *ref_logp,
                               float clip_low, float clip_high, float kl_coef, const float *grad_loss, double *z64,
                               float *loss, float *logp, float *grad, hipStream_t stream) {
     const PolicyArgs a{nullptr, adv, old_logp, ref_logp, grad_loss, clip_low, clip_high, kl_coef, loss, grad};
-    return launch_gradient(tree_kernel<kTreePolicy>, p, max_len, scores, trees, G, counts, z64, logp, a, stream);
+    return launch_trees<kTreePolicy>(p, scores, trees, G, counts, z64, logp, nullptr, a, stream);
 }
 
 }  // namespace crf
