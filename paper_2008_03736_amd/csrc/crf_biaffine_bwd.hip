@@ -65,52 +65,108 @@ struct Rows {
     const void *x;
     const uint8_t *scales;
 };
-// Entries k .. k+7 of row `id` (k a multiple of 8, d one of 4), zero past d;
-// ONE: entry d is 1.
-template <bool Q8, bool ONE>
-__device__ __forceinline__ uint4 load_piece(const Rows &r, int id, int k, int d) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (id >= 0 && k < d) {
+// The plan's tables are constant while a kernel runs: scalar loads where the
+// address is uniform.
+template <typename T>
+__device__ __forceinline__ T constant(const T *p) {
+    return *(const __attribute__((address_space(4))) T *)p;
+}
+
+// Staging goes through registers: loads first, without a branch (addresses that
+// hold nothing for a lane are moved to ones that exist, and what comes from
+// there is left out when it is stored), so that all of them are in flight
+// together until the products of the step before are done.  (A branch around
+// each load made the compiler wait for it there: 5,000 sentences at d = 500,
+// rows 418 us.)
+//
+// Columns k0 .. k0 + COLS of the rows of a block, to LDS with row stride
+// `stride`: wavefront w takes rows 8 w .. 8 w + 7, whose ids are then scalars,
+// kAtOnce of them side by side, a lane eight entries of each.
+template <int COLS, bool Q8>
+struct Staged {
+    static constexpr int kPieces = COLS / 8;                                  // of a row
+    static constexpr int kAtOnce = kPieces <= 32 ? 64 / kPieces : 1;          // rows
+    static constexpr int kEach = 8 / kAtOnce;
+    uint4 v[kEach];   // (Q8: codes in x and y, the scale in z)
+    int id[8];
+    static __device__ __forceinline__ int row(int u) {   // within the wavefront's eight
+        return kAtOnce * u + (kAtOnce > 1 ? (int)(threadIdx.x & 63) / kPieces : 0);
+    }
+    static __device__ __forceinline__ int col() {
+        const int lane = threadIdx.x & 63;
+        return 8 * (kAtOnce > 1 ? lane % kPieces : kPieces < 64 ? min(lane, kPieces - 1) : lane);
+    }
+    __device__ __forceinline__ int id_of(int u) const {
+        int x = id[kAtOnce * u];
+        if constexpr (kAtOnce > 1) {   // (masks: a choice would be one of addresses, and the ids in memory)
+            const int q = (int)(threadIdx.x & 63) / kPieces;
+#pragma unroll
+            for (int t = 1; t < kAtOnce; ++t) {
+                const int m = q == t ? -1 : 0;
+                x = (x & ~m) | (id[kAtOnce * u + t] & m);
+            }
+        }
+        return x;
+    }
+    // post: the block's record
+    __device__ __forceinline__ void load(const Rows &r, const int32_t *post, int k0, int d) {
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = k0 + col();
+#pragma unroll
+        for (int u = 0; u < 8; ++u) id[u] = constant(post + 8 * w + u);
         if constexpr (Q8) {
-            const int wide = row_codes(d);
-            v = eight_of_codes(*reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(r.x) + (size_t)id * wide + k),
-                               r.scales[(size_t)id * (wide / kRowBlock) + k / kRowBlock]);
-            if (k + 4 >= d) v.z = v.w = 0u;
+            const int wide = row_codes(d), kc = min(k, wide - 8);
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+                const size_t row = (size_t)max(id_of(u), 0);
+                const uint2 c = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(r.x) + row * wide + kc);
+                v[u] = make_uint4(c.x, c.y, r.scales[row * (wide / kRowBlock) + kc / kRowBlock], 0u);
+            }
         } else {
-            const uint16_t *row = static_cast<const uint16_t *>(r.x) + (size_t)id * d + k;
-            const uint2 a = *reinterpret_cast<const uint2 *>(row);
-            v.x = a.x;
-            v.y = a.y;
-            if (k + 4 < d) {
-                const uint2 b = *reinterpret_cast<const uint2 *>(row + 4);
-                v.z = b.x;
-                v.w = b.y;
+            // 16 bytes, from any multiple of 8; at a row's end its last 16
+            // (whose upper half counts where d is no multiple of 8)
+            typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(8)));
+            const uint16_t *x = static_cast<const uint16_t *>(r.x);
+            if (d >= 8) {
+                const int kc = min(k, d - 8);
+#pragma unroll
+                for (int u = 0; u < kEach; ++u) {
+                    const u32x4u q = *reinterpret_cast<const u32x4u *>(x + (size_t)max(id_of(u), 0) * d + kc);
+                    v[u] = make_uint4(q[0], q[1], q[2], q[3]);
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < kEach; ++u) {
+                    const uint2 q = *reinterpret_cast<const uint2 *>(x + (size_t)max(id_of(u), 0) * d);
+                    v[u] = make_uint4(0u, 0u, q.x, q.y);
+                }
             }
         }
     }
-    if constexpr (ONE) {
-        if (id >= 0 && k == d) v.x = 0x3F80u;
-        if (id >= 0 && k + 4 == d) v.z = 0x3F80u;
-    }
-    return v;
-}
-
-// Columns k0 .. k0 + COLS of a block's rows into LDS (row stride `stride`).
-template <bool Q8, bool ONE, int COLS>
-__device__ __forceinline__ void stage_rows(const Rows &r, const int32_t *ids, int k0, int d, uint16_t *to, int stride) {
-    constexpr int kPieces = COLS / 8, kEach = kBlk * kPieces / kThreads;
-    uint4 v[kEach];
+    // ONE: entry d is 1
+    template <bool ONE>
+    __device__ __forceinline__ void store(int k0, int d, uint16_t *to, int stride) const {
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = k0 + col();
+        const bool full = k + 8 <= d, half = k + 4 == d;
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        const int t = (int)threadIdx.x + kThreads * u;
-        v[u] = load_piece<Q8, ONE>(r, ids[t / kPieces], k0 + 8 * (t % kPieces), d);
+        for (int u = 0; u < kEach; ++u) {
+            const bool row_in = id_of(u) >= 0;
+            uint4 p = v[u];
+            if constexpr (Q8) {
+                p = eight_of_codes(make_uint2(p.x, p.y), p.z);
+                p = make_uint4(p.x, p.y, full ? p.z : 0u, full ? p.w : 0u);
+            } else {
+                p = make_uint4(full ? p.x : p.z, full ? p.y : p.w, full ? p.z : 0u, full ? p.w : 0u);
+            }
+            const bool in = row_in && (full || half);
+            p = make_uint4(in ? p.x : 0u, in ? p.y : 0u, in ? p.z : 0u, in ? p.w : 0u);
+            if constexpr (ONE) {
+                p.x = row_in && k == d ? 0x3F80u : p.x;
+                p.z = row_in && half ? 0x3F80u : p.z;
+            }
+            *reinterpret_cast<uint4 *>(to + (8 * w + row(u)) * stride + col()) = p;
+        }
     }
-#pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        const int t = (int)threadIdx.x + kThreads * u;
-        *reinterpret_cast<uint4 *>(to + t / kPieces * stride + 8 * (t % kPieces)) = v[u];
-    }
-}
+};
 
 // Where a label's gradient lies: the caller's [B][N1][N1] (COMPACT false), or
 // the compact cells of the label.
@@ -119,30 +175,58 @@ struct Grad {
     const int64_t *cells;   // KernelPlan::post_cells
     int N1;
 };
-// G of rows i in block `bi` and columns j in block `bj` as bf16 hi and lo
-// parts, [i][j], or [j][i] where TR: the cells of one sentence with i < j,
-// zero elsewhere (other cells are not read).
-template <bool COMPACT, bool TR>
-__device__ __forceinline__ void stage_grad(const Grad &g, const int32_t *posts, int bi, int bj, uint16_t *hi, uint16_t *lo) {
-    constexpr int kEach = kBlk / (kThreads / 64);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int32_t *ri = posts + (size_t)bi * kPostRec, *rj = posts + (size_t)bj * kPostRec;
-    const int idj = rj[lane], basej = rj[kBlk + lane];
-    float v[kEach];
+// G of rows i in block `bi` and columns j in block `bj`: the cells of one
+// sentence with i < j, zero elsewhere (other cells are not used).  Wavefront w
+// takes rows 8 w .. 8 w + 7, a lane a column, so that rows are read along
+// memory and a lane's eight rows are one 16-byte store of G^T[j][i]; as bf16 hi
+// and lo parts.
+struct Staged_grad {
+    float v[8];
+    uint32_t in;
+    template <bool COMPACT>
+    __device__ __forceinline__ void load(const Grad &g, const int32_t *posts, int bi, int bj) {
+        const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int32_t *ri = posts + (size_t)bi * kPostRec + 8 * w, *rj = posts + (size_t)bj * kPostRec + lane;
+        const int idj = rj[0], basej = rj[kBlk];
+        in = 0;
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        const int r = wave + (kThreads / 64) * u, idi = ri[r];
-        const bool in = idi >= 0 && idj > idi && ri[kBlk + r] == basej;
-        v[u] = 0.f;
-        if (in) v[u] = g.g[(COMPACT ? g.cells[(size_t)bi * kBlk + r] : (int64_t)idi * g.N1) + (idj - basej)];
+        for (int u = 0; u < 8; ++u) {
+            const int idi = constant(ri + u), basei = constant(ri + kBlk + u);
+            const bool ok = idi >= 0 && idj > idi && basei == basej;
+            in |= ok ? 1u << u : 0u;
+            const int64_t row = COMPACT ? constant(g.cells + (size_t)bi * kBlk + 8 * w + u) : (int64_t)idi * g.N1;
+            v[u] = g.g[ok ? row + (idj - basej) : 0];
+        }
     }
+    __device__ __forceinline__ void store(uint16_t *hi, uint16_t *lo) const {
+        const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        bf16x8 h, l;
 #pragma unroll
-    for (int u = 0; u < kEach; ++u) {
-        const int r = wave + (kThreads / 64) * u, at = TR ? lane * kGS + r : r * kGS + lane;
-        const __bf16 h = (__bf16)v[u];
-        hi[at] = __builtin_bit_cast(uint16_t, h);
-        lo[at] = __builtin_bit_cast(uint16_t, (__bf16)(v[u] - (float)h));
+        for (int u = 0; u < 8; ++u) {
+            const float x = in >> u & 1u ? v[u] : 0.f;
+            h[u] = (__bf16)x;
+            l[u] = (__bf16)(x - (float)h[u]);
+        }
+        *reinterpret_cast<uint4 *>(hi + lane * kGS + 8 * w) = __builtin_bit_cast(uint4, h);
+        *reinterpret_cast<uint4 *>(lo + lane * kGS + 8 * w) = __builtin_bit_cast(uint4, l);
     }
+};
+// Operands of the staged G^T, posts 16 r .. +15 by K offsets 32 ks .. +31: rows
+// j with K over i, or (ROWS_I) rows i with K over j.
+template <bool ROWS_I>
+__device__ __forceinline__ bf16x8 grad_frag(const uint16_t *gt, int r, int ks, int lr, int lg) {
+    if constexpr (ROWS_I) {
+        const uint16_t *p = gt + (32 * ks + 8 * lg + (lr >> 2)) * kGS + 16 * r + 4 * (lr & 3);
+        return frag_rows(p, p + 4 * kGS);
+    } else {
+        return frag(gt + (16 * r + lr) * kGS + 32 * ks + 8 * lg);
+    }
+}
+// Whether that part of a block's product with itself can be other than zero
+// (i < j).
+template <bool ROWS_I>
+__device__ __forceinline__ constexpr bool grad_part(int r, int ks) {
+    return ROWS_I ? 32 * ks + 31 > 16 * r : 32 * ks < 16 * r + 15;
 }
 
 // W's fragments for the dense products, from W transposed as the scorer takes
@@ -201,143 +285,200 @@ __global__ __launch_bounds__(256) void bwd_compact_kernel(const int32_t *__restr
 struct BwdArgs {
     const int32_t *posts;
     const int64_t *post_cells;
-    int n_posts, N1, d, L, per_group;   // per_group: labels of a workgroup
+    int n_posts, N1, d, L, per_group;   // per_group: labels of a group
     Rows rl, rr;
     const uint16_t *wf;                 // bwd_weights_kernel's fragments
     const float *g;
     int64_t cells;                      // floats between the labels of a compact gradient
     uint16_t *out[2];                   // dR^l, dR^r
-    float *part;                        // [label groups][2][posts][16 * column blocks]: partial sums, or NULL
-    int zs;                             // workgroups that share a pair of blocks' output columns
-    int side0;                          // the first grid.y's side
+    float *part;                        // [label groups][2][posts][DP]: partial sums, or NULL
+    int zs;                             // items that share blocks' output columns
+    int items, side0;                   // items of a side; the first grid.y's side
 };
 
-// dR^l (side 0) and dR^r (side 1) of two blocks of posts: for each label, the
-// blocks' U (or X) into LDS as bf16, 128 x DP, then its product with W's
+// dR^l (side 0) and dR^r (side 1) of H blocks of posts: for each label, the
+// blocks' U (or X) into LDS as bf16, 64 H x DP, then its product with W's
 // fragments, which come straight from L2 in the order of the lanes, each read
 // by the one row of wavefronts that needs its columns.  NB: 16-column blocks
 // of U per wavefront (DP = 128 NB); CB: output column blocks of a wavefront,
 // WR: rows of wavefronts.
-template <int NB>
+//
+// A workgroup goes through items (blocks, label group, column share) on its
+// own, and what the next step of staging needs (the rows of R and the cells of
+// G of one pair of blocks) is in flight in registers during this step's
+// products: with a workgroup an item and loads where they are needed, 5,000
+// sentences at d = 500 took 418 us, 200 of them waiting for R and G.
+template <int NB, int H>
 struct RowsShape {
     static constexpr int kDP = 128 * NB, kPS = kDP + kPadCols;
-    // U of 128 posts beside R, or R where U will be (its columns are in
-    // registers until every wavefront has read R)
+    // U beside R, or R where U will be (U's columns are in registers until
+    // every wavefront has read R)
     static constexpr bool kApart = NB <= 2;
-    static constexpr int kLds = 2 * ((kApart ? 4 : 2) * kBlk * kPS + 2 * kBlk * kGS);
+    static constexpr int kLds = 2 * ((kApart ? 2 : 1) * H * kBlk * kPS + 2 * kBlk * kGS);
 };
 
-template <int NB, int CB, int WR, bool Q8, bool COMPACT, int SIDE>
+template <int NB, int H, int CB, int WR, bool Q8, bool COMPACT, int SIDE>
 __device__ __forceinline__ void bwd_rows(const BwdArgs &a, char *smem) {
-    typedef RowsShape<NB> S;
-    constexpr int DP = S::kDP, PS = S::kPS, WC = 8 / WR, RB = 8 / WR;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    typedef RowsShape<NB, H> S;
+    constexpr int DP = S::kDP, PS = S::kPS, WC = 8 / WR, RB = 4 * H / WR;
+    constexpr bool ONE = SIDE == 1, ROWS_I = SIDE == 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 15, lg = lane >> 4;
-    uint16_t *P = reinterpret_cast<uint16_t *>(smem);                  // [128][PS]: U or X
-    uint16_t *R = S::kApart ? P + 2 * kBlk * PS : P;                   // [128][PS]: the partners' rows
-    uint16_t *Gh = R + 2 * kBlk * PS, *Gl = Gh + kBlk * kGS;
-    const int pair = blockIdx.x, cz = (int)blockIdx.z % a.zs, grp = (int)blockIdx.z / a.zs;
-    const int l0 = grp * a.per_group, l1 = min(l0 + a.per_group, a.L);
-    const int wr = wave / WC, wc = wave % WC, col0 = (cz * WC + wc) * CB;   // first output column block
-    const int ksteps = (a.d + 32) / 32;                                      // K of the dense product: d + 1 at most
+    uint16_t *P = reinterpret_cast<uint16_t *>(smem);                  // [64 H][PS]: U or X
+    uint16_t *R = S::kApart ? P + H * kBlk * PS : P;                   // [64 H][PS]: the partners' rows
+    uint16_t *Gh = R + H * kBlk * PS, *Gl = Gh + kBlk * kGS;
+    const int units = a.n_posts / H;
+    const int wr = wave / WC, wc = wave % WC;
+    const int ksteps = (a.d + 32) / 32;   // K of the dense product: d + 1 at most
+    const Rows rows = SIDE == 0 ? a.rr : a.rl;
 
-    f32x4 acc[CB][RB];
-    for (int l = l0;;) {   // (one label, l = 0, unless COMPACT)
-        const Grad g{a.g + (COMPACT ? l * a.cells : 0), a.post_cells, a.N1};
+    // An item: its blocks, labels and column share.
+    struct Item {
+        int unit, l0, l1, cz, grp;
+    };
+    auto item_of = [&](int it) {
+        Item x;
+        x.unit = it % units;
+        const int q = it / units;
+        x.cz = q % a.zs;
+        x.grp = q / a.zs;
+        x.l0 = x.grp * a.per_group;
+        x.l1 = min(x.l0 + a.per_group, a.L);
+        return x;
+    };
+    // A block's partners: side 0 itself and those after it, side 1 those before it and itself.
+    auto first_of = [&](int blk) { return SIDE == 0 ? blk : constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk); };
+    auto last_of = [&](int blk) { return SIDE == 0 ? constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk + 1) : blk; };
+    auto grad_of = [&](int l) { return Grad{a.g + (COMPACT ? l * a.cells : 0), a.post_cells, a.N1}; };
+
+    Staged<DP, Q8> sr;
+    Staged_grad sg;
+    auto load_step = [&](int l, int blk, int q, bool with_r) {
+        sg.load<COMPACT>(grad_of(l), a.posts, SIDE == 0 ? blk : q, SIDE == 0 ? q : blk);
+        if (with_r) sr.load(rows, a.posts + (size_t)q * kPostRec, 0, a.d);
+    };
+    // R stays in LDS from one label to the next where blocks have one partner
+    auto keeps_r = [&](int blk) { return S::kApart && first_of(blk) == last_of(blk); };
+
+    int it = blockIdx.x;
+    if (it >= a.items) return;
+    Item x = item_of(it);
+    load_step(x.l0, H * x.unit, first_of(H * x.unit), true);
+    for (;;) {
+        const int next_it = it + gridDim.x;
+        const Item nx = item_of(min(next_it, a.items - 1));
+        f32x4 acc[CB][RB];
+        for (int l = x.l0;;) {   // (one label, l = 0, unless COMPACT)
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-            const int blk = 2 * pair + h;
-            if (blk >= a.n_posts) break;
-            const int32_t *rec = a.posts + (size_t)blk * kPostRec;
-            const int first = rec[2 * kBlk], last = rec[2 * kBlk + 1];
-            const int q0 = SIDE == 0 ? blk : first, q1 = SIDE == 0 ? last : blk;
-            f32x4 u[NB][4];
+            for (int h = 0; h < H; ++h) {
+                const int blk = H * x.unit + h, q1 = last_of(blk);
+                f32x4 u[NB][4];
 #pragma unroll
-            for (int c = 0; c < NB; ++c)
+                for (int c = 0; c < NB; ++c)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) u[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-            uint16_t *Rh = R + h * kBlk * PS;
-            for (int q = q0; q <= q1; ++q) {
-                __syncthreads();   // the readers of what is staged next are done
-                if (!(S::kApart && l > l0 && first == last))
-                    stage_rows<Q8, SIDE == 1, DP>(SIDE == 0 ? a.rr : a.rl, a.posts + (size_t)q * kPostRec, 0, a.d, Rh, PS);
-                stage_grad<COMPACT, SIDE == 1>(g, a.posts, SIDE == 0 ? blk : q, SIDE == 0 ? q : blk, Gh, Gl);
-                __syncthreads();
+                    for (int r = 0; r < 4; ++r) u[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+                uint16_t *Rh = R + h * kBlk * PS;
+                for (int q = first_of(blk); q <= q1; ++q) {
+                    __syncthreads();   // the readers of what is stored next are done
+                    if (!(l > x.l0 && keeps_r(blk))) sr.template store<ONE>(0, a.d, Rh, PS);
+                    sg.store(Gh, Gl);
+                    // the next step: the next partner, block, label or item
+                    if (q < q1) load_step(l, blk, q + 1, true);
+                    else if (h + 1 < H) load_step(l, blk + 1, first_of(blk + 1), !(l > x.l0 && keeps_r(blk + 1)));
+                    else if (COMPACT && l + 1 < x.l1) load_step(l + 1, H * x.unit, first_of(H * x.unit), !keeps_r(H * x.unit));
+                    else if (next_it < a.items) load_step(nx.l0, H * nx.unit, first_of(H * nx.unit), true);
+                    __syncthreads();
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-                    bf16x8 gh[4], gl[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        gh[r] = frag(Gh + (16 * r + lr) * kGS + 32 * ks + 8 * lg);
-                        gl[r] = frag(Gl + (16 * r + lr) * kGS + 32 * ks + 8 * lg);
-                    }
-#pragma unroll
-                    for (int c = 0; c < NB; ++c) {
-                        const uint16_t *p = Rh + (32 * ks + 8 * lg + (lr >> 2)) * PS + 16 * (wave * NB + c) + 4 * (lr & 3);
-                        const bf16x8 rf = frag_rows(p, p + 4 * PS);
+                    for (int ks = 0; ks < 2; ++ks) {
+                        bf16x8 gh[4], gl[4];
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            u[c][r] = mfma(rf, gh[r], u[c][r]);
-                            u[c][r] = mfma(rf, gl[r], u[c][r]);
+                            gh[r] = grad_frag<ROWS_I>(Gh, r, ks, lr, lg);
+                            gl[r] = grad_frag<ROWS_I>(Gl, r, ks, lr, lg);
+                        }
+#pragma unroll
+                        for (int c = 0; c < NB; ++c) {
+                            const uint16_t *p = Rh + (32 * ks + 8 * lg + (lr >> 2)) * PS + 16 * (wave * NB + c) + 4 * (lr & 3);
+                            const bf16x8 rf = frag_rows(p, p + 4 * PS);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (grad_part<ROWS_I>(r, ks) || q != blk) {
+                                    u[c][r] = mfma(rf, gh[r], u[c][r]);
+                                    u[c][r] = mfma(rf, gl[r], u[c][r]);
+                                }
                         }
                     }
                 }
+                if constexpr (!S::kApart) __syncthreads();   // R's readers are done
+                // u[c][r]: columns 16 (wave NB + c) + 4 lg .. +3 of post 16 r + lr
+#pragma unroll
+                for (int c = 0; c < NB; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        *reinterpret_cast<bf16x4 *>(P + (h * kBlk + 16 * r + lr) * PS + 16 * (wave * NB + c) + 4 * lg) =
+                            __builtin_convertvector(u[c][r], bf16x4);
             }
-            if constexpr (!S::kApart) __syncthreads();   // R's readers are done
-            // u[c][r]: columns 16 (wave NB + c) + 4 lg .. +3 of post 16 r + lr
-#pragma unroll
-            for (int c = 0; c < NB; ++c)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    *reinterpret_cast<bf16x4 *>(P + (h * kBlk + 16 * r + lr) * PS + 16 * (wave * NB + c) + 4 * lg) =
-                        __builtin_convertvector(u[c][r], bf16x4);
-        }
-        __syncthreads();
+            __syncthreads();
 
-        if (!COMPACT || l == l0)
+            if (!COMPACT || l == x.l0)
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
+                for (int c = 0; c < CB; ++c)
 #pragma unroll
-                for (int r = 0; r < RB; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const uint16_t *wf = a.wf + ((((size_t)l * 2 + SIDE) * (DP / 32)) * (DP / 16) + col0) * 512 + 8 * lane;
-        const uint16_t *prow = P + (wr * RB * 16 + lr) * PS + 8 * lg;
-        for (int ks = 0; ks < ksteps; ++ks) {
-            bf16x8 wv[CB];
+                    for (int r = 0; r < RB; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int col0 = (x.cz * WC + wc) * CB;   // the wavefront's first output column block
+            const uint16_t *wf = a.wf + ((((size_t)l * 2 + SIDE) * (DP / 32)) * (DP / 16) + col0) * 512 + 8 * lane;
+            const uint16_t *prow = P + (wr * RB * 16 + lr) * PS + 8 * lg;
+            bf16x8 wv[2][CB];   // two steps of W
 #pragma unroll
-            for (int c = 0; c < CB; ++c) wv[c] = frag(wf + ((size_t)ks * (DP / 16) + c) * 512);
+            for (int c = 0; c < CB; ++c) wv[0][c] = frag(wf + (size_t)c * 512);
+            auto dense_step = [&](int ks, bf16x8 (&now)[CB], bf16x8 (&then)[CB]) {
+                const int kn = min(ks + 1, ksteps - 1);
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const bf16x8 pv = frag(prow + 16 * r * PS + 32 * ks);
+                for (int c = 0; c < CB; ++c) then[c] = frag(wf + ((size_t)kn * (DP / 16) + c) * 512);
 #pragma unroll
-                for (int c = 0; c < CB; ++c) acc[c][r] = mfma(wv[c], pv, acc[c][r]);
+                for (int r = 0; r < RB; ++r) {
+                    const bf16x8 pv = frag(prow + 16 * r * PS + 32 * ks);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) acc[c][r] = mfma(now[c], pv, acc[c][r]);
+                }
+            };
+            int ks = 0;
+            for (; ks + 1 < ksteps; ks += 2) {
+                dense_step(ks, wv[0], wv[1]);
+                dense_step(ks + 1, wv[1], wv[0]);
+            }
+            if (ks < ksteps) dense_step(ks, wv[0], wv[1]);
+            if (!COMPACT || ++l >= x.l1) break;
+        }
+
+        // acc[c][r]: columns 16 (col0 + c) + 4 lg .. +3 of post 16 (wr RB + r) + lr
+        const int col0 = (x.cz * WC + wc) * CB;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int slot = 16 * (wr * RB + r) + lr, blk = H * x.unit + slot / kBlk;
+            const int id = a.posts[(size_t)blk * kPostRec + slot % kBlk];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                const int col = 16 * (col0 + c) + 4 * lg;
+                if (id < 0 || col >= a.d) continue;
+                if (a.part != nullptr)
+                    *reinterpret_cast<f32x4 *>(a.part + (((size_t)x.grp * 2 + SIDE) * a.n_posts * kBlk + H * kBlk * x.unit + slot) * DP + col) =
+                        acc[c][r];
+                else
+                    *reinterpret_cast<bf16x4 *>(a.out[SIDE] + (size_t)id * a.d + col) = __builtin_convertvector(acc[c][r], bf16x4);
             }
         }
-        if (!COMPACT || ++l >= l1) break;
-    }
-
-    // acc[c][r]: columns 16 (col0 + c) + 4 lg .. +3 of post 16 (wr RB + r) + lr
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const int slot = 16 * (wr * RB + r) + lr, blk = 2 * pair + slot / kBlk;
-        const int id = blk < a.n_posts ? a.posts[(size_t)blk * kPostRec + slot % kBlk] : -1;
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-            const int col = 16 * (col0 + c) + 4 * lg;
-            if (id < 0 || col >= a.d) continue;
-            if (a.part != nullptr)
-                *reinterpret_cast<f32x4 *>(a.part + (((size_t)grp * 2 + SIDE) * a.n_posts * kBlk + blk * kBlk + slot % kBlk) * DP + col) =
-                    acc[c][r];
-            else
-                *reinterpret_cast<bf16x4 *>(a.out[SIDE] + (size_t)id * a.d + col) = __builtin_convertvector(acc[c][r], bf16x4);
-        }
+        if (next_it >= a.items) break;
+        it = next_it;
+        x = nx;
     }
 }
 
-template <int NB, int CB, int WR, bool Q8, bool COMPACT>
+template <int NB, int H, int CB, int WR, bool Q8, bool COMPACT>
 __global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdArgs a) {
     extern __shared__ __align__(16) char smem[];
-    if (blockIdx.y + a.side0 == 0) bwd_rows<NB, CB, WR, Q8, COMPACT, 0>(a, smem);
-    else bwd_rows<NB, CB, WR, Q8, COMPACT, 1>(a, smem);
+    if (blockIdx.y + a.side0 == 0) bwd_rows<NB, H, CB, WR, Q8, COMPACT, 0>(a, smem);
+    else bwd_rows<NB, H, CB, WR, Q8, COMPACT, 1>(a, smem);
 }
 
 // The label groups' partial sums of dR^l and dR^r, added in their order: a
@@ -395,8 +536,16 @@ __global__ __launch_bounds__(kThreads) void bwd_weight_kernel(WeightArgs a) {
 #pragma unroll
         for (int c = 0; c < T; ++c) acc[x][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+    Staged<S::kT, Q8> sa, sc;
+    Staged_grad sg;
+    auto load_step = [&](int blk, int q) {
+        sg.load<COMPACT>(g, a.posts, blk, q);
+        sc.load(a.rr, a.posts + (size_t)q * kPostRec, c0, a.d);
+        if (q == blk) sa.load(a.rl, a.posts + (size_t)blk * kPostRec, a0, a.d);
+    };
+    if (b0 < b1) load_step(b0, b0);
     for (int blk = b0; blk < b1; ++blk) {
-        const int last = a.posts[(size_t)blk * kPostRec + 2 * kBlk + 1];
+        const int last = constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk + 1);
         f32x4 u[4][T];
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -404,9 +553,11 @@ __global__ __launch_bounds__(kThreads) void bwd_weight_kernel(WeightArgs a) {
             for (int c = 0; c < T; ++c) u[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int q = blk; q <= last; ++q) {
             __syncthreads();
-            if (q == blk) stage_rows<Q8, true, S::kT>(a.rl, a.posts + (size_t)blk * kPostRec, a0, a.d, Ra, TS);
-            stage_rows<Q8, false, S::kT>(a.rr, a.posts + (size_t)q * kPostRec, c0, a.d, Rc, TS);
-            stage_grad<COMPACT, false>(g, a.posts, blk, q, Gh, Gl);
+            if (q == blk) sa.template store<true>(a0, a.d, Ra, TS);
+            sc.template store<false>(c0, a.d, Rc, TS);
+            sg.store(Gh, Gl);
+            if (q < last) load_step(blk, q + 1);
+            else if (blk + 1 < b1) load_step(blk + 1, blk + 1);
             __syncthreads();
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks)
@@ -415,10 +566,11 @@ __global__ __launch_bounds__(kThreads) void bwd_weight_kernel(WeightArgs a) {
                     const uint16_t *p = Rc + (32 * ks + 8 * lg + (lr >> 2)) * TS + 16 * (wave * T + c) + 4 * (lr & 3);
                     const bf16x8 rf = frag_rows(p, p + 4 * TS);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        u[r][c] = mfma(frag(Gh + (16 * r + lr) * kGS + 32 * ks + 8 * lg), rf, u[r][c]);
-                        u[r][c] = mfma(frag(Gl + (16 * r + lr) * kGS + 32 * ks + 8 * lg), rf, u[r][c]);
-                    }
+                    for (int r = 0; r < 4; ++r)
+                        if (grad_part<true>(r, ks) || q != blk) {
+                            u[r][c] = mfma(grad_frag<true>(Gh, r, ks, lr, lg), rf, u[r][c]);
+                            u[r][c] = mfma(grad_frag<true>(Gl, r, ks, lr, lg), rf, u[r][c]);
+                        }
                 }
         }
 #pragma unroll
@@ -488,10 +640,13 @@ __global__ __launch_bounds__(256) void bwd_join_weight_kernel(int d, int ldw, in
 
 inline int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
+constexpr int kCus = 256;
+
 // How a call is cut up, and its workspace.
 struct BwdPlan {
     int nb, dp;                     // DP = 128 nb
-    int zs, groups, per_group;      // column shares; label groups and labels of one
+    bool small;                     // few blocks: a block an item, its columns shared by nb items
+    int h, zs, groups, per_group;   // blocks of an item; column shares; label groups and labels of one
     int t, tiles_a, tiles_c, splits;
     int64_t w_at, g_at, part_at, wpart_at, bytes;
 };
@@ -499,16 +654,18 @@ BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     BwdPlan b{};
     b.nb = (d + 1 + 127) / 128;
     b.dp = 128 * b.nb;
-    const int pairs = (p.n_posts + 1) / 2;
-    b.zs = 1;
-    b.groups = std::max(1, std::min(L, 512 / (2 * pairs)));
+    b.small = (int64_t)p.n_posts * L < 256;
+    b.h = b.small || b.nb == 1 ? 1 : 2;
+    b.zs = b.small ? b.nb : 1;
+    const int64_t items = (int64_t)p.n_posts / b.h * 2;
+    b.groups = (int)std::max<int64_t>(1, std::min<int64_t>(L, 2 * kCus / items));
     b.per_group = (L + b.groups - 1) / b.groups;
     b.groups = (L + b.per_group - 1) / b.per_group;
     b.t = d + 1 > 128 ? 2 : 1;
     b.tiles_a = (d + 1 + 128 * b.t - 1) / (128 * b.t);
     b.tiles_c = (d + 128 * b.t - 1) / (128 * b.t);
     const int64_t wgs = (int64_t)b.tiles_a * b.tiles_c * L;
-    b.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.n_posts, (b.t == 2 ? 256 : 768) / wgs));
+    b.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.n_posts, (b.t == 2 ? kCus : 3 * kCus) / wgs));
     int64_t at = 0;
     b.w_at = at;
     at += up256((int64_t)L * 2 * b.dp * b.dp * 2);
@@ -522,20 +679,24 @@ BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     return b;
 }
 
-template <int NB, int CB, int WR, bool Q8, bool COMPACT>
-hipError_t launch_rows(const BwdArgs &a, int sides, int groups, hipStream_t stream) {
-    hipLaunchKernelGGL((bwd_rows_kernel<NB, CB, WR, Q8, COMPACT>), dim3((a.n_posts + 1) / 2, sides, a.zs * groups),
-                       dim3(kThreads), RowsShape<NB>::kLds, stream, a);
+template <int NB, int H, int CB, int WR, bool Q8, bool COMPACT>
+hipError_t launch_rows(const BwdArgs &a, int sides, int per_cu, hipStream_t stream) {
+    const int slots = std::max(1, per_cu * kCus / sides);
+    hipLaunchKernelGGL((bwd_rows_kernel<NB, H, CB, WR, Q8, COMPACT>), dim3(std::min(a.items, slots), sides), dim3(kThreads),
+                       (RowsShape<NB, H>::kLds), stream, a);
     return hipGetLastError();
 }
+// Every build of bwd_rows_kernel, with the workgroups of one that a CU holds.
+#define CRF_BWD_ROWS(F)                                                                             \
+    F(1, false, 1, 1, 2, 2, 2) F(2, false, 2, 2, 4, 2, 1) F(3, false, 3, 2, 3, 1, 1) F(4, false, 4, 2, 4, 1, 1) \
+    F(1, true, 1, 1, 1, 1, 2) F(2, true, 2, 1, 1, 1, 1) F(3, true, 3, 1, 1, 1, 1) F(4, true, 4, 1, 1, 1, 1)
 template <bool Q8, bool COMPACT>
-hipError_t launch_rows_nb(int nb, const BwdArgs &a, int sides, int groups, hipStream_t stream) {
-    switch (nb) {
-        case 1: return launch_rows<1, 2, 2, Q8, COMPACT>(a, sides, groups, stream);
-        case 2: return launch_rows<2, 4, 2, Q8, COMPACT>(a, sides, groups, stream);
-        case 3: return launch_rows<3, 3, 1, Q8, COMPACT>(a, sides, groups, stream);
-        default: return launch_rows<4, 4, 1, Q8, COMPACT>(a, sides, groups, stream);
-    }
+hipError_t launch_rows_of(const BwdPlan &b, const BwdArgs &a, int sides, hipStream_t stream) {
+#define CRF_LAUNCH(N, SMALL, NB, H, CB, WR, PER) \
+    if (b.nb == N && b.small == SMALL) return launch_rows<NB, H, CB, WR, Q8, COMPACT>(a, sides, PER, stream);
+    CRF_BWD_ROWS(CRF_LAUNCH)
+#undef CRF_LAUNCH
+    return hipErrorInvalidValue;
 }
 template <bool Q8, bool COMPACT>
 hipError_t launch_weight(const BwdPlan &b, const WeightArgs &a, int L, hipStream_t stream) {
@@ -551,11 +712,11 @@ template <bool Q8, bool COMPACT>
 hipError_t set_attributes() {
     hipError_t e;
     auto set = [&](const void *f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-    if ((e = set((const void *)bwd_rows_kernel<1, 2, 2, Q8, COMPACT>, RowsShape<1>::kLds)) != hipSuccess ||
-        (e = set((const void *)bwd_rows_kernel<2, 4, 2, Q8, COMPACT>, RowsShape<2>::kLds)) != hipSuccess ||
-        (e = set((const void *)bwd_rows_kernel<3, 3, 1, Q8, COMPACT>, RowsShape<3>::kLds)) != hipSuccess ||
-        (e = set((const void *)bwd_rows_kernel<4, 4, 1, Q8, COMPACT>, RowsShape<4>::kLds)) != hipSuccess ||
-        (e = set((const void *)bwd_weight_kernel<1, Q8, COMPACT>, WeightShape<1>::kLds)) != hipSuccess ||
+#define CRF_SET(N, SMALL, NB, H, CB, WR, PER) \
+    if ((e = set((const void *)bwd_rows_kernel<NB, H, CB, WR, Q8, COMPACT>, RowsShape<NB, H>::kLds)) != hipSuccess) return e;
+    CRF_BWD_ROWS(CRF_SET)
+#undef CRF_SET
+    if ((e = set((const void *)bwd_weight_kernel<1, Q8, COMPACT>, WeightShape<1>::kLds)) != hipSuccess ||
         (e = set((const void *)bwd_weight_kernel<2, Q8, COMPACT>, WeightShape<2>::kLds)) != hipSuccess)
         return e;
     return hipSuccess;
@@ -596,11 +757,9 @@ hipError_t launch_biaffine_bwd(const KernelPlan &p, int64_t cells, const void *r
         const int side0 = grad_rl != nullptr ? 0 : 1, sides = (grad_rl != nullptr) + (grad_rr != nullptr);
         float *part = b.groups > 1 ? reinterpret_cast<float *>(ws + b.part_at) : nullptr;
         const BwdArgs a{p.posts, p.post_cells, p.n_posts, p.n1, d, L, b.per_group, Rows{rl, rl_scales}, Rows{rr, rr_scales},
-                        wf, g, cells, {grad_rl, grad_rr}, part, b.zs, side0};
-        e = q8 ? (L > 1 ? launch_rows_nb<true, true>(b.nb, a, sides, b.groups, stream)
-                        : launch_rows_nb<true, false>(b.nb, a, sides, b.groups, stream))
-               : (L > 1 ? launch_rows_nb<false, true>(b.nb, a, sides, b.groups, stream)
-                        : launch_rows_nb<false, false>(b.nb, a, sides, b.groups, stream));
+                        wf, g, cells, {grad_rl, grad_rr}, part, b.zs, p.n_posts / b.h * b.zs * b.groups, side0};
+        e = q8 ? (L > 1 ? launch_rows_of<true, true>(b, a, sides, stream) : launch_rows_of<true, false>(b, a, sides, stream))
+               : (L > 1 ? launch_rows_of<false, true>(b, a, sides, stream) : launch_rows_of<false, false>(b, a, sides, stream));
         if (e != hipSuccess) return e;
         if (part != nullptr) {
             const int64_t n = (int64_t)p.n_posts * kBlk * (d / 4);

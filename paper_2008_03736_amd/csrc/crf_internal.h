@@ -483,7 +483,7 @@ struct KernelPlan {
     // (b N1 + fence post, or -1)
     const int32_t *bia_tiles;
     int32_t n_bia_tiles;
-    // every fence post of the batch once, in blocks: kPostRec ints a block
+    // every fence post of the batch once, in an even number of blocks: kPostRec ints a block
     // (kBiaRows ids b N1 + fence post or -1, the ids b N1 of their sentences'
     // first posts, then the first and the last block that hold posts of its
     // sentences), and for each of them where its row's cells are in a compact

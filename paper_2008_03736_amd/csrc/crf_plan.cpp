@@ -578,6 +578,8 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
             const int at = (int)(posts.size() / crf::kPostRec);
             put_block(ids.data(), (int)ids.size(), at, at);
         }
+        const int blocks = (int)(posts.size() / crf::kPostRec);
+        if (blocks % 2 != 0) put_block(nullptr, 0, blocks, blocks);   // an even number: some kernels take pairs
     }
 
     std::vector<int32_t> len(lengths_host, lengths_host + batch);
