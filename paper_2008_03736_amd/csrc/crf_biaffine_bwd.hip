@@ -64,6 +64,7 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f3
 struct Rows {
     const void *x;
     const uint8_t *scales;
+    int last;   // the last row that 16 bytes of bf16 can be read from (see Staged)
 };
 // The plan's tables are constant while a kernel runs: scalar loads where the
 // address is uniform.
@@ -122,29 +123,23 @@ struct Staged {
                 v[u] = make_uint4(c.x, c.y, r.scales[row * (wide / kRowBlock) + kc / kRowBlock], 0u);
             }
         } else {
-            // 16 bytes, from any multiple of 8; at a row's end its last 16
-            // (whose upper half counts where d is no multiple of 8)
+            // 16 bytes, from any multiple of 8; at a row's end its last 16,
+            // whose upper half counts where d is no multiple of 8.  Rows of
+            // four entries: 16 bytes from the row on, or for the last row of
+            // all from the one before.
             typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(8)));
-            const uint16_t *x = static_cast<const uint16_t *>(r.x);
-            if (d >= 8) {
-                const int kc = min(k, d - 8);
+            const int kc = max(min(k, d - 8), 0);
 #pragma unroll
-                for (int u = 0; u < kEach; ++u) {
-                    const u32x4u q = *reinterpret_cast<const u32x4u *>(x + (size_t)max(id_of(u), 0) * d + kc);
-                    v[u] = make_uint4(q[0], q[1], q[2], q[3]);
-                }
-            } else {
-#pragma unroll
-                for (int u = 0; u < kEach; ++u) {
-                    const uint2 q = *reinterpret_cast<const uint2 *>(x + (size_t)max(id_of(u), 0) * d);
-                    v[u] = make_uint4(0u, 0u, q.x, q.y);
-                }
+            for (int u = 0; u < kEach; ++u) {
+                const uint16_t *x = static_cast<const uint16_t *>(r.x) + (size_t)min(max(id_of(u), 0), r.last) * d;
+                const u32x4u q = *reinterpret_cast<const u32x4u *>(x + kc);
+                v[u] = make_uint4(q[0], q[1], q[2], q[3]);
             }
         }
     }
     // ONE: entry d is 1
     template <bool ONE>
-    __device__ __forceinline__ void store(int k0, int d, uint16_t *to, int stride) const {
+    __device__ __forceinline__ void store(const Rows &r, int k0, int d, uint16_t *to, int stride) const {
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = k0 + col();
         const bool full = k + 8 <= d, half = k + 4 == d;
 #pragma unroll
@@ -155,7 +150,8 @@ struct Staged {
                 p = eight_of_codes(make_uint2(p.x, p.y), p.z);
                 p = make_uint4(p.x, p.y, full ? p.z : 0u, full ? p.w : 0u);
             } else {
-                p = make_uint4(full ? p.x : p.z, full ? p.y : p.w, full ? p.z : 0u, full ? p.w : 0u);
+                const bool low = full || (d < 8 && id_of(u) <= r.last);
+                p = make_uint4(low ? p.x : p.z, low ? p.y : p.w, full ? p.z : 0u, full ? p.w : 0u);
             }
             const bool in = row_in && (full || half);
             p = make_uint4(in ? p.x : 0u, in ? p.y : 0u, in ? p.z : 0u, in ? p.w : 0u);
@@ -168,34 +164,39 @@ struct Staged {
     }
 };
 
-// Where a label's gradient lies: the caller's [B][N1][N1] (COMPACT false), or
-// the compact cells of the label.
+// A label's gradient and where each post's cell (i, i) would be in it: the
+// caller's [B][N1][N1], or the compact cells of the label
+// (KernelPlan::post_cells).
 struct Grad {
     const float *g;
-    const int64_t *cells;   // KernelPlan::post_cells
-    int N1;
+    const int64_t *cells;
 };
 // G of rows i in block `bi` and columns j in block `bj`: the cells of one
-// sentence with i < j, zero elsewhere (other cells are not used).  Wavefront w
-// takes rows 8 w .. 8 w + 7, a lane a column, so that rows are read along
-// memory and a lane's eight rows are one 16-byte store of G^T[j][i]; as bf16 hi
-// and lo parts.
+// sentence with i < j, zero elsewhere (other cells are not used).  Posts of a
+// sentence are neighbours, so row r's cells are its n - i next columns.
+// Wavefront w takes rows 8 w .. 8 w + 7, a lane a column, so that rows are read
+// along memory, what a row needs is scalar and a lane's eight rows are one
+// 16-byte store of G^T[j][i]; as bf16 hi and lo parts.
 struct Staged_grad {
     float v[8];
     uint32_t in;
-    template <bool COMPACT>
     __device__ __forceinline__ void load(const Grad &g, const int32_t *posts, int bi, int bj) {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int32_t *ri = posts + (size_t)bi * kPostRec + 8 * w, *rj = posts + (size_t)bj * kPostRec + lane;
-        const int idj = rj[0], basej = rj[kBlk];
+        const int32_t *rest = posts + (size_t)bi * kPostRec + kBlk + 8 * w;
+        const int64_t *cell = g.cells + (size_t)bi * kBlk + 8 * w;
+        int n[8];
+        int64_t c[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) n[u] = constant(rest + u);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) c[u] = constant(cell + u);
+        const int at = kBlk * (bj - bi) + lane - 8 * w;   // j - i of row 8 w
         in = 0;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const int idi = constant(ri + u), basei = constant(ri + kBlk + u);
-            const bool ok = idi >= 0 && idj > idi && basei == basej;
+            const bool ok = at - u > 0 && at - u <= n[u];
             in |= ok ? 1u << u : 0u;
-            const int64_t row = COMPACT ? constant(g.cells + (size_t)bi * kBlk + 8 * w + u) : (int64_t)idi * g.N1;
-            v[u] = g.g[ok ? row + (idj - basej) : 0];
+            v[u] = (g.g + c[u])[ok ? at - u : 1];   // (cell (i, i+1), which exists)
         }
     }
     __device__ __forceinline__ void store(uint16_t *hi, uint16_t *lo) const {
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(256) void bwd_weights_kernel(const uint16_t *__rest
 constexpr int kTrCells = 32;
 __global__ __launch_bounds__(256) void bwd_compact_kernel(const int32_t *__restrict__ posts,
                                                           const int64_t *__restrict__ post_cells,
-                                                          const int32_t *__restrict__ len, int N1, int L, int64_t cells,
+                                                          const int64_t *__restrict__ square_cells, int L, int64_t cells,
                                                           const float *__restrict__ g, float *__restrict__ out) {
     __shared__ float tile[4][kTrCells][65];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -266,10 +267,10 @@ __global__ __launch_bounds__(256) void bwd_compact_kernel(const int32_t *__restr
     const int32_t *rec = posts + (size_t)(row / kBlk) * kPostRec + row % kBlk;
     const int id = rec[0];
     if (id < 0) return;   // (wavefronts share nothing)
-    const int base = rec[kBlk], i = id - base, n = len[base / N1];
-    const float *src = g + ((int64_t)id * N1) * L + l0;
+    const int n = rec[kBlk];   // cells of the row
+    const float *src = g + square_cells[row] * L + l0;
     const int64_t at = post_cells[row];
-    for (int j0 = i + 1; j0 <= n; j0 += kTrCells) {
+    for (int j0 = 1; j0 <= n; j0 += kTrCells) {
         const int m = min(kTrCells, n + 1 - j0);
         for (int c = 0; c < m; ++c)
             if (l0 + lane < L) tile[wave][c][lane] = src[(int64_t)(j0 + c) * L + lane];
@@ -285,7 +286,7 @@ __global__ __launch_bounds__(256) void bwd_compact_kernel(const int32_t *__restr
 struct BwdArgs {
     const int32_t *posts;
     const int64_t *post_cells;
-    int n_posts, N1, d, L, per_group;   // per_group: labels of a group
+    int n_posts, d, L, per_group;   // per_group: labels of a group
     Rows rl, rr;
     const uint16_t *wf;                 // bwd_weights_kernel's fragments
     const float *g;
@@ -349,12 +350,12 @@ __device__ __forceinline__ void bwd_rows(const BwdArgs &a, char *smem) {
     // A block's partners: side 0 itself and those after it, side 1 those before it and itself.
     auto first_of = [&](int blk) { return SIDE == 0 ? blk : constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk); };
     auto last_of = [&](int blk) { return SIDE == 0 ? constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk + 1) : blk; };
-    auto grad_of = [&](int l) { return Grad{a.g + (COMPACT ? l * a.cells : 0), a.post_cells, a.N1}; };
+    auto grad_of = [&](int l) { return Grad{a.g + (COMPACT ? l * a.cells : 0), a.post_cells}; };
 
     Staged<DP, Q8> sr;
     Staged_grad sg;
     auto load_step = [&](int l, int blk, int q, bool with_r) {
-        sg.load<COMPACT>(grad_of(l), a.posts, SIDE == 0 ? blk : q, SIDE == 0 ? q : blk);
+        sg.load(grad_of(l), a.posts, SIDE == 0 ? blk : q, SIDE == 0 ? q : blk);
         if (with_r) sr.load(rows, a.posts + (size_t)q * kPostRec, 0, a.d);
     };
     // R stays in LDS from one label to the next where blocks have one partner
@@ -380,7 +381,7 @@ __device__ __forceinline__ void bwd_rows(const BwdArgs &a, char *smem) {
                 uint16_t *Rh = R + h * kBlk * PS;
                 for (int q = first_of(blk); q <= q1; ++q) {
                     __syncthreads();   // the readers of what is stored next are done
-                    if (!(l > x.l0 && keeps_r(blk))) sr.template store<ONE>(0, a.d, Rh, PS);
+                    if (!(l > x.l0 && keeps_r(blk))) sr.template store<ONE>(rows, 0, a.d, Rh, PS);
                     sg.store(Gh, Gl);
                     // the next step: the next partner, block, label or item
                     if (q < q1) load_step(l, blk, q + 1, true);
@@ -435,12 +436,17 @@ __device__ __forceinline__ void bwd_rows(const BwdArgs &a, char *smem) {
                 const int kn = min(ks + 1, ksteps - 1);
 #pragma unroll
                 for (int c = 0; c < CB; ++c) then[c] = frag(wf + ((size_t)kn * (DP / 16) + c) * 512);
+                bf16x8 pv = frag(prow + 32 * ks);
+                __builtin_amdgcn_sched_barrier(0);   // (left alone, they are issued where they are waited for)
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
-                    const bf16x8 pv = frag(prow + 16 * r * PS + 32 * ks);
+                    bf16x8 pn = pv;
+                    if (r + 1 < RB) pn = frag(prow + 16 * (r + 1) * PS + 32 * ks);
 #pragma unroll
                     for (int c = 0; c < CB; ++c) acc[c][r] = mfma(now[c], pv, acc[c][r]);
+                    pv = pn;
                 }
+                __builtin_amdgcn_sched_barrier(0);
             };
             int ks = 0;
             for (; ks + 1 < ksteps; ks += 2) {
@@ -453,10 +459,16 @@ __device__ __forceinline__ void bwd_rows(const BwdArgs &a, char *smem) {
 
         // acc[c][r]: columns 16 (col0 + c) + 4 lg .. +3 of post 16 (wr RB + r) + lr
         const int col0 = (x.cz * WC + wc) * CB;
+        int ids[RB];   // (all before the first store, which a later load would wait for)
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-            const int slot = 16 * (wr * RB + r) + lr, blk = H * x.unit + slot / kBlk;
-            const int id = a.posts[(size_t)blk * kPostRec + slot % kBlk];
+            const int slot = 16 * (wr * RB + r) + lr;
+            ids[r] = a.posts[(size_t)(H * x.unit + slot / kBlk) * kPostRec + slot % kBlk];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int slot = 16 * (wr * RB + r) + lr, id = ids[r];
 #pragma unroll
             for (int c = 0; c < CB; ++c) {
                 const int col = 16 * (col0 + c) + 4 * lg;
@@ -505,7 +517,7 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 struct WeightArgs {
     const int32_t *posts;
     const int64_t *post_cells;
-    int n_posts, N1, d, ldw, splits, tiles_a;
+    int n_posts, d, ldw, splits, tiles_a;
     Rows rl, rr;
     const float *g;
     int64_t cells;
@@ -528,7 +540,7 @@ __global__ __launch_bounds__(kThreads) void bwd_weight_kernel(WeightArgs a) {
     const int a0 = S::kT * ((int)blockIdx.x % a.tiles_a), c0 = S::kT * ((int)blockIdx.x / a.tiles_a);
     const int l = blockIdx.y, split = blockIdx.z;
     const int b0 = (int)((int64_t)a.n_posts * split / a.splits), b1 = (int)((int64_t)a.n_posts * (split + 1) / a.splits);
-    const Grad g{a.g + (COMPACT ? l * a.cells : 0), a.post_cells, a.N1};
+    const Grad g{a.g + (COMPACT ? l * a.cells : 0), a.post_cells};
 
     f32x4 acc[AB][T];
 #pragma unroll
@@ -539,7 +551,7 @@ __global__ __launch_bounds__(kThreads) void bwd_weight_kernel(WeightArgs a) {
     Staged<S::kT, Q8> sa, sc;
     Staged_grad sg;
     auto load_step = [&](int blk, int q) {
-        sg.load<COMPACT>(g, a.posts, blk, q);
+        sg.load(g, a.posts, blk, q);
         sc.load(a.rr, a.posts + (size_t)q * kPostRec, c0, a.d);
         if (q == blk) sa.load(a.rl, a.posts + (size_t)blk * kPostRec, a0, a.d);
     };
@@ -553,8 +565,8 @@ __global__ __launch_bounds__(kThreads) void bwd_weight_kernel(WeightArgs a) {
             for (int c = 0; c < T; ++c) u[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int q = blk; q <= last; ++q) {
             __syncthreads();
-            if (q == blk) sa.template store<true>(a0, a.d, Ra, TS);
-            sc.template store<false>(c0, a.d, Rc, TS);
+            if (q == blk) sa.template store<true>(a.rl, a0, a.d, Ra, TS);
+            sc.template store<false>(a.rr, c0, a.d, Rc, TS);
             sg.store(Gh, Gl);
             if (q < last) load_step(blk, q + 1);
             else if (blk + 1 < b1) load_step(blk + 1, blk + 1);
@@ -742,10 +754,14 @@ hipError_t launch_biaffine_bwd(const KernelPlan &p, int64_t cells, const void *r
     uint16_t *wf = reinterpret_cast<uint16_t *>(ws + b.w_at);
     hipError_t e;
     const float *g = grad;
+    const int last = p.B * p.n1 - (d < 8 ? 2 : 1);
+    const Rows rl_rows{rl, rl_scales, last}, rr_rows{rr, rr_scales, last};
+    // (post_cells: the square array's cells, then the compact one's)
+    const int64_t *cell_at = p.post_cells + (L > 1 ? (int64_t)p.n_posts * kBlk : 0);
     if (L > 1) {
         float *gt = reinterpret_cast<float *>(ws + b.g_at);
         hipLaunchKernelGGL(bwd_compact_kernel, dim3(p.n_posts * (kBlk / 4), (L + 63) / 64), dim3(256), 0, stream, p.posts,
-                           p.post_cells, p.len, p.n1, L, cells, grad, gt);
+                           cell_at, p.post_cells, L, cells, grad, gt);
         if ((e = hipGetLastError()) != hipSuccess) return e;
         g = gt;
     }
@@ -756,7 +772,7 @@ hipError_t launch_biaffine_bwd(const KernelPlan &p, int64_t cells, const void *r
         if ((e = hipGetLastError()) != hipSuccess) return e;
         const int side0 = grad_rl != nullptr ? 0 : 1, sides = (grad_rl != nullptr) + (grad_rr != nullptr);
         float *part = b.groups > 1 ? reinterpret_cast<float *>(ws + b.part_at) : nullptr;
-        const BwdArgs a{p.posts, p.post_cells, p.n_posts, p.n1, d, L, b.per_group, Rows{rl, rl_scales}, Rows{rr, rr_scales},
+        const BwdArgs a{p.posts, cell_at, p.n_posts, d, L, b.per_group, rl_rows, rr_rows,
                         wf, g, cells, {grad_rl, grad_rr}, part, b.zs, p.n_posts / b.h * b.zs * b.groups, side0};
         e = q8 ? (L > 1 ? launch_rows_of<true, true>(b, a, sides, stream) : launch_rows_of<true, false>(b, a, sides, stream))
                : (L > 1 ? launch_rows_of<false, true>(b, a, sides, stream) : launch_rows_of<false, false>(b, a, sides, stream));
@@ -770,8 +786,7 @@ hipError_t launch_biaffine_bwd(const KernelPlan &p, int64_t cells, const void *r
     }
     if (grad_w != nullptr) {
         float *part = reinterpret_cast<float *>(ws + b.wpart_at);
-        const WeightArgs a{p.posts, p.post_cells, p.n_posts, p.n1, d, ldw, b.splits, b.tiles_a, Rows{rl, rl_scales},
-                           Rows{rr, rr_scales}, g, cells, b.splits > 1 ? part : grad_w};
+        const WeightArgs a{p.posts, cell_at, p.n_posts, d, ldw, b.splits, b.tiles_a, rl_rows, rr_rows, g, cells, b.splits > 1 ? part : grad_w};
         e = q8 ? (L > 1 ? launch_weight<true, true>(b, a, L, stream) : launch_weight<true, false>(b, a, L, stream))
                : (L > 1 ? launch_weight<false, true>(b, a, L, stream) : launch_weight<false, false>(b, a, L, stream));
         if (e != hipSuccess) return e;

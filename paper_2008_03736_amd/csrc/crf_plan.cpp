@@ -501,7 +501,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     // rows), longer ones cut into blocks of fence posts with a tile per pair
     // of row block <= column block.
     std::vector<int32_t> bia, posts;
-    std::vector<int64_t> post_cells;
+    std::vector<int64_t> post_cells, compact_cells;
     {
         std::vector<std::vector<int32_t>> packed;
         std::vector<std::vector<int32_t>> by_free(crf::kBiaRows + 1);
@@ -551,14 +551,21 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
             const size_t at = posts.size();
             posts.resize(at + crf::kPostRec, -1);
             for (int r = 0; r < crf::kBiaRows; ++r) {
-                int64_t cell = 0;
+                // (a post without cells, n or an empty place: its sentence's
+                // or the first one's (0, 0), whose next cell exists)
+                int64_t square = 0, compact = -1;
+                posts[at + crf::kBiaRows + r] = 0;
                 if (r < count) {
-                    const int32_t b = ids[r] / n1, i = ids[r] - b * n1;
+                    const int32_t b = ids[r] / n1, n = lengths_host[b];
+                    int32_t i = ids[r] - b * n1;
                     posts[at + r] = ids[r];
-                    posts[at + crf::kBiaRows + r] = b * n1;
-                    cell = cell_off[b] + (int64_t)i * lengths_host[b] - 1;
+                    posts[at + crf::kBiaRows + r] = n - i;
+                    if (i == n) i = 0;
+                    square = (int64_t)b * n1 * n1 + (int64_t)i * n1 + i;
+                    compact = cell_off[b] + (int64_t)i * n - 1 + i;
                 }
-                post_cells.push_back(cell);
+                post_cells.push_back(square);
+                compact_cells.push_back(compact);
             }
             posts[at + 2 * crf::kBiaRows] = first;
             posts[at + 2 * crf::kBiaRows + 1] = last;
@@ -580,6 +587,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
         }
         const int blocks = (int)(posts.size() / crf::kPostRec);
         if (blocks % 2 != 0) put_block(nullptr, 0, blocks, blocks);   // an even number: some kernels take pairs
+        post_cells.insert(post_cells.end(), compact_cells.begin(), compact_cells.end());
     }
 
     std::vector<int32_t> len(lengths_host, lengths_host + batch);
