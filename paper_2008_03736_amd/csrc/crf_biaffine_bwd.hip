@@ -38,10 +38,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 512;                // 8 wavefronts, two per SIMD
 constexpr int kBlk = kBiaRows;               // fence posts of a block
 constexpr int kGS = kBlk + 8;                // row stride of the staged G (16-byte reads free of conflicts)
-constexpr int kPadCols = 8;                  // padding of a staged row of R, U or X
 
 __device__ __forceinline__ bf16x8 frag(const uint16_t *p) {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(p));
@@ -81,16 +79,17 @@ __device__ __forceinline__ T constant(const T *p) {
 // rows 418 us.)
 //
 // Columns k0 .. k0 + COLS of the rows of a block, to LDS with row stride
-// `stride`: wavefront w takes rows 8 w .. 8 w + 7, whose ids are then scalars,
-// kAtOnce of them side by side, a lane eight entries of each.
-template <int COLS, bool Q8>
+// `stride`: wavefront w of NW takes kRows rows from kRows w on, whose ids are
+// then scalars, kAtOnce of them side by side, a lane eight entries of each.
+template <int COLS, int NW, bool Q8>
 struct Staged {
+    static constexpr int kRows = kBlk / NW;
     static constexpr int kPieces = COLS / 8;                                  // of a row
     static constexpr int kAtOnce = kPieces <= 32 ? 64 / kPieces : 1;          // rows
-    static constexpr int kEach = 8 / kAtOnce;
+    static constexpr int kEach = kRows / kAtOnce;
     uint4 v[kEach];   // (Q8: codes in x and y, the scale in z)
-    int id[8];
-    static __device__ __forceinline__ int row(int u) {   // within the wavefront's eight
+    int id[kRows];
+    static __device__ __forceinline__ int row(int u) {   // within the wavefront's
         return kAtOnce * u + (kAtOnce > 1 ? (int)(threadIdx.x & 63) / kPieces : 0);
     }
     static __device__ __forceinline__ int col() {
@@ -113,7 +112,7 @@ struct Staged {
     __device__ __forceinline__ void load(const Rows &r, const int32_t *post, int k0, int d) {
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = k0 + col();
 #pragma unroll
-        for (int u = 0; u < 8; ++u) id[u] = constant(post + 8 * w + u);
+        for (int u = 0; u < kRows; ++u) id[u] = constant(post + kRows * w + u);
         if constexpr (Q8) {
             const int wide = row_codes(d), kc = min(k, wide - 8);
 #pragma unroll
@@ -159,10 +158,45 @@ struct Staged {
                 p.x = row_in && k == d ? 0x3F80u : p.x;
                 p.z = row_in && half ? 0x3F80u : p.z;
             }
-            *reinterpret_cast<uint4 *>(to + (8 * w + row(u)) * stride + col()) = p;
+            *reinterpret_cast<uint4 *>(to + (kRows * w + row(u)) * stride + col()) = p;
         }
     }
 };
+
+// The same rows of bf16 straight to LDS, four bytes a lane and load, nothing of
+// them in registers: entries [k0, k0 + COLS) that a row has.  What is to stand
+// past a row's end is put there once (set_ends); rows that do not exist are row
+// 0 (the products take them times 0).  Wait for the loads (loads_done) before
+// the barrier that lets others read.
+template <int COLS, int NW>
+__device__ __forceinline__ void rows_to_lds(const Rows &r, const int32_t *post, int k0, int d, uint16_t *to, int stride) {
+    constexpr int kRows = kBlk / NW;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int words = min(d - k0, COLS) / 2;
+    int id[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) id[u] = constant(post + kRows * w + u);
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+        const uint32_t *row = reinterpret_cast<const uint32_t *>(static_cast<const uint16_t *>(r.x) + (size_t)max(id[u], 0) * d + k0);
+        uint16_t *at = to + (kRows * w + u) * stride;
+#pragma unroll
+        for (int p = 0; p < COLS / 128; ++p)
+            if (64 * p + lane < words)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(row + 64 * p + lane),
+                                                 (__attribute__((address_space(3))) uint32_t *)(at + 128 * p), 4, 0, 0);
+    }
+}
+// Columns of `rows` staged rows that hold no entry: 1 at entry d if ONE, else 0.
+template <bool ONE>
+__device__ __forceinline__ void set_ends(uint16_t *to, int rows, int stride, int k0, int d) {
+    const int from = max(min(d - k0, stride), 0), wide = stride - from;
+    for (int t = threadIdx.x; t < rows * wide; t += blockDim.x) {
+        const int r = t / wide, c = from + t - r * wide;
+        to[r * stride + c] = ONE && k0 + c == d ? 0x3F80u : 0u;
+    }
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // A label's gradient and where each post's cell (i, i) would be in it: the
 // caller's [B][N1][N1], or the compact cells of the label
@@ -174,60 +208,70 @@ struct Grad {
 // G of rows i in block `bi` and columns j in block `bj`: the cells of one
 // sentence with i < j, zero elsewhere (other cells are not used).  Posts of a
 // sentence are neighbours, so row r's cells are its n - i next columns.
-// Wavefront w takes rows 8 w .. 8 w + 7, a lane a column, so that rows are read
-// along memory, what a row needs is scalar and a lane's eight rows are one
-// 16-byte store of G^T[j][i]; as bf16 hi and lo parts.
+// Wavefront w of NW takes kRows rows from kRows w on, a lane a column, so that
+// rows are read along memory, what a row needs is scalar and eight rows of a
+// lane are one 16-byte store of G^T[j][i]; as bf16 hi and lo parts.
+template <int NW>
 struct Staged_grad {
-    float v[8];
+    static constexpr int kRows = kBlk / NW;
+    float v[kRows];
     uint32_t in;
     __device__ __forceinline__ void load(const Grad &g, const int32_t *posts, int bi, int bj) {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int32_t *rest = posts + (size_t)bi * kPostRec + kBlk + 8 * w;
-        const int64_t *cell = g.cells + (size_t)bi * kBlk + 8 * w;
-        int n[8];
-        int64_t c[8];
+        const int32_t *rest = posts + (size_t)bi * kPostRec + kBlk + kRows * w;
+        const int64_t *cell = g.cells + (size_t)bi * kBlk + kRows * w;
+        int n[kRows];
+        int64_t c[kRows];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) n[u] = constant(rest + u);
+        for (int u = 0; u < kRows; ++u) n[u] = constant(rest + u);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) c[u] = constant(cell + u);
-        const int at = kBlk * (bj - bi) + lane - 8 * w;   // j - i of row 8 w
+        for (int u = 0; u < kRows; ++u) c[u] = constant(cell + u);
+        const int at = kBlk * (bj - bi) + lane - kRows * w - 1;   // j - i - 1 of row kRows w
         in = 0;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const bool ok = at - u > 0 && at - u <= n[u];
+        for (int u = 0; u < kRows; ++u) {
+            const bool ok = (uint32_t)(at - u) < (uint32_t)n[u];
             in |= ok ? 1u << u : 0u;
-            v[u] = (g.g + c[u])[ok ? at - u : 1];   // (cell (i, i+1), which exists)
+            v[u] = (g.g + c[u] + 1)[ok ? at - u : 0];   // (else cell (i, i+1), which exists)
         }
     }
+    // hi, lo: [64][kGS] each
     __device__ __forceinline__ void store(uint16_t *hi, uint16_t *lo) const {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        bf16x8 h, l;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const float x = in >> u & 1u ? v[u] : 0.f;
-            h[u] = (__bf16)x;
-            l[u] = (__bf16)(x - (float)h[u]);
+        for (int q = 0; q < kRows / 8; ++q) {
+            bf16x8 h, l;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float x = in >> (8 * q + u) & 1u ? v[8 * q + u] : 0.f;
+                h[u] = (__bf16)x;
+                l[u] = (__bf16)(x - (float)h[u]);
+            }
+            *reinterpret_cast<uint4 *>(hi + lane * kGS + kRows * w + 8 * q) = __builtin_bit_cast(uint4, h);
+            *reinterpret_cast<uint4 *>(lo + lane * kGS + kRows * w + 8 * q) = __builtin_bit_cast(uint4, l);
         }
-        *reinterpret_cast<uint4 *>(hi + lane * kGS + 8 * w) = __builtin_bit_cast(uint4, h);
-        *reinterpret_cast<uint4 *>(lo + lane * kGS + 8 * w) = __builtin_bit_cast(uint4, l);
     }
 };
-// Operands of the staged G^T, posts 16 r .. +15 by K offsets 32 ks .. +31: rows
-// j with K over i, or (ROWS_I) rows i with K over j.
+// Operands of the staged G^T with K numbered as a wavefront holds the other
+// operand after a product: a lane's eight are posts 32 p + 4 lg .. +3 and the
+// four that come 16 later.  Posts 16 r .. +15: rows j with K over i, or (ROWS_I)
+// rows i with K over j.
 template <bool ROWS_I>
-__device__ __forceinline__ bf16x8 grad_frag(const uint16_t *gt, int r, int ks, int lr, int lg) {
+__device__ __forceinline__ bf16x8 grad_frag(const uint16_t *gt, int r, int p, int lr, int lg) {
     if constexpr (ROWS_I) {
-        const uint16_t *p = gt + (32 * ks + 8 * lg + (lr >> 2)) * kGS + 16 * r + 4 * (lr & 3);
-        return frag_rows(p, p + 4 * kGS);
+        const uint16_t *q = gt + (32 * p + 4 * lg + (lr >> 2)) * kGS + 16 * r + 4 * (lr & 3);
+        return frag_rows(q, q + 16 * kGS);
     } else {
-        return frag(gt + (16 * r + lr) * kGS + 32 * ks + 8 * lg);
+        const uint16_t *q = gt + (16 * r + lr) * kGS + 32 * p + 4 * lg;
+        const uint2 x = *reinterpret_cast<const uint2 *>(q), y = *reinterpret_cast<const uint2 *>(q + 16);
+        return __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
     }
 }
 // Whether that part of a block's product with itself can be other than zero
 // (i < j).
 template <bool ROWS_I>
-__device__ __forceinline__ constexpr bool grad_part(int r, int ks) {
-    return ROWS_I ? 32 * ks + 31 > 16 * r : 32 * ks < 16 * r + 15;
+__device__ __forceinline__ constexpr bool grad_part(int r, int p) {
+    return ROWS_I ? 32 * p + 31 > 16 * r : 32 * p < 16 * r + 15;
 }
 
 // W's fragments for the dense products, from W transposed as the scorer takes
@@ -286,7 +330,8 @@ __global__ __launch_bounds__(256) void bwd_compact_kernel(const int32_t *__restr
 struct BwdArgs {
     const int32_t *posts;
     const int64_t *post_cells;
-    int n_posts, d, L, per_group;   // per_group: labels of a group
+    int n_posts, blk0, blks;            // the batch's blocks, and those of this launch
+    int d, L, per_group;                // per_group: labels of a group
     Rows rl, rr;
     const uint16_t *wf;                 // bwd_weights_kernel's fragments
     const float *g;
@@ -296,189 +341,214 @@ struct BwdArgs {
     int zs;                             // items that share blocks' output columns
     int items, side0;                   // items of a side; the first grid.y's side
 };
+// An item: H blocks from blk on, labels and column share.
+struct Item {
+    int blk, l0, l1, cz, grp;
+};
+template <int H>
+__device__ __forceinline__ Item item_of(const BwdArgs &a, int it) {
+    const int units = (a.blks + H - 1) / H, q = it / units;
+    Item x;
+    x.blk = a.blk0 + H * (it - q * units);
+    x.cz = q % a.zs;
+    x.grp = q / a.zs;
+    x.l0 = x.grp * a.per_group;
+    x.l1 = min(x.l0 + a.per_group, a.L);
+    return x;
+}
+__device__ __forceinline__ const uint16_t *weight_frags(const BwdArgs &a, int l, int side, int dp, int col0) {
+    return a.wf + ((((size_t)l * 2 + side) * (dp / 32)) * (dp / 16) + col0) * 512 + 8 * (threadIdx.x & 63);
+}
+// o[c][r]: columns 16 (col0 + c) + 4 lg .. +3 of post 16 r + lr of block blk.
+template <int CB, int SIDE>
+__device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB][4], int blk, int grp, int col0, int dp) {
+    const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+    int ids[4];   // (all before the first store, which a later load would wait for)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) ids[r] = a.posts[(size_t)blk * kPostRec + 16 * r + lr];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            const int col = 16 * (col0 + c) + 4 * lg;
+            if (ids[r] < 0 || col >= a.d) continue;
+            if (a.part != nullptr)
+                *reinterpret_cast<f32x4 *>(a.part + (((size_t)grp * 2 + SIDE) * a.n_posts * kBlk + kBlk * blk + 16 * r + lr) * dp + col) =
+                    o[c][r];
+            else
+                *reinterpret_cast<bf16x4 *>(a.out[SIDE] + (size_t)ids[r] * a.d + col) = __builtin_convertvector(o[c][r], bf16x4);
+        }
+}
 
-// dR^l (side 0) and dR^r (side 1) of H blocks of posts: for each label, the
-// blocks' U (or X) into LDS as bf16, 64 H x DP, then its product with W's
-// fragments, which come straight from L2 in the order of the lanes, each read
-// by the one row of wavefronts that needs its columns.  NB: 16-column blocks
-// of U per wavefront (DP = 128 NB); CB: output column blocks of a wavefront,
-// WR: rows of wavefronts.
-//
-// A workgroup goes through items (blocks, label group, column share) on its
-// own, and what the next step of staging needs (the rows of R and the cells of
-// G of one pair of blocks) is in flight in registers during this step's
-// products: with a workgroup an item and loads where they are needed, 5,000
-// sentences at d = 500 took 418 us, 200 of them waiting for R and G.
-template <int NB, int H>
-struct RowsShape {
-    static constexpr int kDP = 128 * NB, kPS = kDP + kPadCols;
-    // U beside R, or R where U will be (U's columns are in registers until
-    // every wavefront has read R)
-    static constexpr bool kApart = NB <= 2;
-    static constexpr int kLds = 2 * ((kApart ? 2 : 1) * H * kBlk * kPS + 2 * kBlk * kGS);
+// dR^l (side 0) and dR^r (side 1) of blocks that hold whole sentences, as
+// G (R^r W^T) and G^T ([R^l ; 1] W): V = R W first, whose K runs along rows, so
+// that R goes to LDS as it lies in memory (no instruction of a wavefront
+// touches it) and W's fragments come straight from L2 in the order of the
+// lanes.  A wavefront holds V of its 16 CB columns for all posts of H blocks,
+// which is the layout of the second product's operand when K is numbered as in
+// grad_frag: V, rounded to bf16, never leaves the registers.  (As (G R) W^T,
+// whose inner product goes through LDS, 5,000 sentences at d = 500 took 252 us,
+// 75 of them in the dense product, the rest in staging that both products wait
+// for.)  R of the next item is on its way from the end of the dense product on.
+// DP = 128 NB columns, 16 NW CB of them a workgroup.
+template <int NB, int NW, int H, bool COMPACT>
+struct PostsShape {
+    static constexpr int kDP = 128 * NB, kRS = kDP + 8, kGrads = COMPACT ? 2 : 1;
+    static constexpr int kLds = 2 * (H * kBlk * kRS + kGrads * 2 * kBlk * kGS);
 };
 
-template <int NB, int H, int CB, int WR, bool Q8, bool COMPACT, int SIDE>
-__device__ __forceinline__ void bwd_rows(const BwdArgs &a, char *smem) {
-    typedef RowsShape<NB, H> S;
-    constexpr int DP = S::kDP, PS = S::kPS, WC = 8 / WR, RB = 4 * H / WR;
+template <int NB, int NW, int H, int CB, bool Q8, bool COMPACT, int SIDE>
+__device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
+    typedef PostsShape<NB, NW, H, COMPACT> S;
+    static_assert(!COMPACT || H == 1, "sums over labels: a block at a time");
+    constexpr int DP = S::kDP, RS = S::kRS;
     constexpr bool ONE = SIDE == 1, ROWS_I = SIDE == 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 15, lg = lane >> 4;
-    uint16_t *P = reinterpret_cast<uint16_t *>(smem);                  // [64 H][PS]: U or X
-    uint16_t *R = S::kApart ? P + H * kBlk * PS : P;                   // [64 H][PS]: the partners' rows
-    uint16_t *Gh = R + H * kBlk * PS, *Gl = Gh + kBlk * kGS;
-    const int units = a.n_posts / H;
-    const int wr = wave / WC, wc = wave % WC;
+    uint16_t *R = reinterpret_cast<uint16_t *>(smem);   // [64 H][RS]
+    uint16_t *G = R + H * kBlk * RS;                    // [kGrads][2][64][kGS]: G^T, hi and lo
     const int ksteps = (a.d + 32) / 32;   // K of the dense product: d + 1 at most
     const Rows rows = SIDE == 0 ? a.rr : a.rl;
+    const int last_blk = a.blk0 + a.blks - 1;   // (an item's second block past it is it again, and not stored)
 
-    // An item: its blocks, labels and column share.
-    struct Item {
-        int unit, l0, l1, cz, grp;
+    auto stage_r = [&](int blk) {
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            const int32_t *post = a.posts + (size_t)min(blk + h, last_blk) * kPostRec;
+            if constexpr (Q8) {
+                Staged<DP, NW, true> sr;
+                sr.load(rows, post, 0, a.d);
+                sr.template store<ONE>(rows, 0, a.d, R + h * kBlk * RS, RS);
+            } else {
+                rows_to_lds<DP, NW>(rows, post, 0, a.d, R + h * kBlk * RS, RS);
+            }
+        }
     };
-    auto item_of = [&](int it) {
-        Item x;
-        x.unit = it % units;
-        const int q = it / units;
-        x.cz = q % a.zs;
-        x.grp = q / a.zs;
-        x.l0 = x.grp * a.per_group;
-        x.l1 = min(x.l0 + a.per_group, a.L);
-        return x;
+    Staged_grad<NW> sg[H];
+    auto load_grad = [&](int h, int blk, int l) {
+        const int b = min(blk + h, last_blk);
+        sg[h].load(Grad{a.g + (COMPACT ? l * a.cells : 0), a.post_cells}, a.posts, b, b);
     };
-    // A block's partners: side 0 itself and those after it, side 1 those before it and itself.
-    auto first_of = [&](int blk) { return SIDE == 0 ? blk : constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk); };
-    auto last_of = [&](int blk) { return SIDE == 0 ? constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk + 1) : blk; };
-    auto grad_of = [&](int l) { return Grad{a.g + (COMPACT ? l * a.cells : 0), a.post_cells}; };
-
-    Staged<DP, Q8> sr;
-    Staged_grad sg;
-    auto load_step = [&](int l, int blk, int q, bool with_r) {
-        sg.load(grad_of(l), a.posts, SIDE == 0 ? blk : q, SIDE == 0 ? q : blk);
-        if (with_r) sr.load(rows, a.posts + (size_t)q * kPostRec, 0, a.d);
+    f32x4 v[4 * H][CB];
+    // V = R W_l
+    auto dense = [&](int l, int col0) {
+        const uint16_t *wf = weight_frags(a, l, SIDE, DP, col0);
+        const uint16_t *p = R + lr * RS + 8 * lg;
+        bf16x8 wv[2][CB];   // two steps of W
+#pragma unroll
+        for (int c = 0; c < CB; ++c) wv[0][c] = frag(wf + (size_t)c * 512);
+#pragma unroll
+        for (int r = 0; r < 4 * H; ++r)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) v[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto step = [&](int ks, bf16x8 (&now)[CB], bf16x8 (&then)[CB]) {
+            const int kn = min(ks + 1, ksteps - 1);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) then[c] = frag(wf + ((size_t)kn * (DP / 16) + c) * 512);
+            bf16x8 pv = frag(p + 32 * ks);
+            __builtin_amdgcn_sched_barrier(0);   // (left alone, they are issued where they are waited for)
+#pragma unroll
+            for (int r = 0; r < 4 * H; ++r) {
+                bf16x8 pn = pv;
+                if (r + 1 < 4 * H) pn = frag(p + 16 * (r + 1) * RS + 32 * ks);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) v[r][c] = mfma(pv, now[c], v[r][c]);
+                pv = pn;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int ks = 0;
+        for (; ks + 1 < ksteps; ks += 2) {
+            step(ks, wv[0], wv[1]);
+            step(ks + 1, wv[1], wv[0]);
+        }
+        if (ks < ksteps) step(ks, wv[0], wv[1]);
     };
-    // R stays in LDS from one label to the next where blocks have one partner
-    auto keeps_r = [&](int blk) { return S::kApart && first_of(blk) == last_of(blk); };
+    // o += V^T G of block h
+    auto second = [&](int h, const uint16_t *g, f32x4 (&o)[CB][4]) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            bf16x8 vb[CB];
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int t = 0; t < 8; ++t) vb[c][t] = (__bf16)v[4 * h + 2 * p + (t >> 2)][c][t & 3];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (grad_part<ROWS_I>(r, p)) {
+                    const bf16x8 gh = grad_frag<ROWS_I>(g, r, p, lr, lg), gl = grad_frag<ROWS_I>(g + kBlk * kGS, r, p, lr, lg);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) o[c][r] = mfma(vb[c], gh, o[c][r]);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) o[c][r] = mfma(vb[c], gl, o[c][r]);
+                }
+        }
+    };
+    auto clear = [](f32x4 (&o)[CB][4]) {
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
 
     int it = blockIdx.x;
     if (it >= a.items) return;
-    Item x = item_of(it);
-    load_step(x.l0, H * x.unit, first_of(H * x.unit), true);
+    if constexpr (!Q8) {
+        set_ends<ONE>(R, H * kBlk, RS, 0, a.d);
+        __syncthreads();
+    }
+    Item x = item_of<H>(a, it);
+    stage_r(x.blk);
+#pragma unroll
+    for (int h = 0; h < H; ++h) load_grad(h, x.blk, x.l0);
     for (;;) {
         const int next_it = it + gridDim.x;
-        const Item nx = item_of(min(next_it, a.items - 1));
-        f32x4 acc[CB][RB];
-        for (int l = x.l0;;) {   // (one label, l = 0, unless COMPACT)
-#pragma unroll 1
-            for (int h = 0; h < H; ++h) {
-                const int blk = H * x.unit + h, q1 = last_of(blk);
-                f32x4 u[NB][4];
-#pragma unroll
-                for (int c = 0; c < NB; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) u[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-                uint16_t *Rh = R + h * kBlk * PS;
-                for (int q = first_of(blk); q <= q1; ++q) {
-                    __syncthreads();   // the readers of what is stored next are done
-                    if (!(l > x.l0 && keeps_r(blk))) sr.template store<ONE>(rows, 0, a.d, Rh, PS);
-                    sg.store(Gh, Gl);
-                    // the next step: the next partner, block, label or item
-                    if (q < q1) load_step(l, blk, q + 1, true);
-                    else if (h + 1 < H) load_step(l, blk + 1, first_of(blk + 1), !(l > x.l0 && keeps_r(blk + 1)));
-                    else if (COMPACT && l + 1 < x.l1) load_step(l + 1, H * x.unit, first_of(H * x.unit), !keeps_r(H * x.unit));
-                    else if (next_it < a.items) load_step(nx.l0, H * nx.unit, first_of(H * nx.unit), true);
-                    __syncthreads();
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks) {
-                        bf16x8 gh[4], gl[4];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            gh[r] = grad_frag<ROWS_I>(Gh, r, ks, lr, lg);
-                            gl[r] = grad_frag<ROWS_I>(Gl, r, ks, lr, lg);
-                        }
-#pragma unroll
-                        for (int c = 0; c < NB; ++c) {
-                            const uint16_t *p = Rh + (32 * ks + 8 * lg + (lr >> 2)) * PS + 16 * (wave * NB + c) + 4 * (lr & 3);
-                            const bf16x8 rf = frag_rows(p, p + 4 * PS);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (grad_part<ROWS_I>(r, ks) || q != blk) {
-                                    u[c][r] = mfma(rf, gh[r], u[c][r]);
-                                    u[c][r] = mfma(rf, gl[r], u[c][r]);
-                                }
-                        }
-                    }
-                }
-                if constexpr (!S::kApart) __syncthreads();   // R's readers are done
-                // u[c][r]: columns 16 (wave NB + c) + 4 lg .. +3 of post 16 r + lr
-#pragma unroll
-                for (int c = 0; c < NB; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        *reinterpret_cast<bf16x4 *>(P + (h * kBlk + 16 * r + lr) * PS + 16 * (wave * NB + c) + 4 * lg) =
-                            __builtin_convertvector(u[c][r], bf16x4);
-            }
+        const Item nx = item_of<H>(a, min(next_it, a.items - 1));
+        const int col0 = (x.cz * NW + wave) * CB;   // the wavefront's first column block
+        f32x4 o[CB][4];
+        if constexpr (COMPACT) {
+            clear(o);
+            sg[0].store(G, G + kBlk * kGS);
+            if (x.l0 + 1 < x.l1) load_grad(0, x.blk, x.l0 + 1);
+            loads_done();
             __syncthreads();
-
-            if (!COMPACT || l == x.l0)
-#pragma unroll
-                for (int c = 0; c < CB; ++c)
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const int col0 = (x.cz * WC + wc) * CB;   // the wavefront's first output column block
-            const uint16_t *wf = a.wf + ((((size_t)l * 2 + SIDE) * (DP / 32)) * (DP / 16) + col0) * 512 + 8 * lane;
-            const uint16_t *prow = P + (wr * RB * 16 + lr) * PS + 8 * lg;
-            bf16x8 wv[2][CB];   // two steps of W
-#pragma unroll
-            for (int c = 0; c < CB; ++c) wv[0][c] = frag(wf + (size_t)c * 512);
-            auto dense_step = [&](int ks, bf16x8 (&now)[CB], bf16x8 (&then)[CB]) {
-                const int kn = min(ks + 1, ksteps - 1);
-#pragma unroll
-                for (int c = 0; c < CB; ++c) then[c] = frag(wf + ((size_t)kn * (DP / 16) + c) * 512);
-                bf16x8 pv = frag(prow + 32 * ks);
-                __builtin_amdgcn_sched_barrier(0);   // (left alone, they are issued where they are waited for)
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    bf16x8 pn = pv;
-                    if (r + 1 < RB) pn = frag(prow + 16 * (r + 1) * PS + 32 * ks);
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) acc[c][r] = mfma(now[c], pv, acc[c][r]);
-                    pv = pn;
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            };
-            int ks = 0;
-            for (; ks + 1 < ksteps; ks += 2) {
-                dense_step(ks, wv[0], wv[1]);
-                dense_step(ks + 1, wv[1], wv[0]);
+            for (int l = x.l0; l < x.l1; ++l) {
+                uint16_t *now = G + ((l - x.l0) & 1) * 2 * kBlk * kGS, *then = G + ((l - x.l0 + 1) & 1) * 2 * kBlk * kGS;
+                if (l + 1 < x.l1) sg[0].store(then, then + kBlk * kGS);   // (its readers are a barrier behind)
+                if (l + 2 < x.l1) load_grad(0, x.blk, l + 2);
+                else if (l + 1 >= x.l1 && next_it < a.items) load_grad(0, nx.blk, nx.l0);
+                dense(l, col0);
+                second(0, now, o);
+                __syncthreads();
             }
-            if (ks < ksteps) dense_step(ks, wv[0], wv[1]);
-            if (!COMPACT || ++l >= x.l1) break;
-        }
-
-        // acc[c][r]: columns 16 (col0 + c) + 4 lg .. +3 of post 16 (wr RB + r) + lr
-        const int col0 = (x.cz * WC + wc) * CB;
-        int ids[RB];   // (all before the first store, which a later load would wait for)
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const int slot = 16 * (wr * RB + r) + lr;
-            ids[r] = a.posts[(size_t)(H * x.unit + slot / kBlk) * kPostRec + slot % kBlk];
-        }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const int slot = 16 * (wr * RB + r) + lr, id = ids[r];
-#pragma unroll
-            for (int c = 0; c < CB; ++c) {
-                const int col = 16 * (col0 + c) + 4 * lg;
-                if (id < 0 || col >= a.d) continue;
-                if (a.part != nullptr)
-                    *reinterpret_cast<f32x4 *>(a.part + (((size_t)x.grp * 2 + SIDE) * a.n_posts * kBlk + H * kBlk * x.unit + slot) * DP + col) =
-                        acc[c][r];
-                else
-                    *reinterpret_cast<bf16x4 *>(a.out[SIDE] + (size_t)id * a.d + col) = __builtin_convertvector(acc[c][r], bf16x4);
+            if (next_it < a.items) stage_r(nx.blk);
+            store_rows<CB, SIDE>(a, o, x.blk, x.grp, col0, DP);
+        } else {
+            sg[0].store(G, G + kBlk * kGS);
+            loads_done();
+            __syncthreads();
+            dense(0, col0);
+            __syncthreads();   // R's readers are done
+            if (next_it < a.items) stage_r(nx.blk);
+            clear(o);
+            second(0, G, o);
+            if constexpr (H == 2) {
+                store_rows<CB, SIDE>(a, o, x.blk, x.grp, col0, DP);
+                __syncthreads();
+                sg[H - 1].store(G, G + kBlk * kGS);
+                __syncthreads();
             }
+            if (next_it < a.items)
+#pragma unroll
+                for (int h = 0; h < H; ++h) load_grad(h, nx.blk, 0);
+            if constexpr (H == 2) {
+                clear(o);
+                second(H - 1, G, o);
+                if (x.blk + 1 <= last_blk) store_rows<CB, SIDE>(a, o, x.blk + 1, x.grp, col0, DP);
+            } else {
+                store_rows<CB, SIDE>(a, o, x.blk, x.grp, col0, DP);
+            }
+            __syncthreads();   // G's readers are done
         }
         if (next_it >= a.items) break;
         it = next_it;
@@ -486,11 +556,123 @@ __device__ __forceinline__ void bwd_rows(const BwdArgs &a, char *smem) {
     }
 }
 
-template <int NB, int H, int CB, int WR, bool Q8, bool COMPACT>
-__global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdArgs a) {
+template <int NB, int NW, int H, int CB, bool Q8, bool COMPACT>
+__global__ __launch_bounds__(64 * NW) void bwd_posts_kernel(BwdArgs a) {
     extern __shared__ __align__(16) char smem[];
-    if (blockIdx.y + a.side0 == 0) bwd_rows<NB, H, CB, WR, Q8, COMPACT, 0>(a, smem);
-    else bwd_rows<NB, H, CB, WR, Q8, COMPACT, 1>(a, smem);
+    if (blockIdx.y + a.side0 == 0) bwd_posts<NB, NW, H, CB, Q8, COMPACT, 0>(a, smem);
+    else bwd_posts<NB, NW, H, CB, Q8, COMPACT, 1>(a, smem);
+}
+
+// The same of blocks of a sentence that has more than one, as (G R^r) W^T and
+// (G^T [R^l ; 1]) W: a block of posts meets every block on its side of the
+// diagonal, and only the product with G is repeated for them, not the dense
+// one.  U = G R (or X) goes into LDS as bf16, where R was (its columns are in
+// registers until every wavefront has read R), 64 x DP; R and G of the next
+// block are in flight in registers during this one's products.  CB: 16-column
+// blocks of the output a wavefront.
+constexpr int kLongWaves = 8;
+template <int NB>
+struct LongShape {
+    static constexpr int kDP = 128 * NB, kPS = kDP + 8;
+    static constexpr int kLds = 2 * (kBlk * kPS + 2 * kBlk * kGS);
+};
+
+template <int NB, int CB, bool Q8, bool COMPACT, int SIDE>
+__device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
+    typedef LongShape<NB> S;
+    constexpr int DP = S::kDP, PS = S::kPS;
+    constexpr bool ONE = SIDE == 1, ROWS_I = SIDE == 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lr = lane & 15, lg = lane >> 4;
+    uint16_t *P = reinterpret_cast<uint16_t *>(smem);       // [64][PS]: R, then U or X
+    uint16_t *Gh = P + kBlk * PS, *Gl = Gh + kBlk * kGS;
+    const int ksteps = (a.d + 32) / 32;
+    const Rows rows = SIDE == 0 ? a.rr : a.rl;
+
+    // A block's partners: side 0 itself and those after it, side 1 those before it and itself.
+    auto first_of = [&](int blk) { return SIDE == 0 ? blk : constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk); };
+    auto last_of = [&](int blk) { return SIDE == 0 ? constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk + 1) : blk; };
+    Staged<DP, kLongWaves, Q8> sr;
+    Staged_grad<kLongWaves> sg;
+    auto load_step = [&](int l, int blk, int q) {
+        sg.load(Grad{a.g + (COMPACT ? l * a.cells : 0), a.post_cells}, a.posts, SIDE == 0 ? blk : q, SIDE == 0 ? q : blk);
+        sr.load(rows, a.posts + (size_t)q * kPostRec, 0, a.d);
+    };
+
+    const int it = blockIdx.x;
+    if (it >= a.items) return;
+    const Item x = item_of<1>(a, it);
+    const int q0 = first_of(x.blk), q1 = last_of(x.blk), col0 = (x.cz * kLongWaves + wave) * CB;
+    load_step(x.l0, x.blk, q0);
+    f32x4 acc[CB][4];
+    for (int l = x.l0;;) {   // (one label, l = 0, unless COMPACT)
+        f32x4 u[NB][4];
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) u[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int q = q0; q <= q1; ++q) {
+            __syncthreads();   // the readers of what is stored next are done
+            sr.template store<ONE>(rows, 0, a.d, P, PS);
+            sg.store(Gh, Gl);
+            if (q < q1) load_step(l, x.blk, q + 1);
+            else if (COMPACT && l + 1 < x.l1) load_step(l + 1, x.blk, q0);
+            __syncthreads();
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                bf16x8 rf[NB];
+                const uint16_t *at = P + (32 * p + 4 * lg + (lr >> 2)) * PS + 16 * wave * NB + 4 * (lr & 3);
+#pragma unroll
+                for (int c = 0; c < NB; ++c) rf[c] = frag_rows(at + 16 * c, at + 16 * PS + 16 * c);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (grad_part<ROWS_I>(r, p) || q != x.blk) {
+                        const bf16x8 gh = grad_frag<ROWS_I>(Gh, r, p, lr, lg), gl = grad_frag<ROWS_I>(Gl, r, p, lr, lg);
+#pragma unroll
+                        for (int c = 0; c < NB; ++c) {
+                            u[c][r] = mfma(rf[c], gh, u[c][r]);
+                            u[c][r] = mfma(rf[c], gl, u[c][r]);
+                        }
+                    }
+            }
+        }
+        __syncthreads();   // R's readers are done
+        // u[c][r]: columns 16 (wave NB + c) + 4 lg .. +3 of post 16 r + lr
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *reinterpret_cast<bf16x4 *>(P + (16 * r + lr) * PS + 16 * (wave * NB + c) + 4 * lg) =
+                    __builtin_convertvector(u[c][r], bf16x4);
+        __syncthreads();
+
+        if (!COMPACT || l == x.l0)
+#pragma unroll
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const uint16_t *wf = weight_frags(a, l, SIDE, DP, col0), *prow = P + lr * PS + 8 * lg;
+        for (int ks = 0; ks < ksteps; ++ks) {
+            bf16x8 wv[CB];
+#pragma unroll
+            for (int c = 0; c < CB; ++c) wv[c] = frag(wf + ((size_t)ks * (DP / 16) + c) * 512);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bf16x8 pv = frag(prow + 16 * r * PS + 32 * ks);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) acc[c][r] = mfma(wv[c], pv, acc[c][r]);
+            }
+        }
+        if (!COMPACT || ++l >= x.l1) break;
+    }
+    store_rows<CB, SIDE>(a, acc, x.blk, x.grp, col0, DP);
+}
+
+template <int NB, int CB, bool Q8, bool COMPACT>
+__global__ __launch_bounds__(64 * kLongWaves) void bwd_long_kernel(BwdArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    if (blockIdx.y + a.side0 == 0) bwd_long<NB, CB, Q8, COMPACT, 0>(a, smem);
+    else bwd_long<NB, CB, Q8, COMPACT, 1>(a, smem);
 }
 
 // The label groups' partial sums of dR^l and dR^r, added in their order: a
@@ -510,35 +692,47 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
     *reinterpret_cast<bf16x4 *>((side ? out_r : out_l) + (size_t)id * d + col) = __builtin_convertvector(s, bf16x4);
 }
 
-// dW of one label, a tile of 128 T columns a by 128 T rows c, over a share of
-// the blocks of posts: a wavefront holds U of its 16 T columns c in registers,
-// whose layout is that of the second product's operand when K is numbered so
-// that a lane's eight posts are 4 lg .. +3 of two 16-post blocks.
+// dW of one label, a tile of 16 AB columns a by 16 T NW rows c, over a share of
+// the blocks of posts: a wavefront holds U = G R^r of its 16 T columns c in
+// registers, whose layout is that of the second product's operand when K is
+// numbered as in grad_frag, as hi and lo parts.  A step is a block and one of
+// its partners: U grows by their product, then R^r and G of the next step (and
+// [R^l ; 1] of the next block, into the other of its two places) start on their
+// way while [R^l ; 1]^T U of a block that has met all its partners is added.
+//
+// The tiles of a share read the same posts: they are neighbours on one XCD, so
+// that a post's rows come from HBM once.
 struct WeightArgs {
     const int32_t *posts;
     const int64_t *post_cells;
-    int n_posts, d, ldw, splits, tiles_a;
+    int n_posts, d, ldw, L, splits, tiles_a, tiles;
     Rows rl, rr;
     const float *g;
     int64_t cells;
     float *out;   // splits = 1: dW [L][d][ldw]; else partial sums [splits][L][d][d + 4]
 };
-template <int T>
+template <int AB, int T, int NW>
 struct WeightShape {
-    static constexpr int kT = 128 * T, kTS = kT + kPadCols;
-    static constexpr int kLds = 2 * (2 * kBlk * kTS + 2 * kBlk * kGS);
+    static constexpr int kA = 16 * AB, kC = 16 * T * NW, kAS = kA + 8, kCS = kC + 8;
+    static constexpr int kLds = 2 * kBlk * (2 * kAS + kCS + 2 * kGS);
 };
+constexpr int kXcds = 8;
 
-template <int T, bool Q8, bool COMPACT>
-__global__ __launch_bounds__(kThreads) void bwd_weight_kernel(WeightArgs a) {
+template <int AB, int T, int NW, bool Q8, bool COMPACT>
+__global__ __launch_bounds__(64 * NW) void bwd_weight_kernel(WeightArgs a) {
     extern __shared__ __align__(16) char smem[];
-    typedef WeightShape<T> S;
-    constexpr int TS = S::kTS, AB = 8 * T;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    typedef WeightShape<AB, T, NW> S;
+    constexpr int TA = S::kA, TC = S::kC, AS = S::kAS, CS = S::kCS;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 15, lg = lane >> 4;
-    uint16_t *Ra = reinterpret_cast<uint16_t *>(smem), *Rc = Ra + kBlk * TS, *Gh = Rc + kBlk * TS, *Gl = Gh + kBlk * kGS;
-    const int a0 = S::kT * ((int)blockIdx.x % a.tiles_a), c0 = S::kT * ((int)blockIdx.x / a.tiles_a);
-    const int l = blockIdx.y, split = blockIdx.z;
+    uint16_t *Ra = reinterpret_cast<uint16_t *>(smem), *Rc = Ra + 2 * kBlk * AS;
+    uint16_t *Gh = Rc + kBlk * CS, *Gl = Gh + kBlk * kGS;
+    // workgroup b runs on XCD b mod 8: a (share, label)'s tiles side by side there
+    const int per = kXcds * a.tiles, unit = (int)blockIdx.x / per * kXcds + (int)blockIdx.x % kXcds;
+    const int tile = (int)blockIdx.x % per / kXcds;
+    if (unit >= a.splits * a.L) return;
+    const int split = unit / a.L, l = unit - split * a.L;
+    const int a0 = TA * (tile % a.tiles_a), c0 = TC * (tile / a.tiles_a);
     const int b0 = (int)((int64_t)a.n_posts * split / a.splits), b1 = (int)((int64_t)a.n_posts * (split + 1) / a.splits);
     const Grad g{a.g + (COMPACT ? l * a.cells : 0), a.post_cells};
 
@@ -547,75 +741,125 @@ __global__ __launch_bounds__(kThreads) void bwd_weight_kernel(WeightArgs a) {
     for (int x = 0; x < AB; ++x)
 #pragma unroll
         for (int c = 0; c < T; ++c) acc[x][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    Staged<S::kT, Q8> sa, sc;
-    Staged_grad sg;
-    auto load_step = [&](int blk, int q) {
-        sg.load(g, a.posts, blk, q);
-        sc.load(a.rr, a.posts + (size_t)q * kPostRec, c0, a.d);
-        if (q == blk) sa.load(a.rl, a.posts + (size_t)blk * kPostRec, a0, a.d);
-    };
-    if (b0 < b1) load_step(b0, b0);
-    for (int blk = b0; blk < b1; ++blk) {
-        const int last = constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk + 1);
-        f32x4 u[4][T];
+    f32x4 u[4][T];
+    auto clear_u = [&]() {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int c = 0; c < T; ++c) u[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int q = blk; q <= last; ++q) {
-            __syncthreads();
-            if (q == blk) sa.template store<true>(a.rl, a0, a.d, Ra, TS);
-            sc.template store<false>(a.rr, c0, a.d, Rc, TS);
-            sg.store(Gh, Gl);
-            if (q < last) load_step(blk, q + 1);
-            else if (blk + 1 < b1) load_step(blk + 1, blk + 1);
-            __syncthreads();
+    };
+    clear_u();
+
+    auto last_of = [&](int blk) { return constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk + 1); };
+    // Rows of a step on their way (bf16), or in registers (codes) and then stored.
+    Staged<TA, NW, Q8> sa;
+    Staged<TC, NW, Q8> sc;
+    Staged_grad<NW> sg;
+    auto post = [&](int blk) { return a.posts + (size_t)blk * kPostRec; };
+    auto fetch = [&](int blk, int q) {
+        sg.load(g, a.posts, blk, q);
+        if constexpr (Q8) {
+            sc.load(a.rr, post(q), c0, a.d);
+            if (q == blk) sa.load(a.rl, post(blk), a0, a.d);
+        }
+    };
+    auto stage = [&](int blk, int q) {
+        uint16_t *ra = Ra + (blk & 1) * kBlk * AS;
+        if constexpr (Q8) {
+            sc.template store<false>(a.rr, c0, a.d, Rc, CS);
+            if (q == blk) sa.template store<true>(a.rl, a0, a.d, ra, AS);
+        } else {
+            rows_to_lds<TC, NW>(a.rr, post(q), c0, a.d, Rc, CS);
+            if (q == blk) rows_to_lds<TA, NW>(a.rl, post(blk), a0, a.d, ra, AS);
+        }
+        sg.store(Gh, Gl);
+    };
+    if constexpr (!Q8) {
+        set_ends<true>(Ra, 2 * kBlk, AS, a0, a.d);
+        set_ends<false>(Rc, kBlk, CS, c0, a.d);
+        __syncthreads();
+    }
+    int blk = b0, q = b0, last = 0, nblk = b0, nq = b0;   // this step and the next
+    auto advance = [&]() {
+        if (nq < last) {
+            ++nq;
+        } else if (++nblk < b1) {
+            nq = nblk;
+            last = last_of(nblk);
+        }
+    };
+    if (b0 < b1) {
+        last = last_of(b0);
+        fetch(b0, b0);
+        stage(b0, b0);
+        advance();
+        if (nblk < b1) fetch(nblk, nq);
+        loads_done();
+        __syncthreads();
+    }
+    while (blk < b1) {
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
+        for (int p = 0; p < 2; ++p) {
+            const uint16_t *at = Rc + (32 * p + 4 * lg + (lr >> 2)) * CS + 16 * wave * T + 4 * (lr & 3);
+            bf16x8 rf[T];
 #pragma unroll
-                for (int c = 0; c < T; ++c) {
-                    const uint16_t *p = Rc + (32 * ks + 8 * lg + (lr >> 2)) * TS + 16 * (wave * T + c) + 4 * (lr & 3);
-                    const bf16x8 rf = frag_rows(p, p + 4 * TS);
+            for (int c = 0; c < T; ++c) rf[c] = frag_rows(at + 16 * c, at + 16 * CS + 16 * c);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (grad_part<true>(r, ks) || q != blk) {
-                            u[r][c] = mfma(grad_frag<true>(Gh, r, ks, lr, lg), rf, u[r][c]);
-                            u[r][c] = mfma(grad_frag<true>(Gl, r, ks, lr, lg), rf, u[r][c]);
-                        }
+            for (int r = 0; r < 4; ++r)
+                if (grad_part<true>(r, p) || q != blk) {
+                    const bf16x8 gh = grad_frag<true>(Gh, r, p, lr, lg), gl = grad_frag<true>(Gl, r, p, lr, lg);
+#pragma unroll
+                    for (int c = 0; c < T; ++c) u[r][c] = mfma(gh, rf[c], u[r][c]);
+#pragma unroll
+                    for (int c = 0; c < T; ++c) u[r][c] = mfma(gl, rf[c], u[r][c]);
                 }
         }
+        __syncthreads();   // the readers of R^r and G are done
+        const bool whole = nblk != blk;   // the block has met all its partners
+        const int nb = nblk, nqq = nq;
+        if (nb < b1) {
+            stage(nb, nqq);
+            advance();
+            if (nblk < b1) fetch(nblk, nq);
+        }
+        if (whole) {
 #pragma unroll
-        for (int kp = 0; kp < 2; ++kp) {
-            bf16x8 hi[T], lo[T];
+            for (int kp = 0; kp < 2; ++kp) {
+                bf16x8 hi[T], lo[T];
 #pragma unroll
-            for (int c = 0; c < T; ++c)
+                for (int c = 0; c < T; ++c)
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const float v = u[2 * kp + e][c][t];
+                    for (int t = 0; t < 8; ++t) {
+                        const float v = u[2 * kp + (t >> 2)][c][t & 3];
                         const __bf16 h = (__bf16)v;
-                        hi[c][4 * e + t] = h;
-                        lo[c][4 * e + t] = (__bf16)(v - (float)h);
+                        hi[c][t] = h;
+                        lo[c][t] = (__bf16)(v - (float)h);
                     }
-            const uint16_t *p = Ra + (32 * kp + 4 * lg + (lr >> 2)) * TS + 4 * (lr & 3);
+                const uint16_t *p = Ra + (blk & 1) * kBlk * AS + (32 * kp + 4 * lg + (lr >> 2)) * AS + 4 * (lr & 3);
+                bf16x8 af = frag_rows(p, p + 16 * AS);
 #pragma unroll
-            for (int x = 0; x < AB; ++x) {
-                const bf16x8 rf = frag_rows(p + 16 * x, p + 16 * TS + 16 * x);
+                for (int x = 0; x < AB; ++x) {
+                    bf16x8 an = af;
+                    if (x + 1 < AB) an = frag_rows(p + 16 * (x + 1), p + 16 * AS + 16 * (x + 1));
 #pragma unroll
-                for (int c = 0; c < T; ++c) {
-                    acc[x][c] = mfma(rf, hi[c], acc[x][c]);
-                    acc[x][c] = mfma(rf, lo[c], acc[x][c]);
+                    for (int c = 0; c < T; ++c) acc[x][c] = mfma(af, hi[c], acc[x][c]);
+#pragma unroll
+                    for (int c = 0; c < T; ++c) acc[x][c] = mfma(af, lo[c], acc[x][c]);
+                    af = an;
                 }
             }
+            clear_u();
         }
+        loads_done();
+        __syncthreads();
+        blk = nb;
+        q = nqq;
     }
 
     // acc[x][c]: a = a0 + 16 x + 4 lg .. +3 of row c0 + 16 (wave T + c) + lr
     const bool whole = a.splits == 1;
     const int stride = whole ? a.ldw : a.d + 4;
-    float *out = a.out + ((size_t)split * gridDim.y + l) * a.d * stride;
+    float *out = a.out + ((size_t)split * a.L + l) * a.d * stride;
 #pragma unroll
     for (int c = 0; c < T; ++c) {
         const int row = c0 + 16 * (wave * T + c) + lr;
@@ -657,27 +901,26 @@ constexpr int kCus = 256;
 // How a call is cut up, and its workspace.
 struct BwdPlan {
     int nb, dp;                     // DP = 128 nb
-    bool small;                     // few blocks: a block an item, its columns shared by nb items
-    int h, zs, groups, per_group;   // blocks of an item; column shares; label groups and labels of one
-    int t, tiles_a, tiles_c, splits;
+    bool few, few_long;             // few blocks (whole sentences, long ones): nb items share their columns
+    int groups, per_group;          // label groups and labels of one
+    bool wide;                      // dW in tiles of 256 x 256, else 128 x 128
+    int tiles_a, tiles, splits;
     int64_t w_at, g_at, part_at, wpart_at, bytes;
 };
 BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     BwdPlan b{};
     b.nb = (d + 1 + 127) / 128;
     b.dp = 128 * b.nb;
-    b.small = (int64_t)p.n_posts * L < 256;
-    b.h = b.small || b.nb == 1 ? 1 : 2;
-    b.zs = b.small ? b.nb : 1;
-    const int64_t items = (int64_t)p.n_posts / b.h * 2;
-    b.groups = (int)std::max<int64_t>(1, std::min<int64_t>(L, 2 * kCus / items));
+    b.groups = std::max(1, std::min(L, 2 * kCus / p.n_posts));
     b.per_group = (L + b.groups - 1) / b.groups;
     b.groups = (L + b.per_group - 1) / b.per_group;
-    b.t = d + 1 > 128 ? 2 : 1;
-    b.tiles_a = (d + 1 + 128 * b.t - 1) / (128 * b.t);
-    b.tiles_c = (d + 128 * b.t - 1) / (128 * b.t);
-    const int64_t wgs = (int64_t)b.tiles_a * b.tiles_c * L;
-    b.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.n_posts, (b.t == 2 ? kCus : 3 * kCus) / wgs));
+    b.few = (int64_t)(p.n_posts - p.n_long_posts) * b.groups < kCus;
+    b.few_long = (int64_t)p.n_long_posts * b.groups < kCus;
+    b.wide = d + 1 > 128;
+    const int tile = b.wide ? 256 : 128;
+    b.tiles_a = (d + 1 + tile - 1) / tile;
+    b.tiles = b.tiles_a * ((d + tile - 1) / tile);
+    b.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.n_posts, (b.wide ? 1 : 2) * kCus / ((int64_t)b.tiles * L)));
     int64_t at = 0;
     b.w_at = at;
     at += up256((int64_t)L * 2 * b.dp * b.dp * 2);
@@ -691,32 +934,61 @@ BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     return b;
 }
 
-template <int NB, int H, int CB, int WR, bool Q8, bool COMPACT>
-hipError_t launch_rows(const BwdArgs &a, int sides, int per_cu, hipStream_t stream) {
-    const int slots = std::max(1, per_cu * kCus / sides);
-    hipLaunchKernelGGL((bwd_rows_kernel<NB, H, CB, WR, Q8, COMPACT>), dim3(std::min(a.items, slots), sides), dim3(kThreads),
-                       (RowsShape<NB, H>::kLds), stream, a);
+// Every build of bwd_posts_kernel: nb, few, then NB, NW, H, CB and the
+// workgroups of one that a CU holds; and of bwd_long_kernel: nb, few, NB, CB.
+#define CRF_BWD_POSTS(F)                                                                                     \
+    F(1, false, 1, 4, 1, 2, 2) F(2, false, 2, 8, (COMPACT ? 1 : 2), 2, 1) F(3, false, 3, 8, (COMPACT ? 1 : 2), 3, 1) \
+    F(4, false, 4, 8, (COMPACT ? 1 : 2), 4, 1) F(1, true, 1, 8, 1, 1, 1) F(2, true, 2, 8, 1, 1, 1)           \
+    F(3, true, 3, 8, 1, 1, 1) F(4, true, 4, 8, 1, 1, 1)
+#define CRF_BWD_LONG(F) \
+    F(1, false, 1, 1) F(2, false, 2, 2) F(3, false, 3, 3) F(4, false, 4, 4) F(2, true, 2, 1) F(3, true, 3, 1) F(4, true, 4, 1)
+
+template <int NB, int NW, int H, int CB, bool Q8, bool COMPACT>
+hipError_t launch_posts(BwdArgs a, int sides, int groups, int per_cu, hipStream_t stream) {
+    a.zs = 8 * NB / (NW * CB);
+    a.items = (a.blks + H - 1) / H * a.zs * groups;
+    const int slots = per_cu * kCus / sides;
+    hipLaunchKernelGGL((bwd_posts_kernel<NB, NW, H, CB, Q8, COMPACT>), dim3(std::min(a.items, slots), sides), dim3(64 * NW),
+                       (PostsShape<NB, NW, H, COMPACT>::kLds), stream, a);
     return hipGetLastError();
 }
-// Every build of bwd_rows_kernel, with the workgroups of one that a CU holds.
-#define CRF_BWD_ROWS(F)                                                                             \
-    F(1, false, 1, 1, 2, 2, 2) F(2, false, 2, 2, 4, 2, 1) F(3, false, 3, 2, 3, 1, 1) F(4, false, 4, 2, 4, 1, 1) \
-    F(1, true, 1, 1, 1, 1, 2) F(2, true, 2, 1, 1, 1, 1) F(3, true, 3, 1, 1, 1, 1) F(4, true, 4, 1, 1, 1, 1)
+template <int NB, int CB, bool Q8, bool COMPACT>
+hipError_t launch_long(BwdArgs a, int sides, int groups, hipStream_t stream) {
+    a.zs = NB / CB;
+    a.items = a.blks * a.zs * groups;
+    hipLaunchKernelGGL((bwd_long_kernel<NB, CB, Q8, COMPACT>), dim3(a.items, sides), dim3(64 * kLongWaves), LongShape<NB>::kLds,
+                       stream, a);
+    return hipGetLastError();
+}
 template <bool Q8, bool COMPACT>
-hipError_t launch_rows_of(const BwdPlan &b, const BwdArgs &a, int sides, hipStream_t stream) {
-#define CRF_LAUNCH(N, SMALL, NB, H, CB, WR, PER) \
-    if (b.nb == N && b.small == SMALL) return launch_rows<NB, H, CB, WR, Q8, COMPACT>(a, sides, PER, stream);
-    CRF_BWD_ROWS(CRF_LAUNCH)
+hipError_t launch_rows(const BwdPlan &b, BwdArgs a, int n_long, int sides, hipStream_t stream) {
+    if (n_long > 0) {   // (the longest items first)
+        a.blk0 = 0;
+        a.blks = n_long;
+        const bool few = b.few_long && b.nb > 1;
+        hipError_t e = hipErrorInvalidValue;
+#define CRF_LAUNCH(N, FEW, NB, CB) \
+        if (b.nb == N && few == FEW) e = launch_long<NB, CB, Q8, COMPACT>(a, sides, b.groups, stream);
+        CRF_BWD_LONG(CRF_LAUNCH)
+#undef CRF_LAUNCH
+        if (e != hipSuccess) return e;
+    }
+    a.blk0 = n_long;
+    a.blks = a.n_posts - n_long;
+    if (a.blks == 0) return hipSuccess;
+#define CRF_LAUNCH(N, FEW, NB, NW, H, CB, PER) \
+    if (b.nb == N && b.few == FEW) return launch_posts<NB, NW, H, CB, Q8, COMPACT>(a, sides, b.groups, PER, stream);
+    CRF_BWD_POSTS(CRF_LAUNCH)
 #undef CRF_LAUNCH
     return hipErrorInvalidValue;
 }
 template <bool Q8, bool COMPACT>
-hipError_t launch_weight(const BwdPlan &b, const WeightArgs &a, int L, hipStream_t stream) {
-    const dim3 grid(b.tiles_a * b.tiles_c, L, b.splits);
-    if (b.t == 1)
-        hipLaunchKernelGGL((bwd_weight_kernel<1, Q8, COMPACT>), grid, dim3(kThreads), WeightShape<1>::kLds, stream, a);
+hipError_t launch_weight(const BwdPlan &b, const WeightArgs &a, hipStream_t stream) {
+    const dim3 grid((unsigned)(((int64_t)a.splits * a.L + kXcds - 1) / kXcds * kXcds * b.tiles));
+    if (b.wide)
+        hipLaunchKernelGGL((bwd_weight_kernel<16, 2, 8, Q8, COMPACT>), grid, dim3(512), (WeightShape<16, 2, 8>::kLds), stream, a);
     else
-        hipLaunchKernelGGL((bwd_weight_kernel<2, Q8, COMPACT>), grid, dim3(kThreads), WeightShape<2>::kLds, stream, a);
+        hipLaunchKernelGGL((bwd_weight_kernel<8, 2, 4, Q8, COMPACT>), grid, dim3(256), (WeightShape<8, 2, 4>::kLds), stream, a);
     return hipGetLastError();
 }
 
@@ -724,12 +996,16 @@ template <bool Q8, bool COMPACT>
 hipError_t set_attributes() {
     hipError_t e;
     auto set = [&](const void *f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-#define CRF_SET(N, SMALL, NB, H, CB, WR, PER) \
-    if ((e = set((const void *)bwd_rows_kernel<NB, H, CB, WR, Q8, COMPACT>, RowsShape<NB, H>::kLds)) != hipSuccess) return e;
-    CRF_BWD_ROWS(CRF_SET)
+#define CRF_SET(N, FEW, NB, NW, H, CB, PER) \
+    if ((e = set((const void *)bwd_posts_kernel<NB, NW, H, CB, Q8, COMPACT>, PostsShape<NB, NW, H, COMPACT>::kLds)) != hipSuccess) return e;
+    CRF_BWD_POSTS(CRF_SET)
 #undef CRF_SET
-    if ((e = set((const void *)bwd_weight_kernel<1, Q8, COMPACT>, WeightShape<1>::kLds)) != hipSuccess ||
-        (e = set((const void *)bwd_weight_kernel<2, Q8, COMPACT>, WeightShape<2>::kLds)) != hipSuccess)
+#define CRF_SET(N, FEW, NB, CB) \
+    if ((e = set((const void *)bwd_long_kernel<NB, CB, Q8, COMPACT>, LongShape<NB>::kLds)) != hipSuccess) return e;
+    CRF_BWD_LONG(CRF_SET)
+#undef CRF_SET
+    if ((e = set((const void *)bwd_weight_kernel<16, 2, 8, Q8, COMPACT>, WeightShape<16, 2, 8>::kLds)) != hipSuccess ||
+        (e = set((const void *)bwd_weight_kernel<8, 2, 4, Q8, COMPACT>, WeightShape<8, 2, 4>::kLds)) != hipSuccess)
         return e;
     return hipSuccess;
 }
@@ -772,10 +1048,25 @@ hipError_t launch_biaffine_bwd(const KernelPlan &p, int64_t cells, const void *r
         if ((e = hipGetLastError()) != hipSuccess) return e;
         const int side0 = grad_rl != nullptr ? 0 : 1, sides = (grad_rl != nullptr) + (grad_rr != nullptr);
         float *part = b.groups > 1 ? reinterpret_cast<float *>(ws + b.part_at) : nullptr;
-        const BwdArgs a{p.posts, cell_at, p.n_posts, d, L, b.per_group, rl_rows, rr_rows,
-                        wf, g, cells, {grad_rl, grad_rr}, part, b.zs, p.n_posts / b.h * b.zs * b.groups, side0};
-        e = q8 ? (L > 1 ? launch_rows_of<true, true>(b, a, sides, stream) : launch_rows_of<true, false>(b, a, sides, stream))
-               : (L > 1 ? launch_rows_of<false, true>(b, a, sides, stream) : launch_rows_of<false, false>(b, a, sides, stream));
+        BwdArgs a{};
+        a.posts = p.posts;
+        a.post_cells = cell_at;
+        a.n_posts = p.n_posts;
+        a.d = d;
+        a.L = L;
+        a.per_group = b.per_group;
+        a.rl = rl_rows;
+        a.rr = rr_rows;
+        a.wf = wf;
+        a.g = g;
+        a.cells = cells;
+        a.out[0] = grad_rl;
+        a.out[1] = grad_rr;
+        a.part = part;
+        a.side0 = side0;
+        const int n_long = p.n_long_posts;
+        e = q8 ? (L > 1 ? launch_rows<true, true>(b, a, n_long, sides, stream) : launch_rows<true, false>(b, a, n_long, sides, stream))
+               : (L > 1 ? launch_rows<false, true>(b, a, n_long, sides, stream) : launch_rows<false, false>(b, a, n_long, sides, stream));
         if (e != hipSuccess) return e;
         if (part != nullptr) {
             const int64_t n = (int64_t)p.n_posts * kBlk * (d / 4);
@@ -786,9 +1077,10 @@ hipError_t launch_biaffine_bwd(const KernelPlan &p, int64_t cells, const void *r
     }
     if (grad_w != nullptr) {
         float *part = reinterpret_cast<float *>(ws + b.wpart_at);
-        const WeightArgs a{p.posts, cell_at, p.n_posts, d, ldw, b.splits, b.tiles_a, rl_rows, rr_rows, g, cells, b.splits > 1 ? part : grad_w};
-        e = q8 ? (L > 1 ? launch_weight<true, true>(b, a, L, stream) : launch_weight<true, false>(b, a, L, stream))
-               : (L > 1 ? launch_weight<false, true>(b, a, L, stream) : launch_weight<false, false>(b, a, L, stream));
+        const WeightArgs a{p.posts, cell_at, p.n_posts, d, ldw, L, b.splits, b.tiles_a, b.tiles, rl_rows, rr_rows, g, cells,
+                           b.splits > 1 ? part : grad_w};
+        e = q8 ? (L > 1 ? launch_weight<true, true>(b, a, stream) : launch_weight<true, false>(b, a, stream))
+               : (L > 1 ? launch_weight<false, true>(b, a, stream) : launch_weight<false, false>(b, a, stream));
         if (e != hipSuccess) return e;
         if (b.splits > 1) {
             const int64_t n = (int64_t)L * d * (d / 4 + 1);

@@ -483,15 +483,15 @@ struct KernelPlan {
     // (b N1 + fence post, or -1)
     const int32_t *bia_tiles;
     int32_t n_bia_tiles;
-    // every fence post of the batch once, in an even number of blocks: kPostRec
-    // ints a block (kBiaRows ids b N1 + fence post i or -1, for each the n - i
+    // every fence post of the batch once, in blocks, those of sentences that take
+    // several (n_long_posts) first: kPostRec ints a block (kBiaRows ids b N1 + fence post i or -1, for each the n - i
     // cells of its row (0: none), then the first and the last block that hold
     // posts of its sentences); a sentence's posts are neighbours.  post_cells:
     // for each of them where its cell (i, i) would be in the square array
     // [B][N1][N1], then in a compact one of all sentences' n x n cells (i, j),
     // j from 1 (a post without cells has another's: the next cell exists)
     const int32_t *posts;
-    int32_t n_posts;
+    int32_t n_posts, n_long_posts;
     const int64_t *post_cells;
     // the tree calls' pass over the trees, longest sentences first: (sentence,
     // n, first row, rows) of a stripe of rows of at most kTreeCells cells (a

@@ -502,6 +502,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     // of row block <= column block.
     std::vector<int32_t> bia, posts;
     std::vector<int64_t> post_cells, compact_cells;
+    int32_t n_long_posts = 0;
     {
         std::vector<std::vector<int32_t>> packed;
         std::vector<std::vector<int32_t>> by_free(crf::kBiaRows + 1);
@@ -581,12 +582,11 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
                 put_block(ids.data() + k * crf::kBiaRows, std::min(crf::kBiaRows, n + 1 - k * crf::kBiaRows), first,
                           first + nblk - 1);
         }
+        n_long_posts = (int32_t)(posts.size() / crf::kPostRec);
         for (const auto &ids : packed) {
             const int at = (int)(posts.size() / crf::kPostRec);
             put_block(ids.data(), (int)ids.size(), at, at);
         }
-        const int blocks = (int)(posts.size() / crf::kPostRec);
-        if (blocks % 2 != 0) put_block(nullptr, 0, blocks, blocks);   // an even number: some kernels take pairs
         post_cells.insert(post_cells.end(), compact_cells.begin(), compact_cells.end());
     }
 
@@ -657,6 +657,7 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     kp.n_lab_rows = (int32_t)(lab_rows.size() / 4);
     kp.n_bia_tiles = (int32_t)(bia.size() / (crf::kBiaRows + crf::kBiaCols));
     kp.n_posts = (int32_t)(posts.size() / crf::kPostRec);
+    kp.n_long_posts = n_long_posts;
     kp.lab_sp_off = lab_sp_off;
     kp.lab_mu_off = lab_mu_off;
     std::vector<int32_t> rec_mix;

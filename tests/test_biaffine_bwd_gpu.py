@@ -4,9 +4,12 @@ Tolerances, per entry.  A bf16 rounding is off by at most 2^-8 of the value, a
 hi + lo pair by 2^-16, a float32 sum of K terms by K 2^-24 of the terms'
 absolute sum (K below 64 blocks of posts or 512 here, and both).
   grad_w    (2 * 2^-16 + K 2^-24) sum |G| |r^l| |r^r|, K the posts plus 128
-  grad_rl   2^-8 sum_c |U_c| |W_c| (U rounded once) + 2^-8 |result| (and the
-            product of the two roundings, 2^-16) + (2^-16 + 2^-14) sum |G| |r^r| |W|
-  grad_rr   the same with X and [r^l ; 1]
+  grad_rl   the inner product, rounded to bf16 once: of sentences of up to 63
+            words (G (R^r W^T)) V = R^r W^T, 2^-8 sum_j |G| |V_j|; of longer
+            ones ((G R^r) W^T) U = G R^r, 2^-8 sum_c |U_c| |W_c|; + 2^-8 |result|
+            (and the product of the two roundings, 2^-16)
+            + (2^-16 + 2^-14) sum |G| |r^r| |W|
+  grad_rr   the same with [r^l ; 1], V = [r^l ; 1] W and X = G^T [r^l ; 1]
 A pass from the 8-bit form equals the one from the bf16 rows it stands for, bit
 for bit: the codes become those rows before the first product.
 """
@@ -58,8 +61,12 @@ def reference(rl, rr, wt, lengths, g):
             out[0][b, :n + 1] += u @ wl
             out[1][b, :n + 1] += x @ w[q].T
             out[2][q] += u.T @ one
-            tol[0][b, :n + 1] += (2.0 ** -8 + 2.0 ** -16) * np.abs(u) @ wa[:, :d] + (2.0 ** -16 + 2.0 ** -14) * ua @ wa[:, :d]
-            tol[1][b, :n + 1] += (2.0 ** -8 + 2.0 ** -16) * np.abs(x) @ wa.T + (2.0 ** -16 + 2.0 ** -14) * xa @ wa.T
+            if n <= 63:
+                inner = np.abs(gq) @ np.abs(r @ wl), np.abs(gq).T @ np.abs(one @ w[q].T)
+            else:
+                inner = np.abs(u) @ wa[:, :d], np.abs(x) @ wa.T
+            tol[0][b, :n + 1] += (2.0 ** -8 + 2.0 ** -16) * inner[0] + (2.0 ** -16 + 2.0 ** -14) * ua @ wa[:, :d]
+            tol[1][b, :n + 1] += (2.0 ** -8 + 2.0 ** -16) * inner[1] + (2.0 ** -16 + 2.0 ** -14) * xa @ wa.T
             tol[2][q] += ua.T @ np.abs(one)
     tol[0] += 2.0 ** -8 * np.abs(out[0])
     tol[1] += 2.0 ** -8 * np.abs(out[1])
