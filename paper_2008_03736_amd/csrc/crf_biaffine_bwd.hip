@@ -39,7 +39,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlk = kBiaRows;               // fence posts of a block
-constexpr int kGS = kBlk + 8;                // row stride of the staged G (16-byte reads free of conflicts)
+constexpr int kGS = kBlk + 4;                // row stride of the staged G
 
 __device__ __forceinline__ bf16x8 frag(const uint16_t *p) {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(p));
@@ -158,45 +158,10 @@ struct Staged {
                 p.x = row_in && k == d ? 0x3F80u : p.x;
                 p.z = row_in && half ? 0x3F80u : p.z;
             }
-            *reinterpret_cast<uint4 *>(to + (kRows * w + row(u)) * stride + col()) = p;
+            if (col() < stride) *reinterpret_cast<uint4 *>(to + (kRows * w + row(u)) * stride + col()) = p;
         }
     }
 };
-
-// The same rows of bf16 straight to LDS, four bytes a lane and load, nothing of
-// them in registers: entries [k0, k0 + COLS) that a row has.  What is to stand
-// past a row's end is put there once (set_ends); rows that do not exist are row
-// 0 (the products take them times 0).  Wait for the loads (loads_done) before
-// the barrier that lets others read.
-template <int COLS, int NW>
-__device__ __forceinline__ void rows_to_lds(const Rows &r, const int32_t *post, int k0, int d, uint16_t *to, int stride) {
-    constexpr int kRows = kBlk / NW;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int words = min(d - k0, COLS) / 2;
-    int id[kRows];
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) id[u] = constant(post + kRows * w + u);
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-        const uint32_t *row = reinterpret_cast<const uint32_t *>(static_cast<const uint16_t *>(r.x) + (size_t)max(id[u], 0) * d + k0);
-        uint16_t *at = to + (kRows * w + u) * stride;
-#pragma unroll
-        for (int p = 0; p < COLS / 128; ++p)
-            if (64 * p + lane < words)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)(row + 64 * p + lane),
-                                                 (__attribute__((address_space(3))) uint32_t *)(at + 128 * p), 4, 0, 0);
-    }
-}
-// Columns of `rows` staged rows that hold no entry: 1 at entry d if ONE, else 0.
-template <bool ONE>
-__device__ __forceinline__ void set_ends(uint16_t *to, int rows, int stride, int k0, int d) {
-    const int from = max(min(d - k0, stride), 0), wide = stride - from;
-    for (int t = threadIdx.x; t < rows * wide; t += blockDim.x) {
-        const int r = t / wide, c = from + t - r * wide;
-        to[r * stride + c] = ONE && k0 + c == d ? 0x3F80u : 0u;
-    }
-}
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // A label's gradient and where each post's cell (i, i) would be in it: the
 // caller's [B][N1][N1], or the compact cells of the label
@@ -209,8 +174,8 @@ struct Grad {
 // sentence with i < j, zero elsewhere (other cells are not used).  Posts of a
 // sentence are neighbours, so row r's cells are its n - i next columns.
 // Wavefront w of NW takes kRows rows from kRows w on, a lane a column, so that
-// rows are read along memory, what a row needs is scalar and eight rows of a
-// lane are one 16-byte store of G^T[j][i]; as bf16 hi and lo parts.
+// rows are read along memory, what a row needs is scalar and rows of a lane are
+// neighbours in G^T[j][i]; as bf16 hi and lo parts.
 template <int NW>
 struct Staged_grad {
     static constexpr int kRows = kBlk / NW;
@@ -239,16 +204,16 @@ struct Staged_grad {
     __device__ __forceinline__ void store(uint16_t *hi, uint16_t *lo) const {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-        for (int q = 0; q < kRows / 8; ++q) {
-            bf16x8 h, l;
+        for (int q = 0; q < kRows / 4; ++q) {
+            bf16x4 h, l;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float x = in >> (8 * q + u) & 1u ? v[8 * q + u] : 0.f;
+            for (int u = 0; u < 4; ++u) {
+                const float x = in >> (4 * q + u) & 1u ? v[4 * q + u] : 0.f;
                 h[u] = (__bf16)x;
                 l[u] = (__bf16)(x - (float)h[u]);
             }
-            *reinterpret_cast<uint4 *>(hi + lane * kGS + kRows * w + 8 * q) = __builtin_bit_cast(uint4, h);
-            *reinterpret_cast<uint4 *>(lo + lane * kGS + kRows * w + 8 * q) = __builtin_bit_cast(uint4, l);
+            *reinterpret_cast<bf16x4 *>(hi + lane * kGS + kRows * w + 4 * q) = h;
+            *reinterpret_cast<bf16x4 *>(lo + lane * kGS + kRows * w + 4 * q) = l;
         }
     }
 };
@@ -341,15 +306,14 @@ struct BwdArgs {
     int zs;                             // items that share blocks' output columns
     int items, side0;                   // items of a side; the first grid.y's side
 };
-// An item: H blocks from blk on, labels and column share.
+// An item: its block, labels and column share.
 struct Item {
     int blk, l0, l1, cz, grp;
 };
-template <int H>
 __device__ __forceinline__ Item item_of(const BwdArgs &a, int it) {
-    const int units = (a.blks + H - 1) / H, q = it / units;
+    const int q = it / a.blks;
     Item x;
-    x.blk = a.blk0 + H * (it - q * units);
+    x.blk = a.blk0 + it - q * a.blks;
     x.cz = q % a.zs;
     x.grp = q / a.zs;
     x.l0 = x.grp * a.per_group;
@@ -359,77 +323,100 @@ __device__ __forceinline__ Item item_of(const BwdArgs &a, int it) {
 __device__ __forceinline__ const uint16_t *weight_frags(const BwdArgs &a, int l, int side, int dp, int col0) {
     return a.wf + ((((size_t)l * 2 + side) * (dp / 32)) * (dp / 16) + col0) * 512 + 8 * (threadIdx.x & 63);
 }
-// o[c][r]: columns 16 (col0 + c) + 4 lg .. +3 of post 16 r + lr of block blk.
+// Of x and y in the four 16-lane rows of a wavefront, x0 x1 x2 x3 and y0 y1 y2
+// y3: (x0 x2 y0 y2, x1 x3 y1 y3).
+__device__ __forceinline__ uint2 trade(uint32_t x, uint32_t y) {
+    const auto h = __builtin_amdgcn_permlane32_swap(x, y, false, false);         // x0 x1 y0 y1, x2 x3 y2 y3
+    const auto q = __builtin_amdgcn_permlane16_swap(h[0], h[1], false, false);
+    return make_uint2(q[0], q[1]);
+}
+// A lane's posts 16 r + lr of a block (all before the first store, which a later
+// load would wait for).
+struct Row_ids {
+    int id[4];
+    __device__ __forceinline__ void load(const BwdArgs &a, int blk) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) id[r] = a.posts[(size_t)blk * kPostRec + 16 * r + (int)(threadIdx.x & 15)];
+    }
+};
+// o[c]: columns 16 (col0 + c) + 4 lg .. +3 of post 16 r + lr of block blk, whose
+// id is `id`.
 template <int CB, int SIDE>
-__device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB][4], int blk, int grp, int col0, int dp) {
+__device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB], int id, int blk, int r, int grp, int col0,
+                                           int dp) {
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-    int ids[4];   // (all before the first store, which a later load would wait for)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) ids[r] = a.posts[(size_t)blk * kPostRec + 16 * r + lr];
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
+    if (id < 0) return;   // (the four lanes of a post alike)
+    if (a.part != nullptr) {
+        float *row = a.part + (((size_t)grp * 2 + SIDE) * a.n_posts * kBlk + kBlk * blk + 16 * r + lr) * dp;
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
             const int col = 16 * (col0 + c) + 4 * lg;
-            if (ids[r] < 0 || col >= a.d) continue;
-            if (a.part != nullptr)
-                *reinterpret_cast<f32x4 *>(a.part + (((size_t)grp * 2 + SIDE) * a.n_posts * kBlk + kBlk * blk + 16 * r + lr) * dp + col) =
-                    o[c][r];
-            else
-                *reinterpret_cast<bf16x4 *>(a.out[SIDE] + (size_t)ids[r] * a.d + col) = __builtin_convertvector(o[c][r], bf16x4);
+            if (col < a.d) *reinterpret_cast<f32x4 *>(row + col) = o[c];
         }
+        return;
+    }
+    // Two column blocks at a time: the four lanes of a post exchange their
+    // fours, so that each has eight neighbours and a store writes 64 bytes of a
+    // post's row.
+    typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(8)));
+    uint16_t *row = a.out[SIDE] + (size_t)id * a.d;
+#pragma unroll
+    for (int c = 0; c + 1 < CB; c += 2) {
+        const uint2 x = __builtin_bit_cast(uint2, __builtin_convertvector(o[c], bf16x4));
+        const uint2 y = __builtin_bit_cast(uint2, __builtin_convertvector(o[c + 1], bf16x4));
+        const uint2 px = trade(x.x, y.x), py = trade(x.y, y.y);
+        const int col = 16 * (col0 + c) + 8 * lg;
+        if (col + 8 <= a.d) *reinterpret_cast<u32x4u *>(row + col) = u32x4u{px.x, py.x, px.y, py.y};
+        else if (col < a.d) *reinterpret_cast<uint2 *>(row + col) = make_uint2(px.x, py.x);
+    }
+    if constexpr (CB % 2 != 0) {
+        const int col = 16 * (col0 + CB - 1) + 4 * lg;
+        if (col < a.d) *reinterpret_cast<bf16x4 *>(row + col) = __builtin_convertvector(o[CB - 1], bf16x4);
+    }
 }
 
-// dR^l (side 0) and dR^r (side 1) of blocks that hold whole sentences, as
-// G (R^r W^T) and G^T ([R^l ; 1] W): V = R W first, whose K runs along rows, so
-// that R goes to LDS as it lies in memory (no instruction of a wavefront
-// touches it) and W's fragments come straight from L2 in the order of the
-// lanes.  A wavefront holds V of its 16 CB columns for all posts of H blocks,
-// which is the layout of the second product's operand when K is numbered as in
-// grad_frag: V, rounded to bf16, never leaves the registers.  (As (G R) W^T,
-// whose inner product goes through LDS, 5,000 sentences at d = 500 took 252 us,
-// 75 of them in the dense product, the rest in staging that both products wait
-// for.)  R of the next item is on its way from the end of the dense product on.
+// dR^l (side 0) and dR^r (side 1) of a block that holds whole sentences, as
+// G (R^r W^T) and G^T ([R^l ; 1] W): V = R W first, whose K runs along rows of
+// R, and W's fragments come straight from L2 in the order of the lanes.  A
+// wavefront holds V of its 16 CB columns for all 64 posts, which is the layout
+// of the second product's operand when K is numbered as in grad_frag: V,
+// rounded to bf16, never leaves the registers.  (As (G R) W^T, whose inner
+// product goes through LDS, 5,000 sentences at d = 500 took 252 us.)
+//
+// Two workgroups a CU (at d = 500 they fill its LDS): one's staging and stores
+// run beside the other's products.  With 128 posts a workgroup and one on a CU,
+// W came from L2 half as often, but 210 us.  R and G of a workgroup's next
+// block are on their way to registers from the end of the dense product on.
 // DP = 128 NB columns, 16 NW CB of them a workgroup.
-template <int NB, int NW, int H, bool COMPACT>
-struct PostsShape {
-    static constexpr int kDP = 128 * NB, kRS = kDP + 8, kGrads = COMPACT ? 2 : 1;
-    static constexpr int kLds = 2 * (H * kBlk * kRS + kGrads * 2 * kBlk * kGS);
-};
 
-template <int NB, int NW, int H, int CB, bool Q8, bool COMPACT, int SIDE>
+// Row stride of R: past d, and an odd multiple of 16 bytes (16-byte operands of
+// sixteen rows in different banks).  K runs past it into the next row (or G),
+// where W's fragments are zero.
+__host__ __device__ inline int row_stride(int d) { return (d / 8 + 1) * 8 + (d / 8 % 2 != 0 ? 8 : 0); }
+template <bool COMPACT>
+inline int posts_lds(int d) {
+    return 2 * (kBlk * row_stride(d) + (COMPACT ? 2 : 1) * 2 * kBlk * kGS);
+}
+
+template <int NB, int NW, int CB, bool Q8, bool COMPACT, int SIDE>
 __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
-    typedef PostsShape<NB, NW, H, COMPACT> S;
-    static_assert(!COMPACT || H == 1, "sums over labels: a block at a time");
-    constexpr int DP = S::kDP, RS = S::kRS;
+    constexpr int DP = 128 * NB;
     constexpr bool ONE = SIDE == 1, ROWS_I = SIDE == 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lr = lane & 15, lg = lane >> 4;
-    uint16_t *R = reinterpret_cast<uint16_t *>(smem);   // [64 H][RS]
-    uint16_t *G = R + H * kBlk * RS;                    // [kGrads][2][64][kGS]: G^T, hi and lo
+    const int lr = lane & 15, lg = lane >> 4, RS = row_stride(a.d);
+    uint16_t *R = reinterpret_cast<uint16_t *>(smem);   // [64][RS]
+    uint16_t *G = R + kBlk * RS;                        // [COMPACT ? 2 : 1][2][64][kGS]: G^T, hi and lo
     const int ksteps = (a.d + 32) / 32;   // K of the dense product: d + 1 at most
     const Rows rows = SIDE == 0 ? a.rr : a.rl;
-    const int last_blk = a.blk0 + a.blks - 1;   // (an item's second block past it is it again, and not stored)
 
-    auto stage_r = [&](int blk) {
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-            const int32_t *post = a.posts + (size_t)min(blk + h, last_blk) * kPostRec;
-            if constexpr (Q8) {
-                Staged<DP, NW, true> sr;
-                sr.load(rows, post, 0, a.d);
-                sr.template store<ONE>(rows, 0, a.d, R + h * kBlk * RS, RS);
-            } else {
-                rows_to_lds<DP, NW>(rows, post, 0, a.d, R + h * kBlk * RS, RS);
-            }
-        }
+    constexpr bool AHEAD = CB <= 2 || COMPACT;   // (R of the next block beside V, in registers)
+    Staged<DP, NW, Q8> sr;
+    Staged_grad<NW> sg;
+    auto load_r = [&](int blk) { sr.load(rows, a.posts + (size_t)blk * kPostRec, 0, a.d); };
+    auto load_grad = [&](int blk, int l) {
+        sg.load(Grad{a.g + (COMPACT ? l * a.cells : 0), a.post_cells}, a.posts, blk, blk);
     };
-    Staged_grad<NW> sg[H];
-    auto load_grad = [&](int h, int blk, int l) {
-        const int b = min(blk + h, last_blk);
-        sg[h].load(Grad{a.g + (COMPACT ? l * a.cells : 0), a.post_cells}, a.posts, b, b);
-    };
-    f32x4 v[4 * H][CB];
+    f32x4 v[4][CB];
     // V = R W_l
     auto dense = [&](int l, int col0) {
         const uint16_t *wf = weight_frags(a, l, SIDE, DP, col0);
@@ -438,7 +425,7 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
 #pragma unroll
         for (int c = 0; c < CB; ++c) wv[0][c] = frag(wf + (size_t)c * 512);
 #pragma unroll
-        for (int r = 0; r < 4 * H; ++r)
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int c = 0; c < CB; ++c) v[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
         auto step = [&](int ks, bf16x8 (&now)[CB], bf16x8 (&then)[CB]) {
@@ -448,9 +435,9 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
             bf16x8 pv = frag(p + 32 * ks);
             __builtin_amdgcn_sched_barrier(0);   // (left alone, they are issued where they are waited for)
 #pragma unroll
-            for (int r = 0; r < 4 * H; ++r) {
+            for (int r = 0; r < 4; ++r) {
                 bf16x8 pn = pv;
-                if (r + 1 < 4 * H) pn = frag(p + 16 * (r + 1) * RS + 32 * ks);
+                if (r + 1 < 4) pn = frag(p + 16 * (r + 1) * RS + 32 * ks);
 #pragma unroll
                 for (int c = 0; c < CB; ++c) v[r][c] = mfma(pv, now[c], v[r][c]);
                 pv = pn;
@@ -464,91 +451,87 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
         }
         if (ks < ksteps) step(ks, wv[0], wv[1]);
     };
-    // o += V^T G of block h
-    auto second = [&](int h, const uint16_t *g, f32x4 (&o)[CB][4]) {
+    bf16x8 vb[2][CB];
+    auto round_v = [&]() {
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            bf16x8 vb[CB];
+        for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int c = 0; c < CB; ++c)
 #pragma unroll
-                for (int t = 0; t < 8; ++t) vb[c][t] = (__bf16)v[4 * h + 2 * p + (t >> 2)][c][t & 3];
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (grad_part<ROWS_I>(r, p)) {
-                    const bf16x8 gh = grad_frag<ROWS_I>(g, r, p, lr, lg), gl = grad_frag<ROWS_I>(g + kBlk * kGS, r, p, lr, lg);
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) o[c][r] = mfma(vb[c], gh, o[c][r]);
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) o[c][r] = mfma(vb[c], gl, o[c][r]);
-                }
-        }
+                for (int t = 0; t < 8; ++t) vb[p][c][t] = (__bf16)v[2 * p + (t >> 2)][c][t & 3];
     };
-    auto clear = [](f32x4 (&o)[CB][4]) {
+    // o += V^T G, posts 16 r .. +15
+    auto second = [&](int r, const uint16_t *g, f32x4 (&o)[CB]) {
 #pragma unroll
-        for (int c = 0; c < CB; ++c)
+        for (int p = 0; p < 2; ++p)
+            if (grad_part<ROWS_I>(r, p)) {
+                const bf16x8 gh = grad_frag<ROWS_I>(g, r, p, lr, lg), gl = grad_frag<ROWS_I>(g + kBlk * kGS, r, p, lr, lg);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int c = 0; c < CB; ++c) o[c] = mfma(vb[p][c], gh, o[c]);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) o[c] = mfma(vb[p][c], gl, o[c]);
+            }
+    };
+    auto clear = [](f32x4 (&o)[CB]) {
+#pragma unroll
+        for (int c = 0; c < CB; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
 
     int it = blockIdx.x;
     if (it >= a.items) return;
-    if constexpr (!Q8) {
-        set_ends<ONE>(R, H * kBlk, RS, 0, a.d);
-        __syncthreads();
-    }
-    Item x = item_of<H>(a, it);
-    stage_r(x.blk);
-#pragma unroll
-    for (int h = 0; h < H; ++h) load_grad(h, x.blk, x.l0);
+    Item x = item_of(a, it);
+    if constexpr (AHEAD) load_r(x.blk);
+    load_grad(x.blk, x.l0);
     for (;;) {
+        if constexpr (!AHEAD) load_r(x.blk);
         const int next_it = it + gridDim.x;
-        const Item nx = item_of<H>(a, min(next_it, a.items - 1));
+        const Item nx = item_of(a, min(next_it, a.items - 1));
         const int col0 = (x.cz * NW + wave) * CB;   // the wavefront's first column block
-        f32x4 o[CB][4];
+        sr.template store<ONE>(rows, 0, a.d, R, RS);
+        sg.store(G, G + kBlk * kGS);
         if constexpr (COMPACT) {
-            clear(o);
-            sg[0].store(G, G + kBlk * kGS);
-            if (x.l0 + 1 < x.l1) load_grad(0, x.blk, x.l0 + 1);
-            loads_done();
+            f32x4 o[4][CB];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) clear(o[r]);
+            if (x.l0 + 1 < x.l1) load_grad(x.blk, x.l0 + 1);
             __syncthreads();
             for (int l = x.l0; l < x.l1; ++l) {
                 uint16_t *now = G + ((l - x.l0) & 1) * 2 * kBlk * kGS, *then = G + ((l - x.l0 + 1) & 1) * 2 * kBlk * kGS;
-                if (l + 1 < x.l1) sg[0].store(then, then + kBlk * kGS);   // (its readers are a barrier behind)
-                if (l + 2 < x.l1) load_grad(0, x.blk, l + 2);
-                else if (l + 1 >= x.l1 && next_it < a.items) load_grad(0, nx.blk, nx.l0);
+                if (l + 1 < x.l1) sg.store(then, then + kBlk * kGS);   // (its readers are a barrier behind)
+                if (l + 2 < x.l1) load_grad(x.blk, l + 2);
                 dense(l, col0);
-                second(0, now, o);
+                round_v();
+#pragma unroll
+                for (int r = 0; r < 4; ++r) second(r, now, o[r]);
                 __syncthreads();
             }
-            if (next_it < a.items) stage_r(nx.blk);
-            store_rows<CB, SIDE>(a, o, x.blk, x.grp, col0, DP);
+            if (next_it < a.items) {
+                load_r(nx.blk);
+                load_grad(nx.blk, nx.l0);
+            }
+            Row_ids ids;
+            ids.load(a, x.blk);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) store_rows<CB, SIDE>(a, o[r], ids.id[r], x.blk, r, x.grp, col0, DP);
         } else {
-            sg[0].store(G, G + kBlk * kGS);
-            loads_done();
             __syncthreads();
             dense(0, col0);
-            __syncthreads();   // R's readers are done
-            if (next_it < a.items) stage_r(nx.blk);
-            clear(o);
-            second(0, G, o);
-            if constexpr (H == 2) {
-                store_rows<CB, SIDE>(a, o, x.blk, x.grp, col0, DP);
-                __syncthreads();
-                sg[H - 1].store(G, G + kBlk * kGS);
-                __syncthreads();
+            round_v();
+            __builtin_amdgcn_sched_barrier(0);   // (the registers of V hold the next R)
+            Row_ids ids;
+            ids.load(a, x.blk);
+            if (next_it < a.items) {
+                if constexpr (AHEAD) load_r(nx.blk);
+                load_grad(nx.blk, nx.l0);
             }
-            if (next_it < a.items)
 #pragma unroll
-                for (int h = 0; h < H; ++h) load_grad(h, nx.blk, 0);
-            if constexpr (H == 2) {
+            for (int r = 0; r < 4; ++r) {
+                f32x4 o[CB];
                 clear(o);
-                second(H - 1, G, o);
-                if (x.blk + 1 <= last_blk) store_rows<CB, SIDE>(a, o, x.blk + 1, x.grp, col0, DP);
-            } else {
-                store_rows<CB, SIDE>(a, o, x.blk, x.grp, col0, DP);
+                second(r, G, o);
+                store_rows<CB, SIDE>(a, o, ids.id[r], x.blk, r, x.grp, col0, DP);
             }
-            __syncthreads();   // G's readers are done
+            __syncthreads();   // the readers of R and G are done
         }
         if (next_it >= a.items) break;
         it = next_it;
@@ -556,11 +539,13 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
     }
 }
 
-template <int NB, int NW, int H, int CB, bool Q8, bool COMPACT>
-__global__ __launch_bounds__(64 * NW) void bwd_posts_kernel(BwdArgs a) {
+// (four wavefronts a SIMD, fewer with sums over labels beside V)
+constexpr int posts_waves(int cb, bool compact) { return !compact || cb == 1 ? 4 : cb == 2 ? 3 : 2; }
+template <int NB, int NW, int CB, bool Q8, bool COMPACT>
+__global__ __launch_bounds__(64 * NW, posts_waves(CB, COMPACT)) void bwd_posts_kernel(BwdArgs a) {
     extern __shared__ __align__(16) char smem[];
-    if (blockIdx.y + a.side0 == 0) bwd_posts<NB, NW, H, CB, Q8, COMPACT, 0>(a, smem);
-    else bwd_posts<NB, NW, H, CB, Q8, COMPACT, 1>(a, smem);
+    if (blockIdx.y + a.side0 == 0) bwd_posts<NB, NW, CB, Q8, COMPACT, 0>(a, smem);
+    else bwd_posts<NB, NW, CB, Q8, COMPACT, 1>(a, smem);
 }
 
 // The same of blocks of a sentence that has more than one, as (G R^r) W^T and
@@ -601,10 +586,10 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
 
     const int it = blockIdx.x;
     if (it >= a.items) return;
-    const Item x = item_of<1>(a, it);
+    const Item x = item_of(a, it);
     const int q0 = first_of(x.blk), q1 = last_of(x.blk), col0 = (x.cz * kLongWaves + wave) * CB;
     load_step(x.l0, x.blk, q0);
-    f32x4 acc[CB][4];
+    f32x4 acc[4][CB];
     for (int l = x.l0;;) {   // (one label, l = 0, unless COMPACT)
         f32x4 u[NB][4];
 #pragma unroll
@@ -650,7 +635,7 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
 #pragma unroll
             for (int c = 0; c < CB; ++c)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int r = 0; r < 4; ++r) acc[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
         const uint16_t *wf = weight_frags(a, l, SIDE, DP, col0), *prow = P + lr * PS + 8 * lg;
         for (int ks = 0; ks < ksteps; ++ks) {
             bf16x8 wv[CB];
@@ -660,12 +645,15 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
             for (int r = 0; r < 4; ++r) {
                 const bf16x8 pv = frag(prow + 16 * r * PS + 32 * ks);
 #pragma unroll
-                for (int c = 0; c < CB; ++c) acc[c][r] = mfma(wv[c], pv, acc[c][r]);
+                for (int c = 0; c < CB; ++c) acc[r][c] = mfma(wv[c], pv, acc[r][c]);
             }
         }
         if (!COMPACT || ++l >= x.l1) break;
     }
-    store_rows<CB, SIDE>(a, acc, x.blk, x.grp, col0, DP);
+    Row_ids ids;
+    ids.load(a, x.blk);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) store_rows<CB, SIDE>(a, acc[r], ids.id[r], x.blk, r, x.grp, col0, DP);
 }
 
 template <int NB, int CB, bool Q8, bool COMPACT>
@@ -697,8 +685,9 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 // registers, whose layout is that of the second product's operand when K is
 // numbered as in grad_frag, as hi and lo parts.  A step is a block and one of
 // its partners: U grows by their product, then R^r and G of the next step (and
-// [R^l ; 1] of the next block, into the other of its two places) start on their
-// way while [R^l ; 1]^T U of a block that has met all its partners is added.
+// [R^l ; 1] of the next block, into the other of its two places) go from
+// registers to LDS and those of the step after it start on their way, and
+// [R^l ; 1]^T U of a block that has met all its partners is added.
 //
 // The tiles of a share read the same posts: they are neighbours on one XCD, so
 // that a post's rows come from HBM once.
@@ -719,7 +708,7 @@ struct WeightShape {
 constexpr int kXcds = 8;
 
 template <int AB, int T, int NW, bool Q8, bool COMPACT>
-__global__ __launch_bounds__(64 * NW) void bwd_weight_kernel(WeightArgs a) {
+__global__ __launch_bounds__(64 * NW, 2) void bwd_weight_kernel(WeightArgs a) {
     extern __shared__ __align__(16) char smem[];
     typedef WeightShape<AB, T, NW> S;
     constexpr int TA = S::kA, TC = S::kC, AS = S::kAS, CS = S::kCS;
@@ -751,34 +740,20 @@ __global__ __launch_bounds__(64 * NW) void bwd_weight_kernel(WeightArgs a) {
     clear_u();
 
     auto last_of = [&](int blk) { return constant(a.posts + (size_t)blk * kPostRec + 2 * kBlk + 1); };
-    // Rows of a step on their way (bf16), or in registers (codes) and then stored.
     Staged<TA, NW, Q8> sa;
     Staged<TC, NW, Q8> sc;
     Staged_grad<NW> sg;
     auto post = [&](int blk) { return a.posts + (size_t)blk * kPostRec; };
     auto fetch = [&](int blk, int q) {
         sg.load(g, a.posts, blk, q);
-        if constexpr (Q8) {
-            sc.load(a.rr, post(q), c0, a.d);
-            if (q == blk) sa.load(a.rl, post(blk), a0, a.d);
-        }
+        sc.load(a.rr, post(q), c0, a.d);
+        if (q == blk) sa.load(a.rl, post(blk), a0, a.d);
     };
     auto stage = [&](int blk, int q) {
-        uint16_t *ra = Ra + (blk & 1) * kBlk * AS;
-        if constexpr (Q8) {
-            sc.template store<false>(a.rr, c0, a.d, Rc, CS);
-            if (q == blk) sa.template store<true>(a.rl, a0, a.d, ra, AS);
-        } else {
-            rows_to_lds<TC, NW>(a.rr, post(q), c0, a.d, Rc, CS);
-            if (q == blk) rows_to_lds<TA, NW>(a.rl, post(blk), a0, a.d, ra, AS);
-        }
+        sc.template store<false>(a.rr, c0, a.d, Rc, CS);
+        if (q == blk) sa.template store<true>(a.rl, a0, a.d, Ra + (blk & 1) * kBlk * AS, AS);
         sg.store(Gh, Gl);
     };
-    if constexpr (!Q8) {
-        set_ends<true>(Ra, 2 * kBlk, AS, a0, a.d);
-        set_ends<false>(Rc, kBlk, CS, c0, a.d);
-        __syncthreads();
-    }
     int blk = b0, q = b0, last = 0, nblk = b0, nq = b0;   // this step and the next
     auto advance = [&]() {
         if (nq < last) {
@@ -794,7 +769,6 @@ __global__ __launch_bounds__(64 * NW) void bwd_weight_kernel(WeightArgs a) {
         stage(b0, b0);
         advance();
         if (nblk < b1) fetch(nblk, nq);
-        loads_done();
         __syncthreads();
     }
     while (blk < b1) {
@@ -850,7 +824,6 @@ __global__ __launch_bounds__(64 * NW) void bwd_weight_kernel(WeightArgs a) {
             }
             clear_u();
         }
-        loads_done();
         __syncthreads();
         blk = nb;
         q = nqq;
@@ -896,7 +869,7 @@ __global__ __launch_bounds__(256) void bwd_join_weight_kernel(int d, int ldw, in
 
 inline int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
-constexpr int kCus = 256;
+constexpr int kCus = 256, kLdsPerCu = 163840;
 
 // How a call is cut up, and its workspace.
 struct BwdPlan {
@@ -934,22 +907,22 @@ BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     return b;
 }
 
-// Every build of bwd_posts_kernel: nb, few, then NB, NW, H, CB and the
-// workgroups of one that a CU holds; and of bwd_long_kernel: nb, few, NB, CB.
-#define CRF_BWD_POSTS(F)                                                                                     \
-    F(1, false, 1, 4, 1, 2, 2) F(2, false, 2, 8, (COMPACT ? 1 : 2), 2, 1) F(3, false, 3, 8, (COMPACT ? 1 : 2), 3, 1) \
-    F(4, false, 4, 8, (COMPACT ? 1 : 2), 4, 1) F(1, true, 1, 8, 1, 1, 1) F(2, true, 2, 8, 1, 1, 1)           \
-    F(3, true, 3, 8, 1, 1, 1) F(4, true, 4, 8, 1, 1, 1)
+// Every build of bwd_posts_kernel: nb, few, then NB, NW, CB; and of
+// bwd_long_kernel: nb, few, NB, CB.
+#define CRF_BWD_POSTS(F)                                                                            \
+    F(1, false, 1, 4, 2) F(2, false, 2, 8, 2) F(3, false, 3, 8, 3) F(4, false, 4, 8, 4) F(1, true, 1, 8, 1) \
+    F(2, true, 2, 8, 1) F(3, true, 3, 8, 1) F(4, true, 4, 8, 1)
 #define CRF_BWD_LONG(F) \
     F(1, false, 1, 1) F(2, false, 2, 2) F(3, false, 3, 3) F(4, false, 4, 4) F(2, true, 2, 1) F(3, true, 3, 1) F(4, true, 4, 1)
 
-template <int NB, int NW, int H, int CB, bool Q8, bool COMPACT>
-hipError_t launch_posts(BwdArgs a, int sides, int groups, int per_cu, hipStream_t stream) {
+template <int NB, int NW, int CB, bool Q8, bool COMPACT>
+hipError_t launch_posts(BwdArgs a, int sides, int groups, hipStream_t stream) {
     a.zs = 8 * NB / (NW * CB);
-    a.items = (a.blks + H - 1) / H * a.zs * groups;
-    const int slots = per_cu * kCus / sides;
-    hipLaunchKernelGGL((bwd_posts_kernel<NB, NW, H, CB, Q8, COMPACT>), dim3(std::min(a.items, slots), sides), dim3(64 * NW),
-                       (PostsShape<NB, NW, H, COMPACT>::kLds), stream, a);
+    a.items = a.blks * a.zs * groups;
+    const int lds = posts_lds<COMPACT>(a.d), regs = 4 * posts_waves(CB, COMPACT) / NW;   // workgroups a CU, by registers
+    const int slots = std::max(1, std::min(regs, kLdsPerCu / lds)) * kCus / sides;
+    hipLaunchKernelGGL((bwd_posts_kernel<NB, NW, CB, Q8, COMPACT>), dim3(std::min(a.items, slots), sides), dim3(64 * NW), lds,
+                       stream, a);
     return hipGetLastError();
 }
 template <int NB, int CB, bool Q8, bool COMPACT>
@@ -976,8 +949,8 @@ hipError_t launch_rows(const BwdPlan &b, BwdArgs a, int n_long, int sides, hipSt
     a.blk0 = n_long;
     a.blks = a.n_posts - n_long;
     if (a.blks == 0) return hipSuccess;
-#define CRF_LAUNCH(N, FEW, NB, NW, H, CB, PER) \
-    if (b.nb == N && b.few == FEW) return launch_posts<NB, NW, H, CB, Q8, COMPACT>(a, sides, b.groups, PER, stream);
+#define CRF_LAUNCH(N, FEW, NB, NW, CB) \
+    if (b.nb == N && b.few == FEW) return launch_posts<NB, NW, CB, Q8, COMPACT>(a, sides, b.groups, stream);
     CRF_BWD_POSTS(CRF_LAUNCH)
 #undef CRF_LAUNCH
     return hipErrorInvalidValue;
@@ -996,8 +969,8 @@ template <bool Q8, bool COMPACT>
 hipError_t set_attributes() {
     hipError_t e;
     auto set = [&](const void *f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-#define CRF_SET(N, FEW, NB, NW, H, CB, PER) \
-    if ((e = set((const void *)bwd_posts_kernel<NB, NW, H, CB, Q8, COMPACT>, PostsShape<NB, NW, H, COMPACT>::kLds)) != hipSuccess) return e;
+#define CRF_SET(N, FEW, NB, NW, CB) \
+    if ((e = set((const void *)bwd_posts_kernel<NB, NW, CB, Q8, COMPACT>, posts_lds<COMPACT>(kBiaMaxD))) != hipSuccess) return e;
     CRF_BWD_POSTS(CRF_SET)
 #undef CRF_SET
 #define CRF_SET(N, FEW, NB, CB) \
