@@ -493,22 +493,22 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
             f32x4 o[4][CB];
 #pragma unroll
             for (int r = 0; r < 4; ++r) clear(o[r]);
-            if (x.l0 + 1 < x.l1) load_grad(x.blk, x.l0 + 1);
+            load_grad(x.blk, min(x.l0 + 1, x.l1 - 1));
             __syncthreads();
             for (int l = x.l0; l < x.l1; ++l) {
                 uint16_t *now = G + ((l - x.l0) & 1) * 2 * kBlk * kGS, *then = G + ((l - x.l0 + 1) & 1) * 2 * kBlk * kGS;
-                if (l + 1 < x.l1) sg.store(then, then + kBlk * kGS);   // (its readers are a barrier behind)
-                if (l + 2 < x.l1) load_grad(x.blk, l + 2);
+                sg.store(then, then + kBlk * kGS);   // (its readers are a barrier behind)
+                load_grad(x.blk, min(l + 2, x.l1 - 1));
+                __builtin_amdgcn_sched_barrier(0);
                 dense(l, col0);
                 round_v();
 #pragma unroll
                 for (int r = 0; r < 4; ++r) second(r, now, o[r]);
                 __syncthreads();
             }
-            if (next_it < a.items) {
-                load_r(nx.blk);
-                load_grad(nx.blk, nx.l0);
-            }
+            load_r(nx.blk);
+            load_grad(nx.blk, nx.l0);
+            __builtin_amdgcn_sched_barrier(0);
             Row_ids ids;
             ids.load(a, x.blk);
 #pragma unroll
@@ -520,10 +520,9 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
             __builtin_amdgcn_sched_barrier(0);   // (the registers of V hold the next R)
             Row_ids ids;
             ids.load(a, x.blk);
-            if (next_it < a.items) {
-                if constexpr (AHEAD) load_r(nx.blk);
-                load_grad(nx.blk, nx.l0);
-            }
+            if constexpr (AHEAD) load_r(nx.blk);   // (past the last item, that one's again)
+            load_grad(nx.blk, nx.l0);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 f32x4 o[CB];
@@ -600,8 +599,8 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
             __syncthreads();   // the readers of what is stored next are done
             sr.template store<ONE>(rows, 0, a.d, P, PS);
             sg.store(Gh, Gl);
-            if (q < q1) load_step(l, x.blk, q + 1);
-            else if (COMPACT && l + 1 < x.l1) load_step(l + 1, x.blk, q0);
+            // the next partner, or the first one for the next label
+            load_step(COMPACT ? min(q < q1 ? l : l + 1, x.l1 - 1) : l, x.blk, q < q1 ? q + 1 : q0);
             __syncthreads();
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
@@ -858,6 +857,7 @@ __global__ __launch_bounds__(256) void bwd_join_weight_kernel(int d, int ldw, in
     const int col = 4 * (int)(t - row * per);
     const float *p = part + row * (d + 4) + col;
     f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int q = 0; q < splits; ++q) s += *reinterpret_cast<const f32x4 *>(p + (size_t)q * rows * (d + 4));
     float *at = out + row * ldw + col;
     if (col < d) *reinterpret_cast<f32x4 *>(at) = s;
@@ -887,13 +887,14 @@ BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     b.groups = std::max(1, std::min(L, 2 * kCus / p.n_posts));
     b.per_group = (L + b.groups - 1) / b.groups;
     b.groups = (L + b.per_group - 1) / b.per_group;
-    b.few = (int64_t)(p.n_posts - p.n_long_posts) * b.groups < kCus;
-    b.few_long = (int64_t)p.n_long_posts * b.groups < kCus;
+    // (both sides' items, each times nb, still fill at most two a CU, one a CU)
+    b.few = (int64_t)(p.n_posts - p.n_long_posts) * b.groups * b.nb <= kCus;
+    b.few_long = (int64_t)p.n_long_posts * b.groups * b.nb <= kCus / 2;
     b.wide = d + 1 > 128;
     const int tile = b.wide ? 256 : 128;
     b.tiles_a = (d + 1 + tile - 1) / tile;
     b.tiles = b.tiles_a * ((d + tile - 1) / tile);
-    b.splits = (int)std::max<int64_t>(1, std::min<int64_t>(p.n_posts, (b.wide ? 1 : 2) * kCus / ((int64_t)b.tiles * L)));
+    b.splits = (int)std::max<int64_t>(1, std::min<int64_t>((p.n_posts + 1) / 2, (b.wide ? 1 : 2) * kCus / ((int64_t)b.tiles * L)));
     int64_t at = 0;
     b.w_at = at;
     at += up256((int64_t)L * 2 * b.dp * b.dp * 2);
