@@ -277,17 +277,23 @@ __global__ __launch_bounds__(256) void bwd_compact_kernel(const int32_t *__restr
     const int id = rec[0];
     if (id < 0) return;   // (wavefronts share nothing)
     const int n = rec[kBlk];   // cells of the row
-    const float *src = g + square_cells[row] * L + l0;
-    const int64_t at = post_cells[row];
+    const int ls = min(64, L - l0);
+    const float *src = g + square_cells[row] * L + l0 + min(lane, ls - 1);
+    float *to = out + (int64_t)l0 * cells + post_cells[row];
+    const int c = lane % kTrCells, lhalf = lane / kTrCells;
     for (int j0 = 1; j0 <= n; j0 += kTrCells) {
         const int m = min(kTrCells, n + 1 - j0);
-        for (int c = 0; c < m; ++c)
-            if (l0 + lane < L) tile[wave][c][lane] = src[(int64_t)(j0 + c) * L + lane];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        for (int t = lane; t < 64 * kTrCells; t += 64) {
-            const int c = t % kTrCells, l = t / kTrCells;
-            if (c < m && l0 + l < L) out[(int64_t)(l0 + l) * cells + at + j0 + c] = tile[wave][c][l];
+        // eight loads in flight, the last cell's again at the end: no branch
+        for (int x = 0; x < m; x += 8) {
+            float v[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) v[t] = src[(int64_t)(j0 + min(x + t, m - 1)) * L];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) tile[wave][x + t][lane] = v[t];
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (c < m)
+            for (int l = lhalf; l < ls; l += 2) to[(int64_t)l * cells + j0 + c] = tile[wave][c][l];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
