@@ -890,7 +890,10 @@ BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     BwdPlan b{};
     b.nb = (d + 1 + 127) / 128;
     b.dp = 128 * b.nb;
-    b.groups = std::max(1, std::min(L, 2 * kCus / p.n_posts));
+    // (items for 3 workgroups a CU.  100 sentences, 138 labels, rows and the sums of
+    // the groups: 139 us with items for 2, 120 with 3 or 4, 123 with 6, whose sums
+    // cost more)
+    b.groups = std::max(1, std::min(L, 3 * kCus / p.n_posts));
     b.per_group = (L + b.groups - 1) / b.groups;
     b.groups = (L + b.per_group - 1) / b.per_group;
     // (both sides' items, each times nb, still fill at most two a CU, one a CU)
