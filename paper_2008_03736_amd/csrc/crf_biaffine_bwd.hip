@@ -680,6 +680,7 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
     const int col = 4 * (int)(t - slot * per), id = posts[slot / kBlk * kPostRec + slot % kBlk];
     if (id < 0) return;
     f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int q = 0; q < groups; ++q)
         s += *reinterpret_cast<const f32x4 *>(part + (((size_t)q * 2 + side) * n_posts * kBlk + slot) * dp + col);
     *reinterpret_cast<bf16x4 *>((side ? out_r : out_l) + (size_t)id * d + col) = __builtin_convertvector(s, bf16x4);
