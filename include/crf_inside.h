@@ -382,7 +382,8 @@ int crf_tree_logprobs_bwd(const crf_plan *plan, const float *scores, const int32
  *   ref_logp    device float32 [B][G], or NULL: no KL term (kl_coef is 0).
  *   clip_low    0 <= clip_low <= 1; clip_high >= 0; kl_coef >= 0.
  *   grad_loss   device float32[B] upstream gradient dOut/dL_b, or NULL for 1.
- *   loss        device float32[B]: L_b (not scaled by grad_loss).
+ *   loss        device float32[B]: L_b (not scaled by grad_loss).  loss and logp
+ *               must not alias an input.
  *   grad_scores device float32, layout of scores (must not alias scores):
  *               grad_loss[b] dL_b/ds(i,j) on valid cells only.
  * Unlabelled plans only (CRF_EUNSUPPORTED otherwise).
@@ -405,7 +406,8 @@ int crf_policy_loss(const crf_plan *plan, const float *scores, const int32_t *tr
  *   codes   device uint8 [B][N1][dc], dc = d rounded up to a multiple of 32,
  *           16-byte aligned: e4m3 (no infinities) bit patterns, zeros past d.
  *   scales  device uint8 [B][N1][dc/32]: s + 127.
- * Rows past n_b are left as they were.  B, N1 and the lengths are the plan's.
+ * Rows past n_b are left as they were.  x and codes must not alias.  B, N1 and
+ * the lengths are the plan's.
  */
 int crf_pack_rows(const crf_plan *plan, const uint16_t *x, int32_t d, uint8_t *codes, uint8_t *scales, void *stream);
 
@@ -434,7 +436,10 @@ int crf_biaffine_bwd_workspace(const crf_plan *plan, int32_t d, int32_t num_labe
  *               is rounded to bf16 once).
  *   grad_w      device float32 [num_labels][d][ldw], 16-byte aligned, or NULL:
  *               the layout of w; entries a <= d are written.
- * Sums run in a fixed order: equal calls give equal bits.
+ * Sums run in a fixed order: equal calls give equal bits.  Representations of
+ * valid fence posts and gradients of spans must be finite: sentences share
+ * tiles, so one's infinity or NaN can make the gradients of others NaN.  No
+ * gradient may alias an input or another one.
  */
 int crf_biaffine_bwd(const crf_plan *plan, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int32_t d,
                      int32_t ldw, int32_t num_labels, const float *grad_scores, uint16_t *grad_rl, uint16_t *grad_rr,

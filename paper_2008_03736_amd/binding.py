@@ -692,7 +692,8 @@ def tree_log_prob(scores, trees, plan, counts=None):
     return _LogP.apply(scores)
 
 
-def policy_loss(scores, trees, advantages, old_logp, plan, **options):
+def policy_loss(scores, trees, advantages, old_logp, plan, ref_logp=None, counts=None, clip_low=0.2, clip_high=0.2,
+                kl_coef=0.0):
     """Differentiable clipped policy loss, float32 [B] (Plan.policy_loss's
     arguments): the gradient is computed with the loss and kept."""
     import torch
@@ -700,7 +701,8 @@ def policy_loss(scores, trees, advantages, old_logp, plan, **options):
     class _Policy(torch.autograd.Function):
         @staticmethod
         def forward(ctx, s):
-            loss, _, grad = plan.policy_loss(s, trees, advantages, old_logp, **options)
+            loss, _, grad = plan.policy_loss(s, trees, advantages, old_logp, ref_logp=ref_logp, counts=counts,
+                                              clip_low=clip_low, clip_high=clip_high, kl_coef=kl_coef)
             ctx.save_for_backward(grad)
             return loss
 

@@ -136,6 +136,10 @@ int crf_policy_loss(const crf_plan *plan, const float *scores, const int32_t *tr
         grad_scores == nullptr)
         return fail(CRF_EINVAL, "scores/trees/advantages/old_logp/loss/grad_scores is NULL");
     if (scores == grad_scores) return fail(CRF_EINVAL, "grad_scores must not alias scores");
+    // (a long sentence's stripes each read them, and the first one writes)
+    const float *ins[] = {advantages, old_logp, ref_logp, grad_loss};
+    for (const float *in : ins)
+        if (in != nullptr && (in == loss || in == logp)) return fail(CRF_EINVAL, "loss and logp must not alias an input");
     if (!finite_positive(clip_low) || clip_low > 1.f)
         return fail(CRF_EINVAL, "clip_low %g outside [0, 1]", (double)clip_low);
     if (!finite_positive(clip_high))
@@ -160,6 +164,7 @@ int crf_pack_rows(const crf_plan *plan, const uint16_t *x, int32_t d, uint8_t *c
     if (rc != CRF_OK) return rc;
     if (misaligned(x, 8)) return fail(CRF_EINVAL, "x must be 8-byte aligned");
     if (misaligned(codes, 16)) return fail(CRF_EINVAL, "codes must be 16-byte aligned");
+    if (static_cast<const void *>(x) == codes) return fail(CRF_EINVAL, "x and codes must not alias");
     if ((rc = check_device(plan)) != CRF_OK) return rc;
     const hipError_t e = crf::launch_pack_rows(plan->kp, x, d, codes, scales, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_pack_rows launch");
@@ -173,6 +178,7 @@ int crf_unpack_rows(const crf_plan *plan, const uint8_t *codes, const uint8_t *s
     if (rc != CRF_OK) return rc;
     if (misaligned(x, 8)) return fail(CRF_EINVAL, "x must be 8-byte aligned");
     if (misaligned(codes, 16)) return fail(CRF_EINVAL, "codes must be 16-byte aligned");
+    if (static_cast<const void *>(x) == codes) return fail(CRF_EINVAL, "x and codes must not alias");
     if ((rc = check_device(plan)) != CRF_OK) return rc;
     const hipError_t e = crf::launch_unpack_rows(plan->kp, codes, scales, d, x, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_unpack_rows launch");

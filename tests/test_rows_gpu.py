@@ -152,3 +152,13 @@ def test_refusals(torch):
             B.crf_unpack_rows(plan._handle, c.data_ptr() + 1, s.data_ptr(), 8, x(8).data_ptr(), None)
         with pytest.raises(B.CrfError, match="8-byte"):
             B.crf_pack_rows(plan._handle, x(8).data_ptr() + 2, 8, c.data_ptr(), s.data_ptr(), None)
+
+
+def test_refused_aliases(torch):
+    dev = torch.device("cuda", 0)
+    with B.Plan([3, 5], n1=6, device=dev) as plan:
+        x, s = torch.zeros((2, 6, 32), dtype=torch.bfloat16, device=dev), torch.zeros((2, 6, 1), dtype=torch.uint8, device=dev)
+        with pytest.raises(B.CrfError, match="alias"):
+            B.crf_pack_rows(plan._handle, x.data_ptr(), 32, x.data_ptr(), s.data_ptr(), None)
+        with pytest.raises(B.CrfError, match="alias"):
+            B.crf_unpack_rows(plan._handle, x.data_ptr(), s.data_ptr(), 32, x.data_ptr(), None)

@@ -236,3 +236,18 @@ def test_refusals(torch):
         s3 = torch.zeros((2, b.n1, b.n1, 3), device=dev)
         with pytest.raises(B.CrfError, match="labelled"):
             plan.tree_logprobs(s3, t)
+
+
+def test_refused_aliases(torch):
+    # the stripes of a long sentence each read what one of them would overwrite
+    dev = torch.device("cuda", 0)
+    b = W.custom([4, 120], seed=0)
+    s = torch.from_numpy(b.scores).to(dev)
+    t = torch.from_numpy(T.random_trees(b.lengths, b.n1, 2, 0)).to(dev)
+    f, g, up = torch.zeros((2, 2), device=dev), torch.zeros((2, 2), device=dev), torch.ones(2, device=dev)
+    with B.Plan(b.lengths, n1=b.n1, device=dev) as plan:
+        for bad in (dict(logp=f), dict(logp=g), dict(ref_logp=up.repeat(2, 1), loss=up, grad_loss=up)):
+            with pytest.raises(B.CrfError, match="alias"):
+                plan.policy_loss(s, t, f, g, **bad)
+        with pytest.raises(TypeError):   # would scale the gradient but not the loss that it is the gradient of
+            B.policy_loss(s, t, f, g, plan, grad_loss=up)
