@@ -321,8 +321,9 @@ int crf_inside_fwd_bwd_cky_noalloc(const crf_plan *plan, const float *scores, co
  * Workspaces.  The calls below that take one use it, device memory of the
  * caller of at least the size that the plan's query gives, 256-byte aligned,
  * only while they run: calls that may overlap need one each (two graphs that
- * are replayed side by side too).  The calls still use the plan's own
- * workspace like the others, so calls on one plan must not overlap.
+ * are replayed side by side too).  The tree calls still use the plan's own
+ * workspace like the others, so they must not overlap other calls on the plan;
+ * packing, unpacking and the scorer's backward pass use nothing of it and may.
  */
 
 /* crf_tree_workspace -- bytes of workspace of crf_tree_logprobs and

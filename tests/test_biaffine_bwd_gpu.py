@@ -249,3 +249,59 @@ def test_refusals(torch):
         with pytest.raises(B.CrfError, match="workspace"):
             B.crf_biaffine_bwd(plan._handle, rl.data_ptr(), rr.data_ptr(), w.data_ptr(), 8, 12, 1, g.data_ptr(), None, None,
                                None, ws.data_ptr(), ws.numel() - 1, None)
+
+
+@pytest.mark.parametrize("at", ["first", "last"])
+def test_offsets_past_32_bits(torch, at):
+    # a labelled gradient of more than 2^31 entries, all zero but for one
+    # sentence; small integers, whose sums are exact, so that the bits are those
+    # of that sentence alone
+    dev = torch.device("cuda", 0)
+    n1, n, d, L, Bn = 141, 20, 4, 138, 800
+    assert Bn * n1 * n1 * L > 2 ** 31
+    k = 0 if at == "first" else Bn - 1
+    gen = torch.Generator(dev).manual_seed(3)
+    ints = lambda *s: torch.randint(-2, 3, s, device=dev, generator=gen)
+    rl, rr, w = (ints(*s).to(torch.bfloat16) for s in ((Bn, n1, d), (Bn, n1, d), (L, d, 8)))
+    g = torch.zeros((Bn, n1, n1, L), device=dev)
+    g[k] = ints(n1, n1, L)
+    with B.Plan([n] * Bn, n1=n1, device=dev) as plan:
+        got = plan.biaffine_bwd(rl, rr, w, g)
+    one = slice(k, k + 1)
+    with B.Plan([n], n1=n1, device=dev) as plan:
+        want = plan.biaffine_bwd(rl[one].contiguous(), rr[one].contiguous(), w, g[one].contiguous())
+    for x, y in zip(got[:2], want[:2]):
+        assert torch.equal(x[one], y) and int(x.count_nonzero()) == int(y.count_nonzero()) > 0
+    assert torch.equal(got[2], want[2])
+
+
+def test_two_graphs_side_by_side(torch):
+    # each with the workspace of its own pool, on streams of their own; eager
+    # work between the replays
+    dev = torch.device("cuda", 0)
+    lengths, d = [70, 20, 33, 5], 252
+    inp = W.biaffine_inputs(lengths, d, labels=2, seed=6)
+    rl, rr, w = tensors(torch, inp, 256, inp.n1)
+    g = torch.from_numpy(gradient(lengths, inp.n1, 2, 7)).to(dev)
+    grads = [g, g * 0.5]
+    with B.Plan(lengths, n1=inp.n1, device=dev) as plan:
+        want = [plan.biaffine_bwd(rl, rr, w, x) for x in grads]
+        graphs, outs = [], []
+        for x in grads:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                outs.append(plan.biaffine_bwd(rl, rr, w, x))
+            graphs.append(graph)
+        streams = [torch.cuda.Stream() for _ in graphs]
+        for _ in range(3):
+            for s, graph in zip(streams, graphs):
+                s.wait_stream(torch.cuda.current_stream())
+                with torch.cuda.stream(s):
+                    graph.replay()
+            for s in streams:
+                torch.cuda.current_stream().wait_stream(s)
+            plan.biaffine_bwd(rl, rr, w, grads[0])
+            torch.cuda.synchronize()
+            for out, y in zip(outs, want):
+                for a, b in zip(out, y):
+                    assert torch.equal(a, b)
