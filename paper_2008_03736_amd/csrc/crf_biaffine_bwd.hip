@@ -8,14 +8,23 @@
 // The products with G run inside blocks of 64 fence posts (KernelPlan::posts:
 // short sentences packed whole, longer ones cut, a block then meeting every
 // block of its sentence on its side of the diagonal), so that what they cost
-// is small beside the three dense products.
+// is small beside the three dense products.  Blocks of whole sentences multiply
+// by W first, dR^l = G (R^r W^T) and dR^r = G^T ([R^l ; 1] W), which keeps that
+// product in registers; blocks of longer ones by G first (U and X above), so
+// that the dense product is not repeated for each partner.
+//
+// What bounds it: the matrix cores, as far as staging lets them.  5,000
+// sentences (130,000 posts) at d = 500 need 2e11 operations, 160 us at the
+// 1.24e15 a second of a large library product, and 0.5 GB, 103 us.  All kernels
+// together take 500 us: rows 205 (whole sentences) and 23 (long ones), dW 257
+// and the sum of its shares 11, W's fragments 5.  From 8-bit rows 415 in all.
 //
 // Roundings.  R and W are bf16, products and sums fp32.  G, which is fp32, goes
 // in as bf16 hi + lo parts (at most 2^-16 of it is lost), and so does U into
-// dW, which comes out in fp32.  dR^l and dR^r come out in bf16, and there U and
-// X are rounded to bf16 once: each of the d terms of an output is off by at
-// most 2^-8 of itself, independently, as much as the output's own rounding
-// takes.
+// dW, which comes out in fp32.  dR^l and dR^r come out in bf16, and there the
+// inner product (R W or G R) is rounded to bf16 once: each term of an output is
+// off by at most 2^-8 of itself, independently, as much as the output's own
+// rounding takes.
 //
 // MFMA v_mfma_f32_16x16x32_bf16: lane l supplies A row l%16 and B column l%16
 // at K offsets 8(l/16)..+7 and holds D rows 4(l/16)..+3 of column l%16.  An
@@ -387,7 +396,8 @@ __device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB
 // wavefront holds V of its 16 CB columns for all 64 posts, which is the layout
 // of the second product's operand when K is numbered as in grad_frag: V,
 // rounded to bf16, never leaves the registers.  (As (G R) W^T, whose inner
-// product goes through LDS, 5,000 sentences at d = 500 took 252 us.)
+// product goes through LDS, 5,000 sentences at d = 500 took 252 us, this way
+// 205: 0.63e15 operations a second.)
 //
 // Two workgroups a CU (at d = 500 they fill its LDS): one's staging and stores
 // run beside the other's products.  With 128 posts a workgroup and one on a CU,
@@ -697,6 +707,12 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 //
 // The tiles of a share read the same posts: they are neighbours on one XCD, so
 // that a post's rows come from HBM once.
+//
+// 5,000 sentences at d = 500: 257 us, of which the matrix instructions take 90
+// (U's two parts and G's make the products twice as many).  The rest is what
+// two wavefronts a SIMD do not hide: staging's and splitting's arithmetic and
+// LDS reads between the barriers.  Two workgroups of four wavefronts a CU, tiles
+// of 256 x 128, whose phases drift apart, took 284: [R^l ; 1] is staged twice.
 struct WeightArgs {
     const int32_t *posts;
     const int64_t *post_cells;
@@ -897,13 +913,23 @@ BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     b.groups = std::max(1, std::min(L, 3 * kCus / p.n_posts));
     b.per_group = (L + b.groups - 1) / b.groups;
     b.groups = (L + b.per_group - 1) / b.per_group;
-    // (both sides' items, each times nb, still fill at most two a CU, one a CU)
+    // (both sides' items, each times nb, are then at most two a CU, or one a CU of
+    // the long kernel's.  One sentence of 25 words at d = 500: 8.5 us, 10.7 else;
+    // three of 80 words 15.3, 17.8 else.  With twice the bound 200 sentences took
+    // 22.2 and not 15, 5,000 with few long ones 48 for those and not 23: each of
+    // nb items stages the block anew, and the long ones' repeat U.)
     b.few = (int64_t)(p.n_posts - p.n_long_posts) * b.groups * b.nb <= kCus;
     b.few_long = (int64_t)p.n_long_posts * b.groups * b.nb <= kCus / 2;
+    // (a wide tile reads each row for half as many tiles: d = 500 259 us against
+    // 398 of narrow ones for 5,000 sentences, 21.7 against 22.0 for 200; where one
+    // narrow tile holds all it is the other way, d = 100 with 138 labels 73
+    // against 200)
     b.wide = d + 1 > 128;
     const int tile = b.wide ? 256 : 128;
     b.tiles_a = (d + 1 + tile - 1) / tile;
     b.tiles = b.tiles_a * ((d + tile - 1) / tile);
+    // (a share of two blocks at least: of one, 200 sentences at d = 500 take 10.3 us
+    // for the sum of the shares and not 7.6, and dW no less)
     b.splits = (int)std::max<int64_t>(1, std::min<int64_t>((p.n_posts + 1) / 2, (b.wide ? 1 : 2) * kCus / ((int64_t)b.tiles * L)));
     int64_t at = 0;
     b.w_at = at;

@@ -972,7 +972,7 @@ __device__ __forceinline__ f4 load_row(const float *sent, int N1, int i, int J, 
 // Inside (+ marginals) of a bundle: the tile form of inside_block_impl, same
 // outputs.  Returns false, having written no output, when a linear-domain
 // value leaves float32's range.
-template <bool LIN, bool REV, bool GOLD, bool GLOB>
+template <bool LIN, bool REV, bool GOLD, bool GLOB, bool Z64>
 __device__ __forceinline__ bool tile_inside_impl(const KernelPlan &p, const int32_t *rec, char *sm, char *lds,
                                                  const float *__restrict__ scores, const float *__restrict__ grad,
                                                  float *__restrict__ logZ, float *__restrict__ marg,
@@ -980,7 +980,7 @@ __device__ __forceinline__ bool tile_inside_impl(const KernelPlan &p, const int3
     typedef Dom<LIN> Dm;
     __shared__ int flags[kFlags];
     const int tid = this_thread(), NT = (int)blockDim.x, N1 = p.n1;
-    const Io_ctx<GLOB> cx = io_ctx<GLOB>(rec, lds, !GOLD && p.z64 != nullptr);
+    const Io_ctx<GLOB> cx = io_ctx<GLOB>(rec, lds, Z64 && p.z64 != nullptr);
     const int m = cx.m, S = cx.S;
     for (int sb = tid; sb < S; sb += NT) {
         const int id = rec[kTrHeader + 2 * sb];
@@ -1146,7 +1146,7 @@ __device__ __forceinline__ bool tile_inside_impl(const KernelPlan &p, const int3
     };
     if (logZ != nullptr)
         for (int sb = tid; sb < S; sb += NT) logZ[tab<int>(cx, kTabId, sb)] = (float)log_z(sb);
-    if constexpr (!GOLD) if (p.z64 != nullptr)
+    if constexpr (Z64) if (p.z64 != nullptr)
         for (int sb = tid; sb < S; sb += NT) p.z64[tab<int>(cx, kTabId, sb)] = log_z(sb);
     if constexpr (!REV) return true;
 
@@ -1252,15 +1252,16 @@ __device__ __forceinline__ bool tile_inside_impl(const KernelPlan &p, const int3
     return true;
 }
 
-template <bool REV, bool GOLD = false, bool GLOB = false>
+// Z64: the kernel's launches may ask for log Z in float64 (KernelPlan::z64).
+template <bool REV, bool GOLD = false, bool GLOB = false, bool Z64 = false>
 __device__ __forceinline__ void tile_inside(const KernelPlan &p, const int32_t *rec, char *sm, char *lds,
                                             const float *__restrict__ scores, const float *__restrict__ grad,
                                             float *__restrict__ logZ, float *__restrict__ marg,
                                             const int32_t *__restrict__ gold = nullptr,
                                             float *__restrict__ loss = nullptr) {
-    if (tile_inside_impl<true, REV, GOLD, GLOB>(p, rec, sm, lds, scores, grad, logZ, marg, gold, loss)) return;
+    if (tile_inside_impl<true, REV, GOLD, GLOB, Z64>(p, rec, sm, lds, scores, grad, logZ, marg, gold, loss)) return;
     __syncthreads();   // every thread has left the linear attempt
-    tile_inside_impl<false, REV, GOLD, GLOB>(p, rec, sm, lds, scores, grad, logZ, marg, gold, loss);
+    tile_inside_impl<false, REV, GOLD, GLOB, Z64>(p, rec, sm, lds, scores, grad, logZ, marg, gold, loss);
 }
 
 // ---------------------------------------------------------------------------
@@ -1660,7 +1661,7 @@ template <bool REV>
 CRF_TILE_KERNEL tile_inside_kernel(KernelPlan p, const float *__restrict__ scores, const float *__restrict__ grad,
                                    float *__restrict__ logZ, float *__restrict__ marg) {
     extern __shared__ __align__(16) char smem_raw[];
-    tile_inside<REV>(p, p.tile_io.recs + (size_t)blockIdx.x * p.tile_stride, smem_raw, smem_raw, scores, grad, logZ, marg);
+    tile_inside<REV, false, false, true>(p, p.tile_io.recs + (size_t)blockIdx.x * p.tile_stride, smem_raw, smem_raw, scores, grad, logZ, marg);
 }
 
 CRF_TILE_KERNEL tile_loss_kernel(KernelPlan p, const float *__restrict__ scores, const int32_t *__restrict__ gold,
@@ -1719,7 +1720,7 @@ CRF_TILE_WS_KERNEL tile_ws_inside_kernel(KernelPlan p, const float *__restrict__
                                       float *__restrict__ logZ, float *__restrict__ marg) {
     extern __shared__ __align__(16) char smem_raw[];
     const int32_t *rec = ws_record(p, 2 * (int)blockIdx.x);
-    tile_inside<REV, false, true>(p, rec, ws_chart(p, rec), smem_raw, scores, grad, logZ, marg);
+    tile_inside<REV, false, true, true>(p, rec, ws_chart(p, rec), smem_raw, scores, grad, logZ, marg);
 }
 
 CRF_TILE_WS_KERNEL tile_ws_loss_kernel(KernelPlan p, const float *__restrict__ scores, const int32_t *__restrict__ gold,
@@ -1784,8 +1785,8 @@ CRF_TILE_KERNEL tile_both_inside_kernel(KernelPlan p, const float *__restrict__ 
                                         float *__restrict__ logZ, float *__restrict__ marg) {
     extern __shared__ __align__(16) char smem_raw[];
     const Both_work k = both_work(p, p.tile_io, 1, 0);
-    if (k.glob) tile_inside<REV, false, true>(p, k.rec, ws_chart(p, k.rec), smem_raw, scores, grad, logZ, marg);
-    else tile_inside<REV>(p, k.rec, smem_raw, smem_raw, scores, grad, logZ, marg);
+    if (k.glob) tile_inside<REV, false, true, true>(p, k.rec, ws_chart(p, k.rec), smem_raw, scores, grad, logZ, marg);
+    else tile_inside<REV, false, false, true>(p, k.rec, smem_raw, smem_raw, scores, grad, logZ, marg);
 }
 
 CRF_TILE_KERNEL tile_both_loss_kernel(KernelPlan p, const float *__restrict__ scores, const int32_t *__restrict__ gold,
