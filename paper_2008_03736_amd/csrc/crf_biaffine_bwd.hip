@@ -15,9 +15,10 @@
 //
 // What bounds it: the matrix cores, as far as staging lets them.  5,000
 // sentences (130,000 posts) at d = 500 need 2e11 operations, 160 us at the
-// 1.24e15 a second of a large library product, and 0.5 GB, 103 us.  All kernels
-// together take 500 us: rows 205 (whole sentences) and 23 (long ones), dW 257
-// and the sum of its shares 11, W's fragments 5.  From 8-bit rows 415 in all.
+// 1.24e15 a second of a large library product, and 0.5 GB, 103 us.  A call
+// takes 447 us, from 8-bit rows 442.  Kernel by kernel, profiled in ten calls
+// from cold: rows 205 (whole sentences) and 23 (long ones), dW 257 and the sum
+// of its shares 11, W's fragments 5; all figures below are of such profiles.
 //
 // Roundings.  R and W are bf16, products and sums fp32.  G, which is fp32, goes
 // in as bf16 hi + lo parts (at most 2^-16 of it is lost), and so does U into
