@@ -16,8 +16,8 @@
 // What bounds it: the matrix cores, as far as staging lets them.  5,000
 // sentences (130,000 posts) at d = 500 need 2e11 operations, 160 us at the
 // 1.24e15 a second of a large library product, and 0.5 GB, 103 us.  A call
-// takes 447 us, from 8-bit rows 442.  Kernel by kernel, profiled in ten calls
-// from cold: rows 205 (whole sentences) and 23 (long ones), dW 257 and the sum
+// takes 442 us, from 8-bit rows 435.  Kernel by kernel, profiled in ten calls
+// from cold: rows 204 (whole sentences) and 23 (long ones), dW 250 and the sum
 // of its shares 11, W's fragments 5; all figures below are of such profiles.
 //
 // Roundings.  R and W are bf16, products and sums fp32.  G, which is fp32, goes
@@ -65,6 +65,12 @@ __device__ __forceinline__ bf16x8 frag_rows(const uint16_t *p0, const uint16_t *
 }
 __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Two float32 as bf16 parts hi + lo.
+__device__ __forceinline__ void parts(float a, float b, uint32_t &hi, uint32_t &lo) {
+    hi = two_bf16(a, b);
+    lo = two_bf16(a - __builtin_bit_cast(float, hi << 16), b - __builtin_bit_cast(float, hi & 0xFFFF0000u));
 }
 
 // Representations as the caller holds them: bf16 rows, or 8-bit codes and
@@ -191,6 +197,33 @@ struct Staged_grad {
     static constexpr int kRows = kBlk / NW;
     float v[kRows];
     uint32_t in;
+    // What does not depend on the label: where a row's cell (i, i+1) is, and a
+    // lane's place after it in bytes.  (Found anew for each label, the rows of 138
+    // labels took 72 us and not 62.)
+    struct Places {
+        int64_t cell[kRows];
+        uint32_t after[kRows], in;
+    };
+    static __device__ __forceinline__ Places places(const int64_t *cells, const int32_t *posts, int blk) {
+        const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int at = lane - kRows * w - 1;
+        Places p;
+        p.in = 0;
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            p.cell[u] = constant(cells + (size_t)blk * kBlk + kRows * w + u) + 1;
+            const bool ok = (uint32_t)(at - u) < (uint32_t)constant(posts + (size_t)blk * kPostRec + kBlk + kRows * w + u);
+            p.in |= ok ? 1u << u : 0u;
+            p.after[u] = ok ? 4u * (uint32_t)(at - u) : 0u;
+        }
+        return p;
+    }
+    __device__ __forceinline__ void load(const float *g, const Places &p) {
+        in = p.in;
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
+            v[u] = *reinterpret_cast<const float *>(reinterpret_cast<const char *>(g + p.cell[u]) + p.after[u]);
+    }
     __device__ __forceinline__ void load(const Grad &g, const int32_t *posts, int bi, int bj) {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int32_t *rest = posts + (size_t)bi * kPostRec + kBlk + kRows * w;
@@ -215,15 +248,14 @@ struct Staged_grad {
         const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
         for (int q = 0; q < kRows / 4; ++q) {
-            bf16x4 h, l;
+            float x[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float x = in >> (4 * q + u) & 1u ? v[4 * q + u] : 0.f;
-                h[u] = (__bf16)x;
-                l[u] = (__bf16)(x - (float)h[u]);
-            }
-            *reinterpret_cast<bf16x4 *>(hi + lane * kGS + kRows * w + 4 * q) = h;
-            *reinterpret_cast<bf16x4 *>(lo + lane * kGS + kRows * w + 4 * q) = l;
+            for (int u = 0; u < 4; ++u) x[u] = in >> (4 * q + u) & 1u ? v[4 * q + u] : 0.f;
+            uint2 h, l;
+            parts(x[0], x[1], h.x, l.x);
+            parts(x[2], x[3], h.y, l.y);
+            *reinterpret_cast<uint2 *>(hi + lane * kGS + kRows * w + 4 * q) = h;
+            *reinterpret_cast<uint2 *>(lo + lane * kGS + kRows * w + 4 * q) = l;
         }
     }
 };
@@ -398,7 +430,7 @@ __device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB
 // of the second product's operand when K is numbered as in grad_frag: V,
 // rounded to bf16, never leaves the registers.  (As (G R) W^T, whose inner
 // product goes through LDS, 5,000 sentences at d = 500 took 252 us, this way
-// 205: 0.63e15 operations a second.)
+// 204: 0.63e15 operations a second.)
 //
 // Two workgroups a CU (at d = 500 they fill its LDS): one's staging and stores
 // run beside the other's products.  With 128 posts a workgroup and one on a CU,
@@ -510,12 +542,13 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
             f32x4 o[4][CB];
 #pragma unroll
             for (int r = 0; r < 4; ++r) clear(o[r]);
-            load_grad(x.blk, min(x.l0 + 1, x.l1 - 1));
+            const typename Staged_grad<NW>::Places at = sg.places(a.post_cells, a.posts, x.blk);
+            sg.load(a.g + min(x.l0 + 1, x.l1 - 1) * a.cells, at);
             __syncthreads();
             for (int l = x.l0; l < x.l1; ++l) {
                 uint16_t *now = G + ((l - x.l0) & 1) * 2 * kBlk * kGS, *then = G + ((l - x.l0 + 1) & 1) * 2 * kBlk * kGS;
                 sg.store(then, then + kBlk * kGS);   // (its readers are a barrier behind)
-                load_grad(x.blk, min(l + 2, x.l1 - 1));
+                sg.load(a.g + min(l + 2, x.l1 - 1) * a.cells, at);
                 __builtin_amdgcn_sched_barrier(0);
                 dense(l, col0);
                 round_v();
@@ -709,7 +742,7 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 // The tiles of a share read the same posts: they are neighbours on one XCD, so
 // that a post's rows come from HBM once.
 //
-// 5,000 sentences at d = 500: 257 us, of which the matrix instructions take 90
+// 5,000 sentences at d = 500: 250 us, of which the matrix instructions take 90
 // (U's two parts and G's make the products twice as many).  The rest is what
 // two wavefronts a SIMD do not hide: staging's and splitting's arithmetic and
 // LDS reads between the barriers.  Two workgroups of four wavefronts a CU, tiles
@@ -824,14 +857,16 @@ __global__ __launch_bounds__(64 * NW, 2) void bwd_weight_kernel(WeightArgs a) {
             for (int kp = 0; kp < 2; ++kp) {
                 bf16x8 hi[T], lo[T];
 #pragma unroll
-                for (int c = 0; c < T; ++c)
-#pragma unroll
-                    for (int t = 0; t < 8; ++t) {
-                        const float v = u[2 * kp + (t >> 2)][c][t & 3];
-                        const __bf16 h = (__bf16)v;
-                        hi[c][t] = h;
-                        lo[c][t] = (__bf16)(v - (float)h);
-                    }
+                for (int c = 0; c < T; ++c) {
+                    const f32x4 &x = u[2 * kp][c], &y = u[2 * kp + 1][c];
+                    uint4 h, l;
+                    parts(x[0], x[1], h.x, l.x);
+                    parts(x[2], x[3], h.y, l.y);
+                    parts(y[0], y[1], h.z, l.z);
+                    parts(y[2], y[3], h.w, l.w);
+                    hi[c] = __builtin_bit_cast(bf16x8, h);
+                    lo[c] = __builtin_bit_cast(bf16x8, l);
+                }
                 const uint16_t *p = Ra + (blk & 1) * kBlk * AS + (32 * kp + 4 * lg + (lr >> 2)) * AS + 4 * (lr & 3);
                 bf16x8 af = frag_rows(p, p + 16 * AS);
 #pragma unroll
@@ -921,9 +956,9 @@ BwdPlan bwd_plan(const KernelPlan &p, int64_t cells, int d, int L) {
     // nb items stages the block anew, and the long ones' repeat U.)
     b.few = (int64_t)(p.n_posts - p.n_long_posts) * b.groups * b.nb <= kCus;
     b.few_long = (int64_t)p.n_long_posts * b.groups * b.nb <= kCus / 2;
-    // (a wide tile reads each row for half as many tiles: d = 500 259 us against
+    // (a wide tile reads each row for half as many tiles: d = 500 250 us against
     // 398 of narrow ones for 5,000 sentences, 21.7 against 22.0 for 200; where one
-    // narrow tile holds all it is the other way, d = 100 with 138 labels 73
+    // narrow tile holds all it is the other way, d = 100 with 138 labels 70
     // against 200)
     b.wide = d + 1 > 128;
     const int tile = b.wide ? 256 : 128;

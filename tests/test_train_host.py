@@ -107,6 +107,8 @@ def test_scratch_memory():
                  "bwd_posts_kernel", "bwd_long_kernel", "bwd_weight_kernel", "bwd_join_rows_kernel",
                  "bwd_join_weight_kernel"):
         assert any(part in x for x in names), part
+    # (two builds that decode 8-bit rows, once an item, outside the loops over K and labels)
+    least = {"bwd_posts_kernel<4, 8, 4, true, false>": 8, "bwd_posts_kernel<1, 4, 2, true, true>": 16}
     for r in rows:
-        allowed = 8 if "bwd_posts_kernel<4, 8, 4, true, false>" in r["kernel"] else 0
+        allowed = max([v for k, v in least.items() if k in r["kernel"]], default=0)
         assert int(r["ScratchSize [bytes/lane]"]) <= allowed, r["kernel"]
