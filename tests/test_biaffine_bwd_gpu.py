@@ -305,3 +305,26 @@ def test_two_graphs_side_by_side(torch):
             for out, y in zip(outs, want):
                 for a, b in zip(out, y):
                     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_some_gradients_of_labelled_scores(torch, packed):
+    # any of the three alone, and none: on another stream, from packed rows too
+    dev = torch.device("cuda", 0)
+    lengths, d, L = [9, 70, 1], 132, 3
+    inp = W.biaffine_inputs(lengths, d, labels=L, seed=1)
+    rl, rr, w = tensors(torch, inp, 136, inp.n1)
+    g = torch.from_numpy(gradient(lengths, inp.n1, L, 2)).to(dev)
+    side = torch.cuda.Stream()
+    with B.Plan(lengths, n1=inp.n1, device=dev) as plan:
+        if packed:
+            rl, rr = plan.pack_rows(rl), plan.pack_rows(rr)
+        every = plan.biaffine_bwd(rl, rr, w, g)
+        for k in range(8):
+            need = tuple(bool(k >> q & 1) for q in range(3))
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                got = plan.biaffine_bwd(rl, rr, w, g, need=need)
+            torch.cuda.current_stream().wait_stream(side)
+            for x, y, n in zip(got, every, need):
+                assert torch.equal(x, y) if n else x is None
