@@ -18,7 +18,7 @@
 // 1.24e15 a second of a large library product, and 0.5 GB, 103 us.  A call
 // takes 442 us, from 8-bit rows 435.  Kernel by kernel, profiled in ten calls
 // from cold: rows 204 (whole sentences) and 23 (long ones), dW 250 and the sum
-// of its shares 11, W's fragments 5; all figures below are of such profiles.
+// of its shares 11, W's fragments 4; all figures below are of such profiles.
 //
 // Roundings.  R and W are bf16, products and sums fp32.  G, which is fp32, goes
 // in as bf16 hi + lo parts (at most 2^-16 of it is lost), and so does U into
@@ -295,10 +295,19 @@ __global__ __launch_bounds__(256) void bwd_weights_kernel(const uint16_t *__rest
     const int side = (int)(q / nb / (dp / 32) & 1);
     const uint16_t *wl = w + (size_t)(q / nb / (dp / 32) >> 1) * d * ldw;
     uint16_t v[8];
+    if (side) {   // (a wavefront's pieces are of one side.  Fours of a row are inside it up to entry d's)
+        const bool in = col < d;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int c = side ? col : k + e, a = side ? k + e : col;
-        v[e] = c < d && a <= d ? wl[(size_t)c * ldw + a] : (uint16_t)0;
+        for (int h = 0; h < 2; ++h) {
+            const int a = k + 4 * h;
+            const uint2 x = in && a <= d ? *reinterpret_cast<const uint2 *>(wl + (size_t)col * ldw + a) : make_uint2(0u, 0u);
+            const uint32_t words[2] = {x.x, x.y};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * h + e] = a + e <= d ? (uint16_t)(words[e >> 1] >> (16 * (e & 1))) : (uint16_t)0;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = k + e < d && col <= d ? wl[(size_t)(k + e) * ldw + col] : (uint16_t)0;
     }
     *reinterpret_cast<uint4 *>(out + 8 * t) =
         make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
