@@ -313,6 +313,12 @@ class Plan:
             raise ValueError(f"{name} must be contiguous")
         return v.data_ptr()
 
+    def _rewritten(self, x):
+        """The library writes a buffer of the caller's: autograd refuses the
+        backward pass of what it has kept of it before."""
+        if x is not None and not x.is_inference():
+            self._torch.autograd.graph.increment_version(x)
+
     def inside_fwd(self, scores, logZ=None):
         """log Z per sentence (float32 [B])."""
         t = self._torch
@@ -367,6 +373,7 @@ class Plan:
             raise ValueError(f"spans must be contiguous int32 [{self.B}, {R}, 2]")
         if best is None:
             best = t.empty(self.B, dtype=t.float32, device=self.device)
+        self._rewritten(spans)
         crf_inside_fwd_bwd_cky(self._handle, sp, self._vec(grad_logZ, "grad_logZ"),
                                self._vec(logZ, "logZ"), marginals.data_ptr(), spans.data_ptr(),
                                self._vec(best, "best"), _stream_ptr(t, self.device))
@@ -408,6 +415,7 @@ class Plan:
         spans = self._spans_out(spans)
         if best is None:
             best = t.empty(self.B, dtype=t.float32, device=self.device)
+        self._rewritten(spans)
         crf_mbr_decode(self._handle, sp, self._vec(logZ, "logZ"), marginals.data_ptr(), spans.data_ptr(),
                        self._vec(best, "best"), _stream_ptr(t, self.device))
         return logZ, marginals, spans, best
@@ -440,6 +448,7 @@ class Plan:
         labels = self._labels_out(labels)
         if best is None:
             best = t.empty(self.B, dtype=t.float32, device=self.device)
+        self._rewritten(spans)
         crf_cky_decode_labeled(self._handle, sp, spans.data_ptr(), labels.data_ptr(), self._vec(best, "best"),
                                _stream_ptr(t, self.device))
         return spans, labels, best
@@ -480,6 +489,7 @@ class Plan:
             scores = t.full(shape, float("nan"), dtype=t.float32, device=self.device)
         elif tuple(scores.shape) != shape or scores.dtype != t.float32 or not scores.is_contiguous():
             raise ValueError(f"scores must be contiguous float32 {shape}")
+        self._rewritten(scores)
         crf_biaffine_scores(self._handle, rl.data_ptr(), rr.data_ptr(), w.data_ptr(), d, int(w.shape[2]), L,
                             scores.data_ptr(), _stream_ptr(t, self.device))
         return scores
@@ -599,6 +609,7 @@ class Plan:
         d = int(d)
         cp, sc = self._packed(codes, scales, d)
         out = self._out(out, (self.B, self.n1, d), t.bfloat16, zero=True)
+        self._rewritten(out)
         crf_unpack_rows(self._handle, cp, sc, d, self._bf16(out, "out", (self.B, self.n1, d)),
                         _stream_ptr(t, self.device))
         return out
@@ -646,6 +657,7 @@ class Plan:
             raise ValueError(f"spans must be contiguous int32 [{self.B}, {R}, 2]")
         if best is None:
             best = t.empty(self.B, dtype=t.float32, device=self.device)
+        self._rewritten(spans)
         crf_cky_decode(self._handle, sp, spans.data_ptr(), self._vec(best, "best"),
                        _stream_ptr(t, self.device))
         return spans, best
@@ -674,22 +686,24 @@ def log_partition(scores, plan):
 def tree_log_prob(scores, trees, plan, counts=None):
     """Differentiable log-probabilities of given trees (Sec. 2.1,
     Eq. tree-prob), float32 [B, G]: backward returns, per sentence, the trees'
-    upstream gradients on their spans less their sum times the marginals."""
+    upstream gradients on their spans less their sum times the marginals.
+    scores, trees and counts are kept for it, not copied: after a change in
+    place of one of them it raises."""
     import torch
 
     class _LogP(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, s):
-            ctx.save_for_backward(s)
+        def forward(ctx, s, trees, counts):
+            ctx.save_for_backward(s, trees, counts)
             return plan.tree_logprobs(s, trees, counts=counts)[0]
 
         @staticmethod
         def backward(ctx, g):
-            (s,) = ctx.saved_tensors
+            s, trees, counts = ctx.saved_tensors
             g = g.float().contiguous()   # held by this frame until the call has been enqueued
-            return plan.tree_logprobs_bwd(s, trees, g, counts=counts)
+            return plan.tree_logprobs_bwd(s, trees, g, counts=counts), None, None
 
-    return _LogP.apply(scores)
+    return _LogP.apply(scores, trees, counts)
 
 
 def policy_loss(scores, trees, advantages, old_logp, plan, ref_logp=None, counts=None, clip_low=0.2, clip_high=0.2,

@@ -1,0 +1,74 @@
+"""The differentiable forms around a stand-in plan, on the CPU: what they keep
+for the backward pass and what they refuse.  (The stand-in computes nothing;
+what it is handed is what is checked.)"""
+import pytest
+import torch
+
+from paper_2008_03736_amd import binding as B
+
+
+class StandIn:
+    """The Plan methods that the differentiable forms call, on CPU tensors."""
+    B, n1 = 2, 4
+
+    def tree_logprobs(self, scores, trees, counts=None):
+        return torch.zeros(trees.shape[:2]), None
+
+    def tree_logprobs_bwd(self, scores, trees, grad_logp, counts=None):
+        self.seen = trees.clone(), None if counts is None else counts.clone()
+        return torch.zeros_like(scores)
+
+
+def bare_plan(monkeypatch, *raw):
+    """A Plan without a library handle whose raw entry points `raw` do nothing."""
+    plan = object.__new__(B.Plan)
+    plan._torch, plan.device, plan._handle = torch, torch.device("cpu"), None
+    plan.B, plan.n1, plan.L = 2, 4, 1
+    monkeypatch.setattr(B, "_stream_ptr", lambda *a: 0)
+    for name in raw:
+        monkeypatch.setattr(B, name, lambda *a: None)
+    return plan
+
+
+@pytest.mark.parametrize("which", ["trees", "counts"])
+def test_trees_rewritten_before_the_backward_pass(which):
+    # the gradient is that of the trees of the forward pass, or it is refused
+    scores = torch.zeros((2, 4, 4), requires_grad=True)
+    kept = dict(trees=torch.zeros((2, 3, 5, 2), dtype=torch.int32), counts=torch.tensor([3, 2], dtype=torch.int32))
+    plan = StandIn()
+    B.tree_log_prob(scores, kept["trees"], plan, counts=kept["counts"]).sum().backward()
+    assert torch.equal(plan.seen[0], kept["trees"]) and torch.equal(plan.seen[1], kept["counts"])
+    logp = B.tree_log_prob(scores, kept["trees"], plan, counts=kept["counts"])
+    kept[which].add_(1)
+    with pytest.raises(RuntimeError, match="inplace"):
+        logp.sum().backward()
+
+
+@pytest.mark.parametrize("call", ["cky_decode", "parse", "mbr_decode"])
+def test_library_calls_count_as_rewriting(monkeypatch, call):
+    # a buffer of trees that a later decode fills again
+    plan = bare_plan(monkeypatch, "crf_cky_decode", "crf_inside_fwd_bwd_cky", "crf_mbr_decode")
+    scores = torch.zeros((2, 4, 4), requires_grad=True)
+    buf = torch.zeros((2, 5, 2), dtype=torch.int32)
+    logp = B.tree_log_prob(scores, buf[:, None], StandIn())
+    getattr(plan, call)(scores.detach(), spans=buf)
+    with pytest.raises(RuntimeError, match="inplace"):
+        logp.sum().backward()
+
+
+def test_scores_that_the_scorer_fills_again(monkeypatch):
+    plan = bare_plan(monkeypatch, "crf_biaffine_scores")
+    scores = torch.zeros((2, 4, 4), requires_grad=True)
+    logp = B.tree_log_prob(scores, torch.zeros((2, 1, 5, 2), dtype=torch.int32), StandIn())
+    x, w = torch.zeros((2, 4, 8), dtype=torch.int16), torch.zeros((1, 8, 12), dtype=torch.int16)
+    plan.biaffine_scores(x, x, w, scores=scores.detach())
+    with pytest.raises(RuntimeError, match="inplace"):
+        logp.sum().backward()
+
+
+def test_inference_buffers_are_taken(monkeypatch):
+    plan = bare_plan(monkeypatch, "crf_cky_decode")
+    with torch.inference_mode():
+        buf = torch.zeros((2, 5, 2), dtype=torch.int32)
+        assert plan.cky_decode(torch.zeros((2, 4, 4)), spans=buf)[0] is buf
+    assert plan.cky_decode(torch.zeros((2, 4, 4)), spans=buf)[0] is buf
