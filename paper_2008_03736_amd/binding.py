@@ -738,6 +738,9 @@ def biaffine(rl, rr, w, plan, held="bf16"):
 
     if held not in ("bf16", "8bit"):
         raise ValueError('held must be "bf16" or "8bit"')
+    for x, name in ((rl, "rl"), (rr, "rr"), (w, "w")):
+        if x.dtype not in (torch.bfloat16, torch.int16, torch.uint16):
+            raise ValueError(f"{name} must be bfloat16 (or its bit patterns), got {x.dtype}")
 
     class _Biaffine(torch.autograd.Function):
         @staticmethod

@@ -72,3 +72,42 @@ def test_inference_buffers_are_taken(monkeypatch):
         buf = torch.zeros((2, 5, 2), dtype=torch.int32)
         assert plan.cky_decode(torch.zeros((2, 4, 4)), spans=buf)[0] is buf
     assert plan.cky_decode(torch.zeros((2, 4, 4)), spans=buf)[0] is buf
+
+
+class Scorer:
+    """A plan that only counts what biaffine hands it."""
+    B, n1 = 2, 4
+
+    def __init__(self):
+        self.packed = self.scored = 0
+
+    def biaffine_scores(self, rl, rr, w, scores=None):
+        self.scored += 1
+
+    def pack_rows(self, x):
+        self.packed += 1
+        return x.clone(), x.clone()
+
+    def biaffine_bwd(self, rl, rr, w, g, need=None):
+        return torch.zeros((2, 4, 8)), torch.zeros((2, 4, 8)), torch.zeros(w.shape)
+
+
+def rows_and_w(dtype=torch.bfloat16):
+    return (torch.zeros((2, 4, 8), dtype=dtype), torch.zeros((2, 4, 8), dtype=dtype),
+            torch.zeros((1, 8, 12), dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("held", ["bf16", "8bit"])
+@pytest.mark.parametrize("at", [0, 1, 2])
+def test_representations_of_another_type(held, at):
+    # 16 bits of another kind would be read as bf16 (its bit patterns are taken)
+    args = list(rows_and_w())
+    plan = Scorer()
+    B.biaffine(*args, plan, held=held)
+    args[at] = args[at].view(torch.int16)
+    B.biaffine(*args, plan, held=held)
+    assert plan.scored == 2
+    args[at] = args[at].view(torch.float16)
+    with torch.no_grad(), pytest.raises(ValueError, match="bfloat16"):
+        B.biaffine(*args, plan, held=held)
+    assert plan.scored == 2
