@@ -741,6 +741,7 @@ def biaffine(rl, rr, w, plan, held="bf16"):
     for x, name in ((rl, "rl"), (rr, "rr"), (w, "w")):
         if x.dtype not in (torch.bfloat16, torch.int16, torch.uint16):
             raise ValueError(f"{name} must be bfloat16 (or its bit patterns), got {x.dtype}")
+    differentiable = torch.is_grad_enabled() and any(x.requires_grad for x in (rl, rr, w))
 
     class _Biaffine(torch.autograd.Function):
         @staticmethod
@@ -749,8 +750,9 @@ def biaffine(rl, rr, w, plan, held="bf16"):
             shape = (plan.B, plan.n1, plan.n1) if L == 1 else (plan.B, plan.n1, plan.n1, L)
             scores = torch.zeros(shape, dtype=torch.float32, device=rl.device)
             plan.biaffine_scores(rl.view(torch.int16), rr.view(torch.int16), w.view(torch.int16), scores=scores)
-            kept = (*plan.pack_rows(rl), *plan.pack_rows(rr)) if held == "8bit" else (rl, rr)
-            ctx.save_for_backward(w, *kept)
+            if differentiable:
+                kept = (*plan.pack_rows(rl), *plan.pack_rows(rr)) if held == "8bit" else (rl, rr)
+                ctx.save_for_backward(w, *kept)
             return scores
 
         @staticmethod

@@ -111,3 +111,15 @@ def test_representations_of_another_type(held, at):
     with torch.no_grad(), pytest.raises(ValueError, match="bfloat16"):
         B.biaffine(*args, plan, held=held)
     assert plan.scored == 2
+
+
+def test_rows_are_packed_only_for_a_backward_pass():
+    plan = Scorer()
+    rl, rr, w = rows_and_w()
+    B.biaffine(rl, rr, w, plan, held="8bit")                       # nothing needs a gradient
+    with torch.no_grad():
+        B.biaffine(rl.clone().requires_grad_(True), rr, w, plan, held="8bit")
+    assert plan.packed == 0 and plan.scored == 2
+    for args in ((rl.clone().requires_grad_(True), rr, w), (rl, rr, w.clone().requires_grad_(True))):
+        B.biaffine(*args, plan, held="8bit").sum().backward()
+    assert plan.packed == 4
