@@ -675,6 +675,7 @@ def log_partition(scores, plan):
             return plan.inside_fwd(s)
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, g):
             (s,) = ctx.saved_tensors
             g = g.float().contiguous()   # held by this frame until the call has been enqueued
@@ -698,6 +699,7 @@ def tree_log_prob(scores, trees, plan, counts=None):
             return plan.tree_logprobs(s, trees, counts=counts)[0]
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, g):
             s, trees, counts = ctx.saved_tensors
             g = g.float().contiguous()   # held by this frame until the call has been enqueued
@@ -721,6 +723,7 @@ def policy_loss(scores, trees, advantages, old_logp, plan, ref_logp=None, counts
             return loss
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, g):
             (grad,) = ctx.saved_tensors
             return grad * g[:, None, None]
@@ -756,6 +759,7 @@ def biaffine(rl, rr, w, plan, held="bf16"):
             return scores
 
         @staticmethod
+        @torch.autograd.function.once_differentiable
         def backward(ctx, g):
             w, *kept = ctx.saved_tensors
             rl, rr = (kept[:2], kept[2:]) if held == "8bit" else kept

@@ -123,3 +123,43 @@ def test_rows_are_packed_only_for_a_backward_pass():
     for args in ((rl.clone().requires_grad_(True), rr, w), (rl, rr, w.clone().requires_grad_(True))):
         B.biaffine(*args, plan, held="8bit").sum().backward()
     assert plan.packed == 4
+
+
+class Loss:
+    """A plan whose log Z and losses are functions of the scores' sums."""
+    B, n1 = 2, 4
+
+    def inside_fwd(self, s):
+        return s.sum((1, 2)) ** 3
+
+    def inside_bwd(self, s, grad_logZ=None):
+        return (3 * s.sum((1, 2)) ** 2 * grad_logZ)[:, None, None].expand_as(s).contiguous()
+
+    def tree_logprobs(self, s, trees, counts=None):
+        return (s.sum((1, 2)) ** 3)[:, None].expand(trees.shape[:2]).contiguous(), None
+
+    def tree_logprobs_bwd(self, s, trees, g, counts=None):
+        return self.inside_bwd(s, grad_logZ=g.sum(1))
+
+    def policy_loss(self, s, trees, *args, **kw):
+        return s.sum((1, 2)) ** 3, None, self.inside_bwd(s, grad_logZ=torch.ones(2))
+
+
+@pytest.mark.parametrize("form", ["log_partition", "tree_log_prob", "policy_loss", "biaffine"])
+def test_second_derivatives_are_refused(form):
+    # (silently left out of them else: the gradients are no functions of the
+    # scores to autograd)
+    s = torch.ones((2, 4, 4), requires_grad=True)
+    trees = torch.zeros((2, 1, 5, 2), dtype=torch.int32)
+    if form == "biaffine":
+        x = rows_and_w()
+        leaf = x[0].clone().requires_grad_(True)
+        out = B.biaffine(leaf, *x[1:], Scorer())
+    else:
+        leaf = s
+        out = {"log_partition": lambda: B.log_partition(s, Loss()),
+               "tree_log_prob": lambda: B.tree_log_prob(s, trees, Loss()),
+               "policy_loss": lambda: B.policy_loss(s, trees, None, None, Loss())}[form]()
+    (g,) = torch.autograd.grad(out.sum() ** 2, leaf, create_graph=True)   # the gradient itself is there
+    with pytest.raises(RuntimeError, match="differentiate twice"):
+        (g.sum() + leaf.sum()).backward()
