@@ -733,23 +733,29 @@ def policy_loss(scores, trees, advantages, old_logp, plan, ref_logp=None, counts
 
 def biaffine(rl, rr, w, plan, held="bf16"):
     """Differentiable span (or label) scores from boundary representations
-    (Sec. 2.2, Eq. biaffine): rl, rr bfloat16 [B, N1, d], w bfloat16
-    [L, d, ldw]; cells that are no spans are 0.  held="8bit": the backward pass
-    keeps the representations in 8 bits (Plan.pack_rows) and gives the
-    gradients at the values those stand for."""
+    (Sec. 2.2, Eq. biaffine): rl, rr bfloat16 [B, N1, d], w bfloat16 or float32
+    [L, d, ldw]; cells that are no spans are 0.  A float32 w enters the products
+    rounded to bfloat16 and gets its gradient in float32, as it is computed; a
+    bfloat16 one gets it rounded.  held="8bit": the backward pass keeps the
+    representations in 8 bits (Plan.pack_rows) and gives the gradients at the
+    values those stand for."""
     import torch
 
     if held not in ("bf16", "8bit"):
         raise ValueError('held must be "bf16" or "8bit"')
-    for x, name in ((rl, "rl"), (rr, "rr"), (w, "w")):
-        if x.dtype not in (torch.bfloat16, torch.int16, torch.uint16):
-            raise ValueError(f"{name} must be bfloat16 (or its bit patterns), got {x.dtype}")
+    bf16 = (torch.bfloat16, torch.int16, torch.uint16)
+    for x, name, types in ((rl, "rl", bf16), (rr, "rr", bf16), (w, "w", (*bf16, torch.float32))):
+        if x.dtype not in types:
+            raise ValueError(f"{name} must be bfloat16 (or its bit patterns; w also float32), got {x.dtype}")
     differentiable = torch.is_grad_enabled() and any(x.requires_grad for x in (rl, rr, w))
 
     class _Biaffine(torch.autograd.Function):
         @staticmethod
         def forward(ctx, rl, rr, w):
             L = w.shape[0]
+            ctx.w_type = w.dtype
+            if w.dtype == torch.float32:
+                w = w.to(torch.bfloat16)
             shape = (plan.B, plan.n1, plan.n1) if L == 1 else (plan.B, plan.n1, plan.n1, L)
             scores = torch.zeros(shape, dtype=torch.float32, device=rl.device)
             plan.biaffine_scores(rl.view(torch.int16), rr.view(torch.int16), w.view(torch.int16), scores=scores)
@@ -767,7 +773,7 @@ def biaffine(rl, rr, w, plan, held="bf16"):
             need = ctx.needs_input_grad
             if not any(need):
                 return None, None, None
-            grads = plan.biaffine_bwd(rl, rr, w, g, need=need)
-            return tuple(x if x is None else x.to(torch.bfloat16) for x in grads)
+            grad_rl, grad_rr, grad_w = plan.biaffine_bwd(rl, rr, w, g, need=need)
+            return grad_rl, grad_rr, None if grad_w is None else grad_w.to(ctx.w_type)
 
     return _Biaffine.apply(rl, rr, w)

@@ -163,3 +163,25 @@ def test_second_derivatives_are_refused(form):
     (g,) = torch.autograd.grad(out.sum() ** 2, leaf, create_graph=True)   # the gradient itself is there
     with pytest.raises(RuntimeError, match="differentiate twice"):
         (g.sum() + leaf.sum()).backward()
+
+
+def test_float32_w_gets_the_float32_gradient():
+    third = torch.full((1, 8, 12), 1.0 / 3.0)
+
+    class Thirds(Scorer):
+        def biaffine_scores(self, rl, rr, w, scores=None):
+            self.w = w.view(torch.bfloat16)
+
+        def biaffine_bwd(self, rl, rr, w, g, need=None):
+            assert w.dtype == torch.bfloat16
+            return None, None, third
+
+    rl, rr, _ = rows_and_w()
+    for held in ("bf16", "8bit"):
+        plan, w = Thirds(), (third + 1.0).requires_grad_(True)
+        B.biaffine(rl, rr, w, plan, held=held).sum().backward()
+        assert torch.equal(plan.w, w.detach().to(torch.bfloat16))   # the products' operand
+        assert w.grad.dtype == torch.float32 and torch.equal(w.grad, third)
+        w = third.to(torch.bfloat16).requires_grad_(True)
+        B.biaffine(rl, rr, w, plan, held=held).sum().backward()
+        assert w.grad.dtype == torch.bfloat16 and torch.equal(w.grad, third.to(torch.bfloat16))
