@@ -324,6 +324,8 @@ int crf_inside_fwd_bwd_cky_noalloc(const crf_plan *plan, const float *scores, co
  * are replayed side by side too).  The tree calls still use the plan's own
  * workspace like the others, so they must not overlap other calls on the plan;
  * packing, unpacking and the scorer's backward pass use nothing of it and may.
+ * In all of them no output, and not the workspace, may overlap an input or
+ * another output (CRF_EINVAL, by the arrays' full sizes).
  */
 
 /* crf_tree_workspace -- bytes of workspace of crf_tree_logprobs and

@@ -4,6 +4,7 @@
 
 #include <atomic>
 #include <cstring>
+#include <initializer_list>
 
 #include "../../include/crf_inside.h"
 #include "crf_plan.h"
@@ -24,6 +25,34 @@ bool finite_positive(float x) {
 }
 
 bool misaligned(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+// A buffer of a call.
+struct Span {
+    const char *name;
+    const void *at;   // NULL: not given
+    int64_t bytes;
+};
+bool overlap(const Span &a, const Span &b) {
+    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+    return x != 0 && y != 0 && x < y + (uintptr_t)b.bytes && y < x + (uintptr_t)a.bytes;
+}
+// No output (the workspace is one) may share a byte with an input or another
+// output: a call's workgroups read inputs while others write.
+int check_overlap(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+    for (const Span *o = outs.begin(); o != outs.end(); ++o) {
+        for (const Span &i : ins)
+            if (overlap(*o, i)) return fail(CRF_EINVAL, "%s must not alias %s", o->name, i.name);
+        for (const Span *q = outs.begin(); q != o; ++q)
+            if (overlap(*o, *q)) return fail(CRF_EINVAL, "%s and %s must not alias", q->name, o->name);
+    }
+    return CRF_OK;
+}
+// Bytes of the arrays that calls share.
+int64_t scores_bytes(const crf_plan *p, int64_t num_labels) { return 4 * num_labels * p->B * p->n1 * p->n1; }
+int64_t trees_bytes(const crf_plan *p, int64_t num_trees) { return 8 * num_trees * p->B * (2 * (p->n1 - 1) - 1); }
+int64_t rows_bytes(const crf_plan *p, int64_t entry, int64_t per_row) { return entry * per_row * p->B * p->n1; }
+int64_t vec_bytes(const crf_plan *p) { return 4 * (int64_t)p->B; }
+int64_t row_codes(int64_t d) { return (d + 31) / 32 * 32; }
 
 int check_workspace(const void *workspace, int64_t have, int64_t need) {
     if (workspace == nullptr) return fail(CRF_EINVAL, "workspace is NULL");
@@ -68,14 +97,16 @@ int scorer_backward(const crf_plan *plan, const void *rl, const uint8_t *rl_scal
     if (rc != CRF_OK) return rc;
     if (misaligned(grad_rl, 8) || misaligned(grad_rr, 8)) return fail(CRF_EINVAL, "grad_rl/grad_rr must be 8-byte aligned");
     if (misaligned(grad_w, 16)) return fail(CRF_EINVAL, "grad_w must be 16-byte aligned");
-    const void *ins[] = {rl, rr, rl_scales, rr_scales, w, grad_scores};
-    const void *outs[] = {grad_rl, grad_rr, grad_w};
-    for (const void *o : outs)
-        for (const void *i : ins)
-            if (o != nullptr && o == i) return fail(CRF_EINVAL, "a gradient must not alias an input");
-    if (grad_rl != nullptr && grad_rl == grad_rr) return fail(CRF_EINVAL, "grad_rl and grad_rr must not alias");
-    if ((rc = check_workspace(workspace, workspace_bytes, crf::biaffine_bwd_bytes(plan->kp, plan->cells, d, num_labels))) !=
-            CRF_OK ||
+    const int64_t need = crf::biaffine_bwd_bytes(plan->kp, plan->cells, d, num_labels);
+    const int64_t bf16 = rows_bytes(plan, 2, d), w_entries = (int64_t)num_labels * d * ldw;
+    const int64_t rows = rl_scales != nullptr ? rows_bytes(plan, 1, row_codes(d)) : bf16;
+    const int64_t scales = rows_bytes(plan, 1, row_codes(d) / 32);
+    if ((rc = check_workspace(workspace, workspace_bytes, need)) != CRF_OK ||
+        (rc = check_overlap({{"grad_rl", grad_rl, bf16}, {"grad_rr", grad_rr, bf16}, {"grad_w", grad_w, 4 * w_entries},
+                             {"workspace", workspace, need}},
+                            {{"rl", rl, rows}, {"rr", rr, rows}, {"rl_scales", rl_scales, scales},
+                             {"rr_scales", rr_scales, scales}, {"w", w, 2 * w_entries},
+                             {"grad_scores", grad_scores, scores_bytes(plan, num_labels)}})) != CRF_OK ||
         (rc = check_device(plan)) != CRF_OK)
         return rc;
     // best effort, as for the other kernels: a real shortfall surfaces as a launch error
@@ -105,7 +136,12 @@ int crf_tree_logprobs(const crf_plan *plan, const float *scores, const int32_t *
     if (scores == nullptr || trees == nullptr || logp == nullptr)
         return fail(CRF_EINVAL, "scores/trees/logp is NULL");
     int rc = check_trees(plan, trees, num_trees);
-    if (rc != CRF_OK || (rc = check_workspace(workspace, workspace_bytes, tree_bytes(plan))) != CRF_OK ||
+    if (rc != CRF_OK) return rc;
+    const int64_t each = num_trees * vec_bytes(plan);
+    if ((rc = check_workspace(workspace, workspace_bytes, tree_bytes(plan))) != CRF_OK ||
+        (rc = check_overlap({{"logp", logp, each}, {"logZ", logZ, vec_bytes(plan)}, {"workspace", workspace, tree_bytes(plan)}},
+                            {{"scores", scores, scores_bytes(plan, 1)}, {"trees", trees, trees_bytes(plan, num_trees)},
+                             {"counts", counts, vec_bytes(plan)}})) != CRF_OK ||
         (rc = check_device(plan)) != CRF_OK)
         return rc;
     const hipError_t e = crf::launch_tree_logprobs(plan->kp, scores, trees, num_trees, counts,
@@ -119,9 +155,14 @@ int crf_tree_logprobs_bwd(const crf_plan *plan, const float *scores, const int32
     if (plan == nullptr) return fail(CRF_EINVAL, "plan is NULL");
     if (scores == nullptr || trees == nullptr || grad_logp == nullptr || grad_scores == nullptr)
         return fail(CRF_EINVAL, "scores/trees/grad_logp/grad_scores is NULL");
-    if (scores == grad_scores) return fail(CRF_EINVAL, "grad_scores must not alias scores");
     int rc = check_trees(plan, trees, num_trees);
-    if (rc != CRF_OK || (rc = check_device(plan)) != CRF_OK) return rc;
+    if (rc != CRF_OK) return rc;
+    if ((rc = check_overlap({{"grad_scores", grad_scores, scores_bytes(plan, 1)}},
+                            {{"scores", scores, scores_bytes(plan, 1)}, {"trees", trees, trees_bytes(plan, num_trees)},
+                             {"counts", counts, vec_bytes(plan)}, {"grad_logp", grad_logp, num_trees * vec_bytes(plan)}})) !=
+            CRF_OK ||
+        (rc = check_device(plan)) != CRF_OK)
+        return rc;
     const hipError_t e = crf::launch_tree_logprobs_bwd(plan->kp, scores, trees, num_trees, counts,
                                                        grad_logp, grad_scores, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_tree_logprobs_bwd launch");
@@ -135,11 +176,6 @@ int crf_policy_loss(const crf_plan *plan, const float *scores, const int32_t *tr
     if (scores == nullptr || trees == nullptr || advantages == nullptr || old_logp == nullptr || loss == nullptr ||
         grad_scores == nullptr)
         return fail(CRF_EINVAL, "scores/trees/advantages/old_logp/loss/grad_scores is NULL");
-    if (scores == grad_scores) return fail(CRF_EINVAL, "grad_scores must not alias scores");
-    // (a long sentence's stripes each read them, and the first one writes)
-    const float *ins[] = {advantages, old_logp, ref_logp, grad_loss};
-    for (const float *in : ins)
-        if (in != nullptr && (in == loss || in == logp)) return fail(CRF_EINVAL, "loss and logp must not alias an input");
     if (!finite_positive(clip_low) || clip_low > 1.f)
         return fail(CRF_EINVAL, "clip_low %g outside [0, 1]", (double)clip_low);
     if (!finite_positive(clip_high))
@@ -147,7 +183,15 @@ int crf_policy_loss(const crf_plan *plan, const float *scores, const int32_t *tr
     if (!finite_positive(kl_coef)) return fail(CRF_EINVAL, "kl_coef %g is negative or not finite", (double)kl_coef);
     if (kl_coef != 0.f && ref_logp == nullptr) return fail(CRF_EINVAL, "kl_coef %g without ref_logp", (double)kl_coef);
     int rc = check_trees(plan, trees, num_trees);
-    if (rc != CRF_OK || (rc = check_workspace(workspace, workspace_bytes, tree_bytes(plan))) != CRF_OK ||
+    if (rc != CRF_OK) return rc;
+    const int64_t each = num_trees * vec_bytes(plan);
+    if ((rc = check_workspace(workspace, workspace_bytes, tree_bytes(plan))) != CRF_OK ||
+        (rc = check_overlap({{"loss", loss, vec_bytes(plan)}, {"logp", logp, each},
+                             {"grad_scores", grad_scores, scores_bytes(plan, 1)},
+                             {"workspace", workspace, tree_bytes(plan)}},
+                            {{"scores", scores, scores_bytes(plan, 1)}, {"trees", trees, trees_bytes(plan, num_trees)},
+                             {"counts", counts, vec_bytes(plan)}, {"advantages", advantages, each}, {"old_logp", old_logp, each},
+                             {"ref_logp", ref_logp, each}, {"grad_loss", grad_loss, vec_bytes(plan)}})) != CRF_OK ||
         (rc = check_device(plan)) != CRF_OK)
         return rc;
     const hipError_t e = crf::launch_policy_loss(plan->kp, scores, trees, num_trees, counts, advantages,
@@ -164,8 +208,9 @@ int crf_pack_rows(const crf_plan *plan, const uint16_t *x, int32_t d, uint8_t *c
     if (rc != CRF_OK) return rc;
     if (misaligned(x, 8)) return fail(CRF_EINVAL, "x must be 8-byte aligned");
     if (misaligned(codes, 16)) return fail(CRF_EINVAL, "codes must be 16-byte aligned");
-    if (static_cast<const void *>(x) == codes) return fail(CRF_EINVAL, "x and codes must not alias");
-    if ((rc = check_device(plan)) != CRF_OK) return rc;
+    const Span rows[] = {{"x", x, rows_bytes(plan, 2, d)}, {"codes", codes, rows_bytes(plan, 1, row_codes(d))},
+                         {"scales", scales, rows_bytes(plan, 1, row_codes(d) / 32)}};
+    if ((rc = check_overlap({rows[1], rows[2]}, {rows[0]})) != CRF_OK || (rc = check_device(plan)) != CRF_OK) return rc;
     const hipError_t e = crf::launch_pack_rows(plan->kp, x, d, codes, scales, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_pack_rows launch");
 }
@@ -178,8 +223,9 @@ int crf_unpack_rows(const crf_plan *plan, const uint8_t *codes, const uint8_t *s
     if (rc != CRF_OK) return rc;
     if (misaligned(x, 8)) return fail(CRF_EINVAL, "x must be 8-byte aligned");
     if (misaligned(codes, 16)) return fail(CRF_EINVAL, "codes must be 16-byte aligned");
-    if (static_cast<const void *>(x) == codes) return fail(CRF_EINVAL, "x and codes must not alias");
-    if ((rc = check_device(plan)) != CRF_OK) return rc;
+    const Span rows[] = {{"x", x, rows_bytes(plan, 2, d)}, {"codes", codes, rows_bytes(plan, 1, row_codes(d))},
+                         {"scales", scales, rows_bytes(plan, 1, row_codes(d) / 32)}};
+    if ((rc = check_overlap({rows[0]}, {rows[1], rows[2]})) != CRF_OK || (rc = check_device(plan)) != CRF_OK) return rc;
     const hipError_t e = crf::launch_unpack_rows(plan->kp, codes, scales, d, x, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_unpack_rows launch");
 }
