@@ -2,9 +2,9 @@
 // checks and launches, as crf_plan.cpp has them for the others.
 #include <hip/hip_runtime_api.h>
 
-#include <atomic>
 #include <cstring>
 #include <initializer_list>
+#include <mutex>
 
 #include "../../include/crf_inside.h"
 #include "crf_plan.h"
@@ -109,10 +109,13 @@ int scorer_backward(const crf_plan *plan, const void *rl, const uint8_t *rl_scal
                              {"grad_scores", grad_scores, scores_bytes(plan, num_labels)}})) != CRF_OK ||
         (rc = check_device(plan)) != CRF_OK)
         return rc;
-    // best effort, as for the other kernels: a real shortfall surfaces as a launch error
-    static std::atomic<uint64_t> seen{0};
-    const uint64_t bit = (uint64_t)1 << (plan->device & 63);
-    if (!(seen.fetch_or(bit) & bit) && crf::set_biaffine_bwd_attributes() != hipSuccess) (void)hipGetLastError();
+    // Once a device, and before any thread's first launch there: another one's
+    // first call waits.  Best effort, as for the other kernels: a real shortfall
+    // surfaces as a launch error.
+    static std::once_flag set[64];
+    std::call_once(set[plan->device & 63], [] {
+        if (crf::set_biaffine_bwd_attributes() != hipSuccess) (void)hipGetLastError();
+    });
     const hipError_t e = crf::launch_biaffine_bwd(plan->kp, plan->cells, rl, rl_scales, rr, rr_scales, w, d, ldw, num_labels,
                                                   grad_scores, grad_rl, grad_rr, grad_w, static_cast<char *>(workspace),
                                                   static_cast<hipStream_t>(stream));

@@ -223,6 +223,37 @@ int aliases(void *lib) {
     return 0;
 }
 
+// Two threads whose first calls of the scorer's backward pass meet.
+int attributes(void *lib) {
+    ENTRY(crf_plan_create); ENTRY(crf_plan_destroy); ENTRY(crf_biaffine_bwd_workspace); ENTRY(crf_biaffine_bwd);
+    const int32_t len[kB] = {8, 3, 100};
+    constexpr int d = 500, ldw = 504, n1 = 101;
+    crf_plan *p[2] = {nullptr, nullptr};
+    for (auto &x : p)
+        if (crf_plan_create(&x, len, kB, n1, 1, 0) != CRF_OK) return 1;
+    int64_t bytes = 0;
+    crf_biaffine_bwd_workspace(p[0], d, 1, &bytes);
+    ready.clear();
+    launched.clear();
+    slow_attributes = watch_attributes = true;
+    int rc[2] = {0, 0};
+    auto call = [&](int t) {
+        auto at = [&](int k) { return reinterpret_cast<char *>(((uintptr_t)1 << 40) + ((uintptr_t)(16 * t + k) << 28)); };
+        rc[t] = crf_biaffine_bwd(p[t], (uint16_t *)at(0), (uint16_t *)at(1), (uint16_t *)at(2), d, ldw, 1, (float *)at(3),
+                                 (uint16_t *)at(4), (uint16_t *)at(5), (float *)at(6), at(7), bytes, nullptr);
+    };
+    std::thread a(call, 0), b([&]() {
+        std::this_thread::sleep_for(std::chrono::milliseconds(5));   // the first thread is at its attributes
+        call(1);
+    });
+    a.join();
+    b.join();
+    for (const std::string &x : early) std::printf("EARLY %s\n", x.c_str());
+    std::printf("launches %d status %d %d\n", (int)launched.size(), rc[0], rc[1]);
+    for (auto *x : p) crf_plan_destroy(x);
+    return 0;
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
@@ -234,5 +265,6 @@ int main(int argc, char **argv) {
     }
     const std::string mode = argv[1];
     if (mode == "alias") return aliases(lib);
+    if (mode == "attributes") return attributes(lib);
     return 2;
 }

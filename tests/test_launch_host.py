@@ -39,3 +39,11 @@ def test_overlapping_buffers_are_refused(harness):
     for *what, status in rows:
         ok = what[1] == "none" or what[-1] == "beside"   # (buffers that touch share nothing)
         assert int(status) == (B.CRF_OK if ok else B.CRF_EINVAL), what
+
+
+def test_first_calls_of_two_threads(harness):
+    # the LDS attributes of the scorer's backward kernels are set before either launches
+    rows = run(harness, "attributes")
+    assert [r for r in rows if r[0] == "EARLY"] == []
+    (last,) = [r for r in rows if r[0] == "launches"]
+    assert int(last[1]) >= 8 and last[3:] == ["0", "0"]
