@@ -378,7 +378,8 @@ int crf_tree_logprobs_bwd(const crf_plan *plan, const float *scores, const int32
  *   c_g = dL_b/dlog p_g = 1/c [ -r_g A_g [r_g A_g <= clip(r_g) A_g]
  *                               + kl_coef (1 - exp(q_g)) ].
  * log p_g - old_g and q_g above 80 are taken as 80.  A sentence without trees
- * has the loss 0 and the gradient 0.
+ * has the loss 0 and the gradient 0; one with a NaN among its trees'
+ * advantages, old_logp or ref_logp has the loss NaN and a gradient of NaN.
  *   trees, num_trees, counts, logp (or NULL): as crf_tree_logprobs; a repeated
  *               span counts once in the gradient.
  *   advantages, old_logp  device float32 [B][G].

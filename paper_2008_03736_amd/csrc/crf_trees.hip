@@ -41,6 +41,23 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
+// NaN, by the bits: the build takes no account of it in comparisons, and a
+// minimum drops it.  (The compiler knows this test of a float's bits, and that
+// it may take it for false: the asm hides that they are a float's.)
+__device__ __forceinline__ bool is_nan(uint32_t u) {
+    asm("" : "+v"(u));
+    return (u & 0x7FFFFFFFu) > 0x7F800000u;
+}
+__device__ __forceinline__ bool is_nan(uint64_t u) {
+    asm("" : "+v"(u));
+    return (u & 0x7FFFFFFFFFFFFFFFull) > 0x7FF0000000000000ull;
+}
+__device__ __forceinline__ float or_nan(bool lost, float x) {
+    uint32_t u = lost ? 0x7FC00000u : __builtin_bit_cast(uint32_t, x);
+    asm("" : "+v"(u));
+    return __builtin_bit_cast(float, u);
+}
+
 // What a launch is for: log p alone, the gradient of given weights of log p,
 // or the policy loss and its gradient.
 enum TreeMode { kTreeLogp, kTreeBack, kTreePolicy };
@@ -105,17 +122,23 @@ __global__ __launch_bounds__(kTreeThreads) void tree_kernel(TreeArgs ta) {
     const int cnt = ta.counts ? min(max(ta.counts[b], 0), G) : G;
     const int R = 2 * (N1 - 1) - 1, own = 2 * n - 1;
     const size_t sent = (size_t)b * N1 * N1;
-    const double z = MODE == kTreeBack ? 0.0 : ta.z64[b];
+    // (as bits, which is_nan takes)
+    const uint64_t zb = MODE == kTreeBack ? 0 : reinterpret_cast<const uint64_t *>(ta.z64)[b];
+    const double z = __builtin_bit_cast(double, zb);
     const size_t at = (size_t)b * G + min(lane, G - 1);
-    float adv = 0.f, old = 0.f, ref = 0.f, up = 1.f;
+    auto bits = [at](const float *x) { return reinterpret_cast<const uint32_t *>(x)[at]; };
+    uint32_t advb = 0, oldb = 0, refb = 0;
+    float up = 1.f;
     if constexpr (MODE == kTreePolicy) {
-        adv = a.adv[at];
-        old = a.old_logp[at];
-        if (a.ref_logp != nullptr) ref = a.ref_logp[at];
+        advb = bits(a.adv);
+        oldb = bits(a.old_logp);
+        if (a.ref_logp != nullptr) refb = bits(a.ref_logp);
         if (a.grad_loss != nullptr) up = a.grad_loss[b];
     } else if constexpr (MODE == kTreeBack) {
-        adv = a.grad_logp[at];
+        advb = bits(a.grad_logp);
     }
+    const float adv = __builtin_bit_cast(float, advb), old = __builtin_bit_cast(float, oldb),
+                ref = __builtin_bit_cast(float, refb);
     const float inv = 1.0f / (float)n;
     struct Cell {
         int i, j;
@@ -185,9 +208,9 @@ __global__ __launch_bounds__(kTreeThreads) void tree_kernel(TreeArgs ta) {
         const bool here = lane < cnt;
         const double lp = here ? sums[lane] - z : 0.0;
         if (i0 == 0)
-            if (here && ta.logp != nullptr) ta.logp[at] = (float)lp;
+            if (here && ta.logp != nullptr) ta.logp[at] = or_nan(is_nan(zb), (float)lp);
         if constexpr (MODE == kTreeLogp) {
-            if (lane == 0 && ta.logZ != nullptr) ta.logZ[b] = (float)z;
+            if (lane == 0 && ta.logZ != nullptr) ta.logZ[b] = or_nan(is_nan(zb), (float)z);
         } else if constexpr (MODE == kTreeBack) {
             const float c = here ? adv : 0.f;
             const double all = wave_sum((double)c);
@@ -207,12 +230,14 @@ __global__ __launch_bounds__(kTreeThreads) void tree_kernel(TreeArgs ta) {
                     c -= (double)a.kl_coef * e;
                 }
             }
+            // (log Z is NaN where a team's wait ran out)
+            const bool lost = __any(here && (is_nan(zb) || is_nan(advb) || is_nan(oldb) || is_nan(refb)));
             const double share = cnt > 0 ? 1.0 / (double)cnt : 0.0;
             const double total = wave_sum(term) * share, all = wave_sum((double)(float)(c * share));
             if (here) coef[lane] = (float)(c * share);
             if (lane == 0) {
-                coef[CRF_MAX_TREES] = (float)all;
-                if (i0 == 0) a.loss[b] = (float)total;
+                coef[CRF_MAX_TREES] = or_nan(lost, (float)all);
+                if (i0 == 0) a.loss[b] = or_nan(lost, (float)total);
             }
         }
     }

@@ -251,3 +251,33 @@ def test_refused_aliases(torch):
                 plan.policy_loss(s, t, f, g, **bad)
         with pytest.raises(TypeError):   # would scale the gradient but not the loss that it is the gradient of
             B.policy_loss(s, t, f, g, plan, grad_loss=up)
+
+
+@pytest.mark.parametrize("where", ["advantages", "old_logp", "ref_logp", "log Z"])
+def test_nan_reaches_the_loss_and_its_gradient(torch, where):
+    # sentence 1's tree 2 (absent in sentence 3, whose counts leave it out)
+    dev = torch.device("cuda", 0)
+    b = W.custom([6, 100, 9, 5], seed=12)
+    G, counts = 3, [3, 3, 0, 2]
+    trees, lz, mu, lp, old, ref, adv = inputs(b, G, counts, 12)
+    cu = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(dev)
+    s = cu(b.scores)
+    given = dict(advantages=cu(np.abs(adv)), old_logp=cu(old), ref_logp=cu(ref))
+    with B.Plan(b.lengths, n1=b.n1, device=dev) as plan:
+        call = lambda x: plan.policy_loss(x, cu(trees), **given, counts=cu(np.asarray(counts, np.int32)), kl_coef=KL,
+                                          logp=torch.full((4, G), 7.5, device=dev), grad_scores=torch.full_like(s, 7.5))
+        want = call(s)
+        if where == "log Z":
+            s = s.clone()
+            s[1, 4, 5] = float("nan")   # a word: in log Z and in every tree
+        else:
+            given[where][1, 2] = given[where][3, 2] = float("nan")
+        loss, logp, grad = call(s)
+    there, valid = T.here(counts, 4, G), W.valid_mask(np.asarray(b.lengths), b.n1)
+    assert np.array_equal(np.isnan(loss.cpu().numpy()), [False, True, False, False])
+    nan_logp = there & (np.arange(4) == 1)[:, None] if where == "log Z" else np.zeros_like(there)
+    assert np.array_equal(np.isnan(logp.cpu().numpy()), nan_logp)
+    assert np.array_equal(np.isnan(grad.cpu().numpy()), valid & (np.arange(4) == 1)[:, None, None])
+    others = [0, 2, 3]
+    for x, y in zip((loss, logp, grad), want):
+        assert torch.equal(x[others], y[others])
