@@ -383,7 +383,8 @@ int crf_tree_logprobs_bwd(const crf_plan *plan, const float *scores, const int32
  *   trees, num_trees, counts, logp (or NULL): as crf_tree_logprobs; a repeated
  *               span counts once in the gradient.
  *   advantages, old_logp  device float32 [B][G].
- *   ref_logp    device float32 [B][G], or NULL: no KL term (kl_coef is 0).
+ *   ref_logp    device float32 [B][G], or NULL: no KL term (kl_coef is 0, and
+ *               then it is not read).
  *   clip_low    0 <= clip_low <= 1; clip_high >= 0; kl_coef >= 0.
  *   grad_loss   device float32[B] upstream gradient dOut/dL_b, or NULL for 1.
  *   loss        device float32[B]: L_b (not scaled by grad_loss).  loss and logp

@@ -198,7 +198,8 @@ int crf_policy_loss(const crf_plan *plan, const float *scores, const int32_t *tr
         (rc = check_device(plan)) != CRF_OK)
         return rc;
     const hipError_t e = crf::launch_policy_loss(plan->kp, scores, trees, num_trees, counts, advantages,
-                                                 old_logp, ref_logp, clip_low, clip_high, kl_coef, grad_loss,
+                                                 old_logp, kl_coef != 0.f ? ref_logp : nullptr, clip_low, clip_high,
+                                                 kl_coef, grad_loss,
                                                  static_cast<double *>(workspace), loss, logp, grad_scores,
                                                  static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_policy_loss launch");

@@ -281,3 +281,16 @@ def test_nan_reaches_the_loss_and_its_gradient(torch, where):
     others = [0, 2, 3]
     for x, y in zip((loss, logp, grad), want):
         assert torch.equal(x[others], y[others])
+
+
+def test_reference_without_a_kl_term(torch):
+    # kl_coef = 0: the reference is not part of the loss, also a tree it rules out
+    dev = torch.device("cuda", 0)
+    b = W.custom([6, 80], seed=13)
+    trees, lz, mu, lp, old, ref, adv = inputs(b, 2, None, 13)
+    cu = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(dev)
+    ref[0, 1], ref[1, 0] = -np.inf, np.nan
+    with B.Plan(b.lengths, n1=b.n1, device=dev) as plan:
+        call = lambda r: plan.policy_loss(cu(b.scores), cu(trees), cu(adv), cu(old), ref_logp=r)
+        for x, y in zip(call(cu(ref)), call(None)):
+            assert torch.equal(x, y)
