@@ -56,7 +56,11 @@
  *   delays it.  A wait that lasts about 2^21 polls (a second or two) ends
  *   the launch, and the outputs of its workspace sentences are invalid: log
  *   Z and best score NaN when a width step's wait ran out, left unwritten
- *   when the launch's workgroups never were resident together.  Two plans' team launches running at once on different streams
+ *   when the launch's workgroups never were resident together (the
+ *   log-probabilities and log Z of crf_tree_logprobs, and the loss,
+ *   log-probabilities and gradient of crf_policy_loss, are NaN in either
+ *   case; marginals and other gradients do not tell).  Two plans' team
+ *   launches running at once on different streams
  *   can hold each other's room that way: issue calls that may form teams on
  *   one stream, or create the plans with CRF_NO_TEAMS.  Results are
  *   bit-identical to those of one workgroup per pass.

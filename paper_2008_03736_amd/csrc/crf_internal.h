@@ -598,6 +598,11 @@ inline TeamShape team_shape(int jobs, int64_t cap, bool has_area) {
     if (k < kTeamMinK) return TeamShape{1, jobs};
     return TeamShape{k, 8 * m * k};
 }
+// Whether an inside pass runs its workspace sentences by teams.
+inline bool inside_by_teams(const KernelPlan &p) {
+    return p.inside.n_spill > 0 && !(p.tile_on && p.tile_long) &&
+           team_shape(p.inside.n_spill, p.team_cap, p.team_area != nullptr).k > 1;
+}
 
 // The no-allocation entry point's scratch: a file-scope device array of
 // kScratchBytes per GPU (the first kScratchCounterBytes hold the fused

@@ -266,9 +266,22 @@ __global__ __launch_bounds__(kTreeThreads) void tree_kernel(TreeArgs ta) {
     }
 }
 
+// log Z of n sentences as not there, NaN.
+__global__ void mark_missing(const int32_t *ids, int n, double *z64) {
+    for (int t = threadIdx.x; t < n; t += blockDim.x) reinterpret_cast<uint64_t *>(z64)[ids[t]] = 0x7FF8000000000000ull;
+}
+
 }  // namespace
 
+// The sweep.  A launch by teams that the device never holds at once writes
+// nothing, and log Z would be what the workspace held before: it is NaN until
+// a team has it, and with it what the pass over the trees makes of it.
 static hipError_t sweep(const KernelPlan &p, const float *scores, double *z64, float *marg, hipStream_t stream) {
+    if (z64 != nullptr && inside_by_teams(p)) {
+        hipLaunchKernelGGL(mark_missing, dim3(1), dim3(64), 0, stream, p.inside.order_spill, (int)p.inside.n_spill, z64);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     KernelPlan q = p;
     q.z64 = z64;
     return launch_inside(q, scores, nullptr, nullptr, marg, stream);

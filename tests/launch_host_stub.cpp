@@ -5,7 +5,8 @@
 //   attributes LIB       two threads' first calls of the scorer's backward pass:
 //                        "EARLY name" of each kernel launched before its
 //                        attribute was set, then "launches N"
-//   launches LIB FLAGS CALL LENGTHS...   the kernels of a call in order, "K name"
+//   launches LIB CALL FLAGS LENGTHS...   the kernels of a call in order, "K name",
+//                        and "A sentences pointer" of one that marks log Z as missing
 #include <cxxabi.h>
 #include <dlfcn.h>
 #include <hip/hip_runtime_api.h>
@@ -29,7 +30,8 @@ namespace {
 std::mutex mu;
 std::map<const void *, std::string> names;
 std::set<const void *> ready;       // functions whose LDS attribute is set
-std::vector<std::string> launched, early;
+std::vector<std::string> launched, early, marked;
+void *const workspace = reinterpret_cast<void *>((uintptr_t)9 << 40);
 bool slow_attributes = false, watch_attributes = false;
 struct Config {
     dim3 grid, block;
@@ -63,9 +65,15 @@ hipError_t __hipPopCallConfiguration(dim3 *g, dim3 *b, size_t *lds, hipStream_t 
     *s = config.stream;
     return hipSuccess;
 }
-hipError_t hipLaunchKernel(const void *f, dim3, dim3, void **, size_t lds, hipStream_t) {
+hipError_t hipLaunchKernel(const void *f, dim3, dim3, void **args, size_t lds, hipStream_t) {
     std::lock_guard<std::mutex> lock(mu);
     launched.push_back(names[f]);
+    if (names[f].find("mark_missing") != std::string::npos) {   // (ids, how many, log Z)
+        const int32_t *ids = *static_cast<const int32_t **>(args[0]);
+        std::string a = "A";
+        for (int k = 0; k < *static_cast<int *>(args[1]); ++k) a += " " + std::to_string(ids[k]);
+        marked.push_back(a + (*static_cast<void **>(args[2]) == workspace ? " workspace" : " elsewhere"));
+    }
     if (watch_attributes && lds > 65536 && ready.count(f) == 0) early.push_back(names[f]);
     return hipSuccess;
 }
@@ -113,7 +121,7 @@ hipError_t hipOccupancyMaxActiveBlocksPerMultiprocessor(int *n, const void *, in
 namespace {
 
 template <typename F>
-F *entry(void *lib, F *, const char *name) {
+F *entry(void *lib, const char *name) {
     void *p = dlsym(lib, name);
     if (p == nullptr) {
         std::printf("no %s\n", name);
@@ -121,7 +129,7 @@ F *entry(void *lib, F *, const char *name) {
     }
     return reinterpret_cast<F *>(p);
 }
-#define ENTRY(name) auto *const name = entry(lib, &::name, #name)
+#define ENTRY(name) auto *const name = entry<decltype(::name)>(lib, #name)
 
 constexpr int kB = 3, kN1 = 9, kG = 2, kD = 36, kDc = 64, kLdw = 40, kRows = 2 * (kN1 - 1) - 1;
 constexpr int64_t kScores = 4 * kB * kN1 * kN1, kTrees = 8 * kB * kG * kRows, kEach = 4 * kB * kG, kVec = 4 * kB;
@@ -254,6 +262,30 @@ int attributes(void *lib) {
     return 0;
 }
 
+int launches(void *lib, const std::string &call, int flags, const std::vector<int32_t> &len) {
+    ENTRY(crf_plan_create); ENTRY(crf_plan_destroy); ENTRY(crf_tree_workspace); ENTRY(crf_tree_logprobs);
+    ENTRY(crf_tree_logprobs_bwd); ENTRY(crf_policy_loss); ENTRY(crf_inside_fwd_bwd);
+    crf_plan *p = nullptr;
+    if (crf_plan_create(&p, len.data(), (int32_t)len.size(), *std::max_element(len.begin(), len.end()) + 1, 1, flags) != CRF_OK)
+        return 1;
+    int64_t tw = 0;
+    crf_tree_workspace(p, &tw);
+    launched.clear();
+    auto f = [](int k) { return reinterpret_cast<float *>((uintptr_t)(k + 1) << 40); };
+    const int32_t *trees = reinterpret_cast<int32_t *>(f(0));
+    int rc = -1;
+    if (call == "logprobs") rc = crf_tree_logprobs(p, f(1), trees, 2, nullptr, f(2), nullptr, workspace, tw, nullptr);
+    if (call == "logprobs_bwd") rc = crf_tree_logprobs_bwd(p, f(1), trees, 2, nullptr, f(2), f(3), nullptr);
+    if (call == "policy")
+        rc = crf_policy_loss(p, f(1), trees, 2, nullptr, f(2), f(3), nullptr, 0.2f, 0.2f, 0.f, nullptr, f(4), f(5), f(6),
+                             workspace, tw, nullptr);
+    if (call == "inside") rc = crf_inside_fwd_bwd(p, f(1), nullptr, f(2), f(3), nullptr);
+    for (const std::string &x : launched) std::printf("K %s\n", x.c_str());
+    for (const std::string &x : marked) std::printf("%s\n", x.c_str());
+    crf_plan_destroy(p);
+    return rc;
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
@@ -266,5 +298,10 @@ int main(int argc, char **argv) {
     const std::string mode = argv[1];
     if (mode == "alias") return aliases(lib);
     if (mode == "attributes") return attributes(lib);
+    if (mode == "launches" && argc > 5) {
+        std::vector<int32_t> len;
+        for (int k = 5; k < argc; ++k) len.push_back(std::atoi(argv[k]));
+        return launches(lib, argv[3], std::atoi(argv[4]), len);
+    }
     return 2;
 }

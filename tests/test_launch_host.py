@@ -47,3 +47,24 @@ def test_first_calls_of_two_threads(harness):
     assert [r for r in rows if r[0] == "EARLY"] == []
     (last,) = [r for r in rows if r[0] == "launches"]
     assert int(last[1]) >= 8 and last[3:] == ["0", "0"]
+
+
+TEAM = "inside_kernel<%s, true, false, true>"
+
+
+@pytest.mark.parametrize("call,reverse", [("logprobs", "false"), ("policy", "true")])
+def test_log_z_is_missing_until_a_team_has_it(harness, call, reverse):
+    # a launch whose teams never assemble writes nothing: what the pass over
+    # the trees then reads has to say so
+    rows = run(harness, "launches", call, 0, 460, 12, 500, 30)
+    names = [" ".join(r[1:]) for r in rows if r[0] == "K"]
+    team = [k for k, x in enumerate(names) if TEAM % reverse in x]
+    mark = [k for k, x in enumerate(names) if "mark_missing" in x]
+    assert len(team) == len(mark) == 1 and mark[0] < team[0] < len(names) - 1 and "tree_kernel" in names[-1], names
+    assert [r for r in rows if r[0] == "A"] == [["A", "2", "0", "workspace"]]   # both long ones, longest first
+
+
+@pytest.mark.parametrize("call,flags,lengths", [("logprobs", 0, (12, 30, 300)), ("policy", B.CRF_NO_TEAMS, (460, 12)),
+                                                ("logprobs_bwd", 0, (460, 12)), ("inside", 0, (460, 12))])
+def test_calls_without_that_mark(harness, call, flags, lengths):
+    assert not any("mark_missing" in " ".join(r) for r in run(harness, "launches", call, flags, *lengths))
