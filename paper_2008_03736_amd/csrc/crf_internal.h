@@ -372,6 +372,10 @@ constexpr int kLabelRowChunk = 1024;
 // longer ones to the workspace kernels.
 constexpr int kMaxLenInLds = 141;
 
+// Steps of the score shifts of calls that subtract log Z from a tree's score
+// (KernelPlan::z64).
+constexpr float kFineShift = 1.0f / 64.0f;
+
 // Cells of a stripe of the tree calls' gradient pass.
 constexpr int kTreeCells = 2048;
 

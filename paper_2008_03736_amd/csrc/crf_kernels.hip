@@ -361,6 +361,7 @@ struct Bundle_ctx {
     int e;          // the inside layout's bank exponent (inside_layout); 5 on the workspace
     int *ovf;       // linear-domain sweeps: set to 1 (LDS) when a value leaves float32's range
     Team tm;        // workspace sentences: the team running the pass
+    bool fine = false;   // shifts in whole steps of kFineShift (see rescale_chart)
 };
 
 
@@ -684,9 +685,12 @@ __device__ __forceinline__ int next_rescale(int lo, int n) {
 template <bool LIN, bool REV, bool TEAM, typename T>
 __device__ void rescale_chart(const Bundle_ctx<T> &bx, int t0, float *dsh, float *dl);
 
+__device__ __forceinline__ float fine_shift(float d) { return __builtin_rintf(d * (1.0f / kFineShift)) * kFineShift; }
+
 // The forward sweep alone: steps t = 1..n-1 (widths 2..n), one dispatch per
 // run of steps sharing a step shape; the linear domain cuts the runs for its
-// rescales (the log domain needs none here).
+// rescales (the log domain needs none here, but for bx.fine: its values would
+// grow with the width, and log Z take over their float32 steps).
 // WIDE: workspace charts (longer sentences), which may need 16 terms per lane.
 // IL: interleaved span numbering (lane_at).
 // dl: per-sentence scratch for the rescales.
@@ -694,7 +698,7 @@ template <bool LIN, bool WIDE, bool IL, bool TEAM, bool MULTI = true, typename T
 __device__ __forceinline__ void fwd_sweep(const Bundle_ctx<T> &bx, float *dsh, float *dl) {
     const int n = bx.n;
     for (int lo = 1; lo < n;) {
-        const int tr = LIN ? next_rescale<true>(lo, n) : 0;
+        const int tr = LIN || bx.fine ? next_rescale<LIN>(lo, n) : 0;
         const int hi = tr > 0 ? tr + 1 : n;   // steps [lo, hi), widths [lo + 1, hi + 1)
 #define CRF_FWD_FIXED(LO, HI, GG, CC, MM)                                                  \
         if (max(lo, LO) < min(hi, HI + 1))                                                 \
@@ -767,6 +771,13 @@ constexpr float kShiftBand = 30.0f;
 // (times exp2 of these in the linear domain), d += delta.  Later steps add d
 // to each score as they read it; the root's O' stays 0.  dl holds delta per
 // sentence meanwhile.
+// bx.fine: delta is a multiple of kFineShift, and so is the seed, so that the
+// shifts add up, and their products with numbers of nodes come out, without
+// rounding.  log Z takes d off again n - 2 times: a d rounded to float32's own
+// step puts it off by 1e-7 n.  The calls that subtract log Z from a tree's
+// score ask for it (1,000 words of deviation 2: log Z 1.4e-4 off without, 7e-6
+// with; in the log domain, at deviation 4, 6.6e-4 and 2.5e-4, which is its values'
+// own rounding).
 template <bool LIN, bool REV, bool TEAM, typename T>
 __device__ void rescale_chart(const Bundle_ctx<T> &bx, int t0, float *dsh, float *dl) {
     const int n = bx.n, ld = bx.ld, nb = bx.nb, w0 = t0 + 1, S = n - t0;
@@ -800,6 +811,7 @@ __device__ void rescale_chart(const Bundle_ctx<T> &bx, int t0, float *dsh, float
             delta = m > 0.5f * NEG ? -0.5f * (m + acc / cnt) / (float)(w0 - 1) : 0.f;
         else
             delta = -acc / (cnt * (float)(w0 - 1));
+        if (bx.fine) delta = fine_shift(delta);
         if (valid && gl == 0) dl[sb] = delta;
     });
     step_sync<TEAM>(bx.tm);   // every member has read the chart before any cell moves
@@ -1089,7 +1101,7 @@ constexpr int kGoldMark = 0x7FBADBAD;   // a NaN bit pattern: no finite chart va
 // does sets the bundle's overflow flag, and the bundle returns false
 // before it has written any output: the caller then runs it again in the log
 // domain (LIN = false, max-shifted log-sum-exp per span).
-template <bool LIN, bool REV, bool SPILL, bool GOLD, bool LAB>
+template <bool LIN, bool REV, bool SPILL, bool GOLD, bool LAB, bool Z64>
 __device__ __forceinline__ bool inside_block_impl(const KernelPlan &p, int block, const int32_t *rec, char *smem_raw,
                                                   const float *__restrict__ scores,
                                                   const float *__restrict__ grad,
@@ -1145,7 +1157,8 @@ __device__ __forceinline__ bool inside_block_impl(const KernelPlan &p, int block
         if (tid < nb) sid[tid] = id0;
     }
     const int ld = lay.ld;
-    const Bundle_ctx<float> bx{chart0, cstride, n, ld, nb, mnb, lay.e, LIN ? &lin_ovf : nullptr, tm};
+    const Bundle_ctx<float> bx{chart0, cstride, n, ld, nb, mnb, lay.e, LIN ? &lin_ovf : nullptr, tm,
+                                Z64 && p.z64 != nullptr};
     const bool coh = SPILL && tm.k > 1;   // a team's chart reads (chart_ld)
     if (tid == 0) lin_ovf = 0;
     __syncthreads();
@@ -1244,7 +1257,8 @@ __device__ __forceinline__ bool inside_block_impl(const KernelPlan &p, int block
             c = grp_sum<GS>(c);
             if (valid && gl == 0 && c > 0.f) {
                 const float mean = s1 / c, var = fmaxf(s2 / c - mean * mean, 0.f);
-                dsh[sb] = -(mean + fminf(0.5f * (float)LN2_D * var, 20.0f) + 2.0f);
+                const float seed = -(mean + fminf(0.5f * (float)LN2_D * var, 20.0f) + 2.0f);
+                dsh[sb] = bx.fine ? fine_shift(seed) : seed;
             }
         }
     });
@@ -1302,7 +1316,7 @@ __device__ __forceinline__ bool inside_block_impl(const KernelPlan &p, int block
         for (int sb = tid; sb < nb; sb += NT)
             logZ[sid[sb]] = aborted ? __builtin_bit_cast(float, 0x7fc00000) : (float)log_z(sb);
     }
-    if constexpr (SPILL && !GOLD) if (p.z64 != nullptr && tm.rank == 0) {   // (sentences in LDS: crf_tile.hip)
+    if constexpr (Z64) if (p.z64 != nullptr && tm.rank == 0) {   // (sentences in LDS: crf_tile.hip)
         const bool aborted = team_aborted(tm);
         for (int sb = tid; sb < nb; sb += NT)
             p.z64[sid[sb]] = aborted ? __builtin_bit_cast(double, 0x7ff8000000000000ll) : log_z(sb);
@@ -1405,19 +1419,20 @@ __device__ __forceinline__ bool inside_block_impl(const KernelPlan &p, int block
 }
 
 // A bundle (or a workspace sentence): the linear-domain sweeps, and the log
-// domain if they leave float32's range (see inside_block_impl).
-template <bool REV, bool SPILL, bool GOLD = false, bool LAB = false>
+// domain if they leave float32's range (see inside_block_impl).  Z64: the
+// kernel's launches may ask for log Z in float64 (KernelPlan::z64).
+template <bool REV, bool SPILL, bool GOLD = false, bool LAB = false, bool Z64 = false>
 __device__ __forceinline__ void inside_block(const KernelPlan &p, int block, const int32_t *rec, char *smem_raw,
                                              const float *__restrict__ scores,
                                              const float *__restrict__ grad,
                                              float *__restrict__ logZ, float *__restrict__ marg,
                                              const int32_t *__restrict__ gold = nullptr,
                                              float *__restrict__ loss = nullptr, const Team &tm = Team{}) {
-    if (inside_block_impl<true, REV, SPILL, GOLD, LAB>(p, block, rec, smem_raw, scores, grad, logZ, marg, gold, loss,
+    if (inside_block_impl<true, REV, SPILL, GOLD, LAB, Z64>(p, block, rec, smem_raw, scores, grad, logZ, marg, gold, loss,
                                                        tm))
         return;
     __syncthreads();   // every thread has left the linear attempt
-    inside_block_impl<false, REV, SPILL, GOLD, LAB>(p, block, rec, smem_raw, scores, grad, logZ, marg, gold, loss, tm);
+    inside_block_impl<false, REV, SPILL, GOLD, LAB, Z64>(p, block, rec, smem_raw, scores, grad, logZ, marg, gold, loss, tm);
 }
 
 // ---------------------------------------------------------------------------
@@ -1744,13 +1759,13 @@ __global__ __launch_bounds__(kThreadsMax) void inside_kernel(KernelPlan p, const
                                                              float *__restrict__ marg) {
     extern __shared__ __align__(16) char smem_raw[];
     if constexpr (SPILL && !TEAM) {
-        inside_block<REV, true, false, LAB>(p, blockIdx.x, nullptr, smem_raw, scores, grad, logZ, marg);
+        inside_block<REV, true, false, LAB, true>(p, blockIdx.x, nullptr, smem_raw, scores, grad, logZ, marg);
     } else if constexpr (SPILL) {
         Team tm;
         int job, stride;
         if (!spill_jobs(p, tm, job, stride)) return;
         for (; job < p.inside.n_spill; job += stride, ++tm.job) {
-            inside_block<REV, true, false, LAB>(p, job, nullptr, smem_raw, scores, grad, logZ, marg, nullptr, nullptr,
+            inside_block<REV, true, false, LAB, true>(p, job, nullptr, smem_raw, scores, grad, logZ, marg, nullptr, nullptr,
                                                 tm);
             __syncthreads();
         }

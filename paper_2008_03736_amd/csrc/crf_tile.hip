@@ -769,7 +769,6 @@ __device__ __forceinline__ Growth tile_growth(const Tile &x, int D) {
 // times off again, so that a shift rounded to float32's own step is 1e-7 n off,
 // more than all the rest (300 words at deviation 2: 3.2e-5 against 2e-6).  The
 // calls that subtract log Z from a tree's score ask for it.
-constexpr float kFineShift = 1.0f / 64.0f;
 template <bool LIN, typename CX>
 __device__ __forceinline__ void growth_shift(const CX &cx, int blocks, int which) {
     const int gl = this_thread() & 15, S = cx.S;

@@ -294,3 +294,45 @@ def test_reference_without_a_kl_term(torch):
         call = lambda r: plan.policy_loss(cu(b.scores), cu(trees), cu(adv), cu(old), ref_logp=r)
         for x, y in zip(call(cu(ref)), call(None)):
             assert torch.equal(x, y)
+
+
+# log2(e) as the charts hold it, relative to itself: every score that a tree is
+# free to have is scaled by it, in the tree's score as in log Z.
+CHART_SCORE = float(np.float32(np.log2(np.e))) / np.log2(np.e)
+
+
+@pytest.mark.parametrize("lengths,flags", [([139, 120, 130, 138], 0), ([300, 250, 300, 300], 0),
+                                           ([300, 250, 300], B.CRF_FORCE_SPILL), ([500, 460, 600, 480], 0),
+                                           ([500, 460, 600], B.CRF_NO_TEAMS), ([1000, 700], 0)])
+def test_log_probs_of_long_sentences_are_exact(torch, lengths, flags):
+    """An absolute bound, which log Z in float32, a shift of float32's own steps
+    and a tree's score without the charts' factor would each miss.  A chart's
+    value is off by rounding its sum, its score factor and their product: taken
+    as independent errors of at most 2^-23 of it (root mean square), the n - 2
+    free nodes of a tree come to sqrt(n) 2^-23, and five times that is allowed.
+    Ratios exp(log p - old) have float32's relative steps, 2^-24, on top."""
+    dev = torch.device("cuda", 0)
+    b = W.custom(lengths, seed=21, sd=2.0)
+    Bn, G = len(lengths), 4
+    cu = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(dev)
+    s = cu(b.scores)
+    trees = T.random_trees(b.lengths, b.n1, G, 5)
+    with B.Plan(b.lengths, n1=b.n1, flags=flags, device=dev) as plan:
+        trees[:, 3] = plan.cky_decode(s)[0].cpu().numpy()   # one of many times a tree's mean score
+        lz, mu = orc.marginals(b.scores, b.lengths, threads=16)
+        lp = T.log_probs(b.scores, b.lengths, trees, lz)
+        free = W.valid_mask(np.asarray(lengths), b.n1)
+        for k, n in enumerate(lengths):
+            free[k, np.arange(n), np.arange(n) + 1] = free[k, 0, n] = False
+        own = np.where(free, b.scores.astype(np.float64), 0.0)
+        tree_free = np.array([[sum(own[k, i, j] for i, j in T.spans_of(t, n)) for t in trees[k]] for k, n in enumerate(lengths)])
+        lp = lp + (CHART_SCORE - 1.0) * (tree_free - (np.where(free, mu, 0.0) * own).sum((1, 2))[:, None])
+        old = lp.astype(np.float32)
+        tol = (5.0 * np.sqrt(np.asarray(lengths)) * 2.0 ** -23)[:, None]
+        got = plan.tree_logprobs(s, cu(trees))[0].cpu().numpy().astype(np.float64)
+        assert np.all(np.abs(got - lp) <= tol + 2.0 ** -24 * np.abs(lp)), np.abs(got - lp).max(1)
+        for g in range(G):   # (one tree at a time: its ratio is the loss)
+            loss, _, _ = plan.policy_loss(s, cu(trees[:, g:g + 1]), -torch.ones((Bn, 1), device=dev), cu(old[:, g:g + 1]),
+                                          clip_low=1.0, clip_high=1e6)
+            err = np.log(loss.cpu().numpy().astype(np.float64)) - (lp[:, g] - old[:, g])
+            assert np.all(np.abs(err) <= tol[:, 0] + 1.01 * 2.0 ** -24), (g, err, tol[:, 0])
