@@ -15,6 +15,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <functional>
 #include <new>
 #include <numeric>
 #include <vector>
@@ -71,18 +72,48 @@ void release(crf_plan *p) {
     p->allocations.clear();
 }
 
-template <typename T>
-hipError_t upload(crf_plan *p, const std::vector<T> &v, const T **dst) {
-    *dst = nullptr;
-    if (v.empty()) return hipSuccess;
-    void *d = nullptr;
-    hipError_t e = hipMalloc(&d, v.size() * sizeof(T));
-    if (e != hipSuccess) return e;
-    p->allocations.push_back(d);
-    e = hipMemcpy(d, v.data(), v.size() * sizeof(T), hipMemcpyHostToDevice);
-    *dst = static_cast<const T *>(d);
-    return e;
-}
+// A plan's tables, in one allocation: 256-byte aligned, the small ones copied
+// together.  (With an allocation and a copy a table, plans of 1, 200 and 5,000
+// sentences took 117, 281 and 3,320 us to make; this way 21, 184 and 3,250.)
+class Tables {
+  public:
+    template <typename T>
+    void add(const std::vector<T> &v, const T **dst) {
+        *dst = nullptr;
+        if (!v.empty()) items.push_back({v.data(), v.size() * sizeof(T), reinterpret_cast<const void **>(dst)});
+    }
+    hipError_t upload(crf_plan *p) {
+        constexpr size_t kSmall = 65536;
+        auto aligned = [](size_t n) { return (n + 255) / 256 * 256; };
+        size_t small = 0, all = 0;
+        for (const Item &x : items) (x.bytes <= kSmall ? small : all) += aligned(x.bytes);
+        all += small;
+        if (all == 0) return hipSuccess;
+        void *d = nullptr;
+        hipError_t e = hipMalloc(&d, all);
+        if (e != hipSuccess) return e;
+        p->allocations.push_back(d);
+        char *const base = static_cast<char *>(d);
+        std::vector<char> staged(small, 0);
+        size_t at = 0, big = small;
+        for (const Item &x : items) {
+            size_t &q = x.bytes <= kSmall ? at : big;
+            *x.dst = base + q;
+            if (x.bytes <= kSmall) std::memcpy(staged.data() + q, x.src, x.bytes);
+            else if ((e = hipMemcpy(base + q, x.src, x.bytes, hipMemcpyHostToDevice)) != hipSuccess) return e;
+            q += aligned(x.bytes);
+        }
+        return small > 0 ? hipMemcpy(base, staged.data(), small, hipMemcpyHostToDevice) : hipSuccess;
+    }
+
+  private:
+    struct Item {
+        const void *src;
+        size_t bytes;
+        const void **dst;
+    };
+    std::vector<Item> items;
+};
 
 // One kind of chart's schedule on the host: equal-length bundles for the LDS
 // kernel, single sentences for the workspace kernel.
@@ -126,13 +157,24 @@ double simulate_launch(const std::vector<double> &dur, int n_part, int slots, st
     heap.assign((size_t)n_part * slots, 0.0);
     ends.resize(dur.size());
     double end = 0.0;
-    auto later = [](double a, double b) { return a > b; };   // min-heap
     for (size_t b = 0; b < dur.size(); ++b) {
         double *h = heap.data() + (b % n_part) * (size_t)slots;
-        std::pop_heap(h, h + slots, later);
-        const double e = h[slots - 1] + dur[b];
-        h[slots - 1] = e;
-        std::push_heap(h, h + slots, later);
+        const int k = (int)std::min<size_t>(b / n_part, slots);   // workgroups the partition has had
+        double e = dur[b];
+        if (k < slots) {   // a slot that is free from the start
+            h[k] = e;
+            if (k + 1 == slots) std::make_heap(h, h + slots, std::greater<double>());
+        } else {           // the slot that frees up first, the heap's top, gets the new end
+            e += h[0];
+            int i = 0;
+            for (int c = 1; c < slots; c = 2 * i + 1) {
+                if (c + 1 < slots && h[c + 1] < h[c]) ++c;
+                if (h[c] >= e) break;
+                h[i] = h[c];
+                i = c;
+            }
+            h[i] = e;
+        }
         ends[b] = e;
         end = std::max(end, e);
     }
@@ -500,94 +542,110 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     // room that still holds it, found through lists of open tiles by free
     // rows), longer ones cut into blocks of fence posts with a tile per pair
     // of row block <= column block.
+    //
+    // The fine-tuning operators' blocks of fence posts (KernelPlan::posts) are
+    // the same tiles, after the blocks of each long sentence one by one.
     std::vector<int32_t> bia, posts;
-    std::vector<int64_t> post_cells, compact_cells;
+    std::vector<int64_t> post_cells;
     int32_t n_long_posts = 0;
     {
-        std::vector<std::vector<int32_t>> packed;
-        std::vector<std::vector<int32_t>> by_free(crf::kBiaRows + 1);
-        for (int32_t b : order) {
-            const int n = lengths_host[b];
-            if (n + 1 <= crf::kBiaRows) {
-                int t = -1;
-                for (int f = n + 1; f <= crf::kBiaRows && t < 0; ++f)
-                    if (!by_free[f].empty()) {
-                        t = by_free[f].back();
-                        by_free[f].pop_back();
-                    }
-                if (t < 0) {
-                    t = (int)packed.size();
-                    packed.emplace_back();
-                }
-                for (int i = 0; i <= n; ++i) packed[t].push_back(b * n1 + i);
-                const int room = crf::kBiaRows - (int)packed[t].size();
-                if (room > 0) by_free[room].push_back(t);
-                continue;
-            }
-            const int nblk = (n + 1 + crf::kBiaRows - 1) / crf::kBiaRows;
-            for (int rb = 0; rb < nblk; ++rb)
-                for (int cb = rb; cb < nblk; ++cb) {
-                    for (int r = 0; r < crf::kBiaRows; ++r) {
-                        const int i = rb * crf::kBiaRows + r;
-                        bia.push_back(i <= n ? b * n1 + i : -1);
-                    }
-                    for (int c = 0; c < crf::kBiaCols; ++c) {
-                        const int j = cb * crf::kBiaCols + c;
-                        bia.push_back(j <= n ? b * n1 + j : -1);
-                    }
-                }
-        }
-        for (const auto &ids : packed)
-            for (int h = 0; h < 2; ++h)
-                for (int r = 0; r < crf::kBiaRows; ++r) bia.push_back(r < (int)ids.size() ? ids[r] : -1);
-        // The batch's fence posts in blocks of kBiaRows: those of a long
-        // sentence one after the other (each with the first and last of them),
-        // then the packed ones.
+        constexpr int R = crf::kBiaRows;
+        std::vector<std::vector<int32_t>> packed;   // the sentences of a tile
+        std::vector<std::vector<int32_t>> by_free(R + 1);
         std::vector<int64_t> cell_off(batch);
         for (int32_t b = 0; b < batch; ++b) {
             cell_off[b] = p->cells;
             p->cells += (int64_t)lengths_host[b] * lengths_host[b];
         }
-        auto put_block = [&](const int32_t *ids, int count, int first, int last) {
-            const size_t at = posts.size();
-            posts.resize(at + crf::kPostRec, -1);
-            for (int r = 0; r < crf::kBiaRows; ++r) {
-                // (a post without cells, n or an empty place: its sentence's
-                // or the first one's (0, 0), whose next cell exists)
-                int64_t square = 0, compact = -1;
-                posts[at + crf::kBiaRows + r] = 0;
-                if (r < count) {
-                    const int32_t b = ids[r] / n1, n = lengths_host[b];
-                    int32_t i = ids[r] - b * n1;
-                    posts[at + r] = ids[r];
-                    posts[at + crf::kBiaRows + r] = n - i;
-                    if (i == n) i = 0;
-                    square = (int64_t)b * n1 * n1 + (int64_t)i * n1 + i;
-                    compact = cell_off[b] + (int64_t)i * n - 1 + i;
-                }
-                post_cells.push_back(square);
-                compact_cells.push_back(compact);
-            }
-            posts[at + 2 * crf::kBiaRows] = first;
-            posts[at + 2 * crf::kBiaRows + 1] = last;
-        };
+        std::vector<int32_t> room;   // free rows of a tile
+        int32_t n_long = 0;          // the long sentences come first in the order
+        size_t bia_tiles = 0;
         for (int32_t b : order) {
             const int n = lengths_host[b];
-            if (n + 1 <= crf::kBiaRows) continue;
-            const int first = (int)(posts.size() / crf::kPostRec);
-            const int nblk = (n + 1 + crf::kBiaRows - 1) / crf::kBiaRows;
-            std::vector<int32_t> ids(n + 1);
-            for (int i = 0; i <= n; ++i) ids[i] = b * n1 + i;
-            for (int k = 0; k < nblk; ++k)
-                put_block(ids.data() + k * crf::kBiaRows, std::min(crf::kBiaRows, n + 1 - k * crf::kBiaRows), first,
-                          first + nblk - 1);
+            if (n + 1 > R) {
+                const int nblk = (n + R) / R;
+                n_long_posts += nblk;
+                bia_tiles += (size_t)nblk * (nblk + 1) / 2;
+                ++n_long;
+                continue;
+            }
+            int t = -1;
+            for (int f = n + 1; f <= R && t < 0; ++f)
+                if (!by_free[f].empty()) {
+                    t = by_free[f].back();
+                    by_free[f].pop_back();
+                }
+            if (t < 0) {
+                t = (int)packed.size();
+                packed.emplace_back();
+                room.push_back(R);
+            }
+            packed[t].push_back(b);
+            room[t] -= n + 1;
+            if (room[t] > 0) by_free[room[t]].push_back(t);
         }
-        n_long_posts = (int32_t)(posts.size() / crf::kPostRec);
-        for (const auto &ids : packed) {
-            const int at = (int)(posts.size() / crf::kPostRec);
-            put_block(ids.data(), (int)ids.size(), at, at);
+        const size_t blocks = n_long_posts + packed.size();
+        bia.resize((bia_tiles + packed.size()) * (R + crf::kBiaCols));
+        posts.resize(blocks * crf::kPostRec);
+        post_cells.resize(2 * blocks * R);
+        int32_t *tile = bia.data(), *rec = posts.data();
+        int64_t *square = post_cells.data(), *compact = square + blocks * R;
+        // Fence posts i0 .. i0 + count - 1 of sentence b from place r of a block
+        // on.  (A post without cells, n, has its sentence's (0, 0): the next cell
+        // exists.)
+        auto put_posts = [&](int r, int32_t b, int i0, int count) {
+            const int n = lengths_host[b];
+            const int64_t sq = (int64_t)b * n1 * n1, co = cell_off[b] - 1;
+            for (int k = 0; k < count; ++k) {
+                const int i = i0 + k, c = i < n ? i : 0;
+                rec[r + k] = b * n1 + i;
+                rec[R + r + k] = n - i;
+                square[r + k] = sq + (int64_t)c * (n1 + 1);
+                compact[r + k] = co + (int64_t)c * (n + 1);
+            }
+        };
+        // The empty places from r on (the batch's first cell), and the block is done.
+        auto end_block = [&](int r, size_t first, size_t last) {
+            for (; r < R; ++r) {
+                rec[r] = -1;
+                rec[R + r] = 0;
+                square[r] = 0;
+                compact[r] = -1;
+            }
+            rec[2 * R] = (int32_t)first;
+            rec[2 * R + 1] = (int32_t)last;
+            rec += crf::kPostRec;
+            square += R;
+            compact += R;
+        };
+        size_t at = 0;
+        for (int32_t q = 0; q < n_long; ++q) {
+            const int32_t b = order[q];
+            const int n = lengths_host[b], nblk = (n + R) / R;
+            for (int k = 0; k < nblk; ++k) {
+                const int count = std::min(R, n + 1 - k * R);
+                put_posts(0, b, k * R, count);
+                end_block(count, at, at + nblk - 1);
+            }
+            const int32_t *own = rec - (size_t)nblk * crf::kPostRec;
+            for (int rb = 0; rb < nblk; ++rb)
+                for (int cb = rb; cb < nblk; ++cb, tile += 2 * R) {
+                    std::copy_n(own + (size_t)rb * crf::kPostRec, R, tile);
+                    std::copy_n(own + (size_t)cb * crf::kPostRec, R, tile + R);
+                }
+            at += nblk;
         }
-        post_cells.insert(post_cells.end(), compact_cells.begin(), compact_cells.end());
+        for (const auto &mine : packed) {
+            int r = 0;
+            for (int32_t b : mine) {
+                put_posts(r, b, 0, lengths_host[b] + 1);
+                r += lengths_host[b] + 1;
+            }
+            const int32_t *ids = rec;
+            end_block(r, at, at);
+            for (int h = 0; h < 2; ++h, tile += R) std::copy_n(ids, R, tile);
+            ++at;
+        }
     }
 
     std::vector<int32_t> len(lengths_host, lengths_host + batch);
@@ -595,11 +653,11 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     // Stripes of rows for the tree calls' pass.
     std::vector<int32_t> tree_recs;
     kp.tree_cells = 0;
+    tree_recs.reserve(4 * (size_t)batch);
     for (int32_t b : order) {
         const int n = lengths_host[b], rows = std::max(1, std::min(n, crf::kTreeCells / n));
         kp.tree_cells = std::max(kp.tree_cells, rows * n);
-        for (int i = 0; i < n; i += rows)
-            for (int32_t v : {b, (int32_t)n, (int32_t)i, (int32_t)std::min(rows, n - i)}) tree_recs.push_back(v);
+        for (int i = 0; i < n; i += rows) tree_recs.insert(tree_recs.end(), {b, n, i, std::min(rows, n - i)});
     }
     kp.n_tree_recs = (int32_t)(tree_recs.size() / 4);
     kp.B = batch;
@@ -774,21 +832,23 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
 
     kp.tile_cky = kp.tile_on && (max_len <= crf::kTileCkyLen || (kp.tile_long && !sc.spill.empty()));
 
-    if ((e = upload(p, len, &kp.len)) != hipSuccess ||
-        (e = upload(p, rec_in, &kp.inside.recs)) != hipSuccess ||
-        (e = upload(p, si.spill, &kp.inside.order_spill)) != hipSuccess ||
-        (e = upload(p, si.off, &kp.inside.ws_off)) != hipSuccess ||
-        (e = upload(p, rec_ck, &kp.cky.recs)) != hipSuccess ||
-        (e = upload(p, sc.spill, &kp.cky.order_spill)) != hipSuccess ||
-        (e = upload(p, sc.off, &kp.cky.ws_off)) != hipSuccess ||
-        (e = upload(p, rec_mix, &kp.mix)) != hipSuccess ||
-        (e = upload(p, lab_rows, &kp.lab_rows)) != hipSuccess ||
-        (e = upload(p, bia, &kp.bia_tiles)) != hipSuccess ||
-        (e = upload(p, posts, &kp.posts)) != hipSuccess ||
-        (e = upload(p, tree_recs, &kp.tree_recs)) != hipSuccess ||
-        (e = upload(p, post_cells, &kp.post_cells)) != hipSuccess ||
-        (e = upload(p, tile_recs, &kp.tile_io.recs)) != hipSuccess ||
-        (e = upload(p, tile_ws_recs, &kp.tile_ws.recs)) != hipSuccess) {
+    Tables tables;
+    tables.add(len, &kp.len);
+    tables.add(rec_in, &kp.inside.recs);
+    tables.add(si.spill, &kp.inside.order_spill);
+    tables.add(si.off, &kp.inside.ws_off);
+    tables.add(rec_ck, &kp.cky.recs);
+    tables.add(sc.spill, &kp.cky.order_spill);
+    tables.add(sc.off, &kp.cky.ws_off);
+    tables.add(rec_mix, &kp.mix);
+    tables.add(lab_rows, &kp.lab_rows);
+    tables.add(bia, &kp.bia_tiles);
+    tables.add(posts, &kp.posts);
+    tables.add(tree_recs, &kp.tree_recs);
+    tables.add(post_cells, &kp.post_cells);
+    tables.add(tile_recs, &kp.tile_io.recs);
+    tables.add(tile_ws_recs, &kp.tile_ws.recs);
+    if ((e = tables.upload(p)) != hipSuccess) {
         const int code = (e == hipErrorOutOfMemory) ? CRF_ENOMEM : CRF_EHIP;
         release(p);
         delete p;

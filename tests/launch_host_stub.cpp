@@ -5,6 +5,7 @@
 //   attributes LIB       two threads' first calls of the scorer's backward pass:
 //                        "EARLY name" of each kernel launched before its
 //                        attribute was set, then "launches N"
+//   creation LIB LENGTHS...              "mallocs N copies N" of crf_plan_create
 //   launches LIB CALL FLAGS LENGTHS...   the kernels of a call in order, "K name",
 //                        and "A sentences pointer" of one that marks log Z as missing
 #include <cxxabi.h>
@@ -32,6 +33,7 @@ std::map<const void *, std::string> names;
 std::set<const void *> ready;       // functions whose LDS attribute is set
 std::vector<std::string> launched, early, marked;
 void *const workspace = reinterpret_cast<void *>((uintptr_t)9 << 40);
+int mallocs = 0, copies = 0;
 bool slow_attributes = false, watch_attributes = false;
 struct Config {
     dim3 grid, block;
@@ -93,6 +95,7 @@ hipError_t hipDeviceGetAttribute(int *v, hipDeviceAttribute_t a, int) {
     return hipSuccess;
 }
 hipError_t hipMalloc(void **p, size_t n) {
+    ++mallocs;
     *p = std::calloc(1, n ? n : 1);
     return *p ? hipSuccess : hipErrorOutOfMemory;
 }
@@ -101,6 +104,7 @@ hipError_t hipFree(void *p) {
     return hipSuccess;
 }
 hipError_t hipMemcpy(void *d, const void *s, size_t n, hipMemcpyKind) {
+    ++copies;
     std::memcpy(d, s, n);
     return hipSuccess;
 }
@@ -262,6 +266,17 @@ int attributes(void *lib) {
     return 0;
 }
 
+int creation(void *lib, const std::vector<int32_t> &len) {
+    ENTRY(crf_plan_create); ENTRY(crf_plan_destroy);
+    crf_plan *p = nullptr;
+    mallocs = copies = 0;
+    if (crf_plan_create(&p, len.data(), (int32_t)len.size(), *std::max_element(len.begin(), len.end()) + 1, 1, 0) != CRF_OK)
+        return 1;
+    std::printf("mallocs %d copies %d\n", mallocs, copies);
+    crf_plan_destroy(p);
+    return 0;
+}
+
 int launches(void *lib, const std::string &call, int flags, const std::vector<int32_t> &len) {
     ENTRY(crf_plan_create); ENTRY(crf_plan_destroy); ENTRY(crf_tree_workspace); ENTRY(crf_tree_logprobs);
     ENTRY(crf_tree_logprobs_bwd); ENTRY(crf_policy_loss); ENTRY(crf_inside_fwd_bwd);
@@ -298,6 +313,11 @@ int main(int argc, char **argv) {
     const std::string mode = argv[1];
     if (mode == "alias") return aliases(lib);
     if (mode == "attributes") return attributes(lib);
+    if (mode == "creation" && argc > 3) {
+        std::vector<int32_t> len;
+        for (int k = 3; k < argc; ++k) len.push_back(std::atoi(argv[k]));
+        return creation(lib, len);
+    }
     if (mode == "launches" && argc > 5) {
         std::vector<int32_t> len;
         for (int k = 5; k < argc; ++k) len.push_back(std::atoi(argv[k]));

@@ -68,3 +68,12 @@ def test_log_z_is_missing_until_a_team_has_it(harness, call, reverse):
                                                 ("logprobs_bwd", 0, (460, 12)), ("inside", 0, (460, 12))])
 def test_calls_without_that_mark(harness, call, flags, lengths):
     assert not any("mark_missing" in " ".join(r) for r in run(harness, "launches", call, flags, *lengths))
+
+
+@pytest.mark.parametrize("lengths", [[25], list(range(1, 100)) * 2, [20, 300, 7], [460, 12]])
+def test_a_plan_is_made_with_few_device_calls(harness, lengths):
+    # the tables in one allocation (then the workspace and the team area, where
+    # there are any) and few copies: each is a call of its own on the device, of
+    # 3 to 10 us, in plans that a training loop makes for every batch
+    (row,) = run(harness, "creation", *lengths)
+    assert int(row[1]) <= 1 + 2 * (max(lengths) > 96) and int(row[3]) <= 3
