@@ -74,6 +74,7 @@ def test_calls_without_that_mark(harness, call, flags, lengths):
 def test_a_plan_is_made_with_few_device_calls(harness, lengths):
     # the tables in one allocation (then the workspace and the team area, where
     # there are any) and few copies: each is a call of its own on the device, of
-    # 3 to 10 us, in plans that a training loop makes for every batch
+    # 3 to 10 us, in plans that a training loop makes for every batch (the small
+    # tables in one copy, and three of the 198 sentences are past 64 KB)
     (row,) = run(harness, "creation", *lengths)
-    assert int(row[1]) <= 1 + 2 * (max(lengths) > 96) and int(row[3]) <= 3
+    assert int(row[1]) <= 1 + 2 * (max(lengths) > 96) and int(row[3]) <= 1 + 3 * (len(lengths) > 100)
