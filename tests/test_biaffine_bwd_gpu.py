@@ -328,3 +328,41 @@ def test_some_gradients_of_labelled_scores(torch, packed):
             torch.cuda.current_stream().wait_stream(side)
             for x, y, n in zip(got, every, need):
                 assert torch.equal(x, y) if n else x is None
+
+
+MANY = np.random.default_rng(17).integers(1, 62, 3000).tolist() + [140, 64, 99, 128, 127, 63] * 10
+FEW = [40, 99, 3, 70, 61, 62, 63, 64, 30, 1] * 5
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("lengths,d,L", [(MANY, 100, 1), (MANY, 252, 1), (MANY, 500, 1), (MANY, 380, 1), (FEW, 36, 29),
+                                         (FEW, 132, 130), (FEW, 60, 300)])
+def test_weight_gradient_of_many_blocks(torch, lengths, d, L, packed):
+    """dW over hundreds of shares of several blocks each, or one share of all
+    (splits = 1: 130 labels at d = 132, 300 at d = 60), bit for bit.  Integers of
+    at most 2: a post's U is below 2^16, which two bf16 parts hold, and the sums,
+    of random signs, stay far below 2^24 (the assertion on the reference)."""
+    dev = torch.device("cuda", 0)
+    n1, Bn = max(lengths) + 1, len(lengths)
+    gen = torch.Generator(dev).manual_seed(d + L)
+    ints = lambda *s: torch.randint(-2, 3, s, device=dev, generator=gen)
+    n = torch.tensor(lengths, device=dev)
+    post = torch.arange(n1, device=dev)
+    rows = post[None] <= n[:, None]
+    spans = (post[:, None] < post[None])[None] & (post[None, None] <= n[:, None, None])
+    rl, rr = (torch.where(rows[..., None], ints(Bn, n1, d), 0) for _ in range(2))
+    nan = float("nan")
+    held = [torch.where(rows[..., None], x.to(torch.bfloat16), nan) for x in (rl, rr)]
+    g = torch.where(spans[..., None], ints(Bn, n1, n1, L).float(), nan)
+    w = torch.full((L, d, (d + 4) // 4 * 4), nan, dtype=torch.bfloat16, device=dev)
+    w[..., :d + 1] = 1.0
+    with B.Plan(lengths, n1=n1, device=dev) as plan:
+        if packed:
+            held = [plan.pack_rows(x) for x in held]
+        got = plan.biaffine_bwd(*held, w, g if L > 1 else g[..., 0], need=(False, False, True))[2]
+    one = torch.cat([rl, rows[..., None].long()], 2).double().reshape(-1, d + 1)
+    for q in range(L):
+        u = torch.bmm(torch.nan_to_num(g[..., q]).double().contiguous(), rr.double()).reshape(-1, d)
+        want = u.t().contiguous() @ one
+        assert float(want.abs().max()) < 2 ** 20
+        assert torch.equal(got[q, :, :d + 1].double(), want), q
