@@ -4,8 +4,9 @@
 // a power of two: with m the block's largest magnitude,
 //     s = ceil(log2(m / 448)),  code = e4m3(x 2^-s),  x' = code 2^s,
 // so that the largest code's magnitude lies in (224, 448], e4m3's topmost
-// binade and a half, and no value overflows.  A value within 2^-14 of its
-// block's largest is off by at most 2^-4 of itself; smaller ones by 2^-10 of
+// binade and a half, and no value overflows.  A value within 2^-13 of its
+// block's largest is off by at most 2^-4 of itself (2^-6 2^s, from which on e4m3
+// has four digits, is below 2^-13.8 of the largest); smaller ones by 2^-10 of
 // 2^s.  The power is held as a byte, s + 127 (at least 0).
 //
 // Memory-bound: 2 bytes read and 1 + 1/32 written an entry, and back.  Four
