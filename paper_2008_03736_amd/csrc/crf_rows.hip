@@ -4,10 +4,10 @@
 // a power of two: with m the block's largest magnitude,
 //     s = ceil(log2(m / 448)),  code = e4m3(x 2^-s),  x' = code 2^s,
 // so that the largest code's magnitude lies in (224, 448], e4m3's topmost
-// binade and a half, and no value overflows.  A value within 2^-13 of its
-// block's largest is off by at most 2^-4 of itself (2^-6 2^s, from which on e4m3
-// has four digits, is below 2^-13.8 of the largest); smaller ones by 2^-10 of
-// 2^s.  The power is held as a byte, s + 127 (at least 0).
+// binade and a half, and no value overflows.  A value x is off by at most the
+// larger of 2^-4 |x| and 2^-10 2^s: by 2^-4 |x| from 2^-6 2^s on, where e4m3 has
+// four digits, and so within 2^-13 of its block's largest (2^-6 / 224 < 2^-13).
+// The power is held as a byte, s + 127 (at least 0).
 //
 // Memory-bound: 2 bytes read and 1 + 1/32 written an entry, and back.  Four
 // lanes take a block (16 bytes of bf16 each), so a block's largest magnitude
