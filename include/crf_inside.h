@@ -436,13 +436,13 @@ int crf_biaffine_bwd_workspace(const crf_plan *plan, int32_t d, int32_t num_labe
  *   dL/dr^l_i = sum_l sum_j G_l(i,j) W_l r^r_j  (W_l's first d rows),
  *   dL/dr^r_j = sum_l sum_i G_l(i,j) W_l^T [r^l_i ; 1],
  *   dL/dW_l   = sum_b sum_{i<j} G_l(i,j) [r^l_i ; 1] r^r_j^T.
- * Products on the matrix cores with fp32 sums; G_l enters as two bf16 parts.
+ * Products on the matrix cores with fp32 sums; G_l and the inner one of two
+ * products enter as two bf16 parts (2^-16 of each is lost at most).
  *   rl, rr, w, d, ldw, num_labels: as crf_biaffine_scores.
  *   grad_scores device float32, the layout of the scores; only cells
  *               0 <= i < j <= n_b are read.
  *   grad_rl, grad_rr  device bf16 bit patterns [B][N1][d], 8-byte aligned, or
- *               NULL: rows 0..n_b are written (the products' inner d x d side
- *               is rounded to bf16 once).
+ *               NULL: rows 0..n_b are written.
  *   grad_w      device float32 [num_labels][d][ldw], 16-byte aligned, or NULL:
  *               the layout of w; entries a <= d are written.
  * Sums run in a fixed order: equal calls give equal bits.  Representations of

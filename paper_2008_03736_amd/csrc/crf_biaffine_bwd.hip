@@ -21,11 +21,13 @@
 // of its shares 11, W's fragments 4; all figures below are of such profiles.
 //
 // Roundings.  R and W are bf16, products and sums fp32.  G, which is fp32, goes
-// in as bf16 hi + lo parts (at most 2^-16 of it is lost), and so does U into
-// dW, which comes out in fp32.  dR^l and dR^r come out in bf16, and there the
-// inner product (R W or G R) is rounded to bf16 once: each term of an output is
-// off by at most 2^-8 of itself, independently, as much as the output's own
-// rounding takes.
+// in as bf16 hi + lo parts (at most 2^-16 of it is lost), and so does the inner
+// product, R W or G R, into the outer one.  dW comes out in fp32, dR^l and dR^r
+// in bf16, their one rounding of that size.  (With the inner product of dR as one
+// bf16 part they were 2.4e-3 off and not 1.7e-3; the second one costs whole
+// sentences a third of the small product with G: 5,000 sentences at d = 500 no
+// time that shows, 138 labels of 100 sentences 201 -> 213 us a call, most of it
+// the long sentences' dense product, done for both parts.)
 //
 // MFMA v_mfma_f32_16x16x32_bf16: lane l supplies A row l%16 and B column l%16
 // at K offsets 8(l/16)..+7 and holds D rows 4(l/16)..+3 of column l%16.  An
@@ -71,6 +73,17 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f3
 __device__ __forceinline__ void parts(float a, float b, uint32_t &hi, uint32_t &lo) {
     hi = two_bf16(a, b);
     lo = two_bf16(a - __builtin_bit_cast(float, hi << 16), b - __builtin_bit_cast(float, hi & 0xFFFF0000u));
+}
+
+// Two fours of a lane as an operand's eight, as bf16 parts hi + lo.
+__device__ __forceinline__ void two_parts(const f32x4 &x, const f32x4 &y, bf16x8 &hi, bf16x8 &lo) {
+    uint4 h, l;
+    parts(x[0], x[1], h.x, l.x);
+    parts(x[2], x[3], h.y, l.y);
+    parts(y[0], y[1], h.z, l.z);
+    parts(y[2], y[3], h.w, l.w);
+    hi = __builtin_bit_cast(bf16x8, h);
+    lo = __builtin_bit_cast(bf16x8, l);
 }
 
 // Representations as the caller holds them: bf16 rows, or 8-bit codes and
@@ -397,13 +410,13 @@ struct Row_ids {
     }
 };
 // o[c]: columns 16 (col0 + c) + 4 lg .. +3 of post 16 r + lr of block blk, whose
-// id is `id`.
-template <int CB, int SIDE>
+// id is `id`.  GROUPS: there may be label groups, whose sums are partial.
+template <int CB, int SIDE, bool GROUPS>
 __device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB], int id, int blk, int r, int grp, int col0,
                                            int dp) {
     const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
     if (id < 0) return;   // (the four lanes of a post alike)
-    if (a.part != nullptr) {
+    if (GROUPS && a.part != nullptr) {
         float *row = a.part + (((size_t)grp * 2 + SIDE) * a.n_posts * kBlk + kBlk * blk + 16 * r + lr) * dp;
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
@@ -436,8 +449,8 @@ __device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB
 // G (R^r W^T) and G^T ([R^l ; 1] W): V = R W first, whose K runs along rows of
 // R, and W's fragments come straight from L2 in the order of the lanes.  A
 // wavefront holds V of its 16 CB columns for all 64 posts, which is the layout
-// of the second product's operand when K is numbered as in grad_frag: V,
-// rounded to bf16, never leaves the registers.  (As (G R) W^T, whose inner
+// of the second product's operand when K is numbered as in grad_frag: V, as
+// two bf16 parts, never leaves the registers.  (As (G R) W^T, whose inner
 // product goes through LDS, 5,000 sentences at d = 500 took 252 us, this way
 // 204: 0.63e15 operations a second.)
 //
@@ -495,7 +508,11 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 bf16x8 pn = pv;
-                if (r + 1 < 4) pn = frag(p + 16 * (r + 1) * RS + 32 * ks);
+                if (r + 1 < 4) {
+                    int at = 16 * (r + 1) * RS + 32 * ks;
+                    asm("" : "+s"(at));   // (a scalar: addresses kept for every r spill)
+                    pn = frag(p + at);
+                }
 #pragma unroll
                 for (int c = 0; c < CB; ++c) v[r][c] = mfma(pv, now[c], v[r][c]);
                 pv = pn;
@@ -509,14 +526,12 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
         }
         if (ks < ksteps) step(ks, wv[0], wv[1]);
     };
-    bf16x8 vb[2][CB];
-    auto round_v = [&]() {
+    bf16x8 vh[2][CB], vl[2][CB];
+    auto split_v = [&]() {
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int t = 0; t < 8; ++t) vb[p][c][t] = (__bf16)v[2 * p + (t >> 2)][c][t & 3];
+            for (int c = 0; c < CB; ++c) two_parts(v[2 * p][c], v[2 * p + 1][c], vh[p][c], vl[p][c]);
     };
     // o += V^T G, posts 16 r .. +15
     auto second = [&](int r, const uint16_t *g, f32x4 (&o)[CB]) {
@@ -525,9 +540,11 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
             if (grad_part<ROWS_I>(r, p)) {
                 const bf16x8 gh = grad_frag<ROWS_I>(g, r, p, lr, lg), gl = grad_frag<ROWS_I>(g + kBlk * kGS, r, p, lr, lg);
 #pragma unroll
-                for (int c = 0; c < CB; ++c) o[c] = mfma(vb[p][c], gh, o[c]);
+                for (int c = 0; c < CB; ++c) o[c] = mfma(vh[p][c], gh, o[c]);
 #pragma unroll
-                for (int c = 0; c < CB; ++c) o[c] = mfma(vb[p][c], gl, o[c]);
+                for (int c = 0; c < CB; ++c) o[c] = mfma(vh[p][c], gl, o[c]);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) o[c] = mfma(vl[p][c], gh, o[c]);
             }
     };
     auto clear = [](f32x4 (&o)[CB]) {
@@ -538,10 +555,13 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
     int it = blockIdx.x;
     if (it >= a.items) return;
     Item x = item_of(a, it);
-    if constexpr (AHEAD) load_r(x.blk);
-    load_grad(x.blk, x.l0);
+    auto load_item = [&](const Item &y) {
+        load_r(y.blk);
+        load_grad(y.blk, y.l0);
+    };
+    if constexpr (AHEAD) load_item(x);
     for (;;) {
-        if constexpr (!AHEAD) load_r(x.blk);
+        if constexpr (!AHEAD) load_item(x);
         const int next_it = it + gridDim.x;
         const Item nx = item_of(a, min(next_it, a.items - 1));
         const int col0 = (x.cz * NW + wave) * CB;   // the wavefront's first column block
@@ -560,34 +580,33 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
                 sg.load(a.g + min(l + 2, x.l1 - 1) * a.cells, at);
                 __builtin_amdgcn_sched_barrier(0);
                 dense(l, col0);
-                round_v();
+                split_v();
+                if constexpr (CB > 1) __builtin_amdgcn_sched_barrier(0);   // (or a few registers spill)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) second(r, now, o[r]);
                 __syncthreads();
             }
-            load_r(nx.blk);
-            load_grad(nx.blk, nx.l0);
+            load_item(nx);
             __builtin_amdgcn_sched_barrier(0);
             Row_ids ids;
             ids.load(a, x.blk);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) store_rows<CB, SIDE>(a, o[r], ids.id[r], x.blk, r, x.grp, col0, DP);
+            for (int r = 0; r < 4; ++r) store_rows<CB, SIDE, COMPACT>(a, o[r], ids.id[r], x.blk, r, x.grp, col0, DP);
         } else {
             __syncthreads();
             dense(0, col0);
-            round_v();
+            split_v();
             __builtin_amdgcn_sched_barrier(0);   // (the registers of V hold the next R)
             Row_ids ids;
             ids.load(a, x.blk);
-            if constexpr (AHEAD) load_r(nx.blk);   // (past the last item, that one's again)
-            load_grad(nx.blk, nx.l0);
+            if constexpr (AHEAD) load_item(nx);   // (past the last item, that one's again)
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 f32x4 o[CB];
                 clear(o);
                 second(r, G, o);
-                store_rows<CB, SIDE>(a, o, ids.id[r], x.blk, r, x.grp, col0, DP);
+                store_rows<CB, SIDE, COMPACT>(a, o, ids.id[r], x.blk, r, x.grp, col0, DP);
             }
             __syncthreads();   // the readers of R and G are done
         }
@@ -609,15 +628,15 @@ __global__ __launch_bounds__(64 * NW, posts_waves(CB, COMPACT)) void bwd_posts_k
 // The same of blocks of a sentence that has more than one, as (G R^r) W^T and
 // (G^T [R^l ; 1]) W: a block of posts meets every block on its side of the
 // diagonal, and only the product with G is repeated for them, not the dense
-// one.  U = G R (or X) goes into LDS as bf16, where R was (its columns are in
-// registers until every wavefront has read R), 64 x DP; R and G of the next
+// one.  U = G R (or X) goes into LDS as two bf16 parts, the first where R was
+// (its columns are in registers until every wavefront has read R), 64 x DP; R and G of the next
 // block are in flight in registers during this one's products.  CB: 16-column
 // blocks of the output a wavefront.
 constexpr int kLongWaves = 8;
 template <int NB>
 struct LongShape {
     static constexpr int kDP = 128 * NB, kPS = kDP + 8;
-    static constexpr int kLds = 2 * (kBlk * kPS + 2 * kBlk * kGS);
+    static constexpr int kLds = 2 * (2 * kBlk * kPS + 2 * kBlk * kGS);
 };
 
 template <int NB, int CB, bool Q8, bool COMPACT, int SIDE>
@@ -627,8 +646,8 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
     constexpr bool ONE = SIDE == 1, ROWS_I = SIDE == 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 15, lg = lane >> 4;
-    uint16_t *P = reinterpret_cast<uint16_t *>(smem);       // [64][PS]: R, then U or X
-    uint16_t *Gh = P + kBlk * PS, *Gl = Gh + kBlk * kGS;
+    uint16_t *P = reinterpret_cast<uint16_t *>(smem);       // [2][64][PS]: R, then the parts of U or X
+    uint16_t *Gh = P + 2 * kBlk * PS, *Gl = Gh + kBlk * kGS;
     const int ksteps = (a.d + 32) / 32;
     const Rows rows = SIDE == 0 ? a.rr : a.rl;
 
@@ -676,6 +695,7 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
                             u[c][r] = mfma(rf[c], gh, u[c][r]);
                             u[c][r] = mfma(rf[c], gl, u[c][r]);
                         }
+                        if constexpr (COMPACT && CB == 4) __builtin_amdgcn_sched_barrier(0);   // (or registers spill)
                     }
             }
         }
@@ -684,9 +704,14 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
 #pragma unroll
         for (int c = 0; c < NB; ++c)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                *reinterpret_cast<bf16x4 *>(P + (16 * r + lr) * PS + 16 * (wave * NB + c) + 4 * lg) =
-                    __builtin_convertvector(u[c][r], bf16x4);
+            for (int r = 0; r < 4; ++r) {
+                uint2 h, l;
+                parts(u[c][r][0], u[c][r][1], h.x, l.x);
+                parts(u[c][r][2], u[c][r][3], h.y, l.y);
+                uint16_t *at = P + (16 * r + lr) * PS + 16 * (wave * NB + c) + 4 * lg;
+                *reinterpret_cast<uint2 *>(at) = h;
+                *reinterpret_cast<uint2 *>(at + kBlk * PS) = l;
+            }
         __syncthreads();
 
         if (!COMPACT || l == x.l0)
@@ -701,9 +726,11 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
             for (int c = 0; c < CB; ++c) wv[c] = frag(wf + ((size_t)ks * (DP / 16) + c) * 512);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const bf16x8 pv = frag(prow + 16 * r * PS + 32 * ks);
+                const bf16x8 ph = frag(prow + 16 * r * PS + 32 * ks), pl = frag(prow + (kBlk + 16 * r) * PS + 32 * ks);
 #pragma unroll
-                for (int c = 0; c < CB; ++c) acc[r][c] = mfma(wv[c], pv, acc[r][c]);
+                for (int c = 0; c < CB; ++c) acc[r][c] = mfma(wv[c], ph, acc[r][c]);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) acc[r][c] = mfma(wv[c], pl, acc[r][c]);
             }
         }
         if (!COMPACT || ++l >= x.l1) break;
@@ -711,7 +738,7 @@ __device__ __forceinline__ void bwd_long(const BwdArgs &a, char *smem) {
     Row_ids ids;
     ids.load(a, x.blk);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) store_rows<CB, SIDE>(a, acc[r], ids.id[r], x.blk, r, x.grp, col0, DP);
+    for (int r = 0; r < 4; ++r) store_rows<CB, SIDE, COMPACT>(a, acc[r], ids.id[r], x.blk, r, x.grp, col0, DP);
 }
 
 template <int NB, int CB, bool Q8, bool COMPACT>
@@ -866,16 +893,7 @@ __global__ __launch_bounds__(64 * NW, 2) void bwd_weight_kernel(WeightArgs a) {
             for (int kp = 0; kp < 2; ++kp) {
                 bf16x8 hi[T], lo[T];
 #pragma unroll
-                for (int c = 0; c < T; ++c) {
-                    const f32x4 &x = u[2 * kp][c], &y = u[2 * kp + 1][c];
-                    uint4 h, l;
-                    parts(x[0], x[1], h.x, l.x);
-                    parts(x[2], x[3], h.y, l.y);
-                    parts(y[0], y[1], h.z, l.z);
-                    parts(y[2], y[3], h.w, l.w);
-                    hi[c] = __builtin_bit_cast(bf16x8, h);
-                    lo[c] = __builtin_bit_cast(bf16x8, l);
-                }
+                for (int c = 0; c < T; ++c) two_parts(u[2 * kp][c], u[2 * kp + 1][c], hi[c], lo[c]);
                 const uint16_t *p = Ra + (blk & 1) * kBlk * AS + (32 * kp + 4 * lg + (lr >> 2)) * AS + 4 * (lr & 3);
                 bf16x8 af = frag_rows(p, p + 16 * AS);
 #pragma unroll

@@ -366,3 +366,40 @@ def test_weight_gradient_of_many_blocks(torch, lengths, d, L, packed):
         want = u.t().contiguous() @ one
         assert float(want.abs().max()) < 2 ** 20
         assert torch.equal(got[q, :, :d + 1].double(), want), q
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("lengths", [[1, 2, 20, 30, 62, 63, 64, 99, 130, 200, 40, 300], [30, 41] * 250 + [80, 140]])
+@pytest.mark.parametrize("d,L", [(28, 1), (100, 1), (124, 3), (252, 1), (252, 2), (380, 1), (380, 2), (500, 1), (500, 2)])
+def test_row_gradients_are_rounded_once(torch, lengths, d, L, packed):
+    """dR^l and dR^r are the bf16 numbers next to their float64 values: the inner
+    product keeps two bf16 parts.  Integers, so that everything before the last
+    rounding is exact: inner products are below 2^16 (two parts) but often above
+    2^8 (one part), sums below 2^24."""
+    dev = torch.device("cuda", 0)
+    n1, Bn = max(lengths) + 1, len(lengths)
+    gen = torch.Generator(dev).manual_seed(d + L)
+    ints = lambda m, *s: torch.randint(-m, m + 1, s, device=dev, generator=gen)
+    n, post = torch.tensor(lengths, device=dev), torch.arange(n1, device=dev)
+    rows = post[None] <= n[:, None]
+    spans = (post[:, None] < post[None])[None] & (post[None, None] <= n[:, None, None])
+    rl, rr = (torch.where(rows[..., None], ints(8, Bn, n1, d), 0) for _ in range(2))
+    held = [x.to(torch.bfloat16) for x in (rl, rr)]
+    g = torch.where(spans[..., None], ints(3, Bn, n1, n1, L).float(), float("nan"))
+    w = torch.zeros((L, d, (d + 4) // 4 * 4), dtype=torch.bfloat16, device=dev)
+    w[..., :d + 1] = ints(4, L, d, d + 1)
+    with B.Plan(lengths, n1=n1, device=dev) as plan:
+        if packed:
+            held = [plan.pack_rows(x) for x in held]
+        got = plan.biaffine_bwd(*held, w, g if L > 1 else g[..., 0], need=(True, True, False))
+    one = torch.cat([rl, rows[..., None].long()], 2).double()
+    want, inner = [torch.zeros((Bn, n1, d), dtype=torch.float64, device=dev) for _ in range(2)], 0.0
+    for q in range(L):
+        gq, wq = torch.nan_to_num(g[..., q]).double(), w[q, :, :d + 1].double()
+        for k, (a, left, right) in enumerate(((gq, rr.double(), wq[:, :d]), (gq.transpose(1, 2).contiguous(), one, wq.t()))):
+            v = (left.reshape(-1, left.shape[2]) @ right.contiguous()).reshape(Bn, n1, d)
+            inner = max(inner, float(v.abs().max()), float(torch.bmm(a, left).abs().max()))
+            want[k] += torch.bmm(a, v)
+    assert 2 ** 8 < inner < 2 ** 16 and max(float(x.abs().max()) for x in want) < 2 ** 22
+    for x, y in zip(got, want):
+        assert torch.equal(x[rows].double(), y[rows].to(torch.bfloat16).double())
