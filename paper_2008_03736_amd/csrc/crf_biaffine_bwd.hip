@@ -769,7 +769,10 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 // dW of one label, a tile of 16 AB columns a by 16 T NW rows c, over a share of
 // the blocks of posts: a wavefront holds U = G R^r of its 16 T columns c in
 // registers, whose layout is that of the second product's operand when K is
-// numbered as in grad_frag, as hi and lo parts.  A step is a block and one of
+// numbered as in grad_frag, as hi and lo parts.  (dW is 3.1e-6 off for the two
+// pairs of parts.  Three of each, all 24 bits of G and U: 9e-8, and 5,000 sentences
+// at d = 500 a call of 464 us where this one takes 425, 200 of them 45.9 and 43.7:
+// the representations it is made of have 8 bits.)  A step is a block and one of
 // its partners: U grows by their product, then R^r and G of the next step (and
 // [R^l ; 1] of the next block, into the other of its two places) go from
 // registers to LDS and those of the step after it start on their way, and
