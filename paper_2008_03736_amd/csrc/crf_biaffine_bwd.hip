@@ -16,18 +16,18 @@
 // What bounds it: the matrix cores, as far as staging lets them.  5,000
 // sentences (130,000 posts) at d = 500 need 2e11 operations, 160 us at the
 // 1.24e15 a second of a large library product, and 0.5 GB, 103 us.  A call
-// takes 442 us, from 8-bit rows 435.  Kernel by kernel, profiled in ten calls
-// from cold: rows 204 (whole sentences) and 23 (long ones), dW 250 and the sum
-// of its shares 11, W's fragments 4; all figures below are of such profiles.
+// takes 445 us, from 8-bit rows 436.  Kernel by kernel, profiled in ten calls
+// from cold: rows 206 (whole sentences) and 29 (long ones), dW 258 and the sum
+// of its shares 11, W's fragments 5; all figures below are of such profiles.
 //
 // Roundings.  R and W are bf16, products and sums fp32.  G, which is fp32, goes
 // in as bf16 hi + lo parts (at most 2^-16 of it is lost), and so does the inner
 // product, R W or G R, into the outer one.  dW comes out in fp32, dR^l and dR^r
-// in bf16, their one rounding of that size.  (With the inner product of dR as one
-// bf16 part they were 2.4e-3 off and not 1.7e-3; the second one costs whole
-// sentences a third of the small product with G: 5,000 sentences at d = 500 no
-// time that shows, 138 labels of 100 sentences 201 -> 213 us a call, most of it
-// the long sentences' dense product, done for both parts.)
+// in bf16, their one rounding of that size.  (With one bf16 part of the inner
+// product of dR they were 2.4e-3 off, and 1.7e-3 is bf16's own.  The second part
+// makes the small product with G half as long again, and the long sentences'
+// dense one twice as long: 5,000 sentences at d = 500 rows 207 -> 206 us and long
+// ones 23 -> 29, 138 labels of 100 sentences at d = 100 63 -> 74 and 38 -> 43.)
 //
 // MFMA v_mfma_f32_16x16x32_bf16: lane l supplies A row l%16 and B column l%16
 // at K offsets 8(l/16)..+7 and holds D rows 4(l/16)..+3 of column l%16.  An
@@ -452,7 +452,7 @@ __device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB
 // of the second product's operand when K is numbered as in grad_frag: V, as
 // two bf16 parts, never leaves the registers.  (As (G R) W^T, whose inner
 // product goes through LDS, 5,000 sentences at d = 500 took 252 us, this way
-// 204: 0.63e15 operations a second.)
+// 206: 0.63e15 operations a second.)
 //
 // Two workgroups a CU (at d = 500 they fill its LDS): one's staging and stores
 // run beside the other's products.  With 128 posts a workgroup and one on a CU,
@@ -770,9 +770,9 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 // the blocks of posts: a wavefront holds U = G R^r of its 16 T columns c in
 // registers, whose layout is that of the second product's operand when K is
 // numbered as in grad_frag, as hi and lo parts.  (dW is 3.1e-6 off for the two
-// pairs of parts.  Three of each, all 24 bits of G and U: 9e-8, and 5,000 sentences
-// at d = 500 a call of 464 us where this one takes 425, 200 of them 45.9 and 43.7:
-// the representations it is made of have 8 bits.)  A step is a block and one of
+// pairs of parts.  Three of each, all 24 bits of G and U, give 9e-8, and take a
+// call of 5,000 sentences at d = 500 9% and one of 200 5% longer, for a gradient
+// whose representations have 8 bits.)  A step is a block and one of
 // its partners: U grows by their product, then R^r and G of the next step (and
 // [R^l ; 1] of the next block, into the other of its two places) go from
 // registers to LDS and those of the step after it start on their way, and
@@ -781,7 +781,7 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 // The tiles of a share read the same posts: they are neighbours on one XCD, so
 // that a post's rows come from HBM once.
 //
-// 5,000 sentences at d = 500: 250 us, of which the matrix instructions take 90
+// 5,000 sentences at d = 500: 258 us, of which the matrix instructions take 90
 // (U's two parts and G's make the products twice as many).  The rest is what
 // two wavefronts a SIMD do not hide: staging's and splitting's arithmetic and
 // LDS reads between the barriers.  Two workgroups of four wavefronts a CU, tiles
