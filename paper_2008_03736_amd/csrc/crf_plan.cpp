@@ -16,6 +16,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <functional>
+#include <memory>
 #include <new>
 #include <numeric>
 #include <vector>
@@ -413,8 +414,9 @@ const char *crf_status_string(int status) {
 
 const char *crf_last_error(void) { return g_last_error; }
 
-int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, int32_t n1,
-                    int32_t num_labels, uint32_t flags) {
+// crf_plan_create, but for host memory that runs out (an exception).
+static int create_plan(crf_plan **out, const int32_t *lengths_host, int32_t batch, int32_t n1,
+                       int32_t num_labels, uint32_t flags) {
     if (out == nullptr) return fail(CRF_EINVAL, "out is NULL");
     *out = nullptr;
     if (lengths_host == nullptr) return fail(CRF_EINVAL, "lengths_host is NULL");
@@ -433,8 +435,15 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     }
 
     // Arguments are valid: from here on HIP calls are made.
-    crf_plan *p = new (std::nothrow) crf_plan();
-    if (p == nullptr) return fail(CRF_ENOMEM, "host allocation of the plan failed");
+    struct Drop {
+        void operator()(crf_plan *x) const {
+            release(x);
+            delete x;
+        }
+    };
+    std::unique_ptr<crf_plan, Drop> held(new crf_plan());
+    crf_plan *const p = held.get();
+    p->allocations.reserve(3);   // (an allocation is put down without one)
     p->B = batch;
     p->n1 = n1;
     p->L = num_labels;
@@ -442,10 +451,10 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     p->flags = flags;
 
     hipError_t e = hipGetDevice(&p->device);
-    if (e != hipSuccess) { delete p; return hip_fail(e, "hipGetDevice"); }
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
     int lds_cap = 0;
     e = hipDeviceGetAttribute(&lds_cap, hipDeviceAttributeMaxSharedMemoryPerBlock, p->device);
-    if (e != hipSuccess) { delete p; return hip_fail(e, "hipDeviceGetAttribute"); }
+    if (e != hipSuccess) return hip_fail(e, "hipDeviceGetAttribute");
 
     // Longest first; ties keep batch order.
     std::vector<int32_t> order(batch);
@@ -850,8 +859,6 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     tables.add(tile_ws_recs, &kp.tile_ws.recs);
     if ((e = tables.upload(p)) != hipSuccess) {
         const int code = (e == hipErrorOutOfMemory) ? CRF_ENOMEM : CRF_EHIP;
-        release(p);
-        delete p;
         return code == CRF_ENOMEM ? fail(code, "device allocation of the schedule failed")
                                   : hip_fail(e, "schedule upload");
     }
@@ -872,11 +879,8 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
         kp.team_cap = std::max(0, cus) * crf::spill_blocks_per_cu();
         if (kp.team_cap >= 16) {
             void *a = nullptr;
-            if ((e = hipMalloc(&a, (size_t)crf::kTeamAreaBytes)) != hipSuccess || (p->allocations.push_back(a), false)) {
-                release(p);
-                delete p;
-                return hip_fail(e, "team area");
-            }
+            if ((e = hipMalloc(&a, (size_t)crf::kTeamAreaBytes)) != hipSuccess) return hip_fail(e, "team area");
+            p->allocations.push_back(a);
             kp.team_area = static_cast<int32_t *>(a);
         }
     }
@@ -884,12 +888,8 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     if (p->ws_bytes > 0) {
         void *ws = nullptr;
         e = hipMalloc(&ws, (size_t)p->ws_bytes);
-        if (e != hipSuccess) {
-            release(p);
-            delete p;
-            return fail(CRF_ENOMEM, "workspace of %lld bytes: %s", (long long)p->ws_bytes,
-                        hipGetErrorString(e));
-        }
+        if (e != hipSuccess)
+            return fail(CRF_ENOMEM, "workspace of %lld bytes: %s", (long long)p->ws_bytes, hipGetErrorString(e));
         p->allocations.push_back(ws);
         kp.ws = static_cast<char *>(ws);
     }
@@ -902,8 +902,17 @@ int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, 
     // point now (it retries, and reports a failure, on its first call).
     char *scr = nullptr;
     if (crf::scratch_address(p->device, &scr) != hipSuccess) (void)hipGetLastError();
-    *out = p;
+    *out = held.release();
     return ok();
+}
+
+int crf_plan_create(crf_plan **out, const int32_t *lengths_host, int32_t batch, int32_t n1,
+                    int32_t num_labels, uint32_t flags) {
+    try {
+        return create_plan(out, lengths_host, batch, n1, num_labels, flags);
+    } catch (const std::bad_alloc &) {
+        return fail(CRF_ENOMEM, "host allocation of the plan failed");
+    }
 }
 
 int crf_plan_destroy(crf_plan *plan) {

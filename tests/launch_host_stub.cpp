@@ -6,6 +6,9 @@
 //                        "EARLY name" of each kernel launched before its
 //                        attribute was set, then "launches N"
 //   creation LIB LENGTHS...              "mallocs N copies N" of crf_plan_create
+//   memory LIB LENGTHS...                crf_plan_create with host memory that runs out
+//                        after 0, 1, 2, ... allocations: "status N times N" of each
+//                        status in a row, "left N" device allocations never freed
 //   launches LIB CALL FLAGS LENGTHS...   the kernels of a call in order, "K name",
 //                        and "A sentences pointer" of one that marks log Z as missing
 #include <cxxabi.h>
@@ -20,6 +23,7 @@
 #include <cstring>
 #include <map>
 #include <mutex>
+#include <new>
 #include <set>
 #include <string>
 #include <thread>
@@ -33,7 +37,8 @@ std::map<const void *, std::string> names;
 std::set<const void *> ready;       // functions whose LDS attribute is set
 std::vector<std::string> launched, early, marked;
 void *const workspace = reinterpret_cast<void *>((uintptr_t)9 << 40);
-int mallocs = 0, copies = 0;
+int mallocs = 0, frees = 0, copies = 0;
+thread_local int64_t news_left = -1;   // host allocations until one fails; -1: none does
 bool slow_attributes = false, watch_attributes = false;
 struct Config {
     dim3 grid, block;
@@ -42,6 +47,17 @@ struct Config {
 };
 thread_local Config config;
 }  // namespace
+
+// (the library's allocations too)
+void *operator new(size_t n) {
+    if (news_left == 0) throw std::bad_alloc();
+    if (news_left > 0) --news_left;
+    void *p = std::malloc(n ? n : 1);
+    if (p == nullptr) throw std::bad_alloc();
+    return p;
+}
+void operator delete(void *p) noexcept { std::free(p); }
+void operator delete(void *p, size_t) noexcept { std::free(p); }
 
 extern "C" {
 void **__hipRegisterFatBinary(const void *) {
@@ -100,6 +116,7 @@ hipError_t hipMalloc(void **p, size_t n) {
     return *p ? hipSuccess : hipErrorOutOfMemory;
 }
 hipError_t hipFree(void *p) {
+    frees += p != nullptr;
     std::free(p);
     return hipSuccess;
 }
@@ -266,6 +283,29 @@ int attributes(void *lib) {
     return 0;
 }
 
+int memory(void *lib, const std::vector<int32_t> &len) {
+    ENTRY(crf_plan_create); ENTRY(crf_plan_destroy); ENTRY(crf_last_error);
+    int last = -1, times = 0;
+    mallocs = frees = 0;
+    auto tell = [&]() {
+        if (times > 0) std::printf("status %d times %d\n", last, times);
+    };
+    for (int64_t k = 0; last != CRF_OK; ++k) {
+        crf_plan *p = nullptr;
+        news_left = k;
+        const int rc = crf_plan_create(&p, len.data(), (int32_t)len.size(), *std::max_element(len.begin(), len.end()) + 1, 1, 0);
+        news_left = -1;
+        if (rc != CRF_OK && (p != nullptr || crf_last_error()[0] == 0)) return 1;
+        if (rc == CRF_OK) crf_plan_destroy(p);
+        if (rc != last) tell(), times = 0;
+        last = rc;
+        ++times;
+    }
+    tell();
+    std::printf("left %d\n", mallocs - frees);
+    return 0;
+}
+
 int creation(void *lib, const std::vector<int32_t> &len) {
     ENTRY(crf_plan_create); ENTRY(crf_plan_destroy);
     crf_plan *p = nullptr;
@@ -313,10 +353,10 @@ int main(int argc, char **argv) {
     const std::string mode = argv[1];
     if (mode == "alias") return aliases(lib);
     if (mode == "attributes") return attributes(lib);
-    if (mode == "creation" && argc > 3) {
+    if ((mode == "creation" || mode == "memory") && argc > 3) {
         std::vector<int32_t> len;
         for (int k = 3; k < argc; ++k) len.push_back(std::atoi(argv[k]));
-        return creation(lib, len);
+        return mode == "memory" ? memory(lib, len) : creation(lib, len);
     }
     if (mode == "launches" && argc > 5) {
         std::vector<int32_t> len;

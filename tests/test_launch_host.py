@@ -78,3 +78,10 @@ def test_a_plan_is_made_with_few_device_calls(harness, lengths):
     # tables in one copy, and three of the 198 sentences are past 64 KB)
     (row,) = run(harness, "creation", *lengths)
     assert int(row[1]) <= 1 + 2 * (max(lengths) > 96) and int(row[3]) <= 1 + 3 * (len(lengths) > 100)
+
+
+def test_host_memory_that_runs_out(harness):
+    # a status, not an exception out of a C function, and nothing left behind
+    rows = run(harness, "memory", 25, 60, 70, 300, 460)
+    assert [r[:2] for r in rows[:-1]] == [["status", str(B.CRF_ENOMEM)], ["status", str(B.CRF_OK)]]
+    assert int(rows[0][3]) > 50 and rows[-1] == ["left", "0"]
