@@ -16,8 +16,8 @@
 // What bounds it: the matrix cores, as far as staging lets them.  5,000
 // sentences (130,000 posts) at d = 500 need 2e11 operations, 160 us at the
 // 1.24e15 a second of a large library product, and 0.5 GB, 103 us.  A call
-// takes 445 us, from 8-bit rows 436.  Kernel by kernel, profiled in ten calls
-// from cold: rows 206 (whole sentences) and 29 (long ones), dW 258 and the sum
+// takes 437 us, from 8-bit rows 423.  Kernel by kernel, profiled in ten calls
+// from cold: rows 206 (whole sentences) and 29 (long ones), dW 254 and the sum
 // of its shares 11, W's fragments 5; all figures below are of such profiles.
 //
 // Roundings.  R and W are bf16, products and sums fp32.  G, which is fp32, goes
@@ -781,11 +781,12 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 // The tiles of a share read the same posts: they are neighbours on one XCD, so
 // that a post's rows come from HBM once.
 //
-// 5,000 sentences at d = 500: 258 us, of which the matrix instructions take 90
+// 5,000 sentences at d = 500: 254 us, of which the matrix instructions take 90
 // (U's two parts and G's make the products twice as many).  The rest is what
 // two wavefronts a SIMD do not hide: staging's and splitting's arithmetic and
 // LDS reads between the barriers.  Two workgroups of four wavefronts a CU, tiles
-// of 256 x 128, whose phases drift apart, took 284: [R^l ; 1] is staged twice.
+// of 256 x 128, whose phases drift apart, took 284 (then against 250): [R^l ; 1] is
+// staged twice.
 struct WeightArgs {
     const int32_t *posts;
     const int64_t *post_cells;
