@@ -445,10 +445,11 @@ int crf_biaffine_bwd_workspace(const crf_plan *plan, int32_t d, int32_t num_labe
  *               NULL: rows 0..n_b are written.
  *   grad_w      device float32 [num_labels][d][ldw], 16-byte aligned, or NULL:
  *               the layout of w; entries a <= d are written.
- * Sums run in a fixed order: equal calls give equal bits.  Representations of
- * valid fence posts and gradients of spans must be finite: sentences share
- * tiles, so one's infinity or NaN can make the gradients of others NaN.  No
- * gradient may alias an input or another one.
+ * Sums run in a fixed order: equal calls give equal bits.  An infinity or NaN
+ * among a sentence's representations or its spans' gradients makes rows of its
+ * own grad_rl and grad_rr NaN (short sentences: all rows of the one that the
+ * representation enters) and shows in grad_w; other sentences' rows are as
+ * without it.  W must be finite.  No gradient may alias an input or another one.
  */
 int crf_biaffine_bwd(const crf_plan *plan, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int32_t d,
                      int32_t ldw, int32_t num_labels, const float *grad_scores, uint16_t *grad_rl, uint16_t *grad_rr,

@@ -139,10 +139,12 @@ struct Staged {
     }
     // post: the block's record
     __device__ __forceinline__ void load(const Rows &r, const int32_t *post, int k0, int d) {
-        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = k0 + col();
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        int k = k0 + col();
 #pragma unroll
         for (int u = 0; u < kRows; ++u) id[u] = constant(post + kRows * w + u);
         if constexpr (Q8) {
+            asm volatile("" : "+v"(k));   // (places found here: kept over the items, a few of them spill)
             const int wide = row_codes(d), kc = min(k, wide - 8);
 #pragma unroll
             for (int u = 0; u < kEach; ++u) {
@@ -165,30 +167,68 @@ struct Staged {
             }
         }
     }
-    // ONE: entry d is 1
+    // The eight entries of piece u (bf16).  ONE: entry d is 1.
+    template <bool ONE>
+    __device__ __forceinline__ uint4 piece(const Rows &r, int k0, int d, int u) const {
+        const int k = k0 + col();
+        const bool full = k + 8 <= d, half = k + 4 == d, row_in = id_of(u) >= 0;
+        uint4 p = v[u];
+        if constexpr (Q8) {
+            p = eight_of_codes(make_uint2(p.x, p.y), p.z);
+            p = make_uint4(p.x, p.y, full ? p.z : 0u, full ? p.w : 0u);
+        } else {
+            const bool low = full || (d < 8 && id_of(u) <= r.last);
+            p = make_uint4(low ? p.x : p.z, low ? p.y : p.w, full ? p.z : 0u, full ? p.w : 0u);
+        }
+        const bool in = row_in && (full || half);
+        p = make_uint4(in ? p.x : 0u, in ? p.y : 0u, in ? p.z : 0u, in ? p.w : 0u);
+        if constexpr (ONE) {
+            p.x = row_in && k == d ? 0x3F80u : p.x;
+            p.z = row_in && half ? 0x3F80u : p.z;
+        }
+        return p;
+    }
     template <bool ONE>
     __device__ __forceinline__ void store(const Rows &r, int k0, int d, uint16_t *to, int stride) const {
-        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = k0 + col();
-        const bool full = k + 8 <= d, half = k + 4 == d;
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
-            const bool row_in = id_of(u) >= 0;
-            uint4 p = v[u];
-            if constexpr (Q8) {
-                p = eight_of_codes(make_uint2(p.x, p.y), p.z);
-                p = make_uint4(p.x, p.y, full ? p.z : 0u, full ? p.w : 0u);
-            } else {
-                const bool low = full || (d < 8 && id_of(u) <= r.last);
-                p = make_uint4(low ? p.x : p.z, low ? p.y : p.w, full ? p.z : 0u, full ? p.w : 0u);
-            }
-            const bool in = row_in && (full || half);
-            p = make_uint4(in ? p.x : 0u, in ? p.y : 0u, in ? p.z : 0u, in ? p.w : 0u);
-            if constexpr (ONE) {
-                p.x = row_in && k == d ? 0x3F80u : p.x;
-                p.z = row_in && half ? 0x3F80u : p.z;
-            }
+            const uint4 p = piece<ONE>(r, k0, d, u);
             if (col() < stride) *reinterpret_cast<uint4 *>(to + (kRows * w + row(u)) * stride + col()) = p;
         }
+    }
+    // Of the eight, infinities and NaN: bits 0x8000 of the halves.
+    static __device__ __forceinline__ uint32_t not_finite(const uint4 &p) {
+        auto over = [](uint32_t x) { return (x & 0x7FFF7FFFu) + 0x00800080u; };
+        return over(p.x) | over(p.y) | over(p.z) | over(p.w);
+    }
+    // The same, but rows with an infinity or NaN are stored as zeros, and told of:
+    // bit u is row kRows w + u.
+    template <bool ONE>
+    __device__ __forceinline__ uint32_t store_finite(const Rows &r, int k0, int d, uint16_t *to, int stride) const {
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        uint32_t any = 0;
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+            const uint4 p = piece<ONE>(r, k0, d, u);
+            any |= not_finite(p);
+            if (col() < stride) *reinterpret_cast<uint4 *>(to + (kRows * w + row(u)) * stride + col()) = p;
+        }
+        uint32_t bad = 0;
+        if (__ballot((any & 0x80008000u) != 0) == 0) return bad;
+        // (rarely: from LDS, row by row.  The asm keeps what only this needs out of
+        // the registers of the loop around it)
+        int at = 8 * lane, zero = 0;
+        asm volatile("" : "+v"(at), "+v"(zero));
+#pragma unroll 1
+        for (int u = 0; u < kRows; ++u) {
+            uint16_t *p = to + (kRows * w + u) * stride + at;
+            const bool hit = at < min(stride, COLS) && (not_finite(*reinterpret_cast<const uint4 *>(p)) & 0x80008000u) != 0;
+            if (__ballot(hit) == 0) continue;
+            bad |= 1u << u;
+            if (at < stride) *reinterpret_cast<uint4 *>(p) = make_uint4(zero, zero, zero, zero);
+        }
+        return bad;
     }
 };
 
@@ -552,6 +592,32 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
         for (int c = 0; c < CB; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     };
 
+    // A representation that is not finite.  Its row of R is staged as zeros (times
+    // a zero of G or W it would be NaN in the rows of other sentences), and the
+    // rows of its own sentence become NaN through G: row 63 of G^T (ROWS_I) or
+    // column 31 meet each of them in a part that is multiplied, and a V that is
+    // finite (they are past the 24 entries that R's last row runs into).  Which
+    // rows these are goes round in the padding of G's rows.
+    static_assert(kGS - kBlk >= 2 && kBlk / NW <= 16);
+    uint32_t *const bad_rows = reinterpret_cast<uint32_t *>(G + kBlk);   // wavefront w's: word w kGS / 2
+    auto poison = [&](int blk, uint32_t mine) {   // mine: lane w's word (every wavefront alike)
+        if (__ballot(mine != 0) == 0) return;
+        const int32_t *rest = a.posts + (size_t)blk * kPostRec + kBlk;
+        auto is_bad = [&](int post) { return bad_rows[post / (kBlk / NW) * (kGS / 2)] >> (post % (kBlk / NW)) & 1u; };
+        int post = threadIdx.x;
+        asm volatile("" : "+v"(post));
+        if (post < kBlk && rest[post - kBlk] >= 0) {
+            int first = post, last = post;
+            while (first > 0 && rest[first - 1] > 0) --first;   // (a sentence's last post has no cells)
+            while (rest[last] > 0) ++last;
+            uint32_t any = 0;
+            for (int k = first; k <= last; ++k) any |= is_bad(k);
+            if (any) G[ROWS_I ? (kBlk - 1) * kGS + post : post * kGS + 31] = 0x7FC0;
+        }
+        __syncthreads();
+    };
+    auto bad_word = [&]() { return lane < NW ? bad_rows[lane * (kGS / 2)] : 0u; };
+
     int it = blockIdx.x;
     if (it >= a.items) return;
     Item x = item_of(a, it);
@@ -565,7 +631,8 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
         const int next_it = it + gridDim.x;
         const Item nx = item_of(a, min(next_it, a.items - 1));
         const int col0 = (x.cz * NW + wave) * CB;   // the wavefront's first column block
-        sr.template store<ONE>(rows, 0, a.d, R, RS);
+        const uint32_t bad = sr.template store_finite<ONE>(rows, 0, a.d, R, RS);
+        if (lane == 0) bad_rows[wave * (kGS / 2)] = bad;
         sg.store(G, G + kBlk * kGS);
         if constexpr (COMPACT) {
             f32x4 o[4][CB];
@@ -574,6 +641,7 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
             const typename Staged_grad<NW>::Places at = sg.places(a.post_cells, a.posts, x.blk);
             sg.load(a.g + min(x.l0 + 1, x.l1 - 1) * a.cells, at);
             __syncthreads();
+            poison(x.blk, bad_word());
             for (int l = x.l0; l < x.l1; ++l) {
                 uint16_t *now = G + ((l - x.l0) & 1) * 2 * kBlk * kGS, *then = G + ((l - x.l0 + 1) & 1) * 2 * kBlk * kGS;
                 sg.store(then, then + kBlk * kGS);   // (its readers are a barrier behind)
@@ -594,6 +662,7 @@ __device__ __forceinline__ void bwd_posts(const BwdArgs &a, char *smem) {
             for (int r = 0; r < 4; ++r) store_rows<CB, SIDE, COMPACT>(a, o[r], ids.id[r], x.blk, r, x.grp, col0, DP);
         } else {
             __syncthreads();
+            poison(x.blk, bad_word());
             dense(0, col0);
             split_v();
             __builtin_amdgcn_sched_barrier(0);   // (the registers of V hold the next R)

@@ -403,3 +403,49 @@ def test_row_gradients_are_rounded_once(torch, lengths, d, L, packed):
     assert 2 ** 8 < inner < 2 ** 16 and max(float(x.abs().max()) for x in want) < 2 ** 22
     for x, y in zip(got, want):
         assert torch.equal(x[rows].double(), y[rows].to(torch.bfloat16).double())
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("d,L", [(4, 1), (28, 1), (100, 1), (124, 3), (252, 1), (252, 2), (380, 1), (380, 2), (500, 1), (508, 2),
+                                 (60, 40)])
+def test_a_sentence_that_is_not_finite_keeps_to_itself(torch, d, L, packed):
+    """Infinities and NaN in one sentence's representations, at its ends, inside
+    and in the last entries of rows: the rows of the others' gradients are
+    unchanged, its own hold NaN, and dW has them in the entries that they enter."""
+    dev = torch.device("cuda", 0)
+    lengths = [20, 9, 13, 30, 1, 25, 62, 5, 63, 64, 100, 7, 18] * 2
+    inp = W.biaffine_inputs(lengths, d, labels=L, seed=d)
+    n1 = inp.n1
+    rl, rr, w = tensors(torch, inp, (d + 4) // 4 * 4, n1)
+    rl, rr, w = (x.view(torch.bfloat16) for x in (rl, rr, w))
+    g = torch.from_numpy(gradient(lengths, n1, L, 3)).to(dev)
+    there = (torch.arange(n1, device=dev)[None] <= torch.tensor(lengths, device=dev)[:, None])
+    with B.Plan(lengths, n1=n1, device=dev) as plan:
+        rows = lambda x: plan.pack_rows(x) if packed else x
+        call = lambda a, b: plan.biaffine_bwd(rows(a), rows(b), w, g)
+        want = call(rl, rr)
+        assert all(torch.isfinite(x[there]).all() for x in want[:2])
+        for b, post, col, bad in ((0, 0, 0, "nan"), (1, 9, d - 1, "inf"), (2, 6, d // 2, "-inf"), (4, 1, d - 1, "nan"),
+                                  (6, 62, 1, "nan"), (8, 63, d - 1, "inf"), (9, 64, 2, "nan"), (10, 70, d - 2, "nan"),
+                                  (12, 0, d - 1, "inf"), (25, 18, 0, "nan")):
+            for side in range(2):   # (dR^l comes from R^r, dR^r from R^l)
+                x = [rl.clone(), rr.clone()]
+                x[side][b, post, col] = float(bad)
+                got = call(*x)
+                others = [k for k in range(len(lengths)) if k != b]
+                assert torch.equal(got[side], want[side])
+                assert torch.equal(got[1 - side][others], want[1 - side][others]), (b, side)
+                if not (post == 0 and side) and not (post == lengths[b] and not side):   # (which no span has on that side)
+                    assert torch.isnan(got[1 - side][b, :lengths[b] + 1]).any(), (b, side)
+                k = slice(None), (col if side else slice(None)), (slice(None, d + 1) if side else col)
+                keep = torch.ones_like(got[2], dtype=torch.bool)
+                keep[k] = False
+                assert torch.equal(got[2][keep], want[2][keep]), (b, side)
+        for b, i, j, bad in ((0, 0, 1, "nan"), (3, 0, 30, "inf"), (6, 61, 62, "nan"), (10, 3, 99, "nan")):
+            h = g.clone()   # (a span's gradient)
+            h[b, i, j] = float(bad)
+            got = plan.biaffine_bwd(rows(rl), rows(rr), w, h)
+            others = [k for k in range(len(lengths)) if k != b]
+            for side, post in ((0, i), (1, j)):
+                assert torch.equal(got[side][others], want[side][others])
+                assert not torch.isfinite(got[side][b, post]).all()
