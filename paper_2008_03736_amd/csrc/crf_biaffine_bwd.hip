@@ -16,8 +16,8 @@
 // What bounds it: the matrix cores, as far as staging lets them.  5,000
 // sentences (130,000 posts) at d = 500 need 2e11 operations, 160 us at the
 // 1.24e15 a second of a large library product, and 0.5 GB, 103 us.  A call
-// takes 437 us, from 8-bit rows 423.  Kernel by kernel, profiled in ten calls
-// from cold: rows 206 (whole sentences) and 29 (long ones), dW 254 and the sum
+// takes 446 us, from 8-bit rows 444.  Kernel by kernel, profiled in ten calls
+// from cold: rows 207 (whole sentences) and 29 (long ones), dW 252 and the sum
 // of its shares 11, W's fragments 5; all figures below are of such profiles.
 //
 // Roundings.  R and W are bf16, products and sums fp32.  G, which is fp32, goes
@@ -26,8 +26,8 @@
 // in bf16, their one rounding of that size.  (With one bf16 part of the inner
 // product of dR they were 2.4e-3 off, and 1.7e-3 is bf16's own.  The second part
 // makes the small product with G half as long again, and the long sentences'
-// dense one twice as long: 5,000 sentences at d = 500 rows 207 -> 206 us and long
-// ones 23 -> 29, 138 labels of 100 sentences at d = 100 63 -> 74 and 38 -> 43.)
+// dense one twice as long: 5,000 sentences at d = 500 rows 207 us either way and
+// long ones 23 -> 29, 138 labels of 100 sentences at d = 100 63 -> 73 and 38 -> 43.)
 //
 // MFMA v_mfma_f32_16x16x32_bf16: lane l supplies A row l%16 and B column l%16
 // at K offsets 8(l/16)..+7 and holds D rows 4(l/16)..+3 of column l%16.  An
@@ -492,7 +492,7 @@ __device__ __forceinline__ void store_rows(const BwdArgs &a, const f32x4 (&o)[CB
 // of the second product's operand when K is numbered as in grad_frag: V, as
 // two bf16 parts, never leaves the registers.  (As (G R) W^T, whose inner
 // product goes through LDS, 5,000 sentences at d = 500 took 252 us, this way
-// 206: 0.63e15 operations a second.)
+// 207: 0.63e15 operations a second.)
 //
 // Two workgroups a CU (at d = 500 they fill its LDS): one's staging and stores
 // run beside the other's products.  With 128 posts a workgroup and one on a CU,
@@ -850,7 +850,7 @@ __global__ __launch_bounds__(256) void bwd_join_rows_kernel(const int32_t *__res
 // The tiles of a share read the same posts: they are neighbours on one XCD, so
 // that a post's rows come from HBM once.
 //
-// 5,000 sentences at d = 500: 254 us, of which the matrix instructions take 90
+// 5,000 sentences at d = 500: 252 us, of which the matrix instructions take 90
 // (U's two parts and G's make the products twice as many).  The rest is what
 // two wavefronts a SIMD do not hide: staging's and splitting's arithmetic and
 // LDS reads between the barriers.  Two workgroups of four wavefronts a CU, tiles
