@@ -22,7 +22,10 @@
  *     by the biaffine scorer (Sec. 2.2, Eq. biaffine), and the scorer's
  *     backward pass, from the representations or from an 8-bit form of them;
  *   - log-probabilities of given trees and a clipped policy loss on them with
- *     its gradient, for training past the gold trees.
+ *     its gradient, for training past the gold trees;
+ *   - what else training a scorer takes: layer norm of the rows that it reads
+ *     and a learned bias by a span's width, each with its gradients, and the
+ *     update of its weights by their orthogonalised momentum.
  *
  * Conventions
  *   Fence posts.  A sentence of n words has boundaries 0..n; span (i,j),
@@ -103,6 +106,12 @@ enum {
 #define CRF_MAX_LABELS 4096   /* most labels per span */
 #define CRF_MAX_TREES 64      /* most candidate trees per sentence */
 #define CRF_MAX_ROW 8192      /* longest activation row held in 8 bits */
+#define CRF_MAX_BUCKETS 1024  /* most buckets of span widths */
+#define CRF_MAX_STEPS 32      /* most Newton-Schulz steps */
+
+/* Types of rows that a call takes in more than one. */
+#define CRF_BF16 0            /* bf16 bit patterns */
+#define CRF_F32 1             /* float32 */
 
 /* Plan flags. */
 #define CRF_FORCE_SPILL 0x1u  /* run every sentence on the workspace-chart kernels */
@@ -327,7 +336,8 @@ int crf_inside_fwd_bwd_cky_noalloc(const crf_plan *plan, const float *scores, co
  * only while they run: calls that may overlap need one each (two graphs that
  * are replayed side by side too).  The tree calls still use the plan's own
  * workspace like the others, so they must not overlap other calls on the plan;
- * packing, unpacking and the scorer's backward pass use nothing of it and may.
+ * packing, unpacking, the scorer's backward pass, layer norm and the width bias
+ * use nothing of it and may.
  * In all of them no output, and not the workspace, may overlap an input or
  * another output (CRF_EINVAL, by the arrays' full sizes).
  */
@@ -462,6 +472,118 @@ int crf_biaffine_bwd_packed(const crf_plan *plan, const uint8_t *rl_codes, const
                             const uint8_t *rr_codes, const uint8_t *rr_scales, const uint16_t *w, int32_t d, int32_t ldw,
                             int32_t num_labels, const float *grad_scores, uint16_t *grad_rl, uint16_t *grad_rr,
                             float *grad_w, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * crf_layer_norm -- layer norm of activation rows: with m and v the mean and the
+ * variance of a row's d entries,
+ *   y = (x - m) / sqrt(v + eps) * gamma + beta.
+ * Sums in float32; the variance is that of the deviations from the mean.
+ *   x       device [B][N1][d], bf16 bit patterns (x_type CRF_BF16, 8-byte
+ *           aligned) or float32 (CRF_F32); rows past n_b are not read.
+ *   d       4 <= d <= CRF_MAX_ROW, a multiple of 4.
+ *   gamma, beta  device float32[d], or NULL: 1 and 0.
+ *   eps     positive.
+ *   y       device bf16 bit patterns [B][N1][d], 8-byte aligned; must not alias x.
+ * A row with an infinity or NaN becomes NaN, other rows are as without it.  Rows
+ * past n_b are left as they were.  B, N1 and the lengths are the plan's.
+ */
+int crf_layer_norm(const crf_plan *plan, const void *x, int32_t x_type, int32_t d, const float *gamma, const float *beta,
+                   float eps, uint16_t *y, void *stream);
+
+/* crf_layer_norm_bwd_workspace -- bytes of workspace of crf_layer_norm_bwd. */
+int crf_layer_norm_bwd_workspace(const crf_plan *plan, int32_t d, int64_t *bytes);
+
+/*
+ * crf_layer_norm_bwd -- the backward pass of crf_layer_norm.  With h the
+ * normalised row, r = 1 / sqrt(v + eps) and u = grad_y gamma,
+ *   grad_x = r (u - mean(u) - h mean(u h)),
+ *   grad_gamma = sum of grad_y h over the batch's rows, grad_beta = sum of grad_y.
+ * The statistics are taken from x again.
+ *   x, x_type, d, gamma, eps: as crf_layer_norm.
+ *   grad_y      device bf16 bit patterns [B][N1][d], 8-byte aligned; rows past
+ *               n_b are not read.
+ *   grad_x      device, x's type and layout, or NULL: rows 0..n_b are written.
+ *   grad_gamma, grad_beta  device float32[d], or NULL.
+ * Sums run in a fixed order: equal calls give equal bits.
+ */
+int crf_layer_norm_bwd(const crf_plan *plan, const void *x, int32_t x_type, int32_t d, const float *gamma,
+                       const uint16_t *grad_y, float eps, void *grad_x, float *grad_gamma, float *grad_beta,
+                       void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * crf_width_bias -- a learned bias by a span's width, widths in buckets:
+ *   out(i,j,l) = scores(i,j,l) + table[buckets[j - i]][l].
+ *   scores      device float32, [B][N1][N1] when num_labels = 1, else
+ *               [B][N1][N1][num_labels]; only cells 0 <= i < j <= n_b are read.
+ *   num_labels  1 <= num_labels <= CRF_MAX_LABELS (the plan's own is not used).
+ *   table       device float32 [num_buckets][num_labels].
+ *   buckets     device int32[N1]: the bucket of each width (entry 0 is not
+ *               read); spans whose bucket is outside 0 .. num_buckets - 1 get
+ *               no bias.
+ *   num_buckets 1 <= num_buckets <= CRF_MAX_BUCKETS.
+ *   out         device float32, layout of scores, valid cells only; may be
+ *               scores itself, must not overlap it otherwise.
+ */
+int crf_width_bias(const crf_plan *plan, const float *scores, int32_t num_labels, const float *table,
+                   const int32_t *buckets, int32_t num_buckets, float *out, void *stream);
+
+/* crf_width_bias_bwd_workspace -- bytes of workspace of crf_width_bias_bwd. */
+int crf_width_bias_bwd_workspace(const crf_plan *plan, int32_t num_labels, int64_t *bytes);
+
+/*
+ * crf_width_bias_bwd -- the backward pass of crf_width_bias.
+ *   grad_out    device float32, layout of the scores; valid cells are read.
+ *   grad_scores device float32, the same layout, or NULL: grad_out on valid
+ *               cells (the others are left as they were); must not alias it.
+ *   grad_table  device float32 [num_buckets][num_labels], or NULL: for each
+ *               bucket and label the sum of grad_out over the batch's spans of
+ *               the bucket's widths (0 where it has none).
+ * Sums in float32 in a fixed order: equal calls give equal bits.
+ */
+int crf_width_bias_bwd(const crf_plan *plan, const float *grad_out, int32_t num_labels, const int32_t *buckets,
+                       int32_t num_buckets, float *grad_scores, float *grad_table, void *workspace,
+                       int64_t workspace_bytes, void *stream);
+
+/* crf_orthogonalize_workspace -- bytes of workspace of crf_orthogonalize and
+ * crf_muon_step.  The three calls take no plan and run on the current device. */
+int crf_orthogonalize_workspace(int32_t count, int32_t rows, int32_t cols, int64_t *bytes);
+
+/*
+ * crf_orthogonalize -- matrices with their singular values brought towards 1 by
+ * Newton-Schulz products: X = x / (|x|_F + eps), then for each step's (a, b, c)
+ *   A = X X^T,  X <- a X + (b A + c A A) X.
+ * Operands of the products are held as two float16 parts (22 bits), sums are
+ * float32; |x|_F is summed in float64.
+ *   x, out        device float32 [count][rows][ld], entries [..][cols] of a row;
+ *                 the others are neither read nor written.  out must not alias x.
+ *   count         1 <= count <= CRF_MAX_LABELS.
+ *   rows, cols    1 to CRF_MAX_ROW each; ld >= cols.
+ *   coefficients  host float[steps][3], read during the call.  Singular values
+ *                 from [0, 1] must stay in [0, 4] after every step, and
+ *                 |b s^2 + c s^4| within 60 (CRF_EINVAL otherwise: the parts of
+ *                 larger values would overflow).
+ *   steps         1 <= steps <= CRF_MAX_STEPS.
+ *   eps           positive.
+ * A matrix with an infinity or NaN gives NaN everywhere, the others are as
+ * without it; a matrix of zeros gives zeros.
+ */
+int crf_orthogonalize(const float *x, int32_t count, int32_t rows, int32_t cols, int32_t ld, const float *coefficients,
+                      int32_t steps, float eps, float *out, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * crf_muon_step -- weights moved by their orthogonalised momentum: with X the
+ * result of crf_orthogonalize for U,
+ *   momentum_out = mu momentum + grad,
+ *   U = grad + mu momentum_out (nesterov), or momentum_out,
+ *   w_out = (1 - decay) w - rate X.
+ *   w, grad, momentum, w_out, momentum_out  device float32 [count][rows][ld] (the
+ *               scorer's W as it lies: rows d, cols d + 1).  w_out may be w and
+ *               momentum_out momentum; no other buffers may overlap.
+ *   mu, rate    at least 0; 0 <= decay <= 1.
+ */
+int crf_muon_step(const float *w, const float *grad, const float *momentum, int32_t count, int32_t rows, int32_t cols,
+                  int32_t ld, float mu, int32_t nesterov, float rate, float decay, const float *coefficients, int32_t steps,
+                  float eps, float *w_out, float *momentum_out, void *workspace, int64_t workspace_bytes, void *stream);
 
 /* Static description of a status code. */
 const char *crf_status_string(int status);

@@ -20,6 +20,9 @@ CRF_MAX_LEN = 1023
 CRF_MAX_LABELS = 4096
 CRF_MAX_TREES = 64
 CRF_MAX_ROW = 8192
+CRF_MAX_BUCKETS = 1024
+CRF_MAX_STEPS = 32
+CRF_BF16, CRF_F32 = 0, 1
 ROW_BLOCK = 32          # entries of a packed row that share a power of two
 CRF_FORCE_SPILL = 0x1
 CRF_NO_TEAMS = 0x2
@@ -54,6 +57,16 @@ SIGNATURES = {
     "crf_biaffine_bwd_workspace": (ctypes.c_int, [_P, _I32, _I32, ctypes.POINTER(_I64)]),
     "crf_biaffine_bwd": (ctypes.c_int, [_P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P, _P, _I64, _P]),
     "crf_biaffine_bwd_packed": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P, _P, _I64, _P]),
+    "crf_layer_norm": (ctypes.c_int, [_P, _P, _I32, _I32, _P, _P, _F32, _P, _P]),
+    "crf_layer_norm_bwd_workspace": (ctypes.c_int, [_P, _I32, ctypes.POINTER(_I64)]),
+    "crf_layer_norm_bwd": (ctypes.c_int, [_P, _P, _I32, _I32, _P, _P, _F32, _P, _P, _P, _P, _I64, _P]),
+    "crf_width_bias": (ctypes.c_int, [_P, _P, _I32, _P, _P, _I32, _P, _P]),
+    "crf_width_bias_bwd_workspace": (ctypes.c_int, [_P, _I32, ctypes.POINTER(_I64)]),
+    "crf_width_bias_bwd": (ctypes.c_int, [_P, _P, _I32, _P, _I32, _P, _P, _P, _I64, _P]),
+    "crf_orthogonalize_workspace": (ctypes.c_int, [_I32, _I32, _I32, ctypes.POINTER(_I64)]),
+    "crf_orthogonalize": (ctypes.c_int, [_P, _I32, _I32, _I32, _I32, _P, _I32, _F32, _P, _P, _I64, _P]),
+    "crf_muon_step": (ctypes.c_int, [_P, _P, _P, _I32, _I32, _I32, _I32, _F32, _I32, _F32, _F32, _P, _I32, _F32, _P, _P,
+                                     _P, _I64, _P]),
     "crf_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "crf_last_error": (ctypes.c_char_p, []),
 }
@@ -227,6 +240,55 @@ def crf_biaffine_bwd_packed(plan, rl_codes, rl_scales, rr_codes, rr_scales, w, d
     _check(load().crf_biaffine_bwd_packed(plan, rl_codes, rl_scales, rr_codes, rr_scales, w, d, ldw, num_labels,
                                           grad_scores, grad_rl, grad_rr, grad_w, workspace, workspace_bytes, stream),
            "crf_biaffine_bwd_packed")
+
+
+def crf_layer_norm(plan, x, x_type, d, gamma, beta, eps, y, stream):
+    _check(load().crf_layer_norm(plan, x, x_type, d, gamma, beta, eps, y, stream), "crf_layer_norm")
+
+
+def crf_layer_norm_bwd_workspace(plan, d):
+    n = _I64()
+    _check(load().crf_layer_norm_bwd_workspace(plan, d, ctypes.byref(n)), "crf_layer_norm_bwd_workspace")
+    return n.value
+
+
+def crf_layer_norm_bwd(plan, x, x_type, d, gamma, grad_y, eps, grad_x, grad_gamma, grad_beta, workspace,
+                       workspace_bytes, stream):
+    _check(load().crf_layer_norm_bwd(plan, x, x_type, d, gamma, grad_y, eps, grad_x, grad_gamma, grad_beta, workspace,
+                                     workspace_bytes, stream), "crf_layer_norm_bwd")
+
+
+def crf_width_bias(plan, scores, num_labels, table, buckets, num_buckets, out, stream):
+    _check(load().crf_width_bias(plan, scores, num_labels, table, buckets, num_buckets, out, stream), "crf_width_bias")
+
+
+def crf_width_bias_bwd_workspace(plan, num_labels):
+    n = _I64()
+    _check(load().crf_width_bias_bwd_workspace(plan, num_labels, ctypes.byref(n)), "crf_width_bias_bwd_workspace")
+    return n.value
+
+
+def crf_width_bias_bwd(plan, grad_out, num_labels, buckets, num_buckets, grad_scores, grad_table, workspace,
+                       workspace_bytes, stream):
+    _check(load().crf_width_bias_bwd(plan, grad_out, num_labels, buckets, num_buckets, grad_scores, grad_table, workspace,
+                                     workspace_bytes, stream), "crf_width_bias_bwd")
+
+
+def crf_orthogonalize_workspace(count, rows, cols):
+    n = _I64()
+    _check(load().crf_orthogonalize_workspace(count, rows, cols, ctypes.byref(n)), "crf_orthogonalize_workspace")
+    return n.value
+
+
+def crf_orthogonalize(x, count, rows, cols, ld, coefficients, steps, eps, out, workspace, workspace_bytes, stream):
+    _check(load().crf_orthogonalize(x, count, rows, cols, ld, coefficients, steps, eps, out, workspace, workspace_bytes,
+                                    stream), "crf_orthogonalize")
+
+
+def crf_muon_step(w, grad, momentum, count, rows, cols, ld, mu, nesterov, rate, decay, coefficients, steps, eps, w_out,
+                  momentum_out, workspace, workspace_bytes, stream):
+    _check(load().crf_muon_step(w, grad, momentum, count, rows, cols, ld, mu, nesterov, rate, decay, coefficients, steps,
+                                eps, w_out, momentum_out, workspace, workspace_bytes, stream), "crf_muon_step")
 
 
 def crf_status_string(status):
@@ -646,6 +708,99 @@ class Plan:
         call(self._handle, *ins, wp, d, ldw, L, gp, *ptrs, ws.data_ptr(), ws.numel(), _stream_ptr(t, self.device))
         return tuple(out)
 
+    def _norm_rows(self, x, gamma, beta=None):
+        """(d, x's type, pointers of x, gamma and beta)."""
+        t = self._torch
+        if x.dim() != 3:
+            raise ValueError("x must be [B, N1, d]")
+        d = int(x.shape[2])
+        kind = CRF_F32 if x.dtype == t.float32 else CRF_BF16
+        xp = self._tensor(x, "x", (self.B, self.n1, d), (t.bfloat16, t.int16, t.uint16, t.float32))
+        return (d, kind, xp, *(self._tensor(v, name, (d,), (t.float32,), optional=True)
+                               for v, name in ((gamma, "gamma"), (beta, "beta"))))
+
+    def layer_norm(self, x, gamma=None, beta=None, eps=1e-5, out=None):
+        """Layer norm of rows [B, N1, d] (bf16, its bit patterns, or float32)
+        with float32 gamma and beta [d] (default 1 and 0): bf16 rows, what the
+        scorer takes.  Rows past a sentence's last fence post are left as they
+        were (zero in a fresh buffer)."""
+        t = self._torch
+        d, kind, xp, gp, bp = self._norm_rows(x, gamma, beta)
+        out = self._out(out, (self.B, self.n1, d), t.bfloat16, zero=True)
+        op = self._bf16(out, "out", (self.B, self.n1, d))
+        self._rewritten(out)
+        crf_layer_norm(self._handle, xp, kind, d, gp, bp, float(eps), op, _stream_ptr(t, self.device))
+        return out
+
+    def layer_norm_bwd(self, x, gamma, grad, eps=1e-5, grad_x=None, grad_gamma=None, grad_beta=None,
+                       need=(True, True, True)):
+        """Backward pass of layer_norm from the bf16 gradient of its rows:
+        (grad_x of x's type, grad_gamma, grad_beta float32 [d]).  need: which of
+        the three to compute (None in the place of the others); rows past a
+        sentence are left as they were (zero in a fresh buffer)."""
+        t = self._torch
+        d, kind, xp, gp, _ = self._norm_rows(x, gamma)
+        rows = (self.B, self.n1, d)
+        up = self._bf16(grad, "grad", rows)
+        same = (t.float32,) if kind == CRF_F32 else (t.bfloat16, t.int16, t.uint16)
+        out = [self._out(v, s, dt, zero=z) if want else None
+               for v, s, dt, z, want in ((grad_x, rows, t.float32 if kind == CRF_F32 else t.bfloat16, True, need[0]),
+                                         (grad_gamma, (d,), t.float32, False, need[1]),
+                                         (grad_beta, (d,), t.float32, False, need[2]))]
+        ptrs = [self._tensor(v, name, s, dt, optional=True)
+                for v, name, s, dt in zip(out, ("grad_x", "grad_gamma", "grad_beta"), (rows, (d,), (d,)),
+                                          (same, (t.float32,), (t.float32,)))]
+        ws = self._workspace(crf_layer_norm_bwd_workspace(self._handle, d))
+        for v in out:
+            self._rewritten(v)
+        crf_layer_norm_bwd(self._handle, xp, kind, d, gp, up, float(eps), *ptrs, ws.data_ptr(), ws.numel(),
+                           _stream_ptr(t, self.device))
+        return tuple(out)
+
+    def _labels_of(self, scores, name):
+        """(number of labels, pointer) of float32 scores [B, N1, N1] or [B, N1, N1, L]."""
+        if scores.dim() not in (3, 4):
+            raise ValueError(f"{name} must be [B, N1, N1] or [B, N1, N1, L]")
+        shape = (self.B, self.n1, self.n1) + tuple(scores.shape[3:])
+        return (int(shape[3]) if len(shape) == 4 else 1), self._tensor(scores, name, shape, (self._torch.float32,))
+
+    def width_bias(self, scores, table, buckets, out=None):
+        """Scores with a learned bias by a span's width: table float32 [K, L],
+        buckets int32 [N1] (the bucket of each width, see width_buckets; a span
+        whose bucket is outside 0 .. K - 1 gets none).  scores float32
+        [B, N1, N1] or [B, N1, N1, L], any L.  out may be scores itself; a fresh
+        one is zero where no span is."""
+        t = self._torch
+        L, sp = self._labels_of(scores, "scores")
+        if table.dim() != 2:
+            raise ValueError("table must be [K, L]")
+        K = int(table.shape[0])
+        tp = self._tensor(table, "table", (K, L), (t.float32,))
+        bp = self._tensor(buckets, "buckets", (self.n1,), (t.int32,))
+        out = self._out(out, scores.shape, t.float32, zero=True)
+        op = self._tensor(out, "out", scores.shape, (t.float32,))
+        self._rewritten(out)
+        crf_width_bias(self._handle, sp, L, tp, bp, K, op, _stream_ptr(t, self.device))
+        return out
+
+    def width_bias_bwd(self, grad, buckets, num_buckets, grad_scores=None, grad_table=None, need=(True, True)):
+        """Backward pass of width_bias from the gradient of its scores:
+        (grad_scores, on spans only, a fresh one zero elsewhere; grad_table
+        float32 [K, L]).  need: which of the two to compute."""
+        t = self._torch
+        L, gp = self._labels_of(grad, "grad")
+        K = int(num_buckets)
+        bp = self._tensor(buckets, "buckets", (self.n1,), (t.int32,))
+        grad_scores = self._out(grad_scores, grad.shape, t.float32, zero=True) if need[0] else None
+        grad_table = self._out(grad_table, (K, L), t.float32) if need[1] else None
+        outs = (self._tensor(grad_scores, "grad_scores", grad.shape, (t.float32,), optional=True),
+                self._tensor(grad_table, "grad_table", (K, L), (t.float32,), optional=True))
+        ws = self._workspace(crf_width_bias_bwd_workspace(self._handle, L))
+        for v in (grad_scores, grad_table):
+            self._rewritten(v)
+        crf_width_bias_bwd(self._handle, gp, L, bp, K, *outs, ws.data_ptr(), ws.numel(), _stream_ptr(t, self.device))
+        return grad_scores, grad_table
+
     def cky_decode(self, scores, spans=None, best=None):
         """(spans int32 [B, 2(N1-1)-1, 2] preorder padded with -1, best float32 [B])."""
         t = self._torch
@@ -777,3 +932,169 @@ def biaffine(rl, rr, w, plan, held="bf16"):
             return grad_rl, grad_rr, None if grad_w is None else grad_w.to(ctx.w_type)
 
     return _Biaffine.apply(rl, rr, w)
+
+
+def layer_norm(x, plan, gamma=None, beta=None, eps=1e-5):
+    """Differentiable layer norm of rows [B, N1, d] (Plan.layer_norm's
+    arguments): bfloat16 rows for the scorer, rows past a sentence 0.  x bfloat16
+    or float32, gamma and beta float32; each gets its gradient in its own type."""
+    import torch
+
+    class _Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, gamma, beta):
+            ctx.save_for_backward(x, gamma)
+            return plan.layer_norm(x, gamma, beta, eps=eps)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, g):
+            x, gamma = ctx.saved_tensors
+            need = ctx.needs_input_grad
+            if not any(need):
+                return None, None, None
+            g = g.contiguous()   # held by this frame until the call has been enqueued
+            return plan.layer_norm_bwd(x, gamma, g, eps=eps, need=need)
+
+    return _Norm.apply(x, gamma, beta)
+
+
+def width_buckets(n1, num_buckets, reach):
+    """The bucket of each span width 0 .. n1 - 1 (numpy int32; entry 0 is never
+    read): the first half of the buckets hold one width each, the others the
+    widths up to `reach` at equal steps of their logarithm, and the last one
+    everything from there on."""
+    import numpy as np
+
+    n1, K, reach = int(n1), int(num_buckets), int(reach)
+    if n1 < 2 or not 1 <= K <= CRF_MAX_BUCKETS:
+        raise ValueError(f"n1 {n1} or num_buckets {K} out of range")
+    single = (K + 1) // 2
+    if reach <= single and K > 1:
+        raise ValueError(f"reach {reach} must be past the {single} widths that have a bucket each")
+    out = np.zeros(n1, np.int32)
+    k = 0
+    for w in range(1, n1):
+        if w <= single:
+            k = w - 1
+        else:   # the last k with (reach / single)^(k - single) <= (w / single)^(K - single), in whole numbers
+            while k < K - 1 and reach ** (k + 1 - single) * single ** (K - k - 1) <= w ** (K - single):
+                k += 1
+            k = min(max(k, single), K - 1)
+        out[w] = k
+    return out
+
+
+def width_bias(scores, table, buckets, plan):
+    """Differentiable bias by a span's width (Plan.width_bias's arguments):
+    cells that are no spans are 0."""
+    import torch
+
+    class _Width(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, s, table):
+            ctx.save_for_backward(buckets)
+            ctx.count = table.shape[0]
+            return plan.width_bias(s, table, buckets)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, g):
+            (buckets,) = ctx.saved_tensors
+            need = ctx.needs_input_grad
+            if not any(need):
+                return None, None
+            g = g.float().contiguous()   # held by this frame until the call has been enqueued
+            return plan.width_bias_bwd(g, buckets, ctx.count, need=need)
+
+    return _Width.apply(scores, table)
+
+
+# Coefficients (a, b, c) of five Newton-Schulz steps that bring singular values
+# from about 0.01 up to within 0.7 .. 1.2.
+MUON_STEPS = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def _matrices(torch, x, name, cols, like=None):
+    """(count, rows, cols, ld, pointer) of float32 [rows, ld] or [count, rows, ld]."""
+    if x.dtype != torch.float32 or x.dim() not in (2, 3) or not x.is_contiguous():
+        raise ValueError(f"{name} must be contiguous float32 [rows, ld] or [count, rows, ld], got {x.dtype} {tuple(x.shape)}")
+    if not x.is_cuda:
+        raise ValueError(f"{name} on {x.device}")
+    if like is not None and (x.shape != like.shape or x.device != like.device):
+        raise ValueError(f"{name} must be {tuple(like.shape)} on {like.device}, got {tuple(x.shape)} on {x.device}")
+    rows, ld = int(x.shape[-2]), int(x.shape[-1])
+    return (int(x.shape[0]) if x.dim() == 3 else 1), rows, ld if cols is None else int(cols), ld, x.data_ptr()
+
+
+def _coefficients(coefficients):
+    """The steps as a host array of float32 [steps][3]."""
+    import numpy as np
+
+    co = np.ascontiguousarray(np.asarray(coefficients, dtype=np.float32))
+    if co.ndim != 2 or co.shape[1] != 3:
+        raise ValueError("coefficients must be [steps, 3]")
+    return co
+
+
+def _written(x):
+    """The library writes x: autograd refuses what it has kept of it before."""
+    import torch
+
+    if not x.is_inference():
+        torch.autograd.graph.increment_version(x)
+
+
+def orthogonalize(x, cols=None, coefficients=MUON_STEPS, eps=1e-7, out=None):
+    """Matrices float32 [rows, ld] or [count, rows, ld] with their singular
+    values brought towards 1 by Newton-Schulz products: X = x / (|x|_F + eps),
+    then X <- a X + (b A + c A A) X, A = X X^T, for each step's (a, b, c).
+    cols: entries of a row that belong to the matrix (default ld); the others are
+    left as they were (zero in a fresh buffer).  Not differentiable."""
+    import torch
+
+    count, rows, cols, ld, xp = _matrices(torch, x, "x", cols)
+    co = _coefficients(coefficients)
+    if out is None:
+        out = torch.zeros(x.shape, dtype=torch.float32, device=x.device)
+    op = _matrices(torch, out, "out", cols, like=x)[4]
+    with torch.cuda.device(x.device):
+        ws = torch.empty(crf_orthogonalize_workspace(count, rows, cols), dtype=torch.uint8, device=x.device)
+        _written(out)
+        crf_orthogonalize(xp, count, rows, cols, ld, co.ctypes.data, co.shape[0], float(eps), op, ws.data_ptr(), ws.numel(),
+                          _stream_ptr(torch, x.device))
+    return out
+
+
+def muon_step(w, grad, momentum, lr, cols=None, weight_decay=0.0, mu=0.95, nesterov=True, scale=None,
+              coefficients=MUON_STEPS, eps=1e-7, w_out=None, momentum_out=None):
+    """Weights moved by their orthogonalised momentum: momentum <- mu momentum +
+    grad, U = grad + mu momentum (nesterov) or momentum, w <- (1 - lr
+    weight_decay) w - lr scale X with X orthogonalize(U).  w, grad and momentum
+    float32 [rows, ld] or [count, rows, ld]; the scorer's w and the gradient that
+    biaffine_bwd gives for it are taken as they lie, with cols = d + 1 (the
+    entries past it are left as they were).  scale: default
+    sqrt(max(1, rows / cols)).  w and momentum are changed in place, or left as
+    they are where w_out or momentum_out (that are not them) take the results.
+    Returns (w_out, momentum_out)."""
+    import math
+
+    import torch
+
+    count, rows, cols, ld, wp = _matrices(torch, w, "w", cols)
+    gp = _matrices(torch, grad, "grad", cols, like=w)[4]
+    mp = _matrices(torch, momentum, "momentum", cols, like=w)[4]
+    w_out, momentum_out = w if w_out is None else w_out, momentum if momentum_out is None else momentum_out
+    wop = _matrices(torch, w_out, "w_out", cols, like=w)[4]
+    mop = _matrices(torch, momentum_out, "momentum_out", cols, like=w)[4]
+    co = _coefficients(coefficients)
+    if scale is None:
+        scale = math.sqrt(max(1.0, rows / cols))
+    with torch.cuda.device(w.device):
+        ws = torch.empty(crf_orthogonalize_workspace(count, rows, cols), dtype=torch.uint8, device=w.device)
+        _written(w_out)
+        _written(momentum_out)
+        crf_muon_step(wp, gp, mp, count, rows, cols, ld, float(mu), int(bool(nesterov)), float(lr) * float(scale),
+                      float(lr) * float(weight_decay), co.ctypes.data, co.shape[0], float(eps), wop, mop, ws.data_ptr(),
+                      ws.numel(), _stream_ptr(torch, w.device))
+    return w_out, momentum_out

@@ -10,10 +10,13 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 SOURCES = [os.path.join(CSRC, "crf_kernels.hip"), os.path.join(CSRC, "crf_biaffine.hip"),
            os.path.join(CSRC, "crf_tile.hip"), os.path.join(CSRC, "crf_plan.cpp")]
-# the fine-tuning operators, linked into the same library
+# the operators of training and fine-tuning, linked into the same library
 TRAIN_SOURCES = [os.path.join(CSRC, "crf_trees.hip"), os.path.join(CSRC, "crf_rows.hip"),
                  os.path.join(CSRC, "crf_biaffine_bwd.hip"),
+                 os.path.join(CSRC, "crf_norm.hip"), os.path.join(CSRC, "crf_width.hip"), os.path.join(CSRC, "crf_ortho.hip"),
                  os.path.join(CSRC, "crf_train.cpp")]
+# (of which these say what a NaN of the caller's does)
+NAN_SOURCES = [os.path.join(CSRC, name) for name in ("crf_norm.hip", "crf_width.hip", "crf_ortho.hip")]
 LIB = os.path.join(PKG, "libcrfinside.so")
 # microbenchmarks of the ceilings behind the roofline (bench.py --ceilings)
 CEIL_SOURCES = [os.path.join(CSRC, "crf_ceilings.hip")]
@@ -82,7 +85,8 @@ def _compile(sources, lib, verbose, resources=()):
     if resources:
         flags = ["-Rpass-analysis=kernel-resource-usage", "-fno-caret-diagnostics", *flags]
     objs = [f"{lib}.{os.path.basename(src)}.o" for src in sources]
-    cmds = [[HIPCC, *flags, "-c", "-o", obj, src] for src, obj in zip(sources, objs)]
+    cmds = [[HIPCC, *flags, *(["-fhonor-nans"] if src in NAN_SOURCES else []), "-c", "-o", obj, src]
+            for src, obj in zip(sources, objs)]
     with concurrent.futures.ThreadPoolExecutor(len(cmds)) as pool:
         runs = list(pool.map(lambda c: subprocess.run(c, capture_output=True, text=True), cmds))
     for cmd, r in zip(cmds, runs):

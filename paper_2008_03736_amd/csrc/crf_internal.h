@@ -682,5 +682,27 @@ hipError_t set_biaffine_bwd_attributes();
 hipError_t launch_biaffine_bwd(const KernelPlan &p, int64_t cells, const void *rl, const uint8_t *rl_scales, const void *rr,
                                const uint8_t *rr_scales, const uint16_t *w, int d, int ldw, int L, const float *grad,
                                uint16_t *grad_rl, uint16_t *grad_rr, float *grad_w, char *ws, hipStream_t stream);
+// Layer norm of the batch's rows (crf_norm.hip), x in bf16 or float32: the
+// backward pass' workspace bytes and the launches; gamma, beta and any of the
+// backward pass' outputs may be NULL.
+int64_t norm_bwd_bytes(const KernelPlan &p, int d);
+hipError_t launch_norm(const KernelPlan &p, const void *x, bool f32, int d, const float *gamma, const float *beta,
+                       float eps, uint16_t *y, hipStream_t stream);
+hipError_t launch_norm_bwd(const KernelPlan &p, const void *x, bool f32, int d, const float *gamma, const uint16_t *dy,
+                           float eps, void *dx, float *dgamma, float *dbeta, char *ws, hipStream_t stream);
+// A bias by width (crf_width.hip) for sentences of up to `widest` words and L
+// labels: the backward pass' workspace bytes and the launches (its outputs may
+// be NULL).
+int64_t width_bwd_bytes(const KernelPlan &p, int widest, int L);
+hipError_t launch_width(const KernelPlan &p, int widest, int L, const float *table, const int32_t *bucket, int K,
+                        const float *scores, float *out, hipStream_t stream);
+hipError_t launch_width_bwd(const KernelPlan &p, int widest, int L, const float *grad, const int32_t *bucket, int K,
+                            float *grad_scores, float *grad_table, char *ws, hipStream_t stream);
+// The orthogonalised update (crf_ortho.hip): workspace bytes and the launches.
+// momentum NULL: out = X of grad; else momentum_out, and out = keep w - rate X.
+int64_t ortho_bytes(int count, int rows, int cols);
+hipError_t launch_ortho(const float *grad, const float *momentum, const float *w, float *momentum_out, float *out, int count,
+                        int rows, int cols, int ld, float mu, bool nesterov, float keep, float rate, float eps,
+                        const float *coefficients, int steps, char *ws, hipStream_t stream);
 
 }  // namespace crf

@@ -1,0 +1,385 @@
+// crf_norm.hip -- layer norm of fence-post rows, and its backward pass.
+//
+// With m and v the mean and the variance of a row's d entries, r = 1 / sqrt(v + eps)
+// and h = (x - m) r,
+//     y = h gamma + beta,
+//     dx = r (u - mean(u) - h mean(u h)),   u = dy gamma,
+//     dgamma = sum of dy h over the rows,   dbeta = sum of dy.
+//
+// Memory-bound: the rows are read once and written once.  A row lies in the
+// registers of G lanes, eight entries each, so that its mean, its variance (of
+// the deviations, not of squares: a large mean costs no digits) and the two
+// means of the backward pass are sums over lanes, in 32 bits; the backward pass
+// takes the statistics from x again, which it has to read anyway, and nothing is
+// kept for it.  G is the least of 16 .. 1024 whose lanes hold a row: several
+// rows to a wavefront, or several wavefronts to a row, which then meet in LDS.
+// The plan's lists of fence posts give the rows, so that padded ones cost nothing.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "crf_internal.h"
+#include "crf_rows.h"
+
+namespace crf {
+namespace {
+
+constexpr int kNormUnroll = 4;    // rows of a group of lanes in flight, forward
+constexpr int kNormUnrollBwd = 2;
+constexpr int kNormGroups = 512;  // most workgroups (of 256 threads) that sum dgamma and dbeta
+
+__host__ __device__ constexpr int norm_threads(int G) { return G > 256 ? G : 256; }
+
+// Pieces of rows: bf16 rows start at multiples of 8 bytes, float32 ones of 4.
+typedef uint32_t u32x4_a8 __attribute__((ext_vector_type(4), aligned(8)));
+typedef uint32_t u32x2_a8 __attribute__((ext_vector_type(2), aligned(8)));
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+
+__device__ __forceinline__ float low(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
+
+// Entries k .. k + 7 of a row (zeros past d, a multiple of 4), as they lie in memory ...
+template <typename T>
+struct Raw;
+template <>
+struct Raw<uint16_t> {
+    u32x4_a8 v = u32x4_a8{0u, 0u, 0u, 0u};
+    __device__ __forceinline__ void load(const uint16_t *row, int k, int d) {
+        if (k + 8 <= d) {
+            v = *reinterpret_cast<const u32x4_a8 *>(row + k);
+        } else if (k < d) {
+            const u32x2_a8 a = *reinterpret_cast<const u32x2_a8 *>(row + k);
+            v = u32x4_a8{a.x, a.y, 0u, 0u};
+        }
+    }
+    __device__ __forceinline__ void widen(float (&f)[8]) const {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) f[2 * q] = low(v[q]), f[2 * q + 1] = high(v[q]);
+    }
+};
+template <>
+struct Raw<float> {
+    f32x4_a4 v[2] = {f32x4_a4{0.f, 0.f, 0.f, 0.f}, f32x4_a4{0.f, 0.f, 0.f, 0.f}};
+    __device__ __forceinline__ void load(const float *row, int k, int d) {
+        if (k < d) v[0] = *reinterpret_cast<const f32x4_a4 *>(row + k);
+        if (k + 4 < d) v[1] = *reinterpret_cast<const f32x4_a4 *>(row + k + 4);
+    }
+    __device__ __forceinline__ void widen(float (&f)[8]) const {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) f[q] = v[q >> 2][q & 3];
+    }
+};
+// ... and back.
+__device__ __forceinline__ void store(uint16_t *row, int k, int d, const float (&f)[8]) {
+    const u32x4_a8 v = {two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7])};
+    if (k + 8 <= d)
+        *reinterpret_cast<u32x4_a8 *>(row + k) = v;
+    else if (k < d)
+        *reinterpret_cast<u32x2_a8 *>(row + k) = u32x2_a8{v.x, v.y};
+}
+__device__ __forceinline__ void store(float *row, int k, int d, const float (&f)[8]) {
+    if (k < d) *reinterpret_cast<f32x4_a4 *>(row + k) = f32x4_a4{f[0], f[1], f[2], f[3]};
+    if (k + 4 < d) *reinterpret_cast<f32x4_a4 *>(row + k + 4) = f32x4_a4{f[4], f[5], f[6], f[7]};
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+}
+// The sum of v over the G lanes of a row, in every one of them (each adds in
+// the same order).  G > 64: the row's wavefronts meet in `slots`, a place a
+// wavefront; the next sum but one may use them again.
+template <int G, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float *slots) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        v[q] += dpp<0xB1>(v[q]);    // quad_perm(1, 0, 3, 2)
+        v[q] += dpp<0x4E>(v[q]);    // quad_perm(2, 3, 0, 1)
+        v[q] += dpp<0x141>(v[q]);   // row_half_mirror
+        v[q] += dpp<0x140>(v[q]);   // row_mirror
+        if constexpr (G >= 32) {
+            const auto h = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v[q]),
+                                                            __builtin_bit_cast(uint32_t, v[q]), false, false);
+            v[q] = __builtin_bit_cast(float, (uint32_t)h[0]) + __builtin_bit_cast(float, (uint32_t)h[1]);
+        }
+        if constexpr (G >= 64) {
+            const auto h = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v[q]),
+                                                            __builtin_bit_cast(uint32_t, v[q]), false, false);
+            v[q] = __builtin_bit_cast(float, (uint32_t)h[0]) + __builtin_bit_cast(float, (uint32_t)h[1]);
+        }
+    }
+    if constexpr (G > 64) {
+        constexpr int kWaves = norm_threads(G) / 64, kOfRow = G / 64;
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) slots[q * kWaves + wave] = v[q];
+        }
+        __syncthreads();
+        const int first = wave / kOfRow * kOfRow;
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            v[q] = slots[q * kWaves + first];
+#pragma unroll
+            for (int w = 1; w < kOfRow; ++w) v[q] += slots[q * kWaves + first + w];
+        }
+    }
+}
+
+// Deviations from the mean (0 past d) and 1 / sqrt(variance + eps) of N rows.
+template <int G, int N>
+__device__ __forceinline__ void statistics(float (&f)[N][8], float (&r)[N], int k, int d, float eps, float (*slots)[N * 16]) {
+    const float each = 1.f / (float)d;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+        r[u] = ((f[u][0] + f[u][1]) + (f[u][2] + f[u][3])) + ((f[u][4] + f[u][5]) + (f[u][6] + f[u][7]));
+    row_sums<G, N>(r, slots[0]);
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const float m = r[u] * each;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) f[u][q] = k + (q & 4) < d ? f[u][q] - m : 0.f;
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s = fmaf(f[u][q], f[u][q], s);
+        r[u] = s;
+    }
+    row_sums<G, N>(r, slots[1]);
+#pragma unroll
+    for (int u = 0; u < N; ++u) r[u] = 1.f / sqrtf(fmaf(r[u], each, eps));
+}
+
+// A lane's entries of gamma or beta (`none` where there is no array).
+__device__ __forceinline__ void weights(const float *p, int k, int d, float none, float (&f)[8]) {
+    Raw<float> raw;
+    if (p != nullptr) raw.load(p, k, d);
+    raw.widen(f);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) f[q] = p != nullptr ? f[q] : none;
+}
+
+// Rows of a chunk: kBiaRows of a block of posts are a whole number of chunks.
+template <int G, int U>
+__device__ __forceinline__ const int32_t *chunk_ids(const int32_t *posts, int chunk) {
+    constexpr int kRows = norm_threads(G) / G * U, kChunks = kBiaRows / kRows;
+    static_assert(kBiaRows % kRows == 0, "a block of posts is a whole number of chunks");
+    return posts + (size_t)(chunk / kChunks) * kPostRec + chunk % kChunks * kRows + threadIdx.x / G * U;
+}
+
+template <typename T, int G>
+__global__ __launch_bounds__(norm_threads(G)) void norm_kernel(const int32_t *__restrict__ posts, int d,
+                                                               const T *__restrict__ x, const float *__restrict__ gamma,
+                                                               const float *__restrict__ beta, float eps,
+                                                               uint16_t *__restrict__ y) {
+    constexpr int U = kNormUnroll;
+    __shared__ float slots[2][U * 16];
+    const int k = 8 * (threadIdx.x & (G - 1));
+    const int32_t *ids = chunk_ids<G, U>(posts, blockIdx.x);
+    int id[U];
+    Raw<T> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        id[u] = ids[u];
+        if (id[u] >= 0) raw[u].load(x + (size_t)id[u] * d, k, d);
+    }
+    float g[8], b[8], f[U][8], r[U];
+    weights(gamma, k, d, 1.f, g);
+    weights(beta, k, d, 0.f, b);
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u].widen(f[u]);
+    statistics<G, U>(f, r, k, d, eps, slots);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) f[u][q] = fmaf(f[u][q] * r[u], g[q], b[q]);
+        if (id[u] >= 0) store(y + (size_t)id[u] * d, k, d, f[u]);
+    }
+}
+
+// dx, and a workgroup's share of dgamma and dbeta (PARTS; [2][8 G] floats each,
+// or the results themselves where there is one workgroup).
+template <typename T, int G, bool PARTS>
+__global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(const int32_t *__restrict__ posts, int chunks, int d,
+                                                                   const T *__restrict__ x,
+                                                                   const float *__restrict__ gamma,
+                                                                   const uint16_t *__restrict__ dy, float eps,
+                                                                   T *__restrict__ dx, float *__restrict__ parts,
+                                                                   float *__restrict__ dgamma, float *__restrict__ dbeta) {
+    constexpr int U = kNormUnrollBwd, kRows = norm_threads(G) / G;
+    __shared__ float slots[2][U * 16], slots2[2 * U * 16];
+    __shared__ float sums[PARTS && kRows > 1 ? kRows * 16 * G : 1];
+    const int lane = threadIdx.x & (G - 1), k = 8 * lane;
+    const float each = 1.f / (float)d;
+    float g[8], sg[8], sb[8];
+    weights(gamma, k, d, 1.f, g);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sg[q] = sb[q] = 0.f;
+    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const int32_t *ids = chunk_ids<G, U>(posts, c);
+        int id[U];
+        Raw<T> raw[U];
+        Raw<uint16_t> up[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            id[u] = ids[u];
+            if (id[u] >= 0) {
+                raw[u].load(x + (size_t)id[u] * d, k, d);
+                up[u].load(dy + (size_t)id[u] * d, k, d);
+            }
+        }
+        float f[U][8], r[U], e[U][8], two[2 * U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u].widen(f[u]), up[u].widen(e[u]);
+        statistics<G, U>(f, r, k, d, eps, slots);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float s = 0.f, t = 0.f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                f[u][q] *= r[u];
+                if constexpr (PARTS) {   // (a row that is not there adds zeros)
+                    sg[q] = fmaf(e[u][q], f[u][q], sg[q]);
+                    sb[q] += e[u][q];
+                }
+                e[u][q] *= g[q];
+                s += e[u][q];
+                t = fmaf(e[u][q], f[u][q], t);
+            }
+            two[2 * u] = s;
+            two[2 * u + 1] = t;
+        }
+        row_sums<G, 2 * U>(two, slots2);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float s = two[2 * u] * each, t = two[2 * u + 1] * each;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[u][q] = r[u] * (e[u][q] - s - f[u][q] * t);
+            if (dx != nullptr && id[u] >= 0) store(dx + (size_t)id[u] * d, k, d, f[u]);
+        }
+    }
+    if constexpr (PARTS) {
+        if constexpr (kRows > 1) {
+            float *own = sums + (threadIdx.x / G) * 16 * G;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) own[k + q] = sg[q], own[8 * G + k + q] = sb[q];
+            __syncthreads();
+            for (int c = threadIdx.x; c < 16 * G; c += norm_threads(G)) {
+                float s = sums[c];
+                for (int w = 1; w < kRows; ++w) s += sums[w * 16 * G + c];
+                if (gridDim.x > 1) {
+                    parts[(size_t)blockIdx.x * 16 * G + c] = s;
+                } else {
+                    const int a = c & (8 * G - 1);
+                    float *out = c < 8 * G ? dgamma : dbeta;
+                    if (a < d && out != nullptr) out[a] = s;
+                }
+            }
+        } else if (gridDim.x > 1) {
+            float *own = parts + (size_t)blockIdx.x * 16 * G;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) own[k + q] = sg[q], own[8 * G + k + q] = sb[q];
+        } else {
+            if (dgamma != nullptr) store(dgamma, k, d, sg);
+            if (dbeta != nullptr) store(dbeta, k, d, sb);
+        }
+    }
+}
+
+// The shares of dgamma and dbeta added up in a fixed order: a workgroup takes
+// 32 columns, thread (c, p) every 32nd share.
+constexpr int kJoinCols = 32, kJoinLanes = 32;
+__global__ __launch_bounds__(kJoinCols *kJoinLanes) void norm_join_kernel(const float *__restrict__ parts, int count,
+                                                                          int wide, int d, float *__restrict__ dgamma,
+                                                                          float *__restrict__ dbeta) {
+    __shared__ float part[kJoinLanes][kJoinCols + 1];
+    const int c = threadIdx.x % kJoinCols, p = threadIdx.x / kJoinCols, at = blockIdx.x * kJoinCols + c;
+    float s = 0.f;
+#pragma unroll 8
+    for (int q = p; q < count; q += kJoinLanes) s += parts[(size_t)q * 2 * wide + at];
+    part[p][c] = s;
+    __syncthreads();
+    for (int half = kJoinLanes / 2; half > 0; half /= 2) {
+        if (p < half) part[p][c] += part[p + half][c];
+        __syncthreads();
+    }
+    if (p == 0) {
+        const int a = at < wide ? at : at - wide;
+        float *out = at < wide ? dgamma : dbeta;
+        if (a < d && out != nullptr) out[a] = part[0][c];
+    }
+}
+
+// Lanes a row of d entries takes: 16, 32 ... 1024.
+int norm_lanes(int d) {
+    int g = 16;
+    while (8 * g < d) g *= 2;
+    return g;
+}
+int norm_chunks(const KernelPlan &p, int G, int U) { return p.n_posts * (kBiaRows / (norm_threads(G) / G * U)); }
+int norm_parts(const KernelPlan &p, int G) {
+    return std::min(norm_chunks(p, G, kNormUnrollBwd), kNormGroups * 256 / norm_threads(G));
+}
+
+template <typename T, int G>
+void launch_norm_g(const KernelPlan &p, const void *x, int d, const float *gamma, const float *beta, float eps, uint16_t *y,
+                   hipStream_t stream) {
+    hipLaunchKernelGGL((norm_kernel<T, G>), dim3(norm_chunks(p, G, kNormUnroll)), dim3(norm_threads(G)), 0, stream, p.posts,
+                       d, static_cast<const T *>(x), gamma, beta, eps, y);
+}
+
+template <typename T, int G>
+void launch_norm_bwd_g(const KernelPlan &p, const void *x, int d, const float *gamma, const uint16_t *dy, float eps,
+                       void *dx, float *dgamma, float *dbeta, float *parts, hipStream_t stream) {
+    const int chunks = norm_chunks(p, G, kNormUnrollBwd);
+    if (dgamma == nullptr && dbeta == nullptr) {
+        hipLaunchKernelGGL((norm_bwd_kernel<T, G, false>), dim3(chunks), dim3(norm_threads(G)), 0, stream, p.posts, chunks,
+                           d, static_cast<const T *>(x), gamma, dy, eps, static_cast<T *>(dx), nullptr, nullptr, nullptr);
+        return;
+    }
+    const int count = norm_parts(p, G);
+    hipLaunchKernelGGL((norm_bwd_kernel<T, G, true>), dim3(count), dim3(norm_threads(G)), 0, stream, p.posts, chunks, d,
+                       static_cast<const T *>(x), gamma, dy, eps, static_cast<T *>(dx), parts, dgamma, dbeta);
+    if (count > 1)
+        hipLaunchKernelGGL(norm_join_kernel, dim3(16 * G / kJoinCols), dim3(kJoinCols * kJoinLanes), 0, stream, parts, count,
+                           8 * G, d, dgamma, dbeta);
+}
+
+#define CRF_NORM_LANES(T, CALL, ...)                   \
+    switch (norm_lanes(d)) {                           \
+        case 16: CALL<T, 16>(__VA_ARGS__); break;      \
+        case 32: CALL<T, 32>(__VA_ARGS__); break;      \
+        case 64: CALL<T, 64>(__VA_ARGS__); break;      \
+        case 128: CALL<T, 128>(__VA_ARGS__); break;    \
+        case 256: CALL<T, 256>(__VA_ARGS__); break;    \
+        case 512: CALL<T, 512>(__VA_ARGS__); break;    \
+        default: CALL<T, 1024>(__VA_ARGS__); break;    \
+    }
+
+}  // namespace
+
+int64_t norm_bwd_bytes(const KernelPlan &p, int d) {
+    const int G = norm_lanes(d);
+    return ((int64_t)norm_parts(p, G) * 16 * G * 4 + 255) / 256 * 256;
+}
+
+hipError_t launch_norm(const KernelPlan &p, const void *x, bool f32, int d, const float *gamma, const float *beta,
+                       float eps, uint16_t *y, hipStream_t stream) {
+    if (f32)
+        CRF_NORM_LANES(float, launch_norm_g, p, x, d, gamma, beta, eps, y, stream)
+    else
+        CRF_NORM_LANES(uint16_t, launch_norm_g, p, x, d, gamma, beta, eps, y, stream)
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_bwd(const KernelPlan &p, const void *x, bool f32, int d, const float *gamma, const uint16_t *dy,
+                           float eps, void *dx, float *dgamma, float *dbeta, char *ws, hipStream_t stream) {
+    float *parts = reinterpret_cast<float *>(ws);
+    if (f32)
+        CRF_NORM_LANES(float, launch_norm_bwd_g, p, x, d, gamma, dy, eps, dx, dgamma, dbeta, parts, stream)
+    else
+        CRF_NORM_LANES(uint16_t, launch_norm_bwd_g, p, x, d, gamma, dy, eps, dx, dgamma, dbeta, parts, stream)
+    return hipGetLastError();
+}
+
+}  // namespace crf

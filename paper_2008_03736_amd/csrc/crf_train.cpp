@@ -1,7 +1,10 @@
-// crf_train.cpp -- C entry points of the fine-tuning operators: argument
-// checks and launches, as crf_plan.cpp has them for the others.
+// crf_train.cpp -- C entry points of the operators that training a scorer and
+// tuning a parser take: argument checks and launches, as crf_plan.cpp has them
+// for the others.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <initializer_list>
 #include <mutex>
@@ -120,6 +123,68 @@ int scorer_backward(const crf_plan *plan, const void *rl, const uint8_t *rl_scal
                                                   grad_scores, grad_rl, grad_rr, grad_w, static_cast<char *>(workspace),
                                                   static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, what);
+}
+
+// Layer norm's rows: x is bf16 (8-byte aligned) or float32.
+int check_norm(const void *x, int32_t x_type, int32_t d, float eps) {
+    const int rc = check_row(d);
+    if (rc != CRF_OK) return rc;
+    if (x_type != CRF_BF16 && x_type != CRF_F32)
+        return fail(CRF_EINVAL, "x_type %d is neither CRF_BF16 nor CRF_F32", x_type);
+    if (misaligned(x, x_type == CRF_BF16 ? 8 : 4))
+        return fail(CRF_EINVAL, "x must be %d-byte aligned", x_type == CRF_BF16 ? 8 : 4);
+    if (!finite_positive(eps) || eps == 0.f) return fail(CRF_EINVAL, "eps %g is not positive and finite", (double)eps);
+    return CRF_OK;
+}
+
+int check_buckets(int32_t num_buckets, int32_t num_labels) {
+    if (num_buckets < 1 || num_buckets > CRF_MAX_BUCKETS)
+        return fail(CRF_EINVAL, "num_buckets %d outside [1, %d]", num_buckets, CRF_MAX_BUCKETS);
+    if (num_labels < 1 || num_labels > CRF_MAX_LABELS)
+        return fail(CRF_EINVAL, "num_labels %d outside [1, %d]", num_labels, CRF_MAX_LABELS);
+    return CRF_OK;
+}
+
+int check_matrices(int32_t count, int32_t rows, int32_t cols, int32_t ld) {
+    if (count < 1 || count > CRF_MAX_LABELS) return fail(CRF_EINVAL, "count %d outside [1, %d]", count, CRF_MAX_LABELS);
+    if (rows < 1 || rows > CRF_MAX_ROW || cols < 1 || cols > CRF_MAX_ROW)
+        return fail(CRF_EINVAL, "matrices of %d x %d, sides are in [1, %d]", rows, cols, CRF_MAX_ROW);
+    if (ld < cols) return fail(CRF_EINVAL, "ld %d < cols %d", ld, cols);
+    return CRF_OK;
+}
+
+// What singular values, at most 1 at the start, grow to under the steps, and
+// the polynomials of the Gram matrix: the kernels hold both in a float16's range.
+int check_coefficients(const float *coefficients, int32_t steps, float eps) {
+    if (coefficients == nullptr) return fail(CRF_EINVAL, "coefficients is NULL");
+    if (steps < 1 || steps > CRF_MAX_STEPS) return fail(CRF_EINVAL, "steps %d outside [1, %d]", steps, CRF_MAX_STEPS);
+    if (!finite_positive(eps) || eps == 0.f) return fail(CRF_EINVAL, "eps %g is not positive and finite", (double)eps);
+    double most = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        const float *f = coefficients + 3 * k;
+        for (int q = 0; q < 3; ++q)
+            if (!finite_positive(std::fabs(f[q])) || std::fabs(f[q]) > 1000.f)   // (no sum below overflows)
+                return fail(CRF_EINVAL, "step %d's coefficient %g is outside [-1000, 1000]", k, (double)f[q]);
+        const double a = f[0], b = f[1], c = f[2], top = most * most;   // t = s^2 in [0, top]
+        auto value = [&](double t) { return std::sqrt(t) * std::fabs(a + t * (b + t * c)); };
+        auto poly = [&](double t) { return std::fabs(t * (b + t * c)); };
+        double grown = value(top), inner = poly(top);
+        auto at = [&](double t) {
+            if (t > 0.0 && t < top) grown = std::max(grown, value(t)), inner = std::max(inner, poly(t));
+        };
+        if (c != 0.0) {   // where a + 3 b t + 5 c t^2 or b + 2 c t is 0
+            const double disc = 9.0 * b * b - 20.0 * a * c;
+            if (disc >= 0.0) at((-3.0 * b + std::sqrt(disc)) / (10.0 * c)), at((-3.0 * b - std::sqrt(disc)) / (10.0 * c));
+            at(-b / (2.0 * c));
+        } else if (b != 0.0) {
+            at(-a / (3.0 * b));
+        }
+        if (inner > 60.0 || grown > 4.0)
+            return fail(CRF_EINVAL, "step %d takes singular values to %g (at most 4) by a polynomial of %g (at most 60)", k,
+                        grown, inner);
+        most = grown;
+    }
+    return CRF_OK;
 }
 
 }  // namespace
@@ -267,6 +332,150 @@ int crf_biaffine_bwd_packed(const crf_plan *plan, const uint8_t *rl_codes, const
     if (misaligned(w, 8)) return fail(CRF_EINVAL, "w must be 8-byte aligned");
     return scorer_backward(plan, rl_codes, rl_scales, rr_codes, rr_scales, w, d, ldw, num_labels, grad_scores, grad_rl,
                            grad_rr, grad_w, workspace, workspace_bytes, stream, "crf_biaffine_bwd_packed launch");
+}
+
+int crf_layer_norm(const crf_plan *plan, const void *x, int32_t x_type, int32_t d, const float *gamma, const float *beta,
+                   float eps, uint16_t *y, void *stream) {
+    if (plan == nullptr) return fail(CRF_EINVAL, "plan is NULL");
+    if (x == nullptr || y == nullptr) return fail(CRF_EINVAL, "x/y is NULL");
+    int rc = check_norm(x, x_type, d, eps);
+    if (rc != CRF_OK) return rc;
+    if (misaligned(y, 8)) return fail(CRF_EINVAL, "y must be 8-byte aligned");
+    if ((rc = check_overlap({{"y", y, rows_bytes(plan, 2, d)}},
+                            {{"x", x, rows_bytes(plan, x_type == CRF_F32 ? 4 : 2, d)}, {"gamma", gamma, 4 * (int64_t)d},
+                             {"beta", beta, 4 * (int64_t)d}})) != CRF_OK ||
+        (rc = check_device(plan)) != CRF_OK)
+        return rc;
+    const hipError_t e = crf::launch_norm(plan->kp, x, x_type == CRF_F32, d, gamma, beta, eps, y,
+                                          static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "crf_layer_norm launch");
+}
+
+int crf_layer_norm_bwd_workspace(const crf_plan *plan, int32_t d, int64_t *bytes) {
+    if (plan == nullptr || bytes == nullptr) return fail(CRF_EINVAL, "NULL argument");
+    const int rc = check_row(d);
+    if (rc != CRF_OK) return rc;
+    *bytes = crf::norm_bwd_bytes(plan->kp, d);
+    return ok();
+}
+
+int crf_layer_norm_bwd(const crf_plan *plan, const void *x, int32_t x_type, int32_t d, const float *gamma,
+                       const uint16_t *grad_y, float eps, void *grad_x, float *grad_gamma, float *grad_beta,
+                       void *workspace, int64_t workspace_bytes, void *stream) {
+    if (plan == nullptr) return fail(CRF_EINVAL, "plan is NULL");
+    if (x == nullptr || grad_y == nullptr) return fail(CRF_EINVAL, "x/grad_y is NULL");
+    int rc = check_norm(x, x_type, d, eps);
+    if (rc != CRF_OK) return rc;
+    if (misaligned(grad_y, 8)) return fail(CRF_EINVAL, "grad_y must be 8-byte aligned");
+    if (misaligned(grad_x, x_type == CRF_BF16 ? 8 : 4))
+        return fail(CRF_EINVAL, "grad_x must be %d-byte aligned", x_type == CRF_BF16 ? 8 : 4);
+    const int64_t need = crf::norm_bwd_bytes(plan->kp, d), own = rows_bytes(plan, x_type == CRF_F32 ? 4 : 2, d);
+    const int64_t each = 4 * (int64_t)d;
+    if ((rc = check_workspace(workspace, workspace_bytes, need)) != CRF_OK ||
+        (rc = check_overlap({{"grad_x", grad_x, own}, {"grad_gamma", grad_gamma, each}, {"grad_beta", grad_beta, each},
+                             {"workspace", workspace, need}},
+                            {{"x", x, own}, {"gamma", gamma, each}, {"grad_y", grad_y, rows_bytes(plan, 2, d)}})) != CRF_OK ||
+        (rc = check_device(plan)) != CRF_OK)
+        return rc;
+    if (grad_x == nullptr && grad_gamma == nullptr && grad_beta == nullptr) return ok();
+    const hipError_t e = crf::launch_norm_bwd(plan->kp, x, x_type == CRF_F32, d, gamma, grad_y, eps, grad_x, grad_gamma,
+                                              grad_beta, static_cast<char *>(workspace), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "crf_layer_norm_bwd launch");
+}
+
+int crf_width_bias(const crf_plan *plan, const float *scores, int32_t num_labels, const float *table,
+                   const int32_t *buckets, int32_t num_buckets, float *out, void *stream) {
+    if (plan == nullptr) return fail(CRF_EINVAL, "plan is NULL");
+    if (scores == nullptr || table == nullptr || buckets == nullptr || out == nullptr)
+        return fail(CRF_EINVAL, "scores/table/buckets/out is NULL");
+    int rc = check_buckets(num_buckets, num_labels);
+    if (rc != CRF_OK) return rc;
+    const int64_t all = scores_bytes(plan, num_labels);
+    if ((rc = check_overlap({{"out", out, all}},
+                            {{"scores", out == scores ? nullptr : scores, all},   // (a thread reads what it then writes)
+                             {"table", table, 4 * (int64_t)num_buckets * num_labels},
+                             {"buckets", buckets, 4 * (int64_t)plan->n1}})) != CRF_OK ||
+        (rc = check_device(plan)) != CRF_OK)
+        return rc;
+    const hipError_t e = crf::launch_width(plan->kp, plan->max_len, num_labels, table, buckets, num_buckets, scores, out,
+                                           static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "crf_width_bias launch");
+}
+
+int crf_width_bias_bwd_workspace(const crf_plan *plan, int32_t num_labels, int64_t *bytes) {
+    if (plan == nullptr || bytes == nullptr) return fail(CRF_EINVAL, "NULL argument");
+    const int rc = check_buckets(1, num_labels);
+    if (rc != CRF_OK) return rc;
+    *bytes = crf::width_bwd_bytes(plan->kp, plan->max_len, num_labels);
+    return ok();
+}
+
+int crf_width_bias_bwd(const crf_plan *plan, const float *grad_out, int32_t num_labels, const int32_t *buckets,
+                       int32_t num_buckets, float *grad_scores, float *grad_table, void *workspace,
+                       int64_t workspace_bytes, void *stream) {
+    if (plan == nullptr) return fail(CRF_EINVAL, "plan is NULL");
+    if (grad_out == nullptr || buckets == nullptr) return fail(CRF_EINVAL, "grad_out/buckets is NULL");
+    int rc = check_buckets(num_buckets, num_labels);
+    if (rc != CRF_OK) return rc;
+    const int64_t all = scores_bytes(plan, num_labels), need = crf::width_bwd_bytes(plan->kp, plan->max_len, num_labels);
+    if ((rc = check_workspace(workspace, workspace_bytes, need)) != CRF_OK ||
+        (rc = check_overlap({{"grad_scores", grad_scores, all},
+                             {"grad_table", grad_table, 4 * (int64_t)num_buckets * num_labels},
+                             {"workspace", workspace, need}},
+                            {{"grad_out", grad_out, all}, {"buckets", buckets, 4 * (int64_t)plan->n1}})) != CRF_OK ||
+        (rc = check_device(plan)) != CRF_OK)
+        return rc;
+    if (grad_scores == nullptr && grad_table == nullptr) return ok();
+    const hipError_t e = crf::launch_width_bwd(plan->kp, plan->max_len, num_labels, grad_out, buckets, num_buckets,
+                                               grad_scores, grad_table, static_cast<char *>(workspace),
+                                               static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "crf_width_bias_bwd launch");
+}
+
+int crf_orthogonalize_workspace(int32_t count, int32_t rows, int32_t cols, int64_t *bytes) {
+    if (bytes == nullptr) return fail(CRF_EINVAL, "NULL argument");
+    const int rc = check_matrices(count, rows, cols, cols);
+    if (rc != CRF_OK) return rc;
+    *bytes = crf::ortho_bytes(count, rows, cols);
+    return ok();
+}
+
+int crf_orthogonalize(const float *x, int32_t count, int32_t rows, int32_t cols, int32_t ld, const float *coefficients,
+                      int32_t steps, float eps, float *out, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (x == nullptr || out == nullptr) return fail(CRF_EINVAL, "x/out is NULL");
+    int rc = check_matrices(count, rows, cols, ld);
+    if (rc != CRF_OK || (rc = check_coefficients(coefficients, steps, eps)) != CRF_OK) return rc;
+    const int64_t all = 4 * (int64_t)count * rows * ld, need = crf::ortho_bytes(count, rows, cols);
+    if ((rc = check_workspace(workspace, workspace_bytes, need)) != CRF_OK ||
+        (rc = check_overlap({{"out", out, all}, {"workspace", workspace, need}}, {{"x", x, all}})) != CRF_OK)
+        return rc;
+    const hipError_t e = crf::launch_ortho(x, nullptr, nullptr, nullptr, out, count, rows, cols, ld, 0.f, false, 0.f, 0.f,
+                                           eps, coefficients, steps, static_cast<char *>(workspace),
+                                           static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "crf_orthogonalize launch");
+}
+
+int crf_muon_step(const float *w, const float *grad, const float *momentum, int32_t count, int32_t rows, int32_t cols,
+                  int32_t ld, float mu, int32_t nesterov, float rate, float decay, const float *coefficients, int32_t steps,
+                  float eps, float *w_out, float *momentum_out, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (w == nullptr || grad == nullptr || momentum == nullptr || w_out == nullptr || momentum_out == nullptr)
+        return fail(CRF_EINVAL, "w/grad/momentum/w_out/momentum_out is NULL");
+    int rc = check_matrices(count, rows, cols, ld);
+    if (rc != CRF_OK || (rc = check_coefficients(coefficients, steps, eps)) != CRF_OK) return rc;
+    if (!finite_positive(mu)) return fail(CRF_EINVAL, "mu %g is negative or not finite", (double)mu);
+    if (!finite_positive(rate)) return fail(CRF_EINVAL, "rate %g is negative or not finite", (double)rate);
+    if (!finite_positive(decay) || decay > 1.f) return fail(CRF_EINVAL, "decay %g outside [0, 1]", (double)decay);
+    const int64_t all = 4 * (int64_t)count * rows * ld, need = crf::ortho_bytes(count, rows, cols);
+    // (in place: a thread reads what it then writes)
+    if ((rc = check_workspace(workspace, workspace_bytes, need)) != CRF_OK ||
+        (rc = check_overlap({{"w_out", w_out, all}, {"momentum_out", momentum_out, all}, {"workspace", workspace, need}},
+                            {{"w", w == w_out ? nullptr : w, all}, {"grad", grad, all},
+                             {"momentum", momentum == momentum_out ? nullptr : momentum, all}})) != CRF_OK)
+        return rc;
+    const hipError_t e = crf::launch_ortho(grad, momentum, w, momentum_out, w_out, count, rows, cols, ld, mu, nesterov != 0,
+                                           1.f - decay, rate, eps, coefficients, steps, static_cast<char *>(workspace),
+                                           static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "crf_muon_step launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,175 @@
+"""Layer norm, the width bias and the orthogonalised update without a GPU: what
+they refuse, on the host, before any HIP call; the buckets of widths; and
+overlapping buffers and launches on a HIP runtime of host memory
+(tests/scorer_ops_stub.cpp)."""
+import ctypes
+import csv
+import math
+import os
+import shutil
+import subprocess
+from fractions import Fraction
+
+import numpy as np
+import pytest
+
+from paper_2008_03736_amd import binding as B
+from paper_2008_03736_amd import build as BLD
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROCM_INCLUDE = "/opt/rocm/include"
+P, Q, R = (ctypes.c_void_p(k << 40) for k in (1, 2, 3))   # stand for device memory: never dereferenced by a refused call
+S, T = ctypes.c_void_p(4 << 40), ctypes.c_void_p(5 << 40)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.LIB_PATH):
+        pytest.fail("libcrfinside.so is not built (run __graft_entry__.build())")
+    return B.load()
+
+
+def steps(*co):
+    a = np.asarray(co, np.float32)
+    return a, a.ctypes.data, len(a)
+
+
+def test_null_arguments(lib):
+    n = ctypes.c_int64()
+    assert lib.crf_layer_norm(None, P, 0, 8, None, None, 1e-5, Q, None) == B.CRF_EINVAL
+    assert lib.crf_layer_norm_bwd_workspace(None, 8, ctypes.byref(n)) == B.CRF_EINVAL
+    assert lib.crf_layer_norm_bwd(None, P, 0, 8, None, Q, 1e-5, R, None, None, S, 1 << 20, None) == B.CRF_EINVAL
+    assert lib.crf_width_bias(None, P, 1, Q, R, 4, S, None) == B.CRF_EINVAL
+    assert lib.crf_width_bias_bwd_workspace(None, 1, ctypes.byref(n)) == B.CRF_EINVAL
+    assert lib.crf_width_bias_bwd(None, P, 1, R, 4, None, S, T, 1 << 20, None) == B.CRF_EINVAL
+    assert "plan" in B.crf_last_error()
+    _, co, k = steps((1.5, -0.5, 0.0))
+    assert lib.crf_orthogonalize(None, 1, 8, 8, 8, co, k, 1e-7, Q, R, 1 << 30, None) == B.CRF_EINVAL
+    assert lib.crf_orthogonalize(P, 1, 8, 8, 8, None, k, 1e-7, Q, R, 1 << 30, None) == B.CRF_EINVAL
+    assert lib.crf_orthogonalize(P, 1, 8, 8, 8, co, k, 1e-7, Q, None, 1 << 30, None) == B.CRF_EINVAL
+    assert lib.crf_muon_step(P, Q, None, 1, 8, 8, 8, 0.9, 1, 0.1, 0.0, co, k, 1e-7, P, R, S, 1 << 30, None) == B.CRF_EINVAL
+    assert lib.crf_orthogonalize_workspace(1, 8, 8, None) == B.CRF_EINVAL
+
+
+@pytest.mark.parametrize("count,rows,cols,ld", [(0, 8, 8, 8), (4097, 8, 8, 8), (1, 0, 8, 8), (1, 8, 0, 8), (1, 8193, 8, 8),
+                                                (1, 8, 8193, 8193), (1, 8, 8, 7), (-1, 8, 8, 8)])
+def test_sizes_of_matrices(lib, count, rows, cols, ld):
+    _, co, k = steps((1.5, -0.5, 0.0))
+    assert lib.crf_orthogonalize(P, count, rows, cols, ld, co, k, 1e-7, Q, R, 1 << 40, None) == B.CRF_EINVAL
+    if ld >= cols:
+        assert lib.crf_orthogonalize_workspace(count, rows, cols, ctypes.byref(ctypes.c_int64())) == B.CRF_EINVAL
+
+
+@pytest.mark.parametrize("co", [((5.0, 0.0, 0.0),), ((3.0, 0.0, 0.0),) * 2, ((1.0, -61.0, 0.0),), ((1.0, 0.0, 70.0),),
+                                ((1.0, float("nan"), 0.0),), ((float("inf"), 0.0, 0.0),), ((0.5, 1e30, -1e30),),
+                                ((3.4445, -4.7750, 2.0315),) * 33])
+def test_steps_that_leave_the_range(lib, co):
+    _, at, k = steps(*co)
+    assert lib.crf_orthogonalize(P, 1, 8, 8, 8, at, k, 1e-7, Q, R, 1 << 30, None) == B.CRF_EINVAL
+
+
+def test_what_steps_reach():
+    # the check's bound by dense sampling: the usual coefficients pass, for as many steps as are allowed
+    s = np.linspace(0, 1, 100001)
+    most = 1.0
+    for a, b, c in B.MUON_STEPS * 6:
+        t = s * most
+        assert np.abs(b * t ** 2 + c * t ** 4).max() < 60
+        most = np.abs(a * t + b * t ** 3 + c * t ** 5).max()
+        assert most < 4
+
+
+@pytest.mark.parametrize("eps", [0.0, -1.0, float("nan"), float("inf")])
+def test_eps(lib, eps):
+    _, co, k = steps((1.5, -0.5, 0.0))
+    assert lib.crf_orthogonalize(P, 1, 8, 8, 8, co, k, eps, Q, R, 1 << 30, None) == B.CRF_EINVAL
+
+
+def test_constants_match_header():
+    text = open(os.path.join(os.path.dirname(B.PKG), "include", "crf_inside.h")).read()
+    for name in ("CRF_MAX_BUCKETS", "CRF_MAX_STEPS", "CRF_BF16", "CRF_F32"):
+        assert f"#define {name} {getattr(B, name)} " in text
+
+
+@pytest.mark.parametrize("n1,K,reach", [(2, 1, 1), (40, 1, 7), (60, 2, 2), (102, 16, 64), (300, 5, 81), (300, 9, 80), (64, 64, 40),
+                                        (1024, 32, 256), (1024, 1024, 600)])
+def test_width_buckets(n1, K, reach):
+    got = B.width_buckets(n1, K, reach)
+    single = (K + 1) // 2
+    assert got.dtype == np.int32 and got.shape == (n1,) and got.min() >= 0 and got.max() < K
+    for w in range(1, n1):
+        if w <= single or K == 1:
+            assert got[w] == min(w, K) - 1
+            continue
+        far = (K - single) * math.log(w / single) / math.log(reach / single)
+        want = min(K - 1, single + math.floor(far))
+        if abs(far - round(far)) < 1e-9:   # a border: by whole numbers
+            up = Fraction(reach, single) ** round(far) <= Fraction(w, single) ** (K - single)
+            want = min(K - 1, single + (round(far) if up else round(far) - 1))
+        assert got[w] == want, w
+
+
+def test_width_buckets_refuses():
+    for args in ((1, 4, 8), (8, 0, 8), (8, 1025, 2000), (8, 4, 2)):
+        with pytest.raises(ValueError):
+            B.width_buckets(*args)
+
+
+@pytest.fixture(scope="module")
+def harness(tmp_path_factory):
+    cxx = shutil.which("g++")
+    if cxx is None or not os.path.isdir(ROCM_INCLUDE):
+        pytest.skip("needs g++ and the HIP headers")
+    if not os.path.exists(B.LIB_PATH):
+        pytest.fail("libcrfinside.so is not built (run __graft_entry__.build())")
+    out = str(tmp_path_factory.mktemp("ops") / "scorer_ops")
+    subprocess.run([cxx, "-O1", "-g", "-std=c++17", "-rdynamic", "-D__HIP_PLATFORM_AMD__", "-I" + ROCM_INCLUDE,
+                    "-I" + os.path.join(HERE, "..", "include"), "-o", out, os.path.join(HERE, "scorer_ops_stub.cpp"),
+                    "-ldl", "-pthread"], check=True, capture_output=True, text=True)
+    return out
+
+
+def run(harness, *args):
+    res = subprocess.run([harness, args[0], B.LIB_PATH, *map(str, args[1:])], capture_output=True, text=True, timeout=120)
+    assert res.returncode == 0, res.stdout[-2000:] + res.stderr[-2000:]
+    return [line.split() for line in res.stdout.splitlines()]
+
+
+IN_PLACE = [["width", "out", "scores", "same"], ["muon", "w_out", "w", "same"], ["muon", "momentum_out", "momentum", "same"]]
+
+
+def test_overlapping_buffers_are_refused(harness):
+    rows = run(harness, "alias")
+    assert len(rows) > 150
+    for *what, status in rows:
+        ok = what[1] == "none" or what[-1] == "beside" or what in IN_PLACE
+        assert int(status) == (B.CRF_OK if ok else B.CRF_EINVAL), what
+    assert sum(what[:-1] in IN_PLACE for what in rows) == len(IN_PLACE)
+
+
+@pytest.mark.parametrize("lengths", [[1], [1023], [5] * 3000, list(range(1, 141)) * 3])
+@pytest.mark.parametrize("d,labels", [(4, 1), (100, 138), (500, 15), (8192, 4096)])
+def test_launches_fit_the_device(harness, lengths, d, labels):
+    rows = run(harness, "grids", d, labels, *lengths)
+    assert len(rows) >= 5
+    for _, name, gx, gy, gz, threads, lds in rows:
+        assert 1 <= int(gx) < 2 ** 31 and 1 <= int(gy) < 65536 and 1 <= int(gz) < 65536, name
+        assert int(threads) <= 1024 and int(lds) <= 160 * 1024, name
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 1), (4096, 1, 1), (1, 8192, 8192), (138, 100, 101), (1, 500, 501), (4096, 16, 300)])
+def test_update_launches_fit_the_device(harness, shape):
+    rows = run(harness, "update", *shape)
+    assert rows
+    for _, name, gx, gy, gz, threads, lds in rows:
+        assert 1 <= int(gx) < 2 ** 31 and 1 <= int(gy) < 65536 and 1 <= int(gz) < 65536, name
+        assert int(threads) <= 1024 and int(lds) <= 160 * 1024, name
+
+
+def test_scratch_memory():
+    with open(BLD.TRAIN_RESOURCES) as f:
+        rows = list(csv.DictReader(f, delimiter="\t"))
+    mine = [r for r in rows if any(x in r["kernel"] for x in ("norm_kernel", "norm_bwd_kernel", "norm_join", "width_", "ortho_"))]
+    assert len(mine) > 30
+    for r in mine:
+        assert int(r["ScratchSize [bytes/lane]"]) == 0, r["kernel"]

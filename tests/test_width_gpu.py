@@ -1,0 +1,215 @@
+"""The bias by a span's width on the GPU: the scores are one float32 addition,
+so equal bit for bit; the table's gradient is within n 2^-24 of its n terms'
+absolute sum."""
+import numpy as np
+import pytest
+
+from paper_2008_03736_amd import binding as B
+from paper_2008_03736_amd import workloads as W
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as _t
+
+    if not _t.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm device")
+    B.load()
+    return _t
+
+
+def inputs(lengths, n1, L, K, seed):
+    rng = np.random.default_rng(seed)
+    shape = (len(lengths), n1, n1) + ((L,) if L > 1 else ())
+    s = rng.standard_normal(shape).astype(np.float32)
+    s[~W.valid_mask(np.asarray(lengths), n1)] = np.nan
+    return s, rng.standard_normal((K, L)).astype(np.float32), rng.integers(-1, K + 1, n1).astype(np.int32)
+
+
+def biased(s, table, buckets, lengths):
+    """float32 scores with the bias on spans whose bucket is there, 7 elsewhere."""
+    n1, L = s.shape[1], table.shape[1]
+    w = np.arange(n1)[None] - np.arange(n1)[:, None]
+    k = buckets[np.maximum(w, 0)]
+    bias = np.where(((k >= 0) & (k < len(table)))[..., None], table[np.clip(k, 0, len(table) - 1)], np.float32(0))
+    got = s + (bias if s.ndim == 4 else bias[..., 0])[None]
+    got[~W.valid_mask(np.asarray(lengths), n1)] = 7
+    return got
+
+
+def gradient(g, buckets, K, lengths):
+    """float64 [K, L] sums and the terms' numbers and absolute sums."""
+    n1, L = g.shape[1], g.shape[3] if g.ndim == 4 else 1
+    g = g.reshape(g.shape[:3] + (L,)).astype(np.float64)
+    valid = W.valid_mask(np.asarray(lengths), n1)
+    w = np.broadcast_to((np.arange(n1)[None] - np.arange(n1)[:, None])[None], valid.shape)
+    k, g = buckets[w[valid]], g[valid]
+    out = [np.zeros((K, L)) for _ in range(3)]
+    for q in range(K):
+        mine = g[k == q]
+        out[0][q], out[1][q], out[2][q] = mine.sum(0), len(mine), np.abs(mine).sum(0)
+    return out
+
+
+BATCHES = {"one word": ([1], 2), "edges": ([1, 2, 15, 16, 17, 62, 63, 64, 65, 3], 70), "long": ([300, 7], 301),
+           "many": (np.random.default_rng(0).integers(1, 41, 300).tolist(), 44)}
+
+
+@pytest.mark.parametrize("name", sorted(BATCHES))
+@pytest.mark.parametrize("L", [1, 2, 3, 4, 15, 16, 26, 138])
+def test_bias_and_gradient(torch, name, L):
+    lengths, n1 = BATCHES[name]
+    if len(lengths) * n1 * n1 * L > 5e7:
+        lengths = lengths[:40]
+    K = 6
+    s, table, buckets = inputs(lengths, n1, L, K, L)
+    dev = lambda v: torch.from_numpy(v).to("cuda:0")
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        args = dev(s), dev(table), dev(buckets)
+        out = plan.width_bias(*args, out=torch.full(s.shape, 7.0, device="cuda:0"))
+        fresh = plan.width_bias(*args)
+        want = biased(s, table, buckets, lengths)
+        assert np.array_equal(out.cpu().numpy(), want)
+        valid = W.valid_mask(np.asarray(lengths), n1)
+        want[~valid] = 0
+        assert np.array_equal(fresh.cpu().numpy(), want)
+        held = args[0].clone()
+        assert plan.width_bias(held, *args[1:], out=held) is held
+        assert np.array_equal(held.cpu().numpy()[valid], want[valid]) and np.isnan(held.cpu().numpy()[~valid]).all()
+        gs, gt = plan.width_bias_bwd(args[0], args[2], K)
+        alone = plan.width_bias_bwd(args[0], args[2], K, need=(False, True))
+        copied = plan.width_bias_bwd(args[0], args[2], K, need=(True, False))
+        again = plan.width_bias_bwd(args[0], args[2], K)
+    assert alone[0] is None and copied[1] is None and torch.equal(alone[1], gt) and torch.equal(copied[0], gs)
+    assert torch.equal(again[0], gs) and torch.equal(again[1], gt)
+    s[~valid] = 0
+    assert np.array_equal(gs.cpu().numpy(), s)
+    sums, count, size = gradient(s, buckets, K, lengths)
+    assert np.all(np.abs(gt.cpu().numpy() - sums) <= count * 2.0 ** -24 * size)
+
+
+@pytest.mark.parametrize("shift", [1, 2])
+def test_arrays_that_start_inside_a_vector(torch, shift):
+    lengths, n1, L, K = [9, 4, 17], 18, 4, 3
+    s, table, buckets = inputs(lengths, n1, L, K, 3)
+    room = torch.zeros(s.size + 4, device="cuda:0")
+    x = room[shift:shift + s.size].view(s.shape)
+    x.copy_(torch.from_numpy(s))
+    b = torch.from_numpy(buckets).to("cuda:0")
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        out = plan.width_bias(x, torch.from_numpy(table).to("cuda:0"), b, out=torch.full(s.shape, 7.0, device="cuda:0"))
+        gs, gt = plan.width_bias_bwd(x, b, K)
+        want = plan.width_bias_bwd(x.clone(), b, K)
+    assert np.array_equal(out.cpu().numpy(), biased(s, table, buckets, lengths))
+    assert torch.equal(gs, want[0])
+    sums, count, size = gradient(np.nan_to_num(s), buckets, K, lengths)
+    assert np.all(np.abs(gt.cpu().numpy() - sums) <= count * 2.0 ** -24 * size)
+
+
+def test_buckets_without_spans_and_infinities(torch):
+    # buckets that no width has get 0; an infinite gradient stays in its bucket
+    lengths, n1 = [5, 3], 6
+    g = torch.ones((2, n1, n1), device="cuda:0")
+    g[0, 1, 3] = float("inf")
+    buckets = torch.tensor([9, 0, 2, 2, 5, 5], dtype=torch.int32, device="cuda:0")
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        _, gt = plan.width_bias_bwd(g, buckets, 7)
+    want = [5 + 3, 0, float("inf"), 0, 0, 2 + 1, 0]
+    assert gt[:, 0].tolist() == want
+
+
+def test_differentiable(torch):
+    lengths, n1, L = [6, 2, 4], 8, 3
+    rng = np.random.default_rng(1)
+    valid = W.valid_mask(np.asarray(lengths), n1)
+    buckets = torch.from_numpy(B.width_buckets(n1, 4, 6)).to("cuda:0")
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        s = torch.from_numpy(rng.standard_normal((3, n1, n1, L)).astype(np.float32)).to("cuda:0").requires_grad_()
+        table = torch.zeros((4, L), device="cuda:0").requires_grad_()
+        g = torch.from_numpy(rng.standard_normal((3, n1, n1, L)).astype(np.float32)).to("cuda:0")
+        out = B.width_bias(s, table, buckets, plan)
+        (out * g).sum().backward()
+        assert np.array_equal(s.grad.cpu().numpy(), np.where(valid[..., None], g.cpu().numpy(), 0))
+        sums, count, size = gradient(g.cpu().numpy(), buckets.cpu().numpy(), 4, lengths)
+        assert np.all(np.abs(table.grad.cpu().numpy() - sums) <= count * 2.0 ** -24 * size)
+        # the sum is linear in the table: a difference is the gradient but for roundings
+        moved = table.detach().clone()
+        moved[2, 1] += 1.0
+        step = ((B.width_bias(s, moved, buckets, plan) - out).double() * g.double()).sum().item()
+        assert abs(step - sums[2, 1]) <= 4 * 2.0 ** -24 * 8 * size[2, 1]   # (scores below 4: sums off by 2^-23 at most)
+
+
+def test_captured(torch):
+    lengths, n1, K = [30, 7, 64], 66, 5
+    s, table, buckets = inputs(lengths, n1, 1, K, 4)
+    s = np.nan_to_num(s)
+    dev = lambda v: torch.from_numpy(v).to("cuda:0")
+    xs, table, buckets = [dev(s), dev(s[::-1].copy())], dev(table), dev(buckets)
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        call = lambda x: (plan.width_bias(x, table, buckets), *plan.width_bias_bwd(x, buckets, K))
+        want = [call(x) for x in xs]
+        held, graphs = xs[0].clone(), []
+        for _ in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                graphs.append((g, call(held)))
+        for k in (0, 1, 0):
+            held.copy_(xs[k])
+            for g, _ in graphs:
+                g.replay()
+            torch.cuda.synchronize()
+            call(xs[1])
+            for _, out in graphs:
+                for a, b in zip(out, want[k]):
+                    assert torch.equal(a, b)
+
+
+def test_offsets_past_32_bits(torch):
+    # 2.2e9 cells and labels in all, 8.8 GB; the last sentence is checked
+    L, n1, K = 512, 256, 3
+    lengths = [1] * 64 + [255, 200]
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GB")
+    g = torch.zeros((66, n1, n1, L), device="cuda:0")
+    assert g.numel() > 1 << 31
+    rng = np.random.default_rng(5)
+    last = rng.standard_normal((2, n1, n1, L)).astype(np.float32)
+    last[~W.valid_mask(np.asarray(lengths[-2:]), n1)] = 0
+    g[-2:] = torch.from_numpy(last)
+    buckets = torch.from_numpy(rng.integers(0, K, n1).astype(np.int32)).to("cuda:0")
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        _, gt = plan.width_bias_bwd(g, buckets, K, need=(False, True))
+        table = torch.from_numpy(rng.standard_normal((K, L)).astype(np.float32)).to("cuda:0")
+        plan.width_bias(g, table, buckets, out=g)
+    sums, count, size = gradient(last, buckets.cpu().numpy(), K, lengths[-2:])
+    assert np.all(np.abs(gt.cpu().numpy() - sums) <= (count + 64) * 2.0 ** -24 * size)
+    want = biased(last, table.cpu().numpy(), buckets.cpu().numpy(), lengths[-2:])
+    got = g[-2:].cpu().numpy()
+    valid = W.valid_mask(np.asarray(lengths[-2:]), n1)
+    assert np.array_equal(got[valid], want[valid]) and (got[~valid] == 0).all()
+
+
+def test_refusals(torch):
+    dev = torch.device("cuda", 0)
+    with B.Plan([3, 5], n1=6, device=dev) as plan:
+        s, table, buckets = torch.zeros((2, 6, 6), device=dev), torch.zeros((4, 1), device=dev), \
+            torch.zeros(6, dtype=torch.int32, device=dev)
+        with pytest.raises(ValueError):
+            plan.width_bias(s, torch.zeros((4, 2), device=dev), buckets)
+        with pytest.raises(ValueError):
+            plan.width_bias(s, table, buckets.long())
+        with pytest.raises(ValueError):
+            plan.width_bias(s, table, buckets[:5])
+        with pytest.raises(ValueError):
+            plan.width_bias(s.double(), table, buckets)
+        with pytest.raises(ValueError):
+            plan.width_bias(s.transpose(1, 2), table, buckets)
+        with pytest.raises(B.CrfError, match="num_buckets"):
+            plan.width_bias(s, torch.zeros((1025, 1), device=dev), buckets)
+        with pytest.raises(B.CrfError, match="num_buckets"):
+            plan.width_bias_bwd(s, buckets, 0)
+        with pytest.raises(B.CrfError, match="alias"):
+            plan.width_bias_bwd(s, buckets, 4, grad_scores=s)
