@@ -701,6 +701,7 @@ hipError_t launch_width_bwd(const KernelPlan &p, int widest, int L, const float 
 // The orthogonalised update (crf_ortho.hip): workspace bytes and the launches.
 // momentum NULL: out = X of grad; else momentum_out, and out = keep w - rate X.
 int64_t ortho_bytes(int count, int rows, int cols);
+hipError_t set_ortho_attributes();   // the LDS of its kernels (once per device)
 hipError_t launch_ortho(const float *grad, const float *momentum, const float *w, float *momentum_out, float *out, int count,
                         int rows, int cols, int ld, float mu, bool nesterov, float keep, float rate, float eps,
                         const float *coefficients, int steps, char *ws, hipStream_t stream);

@@ -153,6 +153,18 @@ int check_matrices(int32_t count, int32_t rows, int32_t cols, int32_t ld) {
     return CRF_OK;
 }
 
+// Once a device, before any thread's first launch there (see scorer_backward).
+int set_update_attributes() {
+    int device = 0;
+    const hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+    static std::once_flag set[64];
+    std::call_once(set[device & 63], [] {
+        if (crf::set_ortho_attributes() != hipSuccess) (void)hipGetLastError();
+    });
+    return CRF_OK;
+}
+
 // What singular values, at most 1 at the start, grow to under the steps, and
 // the polynomials of the Gram matrix: the kernels hold both in a float16's range.
 int check_coefficients(const float *coefficients, int32_t steps, float eps) {
@@ -447,7 +459,8 @@ int crf_orthogonalize(const float *x, int32_t count, int32_t rows, int32_t cols,
     if (rc != CRF_OK || (rc = check_coefficients(coefficients, steps, eps)) != CRF_OK) return rc;
     const int64_t all = 4 * (int64_t)count * rows * ld, need = crf::ortho_bytes(count, rows, cols);
     if ((rc = check_workspace(workspace, workspace_bytes, need)) != CRF_OK ||
-        (rc = check_overlap({{"out", out, all}, {"workspace", workspace, need}}, {{"x", x, all}})) != CRF_OK)
+        (rc = check_overlap({{"out", out, all}, {"workspace", workspace, need}}, {{"x", x, all}})) != CRF_OK ||
+        (rc = set_update_attributes()) != CRF_OK)
         return rc;
     const hipError_t e = crf::launch_ortho(x, nullptr, nullptr, nullptr, out, count, rows, cols, ld, 0.f, false, 0.f, 0.f,
                                            eps, coefficients, steps, static_cast<char *>(workspace),
@@ -470,7 +483,8 @@ int crf_muon_step(const float *w, const float *grad, const float *momentum, int3
     if ((rc = check_workspace(workspace, workspace_bytes, need)) != CRF_OK ||
         (rc = check_overlap({{"w_out", w_out, all}, {"momentum_out", momentum_out, all}, {"workspace", workspace, need}},
                             {{"w", w == w_out ? nullptr : w, all}, {"grad", grad, all},
-                             {"momentum", momentum == momentum_out ? nullptr : momentum, all}})) != CRF_OK)
+                             {"momentum", momentum == momentum_out ? nullptr : momentum, all}})) != CRF_OK ||
+        (rc = set_update_attributes()) != CRF_OK)
         return rc;
     const hipError_t e = crf::launch_ortho(grad, momentum, w, momentum_out, w_out, count, rows, cols, ld, mu, nesterov != 0,
                                            1.f - decay, rate, eps, coefficients, steps, static_cast<char *>(workspace),
