@@ -560,8 +560,8 @@ int crf_orthogonalize_workspace(int32_t count, int32_t rows, int32_t cols, int64
  *   rows, cols    1 to CRF_MAX_ROW each; ld >= cols.
  *   coefficients  host float[steps][3], read during the call.  Singular values
  *                 from [0, 1] must stay in [0, 4] after every step, and
- *                 |b s^2 + c s^4| within 60 (CRF_EINVAL otherwise: the parts of
- *                 larger values would overflow).
+ *                 |a + b s^2 + c s^4| within 60 (CRF_EINVAL otherwise: the parts
+ *                 of larger values would overflow).
  *   steps         1 <= steps <= CRF_MAX_STEPS.
  *   eps           positive.
  * A matrix with an infinity or NaN gives NaN everywhere, the others are as

@@ -3,7 +3,7 @@
 //
 // With U the matrix (p rows, q >= p columns; a taller one is taken transposed),
 //     X = U / (|U|_F + eps), and for each of the steps' (a, b, c):
-//     A = X X^T,   B = b A + c A A,   X <- a X + B X,
+//     A = X X^T,   B = a I + b A + c A A,   X <- B X,
 // which keeps U's singular vectors and takes each singular value s to
 // a s + b s^3 + c s^5, step by step towards 1.
 //
@@ -30,16 +30,16 @@ namespace {
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTile = 64;             // rows and columns of an output tile
-constexpr int kStepK = 64;            // K staged at a time
-constexpr int kKStride = kStepK + 8;  // row stride of a staged piece
-constexpr int kNormChunk = 8192;      // entries of a share of a matrix's norm
+constexpr int kTile = 64;   // sides are padded to multiples of this, or of twice it
 
 // What X, A and B are held times: entries of at most 8, 32 and 64 fit float16.
 constexpr float kScaleX = 4096.f, kScaleA = 2048.f, kScaleB = 1024.f;
 
+// Matrices of more rows and columns than this are multiplied in tiles of 128 x 128.
+constexpr int kWide = 1024;
 // One matrix's arrays, each two planes (hi, then lo) of float16.
 struct OrthoShape {
     int p, q;          // sides, p <= q
@@ -51,11 +51,17 @@ __host__ __device__ inline OrthoShape ortho_shape(int rows, int cols) {
     OrthoShape s;
     s.p = rows < cols ? rows : cols;
     s.q = rows < cols ? cols : rows;
-    s.pp = (s.p + kTile - 1) / kTile * kTile;
-    s.qq = (s.q + kTile - 1) / kTile * kTile;
+    const int pad = s.p > kWide ? 2 * kTile : kTile;
+    s.pp = (s.p + pad - 1) / pad * pad;
+    s.qq = (s.q + pad - 1) / pad * pad;
     return s;
 }
-inline int norm_shares(int rows, int cols) { return (int)(((int64_t)rows * cols + kNormChunk - 1) / kNormChunk); }
+// Shares of a matrix's norm: of kShareRows x 256 entries, or at most kMostShares.
+constexpr int kShareRows = 4, kMostShares = 1024;
+inline int norm_shares(int rows, int cols) {
+    const int64_t size = (int64_t)rows * cols;
+    return (int)std::min<int64_t>((size + 256 * kShareRows - 1) / (256 * kShareRows), kMostShares);
+}
 
 // The caller's matrices.
 struct OrthoIo {
@@ -72,199 +78,376 @@ __device__ __forceinline__ float updated(const OrthoIo &io, float g, float m) {
 }
 
 // The new momentum, and shares of each matrix's sum of squares of U in 64 bits
-// (squares of float32 values neither overflow there nor vanish).
-__global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoIo io, double *__restrict__ shares) {
-    __shared__ double part[256];
-    const int64_t size = (int64_t)io.rows * io.ld, first = (int64_t)blockIdx.x * kNormChunk;
-    const int64_t base = blockIdx.y * size, count = (int64_t)io.rows * io.cols;
-    double s = 0.0;
-    for (int64_t k = first + threadIdx.x; k < min(first + kNormChunk, count); k += 256) {
-        const int64_t row = k / io.cols, at = base + row * io.ld + (k - row * io.cols);
-        float u = io.grad[at];
-        if (io.momentum != nullptr) {
-            const float m = fmaf(io.mu, io.momentum[at], u);
-            io.momentum_out[at] = m;
-            u = updated(io, u, m);
-        }
-        s += (double)u * (double)u;
-    }
+// (squares of float32 values neither overflow there nor vanish).  A workgroup
+// takes every gridDim.x-th run of kShareRows x 256 entries.
+__device__ __forceinline__ double sum_of_threads(double s, double *part) {
     part[threadIdx.x] = s;
     __syncthreads();
     for (int half = 128; half > 0; half /= 2) {
         if (threadIdx.x < half) part[threadIdx.x] += part[threadIdx.x + half];
         __syncthreads();
     }
-    if (threadIdx.x == 0) shares[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = part[0];
+    return part[0];
 }
-
-__device__ __forceinline__ void split(float v, _Float16 &hi, _Float16 &lo) {
-    hi = (_Float16)v;
-    lo = (_Float16)(v - (float)hi);
+__global__ __launch_bounds__(256) void ortho_norm_kernel(OrthoIo io, double *__restrict__ shares) {
+    __shared__ double part[256];
+    const int64_t base = (int64_t)blockIdx.y * io.rows * io.ld;
+    const int count = io.rows * io.cols;   // (at most 2^26)
+    double s = 0.0;
+    for (int first = blockIdx.x * 256 * kShareRows; first < count; first += gridDim.x * 256 * kShareRows) {
+        int64_t at[kShareRows];
+        float u[kShareRows], m[kShareRows];
+#pragma unroll
+        for (int e = 0; e < kShareRows; ++e) {
+            const int k = min(first + 256 * e + (int)threadIdx.x, count - 1), row = k / io.cols;
+            at[e] = base + (int64_t)row * io.ld + (k - row * io.cols);
+            u[e] = io.grad[at[e]];
+            if (io.momentum != nullptr) m[e] = io.momentum[at[e]];
+        }
+#pragma unroll
+        for (int e = 0; e < kShareRows; ++e)
+            if (first + 256 * e + (int)threadIdx.x < count) {
+                if (io.momentum != nullptr) {
+                    m[e] = fmaf(io.mu, m[e], u[e]);
+                    io.momentum_out[at[e]] = m[e];
+                    u[e] = updated(io, u[e], m[e]);
+                }
+                s += (double)u[e] * (double)u[e];
+            }
+    }
+    s = sum_of_threads(s, part);
+    if (threadIdx.x == 0) shares[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
 }
 
 __device__ __forceinline__ void split(const f32x4 &v, f16x4 &hi, f16x4 &lo) {
     hi = __builtin_convertvector(v, f16x4);
     lo = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
 }
+__device__ __forceinline__ void split(const float (&v)[8], f16x8 &hi, f16x8 &lo) {
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+        f16x4 a, b;
+        split(f32x4{v[h], v[h + 1], v[h + 2], v[h + 3]}, a, b);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) hi[h + t] = a[t], lo[h + t] = b[t];
+    }
+}
 __device__ __forceinline__ f32x4 joined(const f16x4 &hi, const f16x4 &lo) {
     return __builtin_convertvector(hi, f32x4) + __builtin_convertvector(lo, f32x4);
+}
+
+// A stored matrix of rows of K entries lies in blocks of 32 rows x 16 entries,
+// each an operand's fragment for the 64 lanes of a wavefront: a load or store of
+// one is 1 KB on end.  Entries 8 c .. 8 c + 7 of row r (one lane's) start at:
+__device__ __forceinline__ int64_t piece(int r, int c, int K) {
+    return ((int64_t)(r >> 5) * (K >> 4) + (c >> 1)) * 512 + ((r & 31) + 32 * (c & 1)) * 8;
 }
 
 // X = U / (|U|_F + eps) in parts, and its transpose; zeros past the matrix.
 __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoIo io, const double *__restrict__ shares, int n_shares,
                                                          _Float16 *__restrict__ x, _Float16 *__restrict__ xt) {
     __shared__ float tile[kTile][kTile + 1];
-    __shared__ double total;
+    __shared__ double part[256];
     const OrthoShape sh = ortho_shape(io.rows, io.cols);
-    if (threadIdx.x == 0) {
-        double s = 0.0;
-        for (int k = 0; k < n_shares; ++k) s += shares[(int64_t)blockIdx.z * n_shares + k];
-        total = s;
-    }
-    __syncthreads();
-    // (a sum that is not finite makes the whole matrix NaN)
-    const double inv = (double)kScaleX / (sqrt(total) + (double)io.eps) + 0.0 * total;
     const bool tall = io.rows > io.cols;
     const int i0 = blockIdx.y * kTile, j0 = blockIdx.x * kTile;   // of X
     const int64_t base = (int64_t)blockIdx.z * io.rows * io.ld;
-    for (int t = threadIdx.x; t < kTile * kTile; t += 256) {
-        const int r = t / kTile, c = t % kTile;   // along the caller's rows
-        const int row = (tall ? j0 : i0) + r, col = (tall ? i0 : j0) + c;
-        float u = 0.f;
-        if (row < io.rows && col < io.cols) {
-            const int64_t at = base + (int64_t)row * io.ld + col;
-            u = io.grad[at];
-            if (io.momentum != nullptr) u = updated(io, u, io.momentum_out[at]);
-            u = (float)((double)u * inv);
-        }
-        tile[tall ? c : r][tall ? r : c] = u;
+    float u[16], m[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {   // along the caller's rows, from their place 4 e + t / 64 on
+        const int row = (tall ? j0 : i0) + 4 * e + ((int)threadIdx.x >> 6), col = (tall ? i0 : j0) + ((int)threadIdx.x & 63);
+        const int64_t at = base + (int64_t)min(row, io.rows - 1) * io.ld + min(col, io.cols - 1);
+        u[e] = io.grad[at];
+        if (io.momentum != nullptr) m[e] = io.momentum_out[at];
+    }
+    double s = 0.0;
+    for (int k = threadIdx.x; k < n_shares; k += 256) s += shares[(int64_t)blockIdx.z * n_shares + k];
+    s = sum_of_threads(s, part);
+    // (a sum that is not finite makes the whole matrix NaN)
+    const double inv = (double)kScaleX / (sqrt(s) + (double)io.eps) + 0.0 * s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int r = 4 * e + ((int)threadIdx.x >> 6), c = (int)threadIdx.x & 63;
+        const bool there = (tall ? j0 : i0) + r < io.rows && (tall ? i0 : j0) + c < io.cols;
+        const float v = io.momentum != nullptr ? updated(io, u[e], m[e]) : u[e];
+        tile[tall ? c : r][tall ? r : c] = there ? (float)((double)v * inv) : 0.f;
     }
     __syncthreads();
     x += blockIdx.z * 2 * sh.x_plane();
     xt += blockIdx.z * 2 * sh.x_plane();
-    for (int t = threadIdx.x; t < kTile * kTile; t += 256) {
-        const int r = t / kTile, c = t % kTile;
-        _Float16 hi, lo;
-        split(tile[r][c], hi, lo);
-        const int64_t at = (int64_t)(i0 + r) * sh.qq + j0 + c;
-        x[at] = hi;
-        x[sh.x_plane() + at] = lo;
-        split(tile[c][r], hi, lo);
-        const int64_t tat = (int64_t)(j0 + r) * sh.pp + i0 + c;
-        xt[tat] = hi;
-        xt[sh.x_plane() + tat] = lo;
+    for (int e = threadIdx.x; e < kTile * kTile / 8; e += 256) {
+        const int r = e % kTile, c = e / kTile;
+        f16x8 hi, lo;
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = tile[r][8 * c + q];
+        split(v, hi, lo);
+        const int64_t at = piece(i0 + r, j0 / 8 + c, sh.qq), to = piece(j0 + r, i0 / 8 + c, sh.pp);
+        *reinterpret_cast<f16x8 *>(x + at) = hi;
+        *reinterpret_cast<f16x8 *>(x + sh.x_plane() + at) = lo;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = tile[8 * c + q][r];
+        split(v, hi, lo);
+        *reinterpret_cast<f16x8 *>(xt + to) = hi;
+        *reinterpret_cast<f16x8 *>(xt + sh.x_plane() + to) = lo;
     }
 }
 
-enum Product { kGram, kPoly, kNext, kLast };
-
 // One tile of a product of two matrices whose rows run along K:
-//   kGram  A = X X^T;             kPoly  B = b A + c A A;
-//   kNext  X' = a X + B X (from B and X^T), and its transpose;   kLast  the same, to the caller.
+//   kGram  A = X X^T;      kPoly  B = a I + b A + c A A;
+//   kNext  X' = B X (from B and X^T), and its transpose;   kLast  the same, to the caller.
+// A and B are symmetric: a tile on or above the diagonal is computed, and stored
+// as its mirror image too.
+enum Product { kGram, kPoly, kNext, kLast };
 struct ProductArgs {
     const _Float16 *left, *right;   // operands
-    const _Float16 *add;            // A for kPoly, X for kNext and kLast
-    _Float16 *out, *out_t;
-    int k, add_stride;              // K; row stride of add and out
-    int64_t left_plane, right_plane, add_plane;
-    float a, c;                     // out = a add + c product, in the scales of the result
-    int t_stride;
+    const _Float16 *add;            // A for kPoly
+    _Float16 *out, *out_t;          // the result and its transpose
+    int k, stride, t_stride;        // K; the entries of their rows
+    int across;                     // tiles of a row of tiles
+    int64_t left_plane, right_plane, out_plane;
+    float a, b, c;                  // in the scale of the result
 };
+
+// Workgroup's tile (i, j).
+template <int KIND>
+__device__ __forceinline__ void tile_of(const ProductArgs &g, int &i, int &j) {
+    const int t = blockIdx.x;
+    if constexpr (KIND == kGram || KIND == kPoly) {   // t = j (j + 1) / 2 + i, i <= j
+        j = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+        while ((j + 1) * (j + 2) / 2 <= t) ++j;
+        while (j * (j + 1) / 2 > t) --j;
+        i = t - j * (j + 1) / 2;
+    } else {
+        i = t / g.across;
+        j = t - i * g.across;
+    }
+}
 
 __device__ __forceinline__ f16x8 frag(const _Float16 *p) { return *reinterpret_cast<const f16x8 *>(p); }
 
-template <int KIND>
-__global__ __launch_bounds__(256) void ortho_product_kernel(ProductArgs g, OrthoIo io) {
-    __shared__ __align__(16) _Float16 stage[4][kTile][kKStride];   // left hi, lo, right hi, lo
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int i0 = blockIdx.y * kTile, j0 = blockIdx.x * kTile;
-    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + (int64_t)i0 * g.k;
-    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + (int64_t)j0 * g.k;
-    // thread t stages rows t / 8 and t / 8 + 32, entries 8 (t % 8) .. + 7
-    const int sr = tid >> 3, sk = 8 * (tid & 7);
-    u32x4 next[4][2];
-    auto load = [&](int k0) {
+// A tile's sums, in LDS at a row stride of T + 1, to where they belong: rows of
+// the result, then (from LDS, so that both are whole lines) rows of its transpose.
+template <int KIND, int T>
+__device__ __forceinline__ void finish_tile(float *tile, const ProductArgs &g, const OrthoIo &io, int i0, int j0) {
+    constexpr int kRow = T + 1, kPieces = T / 8;
+    const int tid = threadIdx.x;
+    if constexpr (KIND == kLast) {
+        const OrthoShape sh = ortho_shape(io.rows, io.cols);
+        const bool tall = io.rows > io.cols;
+        const int64_t base = (int64_t)blockIdx.z * io.rows * io.ld;
+        for (int e = tid; e < T * T; e += 256) {
+            const int r = e / T, c = e % T;   // along the caller's rows
+            const int i = i0 + (tall ? c : r), j = j0 + (tall ? r : c);
+            if (i < sh.p && j < sh.q) {
+                const float v = g.c * tile[tall ? c * kRow + r : r * kRow + c];
+                const int64_t to = base + (tall ? (int64_t)j * io.ld + i : (int64_t)i * io.ld + j);
+                io.out[to] = io.w != nullptr ? fmaf(-io.rate, v, io.keep * io.w[to]) : v;
+            }
+        }
+        return;
+    }
+    const bool mirror = KIND == kNext || i0 != j0;
+    _Float16 *out = g.out + blockIdx.z * 2 * g.out_plane;
+    const _Float16 *add = KIND == kPoly ? g.add + blockIdx.z * 2 * g.out_plane : nullptr;
+    for (int e = tid; e < T * kPieces; e += 256) {
+        const int r = e % T, c = e / T;
+        const int64_t at = piece(i0 + r, j0 / 8 + c, g.stride);
+        float *in = tile + r * kRow + 8 * c, v[8];
+        f16x8 hi, lo;
+        if constexpr (KIND == kPoly) {
+            hi = frag(add + at);
+            lo = frag(add + g.out_plane + at);
+        }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t at = (int64_t)(sr + 32 * h) * g.k + k0 + sk;
-            next[0][h] = *reinterpret_cast<const u32x4 *>(left + at);
-            next[1][h] = *reinterpret_cast<const u32x4 *>(left + g.left_plane + at);
-            next[2][h] = *reinterpret_cast<const u32x4 *>(right + at);
-            next[3][h] = *reinterpret_cast<const u32x4 *>(right + g.right_plane + at);
+        for (int q = 0; q < 8; ++q) {
+            v[q] = in[q] * g.c;
+            if constexpr (KIND == kPoly) {
+                v[q] = fmaf(g.b, (float)hi[q] + (float)lo[q], v[q]);
+                if (i0 + r == j0 + 8 * c + q) v[q] += g.a;
+                if (mirror) in[q] = v[q];
+            }
+        }
+        split(v, hi, lo);
+        *reinterpret_cast<f16x8 *>(out + at) = hi;
+        *reinterpret_cast<f16x8 *>(out + g.out_plane + at) = lo;
+    }
+    if (!mirror) return;
+    if constexpr (KIND == kPoly) __syncthreads();
+    _Float16 *out_t = g.out_t + blockIdx.z * 2 * g.out_plane;
+    for (int e = tid; e < T * kPieces; e += 256) {
+        const int r = e % T, c = e / T;
+        const int64_t at = piece(j0 + r, i0 / 8 + c, g.t_stride);
+        float v[8];
+        f16x8 hi, lo;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = tile[(8 * c + q) * kRow + r] * (KIND == kPoly ? 1.f : g.c);
+        split(v, hi, lo);
+        *reinterpret_cast<f16x8 *>(out_t + at) = hi;
+        *reinterpret_cast<f16x8 *>(out_t + g.out_plane + at) = lo;
+    }
+}
+
+// MFMA v_mfma_f32_32x32x16_f16: lane l supplies row l % 32 of either operand at K
+// offsets 8 (l / 32) .. + 7, and holds rows 8 (t / 4) + 4 (l / 32) + t % 4 of
+// column l % 32.
+__device__ __forceinline__ void put_sums(float *tile, int stride, const f32x16 &acc, int lane) {
+#pragma unroll
+    for (int t = 0; t < 16; ++t) tile[(8 * (t >> 2) + 4 * (lane >> 5) + (t & 3)) * stride + (lane & 31)] = acc[t];
+}
+
+// Few tiles: 32 x 32 a workgroup, K split over its four wavefronts, whose
+// fragments come straight from L2 (each is used once) and whose sums meet in LDS.
+constexpr int kFewTile = 32, kFewAhead = 4;   // steps of K (of 16) in flight together
+template <int KIND>
+__global__ __launch_bounds__(256) void ortho_few_kernel(ProductArgs g, OrthoIo io) {
+    __shared__ float sums[4][kFewTile * (kFewTile + 1)];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int i, j;
+    tile_of<KIND>(g, i, j);
+    const int steps = g.k / 16, part = steps / 4;   // (K is a multiple of 64)
+    const int64_t own = ((int64_t)wave * part) * 512 + 8 * lane;
+    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + (int64_t)i * steps * 512 + own;
+    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + (int64_t)j * steps * 512 + own;
+    f16x8 next[kFewAhead][4];
+    auto load = [&](int first) {
+#pragma unroll
+        for (int s = 0; s < kFewAhead; ++s) {
+            const int64_t at = 512 * (int64_t)min(first + s, part - 1);
+            next[s][0] = frag(left + at);
+            next[s][1] = frag(left + g.left_plane + at);
+            next[s][2] = frag(right + at);
+            next[s][3] = frag(right + g.right_plane + at);
         }
     };
     load(0);
-    f32x4 acc[2][2];
+    f32x16 acc[3];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int t = 0; t < 3; ++t)
 #pragma unroll
-        for (int n = 0; n < 2; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int wi = 32 * (wave >> 1), wj = 32 * (wave & 1);   // the wavefront's part of the tile
-    for (int k0 = 0; k0 < g.k; k0 += kStepK) {
-        __syncthreads();
+        for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+    for (int first = 0; first < part; first += kFewAhead) {
+        f16x8 now[kFewAhead][4];
+#pragma unroll
+        for (int s = 0; s < kFewAhead; ++s)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) now[s][t] = next[s][t];
+        if (first + kFewAhead < part) load(first + kFewAhead);
+#pragma unroll
+        for (int s = 0; s < kFewAhead; ++s)
+            if (first + s < part) {
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[s][0], now[s][3], acc[0], 0, 0, 0);
+                acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[s][1], now[s][2], acc[1], 0, 0, 0);
+                acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[s][0], now[s][2], acc[2], 0, 0, 0);
+            }
+    }
+    put_sums(sums[wave], kFewTile + 1, (acc[0] + acc[1]) + acc[2], lane);
+    __syncthreads();
+    for (int e = threadIdx.x; e < kFewTile * (kFewTile + 1); e += 256)
+        sums[0][e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+    __syncthreads();
+    finish_tile<KIND, kFewTile>(sums[0], g, io, kFewTile * i, kFewTile * j);
+}
+
+// Many: 64 M x 64 M a workgroup, staged through LDS 32 of K at a time, block by
+// block as they lie; a wavefront takes M x M tiles of 32 x 32.  2 M steps' loads
+// are on their way in registers: one from another XCD's L2 or from HBM takes as
+// long as two or three steps' products.
+constexpr int kStepK = 32;
+template <int M>
+constexpr int staged_bytes() { return std::max(2 * 16 * M * 1024, 64 * M * (64 * M + 1) * 4); }
+template <int KIND, int M>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ? 2 : 8))) void ortho_tile_kernel(ProductArgs g, OrthoIo io) {
+    constexpr int T = 64 * M, D = 2 * M, kPlane = 4 * M * 512, kBuffer = 4 * kPlane;   // left hi, lo, right hi, lo
+    extern __shared__ __align__(16) char smem[];
+    _Float16 *stage = reinterpret_cast<_Float16 *>(smem);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int i, j;
+    tile_of<KIND>(g, i, j);
+    // wavefront w moves blocks w + 4 h of each matrix's 4 M: row block / 2, K block
+    const int steps = g.k / 16;
+    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + ((int64_t)2 * M * i * steps) * 512 + 8 * lane;
+    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + ((int64_t)2 * M * j * steps) * 512 + 8 * lane;
+    f16x8 next[D][4][M];
+    auto load = [&](int d, int k0) {
+#pragma unroll
+        for (int h = 0; h < M; ++h) {
+            const int b = wave + 4 * h;
+            const int64_t at = ((int64_t)(b >> 1) * steps + k0 / 16 + (b & 1)) * 512;
+            next[d][0][h] = frag(left + at);
+            next[d][1][h] = frag(left + g.left_plane + at);
+            next[d][2][h] = frag(right + at);
+            next[d][3][h] = frag(right + g.right_plane + at);
+        }
+    };
+    auto store = [&](int d, int buffer) {
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) *reinterpret_cast<u32x4 *>(&stage[s][sr + 32 * h][sk]) = next[s][h];
-        __syncthreads();
-        if (k0 + kStepK < g.k) load(k0 + kStepK);
+            for (int h = 0; h < M; ++h)
+                *reinterpret_cast<f16x8 *>(stage + buffer * kBuffer + s * kPlane + (wave + 4 * h) * 512 + 8 * lane) = next[d][s][h];
+    };
 #pragma unroll
-        for (int k = 0; k < kStepK; k += 32) {
-            f16x8 l[2][2], r[2][2];
+    for (int d = 0; d < D; ++d) load(d, kStepK * d);
+    store(0, 0);
+    __syncthreads();
+    f32x16 acc[M][M];
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    l[s][m] = frag(&stage[s][wi + 16 * m + (lane & 15)][k + 8 * (lane >> 4)]);
-                    r[s][m] = frag(&stage[2 + s][wj + 16 * m + (lane & 15)][k + 8 * (lane >> 4)]);
-                }
+        for (int n = 0; n < M; ++n)
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int e = 0; e < 16; ++e) acc[m][n][e] = 0.f;
+    const int wi = 32 * M * (wave >> 1), wj = 32 * M * (wave & 1);   // the wavefront's part of the tile
+    for (int k0 = 0; k0 < g.k; k0 += kStepK * D)   // (K is a multiple of 64 M)
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(l[0][m], r[1][n], acc[m][n], 0, 0, 0);
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(l[1][m], r[0][n], acc[m][n], 0, 0, 0);
-                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(l[0][m], r[0][n], acc[m][n], 0, 0, 0);
-                }
-        }
-    }
-    // a lane holds rows 4 (lane / 16) .. + 3 of column lane % 16
-    const OrthoShape sh = ortho_shape(io.rows, io.cols);
-    const bool tall = io.rows > io.cols;
-    const _Float16 *add = KIND == kGram ? nullptr : g.add + blockIdx.z * 2 * g.add_plane;
+        for (int d = 0; d < D; ++d) {
+            const int now = k0 + kStepK * d;
+            load(d, min(now + kStepK * D, g.k - kStepK));   // (the last loads' data goes nowhere)
+            const _Float16 *from = stage + (d & 1) * kBuffer + 8 * lane;
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+            for (int k = 0; k < 2; ++k) {
+                f16x8 l[2][M], r[2][M];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int i = i0 + wi + 16 * m + 4 * (lane >> 4), j = j0 + wj + 16 * n + (lane & 15);
-            f16x4 hi, lo;
+                for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int64_t at = (int64_t)(i + t) * g.add_stride + j;
-                float v = g.c * acc[m][n][t];
-                if constexpr (KIND != kGram) v = fmaf(g.a, (float)add[at] + (float)add[g.add_plane + at], v);
-                if constexpr (KIND == kLast) {
-                    if (i + t < sh.p && j < sh.q) {
-                        const int64_t to = (int64_t)blockIdx.z * io.rows * io.ld +
-                                           (tall ? (int64_t)j * io.ld + i + t : (int64_t)(i + t) * io.ld + j);
-                        io.out[to] = io.w != nullptr ? fmaf(-io.rate, v, io.keep * io.w[to]) : v;
+                    for (int m = 0; m < M; ++m) {
+                        l[s][m] = frag(from + s * kPlane + (2 * (wi / 32 + m) + k) * 512);
+                        r[s][m] = frag(from + (2 + s) * kPlane + (2 * (wj / 32 + m) + k) * 512);
                     }
-                } else {
-                    _Float16 a, b;
-                    split(v, a, b);
-                    hi[t] = a;
-                    lo[t] = b;
-                    _Float16 *out = g.out + blockIdx.z * 2 * g.add_plane;
-                    out[at] = a;
-                    out[g.add_plane + at] = b;
-                }
+#pragma unroll
+                for (int s = 0; s < 3; ++s)   // hi lo, lo hi, hi hi
+#pragma unroll
+                    for (int m = 0; m < M; ++m)
+#pragma unroll
+                        for (int n = 0; n < M; ++n)
+                            acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[s == 1][m], r[s == 0][n], acc[m][n], 0, 0, 0);
             }
-            if constexpr (KIND == kNext) {
-                _Float16 *out = g.out_t + blockIdx.z * 2 * g.add_plane + (int64_t)j * g.t_stride + i;
-                *reinterpret_cast<f16x4 *>(out) = hi;
-                *reinterpret_cast<f16x4 *>(out + g.add_plane) = lo;
-            }
+            store((d + 1) % D, (d + 1) & 1);
+            __syncthreads();
         }
+    float *tile = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int n = 0; n < M; ++n) put_sums(tile + (wi + 32 * m) * (T + 1) + wj + 32 * n, T + 1, acc[m][n], lane);
+    __syncthreads();
+    finish_tile<KIND, T>(tile, g, io, T * i, T * j);
+}
+
+template <int KIND>
+void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int cols, int count, int T, hipStream_t stream) {
+    ProductArgs g = args;
+    g.across = cols / T;
+    const int down = rows / T;
+    const int tiles = KIND == kGram || KIND == kPoly ? down * (down + 1) / 2 : down * g.across;
+    const dim3 grid(tiles, 1, count);
+    if (T == kFewTile)
+        hipLaunchKernelGGL(ortho_few_kernel<KIND>, grid, dim3(256), 0, stream, g, io);
+    else if (T == 64)
+        hipLaunchKernelGGL((ortho_tile_kernel<KIND, 1>), grid, dim3(256), staged_bytes<1>(), stream, g, io);
+    else
+        hipLaunchKernelGGL((ortho_tile_kernel<KIND, 2>), grid, dim3(256), staged_bytes<2>(), stream, g, io);
 }
 
 // Matrices of up to kSmall x kSmall: a workgroup of W wavefronts each, which never
@@ -471,7 +654,7 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
         }
         __syncthreads();
 
-        // B = b A + c A A, held until every wavefront has read A
+        // B = a I + b A + c A A, held until every wavefront has read A
         f32x4 poly[kT];
         if (j < PT) {
             f16x8 rh[kKP], rl[kKP];
@@ -485,6 +668,11 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
                 const f16x4 hi = *reinterpret_cast<const f16x4 *>(gs + place(row_tile(u)));
                 const f16x4 lo = *reinterpret_cast<const f16x4 *>(gs + g_plane + place(row_tile(u)));
                 poly[u] = acc * (c3 * (kScaleB / (kScaleA * kScaleA))) + joined(hi, lo) * (b * (kScaleB / kScaleA));
+                if (u == 0) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (4 * g + t == n) poly[u][t] += a * kScaleB;
+                }
             });
         }
         __syncthreads();
@@ -495,15 +683,10 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
         }
         __syncthreads();
 
-        // X <- a X + B X, in the owner's registers
+        // X <- B X, in the owner's registers
         if (wave < qt)
             row_tiles<PT>(gs + n * kSG + 8 * g, g_plane, kSG, kKP, xh, xl, [](int i) { return i; },
-                          [&](int i, const f32x4 &acc) {
-                              const int h = 4 * (i & 1);
-                              const f16x4 hi = {xh[i >> 1][h], xh[i >> 1][h + 1], xh[i >> 1][h + 2], xh[i >> 1][h + 3]};
-                              const f16x4 lo = {xl[i >> 1][h], xl[i >> 1][h + 1], xl[i >> 1][h + 2], xl[i >> 1][h + 3]};
-                              x[i] = joined(hi, lo) * (a / kScaleX) + acc * (1.f / (kScaleB * kScaleX));
-                          });
+                          [&](int i, const f32x4 &acc) { x[i] = acc * (1.f / (kScaleB * kScaleX)); });
         // (the rows in LDS were last read before two barriers; B is next written after two more)
     }
 
@@ -539,8 +722,19 @@ void launch_small(const OrthoIo &io, const Steps &steps, int count, hipStream_t 
     hipLaunchKernelGGL((ortho_small_kernel<PT, 8>), dim3(count), dim3(512), (size_t)small_lds(p, q), stream, io, steps);
 }
 
+// The side of a workgroup's tile.
+int product_tile(const OrthoShape &sh, int count) {
+    if (sh.p > kWide) return 128;
+    return (int64_t)(sh.pp / 64) * (sh.qq / 64) * count <= 256 ? kFewTile : 64;
+}
+
 int64_t aligned(int64_t n) { return (n + 255) / 256 * 256; }
 
+template <int KIND>
+hipError_t tile_attribute() {
+    return hipFuncSetAttribute((const void *)ortho_tile_kernel<KIND, 2>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                               staged_bytes<2>());
+}
 template <int PT>
 hipError_t small_attribute() {
     const int most = (int)small_lds(16 * PT, kSmall);
@@ -556,7 +750,8 @@ hipError_t small_attribute() {
 
 hipError_t set_ortho_attributes() {
     for (auto set : {small_attribute<1>, small_attribute<2>, small_attribute<3>, small_attribute<4>, small_attribute<5>,
-                     small_attribute<6>, small_attribute<7>, small_attribute<8>}) {
+                     small_attribute<6>, small_attribute<7>, small_attribute<8>, tile_attribute<kGram>, tile_attribute<kPoly>,
+                     tile_attribute<kNext>, tile_attribute<kLast>}) {
         const hipError_t e = set();
         if (e != hipSuccess) return e;
     }
@@ -597,26 +792,28 @@ hipError_t launch_ortho(const float *grad, const float *momentum, const float *w
     for (int k = 0; k < 2; ++k) x[k] = take(sh.x_plane()), xt[k] = take(sh.x_plane());
     a = take(sh.a_plane());
     b = take(sh.a_plane());
-    const int n_shares = norm_shares(rows, cols), tp = sh.pp / kTile, tq = sh.qq / kTile;
+    const int n_shares = norm_shares(rows, cols);
     hipLaunchKernelGGL(ortho_norm_kernel, dim3(n_shares, count), dim3(256), 0, stream, io, shares);
-    hipLaunchKernelGGL(ortho_load_kernel, dim3(tq, tp, count), dim3(256), 0, stream, io, shares, n_shares, x[0], xt[0]);
+    hipLaunchKernelGGL(ortho_load_kernel, dim3(sh.qq / kTile, sh.pp / kTile, count), dim3(256), 0, stream, io, shares,
+                       n_shares, x[0], xt[0]);
+    const int T = product_tile(sh, count);
     for (int s = 0; s < steps; ++s) {
         const float *co = coefficients + 3 * s;
         const int now = s & 1;
-        const ProductArgs gram{x[now], x[now], nullptr, a, nullptr, sh.qq, sh.pp, sh.x_plane(), sh.x_plane(), sh.a_plane(),
-                               0.f, kScaleA / (kScaleX * kScaleX), 0};
-        const ProductArgs poly{a, a, a, b, nullptr, sh.pp, sh.pp, sh.a_plane(), sh.a_plane(), sh.a_plane(),
-                               co[1] * (kScaleB / kScaleA), co[2] * (kScaleB / (kScaleA * kScaleA)), 0};
-        hipLaunchKernelGGL(ortho_product_kernel<kGram>, dim3(tp, tp, count), dim3(256), 0, stream, gram, io);
-        hipLaunchKernelGGL(ortho_product_kernel<kPoly>, dim3(tp, tp, count), dim3(256), 0, stream, poly, io);
-        const bool last = s + 1 == steps;
-        const float to = last ? 1.f : kScaleX;
-        const ProductArgs next{b, xt[now], x[now], x[now ^ 1], xt[now ^ 1], sh.pp, sh.qq, sh.a_plane(), sh.x_plane(),
-                               sh.x_plane(), co[0] * (to / kScaleX), to / (kScaleB * kScaleX), sh.pp};
-        if (last)
-            hipLaunchKernelGGL(ortho_product_kernel<kLast>, dim3(tq, tp, count), dim3(256), 0, stream, next, io);
-        else
-            hipLaunchKernelGGL(ortho_product_kernel<kNext>, dim3(tq, tp, count), dim3(256), 0, stream, next, io);
+        const ProductArgs gram{x[now], x[now], nullptr, a, a, sh.qq, sh.pp, sh.pp, 0, sh.x_plane(), sh.x_plane(), sh.a_plane(),
+                               0.f, 0.f, kScaleA / (kScaleX * kScaleX)};
+        const ProductArgs poly{a, a, a, b, b, sh.pp, sh.pp, sh.pp, 0, sh.a_plane(), sh.a_plane(), sh.a_plane(),
+                               co[0] * kScaleB, co[1] * (kScaleB / kScaleA), co[2] * (kScaleB / (kScaleA * kScaleA))};
+        ProductArgs next{b, xt[now], nullptr, x[now ^ 1], xt[now ^ 1], sh.pp, sh.qq, sh.pp, 0, sh.a_plane(), sh.x_plane(),
+                         sh.x_plane(), 0.f, 0.f, 1.f / kScaleB};
+        launch_product<kGram>(gram, io, sh.pp, sh.pp, count, T, stream);
+        launch_product<kPoly>(poly, io, sh.pp, sh.pp, count, T, stream);
+        if (s + 1 == steps) {
+            next.c /= kScaleX;
+            launch_product<kLast>(next, io, sh.pp, sh.qq, count, T, stream);
+        } else {
+            launch_product<kNext>(next, io, sh.pp, sh.qq, count, T, stream);
+        }
     }
     return hipGetLastError();
 }

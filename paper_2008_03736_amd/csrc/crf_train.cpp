@@ -165,8 +165,8 @@ int set_update_attributes() {
     return CRF_OK;
 }
 
-// What singular values, at most 1 at the start, grow to under the steps, and
-// the polynomials of the Gram matrix: the kernels hold both in a float16's range.
+// What singular values, at most 1 at the start, grow to under the steps, and the
+// polynomials that they are multiplied by: the kernels hold both in a float16's range.
 int check_coefficients(const float *coefficients, int32_t steps, float eps) {
     if (coefficients == nullptr) return fail(CRF_EINVAL, "coefficients is NULL");
     if (steps < 1 || steps > CRF_MAX_STEPS) return fail(CRF_EINVAL, "steps %d outside [1, %d]", steps, CRF_MAX_STEPS);
@@ -179,8 +179,8 @@ int check_coefficients(const float *coefficients, int32_t steps, float eps) {
                 return fail(CRF_EINVAL, "step %d's coefficient %g is outside [-1000, 1000]", k, (double)f[q]);
         const double a = f[0], b = f[1], c = f[2], top = most * most;   // t = s^2 in [0, top]
         auto value = [&](double t) { return std::sqrt(t) * std::fabs(a + t * (b + t * c)); };
-        auto poly = [&](double t) { return std::fabs(t * (b + t * c)); };
-        double grown = value(top), inner = poly(top);
+        auto poly = [&](double t) { return std::fabs(a + t * (b + t * c)); };
+        double grown = value(top), inner = std::max(poly(0.0), poly(top));
         auto at = [&](double t) {
             if (t > 0.0 && t < top) grown = std::max(grown, value(t)), inner = std::max(inner, poly(t));
         };
