@@ -38,8 +38,8 @@ constexpr int kTile = 64;   // sides are padded to multiples of this, or of twic
 // What X, A and B are held times: entries of at most 8, 32 and 64 fit float16.
 constexpr float kScaleX = 4096.f, kScaleA = 2048.f, kScaleB = 1024.f;
 
-// Matrices of more rows and columns than this are multiplied in tiles of 128 x 128.
-constexpr int kWide = 1024;
+// Matrices of more rows and columns than this are padded to whole tiles of 128 x 128.
+constexpr int kWide = 512;
 // One matrix's arrays, each two planes (hi, then lo) of float16.
 struct OrthoShape {
     int p, q;          // sides, p <= q
@@ -435,13 +435,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ?
     finish_tile<KIND, T>(tile, g, io, T * i, T * j);
 }
 
+// The largest tile of which there are kEnoughTiles (half the CUs), or the least:
+// per step, one matrix of 768 x 768 30 us in tiles of 32 (34 of 64), of 1,024 x
+// 1,024 43 of 64 (47 of 32, 84 of 128), of 1,024 x 4,096 98 of 64 (150 of 128),
+// 16 of 500 x 501 75 of 128 (81 of 64, 99 of 32), one of 2,048 x 2,048 165 of 128
+// (179 of 64, 249 of 32).
+constexpr int kEnoughTiles = 128;
 template <int KIND>
-void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int cols, int count, int T, hipStream_t stream) {
+void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int cols, int count, hipStream_t stream) {
+    auto tiles = [&](int T) {
+        const int64_t down = rows / T, across = cols / T;
+        return KIND == kGram || KIND == kPoly ? down * (down + 1) / 2 : down * across;
+    };
     ProductArgs g = args;
+    const int T = rows % 128 == 0 && cols % 128 == 0 && tiles(128) * count >= kEnoughTiles ? 128
+                  : tiles(64) * count >= kEnoughTiles                                     ? 64
+                                                                                           : kFewTile;
     g.across = cols / T;
-    const int down = rows / T;
-    const int tiles = KIND == kGram || KIND == kPoly ? down * (down + 1) / 2 : down * g.across;
-    const dim3 grid(tiles, 1, count);
+    const dim3 grid((uint32_t)tiles(T), 1, count);
     if (T == kFewTile)
         hipLaunchKernelGGL(ortho_few_kernel<KIND>, grid, dim3(256), 0, stream, g, io);
     else if (T == 64)
@@ -722,12 +733,6 @@ void launch_small(const OrthoIo &io, const Steps &steps, int count, hipStream_t 
     hipLaunchKernelGGL((ortho_small_kernel<PT, 8>), dim3(count), dim3(512), (size_t)small_lds(p, q), stream, io, steps);
 }
 
-// The side of a workgroup's tile.
-int product_tile(const OrthoShape &sh, int count) {
-    if (sh.p > kWide) return 128;
-    return (int64_t)(sh.pp / 64) * (sh.qq / 64) * count <= 256 ? kFewTile : 64;
-}
-
 int64_t aligned(int64_t n) { return (n + 255) / 256 * 256; }
 
 template <int KIND>
@@ -796,7 +801,6 @@ hipError_t launch_ortho(const float *grad, const float *momentum, const float *w
     hipLaunchKernelGGL(ortho_norm_kernel, dim3(n_shares, count), dim3(256), 0, stream, io, shares);
     hipLaunchKernelGGL(ortho_load_kernel, dim3(sh.qq / kTile, sh.pp / kTile, count), dim3(256), 0, stream, io, shares,
                        n_shares, x[0], xt[0]);
-    const int T = product_tile(sh, count);
     for (int s = 0; s < steps; ++s) {
         const float *co = coefficients + 3 * s;
         const int now = s & 1;
@@ -806,13 +810,13 @@ hipError_t launch_ortho(const float *grad, const float *momentum, const float *w
                                co[0] * kScaleB, co[1] * (kScaleB / kScaleA), co[2] * (kScaleB / (kScaleA * kScaleA))};
         ProductArgs next{b, xt[now], nullptr, x[now ^ 1], xt[now ^ 1], sh.pp, sh.qq, sh.pp, 0, sh.a_plane(), sh.x_plane(),
                          sh.x_plane(), 0.f, 0.f, 1.f / kScaleB};
-        launch_product<kGram>(gram, io, sh.pp, sh.pp, count, T, stream);
-        launch_product<kPoly>(poly, io, sh.pp, sh.pp, count, T, stream);
+        launch_product<kGram>(gram, io, sh.pp, sh.pp, count, stream);
+        launch_product<kPoly>(poly, io, sh.pp, sh.pp, count, stream);
         if (s + 1 == steps) {
             next.c /= kScaleX;
-            launch_product<kLast>(next, io, sh.pp, sh.qq, count, T, stream);
+            launch_product<kLast>(next, io, sh.pp, sh.qq, count, stream);
         } else {
-            launch_product<kNext>(next, io, sh.pp, sh.qq, count, T, stream);
+            launch_product<kNext>(next, io, sh.pp, sh.qq, count, stream);
         }
     }
     return hipGetLastError();
