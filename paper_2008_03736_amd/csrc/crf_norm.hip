@@ -26,10 +26,17 @@ namespace crf {
 namespace {
 
 constexpr int kNormUnroll = 4;    // rows of a group of lanes in flight, forward
-constexpr int kNormUnrollBwd = 2;
-constexpr int kNormGroups = 512;  // most workgroups (of 256 threads) that sum dgamma and dbeta
+// Most workgroups (of 256 threads) that sum dgamma and dbeta: four a CU (5,000
+// sentences of d = 500: 114 us at 768, 100.5, 106 at 2,048).
+constexpr int kNormGroups = 1024;
 
 __host__ __device__ constexpr int norm_threads(int G) { return G > 256 ? G : 256; }
+
+// Rows of a group of lanes in flight, backward: the registers of two cost
+// wavefronts where rows are float32 or meet in LDS (24 paragraphs of d = 4,096 in
+// float32 69.7 us with two, 61.6 with one; 5,000 sentences of d = 500 100.5 and 104).
+template <typename T, int G>
+constexpr int norm_unroll_bwd() { return sizeof(T) == 4 || G > 64 ? 1 : 2; }
 
 // Pieces of rows: bf16 rows start at multiples of 8 bytes, float32 ones of 4.
 typedef uint32_t u32x4_a8 __attribute__((ext_vector_type(4), aligned(8)));
@@ -206,7 +213,7 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(const int32_t
                                                                    const uint16_t *__restrict__ dy, float eps,
                                                                    T *__restrict__ dx, float *__restrict__ parts,
                                                                    float *__restrict__ dgamma, float *__restrict__ dbeta) {
-    constexpr int U = kNormUnrollBwd, kRows = norm_threads(G) / G;
+    constexpr int U = norm_unroll_bwd<T, G>(), kRows = norm_threads(G) / G;
     __shared__ float slots[2][U * 16], slots2[2 * U * 16];
     __shared__ float sums[PARTS && kRows > 1 ? kRows * 16 * G : 1];
     const int lane = threadIdx.x & (G - 1), k = 8 * lane;
@@ -215,22 +222,41 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(const int32_t
     weights(gamma, k, d, 1.f, g);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sg[q] = sb[q] = 0.f;
-    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const int32_t *ids = chunk_ids<G, U>(posts, c);
-        int id[U];
-        Raw<T> raw[U];
-        Raw<uint16_t> up[U];
+    // the next chunk's rows are on their way while this one's are worked on, and
+    // the ids of the one after it
+    int id[U], id1[U], id2[U];
+    Raw<T> raw1[U];
+    Raw<uint16_t> up1[U];
+    auto ids_of = [&](int (&to)[U], int c) {
+        const int32_t *ids = chunk_ids<G, U>(posts, min(c, chunks - 1));
+#pragma unroll
+        for (int u = 0; u < U; ++u) to[u] = c < chunks ? ids[u] : -1;
+    };
+    auto load = [&]() {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            id[u] = ids[u];
-            if (id[u] >= 0) {
-                raw[u].load(x + (size_t)id[u] * d, k, d);
-                up[u].load(dy + (size_t)id[u] * d, k, d);
+            raw1[u] = Raw<T>();
+            up1[u] = Raw<uint16_t>();
+            if (id1[u] >= 0) {
+                raw1[u].load(x + (size_t)id1[u] * d, k, d);
+                up1[u].load(dy + (size_t)id1[u] * d, k, d);
             }
         }
+    };
+    ids_of(id1, blockIdx.x);
+    ids_of(id2, blockIdx.x + gridDim.x);
+    load();
+    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         float f[U][8], r[U], e[U][8], two[2 * U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u].widen(f[u]), up[u].widen(e[u]);
+        for (int u = 0; u < U; ++u) {
+            raw1[u].widen(f[u]);
+            up1[u].widen(e[u]);
+            id[u] = id1[u];
+            id1[u] = id2[u];
+        }
+        load();
+        ids_of(id2, c + 2 * gridDim.x);
         statistics<G, U>(f, r, k, d, eps, slots);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -317,9 +343,7 @@ int norm_lanes(int d) {
     return g;
 }
 int norm_chunks(const KernelPlan &p, int G, int U) { return p.n_posts * (kBiaRows / (norm_threads(G) / G * U)); }
-int norm_parts(const KernelPlan &p, int G) {
-    return std::min(norm_chunks(p, G, kNormUnrollBwd), kNormGroups * 256 / norm_threads(G));
-}
+int norm_parts(int chunks, int G) { return std::min(chunks, kNormGroups * 256 / norm_threads(G)); }
 
 template <typename T, int G>
 void launch_norm_g(const KernelPlan &p, const void *x, int d, const float *gamma, const float *beta, float eps, uint16_t *y,
@@ -331,13 +355,13 @@ void launch_norm_g(const KernelPlan &p, const void *x, int d, const float *gamma
 template <typename T, int G>
 void launch_norm_bwd_g(const KernelPlan &p, const void *x, int d, const float *gamma, const uint16_t *dy, float eps,
                        void *dx, float *dgamma, float *dbeta, float *parts, hipStream_t stream) {
-    const int chunks = norm_chunks(p, G, kNormUnrollBwd);
+    const int chunks = norm_chunks(p, G, norm_unroll_bwd<T, G>());
     if (dgamma == nullptr && dbeta == nullptr) {
         hipLaunchKernelGGL((norm_bwd_kernel<T, G, false>), dim3(chunks), dim3(norm_threads(G)), 0, stream, p.posts, chunks,
                            d, static_cast<const T *>(x), gamma, dy, eps, static_cast<T *>(dx), nullptr, nullptr, nullptr);
         return;
     }
-    const int count = norm_parts(p, G);
+    const int count = norm_parts(chunks, G);
     hipLaunchKernelGGL((norm_bwd_kernel<T, G, true>), dim3(count), dim3(norm_threads(G)), 0, stream, p.posts, chunks, d,
                        static_cast<const T *>(x), gamma, dy, eps, static_cast<T *>(dx), parts, dgamma, dbeta);
     if (count > 1)
@@ -360,7 +384,7 @@ void launch_norm_bwd_g(const KernelPlan &p, const void *x, int d, const float *g
 
 int64_t norm_bwd_bytes(const KernelPlan &p, int d) {
     const int G = norm_lanes(d);
-    return ((int64_t)norm_parts(p, G) * 16 * G * 4 + 255) / 256 * 256;
+    return ((int64_t)norm_parts(norm_chunks(p, G, 1), G) * 16 * G * 4 + 255) / 256 * 256;   // (of either type)
 }
 
 hipError_t launch_norm(const KernelPlan &p, const void *x, bool f32, int d, const float *gamma, const float *beta,

@@ -22,8 +22,13 @@ namespace crf {
 namespace {
 
 constexpr int kWidthThreads = 256;
-constexpr int kWidthGroups = 2048;   // workgroups that fill the chip
-constexpr int kWidthShares = 512;    // most shares of the rows whose sums are joined
+constexpr int kFewBuckets = 64;
+constexpr int kMaxWidth = 1023;      // a sentence's most words
+// Workgroups that a call aims at.  Forward, 100 sentences of 138 labels: 19.6 us at
+// 1,024, 14.8 at 2,048, 12.7 at 4,096.  Back, where each adds a share to what is
+// joined: 18.6 and 5.4 us at 1,024, 15.4 and 4.5 at 2,048, 14.9 and 7.9 at 4,096.
+constexpr int kWidthGroups = 4096, kWidthSumGroups = 2048;
+constexpr int kWidthShares = 1024;   // most shares (5,000 sentences: 18.9 us at 512, 15.4, 16.6 at 2,048)
 
 template <int V>
 struct Cells;
@@ -44,32 +49,40 @@ struct Cells<4> {
 template <int V>
 __device__ __forceinline__ typename Cells<V>::type entry(const float *table, const int32_t *bucket, int K, int L, int w,
                                                          int label) {
-    typename Cells<V>::type v = 0.f;
+    typename Cells<V>::type v;
     const int k = bucket[w];
-    if (k >= 0 && k < K) {
-        const float *row = table + (size_t)k * L + label;
-        if constexpr (V == 1) {
-            v = row[0];
-        } else {
+    const bool there = k >= 0 && k < K;
+    const float *row = table + (size_t)(there ? k : 0) * L + label;
+    if constexpr (V == 1) {
+        v = there ? row[0] : 0.f;
+    } else {
 #pragma unroll
-            for (int q = 0; q < V; ++q) v[q] = row[q];
-        }
+        for (int q = 0; q < V; ++q) v[q] = there ? row[q] : 0.f;
     }
     return v;
 }
 
-// A workgroup takes a block of posts and every gridDim.y-th tile of P places.
-template <int V, int P>
+// Thread t's first row of a block of posts: with P = 64 a wavefront's, so that
+// what is looked up by it is in scalar registers.
+template <int P>
+__device__ __forceinline__ int first_row() {
+    const int r = threadIdx.x / P;
+    return P == 64 ? __builtin_amdgcn_readfirstlane(r) : r;
+}
+
+// A workgroup takes a block of posts and every gridDim.y-th group of N tiles of P
+// places.
+template <int V, int P, int N>
 __global__ __launch_bounds__(kWidthThreads) void width_kernel(const int32_t *__restrict__ posts,
-                                                              const int64_t *__restrict__ post_cells, int widest, int L,
-                                                              int K, const float *__restrict__ table,
-                                                              const int32_t *__restrict__ bucket,
-                                                              const float *scores, float *out) {
+                                                              const int64_t *__restrict__ post_cells, int L, int K,
+                                                              const float *__restrict__ table,
+                                                              const int32_t *__restrict__ bucket, const float *scores,
+                                                              float *out) {
     typedef typename Cells<V>::type cells;
     constexpr int kRows = kWidthThreads / P, kMine = kBiaRows / kRows;
     const int32_t *rest = posts + (size_t)blockIdx.x * kPostRec + kBiaRows;
     const int64_t *at = post_cells + (size_t)blockIdx.x * kBiaRows;
-    const int r0 = threadIdx.x / P, per = L / V;   // places of a width
+    const int r0 = first_row<P>(), per = L / V;   // places of a width
     int wide[kMine], most = 0;
     size_t base[kMine];
 #pragma unroll
@@ -78,119 +91,234 @@ __global__ __launch_bounds__(kWidthThreads) void width_kernel(const int32_t *__r
         base[m] = (size_t)at[r0 + m * kRows] * L;
         most = max(most, wide[m]);
     }
-    for (int e = blockIdx.y * P + threadIdx.x % P; e < most * per; e += gridDim.y * P) {
-        const int w = e / per, label = (e - w * per) * V;
-        const cells bias = entry<V>(table, bucket, K, L, w + 1, label);
-        const size_t off = (size_t)(w + 1) * L + label;
-        cells v[kMine];
+    for (int e0 = blockIdx.y * N * P + threadIdx.x % P; e0 < most * per; e0 += gridDim.y * N * P) {
+        int w[N];
+        size_t off[N];
+        cells v[N][kMine], bias[N];
 #pragma unroll
-        for (int m = 0; m < kMine; ++m)
-            if (w < wide[m]) v[m] = *reinterpret_cast<const cells *>(scores + base[m] + off);
+        for (int t = 0; t < N; ++t) {
+            const int e = e0 + t * P;
+            w[t] = e / per;
+            off[t] = (size_t)(w[t] + 1) * L + (e - w[t] * per) * V;
 #pragma unroll
-        for (int m = 0; m < kMine; ++m)
-            if (w < wide[m]) *reinterpret_cast<cells *>(out + base[m] + off) = v[m] + bias;
+            for (int m = 0; m < kMine; ++m)
+                if (w[t] < wide[m]) v[t][m] = *reinterpret_cast<const cells *>(scores + base[m] + off[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < N; ++t)   // (on its way beside the scores; widths past the row's are not there)
+            bias[t] = entry<V>(table, bucket, K, L, min(w[t] + 1, most), (e0 + t * P - w[t] * per) * V);
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int m = 0; m < kMine; ++m)
+                if (w[t] < wide[m]) *reinterpret_cast<cells *>(out + base[m] + off[t]) = v[t][m] + bias[t];
     }
 }
 
-// A workgroup takes tile blockIdx.y of P places and every gridDim.x-th block of posts.
-template <int V, int P>
+// A workgroup takes N tiles of P places, from tile N blockIdx.y on, and every
+// gridDim.x-th block of posts.
+template <int V, int P, int N>
 __global__ __launch_bounds__(kWidthThreads) void width_bwd_kernel(const int32_t *__restrict__ posts,
                                                                   const int64_t *__restrict__ post_cells, int n_posts,
                                                                   int widest, int L, const float *__restrict__ grad,
+                                                                  const int32_t *__restrict__ bucket, int K,
                                                                   float *__restrict__ grad_scores,
                                                                   float *__restrict__ parts) {
     typedef typename Cells<V>::type cells;
     constexpr int kRows = kWidthThreads / P, kMine = kBiaRows / kRows;
-    __shared__ cells sums[kRows][P];
-    const int r0 = threadIdx.x / P, c = threadIdx.x % P, per = L / V;
-    const int e = blockIdx.y * P + c, w = e / per, label = (e - w * per) * V;
-    const size_t off = (size_t)(w + 1) * L + label;
-    cells sum = 0.f;
-    for (int block = blockIdx.x; block < n_posts; block += gridDim.x) {
+    __shared__ cells sums[kRows][N * P];
+    __shared__ int buckets[P == 16 ? N * P + 1 : 1];
+    const int r0 = first_row<P>(), c = threadIdx.x % P, per = L / V, e0 = blockIdx.y * N * P + c;
+    int w[N];
+    size_t off[N];
+    cells sum[N];
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        const int e = e0 + t * P;
+        w[t] = e / per;
+        off[t] = (size_t)(w[t] + 1) * L + (e - w[t] * per) * V;
+        sum[t] = 0.f;
+    }
+    // (the next block's rows are looked up while this one's cells are read)
+    int wide[kMine], wide1[kMine];
+    size_t base[kMine], base1[kMine];
+    auto look = [&](int block) {
         const int32_t *rest = posts + (size_t)block * kPostRec + kBiaRows;
         const int64_t *at = post_cells + (size_t)block * kBiaRows;
-        cells v[kMine];
 #pragma unroll
         for (int m = 0; m < kMine; ++m) {
-            const int r = r0 + m * kRows;
-            v[m] = 0.f;
-            if (w < rest[r]) {
-                const size_t cell = (size_t)at[r] * L + off;
-                v[m] = *reinterpret_cast<const cells *>(grad + cell);
-                if (grad_scores != nullptr) *reinterpret_cast<cells *>(grad_scores + cell) = v[m];
+            wide1[m] = rest[r0 + m * kRows];
+            base1[m] = (size_t)at[r0 + m * kRows] * L;
+        }
+    };
+    look(blockIdx.x);
+    for (int block = blockIdx.x; block < n_posts; block += gridDim.x) {
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) wide[m] = wide1[m], base[m] = base1[m];
+        if (block + (int)gridDim.x < n_posts) look(block + (int)gridDim.x);
+        cells v[N][kMine];
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int m = 0; m < kMine; ++m) {
+                v[t][m] = 0.f;
+                if (w[t] < wide[m]) v[t][m] = *reinterpret_cast<const cells *>(grad + base[m] + off[t]);
             }
+        if (grad_scores != nullptr) {
+#pragma unroll
+            for (int t = 0; t < N; ++t)
+#pragma unroll
+                for (int m = 0; m < kMine; ++m)
+                    if (w[t] < wide[m]) *reinterpret_cast<cells *>(grad_scores + base[m] + off[t]) = v[t][m];
         }
 #pragma unroll
-        for (int m = 0; m < kMine; ++m) sum += v[m];
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int m = 0; m < kMine; ++m) sum[t] += v[t][m];
     }
     if (parts == nullptr) return;
-    sums[r0][c] = sum;
+#pragma unroll
+    for (int t = 0; t < N; ++t) sums[r0][t * P + c] = sum[t];
     __syncthreads();
-    for (int half = kRows / 2; half > 0; half /= 2) {
-        if (r0 < half) sums[r0][c] += sums[r0 + half][c];
-        __syncthreads();
+    // to parts[width's label][share], or parts[bucket's label][share] (K > 0)
+    const int shares = gridDim.x * (K > 0 ? gridDim.y : 1), share = K > 0 ? blockIdx.y * gridDim.x + blockIdx.x : blockIdx.x;
+    const int first = blockIdx.y * N * P;
+    for (int q = threadIdx.x; q < N * P; q += kWidthThreads) {
+        cells s = sums[0][q];
+        for (int r = 1; r < kRows; ++r) s += sums[r][q];
+        if (P == 16 && K > 0) {
+            sums[0][q] = s;
+        } else if (first + q < widest * per) {
+            float *to = parts + (size_t)(first + q) * V * shares + share;
+            if constexpr (V == 1) {
+                to[0] = s;
+            } else {
+#pragma unroll
+                for (int h = 0; h < V; ++h) to[h * shares] = s[h];
+            }
+        }
     }
-    if (r0 == 0 && e < widest * per)
-        *reinterpret_cast<cells *>(parts + ((size_t)blockIdx.x * widest * per + e) * V) = sums[0][c];
+    if constexpr (P == 16) {
+        if (K == 0) return;
+        // the widths that this workgroup has places of, and their buckets
+        const int w0 = first / per, w1 = min((first + N * P - 1) / per, widest - 1);
+        for (int q = threadIdx.x; w0 + q <= w1; q += kWidthThreads) buckets[q] = bucket[w0 + q + 1];
+        __syncthreads();
+        // sixteen lanes a bucket's label, every sixteenth width each
+        for (int q = threadIdx.x / 16; q < K * L; q += kWidthThreads / 16) {
+            const int k = q / L, label = q - k * L, part = label / V, h = label - part * V;
+            float s = 0.f;
+            for (int v = w0 + threadIdx.x % 16; v <= w1; v += 16) {
+                const int place = v * per + part - first;
+                if (buckets[v - w0] == k && place >= 0 && place < N * P)
+                    s += reinterpret_cast<const float *>(sums[0])[place * V + h];
+            }
+#pragma unroll
+            for (int x = 1; x < 16; x *= 2) s += __shfl_xor(s, x, 16);
+            if (threadIdx.x % 16 == 0) parts[(size_t)q * shares + share] = s;
+        }
+    }
 }
 
-// A bucket's widths and the shares of the rows added up: 16 labels a workgroup,
-// thread (l, p) every 16th of the bucket's (width, share) pairs.
-constexpr int kJoinLabels = 16, kJoinLanes = 16;
-__global__ __launch_bounds__(kJoinLabels *kJoinLanes) void width_join_kernel(const float *__restrict__ parts, int shares,
-                                                                             int widest, int L,
-                                                                             const int32_t *__restrict__ bucket,
-                                                                             float *__restrict__ grad_table) {
-    __shared__ float part[kJoinLanes][kJoinLabels + 1];
-    const int k = blockIdx.x, l = threadIdx.x % kJoinLabels, p = threadIdx.x / kJoinLabels;
-    const int label = blockIdx.y * kJoinLabels + l;
+// A bucket's widths and the shares of the rows added up in a fixed order: J
+// labels a workgroup, thread (l, p) every kLanes-th of the bucket's (width,
+// share) pairs.
+constexpr int kJoinThreads = 1024;
+template <int J>
+__global__ __launch_bounds__(kJoinThreads) void width_join_kernel(const float *__restrict__ parts, int shares, int widest,
+                                                                  int L, const int32_t *__restrict__ bucket,
+                                                                  bool by_bucket, float *__restrict__ grad_table) {
+    constexpr int kLanes = kJoinThreads / J;
+    __shared__ float part[kLanes][J + 1];
+    __shared__ uint16_t widths[1024];   // the bucket's, in order
+    __shared__ int before[kJoinThreads / 64];
+    static_assert(kMaxWidth <= 1024 && kMaxWidth <= kJoinThreads, "a thread a width");
+    const int k = blockIdx.x, tid = threadIdx.x, l = tid % J, p = tid / J, label = blockIdx.y * J + l;
+    // the rows of parts that are the bucket's: its widths, or itself
+    const bool mine = by_bucket ? tid == k : tid < widest && bucket[tid + 1] == k;
+    const uint64_t all = __ballot(mine);
+    if ((tid & 63) == 0) before[tid >> 6] = __popcll(all);
+    __syncthreads();
+    int count = 0, at = 0;
+    for (int w = 0; w < kJoinThreads / 64; ++w) {
+        if (w == tid >> 6) at = count;
+        count += before[w];
+    }
+    if (mine) widths[at + __popcll(all & ((1ull << (tid & 63)) - 1))] = (uint16_t)tid;
+    __syncthreads();
     float s = 0.f;
-    if (label < L)
-        for (int w = 0; w < widest; ++w) {
-            if (bucket[w + 1] != k) continue;
-#pragma unroll 4
-            for (int q = p; q < shares; q += kJoinLanes) s += parts[((size_t)q * widest + w) * L + label];
+    if (label < L) {
+#pragma unroll 8
+        for (int q = p; q < count * shares; q += kLanes) {
+            const int w = q / shares;
+            s += parts[((size_t)widths[w] * L + label) * shares + q - w * shares];
         }
+    }
     part[p][l] = s;
     __syncthreads();
-    for (int half = kJoinLanes / 2; half > 0; half /= 2) {
+    for (int half = kLanes / 2; half > 0; half /= 2) {
         if (p < half) part[p][l] += part[p + half][l];
         __syncthreads();
     }
     if (p == 0 && label < L) grad_table[(size_t)k * L + label] = part[0][l];
 }
 
-// Places of a tile: rows of one label are short, those of many long.
+// Places of a tile, and tiles a workgroup has in flight: rows of one label are
+// short, those of many long.
 bool many_labels(int L) { return L >= 16; }
-int tiles(int widest, int L, int V) { return (int)(((int64_t)widest * (L / V) + (many_labels(L) ? 63 : 15)) / (many_labels(L) ? 64 : 16)); }
+constexpr int tiles_in_flight(int V, int P) { return P == 64 ? 1 : 8 / V; }
+int tiles(int widest, int L, int V) {
+    const int P = many_labels(L) ? 64 : 16;
+    return (int)(((int64_t)widest * (L / V) + P - 1) / P);
+}
 // Labels a thread takes: what the arrays' alignment allows.
 int labels_each(int L, const void *a, const void *b) {
     const uintptr_t at = (uintptr_t)a | (uintptr_t)b;
     return L % 4 == 0 && at % 16 == 0 ? 4 : L % 2 == 0 && at % 8 == 0 ? 2 : 1;
 }
-int width_shares(const KernelPlan &p, int widest, int L) {
-    const int t = tiles(widest, L, 1);
-    return std::min({p.n_posts, kWidthShares, std::max(8, (2 * kWidthGroups + t - 1) / t)});
+// Shares of the rows; with few labels and buckets the workgroups add up a
+// bucket's widths themselves.
+int tile_groups(int widest, int L, int V) {
+    const int N = many_labels(L) ? 1 : 8 / V;
+    return (tiles(widest, L, V) + N - 1) / N;
 }
+int width_shares(const KernelPlan &p, int widest, int L) {
+    const int t = tile_groups(widest, L, 1);
+    return std::min({p.n_posts, kWidthShares, std::max(8, (kWidthSumGroups + t - 1) / t)});
+}
+bool by_bucket(int L, int K) { return !many_labels(L) && K <= kFewBuckets; }
 
 template <int V, int P>
 void launch_width_v(const KernelPlan &p, int widest, int L, const float *table, const int32_t *bucket, int K,
                     const float *scores, float *out, hipStream_t stream) {
-    const int y = std::max(1, std::min(tiles(widest, L, V), kWidthGroups / p.n_posts));
-    hipLaunchKernelGGL((width_kernel<V, P>), dim3(p.n_posts, y), dim3(kWidthThreads), 0, stream, p.posts, p.post_cells,
-                       widest, L, K, table, bucket, scores, out);
+    constexpr int N = P == 64 ? 1 : 4 / V;
+    const int y = std::max(1, std::min((tiles(widest, L, V) + N - 1) / N, kWidthGroups / p.n_posts));
+    hipLaunchKernelGGL((width_kernel<V, P, N>), dim3(p.n_posts, y), dim3(kWidthThreads), 0, stream, p.posts, p.post_cells, L,
+                       K, table, bucket, scores, out);
 }
 template <int V, int P>
 void launch_width_bwd_v(const KernelPlan &p, int widest, int L, const float *grad, float *grad_scores, float *parts,
-                        hipStream_t stream) {
-    hipLaunchKernelGGL((width_bwd_kernel<V, P>), dim3(width_shares(p, widest, L), tiles(widest, L, V)), dim3(kWidthThreads),
-                       0, stream, p.posts, p.post_cells, p.n_posts, widest, L, grad, grad_scores, parts);
+                        const int32_t *bucket, int K, hipStream_t stream) {
+    constexpr int N = tiles_in_flight(V, P);
+    hipLaunchKernelGGL((width_bwd_kernel<V, P, N>), dim3(width_shares(p, widest, L), tile_groups(widest, L, V)),
+                       dim3(kWidthThreads), 0, stream, p.posts, p.post_cells, p.n_posts, widest, L, grad, bucket,
+                       by_bucket(L, K) ? K : 0, grad_scores, parts);
+}
+
+template <int J>
+void launch_join(const KernelPlan &p, int widest, int L, int V, const int32_t *bucket, int K, const float *parts,
+                 float *grad_table, hipStream_t stream) {
+    const bool own = by_bucket(L, K);
+    hipLaunchKernelGGL(width_join_kernel<J>, dim3(K, (L + J - 1) / J), dim3(kJoinThreads), 0, stream, parts,
+                       width_shares(p, widest, L) * (own ? tile_groups(widest, L, V) : 1), widest, L, bucket, own, grad_table);
 }
 
 }  // namespace
 
 int64_t width_bwd_bytes(const KernelPlan &p, int widest, int L) {
-    return ((int64_t)width_shares(p, widest, L) * widest * L * 4 + 255) / 256 * 256;
+    // (by width, or by bucket: at most kFewBuckets for each group of tiles of one label)
+    const int64_t rows = many_labels(L) ? widest : std::max(widest, kFewBuckets * tile_groups(widest, L, 1));
+    return ((int64_t)width_shares(p, widest, L) * rows * L * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_width(const KernelPlan &p, int widest, int L, const float *table, const int32_t *bucket, int K,
@@ -211,13 +339,12 @@ hipError_t launch_width_bwd(const KernelPlan &p, int widest, int L, const float 
     const int V = labels_each(L, grad, grad_scores);
     if (many_labels(L))
         (V == 4 ? launch_width_bwd_v<4, 64> : V == 2 ? launch_width_bwd_v<2, 64> : launch_width_bwd_v<1, 64>)(
-            p, widest, L, grad, grad_scores, parts, stream);
+            p, widest, L, grad, grad_scores, parts, bucket, K, stream);
     else
         (V == 4 ? launch_width_bwd_v<4, 16> : V == 2 ? launch_width_bwd_v<2, 16> : launch_width_bwd_v<1, 16>)(
-            p, widest, L, grad, grad_scores, parts, stream);
+            p, widest, L, grad, grad_scores, parts, bucket, K, stream);
     if (grad_table != nullptr)
-        hipLaunchKernelGGL(width_join_kernel, dim3(K, (L + kJoinLabels - 1) / kJoinLabels), dim3(kJoinLabels * kJoinLanes), 0,
-                           stream, parts, width_shares(p, widest, L), widest, L, bucket, grad_table);
+        (L == 1 ? launch_join<1> : L < 16 ? launch_join<4> : launch_join<16>)(p, widest, L, V, bucket, K, parts, grad_table, stream);
     return hipGetLastError();
 }
 
