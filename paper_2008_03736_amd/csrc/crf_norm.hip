@@ -25,13 +25,16 @@
 namespace crf {
 namespace {
 
-constexpr int kNormUnroll = 4;    // rows of a group of lanes in flight, forward
 // Most workgroups (of 256 threads) that sum dgamma and dbeta: four a CU (5,000
 // sentences of d = 500: 114 us at 768, 100.5, 106 at 2,048).
 constexpr int kNormGroups = 1024;
 
 __host__ __device__ constexpr int norm_threads(int G) { return G > 256 ? G : 256; }
 
+// Forward a group of lanes has one row in flight and one under way, in at most so
+// many workgroups of 256 threads (24 paragraphs of d = 8,192: 60 us with a chunk a
+// workgroup, 43 so; two rows at 4,096 workgroups 45).
+constexpr int kNormMost = 2048;
 // Rows of a group of lanes in flight, backward: the registers of two cost
 // wavefronts where rows are float32 or meet in LDS (24 paragraphs of d = 4,096 in
 // float32 69.7 us with two, 61.6 with one; 5,000 sentences of d = 500 100.5 and 104).
@@ -174,33 +177,63 @@ __device__ __forceinline__ const int32_t *chunk_ids(const int32_t *posts, int ch
     return posts + (size_t)(chunk / kChunks) * kPostRec + chunk % kChunks * kRows + threadIdx.x / G * U;
 }
 
+// Rows of a workgroup's chunks, the next chunk's on their way while one is worked
+// on, and the ids of the one after it.
+template <int G, int U>
+struct Ahead {
+    const int32_t *posts;
+    int chunks, id[U], id1[U], id2[U];
+    __device__ __forceinline__ void ids_of(int (&to)[U], int c) {
+        const int32_t *ids = chunk_ids<G, U>(posts, min(c, chunks - 1));
+#pragma unroll
+        for (int u = 0; u < U; ++u) to[u] = c < chunks ? ids[u] : -1;
+    }
+    __device__ __forceinline__ Ahead(const int32_t *posts, int chunks) : posts(posts), chunks(chunks) {
+        ids_of(id1, blockIdx.x);
+        ids_of(id2, blockIdx.x + gridDim.x);
+    }
+    // chunk c's rows are taken; then the next one's are loaded
+    __device__ __forceinline__ void take() {
+#pragma unroll
+        for (int u = 0; u < U; ++u) id[u] = id1[u], id1[u] = id2[u];
+    }
+};
+
 template <typename T, int G>
-__global__ __launch_bounds__(norm_threads(G)) void norm_kernel(const int32_t *__restrict__ posts, int d,
+__global__ __launch_bounds__(norm_threads(G)) void norm_kernel(const int32_t *__restrict__ posts, int chunks, int d,
                                                                const T *__restrict__ x, const float *__restrict__ gamma,
                                                                const float *__restrict__ beta, float eps,
                                                                uint16_t *__restrict__ y) {
-    constexpr int U = kNormUnroll;
+    constexpr int U = 1;
     __shared__ float slots[2][U * 16];
     const int k = 8 * (threadIdx.x & (G - 1));
-    const int32_t *ids = chunk_ids<G, U>(posts, blockIdx.x);
-    int id[U];
+    Ahead<G, U> rows(posts, chunks);
     Raw<T> raw[U];
+    auto load = [&]() {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        id[u] = ids[u];
-        if (id[u] >= 0) raw[u].load(x + (size_t)id[u] * d, k, d);
-    }
-    float g[8], b[8], f[U][8], r[U];
+        for (int u = 0; u < U; ++u) {
+            raw[u] = Raw<T>();
+            if (rows.id1[u] >= 0) raw[u].load(x + (size_t)rows.id1[u] * d, k, d);
+        }
+    };
+    load();
+    float g[8], b[8];
     weights(gamma, k, d, 1.f, g);
     weights(beta, k, d, 0.f, b);
+    for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+        float f[U][8], r[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u].widen(f[u]);
-    statistics<G, U>(f, r, k, d, eps, slots);
+        for (int u = 0; u < U; ++u) raw[u].widen(f[u]);
+        rows.take();
+        load();
+        rows.ids_of(rows.id2, c + 2 * gridDim.x);
+        statistics<G, U>(f, r, k, d, eps, slots);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) f[u][q] = fmaf(f[u][q] * r[u], g[q], b[q]);
-        if (id[u] >= 0) store(y + (size_t)id[u] * d, k, d, f[u]);
+            for (int q = 0; q < 8; ++q) f[u][q] = fmaf(f[u][q] * r[u], g[q], b[q]);
+            if (rows.id[u] >= 0) store(y + (size_t)rows.id[u] * d, k, d, f[u]);
+        }
     }
 }
 
@@ -222,41 +255,28 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(const int32_t
     weights(gamma, k, d, 1.f, g);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sg[q] = sb[q] = 0.f;
-    // the next chunk's rows are on their way while this one's are worked on, and
-    // the ids of the one after it
-    int id[U], id1[U], id2[U];
-    Raw<T> raw1[U];
-    Raw<uint16_t> up1[U];
-    auto ids_of = [&](int (&to)[U], int c) {
-        const int32_t *ids = chunk_ids<G, U>(posts, min(c, chunks - 1));
-#pragma unroll
-        for (int u = 0; u < U; ++u) to[u] = c < chunks ? ids[u] : -1;
-    };
+    Ahead<G, U> rows(posts, chunks);
+    Raw<T> raw[U];
+    Raw<uint16_t> up[U];
     auto load = [&]() {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            raw1[u] = Raw<T>();
-            up1[u] = Raw<uint16_t>();
-            if (id1[u] >= 0) {
-                raw1[u].load(x + (size_t)id1[u] * d, k, d);
-                up1[u].load(dy + (size_t)id1[u] * d, k, d);
+            raw[u] = Raw<T>();
+            up[u] = Raw<uint16_t>();
+            if (rows.id1[u] >= 0) {
+                raw[u].load(x + (size_t)rows.id1[u] * d, k, d);
+                up[u].load(dy + (size_t)rows.id1[u] * d, k, d);
             }
         }
     };
-    ids_of(id1, blockIdx.x);
-    ids_of(id2, blockIdx.x + gridDim.x);
     load();
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         float f[U][8], r[U], e[U][8], two[2 * U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            raw1[u].widen(f[u]);
-            up1[u].widen(e[u]);
-            id[u] = id1[u];
-            id1[u] = id2[u];
-        }
+        for (int u = 0; u < U; ++u) raw[u].widen(f[u]), up[u].widen(e[u]);
+        rows.take();
         load();
-        ids_of(id2, c + 2 * gridDim.x);
+        rows.ids_of(rows.id2, c + 2 * gridDim.x);
         statistics<G, U>(f, r, k, d, eps, slots);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -281,7 +301,7 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(const int32_t
             const float s = two[2 * u] * each, t = two[2 * u + 1] * each;
 #pragma unroll
             for (int q = 0; q < 8; ++q) f[u][q] = r[u] * (e[u][q] - s - f[u][q] * t);
-            if (dx != nullptr && id[u] >= 0) store(dx + (size_t)id[u] * d, k, d, f[u]);
+            if (dx != nullptr && rows.id[u] >= 0) store(dx + (size_t)rows.id[u] * d, k, d, f[u]);
         }
     }
     if constexpr (PARTS) {
@@ -348,8 +368,9 @@ int norm_parts(int chunks, int G) { return std::min(chunks, kNormGroups * 256 / 
 template <typename T, int G>
 void launch_norm_g(const KernelPlan &p, const void *x, int d, const float *gamma, const float *beta, float eps, uint16_t *y,
                    hipStream_t stream) {
-    hipLaunchKernelGGL((norm_kernel<T, G>), dim3(norm_chunks(p, G, kNormUnroll)), dim3(norm_threads(G)), 0, stream, p.posts,
-                       d, static_cast<const T *>(x), gamma, beta, eps, y);
+    const int chunks = norm_chunks(p, G, 1);
+    hipLaunchKernelGGL((norm_kernel<T, G>), dim3(std::min(chunks, kNormMost * 256 / norm_threads(G))), dim3(norm_threads(G)),
+                       0, stream, p.posts, chunks, d, static_cast<const T *>(x), gamma, beta, eps, y);
 }
 
 template <typename T, int G>
