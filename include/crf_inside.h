@@ -527,6 +527,15 @@ int crf_layer_norm_bwd(const crf_plan *plan, const void *x, int32_t x_type, int3
 int crf_width_bias(const crf_plan *plan, const float *scores, int32_t num_labels, const float *table,
                    const int32_t *buckets, int32_t num_buckets, float *out, void *stream);
 
+/*
+ * crf_biaffine_scores_biased -- crf_biaffine_scores and crf_width_bias in one:
+ * the same scores, the bias added to each (in float32) where it is written.
+ * scores must not overlap an input.
+ */
+int crf_biaffine_scores_biased(const crf_plan *plan, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int32_t d,
+                               int32_t ldw, int32_t num_labels, const float *table, const int32_t *buckets,
+                               int32_t num_buckets, float *scores, void *stream);
+
 /* crf_width_bias_bwd_workspace -- bytes of workspace of crf_width_bias_bwd. */
 int crf_width_bias_bwd_workspace(const crf_plan *plan, int32_t num_labels, int64_t *bytes);
 

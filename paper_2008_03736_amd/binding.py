@@ -61,6 +61,7 @@ SIGNATURES = {
     "crf_layer_norm_bwd_workspace": (ctypes.c_int, [_P, _I32, ctypes.POINTER(_I64)]),
     "crf_layer_norm_bwd": (ctypes.c_int, [_P, _P, _I32, _I32, _P, _P, _F32, _P, _P, _P, _P, _I64, _P]),
     "crf_width_bias": (ctypes.c_int, [_P, _P, _I32, _P, _P, _I32, _P, _P]),
+    "crf_biaffine_scores_biased": (ctypes.c_int, [_P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _I32, _P, _P]),
     "crf_width_bias_bwd_workspace": (ctypes.c_int, [_P, _I32, ctypes.POINTER(_I64)]),
     "crf_width_bias_bwd": (ctypes.c_int, [_P, _P, _I32, _P, _I32, _P, _P, _P, _I64, _P]),
     "crf_orthogonalize_workspace": (ctypes.c_int, [_I32, _I32, _I32, ctypes.POINTER(_I64)]),
@@ -260,6 +261,11 @@ def crf_layer_norm_bwd(plan, x, x_type, d, gamma, grad_y, eps, grad_x, grad_gamm
 
 def crf_width_bias(plan, scores, num_labels, table, buckets, num_buckets, out, stream):
     _check(load().crf_width_bias(plan, scores, num_labels, table, buckets, num_buckets, out, stream), "crf_width_bias")
+
+
+def crf_biaffine_scores_biased(plan, rl, rr, w, d, ldw, num_labels, table, buckets, num_buckets, scores, stream):
+    _check(load().crf_biaffine_scores_biased(plan, rl, rr, w, d, ldw, num_labels, table, buckets, num_buckets, scores,
+                                             stream), "crf_biaffine_scores_biased")
 
 
 def crf_width_bias_bwd_workspace(plan, num_labels):
@@ -530,12 +536,13 @@ class Plan:
                         labels.data_ptr(), _stream_ptr(t, self.device))
         return labels
 
-    def biaffine_scores(self, rl, rr, w, scores=None):
+    def biaffine_scores(self, rl, rr, w, scores=None, table=None, buckets=None):
         """Span (or label) scores from boundary representations (Sec. 2.2,
         Eq. biaffine).  rl, rr: bf16 bit patterns as int16/uint16 tensors
         [B, N1, d]; w: [L, d, ldw] (W transposed, bias at index d).  Returns
         float32 [B, N1, N1] (L = 1) or [B, N1, N1, L]; a fresh buffer is
-        NaN-filled, and only valid cells are written."""
+        NaN-filled, and only valid cells are written.  With table and buckets
+        (width_bias) the bias is added as the scores are written."""
         t = self._torch
         if rl.dim() != 3 or tuple(rl.shape[:2]) != (self.B, self.n1) or tuple(rr.shape) != tuple(rl.shape):
             raise ValueError(f"rl and rr must be [{self.B}, {self.n1}, d]")
@@ -551,6 +558,17 @@ class Plan:
             scores = t.full(shape, float("nan"), dtype=t.float32, device=self.device)
         elif tuple(scores.shape) != shape or scores.dtype != t.float32 or not scores.is_contiguous():
             raise ValueError(f"scores must be contiguous float32 {shape}")
+        if (table is None) != (buckets is None):
+            raise ValueError("table and buckets go together")
+        if table is not None:
+            if table.dim() != 2 or int(table.shape[1]) != L:
+                raise ValueError(f"table must be [K, {L}]")
+            K = int(table.shape[0])
+            bias = (self._tensor(table, "table", (K, L), (t.float32,)), self._tensor(buckets, "buckets", (self.n1,), (t.int32,)))
+            self._rewritten(scores)
+            crf_biaffine_scores_biased(self._handle, rl.data_ptr(), rr.data_ptr(), w.data_ptr(), d, int(w.shape[2]), L, *bias,
+                                       K, self._tensor(scores, "scores", shape, (t.float32,)), _stream_ptr(t, self.device))
+            return scores
         self._rewritten(scores)
         crf_biaffine_scores(self._handle, rl.data_ptr(), rr.data_ptr(), w.data_ptr(), d, int(w.shape[2]), L,
                             scores.data_ptr(), _stream_ptr(t, self.device))
@@ -886,14 +904,15 @@ def policy_loss(scores, trees, advantages, old_logp, plan, ref_logp=None, counts
     return _Policy.apply(scores)
 
 
-def biaffine(rl, rr, w, plan, held="bf16"):
+def biaffine(rl, rr, w, plan, held="bf16", table=None, buckets=None):
     """Differentiable span (or label) scores from boundary representations
     (Sec. 2.2, Eq. biaffine): rl, rr bfloat16 [B, N1, d], w bfloat16 or float32
     [L, d, ldw]; cells that are no spans are 0.  A float32 w enters the products
     rounded to bfloat16 and gets its gradient in float32, as it is computed; a
     bfloat16 one gets it rounded.  held="8bit": the backward pass keeps the
     representations in 8 bits (Plan.pack_rows) and gives the gradients at the
-    values those stand for."""
+    values those stand for.  table float32 [K, L] and buckets (width_bias): a
+    bias by the spans' widths, added as the scores are written, with its gradient."""
     import torch
 
     if held not in ("bf16", "8bit"):
@@ -902,36 +921,44 @@ def biaffine(rl, rr, w, plan, held="bf16"):
     for x, name, types in ((rl, "rl", bf16), (rr, "rr", bf16), (w, "w", (*bf16, torch.float32))):
         if x.dtype not in types:
             raise ValueError(f"{name} must be bfloat16 (or its bit patterns; w also float32), got {x.dtype}")
+    if (table is None) != (buckets is None):
+        raise ValueError("table and buckets go together")
     differentiable = torch.is_grad_enabled() and any(x.requires_grad for x in (rl, rr, w))
+    bias = dict(table=table, buckets=buckets) if table is not None else {}
 
     class _Biaffine(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, rl, rr, w):
+        def forward(ctx, rl, rr, w, table):
             L = w.shape[0]
             ctx.w_type = w.dtype
             if w.dtype == torch.float32:
                 w = w.to(torch.bfloat16)
             shape = (plan.B, plan.n1, plan.n1) if L == 1 else (plan.B, plan.n1, plan.n1, L)
             scores = torch.zeros(shape, dtype=torch.float32, device=rl.device)
-            plan.biaffine_scores(rl.view(torch.int16), rr.view(torch.int16), w.view(torch.int16), scores=scores)
+            plan.biaffine_scores(rl.view(torch.int16), rr.view(torch.int16), w.view(torch.int16), scores=scores, **bias)
+            kept = ()
             if differentiable:
-                kept = (*plan.pack_rows(rl), *plan.pack_rows(rr)) if held == "8bit" else (rl, rr)
-                ctx.save_for_backward(w, *kept)
+                kept = (w, *plan.pack_rows(rl), *plan.pack_rows(rr)) if held == "8bit" else (w, rl, rr)
+            ctx.count = None if table is None else table.shape[0]
+            ctx.save_for_backward(buckets, *kept)
             return scores
 
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, g):
-            w, *kept = ctx.saved_tensors
-            rl, rr = (kept[:2], kept[2:]) if held == "8bit" else kept
+            buckets, *kept = ctx.saved_tensors
             g = g.float().contiguous()   # held by this frame until the call has been enqueued
             need = ctx.needs_input_grad
-            if not any(need):
-                return None, None, None
-            grad_rl, grad_rr, grad_w = plan.biaffine_bwd(rl, rr, w, g, need=need)
-            return grad_rl, grad_rr, None if grad_w is None else grad_w.to(ctx.w_type)
+            grad_rl = grad_rr = grad_w = grad_table = None
+            if any(need[:3]):
+                w, *kept = kept
+                rl, rr = (kept[:2], kept[2:]) if held == "8bit" else kept
+                grad_rl, grad_rr, grad_w = plan.biaffine_bwd(rl, rr, w, g, need=need[:3])
+            if need[3]:
+                grad_table = plan.width_bias_bwd(g, buckets, ctx.count, need=(False, True))[1]
+            return grad_rl, grad_rr, None if grad_w is None else grad_w.to(ctx.w_type), grad_table
 
-    return _Biaffine.apply(rl, rr, w)
+    return _Biaffine.apply(rl, rr, w, table)
 
 
 def layer_norm(x, plan, gamma=None, beta=None, eps=1e-5):

@@ -97,6 +97,25 @@ __device__ __forceinline__ uint32_t keep_word(int k, int d) {
     return (k <= d ? 0x0000FFFFu : 0u) | (k + 1 <= d ? 0xFFFF0000u : 0u);
 }
 
+// A bias by a span's width on the scores (crf_width.hip), added where they are
+// written: table NULL, or the bias of width w and label l at table[bucket[w] L + l]
+// (none where the bucket is outside 0 .. K - 1).  A tile's rows and columns are
+// neighbours in a sentence, or the same packed ones: their widths lie in a window
+// of 127 from `base` on, whose biases wait in LDS.
+struct WidthBias {
+    const float *table;
+    const int32_t *bucket;
+    int K;
+};
+constexpr int kWindow = 128;
+__device__ __forceinline__ int window_base(const int32_t *rec, int N1) {
+    return rec[kBiaRows] % N1 - rec[0] % N1 - (kBiaRows - 1);
+}
+__device__ __forceinline__ int window_bucket(const WidthBias &bias, int w, int N1) {
+    const int k = w >= 1 && w < N1 ? bias.bucket[w] : -1;
+    return k < bias.K ? k : -1;
+}
+
 // Tile record: kBiaRows row ids then kBiaCols column ids, each b * N1 + i
 // (sentence b, fence post i) or -1.  KS = K / 32 steps of the first product
 // (K = d + 1 padded to 256 or 512); each wavefront takes KS / 4 of them.
@@ -105,7 +124,7 @@ template <int KS, int P, bool ONE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void biaffine_kernel(
     const int32_t *__restrict__ tiles, const int32_t *__restrict__ len, int N1, int d, int ldw, int L, int n_work,
     int groups, int per_group, const uint16_t *__restrict__ rl, const uint16_t *__restrict__ rr, const uint16_t *__restrict__ w,
-    float *__restrict__ scores) {
+    WidthBias bias, float *__restrict__ scores) {
     static_assert(KS % 4 == 0, "K splits four ways");
     constexpr int KQ = KS / 4;               // steps of this wavefront's quarter of K
     extern __shared__ __align__(16) char smem_raw[];
@@ -118,6 +137,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     int32_t *Ob = reinterpret_cast<int32_t *>(Ul + kBiaRows * kUStride);   // [kBiaRows + kBiaCols]
     int32_t *Oi = Ob + kBiaRows + kBiaCols;                                // [kBiaRows + kBiaCols]
     int32_t *On = Oi + kBiaRows + kBiaCols;                                // [kBiaRows]
+    float *Wb = reinterpret_cast<float *>(On + kBiaRows);                  // [2][kWindow], with a bias
     // Workgroup b runs on XCD b mod 8 (dealt in turn); each XCD takes a
     // contiguous share of the work, a tile's label groups side by side: a
     // cell's labels are neighbours in memory, and lines written by several
@@ -205,8 +225,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (tid < kBiaRows) On[tid] = len[b >= 0 ? b : 0];
     }
 
+    const int base = bias.table != nullptr ? window_base(rec, N1) : 0;
+    const int my_bucket = bias.table != nullptr && tid < kWindow ? window_bucket(bias, base + tid, N1) : -1;
+
     // A label at a time: the tile's rows stay in registers.
     for (int l = l0; ONE ? l == l0 : l < l1; ++l) {
+    // (two windows in turn: wavefronts may still read the last label's)
+    float *window = Wb + ((l - l0) & 1) * kWindow;
+    if (bias.table != nullptr && tid < kWindow) window[tid] = my_bucket >= 0 ? bias.table[(size_t)my_bucket * L + l] : 0.f;
     if (!ONE && l > l0) {
         wl += (size_t)d * ldw;
         load_wq<KQ, P>(wf, wl, 0, d, ldw, kq0, lane);
@@ -313,7 +339,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
         for (int c = 0; c < kBiaCols / 16; ++c) {
             const int q = kBiaRows + 16 * c + (lane & 15), j = Oi[q];
-            if (b == Ob[q] && i < j && j <= n) scores[(((size_t)b * N1 + i) * N1 + j) * L + l] = acc[c][t];
+            if (b == Ob[q] && i < j && j <= n) {
+                float v = acc[c][t];
+                if (bias.table != nullptr) v += window[j - i - base];
+                scores[(((size_t)b * N1 + i) * N1 + j) * L + l] = v;
+            }
         }
     }
     }
@@ -341,7 +371,7 @@ template <int P>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void biaffine_small_kernel(
     const int32_t *__restrict__ tiles, const int32_t *__restrict__ len, int N1, int d, int ldw, int L, int n_work,
     int groups, int per_group, const uint16_t *__restrict__ rl, const uint16_t *__restrict__ rr,
-    const uint16_t *__restrict__ w, float *__restrict__ scores) {
+    const uint16_t *__restrict__ w, WidthBias bias, float *__restrict__ scores) {
     constexpr int KS = 4, kPieces = 128 * 128 / 8 / 256;   // steps of K; pieces of W a thread stages
     extern __shared__ __align__(16) char smem_raw[];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rows = small_rows(d);
@@ -351,6 +381,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     uint16_t *Ul = Uh + 16 * kUStride;                                    // and lo
     int32_t *Ob = reinterpret_cast<int32_t *>(Rs + kBiaCols * kWStride + 2 * kBiaRows * kUStride);
     int32_t *Oi = Ob + kBiaRows + kBiaCols, *On = Oi + kBiaRows + kBiaCols;
+    float *Wb = reinterpret_cast<float *>(On + kBiaRows);   // [kWindow], with a bias
     const int per_xcd = (n_work + 7) >> 3;   // (the work's order: see biaffine_kernel)
     const int work = groups > 1 ? ((int)blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
     if (work >= n_work) return;
@@ -425,8 +456,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (tid < kBiaRows) On[tid] = len[b >= 0 ? b : 0];
     }
 
+    const int base = bias.table != nullptr ? window_base(rec, N1) : 0;
+    const int my_bucket = bias.table != nullptr && tid < kWindow ? window_bucket(bias, base + tid, N1) : -1;
+    float my_bias = 0.f;   // of the label to come
+    auto load_bias = [&](int l) {
+        if (my_bucket >= 0) my_bias = bias.table[(size_t)my_bucket * L + l];
+    };
+    load_bias(l0);
+
     for (int l = l0; l < l1; ++l) {
-        __syncthreads();   // the last label's readers of Ws are done
+        __syncthreads();   // the last label's readers of Ws and Wb are done
+        if (bias.table != nullptr && tid < kWindow) Wb[tid] = my_bias;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int q = tid + 256 * i, k = 8 * (q & 15);
@@ -435,7 +475,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     make_uint4(wr[i].x & keep_word(k, d), wr[i].y & keep_word(k + 2, d), wr[i].z & keep_word(k + 4, d),
                                wr[i].w & keep_word(k + 6, d));
         }
-        if (l + 1 < l1) load_w(l + 1);
+        if (l + 1 < l1) {
+            load_w(l + 1);
+            load_bias(l + 1);
+        }
         __syncthreads();
 
         f32x4 acc[kBiaCols / 16];   // S rows 16 wave + 4 (lane/16) + t, columns 16 c + lane%16
@@ -479,7 +522,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
             for (int c = 0; c < kBiaCols / 16; ++c) {
                 const int q = kBiaRows + 16 * c + (lane & 15), j = Oi[q];
-                if (b == Ob[q] && i < j && j <= n) scores[(((size_t)b * N1 + i) * N1 + j) * L + l] = acc[c][t];
+                if (b == Ob[q] && i < j && j <= n) {
+                    float v = acc[c][t];
+                    if (bias.table != nullptr) v += Wb[j - i - base];
+                    scores[(((size_t)b * N1 + i) * N1 + j) * L + l] = v;
+                }
             }
         }
     }
@@ -493,12 +540,14 @@ hipError_t set_biaffine_attributes() {
                          (const void *)biaffine_kernel<8, 4, true>, (const void *)biaffine_kernel<16, 4, true>,
                          (const void *)biaffine_kernel<8, 8, true>, (const void *)biaffine_kernel<16, 8, true>};
     for (const void *f : fns) {
-        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)biaffine_lds_bytes(kBiaMaxD));
+        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)biaffine_lds_bytes(kBiaMaxD) + 8 * kWindow);
         if (e != hipSuccess) return e;
     }
     const void *small[] = {(const void *)biaffine_small_kernel<4>, (const void *)biaffine_small_kernel<8>};
     for (const void *f : small) {
-        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)small_lds_bytes(kBiaSmallD));
+        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)small_lds_bytes(kBiaSmallD) + 8 * kWindow);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -512,25 +561,26 @@ int64_t biaffine_lds_bytes(int) {
 template <int P>
 static void launch_biaffine_p(const KernelPlan &p, int n_work, int groups, int per_group, bool one, size_t lds,
                               hipStream_t stream, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
-                              int ldw, int L, float *scores) {
+                              int ldw, int L, const WidthBias &bias, float *scores) {
+    const size_t extra = bias.table != nullptr ? 2 * kWindow * sizeof(float) : 0;
     const dim3 grid(groups > 1 ? (n_work + 7) / 8 * 8 : n_work), block(256);
     const int kp = bia_kp(d);
     // K in one wavefront's registers and W in LDS, or K split over four (98.4
     // and 76.6 us at d = 100)
     if (d <= kBiaSmallD)
-        hipLaunchKernelGGL((biaffine_small_kernel<P>), grid, block, (size_t)small_lds_bytes(d), stream, p.bia_tiles, p.len,
-                           p.n1, d, ldw, L, n_work, groups, per_group, rl, rr, w, scores);
+        hipLaunchKernelGGL((biaffine_small_kernel<P>), grid, block, (size_t)small_lds_bytes(d) + extra, stream, p.bia_tiles, p.len,
+                           p.n1, d, ldw, L, n_work, groups, per_group, rl, rr, w, bias, scores);
     else if (one)
         hipLaunchKernelGGL((kp == 256 ? biaffine_kernel<8, P, true> : biaffine_kernel<16, P, true>),
-                           dim3(p.n_bia_tiles, L), block, lds, stream, p.bia_tiles, p.len, p.n1, d, ldw, L, n_work, groups,
-                           per_group, rl, rr, w, scores);
+                           dim3(p.n_bia_tiles, L), block, lds + extra, stream, p.bia_tiles, p.len, p.n1, d, ldw, L, n_work, groups,
+                           per_group, rl, rr, w, bias, scores);
     else
-        hipLaunchKernelGGL((kp == 256 ? biaffine_kernel<8, P, false> : biaffine_kernel<16, P, false>), grid, block, lds,
-                           stream, p.bia_tiles, p.len, p.n1, d, ldw, L, n_work, groups, per_group, rl, rr, w, scores);
+        hipLaunchKernelGGL((kp == 256 ? biaffine_kernel<8, P, false> : biaffine_kernel<16, P, false>), grid, block, lds + extra,
+                           stream, p.bia_tiles, p.len, p.n1, d, ldw, L, n_work, groups, per_group, rl, rr, w, bias, scores);
 }
 
-hipError_t launch_biaffine(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
-                           int ldw, int L, float *scores, hipStream_t stream) {
+static hipError_t launch_scorer(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
+                                int ldw, int L, const WidthBias &bias, float *scores, hipStream_t stream) {
     if (p.n_bia_tiles < 1) return hipSuccess;
     const size_t lds = (size_t)biaffine_lds_bytes(d);
     // Labels per workgroup: enough workgroups for a few per CU slot first (two
@@ -552,10 +602,21 @@ hipError_t launch_biaffine(const KernelPlan &p, const uint16_t *rl, const uint16
     const bool one = per_group == 1 && (L == 1 || (p.n_bia_tiles <= 32 && (all <= 64 || all > 1024)));
     // 16-byte W pieces when every row starts 16-byte aligned
     if (ldw % 8 == 0 && ((uintptr_t)w & 15) == 0)
-        launch_biaffine_p<8>(p, n_work, groups, per_group, one, lds, stream, rl, rr, w, d, ldw, L, scores);
+        launch_biaffine_p<8>(p, n_work, groups, per_group, one, lds, stream, rl, rr, w, d, ldw, L, bias, scores);
     else
-        launch_biaffine_p<4>(p, n_work, groups, per_group, one, lds, stream, rl, rr, w, d, ldw, L, scores);
+        launch_biaffine_p<4>(p, n_work, groups, per_group, one, lds, stream, rl, rr, w, d, ldw, L, bias, scores);
     return hipGetLastError();
+}
+
+hipError_t launch_biaffine(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
+                           int ldw, int L, float *scores, hipStream_t stream) {
+    return launch_scorer(p, rl, rr, w, d, ldw, L, WidthBias{nullptr, nullptr, 0}, scores, stream);
+}
+
+hipError_t launch_biaffine_biased(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
+                                  int ldw, int L, const float *table, const int32_t *bucket, int K, float *scores,
+                                  hipStream_t stream) {
+    return launch_scorer(p, rl, rr, w, d, ldw, L, WidthBias{table, bucket, K}, scores, stream);
 }
 
 }  // namespace crf

@@ -658,6 +658,10 @@ int64_t biaffine_lds_bytes(int d);
 hipError_t set_biaffine_attributes();   // once per plan: the LDS of the largest d
 hipError_t launch_biaffine(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
                            int ldw, int L, float *scores, hipStream_t stream);
+// The same with a bias by width (table [K][L], bucket [N1]) added.
+hipError_t launch_biaffine_biased(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
+                                  int ldw, int L, const float *table, const int32_t *bucket, int K, float *scores,
+                                  hipStream_t stream);
 // Log-probabilities of given trees and the clipped policy loss (crf_trees.hip):
 // the inside sweep, then a pass over the trees.  z64: [B] of workspace.
 hipError_t launch_tree_logprobs(const KernelPlan &p, const float *scores, const int32_t *trees, int G,

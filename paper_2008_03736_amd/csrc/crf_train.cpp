@@ -414,6 +414,28 @@ int crf_width_bias(const crf_plan *plan, const float *scores, int32_t num_labels
     return e == hipSuccess ? ok() : hip_fail(e, "crf_width_bias launch");
 }
 
+int crf_biaffine_scores_biased(const crf_plan *plan, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int32_t d,
+                               int32_t ldw, int32_t num_labels, const float *table, const int32_t *buckets,
+                               int32_t num_buckets, float *scores, void *stream) {
+    if (plan == nullptr) return fail(CRF_EINVAL, "plan is NULL");
+    if (rl == nullptr || rr == nullptr || w == nullptr || table == nullptr || buckets == nullptr || scores == nullptr)
+        return fail(CRF_EINVAL, "rl/rr/w/table/buckets/scores is NULL");
+    int rc = check_scorer(d, ldw, num_labels);
+    if (rc != CRF_OK || (rc = check_buckets(num_buckets, num_labels)) != CRF_OK) return rc;
+    if (misaligned(rl, 8) || misaligned(rr, 8) || misaligned(w, 8))
+        return fail(CRF_EINVAL, "rl/rr/w must be 8-byte aligned");
+    const int64_t rows = rows_bytes(plan, 2, d);
+    if ((rc = check_overlap({{"scores", scores, scores_bytes(plan, num_labels)}},
+                            {{"rl", rl, rows}, {"rr", rr, rows}, {"w", w, 2 * (int64_t)num_labels * d * ldw},
+                             {"table", table, 4 * (int64_t)num_buckets * num_labels},
+                             {"buckets", buckets, 4 * (int64_t)plan->n1}})) != CRF_OK ||
+        (rc = check_device(plan)) != CRF_OK)
+        return rc;
+    const hipError_t e = crf::launch_biaffine_biased(plan->kp, rl, rr, w, d, ldw, num_labels, table, buckets, num_buckets,
+                                                     scores, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? ok() : hip_fail(e, "crf_biaffine_scores_biased launch");
+}
+
 int crf_width_bias_bwd_workspace(const crf_plan *plan, int32_t num_labels, int64_t *bytes) {
     if (plan == nullptr || bytes == nullptr) return fail(CRF_EINVAL, "NULL argument");
     const int rc = check_buckets(1, num_labels);

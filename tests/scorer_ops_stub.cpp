@@ -32,6 +32,7 @@ int op_aliases(void *lib) {
     ENTRY(crf_plan_create); ENTRY(crf_plan_destroy); ENTRY(crf_layer_norm); ENTRY(crf_layer_norm_bwd);
     ENTRY(crf_layer_norm_bwd_workspace); ENTRY(crf_width_bias); ENTRY(crf_width_bias_bwd);
     ENTRY(crf_width_bias_bwd_workspace); ENTRY(crf_orthogonalize); ENTRY(crf_orthogonalize_workspace); ENTRY(crf_muon_step);
+    ENTRY(crf_biaffine_scores_biased);
     const int32_t len[kB] = {8, 3, 5};
     constexpr int64_t rows = (int64_t)kB * kN1 * kD, vec = 4 * kD, K = 5, L = 3;
     crf_plan *p = nullptr;
@@ -64,6 +65,13 @@ int op_aliases(void *lib) {
           [&](const std::vector<Buffer> &b) {
               return crf_width_bias_bwd(p, as<float>(b[0]), (int)L, as<int32_t>(b[1]), (int)K, as<float>(b[2]), as<float>(b[3]),
                                         b[4].at, ww, nullptr);
+          });
+    pairs("scorer",
+          {{"rl", kBf16, false}, {"rr", kBf16, false}, {"w", kW, false}, {"table", 4 * K, false}, {"buckets", 4 * kN1, false},
+           {"scores", kScores, true}},
+          [&](const std::vector<Buffer> &b) {
+              return crf_biaffine_scores_biased(p, as<uint16_t>(b[0]), as<uint16_t>(b[1]), as<uint16_t>(b[2]), kD, kLdw, 1,
+                                                as<float>(b[3]), as<int32_t>(b[4]), (int)K, as<float>(b[5]), nullptr);
           });
     constexpr int64_t all = 4 * 2 * 20 * 32;
     pairs("ortho", {{"x", all, false}, {"out", all, true}, {"workspace", ow, true}}, [&](const std::vector<Buffer> &b) {

@@ -42,6 +42,7 @@ def test_null_arguments(lib):
     assert lib.crf_width_bias(None, P, 1, Q, R, 4, S, None) == B.CRF_EINVAL
     assert lib.crf_width_bias_bwd_workspace(None, 1, ctypes.byref(n)) == B.CRF_EINVAL
     assert lib.crf_width_bias_bwd(None, P, 1, R, 4, None, S, T, 1 << 20, None) == B.CRF_EINVAL
+    assert lib.crf_biaffine_scores_biased(None, P, Q, R, 8, 12, 1, S, T, 4, P, None) == B.CRF_EINVAL
     assert "plan" in B.crf_last_error()
     _, co, k = steps((1.5, -0.5, 0.0))
     assert lib.crf_orthogonalize(None, 1, 8, 8, 8, co, k, 1e-7, Q, R, 1 << 30, None) == B.CRF_EINVAL
