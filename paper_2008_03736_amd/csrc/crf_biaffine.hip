@@ -120,7 +120,7 @@ __device__ __forceinline__ int window_bucket(const WidthBias &bias, int w, int N
 // (sentence b, fence post i) or -1.  KS = K / 32 steps of the first product
 // (K = d + 1 padded to 256 or 512); each wavefront takes KS / 4 of them.
 constexpr int kRAhead = 3;   // chunks of r^r in flight
-template <int KS, int P, bool ONE>
+template <int KS, int P, bool ONE, bool BIASED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void biaffine_kernel(
     const int32_t *__restrict__ tiles, const int32_t *__restrict__ len, int N1, int d, int ldw, int L, int n_work,
     int groups, int per_group, const uint16_t *__restrict__ rl, const uint16_t *__restrict__ rr, const uint16_t *__restrict__ w,
@@ -225,14 +225,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (tid < kBiaRows) On[tid] = len[b >= 0 ? b : 0];
     }
 
-    const int base = bias.table != nullptr ? window_base(rec, N1) : 0;
-    const int my_bucket = bias.table != nullptr && tid < kWindow ? window_bucket(bias, base + tid, N1) : -1;
+    int base = 0, my_bucket = -1;
+    if constexpr (BIASED) {
+        base = window_base(rec, N1);
+        if (tid < kWindow) my_bucket = window_bucket(bias, base + tid, N1);
+    }
 
     // A label at a time: the tile's rows stay in registers.
     for (int l = l0; ONE ? l == l0 : l < l1; ++l) {
     // (two windows in turn: wavefronts may still read the last label's)
     float *window = Wb + ((l - l0) & 1) * kWindow;
-    if (bias.table != nullptr && tid < kWindow) window[tid] = my_bucket >= 0 ? bias.table[(size_t)my_bucket * L + l] : 0.f;
+    if constexpr (BIASED) {
+        if (tid < kWindow) window[tid] = my_bucket >= 0 ? bias.table[(size_t)my_bucket * L + l] : 0.f;
+    }
     if (!ONE && l > l0) {
         wl += (size_t)d * ldw;
         load_wq<KQ, P>(wf, wl, 0, d, ldw, kq0, lane);
@@ -341,7 +346,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             const int q = kBiaRows + 16 * c + (lane & 15), j = Oi[q];
             if (b == Ob[q] && i < j && j <= n) {
                 float v = acc[c][t];
-                if (bias.table != nullptr) v += window[j - i - base];
+                if constexpr (BIASED) v += window[j - i - base];
                 scores[(((size_t)b * N1 + i) * N1 + j) * L + l] = v;
             }
         }
@@ -367,7 +372,7 @@ inline int64_t small_lds_bytes(int d) {
            4 * (2 * (kBiaRows + kBiaCols) + kBiaRows);
 }
 
-template <int P>
+template <int P, bool BIASED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void biaffine_small_kernel(
     const int32_t *__restrict__ tiles, const int32_t *__restrict__ len, int N1, int d, int ldw, int L, int n_work,
     int groups, int per_group, const uint16_t *__restrict__ rl, const uint16_t *__restrict__ rr,
@@ -456,17 +461,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if (tid < kBiaRows) On[tid] = len[b >= 0 ? b : 0];
     }
 
-    const int base = bias.table != nullptr ? window_base(rec, N1) : 0;
-    const int my_bucket = bias.table != nullptr && tid < kWindow ? window_bucket(bias, base + tid, N1) : -1;
+    int base = 0, my_bucket = -1;
+    if constexpr (BIASED) {
+        base = window_base(rec, N1);
+        if (tid < kWindow) my_bucket = window_bucket(bias, base + tid, N1);
+    }
     float my_bias = 0.f;   // of the label to come
     auto load_bias = [&](int l) {
-        if (my_bucket >= 0) my_bias = bias.table[(size_t)my_bucket * L + l];
+        if constexpr (BIASED) {
+            if (my_bucket >= 0) my_bias = bias.table[(size_t)my_bucket * L + l];
+        }
     };
     load_bias(l0);
 
     for (int l = l0; l < l1; ++l) {
         __syncthreads();   // the last label's readers of Ws and Wb are done
-        if (bias.table != nullptr && tid < kWindow) Wb[tid] = my_bias;
+        if constexpr (BIASED) {
+            if (tid < kWindow) Wb[tid] = my_bias;
+        }
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int q = tid + 256 * i, k = 8 * (q & 15);
@@ -524,7 +536,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 const int q = kBiaRows + 16 * c + (lane & 15), j = Oi[q];
                 if (b == Ob[q] && i < j && j <= n) {
                     float v = acc[c][t];
-                    if (bias.table != nullptr) v += Wb[j - i - base];
+                    if constexpr (BIASED) v += Wb[j - i - base];
                     scores[(((size_t)b * N1 + i) * N1 + j) * L + l] = v;
                 }
             }
@@ -532,22 +544,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
 }
 
+template <int P, bool BIASED>
+hipError_t scorer_attributes() {
+    const int extra = BIASED ? 2 * kWindow * (int)sizeof(float) : 0;
+    for (const void *f : {(const void *)biaffine_kernel<8, P, false, BIASED>, (const void *)biaffine_kernel<16, P, false, BIASED>,
+                          (const void *)biaffine_kernel<8, P, true, BIASED>, (const void *)biaffine_kernel<16, P, true, BIASED>}) {
+        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)biaffine_lds_bytes(kBiaMaxD) + extra);
+        if (e != hipSuccess) return e;
+    }
+    return hipFuncSetAttribute((const void *)biaffine_small_kernel<P, BIASED>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                               (int)small_lds_bytes(kBiaSmallD) + extra);
+}
+
 }  // namespace
 
 hipError_t set_biaffine_attributes() {
-    const void *fns[] = {(const void *)biaffine_kernel<8, 4, false>, (const void *)biaffine_kernel<16, 4, false>,
-                         (const void *)biaffine_kernel<8, 8, false>, (const void *)biaffine_kernel<16, 8, false>,
-                         (const void *)biaffine_kernel<8, 4, true>, (const void *)biaffine_kernel<16, 4, true>,
-                         (const void *)biaffine_kernel<8, 8, true>, (const void *)biaffine_kernel<16, 8, true>};
-    for (const void *f : fns) {
-        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)biaffine_lds_bytes(kBiaMaxD) + 8 * kWindow);
-        if (e != hipSuccess) return e;
-    }
-    const void *small[] = {(const void *)biaffine_small_kernel<4>, (const void *)biaffine_small_kernel<8>};
-    for (const void *f : small) {
-        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)small_lds_bytes(kBiaSmallD) + 8 * kWindow);
+    for (auto set : {scorer_attributes<4, false>, scorer_attributes<8, false>, scorer_attributes<4, true>, scorer_attributes<8, true>}) {
+        const hipError_t e = set();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -558,24 +572,24 @@ int64_t biaffine_lds_bytes(int) {
            4 * (2 * (kBiaRows + kBiaCols) + kBiaRows);
 }
 
-template <int P>
+template <int P, bool BIASED>
 static void launch_biaffine_p(const KernelPlan &p, int n_work, int groups, int per_group, bool one, size_t lds,
                               hipStream_t stream, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
                               int ldw, int L, const WidthBias &bias, float *scores) {
-    const size_t extra = bias.table != nullptr ? 2 * kWindow * sizeof(float) : 0;
+    const size_t extra = BIASED ? 2 * kWindow * sizeof(float) : 0;
     const dim3 grid(groups > 1 ? (n_work + 7) / 8 * 8 : n_work), block(256);
     const int kp = bia_kp(d);
     // K in one wavefront's registers and W in LDS, or K split over four (98.4
     // and 76.6 us at d = 100)
     if (d <= kBiaSmallD)
-        hipLaunchKernelGGL((biaffine_small_kernel<P>), grid, block, (size_t)small_lds_bytes(d) + extra, stream, p.bia_tiles, p.len,
+        hipLaunchKernelGGL((biaffine_small_kernel<P, BIASED>), grid, block, (size_t)small_lds_bytes(d) + extra, stream, p.bia_tiles, p.len,
                            p.n1, d, ldw, L, n_work, groups, per_group, rl, rr, w, bias, scores);
     else if (one)
-        hipLaunchKernelGGL((kp == 256 ? biaffine_kernel<8, P, true> : biaffine_kernel<16, P, true>),
+        hipLaunchKernelGGL((kp == 256 ? biaffine_kernel<8, P, true, BIASED> : biaffine_kernel<16, P, true, BIASED>),
                            dim3(p.n_bia_tiles, L), block, lds + extra, stream, p.bia_tiles, p.len, p.n1, d, ldw, L, n_work, groups,
                            per_group, rl, rr, w, bias, scores);
     else
-        hipLaunchKernelGGL((kp == 256 ? biaffine_kernel<8, P, false> : biaffine_kernel<16, P, false>), grid, block, lds + extra,
+        hipLaunchKernelGGL((kp == 256 ? biaffine_kernel<8, P, false, BIASED> : biaffine_kernel<16, P, false, BIASED>), grid, block, lds + extra,
                            stream, p.bia_tiles, p.len, p.n1, d, ldw, L, n_work, groups, per_group, rl, rr, w, bias, scores);
 }
 
@@ -601,10 +615,10 @@ static hipError_t launch_scorer(const KernelPlan &p, const uint16_t *rl, const u
     // 25.1) nor for more tiles (220, 8 labels: d = 252 60.8 and 67.5).
     const bool one = per_group == 1 && (L == 1 || (p.n_bia_tiles <= 32 && (all <= 64 || all > 1024)));
     // 16-byte W pieces when every row starts 16-byte aligned
-    if (ldw % 8 == 0 && ((uintptr_t)w & 15) == 0)
-        launch_biaffine_p<8>(p, n_work, groups, per_group, one, lds, stream, rl, rr, w, d, ldw, L, bias, scores);
-    else
-        launch_biaffine_p<4>(p, n_work, groups, per_group, one, lds, stream, rl, rr, w, d, ldw, L, bias, scores);
+    const bool wide = ldw % 8 == 0 && ((uintptr_t)w & 15) == 0, biased = bias.table != nullptr;
+    (wide ? (biased ? launch_biaffine_p<8, true> : launch_biaffine_p<8, false>)
+          : (biased ? launch_biaffine_p<4, true> : launch_biaffine_p<4, false>))(p, n_work, groups, per_group, one, lds, stream, rl,
+                                                                             rr, w, d, ldw, L, bias, scores);
     return hipGetLastError();
 }
 
