@@ -38,14 +38,22 @@ constexpr int kTile = 64;   // sides are padded to multiples of this, or of twic
 // What X, A and B are held times: entries of at most 8, 32 and 64 fit float16.
 constexpr float kScaleX = 4096.f, kScaleA = 2048.f, kScaleB = 1024.f;
 
+// A stored matrix of rows of K entries lies in blocks of 32 rows x 16 entries,
+// each an operand's fragment for the 64 lanes of a wavefront: a load or store of
+// one is 1 KB on end.  A row of blocks has one to spare: workgroups read blocks of
+// many of them at one place of K at a time, and a power of two between those
+// would put them all on a few of the caches' and the memory's channels.
+__host__ __device__ constexpr int64_t row_blocks(int K) { return K / 16 + 1; }
+
 // Matrices of more rows and columns than this are padded to whole tiles of 128 x 128.
 constexpr int kWide = 512;
 // One matrix's arrays, each two planes (hi, then lo) of float16.
 struct OrthoShape {
     int p, q;          // sides, p <= q
     int pp, qq;        // padded to whole tiles
-    __host__ __device__ int64_t x_plane() const { return (int64_t)pp * qq; }
-    __host__ __device__ int64_t a_plane() const { return (int64_t)pp * pp; }
+    __host__ __device__ int64_t x_plane() const { return (int64_t)pp / 32 * row_blocks(qq) * 512; }
+    __host__ __device__ int64_t xt_plane() const { return (int64_t)qq / 32 * row_blocks(pp) * 512; }
+    __host__ __device__ int64_t a_plane() const { return (int64_t)pp / 32 * row_blocks(pp) * 512; }
 };
 __host__ __device__ inline OrthoShape ortho_shape(int rows, int cols) {
     OrthoShape s;
@@ -136,11 +144,9 @@ __device__ __forceinline__ f32x4 joined(const f16x4 &hi, const f16x4 &lo) {
     return __builtin_convertvector(hi, f32x4) + __builtin_convertvector(lo, f32x4);
 }
 
-// A stored matrix of rows of K entries lies in blocks of 32 rows x 16 entries,
-// each an operand's fragment for the 64 lanes of a wavefront: a load or store of
-// one is 1 KB on end.  Entries 8 c .. 8 c + 7 of row r (one lane's) start at:
+// Where entries 8 c .. 8 c + 7 of row r (one lane's of a fragment) start.
 __device__ __forceinline__ int64_t piece(int r, int c, int K) {
-    return ((int64_t)(r >> 5) * (K >> 4) + (c >> 1)) * 512 + ((r & 31) + 32 * (c & 1)) * 8;
+    return ((r >> 5) * row_blocks(K) + (c >> 1)) * 512 + ((r & 31) + 32 * (c & 1)) * 8;
 }
 
 // X = U / (|U|_F + eps) in parts, and its transpose; zeros past the matrix.
@@ -174,7 +180,7 @@ __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoIo io, const doubl
     }
     __syncthreads();
     x += blockIdx.z * 2 * sh.x_plane();
-    xt += blockIdx.z * 2 * sh.x_plane();
+    xt += blockIdx.z * 2 * sh.xt_plane();
     for (int e = threadIdx.x; e < kTile * kTile / 8; e += 256) {
         const int r = e % kTile, c = e / kTile;
         f16x8 hi, lo;
@@ -189,7 +195,7 @@ __global__ __launch_bounds__(256) void ortho_load_kernel(OrthoIo io, const doubl
         for (int q = 0; q < 8; ++q) v[q] = tile[8 * c + q][r];
         split(v, hi, lo);
         *reinterpret_cast<f16x8 *>(xt + to) = hi;
-        *reinterpret_cast<f16x8 *>(xt + sh.x_plane() + to) = lo;
+        *reinterpret_cast<f16x8 *>(xt + sh.xt_plane() + to) = lo;
     }
 }
 
@@ -205,7 +211,7 @@ struct ProductArgs {
     _Float16 *out, *out_t;          // the result and its transpose
     int k, stride, t_stride;        // K; the entries of their rows
     int across;                     // tiles of a row of tiles
-    int64_t left_plane, right_plane, out_plane;
+    int64_t left_plane, right_plane, out_plane, out_t_plane;
     float a, b, c;                  // in the scale of the result
 };
 
@@ -274,7 +280,7 @@ __device__ __forceinline__ void finish_tile(float *tile, const ProductArgs &g, c
     }
     if (!mirror) return;
     if constexpr (KIND == kPoly) __syncthreads();
-    _Float16 *out_t = g.out_t + blockIdx.z * 2 * g.out_plane;
+    _Float16 *out_t = g.out_t + blockIdx.z * 2 * g.out_t_plane;
     for (int e = tid; e < T * kPieces; e += 256) {
         const int r = e % T, c = e / T;
         const int64_t at = piece(j0 + r, i0 / 8 + c, g.t_stride);
@@ -284,7 +290,7 @@ __device__ __forceinline__ void finish_tile(float *tile, const ProductArgs &g, c
         for (int q = 0; q < 8; ++q) v[q] = tile[(8 * c + q) * kRow + r] * (KIND == kPoly ? 1.f : g.c);
         split(v, hi, lo);
         *reinterpret_cast<f16x8 *>(out_t + at) = hi;
-        *reinterpret_cast<f16x8 *>(out_t + g.out_plane + at) = lo;
+        *reinterpret_cast<f16x8 *>(out_t + g.out_t_plane + at) = lo;
     }
 }
 
@@ -307,8 +313,8 @@ __global__ __launch_bounds__(256) void ortho_few_kernel(ProductArgs g, OrthoIo i
     tile_of<KIND>(g, i, j);
     const int steps = g.k / 16, part = steps / 4;   // (K is a multiple of 64)
     const int64_t own = ((int64_t)wave * part) * 512 + 8 * lane;
-    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + (int64_t)i * steps * 512 + own;
-    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + (int64_t)j * steps * 512 + own;
+    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + i * row_blocks(g.k) * 512 + own;
+    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + j * row_blocks(g.k) * 512 + own;
     f16x8 next[kFewAhead][4];
     auto load = [&](int first) {
 #pragma unroll
@@ -349,15 +355,20 @@ __global__ __launch_bounds__(256) void ortho_few_kernel(ProductArgs g, OrthoIo i
     finish_tile<KIND, kFewTile>(sums[0], g, io, kFewTile * i, kFewTile * j);
 }
 
-// Many: 64 M x 64 M a workgroup, staged through LDS 32 of K at a time, block by
-// block as they lie; a wavefront takes M x M tiles of 32 x 32.  2 M steps' loads
-// are on their way in registers: one from another XCD's L2 or from HBM takes as
-// long as two or three steps' products.
-constexpr int kStepK = 32;
+// Many: 64 M x 64 M a workgroup, a wavefront M x M tiles of 32 x 32.  Operands go
+// through LDS 32 of K at a time, block by block as they lie, and all that a step
+// does is for a later one: it loads step s + 2 + 2 M from memory into registers,
+// stores step s + 2 to LDS, reads step s + 1's fragments and multiplies step s's,
+// with one barrier.  (Read, multiplied and stored one after the other, with loads
+// ahead alone, the four wavefronts of a CU leave the matrix cores idle for 60% of
+// the time.)
+constexpr int kStepK = 32, kRing = 3;
+constexpr int kMfma = 0x008, kLoad = 0x020, kLdsRead = 0x100, kLdsWrite = 0x200;   // kinds of instructions to the scheduler
 template <int M>
-constexpr int staged_bytes() { return std::max(2 * 16 * M * 1024, 64 * M * (64 * M + 1) * 4); }
+constexpr int staged_bytes() { return std::max(kRing * 16 * M * 1024, 64 * M * (64 * M + 1) * 4); }
 template <int KIND, int M>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ? 2 : 8))) void ortho_tile_kernel(ProductArgs g, OrthoIo io) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ? 1 : 3))) void ortho_tile_kernel(ProductArgs g,
+                                                                                                     OrthoIo io) {
     constexpr int T = 64 * M, D = 2 * M, kPlane = 4 * M * 512, kBuffer = 4 * kPlane;   // left hi, lo, right hi, lo
     extern __shared__ __align__(16) char smem[];
     _Float16 *stage = reinterpret_cast<_Float16 *>(smem);
@@ -365,15 +376,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ?
     int i, j;
     tile_of<KIND>(g, i, j);
     // wavefront w moves blocks w + 4 h of each matrix's 4 M: row block / 2, K block
-    const int steps = g.k / 16;
-    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + ((int64_t)2 * M * i * steps) * 512 + 8 * lane;
-    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + ((int64_t)2 * M * j * steps) * 512 + 8 * lane;
+    const int64_t across = row_blocks(g.k);
+    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + 2 * M * i * across * 512 + 8 * lane;
+    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + 2 * M * j * across * 512 + 8 * lane;
     f16x8 next[D][4][M];
-    auto load = [&](int d, int k0) {
+    auto load = [&](int d, int step) {   // (past the last step: the last one's again, which goes nowhere)
+        const int k0 = min(step * kStepK, g.k - kStepK);
 #pragma unroll
         for (int h = 0; h < M; ++h) {
             const int b = wave + 4 * h;
-            const int64_t at = ((int64_t)(b >> 1) * steps + k0 / 16 + (b & 1)) * 512;
+            const int64_t at = ((b >> 1) * across + k0 / 16 + (b & 1)) * 512;
             next[d][0][h] = frag(left + at);
             next[d][1][h] = frag(left + g.left_plane + at);
             next[d][2][h] = frag(right + at);
@@ -387,10 +399,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ?
             for (int h = 0; h < M; ++h)
                 *reinterpret_cast<f16x8 *>(stage + buffer * kBuffer + s * kPlane + (wave + 4 * h) * 512 + 8 * lane) = next[d][s][h];
     };
+    const int wi = 32 * M * (wave >> 1), wj = 32 * M * (wave & 1);   // the wavefront's part of the tile
+    f16x8 l[2][2][2][M], r[2][2][2][M];   // of two steps: K block, part, tile
+    auto read = [&](int w, int buffer) {
+        const _Float16 *from = stage + buffer * kBuffer + 8 * lane;
 #pragma unroll
-    for (int d = 0; d < D; ++d) load(d, kStepK * d);
-    store(0, 0);
-    __syncthreads();
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    l[w][k][s][m] = frag(from + s * kPlane + (2 * (wi / 32 + m) + k) * 512);
+                    r[w][k][s][m] = frag(from + (2 + s) * kPlane + (2 * (wj / 32 + m) + k) * 512);
+                }
+    };
     f32x16 acc[M][M];
 #pragma unroll
     for (int m = 0; m < M; ++m)
@@ -398,34 +420,53 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ?
         for (int n = 0; n < M; ++n)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[m][n][e] = 0.f;
-    const int wi = 32 * M * (wave >> 1), wj = 32 * M * (wave & 1);   // the wavefront's part of the tile
-    for (int k0 = 0; k0 < g.k; k0 += kStepK * D)   // (K is a multiple of 64 M)
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(d, d);
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+        store(d, d);
+        load(d, d + D);
+    }
+    __syncthreads();
+    read(0, 0);
+    int ahead = 1, free = 2;   // buffers of steps s + 1 and s + 2
+    for (int s0 = 0; s0 < g.k / kStepK; s0 += D)   // (K is a multiple of 64 M)
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-            const int now = k0 + kStepK * d;
-            load(d, min(now + kStepK * D, g.k - kStepK));   // (the last loads' data goes nowhere)
-            const _Float16 *from = stage + (d & 1) * kBuffer + 8 * lane;
+            read((d + 1) & 1, ahead);
+            store((d + 2) % D, free);
+            load((d + 2) % D, s0 + d + 2 + D);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                f16x8 l[2][M], r[2][M];
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int m = 0; m < M; ++m) {
-                        l[s][m] = frag(from + s * kPlane + (2 * (wi / 32 + m) + k) * 512);
-                        r[s][m] = frag(from + (2 + s) * kPlane + (2 * (wj / 32 + m) + k) * 512);
-                    }
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int s = 0; s < 3; ++s)   // hi lo, lo hi, hi hi
 #pragma unroll
                     for (int m = 0; m < M; ++m)
 #pragma unroll
                         for (int n = 0; n < M; ++n)
-                            acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[s == 1][m], r[s == 0][n], acc[m][n], 0, 0, 0);
+                            acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[d & 1][k][s == 1][m], r[d & 1][k][s == 0][n],
+                                                                               acc[m][n], 0, 0, 0);
+            // a wavefront issues in order: the others go between the products, or
+            // the products wait for them
+#pragma unroll
+            for (int q = 0; q < (M == 2 ? 8 : 2); ++q) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsRead, M == 2 ? 2 : 4, 0);
             }
-            store((d + 1) % D, (d + 1) & 1);
+#pragma unroll
+            for (int q = 0; q < 4 * M; ++q) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, M, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsWrite, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kLoad, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
             __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+            const int was = kRing - ahead - free;
+            ahead = free;
+            free = was;
         }
+    __syncthreads();   // (the reads of a step past the last have ended)
     float *tile = reinterpret_cast<float *>(smem);
 #pragma unroll
     for (int m = 0; m < M; ++m)
@@ -766,8 +807,8 @@ hipError_t set_ortho_attributes() {
 int64_t ortho_bytes(int count, int rows, int cols) {
     if (std::max(rows, cols) <= kSmall) return 256;
     const OrthoShape sh = ortho_shape(rows, cols);
-    return aligned(8 * (int64_t)count * norm_shares(rows, cols)) + 4 * aligned(4 * count * sh.x_plane()) +
-           2 * aligned(4 * count * sh.a_plane());
+    return aligned(8 * (int64_t)count * norm_shares(rows, cols)) + 2 * aligned(4 * count * sh.x_plane()) +
+           2 * aligned(4 * count * sh.xt_plane()) + 2 * aligned(4 * count * sh.a_plane());
 }
 
 hipError_t launch_ortho(const float *grad, const float *momentum, const float *w, float *momentum_out, float *out, int count,
@@ -794,7 +835,7 @@ hipError_t launch_ortho(const float *grad, const float *momentum, const float *w
         ws += aligned(4 * count * plane);
         return at;
     };
-    for (int k = 0; k < 2; ++k) x[k] = take(sh.x_plane()), xt[k] = take(sh.x_plane());
+    for (int k = 0; k < 2; ++k) x[k] = take(sh.x_plane()), xt[k] = take(sh.xt_plane());
     a = take(sh.a_plane());
     b = take(sh.a_plane());
     const int n_shares = norm_shares(rows, cols);
@@ -805,11 +846,11 @@ hipError_t launch_ortho(const float *grad, const float *momentum, const float *w
         const float *co = coefficients + 3 * s;
         const int now = s & 1;
         const ProductArgs gram{x[now], x[now], nullptr, a, a, sh.qq, sh.pp, sh.pp, 0, sh.x_plane(), sh.x_plane(), sh.a_plane(),
-                               0.f, 0.f, kScaleA / (kScaleX * kScaleX)};
+                               sh.a_plane(), 0.f, 0.f, kScaleA / (kScaleX * kScaleX)};
         const ProductArgs poly{a, a, a, b, b, sh.pp, sh.pp, sh.pp, 0, sh.a_plane(), sh.a_plane(), sh.a_plane(),
-                               co[0] * kScaleB, co[1] * (kScaleB / kScaleA), co[2] * (kScaleB / (kScaleA * kScaleA))};
-        ProductArgs next{b, xt[now], nullptr, x[now ^ 1], xt[now ^ 1], sh.pp, sh.qq, sh.pp, 0, sh.a_plane(), sh.x_plane(),
-                         sh.x_plane(), 0.f, 0.f, 1.f / kScaleB};
+                               sh.a_plane(), co[0] * kScaleB, co[1] * (kScaleB / kScaleA), co[2] * (kScaleB / (kScaleA * kScaleA))};
+        ProductArgs next{b, xt[now], nullptr, x[now ^ 1], xt[now ^ 1], sh.pp, sh.qq, sh.pp, 0, sh.a_plane(), sh.xt_plane(),
+                         sh.x_plane(), sh.xt_plane(), 0.f, 0.f, 1.f / kScaleB};
         launch_product<kGram>(gram, io, sh.pp, sh.pp, count, stream);
         launch_product<kPoly>(poly, io, sh.pp, sh.pp, count, stream);
         if (s + 1 == steps) {
