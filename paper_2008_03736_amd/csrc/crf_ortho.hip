@@ -232,44 +232,77 @@ __device__ __forceinline__ void tile_of(const ProductArgs &g, int &i, int &j) {
 
 __device__ __forceinline__ f16x8 frag(const _Float16 *p) { return *reinterpret_cast<const f16x8 *>(p); }
 
+// What a tile's end reads from memory: A's entries or the weights of its places, a
+// thread of NT's share.  Small tiles ask for it before the products.
+template <int KIND, int T, int NT>
+struct Held {
+    static constexpr int kPieces = (T * T / 8 + NT - 1) / NT, kEntries = T * T / NT;   // a thread's
+    f16x8 hi[KIND == kPoly ? kPieces : 1], lo[KIND == kPoly ? kPieces : 1];
+    float w[KIND == kLast ? kEntries : 1];
+    // entry e of the tile at (i0, j0), along the caller's rows; false: past the matrix
+    static __device__ __forceinline__ bool entry(const OrthoIo &io, int i0, int j0, int e, int &at_tile, int64_t &at) {
+        const bool tall = io.rows > io.cols;
+        const int r = e / T, c = e % T, row = (tall ? j0 : i0) + r, col = (tall ? i0 : j0) + c;
+        at_tile = tall ? c * (T + 1) + r : r * (T + 1) + c;
+        at = (int64_t)blockIdx.z * io.rows * io.ld + (int64_t)row * io.ld + col;
+        return row < io.rows && col < io.cols;
+    }
+    __device__ __forceinline__ void load(const ProductArgs &g, const OrthoIo &io, int i0, int j0) {
+        if constexpr (KIND == kPoly) {
+            const _Float16 *add = g.add + blockIdx.z * 2 * g.out_plane;
+#pragma unroll
+            for (int h = 0; h < kPieces; ++h) {
+                const int e = min((int)threadIdx.x + h * NT, T * T / 8 - 1);
+                const int64_t at = piece(i0 + e % T, j0 / 8 + e / T, g.stride);
+                hi[h] = frag(add + at);
+                lo[h] = frag(add + g.out_plane + at);
+            }
+        }
+        if constexpr (KIND == kLast) {
+            if (io.w == nullptr) return;
+#pragma unroll
+            for (int h = 0; h < kEntries; ++h) {
+                int at_tile;
+                int64_t at;
+                w[h] = entry(io, i0, j0, threadIdx.x + h * NT, at_tile, at) ? io.w[at] : 0.f;
+            }
+        }
+    }
+};
+
 // A tile's sums, in LDS at a row stride of T + 1, to where they belong: rows of
 // the result, then (from LDS, so that both are whole lines) rows of its transpose.
-template <int KIND, int T>
-__device__ __forceinline__ void finish_tile(float *tile, const ProductArgs &g, const OrthoIo &io, int i0, int j0) {
-    constexpr int kRow = T + 1, kPieces = T / 8;
+template <int KIND, int T, int NT>
+__device__ __forceinline__ void finish_tile(float *tile, const Held<KIND, T, NT> &held, const ProductArgs &g, const OrthoIo &io,
+                                            int i0, int j0) {
+    constexpr int kRow = T + 1;
     const int tid = threadIdx.x;
     if constexpr (KIND == kLast) {
-        const OrthoShape sh = ortho_shape(io.rows, io.cols);
-        const bool tall = io.rows > io.cols;
-        const int64_t base = (int64_t)blockIdx.z * io.rows * io.ld;
-        for (int e = tid; e < T * T; e += 256) {
-            const int r = e / T, c = e % T;   // along the caller's rows
-            const int i = i0 + (tall ? c : r), j = j0 + (tall ? r : c);
-            if (i < sh.p && j < sh.q) {
-                const float v = g.c * tile[tall ? c * kRow + r : r * kRow + c];
-                const int64_t to = base + (tall ? (int64_t)j * io.ld + i : (int64_t)i * io.ld + j);
-                io.out[to] = io.w != nullptr ? fmaf(-io.rate, v, io.keep * io.w[to]) : v;
+#pragma unroll
+        for (int h = 0; h < held.kEntries; ++h) {
+            int from;
+            int64_t to;
+            if (held.entry(io, i0, j0, tid + h * NT, from, to)) {
+                const float v = g.c * tile[from];
+                io.out[to] = io.w != nullptr ? fmaf(-io.rate, v, io.keep * held.w[h]) : v;
             }
         }
         return;
     }
     const bool mirror = KIND == kNext || i0 != j0;
     _Float16 *out = g.out + blockIdx.z * 2 * g.out_plane;
-    const _Float16 *add = KIND == kPoly ? g.add + blockIdx.z * 2 * g.out_plane : nullptr;
-    for (int e = tid; e < T * kPieces; e += 256) {
-        const int r = e % T, c = e / T;
+#pragma unroll
+    for (int h = 0; h < held.kPieces; ++h) {
+        const int e = tid + h * NT, r = e % T, c = e / T;
+        if (T * T / 8 < NT && e >= T * T / 8) break;
         const int64_t at = piece(i0 + r, j0 / 8 + c, g.stride);
         float *in = tile + r * kRow + 8 * c, v[8];
         f16x8 hi, lo;
-        if constexpr (KIND == kPoly) {
-            hi = frag(add + at);
-            lo = frag(add + g.out_plane + at);
-        }
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             v[q] = in[q] * g.c;
             if constexpr (KIND == kPoly) {
-                v[q] = fmaf(g.b, (float)hi[q] + (float)lo[q], v[q]);
+                v[q] = fmaf(g.b, (float)held.hi[h][q] + (float)held.lo[h][q], v[q]);
                 if (i0 + r == j0 + 8 * c + q) v[q] += g.a;
                 if (mirror) in[q] = v[q];
             }
@@ -281,8 +314,10 @@ __device__ __forceinline__ void finish_tile(float *tile, const ProductArgs &g, c
     if (!mirror) return;
     if constexpr (KIND == kPoly) __syncthreads();
     _Float16 *out_t = g.out_t + blockIdx.z * 2 * g.out_t_plane;
-    for (int e = tid; e < T * kPieces; e += 256) {
-        const int r = e % T, c = e / T;
+#pragma unroll
+    for (int h = 0; h < held.kPieces; ++h) {
+        const int e = tid + h * NT, r = e % T, c = e / T;
+        if (T * T / 8 < NT && e >= T * T / 8) break;
         const int64_t at = piece(j0 + r, i0 / 8 + c, g.t_stride);
         float v[8];
         f16x8 hi, lo;
@@ -302,57 +337,56 @@ __device__ __forceinline__ void put_sums(float *tile, int stride, const f32x16 &
     for (int t = 0; t < 16; ++t) tile[(8 * (t >> 2) + 4 * (lane >> 5) + (t & 3)) * stride + (lane & 31)] = acc[t];
 }
 
-// Few tiles: 32 x 32 a workgroup, K split over its four wavefronts, whose
-// fragments come straight from L2 (each is used once) and whose sums meet in LDS.
-constexpr int kFewTile = 32, kFewAhead = 4;   // steps of K (of 16) in flight together
+// Few tiles: 32 x 32 a workgroup, K split over its eight wavefronts, whose
+// fragments come straight from L2 (each is used once), all in flight together up
+// to K = 512, and whose sums meet in LDS.
+constexpr int kFewTile = 32, kFewWaves = 8, kFewThreads = 64 * kFewWaves;
+constexpr int kFewAhead = 4;   // steps of K (of 16) a wavefront has in flight
 template <int KIND>
-__global__ __launch_bounds__(256) void ortho_few_kernel(ProductArgs g, OrthoIo io) {
-    __shared__ float sums[4][kFewTile * (kFewTile + 1)];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(kFewThreads) void ortho_few_kernel(ProductArgs g, OrthoIo io) {
+    __shared__ float sums[kFewWaves][kFewTile * (kFewTile + 1)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int i, j;
     tile_of<KIND>(g, i, j);
-    const int steps = g.k / 16, part = steps / 4;   // (K is a multiple of 64)
-    const int64_t own = ((int64_t)wave * part) * 512 + 8 * lane;
-    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + i * row_blocks(g.k) * 512 + own;
-    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + j * row_blocks(g.k) * 512 + own;
-    f16x8 next[kFewAhead][4];
-    auto load = [&](int first) {
-#pragma unroll
-        for (int s = 0; s < kFewAhead; ++s) {
-            const int64_t at = 512 * (int64_t)min(first + s, part - 1);
-            next[s][0] = frag(left + at);
-            next[s][1] = frag(left + g.left_plane + at);
-            next[s][2] = frag(right + at);
-            next[s][3] = frag(right + g.right_plane + at);
-        }
-    };
-    load(0);
+    const int steps = g.k / 16, part = (steps + kFewWaves - 1) / kFewWaves;
+    const int first = wave * part, end = min(first + part, steps);
+    const _Float16 *left = g.left + blockIdx.z * 2 * g.left_plane + i * row_blocks(g.k) * 512 + 8 * lane;
+    const _Float16 *right = g.right + blockIdx.z * 2 * g.right_plane + j * row_blocks(g.k) * 512 + 8 * lane;
+    Held<KIND, kFewTile, kFewThreads> held;
+    held.load(g, io, kFewTile * i, kFewTile * j);
     f32x16 acc[3];
 #pragma unroll
     for (int t = 0; t < 3; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
-    for (int first = 0; first < part; first += kFewAhead) {
-        f16x8 now[kFewAhead][4];
+    for (int s0 = first; s0 < end; s0 += kFewAhead) {
+        f16x8 f[kFewAhead][4];
+#pragma unroll
+        for (int s = 0; s < kFewAhead; ++s) {
+            const int64_t at = 512 * (int64_t)min(s0 + s, end - 1);
+            f[s][0] = frag(left + at);
+            f[s][1] = frag(left + g.left_plane + at);
+            f[s][2] = frag(right + at);
+            f[s][3] = frag(right + g.right_plane + at);
+        }
 #pragma unroll
         for (int s = 0; s < kFewAhead; ++s)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) now[s][t] = next[s][t];
-        if (first + kFewAhead < part) load(first + kFewAhead);
-#pragma unroll
-        for (int s = 0; s < kFewAhead; ++s)
-            if (first + s < part) {
-                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[s][0], now[s][3], acc[0], 0, 0, 0);
-                acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[s][1], now[s][2], acc[1], 0, 0, 0);
-                acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[s][0], now[s][2], acc[2], 0, 0, 0);
+            if (s0 + s < end) {
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[s][0], f[s][3], acc[0], 0, 0, 0);
+                acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[s][1], f[s][2], acc[1], 0, 0, 0);
+                acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[s][0], f[s][2], acc[2], 0, 0, 0);
             }
     }
     put_sums(sums[wave], kFewTile + 1, (acc[0] + acc[1]) + acc[2], lane);
     __syncthreads();
-    for (int e = threadIdx.x; e < kFewTile * (kFewTile + 1); e += 256)
-        sums[0][e] = (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+    for (int e = threadIdx.x; e < kFewTile * (kFewTile + 1); e += kFewThreads) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) s += sums[w][e];
+        sums[0][e] = s;
+    }
     __syncthreads();
-    finish_tile<KIND, kFewTile>(sums[0], g, io, kFewTile * i, kFewTile * j);
+    finish_tile<KIND, kFewTile, kFewThreads>(sums[0], held, g, io, kFewTile * i, kFewTile * j);
 }
 
 // Many: 64 M x 64 M a workgroup, a wavefront M x M tiles of 32 x 32.  Operands go
@@ -473,7 +507,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ?
 #pragma unroll
         for (int n = 0; n < M; ++n) put_sums(tile + (wi + 32 * m) * (T + 1) + wj + 32 * n, T + 1, acc[m][n], lane);
     __syncthreads();
-    finish_tile<KIND, T>(tile, g, io, T * i, T * j);
+    Held<KIND, T, 256> held;
+    held.load(g, io, T * i, T * j);
+    finish_tile<KIND, T, 256>(tile, held, g, io, T * i, T * j);
 }
 
 // The largest tile of which there are kEnoughTiles (half the CUs), or the least:
@@ -495,7 +531,7 @@ void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int co
     g.across = cols / T;
     const dim3 grid((uint32_t)tiles(T), 1, count);
     if (T == kFewTile)
-        hipLaunchKernelGGL(ortho_few_kernel<KIND>, grid, dim3(256), 0, stream, g, io);
+        hipLaunchKernelGGL(ortho_few_kernel<KIND>, grid, dim3(kFewThreads), 0, stream, g, io);
     else if (T == 64)
         hipLaunchKernelGGL((ortho_tile_kernel<KIND, 1>), grid, dim3(256), staged_bytes<1>(), stream, g, io);
     else

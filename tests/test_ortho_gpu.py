@@ -86,7 +86,8 @@ def check(got, u, steps, eps):
 SHAPES = [(1, 1, 1, 1), (1, 1, 9, 9), (2, 9, 1, 3), (3, 2, 3, 5), (1, 15, 16, 16), (2, 16, 17, 20), (5, 31, 33, 33),
           (3, 33, 31, 40), (2, 64, 64, 64), (3, 63, 65, 68), (7, 100, 101, 104), (2, 101, 100, 100), (2, 112, 128, 128),
           (2, 128, 128, 130), (2, 128, 129, 132), (1, 129, 127, 127), (2, 40, 300, 304), (1, 300, 40, 41), (1, 7, 1000, 1000),
-          (1, 500, 501, 504), (1, 512, 512, 512), (1, 513, 260, 263), (1, 700, 1030, 1030)]
+          (1, 500, 501, 504), (1, 512, 512, 512), (1, 513, 260, 263), (1, 700, 1030, 1030), (40, 20, 130, 130),
+          (9, 200, 300, 300), (1, 2, 8192, 8192), (1, 1537, 1030, 1030), (3, 1025, 1290, 1290)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
@@ -152,7 +153,9 @@ def test_zeros_and_what_is_not_finite(torch, shape):
 
 
 @pytest.mark.parametrize("nesterov", [True, False])
-@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (5, 20, 21, 24), (7, 100, 101, 104), (1, 300, 200, 200), (1, 500, 501, 504)])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (5, 20, 21, 24), (7, 100, 101, 104), (1, 300, 200, 200), (1, 500, 501, 504),
+                                   (2, 40, 300, 304), (3, 200, 60, 64), (1, 129, 190, 191), (1, 257, 330, 330),
+                                   (9, 260, 500, 500), (2, 1030, 1100, 1101)])
 def test_muon_step(torch, shape, nesterov):
     count, rows, cols, ld = shape
     w, g, m = (matrices(count, rows, cols, ld, k) * np.float32(f) for k, f in ((1, 100), (2, 1), (3, 5)))
