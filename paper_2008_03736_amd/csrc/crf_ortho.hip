@@ -552,8 +552,7 @@ constexpr int kSmall = 128;
 __host__ __device__ constexpr int small_stride(int tiles) { return (tiles + 1) / 2 * 32 + 8; }   // of a row of 16 `tiles`
 inline int64_t small_lds(int p, int q) {
     const int pt = (p + 15) / 16, qt = (q + 15) / 16;
-    const int64_t parts = 2 * 2 * 16 * pt * (int64_t)(small_stride(pt) + small_stride(qt));
-    return std::max<int64_t>(parts, 4 * (int64_t)q * (p + 1));
+    return std::max<int64_t>(2 * 2 * 2 * 16 * pt * (int64_t)small_stride(qt), 4 * (int64_t)q * (p + 1));
 }
 
 struct Steps {
@@ -564,7 +563,8 @@ struct Steps {
 // U row tiles of a stored matrix (hi, and lo `plane` entries on) times a column
 // tile in registers: tile u is at row tile row(u), and done(u, acc) takes its
 // result.  ks: steps of K.  The next tile's fragments fly while this one's
-// products run, in a chain for each of the three.
+// products run, in a chain for each of the three, and the last one's result is
+// taken.
 template <int U, int KS, typename Row, typename Done>
 __device__ __forceinline__ void row_tiles(const _Float16 *from, int plane, int stride, int ks, const f16x8 (&rh)[KS],
                                           const f16x8 (&rl)[KS], Row row, Done done) {
@@ -579,22 +579,24 @@ __device__ __forceinline__ void row_tiles(const _Float16 *from, int plane, int s
             }
     };
     load(0);
+    f32x4 acc[2][3];
+    auto sum = [&](int u) { return (acc[u & 1][0] + acc[u & 1][1]) + acc[u & 1][2]; };
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (u + 1 < U) load(u + 1);
-        f32x4 acc[3];
 #pragma unroll
-        for (int t = 0; t < 3; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < 3; ++t) acc[u & 1][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < KS; ++s)
             if (s < ks) {
-                acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[u & 1][s], rl[s], acc[0], 0, 0, 0);
-                acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ll[u & 1][s], rh[s], acc[1], 0, 0, 0);
-                acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[u & 1][s], rh[s], acc[2], 0, 0, 0);
+                acc[u & 1][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[u & 1][s], rl[s], acc[u & 1][0], 0, 0, 0);
+                acc[u & 1][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ll[u & 1][s], rh[s], acc[u & 1][1], 0, 0, 0);
+                acc[u & 1][2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[u & 1][s], rh[s], acc[u & 1][2], 0, 0, 0);
             }
-        done(u, (acc[0] + acc[1]) + acc[2]);
+        if (u > 0) done(u - 1, sum(u - 1));
         __builtin_amdgcn_sched_barrier(0);   // (no further loads ahead: their registers spill)
     }
+    done(U - 1, sum(U - 1));
 }
 
 template <int PT, int W>
@@ -611,9 +613,9 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
     const bool tall = io.rows > io.cols;
     const int p = tall ? io.cols : io.rows, q = tall ? io.rows : io.cols;
     const int qt = (q + 15) / 16, kq = (qt + 1) / 2, sx = small_stride(qt);
-    _Float16 *xs = reinterpret_cast<_Float16 *>(smem), *gs = xs + 2 * 16 * PT * sx;
-    const int x_plane = 16 * PT * sx;
+    const int x_plane = 16 * PT * sx;   // (no less than a plane of A's: q >= p)
     constexpr int g_plane = 16 * PT * kSG;
+    _Float16 *xs = reinterpret_cast<_Float16 *>(smem), *gs = xs + 2 * x_plane;
     const int64_t base = (int64_t)blockIdx.x * io.rows * io.ld;
 
     // U, the new momentum and the norm
@@ -658,50 +660,60 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
     for (int w = 1; w < W; ++w) sum += norm[w];
     // (a sum that is not finite makes the whole matrix NaN)
     const double inv = 1.0 / (sqrt(sum) + (double)io.eps) + 0.0 * sum;
-    // tile i: rows 16 i + 4 g .. + 3 of column own
-    f32x4 x[PT];
+    // X's parts, tile i: rows 16 i + 4 g .. + 3 of column own
+    f16x8 xh[kKP], xl[kKP];
     const int own = 16 * wave + n;
+    auto set = [&](f16x8 (&hi8)[kKP], f16x8 (&lo8)[kKP], int i, const f16x4 &hi, const f16x4 &lo) {
 #pragma unroll
-    for (int i = 0; i < PT; ++i)
+        for (int t = 0; t < 4; ++t) {
+            hi8[i >> 1][4 * (i & 1) + t] = hi[t];
+            lo8[i >> 1][4 * (i & 1) + t] = lo[t];
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < 2 * kKP; ++i) {
+        f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const int r = 16 * i + 4 * g + t, row = min(r, p - 1), at = min(own, q - 1);
             const float u = (float)((double)us[tall ? at * us_stride + row : row * us_stride + at] * inv);
-            x[i][t] = r < p && own < q ? u : 0.f;
+            x[t] = r < p && own < q ? u : 0.f;
         }
+        f16x4 hi, lo;
+        split(kScaleX * x, hi, lo);
+        set(xh, xl, i, hi, lo);
+    }
     __syncthreads();
-    for (int k = tid; k < (2 * x_plane + 2 * g_plane) / 8; k += kThreads) reinterpret_cast<u32x4 *>(xs)[k] = u32x4{0u, 0u, 0u, 0u};
+    // (what lies past the tiles in the last step of K is multiplied by zeros, so it has to be finite)
+    for (int k = tid; k < 4 * x_plane / 8; k += kThreads) reinterpret_cast<u32x4 *>(xs)[k] = u32x4{0u, 0u, 0u, 0u};
+    __syncthreads();
+    // a tile's parts into the rows of X
+    auto put_x = [&](_Float16 *to, int i, const f16x4 &hi, const f16x4 &lo) {
+        to += (16 * i + 4 * g) * sx + 16 * wave + n;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            to[t * sx] = hi[t];
+            to[x_plane + t * sx] = lo[t];
+        }
+    };
+    if (wave < qt) {
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+            const int h = 4 * (i & 1);
+            put_x(xs, i, f16x4{xh[i >> 1][h], xh[i >> 1][h + 1], xh[i >> 1][h + 2], xh[i >> 1][h + 3]},
+                  f16x4{xl[i >> 1][h], xl[i >> 1][h + 1], xl[i >> 1][h + 2], xl[i >> 1][h + 3]});
+        }
+    }
     __syncthreads();
 
+    // X lies in xs; A goes to gs, B to xs, and the new X to gs: each is read by all
+    // wavefronts before the barrier after which its place is written
 #pragma unroll 1
     for (int step = 0; step < steps.count; ++step) {
         const float a = steps.f[step][0], b = steps.f[step][1], c3 = steps.f[step][2];
         // (a step's LDS addresses are taken from these anew: kept over the loop,
         // some hundred of them, they would take the registers that X lies in)
         asm("" : "+v"(n), "+v"(g));
-        // X's parts: the owner's columns into the rows in LDS, and kept as fragments
-        f16x8 xh[kKP], xl[kKP];
-#pragma unroll
-        for (int i = 0; i < 2 * kKP; ++i) {
-            f16x4 hi = f16x4{0, 0, 0, 0}, lo = hi;
-            if (i < PT) {
-                split(kScaleX * x[i < PT ? i : 0], hi, lo);
-                if (wave < qt) {
-                    _Float16 *to = xs + (16 * i + 4 * g) * sx + 16 * wave + n;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        to[t * sx] = hi[t];
-                        to[x_plane + t * sx] = lo[t];
-                    }
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                xh[i >> 1][4 * (i & 1) + t] = hi[t];
-                xl[i >> 1][4 * (i & 1) + t] = lo[t];
-            }
-        }
-        __syncthreads();
 
         // Symmetric products: column tile j, row tiles j + u (cyclically)
         const int j = wave;
@@ -710,18 +722,18 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
         // where tile (i, j)'s lane puts its four rows: row 16 j + n of the stored
         // matrix, columns 16 i + 4 g .. + 3 in their order, and the mirror image
         auto place = [&](int i) { return (16 * j + n) * kSG + 32 * (i >> 1) + 8 * g + 4 * (i & 1); };
-        auto put = [&](int u, const f32x4 &v) {
+        auto put = [&](_Float16 *to, int u, const f32x4 &v) {
             const int i = row_tile(u);
             f16x4 hi, lo;
             split(v, hi, lo);
-            *reinterpret_cast<f16x4 *>(gs + place(i)) = hi;
-            *reinterpret_cast<f16x4 *>(gs + g_plane + place(i)) = lo;
+            *reinterpret_cast<f16x4 *>(to + place(i)) = hi;
+            *reinterpret_cast<f16x4 *>(to + g_plane + place(i)) = lo;
             if (u > 0) {
                 const int at = (16 * i + 4 * g) * kSG + 32 * (j >> 1) + 8 * (n >> 2) + 4 * (j & 1) + (n & 3);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    gs[at + t * kSG] = hi[t];
-                    gs[g_plane + at + t * kSG] = lo[t];
+                    to[at + t * kSG] = hi[t];
+                    to[g_plane + at + t * kSG] = lo[t];
                 }
             }
         };
@@ -735,15 +747,15 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
                     const _Float16 *from = xs + (16 * j + n) * sx + 32 * s + 8 * g;
                     rh[s] = frag(from);
                     rl[s] = frag(from + x_plane);
+                    if (2 * s + 1 == qt && g >= 2) rh[s] = rl[s] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
                 }
             row_tiles<kT>(xs + n * sx + 8 * g, x_plane, sx, kq, rh, rl, row_tile, [&](int u, const f32x4 &acc) {
-                if (wanted(u)) put(u, acc * (kScaleA / (kScaleX * kScaleX)));
+                if (wanted(u)) put(gs, u, acc * (kScaleA / (kScaleX * kScaleX)));
             });
         }
         __syncthreads();
 
-        // B = a I + b A + c A A, held until every wavefront has read A
-        f32x4 poly[kT];
+        // B = a I + b A + c A A
         if (j < PT) {
             f16x8 rh[kKP], rl[kKP];
 #pragma unroll
@@ -752,32 +764,50 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
                 rh[s] = frag(from);
                 rl[s] = frag(from + g_plane);
             }
+            if constexpr (PT % 2 != 0) {
+#pragma unroll
+                for (int t = 4; t < 8; ++t) rh[kKP - 1][t] = rl[kKP - 1][t] = (_Float16)0.f;
+            }
             row_tiles<kT>(gs + n * kSG + 8 * g, g_plane, kSG, kKP, rh, rl, row_tile, [&](int u, const f32x4 &acc) {
                 const f16x4 hi = *reinterpret_cast<const f16x4 *>(gs + place(row_tile(u)));
                 const f16x4 lo = *reinterpret_cast<const f16x4 *>(gs + g_plane + place(row_tile(u)));
-                poly[u] = acc * (c3 * (kScaleB / (kScaleA * kScaleA))) + joined(hi, lo) * (b * (kScaleB / kScaleA));
+                f32x4 v = acc * (c3 * (kScaleB / (kScaleA * kScaleA))) + joined(hi, lo) * (b * (kScaleB / kScaleA));
                 if (u == 0) {
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        if (4 * g + t == n) poly[u][t] += a * kScaleB;
+                        if (4 * g + t == n) v[t] += a * kScaleB;
                 }
+                if (wanted(u)) put(xs, u, v);
             });
-        }
-        __syncthreads();
-        if (j < PT) {
-#pragma unroll
-            for (int u = 0; u < kT; ++u)
-                if (wanted(u)) put(u, poly[u]);
         }
         __syncthreads();
 
         // X <- B X, in the owner's registers
-        if (wave < qt)
-            row_tiles<PT>(gs + n * kSG + 8 * g, g_plane, kSG, kKP, xh, xl, [](int i) { return i; },
-                          [&](int i, const f32x4 &acc) { x[i] = acc * (1.f / (kScaleB * kScaleX)); });
-        // (the rows in LDS were last read before two barriers; B is next written after two more)
+        if (wave < qt) {
+            f16x8 nh[kKP], nl[kKP];
+            if constexpr (PT % 2 != 0) set(nh, nl, PT, f16x4{0, 0, 0, 0}, f16x4{0, 0, 0, 0});
+            row_tiles<PT>(xs + n * kSG + 8 * g, g_plane, kSG, kKP, xh, xl, [](int i) { return i; }, [&](int i, const f32x4 &acc) {
+                f16x4 hi, lo;
+                split(acc * (1.f / kScaleB), hi, lo);
+                set(nh, nl, i, hi, lo);
+                put_x(gs, i, hi, lo);
+            });
+#pragma unroll
+            for (int s = 0; s < kKP; ++s) xh[s] = nh[s], xl[s] = nl[s];
+        }
+        __syncthreads();
+        _Float16 *was = xs;
+        xs = gs;
+        gs = was;
     }
 
+    f32x4 x[PT];
+#pragma unroll
+    for (int i = 0; i < PT; ++i) {
+        const int h = 4 * (i & 1);
+        x[i] = joined(f16x4{xh[i >> 1][h], xh[i >> 1][h + 1], xh[i >> 1][h + 2], xh[i >> 1][h + 3]},
+                      f16x4{xl[i >> 1][h], xl[i >> 1][h + 1], xl[i >> 1][h + 2], xl[i >> 1][h + 3]}) * (1.f / kScaleX);
+    }
     // to the caller, the weights in flight together
     const int step_r = tall ? 1 : io.ld, step_c = tall ? io.ld : 1;
     const int64_t from = base + (int64_t)min(own, q - 1) * step_c;
