@@ -25,21 +25,15 @@
 namespace crf {
 namespace {
 
-// Most workgroups (of 256 threads) that sum dgamma and dbeta: four a CU (5,000
-// sentences of d = 500: 114 us at 768, 100.5, 106 at 2,048).
-constexpr int kNormGroups = 1024;
+// Most workgroups of 256 threads, forward (24 paragraphs of d = 8,192: 60 us with
+// a workgroup for every four rows, 43 so) and backward, where each adds a share to
+// the sums that are joined: for rows within a wavefront (5,000 sentences of d =
+// 500: 98 us at 1,024 with two rows in flight, 95.6 at 1,280, 94.5), and for rows of
+// several (24 paragraphs of d = 4,096 in float32: 59.4 us, 73.2 at 1,280, 67.7 at
+// 1,536).
+constexpr int kNormMost = 2048, kNormMostBwd = 1536, kNormMostBwdWide = 1024;
 
 __host__ __device__ constexpr int norm_threads(int G) { return G > 256 ? G : 256; }
-
-// Forward a group of lanes has one row in flight and one under way, in at most so
-// many workgroups of 256 threads (24 paragraphs of d = 8,192: 60 us with a chunk a
-// workgroup, 43 so; two rows at 4,096 workgroups 45).
-constexpr int kNormMost = 2048;
-// Rows of a group of lanes in flight, backward: the registers of two cost
-// wavefronts where rows are float32 or meet in LDS (24 paragraphs of d = 4,096 in
-// float32 69.7 us with two, 61.6 with one; 5,000 sentences of d = 500 100.5 and 104).
-template <typename T, int G>
-constexpr int norm_unroll_bwd() { return sizeof(T) == 4 || G > 64 ? 1 : 2; }
 
 // Pieces of rows: bf16 rows start at multiples of 8 bytes, float32 ones of 4.
 typedef uint32_t u32x4_a8 __attribute__((ext_vector_type(4), aligned(8)));
@@ -137,27 +131,29 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *slots) {
     }
 }
 
-// Deviations from the mean (0 past d) and 1 / sqrt(variance + eps) of N rows.
-template <int G, int N>
-__device__ __forceinline__ void statistics(float (&f)[N][8], float (&r)[N], int k, int d, float eps, float (*slots)[N * 16]) {
+// 1 / sqrt(v) for v > 0: the instruction's value (off by 2^-23 at most) and a
+// Newton step, 8 instructions where the library's root and division take 40.  (v
+// below the least normal number is taken as that: deviations are all 0 then.)
+__device__ __forceinline__ float reciprocal_root(float v) {
+    v = v < 1.17549435e-38f ? 1.17549435e-38f : v;   // (a NaN stays one)
+    const float r = __builtin_amdgcn_rsqf(v);
+    return fmaf(0.5f * r, fmaf(-(v * r), r, 1.f), r);
+}
+
+// Deviations from the mean (0 past d) in place, and 1 / sqrt(variance + eps).
+template <int G>
+__device__ __forceinline__ float statistics(float (&f)[8], int k, int d, float eps, float (*slots)[16]) {
     const float each = 1.f / (float)d;
+    float s[1] = {((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]))};
+    row_sums<G, 1>(s, slots[0]);
+    const float m = s[0] * each, m0 = k < d ? m : 0.f, m1 = k + 4 < d ? m : 0.f;   // (entries past d are 0)
 #pragma unroll
-    for (int u = 0; u < N; ++u)
-        r[u] = ((f[u][0] + f[u][1]) + (f[u][2] + f[u][3])) + ((f[u][4] + f[u][5]) + (f[u][6] + f[u][7]));
-    row_sums<G, N>(r, slots[0]);
+    for (int q = 0; q < 8; ++q) f[q] -= q < 4 ? m0 : m1;
+    s[0] = 0.f;
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-        const float m = r[u] * each;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) f[u][q] = k + (q & 4) < d ? f[u][q] - m : 0.f;
-        float s = 0.f;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) s = fmaf(f[u][q], f[u][q], s);
-        r[u] = s;
-    }
-    row_sums<G, N>(r, slots[1]);
-#pragma unroll
-    for (int u = 0; u < N; ++u) r[u] = 1.f / sqrtf(fmaf(r[u], each, eps));
+    for (int q = 0; q < 8; ++q) s[0] = fmaf(f[q], f[q], s[0]);
+    row_sums<G, 1>(s, slots[1]);
+    return reciprocal_root(fmaf(s[0], each, eps));
 }
 
 // A lane's entries of gamma or beta (`none` where there is no array).
@@ -169,34 +165,25 @@ __device__ __forceinline__ void weights(const float *p, int k, int d, float none
     for (int q = 0; q < 8; ++q) f[q] = p != nullptr ? f[q] : none;
 }
 
-// Rows of a chunk: kBiaRows of a block of posts are a whole number of chunks.
-template <int G, int U>
-__device__ __forceinline__ const int32_t *chunk_ids(const int32_t *posts, int chunk) {
-    constexpr int kRows = norm_threads(G) / G * U, kChunks = kBiaRows / kRows;
-    static_assert(kBiaRows % kRows == 0, "a block of posts is a whole number of chunks");
-    return posts + (size_t)(chunk / kChunks) * kPostRec + chunk % kChunks * kRows + threadIdx.x / G * U;
-}
-
-// Rows of a workgroup's chunks, the next chunk's on their way while one is worked
-// on, and the ids of the one after it.
-template <int G, int U>
+// A workgroup's chunks of the rows, a row for each of its groups of lanes: the
+// next chunk's is on its way while one is worked on, and the id of the one after
+// it.
+template <int G>
 struct Ahead {
     const int32_t *posts;
-    int chunks, id[U], id1[U], id2[U];
-    __device__ __forceinline__ void ids_of(int (&to)[U], int c) {
-        const int32_t *ids = chunk_ids<G, U>(posts, min(c, chunks - 1));
-#pragma unroll
-        for (int u = 0; u < U; ++u) to[u] = c < chunks ? ids[u] : -1;
+    int chunks, id, id1, id2;
+    __device__ __forceinline__ int id_of(int chunk) const {
+        constexpr int kRows = norm_threads(G) / G, kChunks = kBiaRows / kRows;
+        static_assert(kBiaRows % kRows == 0, "a block of posts is a whole number of chunks");
+        const int c = min(chunk, chunks - 1);
+        const int v = posts[(size_t)(c / kChunks) * kPostRec + c % kChunks * kRows + threadIdx.x / G];
+        return chunk < chunks ? v : -1;
     }
     __device__ __forceinline__ Ahead(const int32_t *posts, int chunks) : posts(posts), chunks(chunks) {
-        ids_of(id1, blockIdx.x);
-        ids_of(id2, blockIdx.x + gridDim.x);
+        id1 = id_of(blockIdx.x);
+        id2 = id_of(blockIdx.x + gridDim.x);
     }
-    // chunk c's rows are taken; then the next one's are loaded
-    __device__ __forceinline__ void take() {
-#pragma unroll
-        for (int u = 0; u < U; ++u) id[u] = id1[u], id1[u] = id2[u];
-    }
+    __device__ __forceinline__ void take() { id = id1, id1 = id2; }
 };
 
 template <typename T, int G>
@@ -204,36 +191,28 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_kernel(const int32_t *__
                                                                const T *__restrict__ x, const float *__restrict__ gamma,
                                                                const float *__restrict__ beta, float eps,
                                                                uint16_t *__restrict__ y) {
-    constexpr int U = 1;
-    __shared__ float slots[2][U * 16];
+    __shared__ float slots[2][16];
     const int k = 8 * (threadIdx.x & (G - 1));
-    Ahead<G, U> rows(posts, chunks);
-    Raw<T> raw[U];
+    Ahead<G> rows(posts, chunks);
+    Raw<T> raw;
     auto load = [&]() {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            raw[u] = Raw<T>();
-            if (rows.id1[u] >= 0) raw[u].load(x + (size_t)rows.id1[u] * d, k, d);
-        }
+        raw = Raw<T>();
+        if (rows.id1 >= 0) raw.load(x + (size_t)rows.id1 * d, k, d);
     };
     load();
     float g[8], b[8];
     weights(gamma, k, d, 1.f, g);
     weights(beta, k, d, 0.f, b);
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        float f[U][8], r[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) raw[u].widen(f[u]);
+        float f[8];
+        raw.widen(f);
         rows.take();
         load();
-        rows.ids_of(rows.id2, c + 2 * gridDim.x);
-        statistics<G, U>(f, r, k, d, eps, slots);
+        rows.id2 = rows.id_of(c + 2 * gridDim.x);
+        const float r = statistics<G>(f, k, d, eps, slots);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) f[u][q] = fmaf(f[u][q] * r[u], g[q], b[q]);
-            if (rows.id[u] >= 0) store(y + (size_t)rows.id[u] * d, k, d, f[u]);
-        }
+        for (int q = 0; q < 8; ++q) f[q] = fmaf(f[q] * r, g[q], b[q]);
+        if (rows.id >= 0) store(y + (size_t)rows.id * d, k, d, f);
     }
 }
 
@@ -246,63 +225,51 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(const int32_t
                                                                    const uint16_t *__restrict__ dy, float eps,
                                                                    T *__restrict__ dx, float *__restrict__ parts,
                                                                    float *__restrict__ dgamma, float *__restrict__ dbeta) {
-    constexpr int U = norm_unroll_bwd<T, G>(), kRows = norm_threads(G) / G;
-    __shared__ float slots[2][U * 16], slots2[2 * U * 16];
+    constexpr int kRows = norm_threads(G) / G;
+    __shared__ float slots[2][16], slots2[2 * 16];
     __shared__ float sums[PARTS && kRows > 1 ? kRows * 16 * G : 1];
-    const int lane = threadIdx.x & (G - 1), k = 8 * lane;
+    const int k = 8 * (threadIdx.x & (G - 1));
     const float each = 1.f / (float)d;
     float g[8], sg[8], sb[8];
     weights(gamma, k, d, 1.f, g);
 #pragma unroll
     for (int q = 0; q < 8; ++q) sg[q] = sb[q] = 0.f;
-    Ahead<G, U> rows(posts, chunks);
-    Raw<T> raw[U];
-    Raw<uint16_t> up[U];
+    Ahead<G> rows(posts, chunks);
+    Raw<T> raw;
+    Raw<uint16_t> up;
     auto load = [&]() {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            raw[u] = Raw<T>();
-            up[u] = Raw<uint16_t>();
-            if (rows.id1[u] >= 0) {
-                raw[u].load(x + (size_t)rows.id1[u] * d, k, d);
-                up[u].load(dy + (size_t)rows.id1[u] * d, k, d);
-            }
+        raw = Raw<T>();
+        up = Raw<uint16_t>();
+        if (rows.id1 >= 0) {
+            raw.load(x + (size_t)rows.id1 * d, k, d);
+            up.load(dy + (size_t)rows.id1 * d, k, d);
         }
     };
     load();
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        float f[U][8], r[U], e[U][8], two[2 * U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) raw[u].widen(f[u]), up[u].widen(e[u]);
+        float f[8], e[8], two[2] = {0.f, 0.f};
+        raw.widen(f);
+        up.widen(e);
         rows.take();
         load();
-        rows.ids_of(rows.id2, c + 2 * gridDim.x);
-        statistics<G, U>(f, r, k, d, eps, slots);
+        rows.id2 = rows.id_of(c + 2 * gridDim.x);
+        const float r = statistics<G>(f, k, d, eps, slots);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float s = 0.f, t = 0.f;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                f[u][q] *= r[u];
-                if constexpr (PARTS) {   // (a row that is not there adds zeros)
-                    sg[q] = fmaf(e[u][q], f[u][q], sg[q]);
-                    sb[q] += e[u][q];
-                }
-                e[u][q] *= g[q];
-                s += e[u][q];
-                t = fmaf(e[u][q], f[u][q], t);
+        for (int q = 0; q < 8; ++q) {
+            f[q] *= r;
+            if constexpr (PARTS) {   // (a row that is not there adds zeros)
+                sg[q] = fmaf(e[q], f[q], sg[q]);
+                sb[q] += e[q];
             }
-            two[2 * u] = s;
-            two[2 * u + 1] = t;
+            e[q] *= g[q];
+            two[0] += e[q];
+            two[1] = fmaf(e[q], f[q], two[1]);
         }
-        row_sums<G, 2 * U>(two, slots2);
+        row_sums<G, 2>(two, slots2);
+        const float s = -r * (two[0] * each), t = -r * (two[1] * each);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const float s = two[2 * u] * each, t = two[2 * u + 1] * each;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) f[u][q] = r[u] * (e[u][q] - s - f[u][q] * t);
-            if (dx != nullptr && rows.id[u] >= 0) store(dx + (size_t)rows.id[u] * d, k, d, f[u]);
-        }
+        for (int q = 0; q < 8; ++q) f[q] = fmaf(f[q], t, fmaf(e[q], r, s));
+        if (dx != nullptr && rows.id >= 0) store(dx + (size_t)rows.id * d, k, d, f);
     }
     if constexpr (PARTS) {
         if constexpr (kRows > 1) {
@@ -362,13 +329,18 @@ int norm_lanes(int d) {
     while (8 * g < d) g *= 2;
     return g;
 }
-int norm_chunks(const KernelPlan &p, int G, int U) { return p.n_posts * (kBiaRows / (norm_threads(G) / G * U)); }
-int norm_parts(int chunks, int G) { return std::min(chunks, kNormGroups * 256 / norm_threads(G)); }
+int norm_chunks(const KernelPlan &p, int G) { return p.n_posts * (kBiaRows / (norm_threads(G) / G)); }
+// Workgroups that share the sums: two chunks each at least, where there are many
+// (200 sentences of d = 500: 15.4 us with one, 14.5 with two, 15.6 with three).
+int norm_parts(const KernelPlan &p, int G) {
+    const int chunks = norm_chunks(p, G), most = (G > 64 ? kNormMostBwdWide : kNormMostBwd) * 256 / norm_threads(G);
+    return std::min(std::max(std::min(chunks, 512), chunks / 2), most);
+}
 
 template <typename T, int G>
 void launch_norm_g(const KernelPlan &p, const void *x, int d, const float *gamma, const float *beta, float eps, uint16_t *y,
                    hipStream_t stream) {
-    const int chunks = norm_chunks(p, G, 1);
+    const int chunks = norm_chunks(p, G);
     hipLaunchKernelGGL((norm_kernel<T, G>), dim3(std::min(chunks, kNormMost * 256 / norm_threads(G))), dim3(norm_threads(G)),
                        0, stream, p.posts, chunks, d, static_cast<const T *>(x), gamma, beta, eps, y);
 }
@@ -376,13 +348,13 @@ void launch_norm_g(const KernelPlan &p, const void *x, int d, const float *gamma
 template <typename T, int G>
 void launch_norm_bwd_g(const KernelPlan &p, const void *x, int d, const float *gamma, const uint16_t *dy, float eps,
                        void *dx, float *dgamma, float *dbeta, float *parts, hipStream_t stream) {
-    const int chunks = norm_chunks(p, G, norm_unroll_bwd<T, G>());
+    const int chunks = norm_chunks(p, G), count = norm_parts(p, G);
     if (dgamma == nullptr && dbeta == nullptr) {
-        hipLaunchKernelGGL((norm_bwd_kernel<T, G, false>), dim3(chunks), dim3(norm_threads(G)), 0, stream, p.posts, chunks,
-                           d, static_cast<const T *>(x), gamma, dy, eps, static_cast<T *>(dx), nullptr, nullptr, nullptr);
+        hipLaunchKernelGGL((norm_bwd_kernel<T, G, false>), dim3(std::min(chunks, kNormMost * 256 / norm_threads(G))),
+                           dim3(norm_threads(G)), 0, stream, p.posts, chunks, d, static_cast<const T *>(x), gamma, dy, eps,
+                           static_cast<T *>(dx), nullptr, nullptr, nullptr);
         return;
     }
-    const int count = norm_parts(chunks, G);
     hipLaunchKernelGGL((norm_bwd_kernel<T, G, true>), dim3(count), dim3(norm_threads(G)), 0, stream, p.posts, chunks, d,
                        static_cast<const T *>(x), gamma, dy, eps, static_cast<T *>(dx), parts, dgamma, dbeta);
     if (count > 1)
@@ -405,7 +377,7 @@ void launch_norm_bwd_g(const KernelPlan &p, const void *x, int d, const float *g
 
 int64_t norm_bwd_bytes(const KernelPlan &p, int d) {
     const int G = norm_lanes(d);
-    return ((int64_t)norm_parts(norm_chunks(p, G, 1), G) * 16 * G * 4 + 255) / 256 * 256;   // (of either type)
+    return ((int64_t)norm_parts(p, G) * 16 * G * 4 + 255) / 256 * 256;
 }
 
 hipError_t launch_norm(const KernelPlan &p, const void *x, bool f32, int d, const float *gamma, const float *beta,
