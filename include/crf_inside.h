@@ -484,8 +484,9 @@ int crf_biaffine_bwd_packed(const crf_plan *plan, const uint8_t *rl_codes, const
  *   gamma, beta  device float32[d], or NULL: 1 and 0.
  *   eps     positive.
  *   y       device bf16 bit patterns [B][N1][d], 8-byte aligned; must not alias x.
- * A row with an infinity or NaN becomes NaN, other rows are as without it.  Rows
- * past n_b are left as they were.  B, N1 and the lengths are the plan's.
+ * A row with an infinity or NaN, or whose sum of squared deviations passes what
+ * float32 holds, becomes NaN, other rows are as without it.  Rows past n_b are
+ * left as they were.  B, N1 and the lengths are the plan's.
  */
 int crf_layer_norm(const crf_plan *plan, const void *x, int32_t x_type, int32_t d, const float *gamma, const float *beta,
                    float eps, uint16_t *y, void *stream);

@@ -165,6 +165,50 @@ def test_one_row_is_not_finite(torch, d, bad):
     assert torch.equal(back[2], sore[2])
 
 
+def test_squares_past_float32(torch):
+    # finite entries whose squared deviations sum to more than float32 holds: the
+    # row says so, the others are as without it
+    raw, _ = values(LENGTHS, N1, 100, 16, True)
+    hurt = raw.copy()
+    hurt[2, 7, 3] = 1e25
+    with B.Plan(LENGTHS, n1=N1, device="cuda:0") as plan:
+        clean, got = (plan.layer_norm(device(torch, v)) for v in (raw, hurt))
+    assert torch.isnan(got[2, 7]).all()
+    got[2, 7] = clean[2, 7]
+    assert torch.equal(clean, got)
+
+
+def test_offsets_past_32_bits(torch):
+    # 2.2e9 entries in all, 4.4 GB of bf16; the last sentence is checked
+    lengths, n1, d = [1] * 549 + [1000], 1001, 4000
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    x = torch.zeros((550, n1, d), dtype=torch.bfloat16, device="cuda:0")
+    assert x.numel() > 1 << 31
+    raw, want = values([1000], n1, d, 17, False)
+    bits, dy = values([1000], n1, d, 18, False)
+    x[-1] = device(torch, raw)[0]
+    up = torch.zeros_like(x)
+    up[-1] = device(torch, bits)[0]
+    eps = float(np.float32(1e-5))
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        y = plan.layer_norm(x)[-1].float().cpu().numpy()
+        dx, dg, db = plan.layer_norm_bwd(x, None, up)
+        dx = dx[-1].float().cpu().numpy()
+    h, r, t, off = statistics(want[0], eps)
+    check(y, h, t + 3 * U * np.abs(h) + rounded(h, False))
+    mean = lambda v: v.mean(-1, keepdims=True)
+    u = dy[0]
+    s, q = mean(u), mean(u * h)
+    e1, e2 = 27 * U * mean(np.abs(u)), 27 * U * mean(np.abs(u * h)) + mean(np.abs(u) * t)
+    tol = r * (3 * U * np.abs(u) + e1 + np.abs(h) * e2 + t * np.abs(q) + 4 * U * (np.abs(s) + np.abs(h * q)))
+    grad = r * (u - s - h * q)
+    check(dx, grad, tol + np.abs(grad) * off + rounded(grad, False))
+    rows = 1001 + 2 * 549
+    check(db.cpu(), u.sum(0), rows * U * np.abs(u).sum(0))
+    check(dg.cpu(), (u * h).sum(0), (np.abs(u) * t).sum(0) + rows * U * np.abs(u * h).sum(0))
+
+
 def test_gradient_by_differences(torch):
     lengths, n1, d = [4, 2], 6, 24
     _, x = values(lengths, n1, d, 8, True, offset=0.0)

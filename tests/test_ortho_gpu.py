@@ -185,6 +185,21 @@ def test_muon_step(torch, shape, nesterov):
         assert off <= rate * tolerance(u, B.MUON_STEPS, 1e-7) + 2.0 ** -22 * np.linalg.norm(wq)
 
 
+@pytest.mark.parametrize("rows,cols,ld", [(40, 50, 30_000_000), (200, 190, 6_000_000)])
+def test_offsets_past_32_bits(torch, rows, cols, ld):
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB")
+    x = torch.zeros((2, rows, ld), device="cuda:0")
+    assert x.numel() > 1 << 31
+    m = matrices(2, rows, cols, cols, 9)
+    x[:, :, :cols] = torch.from_numpy(m).to("cuda:0")
+    out = torch.full_like(x, 2.0)
+    B.orthogonalize(x, cols=cols, out=out)
+    assert bool((out[:, :, cols:cols + 1000] == 2.0).all()) and bool((out[:, :, -1000:] == 2.0).all())
+    for q in range(2):
+        check(out[q, :, :cols].cpu().numpy(), m[q], B.MUON_STEPS, float(np.float32(1e-7)))
+
+
 def test_two_dimensions_streams_and_graphs(torch):
     x = [torch.from_numpy(matrices(1, r, c, c, k)[0]).to("cuda:0") for k, (r, c) in enumerate(((90, 101), (300, 260)))]
     want = [B.orthogonalize(v) for v in x]
