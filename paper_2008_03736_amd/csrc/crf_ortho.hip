@@ -538,21 +538,27 @@ void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int co
         hipLaunchKernelGGL((ortho_tile_kernel<KIND, 2>), grid, dim3(256), staged_bytes<2>(), stream, g, io);
 }
 
-// Matrices of up to kSmall x kSmall: a workgroup of W wavefronts each, which never
-// leaves its CU.  Wavefront w owns X's columns 16 w .. + 15, in registers.  Their
-// parts are wanted twice over: in LDS, as rows of X, for the Gram matrix, and in
-// the owner's registers as the right operand of B X -- a product's result has, a
-// lane, four consecutive rows of one column, and two tiles of it are just a right
-// operand's fragment whose K runs 0-3, 16-19 | 4-7, 20-23 | ...; the Gram matrix
-// and B are stored with their columns in that order, so that no product minds.
-// A and B are symmetric: of the tiles (i, j) and (j, i) one is computed, column
-// j taking rows j, j + 1 .. j + PT / 2 (cyclically), which shares the work
-// evenly.
-constexpr int kSmall = 128;
+// Matrices whose parts fit LDS twice over: a workgroup of W wavefronts each, which
+// never leaves its CU.  Wavefront w owns C of X's tiles of 16 columns, w, w + W ..,
+// in registers.  Their parts are wanted twice over: in LDS, as rows of X, for the
+// Gram matrix, and in the owner's registers as the right operand of B X -- a
+// product's result has, a lane, four consecutive rows of one column, and two
+// tiles of it are just a right operand's fragment whose K runs 0-3, 16-19 | 4-7,
+// 20-23 | ...; the Gram matrix and B are stored with their columns in that order,
+// so that no product minds.  A and B are symmetric: of the tiles (i, j) and (j, i)
+// one is computed, column j taking rows j, j + 1 .. j + PT / 2 (cyclically), which
+// shares the work evenly.
+constexpr int kSmallRows = 128;
 __host__ __device__ constexpr int small_stride(int tiles) { return (tiles + 1) / 2 * 32 + 8; }   // of a row of 16 `tiles`
 inline int64_t small_lds(int p, int q) {
     const int pt = (p + 15) / 16, qt = (q + 15) / 16;
     return std::max<int64_t>(2 * 2 * 2 * 16 * pt * (int64_t)small_stride(qt), 4 * (int64_t)q * (p + 1));
+}
+// Column tiles of a wavefront of eight, for `pt` row tiles at most.
+constexpr int small_most(int pt) { return pt == 1 ? 8 : pt <= 3 ? 4 : pt <= 7 ? 2 : 1; }
+inline bool is_small(int rows, int cols) {
+    const int p = std::min(rows, cols), q = std::max(rows, cols);
+    return p <= kSmallRows && (q + 127) / 128 <= small_most((p + 15) / 16) && small_lds(p, q) <= 160 * 1024 - 256;
 }
 
 struct Steps {
@@ -599,10 +605,10 @@ __device__ __forceinline__ void row_tiles(const _Float16 *from, int plane, int s
     done(U - 1, sum(U - 1));
 }
 
-template <int PT, int W>
+template <int PT, int W, int C>
 __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps steps) {
-    constexpr int kKP = (PT + 1) / 2;   // steps of K over p
-    constexpr int kKQ = W / 2;          // most steps of K over q
+    constexpr int kKP = (PT + 1) / 2;          // steps of K over p
+    constexpr int kKQ = C == 1 ? W / 2 : 4;    // of K over q at a time
     constexpr int kT = PT / 2 + 1;      // row tiles of a column of A and B
     constexpr int kSG = small_stride(PT);
     constexpr int kThreads = 64 * W;
@@ -660,9 +666,9 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
     for (int w = 1; w < W; ++w) sum += norm[w];
     // (a sum that is not finite makes the whole matrix NaN)
     const double inv = 1.0 / (sqrt(sum) + (double)io.eps) + 0.0 * sum;
-    // X's parts, tile i: rows 16 i + 4 g .. + 3 of column own
-    f16x8 xh[kKP], xl[kKP];
-    const int own = 16 * wave + n;
+    // X's parts, tile (i, c): rows 16 i + 4 g .. + 3 of column 16 tile(c) + n
+    f16x8 xh[C][kKP], xl[C][kKP];
+    auto tile = [&](int c) { return c * W + wave; };
     auto set = [&](f16x8 (&hi8)[kKP], f16x8 (&lo8)[kKP], int i, const f16x4 &hi, const f16x4 &lo) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -670,40 +676,44 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
             lo8[i >> 1][4 * (i & 1) + t] = lo[t];
         }
     };
+    auto get = [&](const f16x8 (&v)[kKP], int i) {
+        const int h = 4 * (i & 1);
+        return f16x4{v[i >> 1][h], v[i >> 1][h + 1], v[i >> 1][h + 2], v[i >> 1][h + 3]};
+    };
 #pragma unroll
-    for (int i = 0; i < 2 * kKP; ++i) {
-        f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int r = 16 * i + 4 * g + t, row = min(r, p - 1), at = min(own, q - 1);
-            const float u = (float)((double)us[tall ? at * us_stride + row : row * us_stride + at] * inv);
-            x[t] = r < p && own < q ? u : 0.f;
+        for (int i = 0; i < 2 * kKP; ++i) {
+            f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int r = 16 * i + 4 * g + t, col = 16 * tile(c) + n, row = min(r, p - 1), at = min(col, q - 1);
+                const float u = (float)((double)us[tall ? at * us_stride + row : row * us_stride + at] * inv);
+                x[t] = r < p && col < q ? u : 0.f;
+            }
+            f16x4 hi, lo;
+            split(kScaleX * x, hi, lo);
+            set(xh[c], xl[c], i, hi, lo);
         }
-        f16x4 hi, lo;
-        split(kScaleX * x, hi, lo);
-        set(xh, xl, i, hi, lo);
-    }
     __syncthreads();
     // (what lies past the tiles in the last step of K is multiplied by zeros, so it has to be finite)
     for (int k = tid; k < 4 * x_plane / 8; k += kThreads) reinterpret_cast<u32x4 *>(xs)[k] = u32x4{0u, 0u, 0u, 0u};
     __syncthreads();
     // a tile's parts into the rows of X
-    auto put_x = [&](_Float16 *to, int i, const f16x4 &hi, const f16x4 &lo) {
-        to += (16 * i + 4 * g) * sx + 16 * wave + n;
+    auto put_x = [&](_Float16 *to, int i, int c, const f16x4 &hi, const f16x4 &lo) {
+        to += (16 * i + 4 * g) * sx + 16 * tile(c) + n;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             to[t * sx] = hi[t];
             to[x_plane + t * sx] = lo[t];
         }
     };
-    if (wave < qt) {
 #pragma unroll
-        for (int i = 0; i < PT; ++i) {
-            const int h = 4 * (i & 1);
-            put_x(xs, i, f16x4{xh[i >> 1][h], xh[i >> 1][h + 1], xh[i >> 1][h + 2], xh[i >> 1][h + 3]},
-                  f16x4{xl[i >> 1][h], xl[i >> 1][h + 1], xl[i >> 1][h + 2], xl[i >> 1][h + 3]});
+    for (int c = 0; c < C; ++c)
+        if (tile(c) < qt) {
+#pragma unroll
+            for (int i = 0; i < PT; ++i) put_x(xs, i, c, get(xh[c], i), get(xl[c], i));
         }
-    }
     __syncthreads();
 
     // X lies in xs; A goes to gs, B to xs, and the new X to gs: each is read by all
@@ -741,17 +751,46 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
         // A = X X^T
         if (j < PT) {
             f16x8 rh[kKQ], rl[kKQ];
+            auto columns = [&](int s0) {
 #pragma unroll
-            for (int s = 0; s < kKQ; ++s)
-                if (s < kq) {
-                    const _Float16 *from = xs + (16 * j + n) * sx + 32 * s + 8 * g;
-                    rh[s] = frag(from);
-                    rl[s] = frag(from + x_plane);
-                    if (2 * s + 1 == qt && g >= 2) rh[s] = rl[s] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
-                }
-            row_tiles<kT>(xs + n * sx + 8 * g, x_plane, sx, kq, rh, rl, row_tile, [&](int u, const f32x4 &acc) {
+                for (int s = 0; s < kKQ; ++s)
+                    if (s0 + s < kq) {
+                        const _Float16 *from = xs + (16 * j + n) * sx + 32 * (s0 + s) + 8 * g;
+                        rh[s] = frag(from);
+                        rl[s] = frag(from + x_plane);
+                        if (2 * (s0 + s) + 1 == qt && g >= 2) rh[s] = rl[s] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                    }
+            };
+            auto done = [&](int u, const f32x4 &acc) {
                 if (wanted(u)) put(gs, u, acc * (kScaleA / (kScaleX * kScaleX)));
-            });
+            };
+            if constexpr (C == 1) {
+                columns(0);
+                row_tiles<kT>(xs + n * sx + 8 * g, x_plane, sx, kq, rh, rl, row_tile, done);
+            } else {   // all row tiles' sums together, kKQ steps of K at a time
+                f32x4 acc[kT][3];
+#pragma unroll
+                for (int u = 0; u < kT; ++u)
+#pragma unroll
+                    for (int t = 0; t < 3; ++t) acc[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int s0 = 0; s0 < kq; s0 += kKQ) {
+                    columns(s0);
+#pragma unroll
+                    for (int u = 0; u < kT; ++u)
+#pragma unroll
+                        for (int s = 0; s < kKQ; ++s)
+                            if (s0 + s < kq) {
+                                const _Float16 *at = xs + (16 * row_tile(u) + n) * sx + 32 * (s0 + s) + 8 * g;
+                                const f16x8 lh = frag(at), ll = frag(at + x_plane);
+                                acc[u][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh, rl[s], acc[u][0], 0, 0, 0);
+                                acc[u][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ll, rh[s], acc[u][1], 0, 0, 0);
+                                acc[u][2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh, rh[s], acc[u][2], 0, 0, 0);
+                            }
+                }
+#pragma unroll
+                for (int u = 0; u < kT; ++u) done(u, (acc[u][0] + acc[u][1]) + acc[u][2]);
+            }
         }
         __syncthreads();
 
@@ -784,16 +823,51 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
 
         // X <- B X, in the owner's registers
         if (wave < qt) {
-            f16x8 nh[kKP], nl[kKP];
-            if constexpr (PT % 2 != 0) set(nh, nl, PT, f16x4{0, 0, 0, 0}, f16x4{0, 0, 0, 0});
-            row_tiles<PT>(xs + n * kSG + 8 * g, g_plane, kSG, kKP, xh, xl, [](int i) { return i; }, [&](int i, const f32x4 &acc) {
+            f16x8 nh[C][kKP], nl[C][kKP];
+            auto done = [&](int i, int c, const f32x4 &acc) {
                 f16x4 hi, lo;
                 split(acc * (1.f / kScaleB), hi, lo);
-                set(nh, nl, i, hi, lo);
-                put_x(gs, i, hi, lo);
-            });
+                set(nh[c], nl[c], i, hi, lo);
+                put_x(gs, i, c, hi, lo);
+            };
+            if constexpr (PT % 2 != 0) {
 #pragma unroll
-            for (int s = 0; s < kKP; ++s) xh[s] = nh[s], xl[s] = nl[s];
+                for (int c = 0; c < C; ++c) set(nh[c], nl[c], PT, f16x4{0, 0, 0, 0}, f16x4{0, 0, 0, 0});
+            }
+            if constexpr (C == 1) {
+                row_tiles<PT>(xs + n * kSG + 8 * g, g_plane, kSG, kKP, xh[0], xl[0], [](int i) { return i; },
+                              [&](int i, const f32x4 &acc) { done(i, 0, acc); });
+            } else {   // a row tile of B for all of the wavefront's columns
+#pragma unroll
+                for (int i = 0; i < PT; ++i) {
+                    f16x8 lh[kKP], ll[kKP];
+#pragma unroll
+                    for (int s = 0; s < kKP; ++s) {
+                        const _Float16 *at = xs + (16 * i + n) * kSG + 32 * s + 8 * g;
+                        lh[s] = frag(at);
+                        ll[s] = frag(at + g_plane);
+                    }
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        f32x4 acc[3];
+#pragma unroll
+                        for (int t = 0; t < 3; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int s = 0; s < kKP; ++s) {
+                            acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[s], xl[c][s], acc[0], 0, 0, 0);
+                            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ll[s], xh[c][s], acc[1], 0, 0, 0);
+                            acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[s], xh[c][s], acc[2], 0, 0, 0);
+                        }
+                        if (tile(c) < qt) done(i, c, (acc[0] + acc[1]) + acc[2]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (tile(c) < qt) {
+#pragma unroll
+                    for (int s = 0; s < kKP; ++s) xh[c][s] = nh[c][s], xl[c][s] = nl[c][s];
+                }
         }
         __syncthreads();
         _Float16 *was = xs;
@@ -801,43 +875,49 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
         gs = was;
     }
 
-    f32x4 x[PT];
-#pragma unroll
-    for (int i = 0; i < PT; ++i) {
-        const int h = 4 * (i & 1);
-        x[i] = joined(f16x4{xh[i >> 1][h], xh[i >> 1][h + 1], xh[i >> 1][h + 2], xh[i >> 1][h + 3]},
-                      f16x4{xl[i >> 1][h], xl[i >> 1][h + 1], xl[i >> 1][h + 2], xl[i >> 1][h + 3]}) * (1.f / kScaleX);
-    }
-    // to the caller, the weights in flight together
+    // to the caller, a column tile's weights in flight together
     const int step_r = tall ? 1 : io.ld, step_c = tall ? io.ld : 1;
-    const int64_t from = base + (int64_t)min(own, q - 1) * step_c;
-    f32x4 w[PT];
-    if (io.w != nullptr) {
 #pragma unroll
-        for (int i = 0; i < PT; ++i)
+    for (int c = 0; c < C; ++c) {
+        const int own = 16 * tile(c) + n;
+        const int64_t from = base + (int64_t)min(own, q - 1) * step_c;
+        f32x4 x[PT], w[PT];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) w[i][t] = io.w[from + (int64_t)min(16 * i + 4 * g + t, p - 1) * step_r];
+        for (int i = 0; i < PT; ++i) x[i] = joined(get(xh[c], i), get(xl[c], i)) * (1.f / kScaleX);
+        if (io.w != nullptr) {
 #pragma unroll
-        for (int i = 0; i < PT; ++i) x[i] = io.keep * w[i] - io.rate * x[i];
-    }
-    if (own < q) {
+            for (int i = 0; i < PT; ++i)
 #pragma unroll
-        for (int i = 0; i < PT; ++i)
+                for (int t = 0; t < 4; ++t) w[i][t] = io.w[from + (int64_t)min(16 * i + 4 * g + t, p - 1) * step_r];
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (16 * i + 4 * g + t < p) io.out[from + (int64_t)(16 * i + 4 * g + t) * step_r] = x[i][t];
+            for (int i = 0; i < PT; ++i) x[i] = io.keep * w[i] - io.rate * x[i];
+        }
+        if (own < q) {
+#pragma unroll
+            for (int i = 0; i < PT; ++i)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (16 * i + 4 * g + t < p) io.out[from + (int64_t)(16 * i + 4 * g + t) * step_r] = x[i][t];
+        }
     }
 }
 
+template <int PT, int W, int C>
+void launch_small_c(const OrthoIo &io, const Steps &steps, int count, hipStream_t stream) {
+    hipLaunchKernelGGL((ortho_small_kernel<PT, W, C>), dim3(count), dim3(64 * W),
+                       (size_t)small_lds(std::min(io.rows, io.cols), std::max(io.rows, io.cols)), stream, io, steps);
+}
 template <int PT>
 void launch_small(const OrthoIo &io, const Steps &steps, int count, hipStream_t stream) {
-    const int p = std::min(io.rows, io.cols), q = std::max(io.rows, io.cols);
+    const int q = std::max(io.rows, io.cols);
     if constexpr (PT <= 4)
-        if (q <= 64) {
-            hipLaunchKernelGGL((ortho_small_kernel<PT, 4>), dim3(count), dim3(256), (size_t)small_lds(p, q), stream, io, steps);
-            return;
-        }
-    hipLaunchKernelGGL((ortho_small_kernel<PT, 8>), dim3(count), dim3(512), (size_t)small_lds(p, q), stream, io, steps);
+        if (q <= 64) return launch_small_c<PT, 4, 1>(io, steps, count, stream);
+    if (q <= 128) return launch_small_c<PT, 8, 1>(io, steps, count, stream);
+    if constexpr (small_most(PT) >= 2)
+        if (q <= 256) return launch_small_c<PT, 8, 2>(io, steps, count, stream);
+    if constexpr (small_most(PT) >= 4)
+        if (q <= 512) return launch_small_c<PT, 8, 4>(io, steps, count, stream);
+    if constexpr (small_most(PT) >= 8) launch_small_c<PT, 8, 8>(io, steps, count, stream);
 }
 
 int64_t aligned(int64_t n) { return (n + 255) / 256 * 256; }
@@ -849,13 +929,19 @@ hipError_t tile_attribute() {
 }
 template <int PT>
 hipError_t small_attribute() {
-    const int most = (int)small_lds(16 * PT, kSmall);
-    if constexpr (PT <= 4) {
-        const hipError_t e = hipFuncSetAttribute((const void *)ortho_small_kernel<PT, 4>,
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, most);
-        if (e != hipSuccess) return e;
-    }
-    return hipFuncSetAttribute((const void *)ortho_small_kernel<PT, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    auto set = [](const void *f) {
+        return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - 256);
+    };
+    hipError_t e = set((const void *)ortho_small_kernel<PT, 8, 1>);
+    if constexpr (PT <= 4)
+        if (e == hipSuccess) e = set((const void *)ortho_small_kernel<PT, 4, 1>);
+    if constexpr (small_most(PT) >= 2)
+        if (e == hipSuccess) e = set((const void *)ortho_small_kernel<PT, 8, 2>);
+    if constexpr (small_most(PT) >= 4)
+        if (e == hipSuccess) e = set((const void *)ortho_small_kernel<PT, 8, 4>);
+    if constexpr (small_most(PT) >= 8)
+        if (e == hipSuccess) e = set((const void *)ortho_small_kernel<PT, 8, 8>);
+    return e;
 }
 
 }  // namespace
@@ -871,7 +957,7 @@ hipError_t set_ortho_attributes() {
 }
 
 int64_t ortho_bytes(int count, int rows, int cols) {
-    if (std::max(rows, cols) <= kSmall) return 256;
+    if (is_small(rows, cols)) return 256;
     const OrthoShape sh = ortho_shape(rows, cols);
     return aligned(8 * (int64_t)count * norm_shares(rows, cols)) + 2 * aligned(4 * count * sh.x_plane()) +
            2 * aligned(4 * count * sh.xt_plane()) + 2 * aligned(4 * count * sh.a_plane());
@@ -882,7 +968,7 @@ hipError_t launch_ortho(const float *grad, const float *momentum, const float *w
                         const float *coefficients, int steps, char *ws, hipStream_t stream) {
     const OrthoShape sh = ortho_shape(rows, cols);
     OrthoIo io{grad, momentum, w, momentum_out, out, rows, cols, ld, mu, nesterov, keep, rate, eps};
-    if (std::max(rows, cols) <= kSmall) {
+    if (is_small(rows, cols)) {
         Steps all;
         all.count = steps;
         for (int k = 0; k < steps; ++k)

@@ -87,7 +87,9 @@ SHAPES = [(1, 1, 1, 1), (1, 1, 9, 9), (2, 9, 1, 3), (3, 2, 3, 5), (1, 15, 16, 16
           (3, 33, 31, 40), (2, 64, 64, 64), (3, 63, 65, 68), (7, 100, 101, 104), (2, 101, 100, 100), (2, 112, 128, 128),
           (2, 128, 128, 130), (2, 128, 129, 132), (1, 129, 127, 127), (2, 40, 300, 304), (1, 300, 40, 41), (1, 7, 1000, 1000),
           (1, 500, 501, 504), (1, 512, 512, 512), (1, 513, 260, 263), (1, 700, 1030, 1030), (40, 20, 130, 130),
-          (9, 200, 300, 300), (1, 2, 8192, 8192), (1, 1537, 1030, 1030), (3, 1025, 1290, 1290)]
+          (9, 200, 300, 300), (3, 1, 1024, 1024), (2, 16, 1007, 1007), (2, 1024, 15, 17), (2, 17, 513, 513), (3, 32, 500, 500),
+          (2, 257, 31, 31), (2, 48, 400, 401), (1, 417, 48, 48), (2, 64, 256, 256), (2, 64, 257, 257), (1, 80, 241, 241),
+          (2, 190, 95, 95), (2, 112, 160, 160), (1, 112, 161, 161), (2, 128, 129, 129), (1, 2, 8192, 8192), (1, 1537, 1030, 1030), (3, 1025, 1290, 1290)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
@@ -154,7 +156,7 @@ def test_zeros_and_what_is_not_finite(torch, shape):
 
 @pytest.mark.parametrize("nesterov", [True, False])
 @pytest.mark.parametrize("shape", [(1, 1, 1, 1), (5, 20, 21, 24), (7, 100, 101, 104), (1, 300, 200, 200), (1, 500, 501, 504),
-                                   (2, 40, 300, 304), (3, 200, 60, 64), (1, 129, 190, 191), (1, 257, 330, 330),
+                                   (2, 40, 300, 304), (3, 200, 60, 64), (2, 12, 700, 703), (2, 300, 70, 72), (1, 129, 190, 191), (1, 257, 330, 330),
                                    (9, 260, 500, 500), (2, 1030, 1100, 1101)])
 def test_muon_step(torch, shape, nesterov):
     count, rows, cols, ld = shape
