@@ -513,10 +513,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ?
 }
 
 // The largest tile of which there are kEnoughTiles (half the CUs), or the least:
-// per step, one matrix of 768 x 768 30 us in tiles of 32 (34 of 64), of 1,024 x
-// 1,024 43 of 64 (47 of 32, 84 of 128), of 1,024 x 4,096 98 of 64 (150 of 128),
-// 16 of 500 x 501 75 of 128 (81 of 64, 99 of 32), one of 2,048 x 2,048 165 of 128
-// (179 of 64, 249 of 32).
+// five steps of one matrix of 640 x 640 take 110 us in tiles of 32 (134 of 64), of
+// 1,024 x 1,024 183 of 64 (215 of 32, 331 of 128), of 1,536 x 1,536 418 of 128 for
+// two products and 64 for the symmetric two (431 of 64, 450 of 128), of 2,048 x
+// 2,048 707 of 128 (814 of 64, 1,254 of 32), 16 of 512 x 512 353 of 128 (392 of 64,
+// 443 of 32).
 constexpr int kEnoughTiles = 128;
 template <int KIND>
 void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int cols, int count, hipStream_t stream) {
