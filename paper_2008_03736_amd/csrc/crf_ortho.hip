@@ -822,54 +822,22 @@ __global__ __launch_bounds__(64 * W) void ortho_small_kernel(OrthoIo io, Steps s
         }
         __syncthreads();
 
-        // X <- B X, in the owner's registers
-        if (wave < qt) {
-            f16x8 nh[C][kKP], nl[C][kKP];
-            auto done = [&](int i, int c, const f32x4 &acc) {
-                f16x4 hi, lo;
-                split(acc * (1.f / kScaleB), hi, lo);
-                set(nh[c], nl[c], i, hi, lo);
-                put_x(gs, i, c, hi, lo);
-            };
-            if constexpr (PT % 2 != 0) {
+        // X <- B X, in the owner's registers, a column tile at a time
 #pragma unroll
-                for (int c = 0; c < C; ++c) set(nh[c], nl[c], PT, f16x4{0, 0, 0, 0}, f16x4{0, 0, 0, 0});
+        for (int c = 0; c < C; ++c)
+            if (tile(c) < qt) {
+                f16x8 nh[kKP], nl[kKP];
+                if constexpr (PT % 2 != 0) set(nh, nl, PT, f16x4{0, 0, 0, 0}, f16x4{0, 0, 0, 0});
+                row_tiles<PT>(xs + n * kSG + 8 * g, g_plane, kSG, kKP, xh[c], xl[c], [](int i) { return i; },
+                              [&](int i, const f32x4 &acc) {
+                                  f16x4 hi, lo;
+                                  split(acc * (1.f / kScaleB), hi, lo);
+                                  set(nh, nl, i, hi, lo);
+                                  put_x(gs, i, c, hi, lo);
+                              });
+#pragma unroll
+                for (int s = 0; s < kKP; ++s) xh[c][s] = nh[s], xl[c][s] = nl[s];
             }
-            if constexpr (C == 1) {
-                row_tiles<PT>(xs + n * kSG + 8 * g, g_plane, kSG, kKP, xh[0], xl[0], [](int i) { return i; },
-                              [&](int i, const f32x4 &acc) { done(i, 0, acc); });
-            } else {   // a row tile of B for all of the wavefront's columns
-#pragma unroll
-                for (int i = 0; i < PT; ++i) {
-                    f16x8 lh[kKP], ll[kKP];
-#pragma unroll
-                    for (int s = 0; s < kKP; ++s) {
-                        const _Float16 *at = xs + (16 * i + n) * kSG + 32 * s + 8 * g;
-                        lh[s] = frag(at);
-                        ll[s] = frag(at + g_plane);
-                    }
-#pragma unroll
-                    for (int c = 0; c < C; ++c) {
-                        f32x4 acc[3];
-#pragma unroll
-                        for (int t = 0; t < 3; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int s = 0; s < kKP; ++s) {
-                            acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[s], xl[c][s], acc[0], 0, 0, 0);
-                            acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ll[s], xh[c][s], acc[1], 0, 0, 0);
-                            acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lh[s], xh[c][s], acc[2], 0, 0, 0);
-                        }
-                        if (tile(c) < qt) done(i, c, (acc[0] + acc[1]) + acc[2]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-                if (tile(c) < qt) {
-#pragma unroll
-                    for (int s = 0; s < kKP; ++s) xh[c][s] = nh[c][s], xl[c][s] = nl[c][s];
-                }
-        }
         __syncthreads();
         _Float16 *was = xs;
         xs = gs;
