@@ -562,8 +562,9 @@ int crf_orthogonalize_workspace(int32_t count, int32_t rows, int32_t cols, int64
  * crf_orthogonalize -- matrices with their singular values brought towards 1 by
  * Newton-Schulz products: X = x / (|x|_F + eps), then for each step's (a, b, c)
  *   A = X X^T,  X <- a X + (b A + c A A) X.
- * Operands of the products are held as two float16 parts (22 bits), sums are
- * float32; |x|_F is summed in float64.
+ * Operands of the products are held as two float16 parts (22 bits; float32 where
+ * the shorter side is at most 16 and the longer at most 2,048), sums are float32;
+ * |x|_F is summed in float64.
  *   x, out        device float32 [count][rows][ld], entries [..][cols] of a row;
  *                 the others are neither read nor written.  out must not alias x.
  *   count         1 <= count <= CRF_MAX_LABELS.

@@ -15,7 +15,13 @@
 // out): three float16 products at 16 times the float32 rate each.  Parts of
 // values below float16's normal range lose digits, so X, A and B are held
 // scaled by powers of two that leave room for what the caller's coefficients
-// let the entries grow to, and no more.
+// let the entries grow to, and no more.  Float32 itself is for matrices of up to
+// 16 rows, which are bound by latency.
+//
+// Three ways, by size (five steps): thin matrices whole in registers (one of 16 x
+// 1,000 in 26 us), small ones in a workgroup's LDS and registers (138 of 100 x 101
+// in 46 us, 300 of 32 x 500 in 77), others a launch a product, tile by tile (one of
+// 500 x 501 in 92 us, of 2,048 x 2,048 in 707).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -539,7 +545,146 @@ void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int co
         hipLaunchKernelGGL((ortho_tile_kernel<KIND, 2>), grid, dim3(256), staged_bytes<2>(), stream, g, io);
 }
 
-// Matrices whose parts fit LDS twice over: a workgroup of W wavefronts each, which
+struct Steps {
+    float f[CRF_MAX_STEPS][3];
+    int count;
+};
+
+// Matrices of up to 16 x 2,048: a workgroup of W wavefronts each, a wavefront C of
+// X's tiles of 16 columns, and float32's own matrix instruction (the parts of 22
+// bits, and not its length, are what 16 rows' error comes from: 1.1e-6 against
+// 0.7e-6 on 155 x 7).  Its result has, a lane l, rows 4 (l / 16) + t of column
+// l % 16, t = 0 .. 3, and its operand t is a row of K for a lane l / 16: so a
+// result's register t is operand t of a product that runs K in the order 0, 4, 8,
+// 12 | 1, 5 .., as the right one, and as the left one it is the transpose.  Hence
+// X^T B from X and B, X X^T from X^T, B X from the symmetric B and X, all without
+// leaving the registers; only the wavefronts' sums of A meet in LDS, once a step.
+// (Five steps of one 16 x 1,000: 26 us, as parts in LDS 39; of 300 of them 47, 80.)
+constexpr int kThinRows = 16, kThinCols = 2048;
+inline bool is_thin(int rows, int cols) { return std::min(rows, cols) <= kThinRows && std::max(rows, cols) <= kThinCols; }
+// left^T right (+ acc)
+__device__ __forceinline__ f32x4 times(const f32x4 &left, const f32x4 &right, f32x4 acc) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(left[t], right[t], acc, 0, 0, 0);
+    return acc;
+}
+template <int W, int C>
+__global__ __launch_bounds__(64 * W) void ortho_thin_kernel(OrthoIo io, Steps steps) {
+    __shared__ f32x4 part[2][W][64];
+    __shared__ double norm[W];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int n = lane & 15;
+    const int g = lane >> 4;
+    const bool tall = io.rows > io.cols;
+    const int p = tall ? io.cols : io.rows, q = tall ? io.rows : io.cols;
+    const int64_t step_r = tall ? 1 : io.ld, step_c = tall ? io.ld : 1;   // of X, in the caller's arrays
+    int64_t row[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) row[t] = min(4 * g + t, p - 1) * step_r + (int64_t)blockIdx.x * io.rows * io.ld;
+    auto tile = [&](int c) { return c * W + wave; };
+    auto column = [&](int c) { return min(16 * tile(c) + n, q - 1) * step_c; };
+    auto there = [&](int c, int t) { return 4 * g + t < p && 16 * tile(c) + n < q; };
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+    // U, the new momentum and the norm
+    f32x4 x[C], m[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            x[c][t] = io.grad[row[t] + column(c)];
+            m[c][t] = io.momentum != nullptr ? io.momentum[row[t] + column(c)] : 0.f;
+        }
+    asm("" : "+v"(n));   // (places are worked out again, here and below: kept for all columns, they spill)
+    double sum = 0.0;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (io.momentum != nullptr) {
+                m[c][t] = fmaf(io.mu, m[c][t], x[c][t]);
+                if (there(c, t)) io.momentum_out[row[t] + column(c)] = m[c][t];
+                x[c][t] = updated(io, x[c][t], m[c][t]);
+            }
+            x[c][t] = there(c, t) ? x[c][t] : 0.f;
+            sum += (double)x[c][t] * (double)x[c][t];
+        }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
+    if constexpr (W > 1) {
+        if (lane == 0) norm[wave] = sum;
+        __syncthreads();
+        sum = norm[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) sum += norm[w];
+    }
+    // (a sum that is not finite makes the whole matrix NaN)
+    const double inv = 1.0 / (sqrt(sum) + (double)io.eps) + 0.0 * sum;
+    f32x4 one, gram[2] = {zero, zero};   // the wavefront's sum of A, in two chains
+#pragma unroll
+    for (int t = 0; t < 4; ++t) one[t] = 4 * g + t == n ? 1.f : 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x[c][t] = (float)((double)x[c][t] * inv);
+        const f32x4 xt = times(x[c], one, zero);   // (exact)
+        gram[c & 1] = times(xt, xt, gram[c & 1]);
+    }
+
+    asm("" : "+v"(n));
+    for (int k = 0; k < steps.count; ++k) {
+        f32x4 a = gram[0] + gram[1];
+        if constexpr (W > 1) {
+            part[k & 1][wave][lane] = a;   // (the readers of step k - 2 are past the last step's barrier)
+            __syncthreads();
+            a = part[k & 1][0][lane];
+#pragma unroll
+            for (int w = 1; w < W; ++w) a += part[k & 1][w][lane];
+        }
+        const f32x4 square = times(a, a, zero);
+        f32x4 b;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) b[t] = fmaf(steps.f[k][2], square[t], fmaf(steps.f[k][1], a[t], steps.f[k][0] * one[t]));
+        gram[0] = gram[1] = zero;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const f32x4 xt = times(x[c], b, zero);
+            x[c] = times(b, x[c], zero);
+            gram[c & 1] = times(xt, xt, gram[c & 1]);   // (after the last step nobody asks)
+        }
+    }
+
+    asm("" : "+v"(n));
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) m[c][t] = io.w != nullptr ? io.w[row[t] + column(c)] : 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (there(c, t)) io.out[row[t] + column(c)] = io.w != nullptr ? fmaf(-io.rate, x[c][t], io.keep * m[c][t]) : x[c][t];
+}
+
+template <int W, int C>
+void launch_thin_c(const OrthoIo &io, const Steps &steps, int count, hipStream_t stream) {
+    hipLaunchKernelGGL((ortho_thin_kernel<W, C>), dim3(count), dim3(64 * W), 0, stream, io, steps);
+}
+void launch_thin(const OrthoIo &io, const Steps &steps, int count, hipStream_t stream) {
+    const int q = std::max(io.rows, io.cols);
+    (q <= 16     ? launch_thin_c<1, 1>
+     : q <= 64   ? launch_thin_c<4, 1>
+     : q <= 128  ? launch_thin_c<8, 1>
+     : q <= 256  ? launch_thin_c<8, 2>
+     : q <= 384  ? launch_thin_c<8, 3>
+     : q <= 512  ? launch_thin_c<8, 4>
+     : q <= 768  ? launch_thin_c<8, 6>
+     : q <= 1024 ? launch_thin_c<8, 8>
+     : q <= 1536 ? launch_thin_c<8, 12>
+                 : launch_thin_c<8, 16>)(io, steps, count, stream);
+}
+
+// More rows, whose parts fit LDS twice over: a workgroup of W wavefronts each, which
 // never leaves its CU.  Wavefront w owns C of X's tiles of 16 columns, w, w + W ..,
 // in registers.  Their parts are wanted twice over: in LDS, as rows of X, for the
 // Gram matrix, and in the owner's registers as the right operand of B X -- a
@@ -548,7 +693,10 @@ void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int co
 // 20-23 | ...; the Gram matrix and B are stored with their columns in that order,
 // so that no product minds.  A and B are symmetric: of the tiles (i, j) and (j, i)
 // one is computed, column j taking rows j, j + 1 .. j + PT / 2 (cyclically), which
-// shares the work evenly.
+// shares the work evenly.  Bound by a step's three chains (products, LDS, barrier):
+// 6.6 us a step of 100 x 101 whether there is one matrix or 138, the matrix cores
+// 23% busy; 300 of 100 x 150 take 116 us, a launch a product 351, 300 of 32 x 500
+// 77 and 221.
 constexpr int kSmallRows = 128;
 __host__ __device__ constexpr int small_stride(int tiles) { return (tiles + 1) / 2 * 32 + 8; }   // of a row of 16 `tiles`
 inline int64_t small_lds(int p, int q) {
@@ -556,16 +704,11 @@ inline int64_t small_lds(int p, int q) {
     return std::max<int64_t>(2 * 2 * 2 * 16 * pt * (int64_t)small_stride(qt), 4 * (int64_t)q * (p + 1));
 }
 // Column tiles of a wavefront of eight, for `pt` row tiles at most.
-constexpr int small_most(int pt) { return pt == 1 ? 8 : pt <= 3 ? 4 : pt <= 7 ? 2 : 1; }
+constexpr int small_most(int pt) { return pt <= 3 ? 4 : pt <= 7 ? 2 : 1; }
 inline bool is_small(int rows, int cols) {
     const int p = std::min(rows, cols), q = std::max(rows, cols);
     return p <= kSmallRows && (q + 127) / 128 <= small_most((p + 15) / 16) && small_lds(p, q) <= 160 * 1024 - 256;
 }
-
-struct Steps {
-    float f[CRF_MAX_STEPS][3];
-    int count;
-};
 
 // U row tiles of a stored matrix (hi, and lo `plane` entries on) times a column
 // tile in registers: tile u is at row tile row(u), and done(u, acc) takes its
@@ -884,9 +1027,7 @@ void launch_small(const OrthoIo &io, const Steps &steps, int count, hipStream_t 
     if (q <= 128) return launch_small_c<PT, 8, 1>(io, steps, count, stream);
     if constexpr (small_most(PT) >= 2)
         if (q <= 256) return launch_small_c<PT, 8, 2>(io, steps, count, stream);
-    if constexpr (small_most(PT) >= 4)
-        if (q <= 512) return launch_small_c<PT, 8, 4>(io, steps, count, stream);
-    if constexpr (small_most(PT) >= 8) launch_small_c<PT, 8, 8>(io, steps, count, stream);
+    if constexpr (small_most(PT) >= 4) launch_small_c<PT, 8, 4>(io, steps, count, stream);
 }
 
 int64_t aligned(int64_t n) { return (n + 255) / 256 * 256; }
@@ -908,17 +1049,15 @@ hipError_t small_attribute() {
         if (e == hipSuccess) e = set((const void *)ortho_small_kernel<PT, 8, 2>);
     if constexpr (small_most(PT) >= 4)
         if (e == hipSuccess) e = set((const void *)ortho_small_kernel<PT, 8, 4>);
-    if constexpr (small_most(PT) >= 8)
-        if (e == hipSuccess) e = set((const void *)ortho_small_kernel<PT, 8, 8>);
     return e;
 }
 
 }  // namespace
 
 hipError_t set_ortho_attributes() {
-    for (auto set : {small_attribute<1>, small_attribute<2>, small_attribute<3>, small_attribute<4>, small_attribute<5>,
-                     small_attribute<6>, small_attribute<7>, small_attribute<8>, tile_attribute<kGram>, tile_attribute<kPoly>,
-                     tile_attribute<kNext>, tile_attribute<kLast>}) {
+    for (auto set : {small_attribute<2>, small_attribute<3>, small_attribute<4>, small_attribute<5>, small_attribute<6>,
+                     small_attribute<7>, small_attribute<8>, tile_attribute<kGram>, tile_attribute<kPoly>, tile_attribute<kNext>,
+                     tile_attribute<kLast>}) {
         const hipError_t e = set();
         if (e != hipSuccess) return e;
     }
@@ -926,7 +1065,7 @@ hipError_t set_ortho_attributes() {
 }
 
 int64_t ortho_bytes(int count, int rows, int cols) {
-    if (is_small(rows, cols)) return 256;
+    if (is_thin(rows, cols) || is_small(rows, cols)) return 256;
     const OrthoShape sh = ortho_shape(rows, cols);
     return aligned(8 * (int64_t)count * norm_shares(rows, cols)) + 2 * aligned(4 * count * sh.x_plane()) +
            2 * aligned(4 * count * sh.xt_plane()) + 2 * aligned(4 * count * sh.a_plane());
@@ -937,13 +1076,13 @@ hipError_t launch_ortho(const float *grad, const float *momentum, const float *w
                         const float *coefficients, int steps, char *ws, hipStream_t stream) {
     const OrthoShape sh = ortho_shape(rows, cols);
     OrthoIo io{grad, momentum, w, momentum_out, out, rows, cols, ld, mu, nesterov, keep, rate, eps};
-    if (is_small(rows, cols)) {
+    if (is_thin(rows, cols) || is_small(rows, cols)) {
         Steps all;
         all.count = steps;
         for (int k = 0; k < steps; ++k)
             for (int q = 0; q < 3; ++q) all.f[k][q] = coefficients[3 * k + q];
         void (*const by_tiles[])(const OrthoIo &, const Steps &, int, hipStream_t) = {
-            launch_small<1>, launch_small<2>, launch_small<3>, launch_small<4>,
+            launch_thin,     launch_small<2>, launch_small<3>, launch_small<4>,
             launch_small<5>, launch_small<6>, launch_small<7>, launch_small<8>};
         by_tiles[(sh.p - 1) / 16](io, all, count, stream);
         return hipGetLastError();

@@ -87,7 +87,7 @@ SHAPES = [(1, 1, 1, 1), (1, 1, 9, 9), (2, 9, 1, 3), (3, 2, 3, 5), (1, 15, 16, 16
           (3, 33, 31, 40), (2, 64, 64, 64), (3, 63, 65, 68), (7, 100, 101, 104), (2, 101, 100, 100), (2, 112, 128, 128),
           (2, 128, 128, 130), (2, 128, 129, 132), (1, 129, 127, 127), (2, 40, 300, 304), (1, 300, 40, 41), (1, 7, 1000, 1000),
           (1, 500, 501, 504), (1, 512, 512, 512), (1, 513, 260, 263), (1, 700, 1030, 1030), (40, 20, 130, 130),
-          (9, 200, 300, 300), (3, 1, 1024, 1024), (2, 16, 1007, 1007), (2, 1024, 15, 17), (2, 17, 513, 513), (3, 32, 500, 500),
+          (9, 200, 300, 300), (3, 1, 1024, 1024), (1, 9, 1200, 1200), (2, 2048, 16, 19), (1, 5, 2049, 2049), (4, 11, 385, 385), (3, 700, 13, 13), (2, 3, 17, 17), (2, 16, 1007, 1007), (2, 1024, 15, 17), (2, 17, 513, 513), (3, 32, 500, 500),
           (2, 257, 31, 31), (2, 48, 400, 401), (1, 417, 48, 48), (2, 64, 256, 256), (2, 64, 257, 257), (1, 80, 241, 241),
           (2, 190, 95, 95), (2, 112, 160, 160), (1, 112, 161, 161), (2, 128, 129, 129), (1, 2, 8192, 8192), (1, 1537, 1030, 1030), (3, 1025, 1290, 1290)]
 
