@@ -158,7 +158,8 @@ def test_launches_fit_the_device(harness, lengths, d, labels):
         assert int(threads) <= 1024 and int(lds) <= 160 * 1024, name
 
 
-@pytest.mark.parametrize("shape", [(1, 1, 1), (4096, 1, 1), (1, 8192, 8192), (138, 100, 101), (1, 500, 501), (4096, 16, 300)])
+@pytest.mark.parametrize("shape", [(1, 1, 1), (4096, 1, 1), (1, 8192, 8192), (138, 100, 101), (1, 500, 501), (4096, 16, 300), (1, 16, 2048),
+                                   (2, 2049, 16), (300, 32, 500), (2, 112, 160), (1, 512, 17), (1, 128, 129)])
 def test_update_launches_fit_the_device(harness, shape):
     rows = run(harness, "update", *shape)
     assert rows
