@@ -26,7 +26,7 @@ constexpr int kFewBuckets = 64;
 constexpr int kMaxWidth = 1023;      // a sentence's most words
 // Workgroups that a call aims at.  Forward, 100 sentences of 138 labels: 19.6 us at
 // 1,024, 14.8 at 2,048, 12.7 at 4,096.  Back, where each adds a share to what is
-// joined: 18.6 and 5.4 us at 1,024, 15.4 and 4.5 at 2,048, 14.9 and 7.9 at 4,096.
+// joined: 18.4 us both at 1,024, 16.4 at 2,048, 19.0 at 4,096.
 constexpr int kWidthGroups = 4096, kWidthSumGroups = 2048;
 constexpr int kWidthShares = 1024;   // most shares (5,000 sentences: 18.9 us at 512, 15.4, 16.6 at 2,048)
 
@@ -62,12 +62,19 @@ __device__ __forceinline__ typename Cells<V>::type entry(const float *table, con
     return v;
 }
 
-// Thread t's first row of a block of posts: with P = 64 a wavefront's, so that
-// what is looked up by it is in scalar registers.
+// The rows of a block of posts that are group r's, a row's threads: with P = 64 a
+// wavefront's run of them, so that what is looked up by a row comes by scalar
+// loads, many rows in each.  (A load a row keeps the scalar caches busy for 4 us
+// more with 100 sentences of 138 labels; with P = 16 runs are 1 us slower.)
 template <int P>
-__device__ __forceinline__ int first_row() {
+__device__ __forceinline__ int row_group() {
     const int r = threadIdx.x / P;
     return P == 64 ? __builtin_amdgcn_readfirstlane(r) : r;
+}
+template <int P>
+__device__ __forceinline__ int row_of(int group, int m) {
+    constexpr int kRows = kWidthThreads / P, kMine = kBiaRows / kRows;
+    return P == 64 ? group * kMine + m : group + m * kRows;
 }
 
 // A workgroup takes a block of posts and every gridDim.y-th group of N tiles of P
@@ -82,13 +89,13 @@ __global__ __launch_bounds__(kWidthThreads) void width_kernel(const int32_t *__r
     constexpr int kRows = kWidthThreads / P, kMine = kBiaRows / kRows;
     const int32_t *rest = posts + (size_t)blockIdx.x * kPostRec + kBiaRows;
     const int64_t *at = post_cells + (size_t)blockIdx.x * kBiaRows;
-    const int r0 = first_row<P>(), per = L / V;   // places of a width
+    const int group = row_group<P>(), per = L / V;   // (per: places of a width)
     int wide[kMine], most = 0;
     size_t base[kMine];
 #pragma unroll
     for (int m = 0; m < kMine; ++m) {
-        wide[m] = rest[r0 + m * kRows];
-        base[m] = (size_t)at[r0 + m * kRows] * L;
+        wide[m] = rest[row_of<P>(group, m)];
+        base[m] = (size_t)at[row_of<P>(group, m)] * L;
         most = max(most, wide[m]);
     }
     for (int e0 = blockIdx.y * N * P + threadIdx.x % P; e0 < most * per; e0 += gridDim.y * N * P) {
@@ -128,7 +135,7 @@ __global__ __launch_bounds__(kWidthThreads) void width_bwd_kernel(const int32_t 
     constexpr int kRows = kWidthThreads / P, kMine = kBiaRows / kRows;
     __shared__ cells sums[kRows][N * P];
     __shared__ int buckets[P == 16 ? N * P + 1 : 1];
-    const int r0 = first_row<P>(), c = threadIdx.x % P, per = L / V, e0 = blockIdx.y * N * P + c;
+    const int group = row_group<P>(), c = threadIdx.x % P, per = L / V, e0 = blockIdx.y * N * P + c;
     int w[N];
     size_t off[N];
     cells sum[N];
@@ -147,8 +154,8 @@ __global__ __launch_bounds__(kWidthThreads) void width_bwd_kernel(const int32_t 
         const int64_t *at = post_cells + (size_t)block * kBiaRows;
 #pragma unroll
         for (int m = 0; m < kMine; ++m) {
-            wide1[m] = rest[r0 + m * kRows];
-            base1[m] = (size_t)at[r0 + m * kRows] * L;
+            wide1[m] = rest[row_of<P>(group, m)];
+            base1[m] = (size_t)at[row_of<P>(group, m)] * L;
         }
     };
     look(blockIdx.x);
@@ -178,9 +185,9 @@ __global__ __launch_bounds__(kWidthThreads) void width_bwd_kernel(const int32_t 
     }
     if (parts == nullptr) return;
 #pragma unroll
-    for (int t = 0; t < N; ++t) sums[r0][t * P + c] = sum[t];
+    for (int t = 0; t < N; ++t) sums[group][t * P + c] = sum[t];
     __syncthreads();
-    // to parts[width's label][share], or parts[bucket's label][share] (K > 0)
+    // to parts[share][width's label], or parts[bucket's label][share] (K > 0)
     const int shares = gridDim.x * (K > 0 ? gridDim.y : 1), share = K > 0 ? blockIdx.y * gridDim.x + blockIdx.x : blockIdx.x;
     const int first = blockIdx.y * N * P;
     for (int q = threadIdx.x; q < N * P; q += kWidthThreads) {
@@ -189,13 +196,7 @@ __global__ __launch_bounds__(kWidthThreads) void width_bwd_kernel(const int32_t 
         if (P == 16 && K > 0) {
             sums[0][q] = s;
         } else if (first + q < widest * per) {
-            float *to = parts + (size_t)(first + q) * V * shares + share;
-            if constexpr (V == 1) {
-                to[0] = s;
-            } else {
-#pragma unroll
-                for (int h = 0; h < V; ++h) to[h * shares] = s[h];
-            }
+            *reinterpret_cast<cells *>(parts + (size_t)share * widest * L + (size_t)(first + q) * V) = s;
         }
     }
     if constexpr (P == 16) {
@@ -250,8 +251,9 @@ __global__ __launch_bounds__(kJoinThreads) void width_join_kernel(const float *_
     if (label < L) {
 #pragma unroll 8
         for (int q = p; q < count * shares; q += kLanes) {
-            const int w = q / shares;
-            s += parts[((size_t)widths[w] * L + label) * shares + q - w * shares];
+            const int w = q / shares, share = q - w * shares;
+            s += by_bucket ? parts[((size_t)widths[w] * L + label) * shares + share]
+                           : parts[((size_t)share * widest + widths[w]) * L + label];
         }
     }
     part[p][l] = s;
