@@ -84,12 +84,15 @@ def check(got, u, steps, eps):
 
 
 SHAPES = [(1, 1, 1, 1), (1, 1, 9, 9), (2, 9, 1, 3), (3, 2, 3, 5), (1, 15, 16, 16), (2, 16, 17, 20), (5, 31, 33, 33),
-          (3, 33, 31, 40), (2, 64, 64, 64), (3, 63, 65, 68), (7, 100, 101, 104), (2, 101, 100, 100), (2, 112, 128, 128),
-          (2, 128, 128, 130), (2, 128, 129, 132), (1, 129, 127, 127), (2, 40, 300, 304), (1, 300, 40, 41), (1, 7, 1000, 1000),
-          (1, 500, 501, 504), (1, 512, 512, 512), (1, 513, 260, 263), (1, 700, 1030, 1030), (40, 20, 130, 130),
-          (9, 200, 300, 300), (3, 1, 1024, 1024), (1, 9, 1200, 1200), (2, 2048, 16, 19), (1, 5, 2049, 2049), (4, 11, 385, 385), (3, 700, 13, 13), (2, 3, 17, 17), (2, 16, 1007, 1007), (2, 1024, 15, 17), (2, 17, 513, 513), (3, 32, 500, 500),
-          (2, 257, 31, 31), (2, 48, 400, 401), (1, 417, 48, 48), (2, 64, 256, 256), (2, 64, 257, 257), (1, 80, 241, 241),
-          (2, 190, 95, 95), (2, 112, 160, 160), (1, 112, 161, 161), (2, 128, 129, 129), (1, 2, 8192, 8192), (1, 1537, 1030, 1030), (3, 1025, 1290, 1290)]
+          (3, 33, 31, 40), (2, 64, 64, 64), (3, 63, 65, 68), (7, 100, 101, 104), (2, 101, 100, 100),
+          (2, 112, 128, 128), (2, 128, 128, 130), (2, 128, 129, 132), (1, 129, 127, 127), (2, 40, 300, 304),
+          (1, 300, 40, 41), (1, 7, 1000, 1000), (1, 500, 501, 504), (1, 512, 512, 512), (1, 513, 260, 263),
+          (1, 700, 1030, 1030), (40, 20, 130, 130), (9, 200, 300, 300), (3, 1, 1024, 1024), (1, 9, 1200, 1200),
+          (2, 2048, 16, 19), (1, 5, 2049, 2049), (4, 11, 385, 385), (3, 700, 13, 13), (2, 3, 17, 17),
+          (2, 16, 1007, 1007), (2, 1024, 15, 17), (2, 17, 513, 513), (3, 32, 500, 500), (2, 257, 31, 31),
+          (2, 48, 400, 401), (1, 417, 48, 48), (2, 64, 256, 256), (2, 64, 257, 257), (1, 80, 241, 241),
+          (2, 190, 95, 95), (2, 112, 160, 160), (1, 112, 161, 161), (2, 128, 129, 129), (1, 2, 8192, 8192),
+          (1, 1537, 1030, 1030), (3, 1025, 1290, 1290)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
@@ -109,7 +112,7 @@ def test_orthogonalize(torch, shape):
 
 
 @pytest.mark.parametrize("steps", [CUBIC, FIFTH, ((1.0, 0.0, 0.0),), ((3.4445, -4.775, 2.0315),), FIFTH + CUBIC + FIFTH])
-@pytest.mark.parametrize("shape", [(2, 50, 60, 60), (1, 200, 140, 144)])
+@pytest.mark.parametrize("shape", [(2, 50, 60, 60), (1, 200, 140, 144), (3, 12, 90, 90), (2, 24, 400, 400)])
 def test_coefficients(torch, steps, shape):
     count, rows, cols, ld = shape
     x = matrices(count, rows, cols, ld, 3)
@@ -131,17 +134,18 @@ def test_singular_values_near_one(torch):
 
 
 @pytest.mark.parametrize("scale", [1e-38, 1e-25, 1.0, 1e18, 1e37])
-def test_scales(torch, scale):
+@pytest.mark.parametrize("rows,cols", [(60, 70), (14, 130), (30, 300)])
+def test_scales(torch, rows, cols, scale):
     # squares past float32's range on either side; eps has no share in the
     # large ones and rules the smallest
-    x = (matrices(1, 60, 70, 70, 5).astype(np.float64) * (scale * 100)).astype(np.float32)[0]
+    x = (matrices(1, rows, cols, cols, 5).astype(np.float64) * (scale * 100)).astype(np.float32)[0]
     assert np.isfinite(x).all()
     got = B.orthogonalize(torch.from_numpy(x).to("cuda:0")).cpu().numpy()
     assert np.isfinite(got).all()
     check(got, x, B.MUON_STEPS, float(np.float32(1e-7)))
 
 
-@pytest.mark.parametrize("shape", [(4, 30, 40, 40), (4, 200, 150, 150)])
+@pytest.mark.parametrize("shape", [(4, 30, 40, 40), (4, 200, 150, 150), (4, 10, 300, 300), (4, 90, 7, 7), (4, 20, 200, 200)])
 def test_zeros_and_what_is_not_finite(torch, shape):
     count, rows, cols, ld = shape
     x = matrices(count, rows, cols, ld, 6)
@@ -187,7 +191,7 @@ def test_muon_step(torch, shape, nesterov):
         assert off <= rate * tolerance(u, B.MUON_STEPS, 1e-7) + 2.0 ** -22 * np.linalg.norm(wq)
 
 
-@pytest.mark.parametrize("rows,cols,ld", [(40, 50, 30_000_000), (200, 190, 6_000_000)])
+@pytest.mark.parametrize("rows,cols,ld", [(40, 50, 30_000_000), (200, 190, 6_000_000), (10, 200, 110_000_000), (30, 200, 40_000_000)])
 def test_offsets_past_32_bits(torch, rows, cols, ld):
     if torch.cuda.mem_get_info()[0] < 48 << 30:
         pytest.skip("needs 48 GB")
@@ -203,7 +207,7 @@ def test_offsets_past_32_bits(torch, rows, cols, ld):
 
 
 def test_two_dimensions_streams_and_graphs(torch):
-    x = [torch.from_numpy(matrices(1, r, c, c, k)[0]).to("cuda:0") for k, (r, c) in enumerate(((90, 101), (300, 260)))]
+    x = [torch.from_numpy(matrices(1, r, c, c, k)[0]).to("cuda:0") for k, (r, c) in enumerate(((90, 101), (300, 260), (16, 300)))]
     want = [B.orthogonalize(v) for v in x]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -216,11 +220,11 @@ def test_two_dimensions_streams_and_graphs(torch):
     states = [[v.clone() for v in x] + [torch.zeros_like(v) for v in x] for _ in range(2)]
     held = [v.clone() for v in x]
     graphs = []
-    for w1, w2, m1, m2 in states:
+    for state in states:
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
-            B.muon_step(w1, held[0], m1, lr=0.1)
-            B.muon_step(w2, held[1], m2, lr=0.1)
+            for w, h, m in zip(state[:3], held, state[3:]):
+                B.muon_step(w, h, m, lr=0.1)
         graphs.append(g)
     eager = [v.clone() for v in x] + [torch.zeros_like(v) for v in x]
     for k in range(3):
@@ -228,8 +232,8 @@ def test_two_dimensions_streams_and_graphs(torch):
             h.copy_(v * (1.0 - 0.3 * k) + 0.01 * v.flip(0))
         for g in graphs:
             g.replay()
-        B.muon_step(eager[0], held[0], eager[2], lr=0.1)
-        B.muon_step(eager[1], held[1], eager[3], lr=0.1)
+        for w, h, m in zip(eager[:3], held, eager[3:]):
+            B.muon_step(w, h, m, lr=0.1)
         torch.cuda.synchronize()
         for st in states:
             for a, b in zip(st, eager):
