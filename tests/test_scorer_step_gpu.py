@@ -180,6 +180,45 @@ def test_captured_step(torch):
         assert np.isfinite(seen).all() and len(set(seen)) == 4
 
 
+def test_captured_autograd(torch):
+    # forward and backward through the differentiable forms in one graph; no eager
+    # graph of its leaves is alive meanwhile (torch would add to their gradients
+    # on that one's stream)
+    with B.Plan(LENGTHS, n1=N1, device="cuda:0") as plan:
+        s = Step(torch, plan, seed=7)
+
+        def run(leaves):
+            for v in leaves:
+                v.grad = None
+            x, gamma, beta, w, table = leaves
+            y = B.layer_norm(x, plan, gamma, beta)
+            scores = B.width_bias(B.biaffine(y, y, w, plan, table=table, buckets=s.buckets), table, s.buckets, plan)
+            loss, g = plan.gold_loss(scores.detach(), s.gold)
+            scores.backward(g)
+            return loss
+
+        held = [v.clone().requires_grad_() for v in s.leaves]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            run(held)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            loss = run(held)
+        for k in range(3):
+            with torch.no_grad():
+                held[0].copy_(torch.randn((plan.B, N1, D), generator=torch.Generator().manual_seed(60 + k)))
+                held[4].fill_(0.1 * k)
+            graph.replay()
+            eager = [v.detach().clone().requires_grad_() for v in held]
+            want = run(eager)
+            torch.cuda.synchronize()
+            assert torch.equal(loss, want)
+            for v, w in zip(held, eager):
+                assert torch.equal(v.grad, w.grad) and bool(v.grad.abs().sum() > 0)
+
+
 def test_second_derivatives_raise(torch):
     with B.Plan([3], n1=4, device="cuda:0") as plan:
         x = torch.randn((1, 4, 8), device="cuda:0", requires_grad=True)
