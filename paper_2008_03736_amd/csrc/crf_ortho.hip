@@ -472,7 +472,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ?
     __syncthreads();
     read(0, 0);
     int ahead = 1, free = 2;   // buffers of steps s + 1 and s + 2
-    for (int s0 = 0; s0 < g.k / kStepK; s0 += D)   // (K is a multiple of 64 M)
+    for (int s0 = 0; s0 < g.k / kStepK; s0 += D)   // (K is a multiple of D steps, 64 M: see launch_product)
 #pragma unroll
         for (int d = 0; d < D; ++d) {
             read((d + 1) & 1, ahead);
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, M == 2 ?
     finish_tile<KIND, T, 256>(tile, held, g, io, T * i, T * j);
 }
 
-// The largest tile of which there are kEnoughTiles (half the CUs), or the least:
+// The largest tile that divides K and of which there are kEnoughTiles (half the CUs), or the least:
 // five steps of one matrix of 640 x 640 take 110 us in tiles of 32 (134 of 64), of
 // 1,024 x 1,024 183 of 64 (215 of 32, 331 of 128), of 1,536 x 1,536 418 of 128 for
 // two products and 64 for the symmetric two (431 of 64, 450 of 128), of 2,048 x
@@ -533,10 +533,13 @@ void launch_product(const ProductArgs &args, const OrthoIo &io, int rows, int co
         const int64_t down = rows / T, across = cols / T;
         return KIND == kGram || KIND == kPoly ? down * (down + 1) / 2 : down * across;
     };
+    // (a tile of T takes K in rounds of T: X X^T runs along qq, which a result of
+    // pp x pp says nothing of)
+    auto fits = [&](int T) {
+        return rows % T == 0 && cols % T == 0 && args.k % T == 0 && tiles(T) * count >= kEnoughTiles;
+    };
     ProductArgs g = args;
-    const int T = rows % 128 == 0 && cols % 128 == 0 && tiles(128) * count >= kEnoughTiles ? 128
-                  : tiles(64) * count >= kEnoughTiles                                     ? 64
-                                                                                           : kFewTile;
+    const int T = fits(128) ? 128 : fits(64) ? 64 : kFewTile;
     g.across = cols / T;
     const dim3 grid((uint32_t)tiles(T), 1, count);
     if (T == kFewTile)

@@ -4,6 +4,9 @@
 //   grids LIB D LABELS LENGTHS...   "L name grid(x y z) threads lds" of each launch of layer
 //                                norm and of the width bias
 //   update LIB COUNT ROWS COLS   the same of the orthogonalised update
+//   products LIB SIDES COUNTS    "T kind tiles k" of each product in tiles of 64 x tiles that
+//                                the update launches for matrices of up to SIDES x 64 rows and
+//                                columns, 1 to COUNTS of them
 #define main launch_main
 #define hipLaunchKernel plain_hipLaunchKernel
 #include "launch_host_stub.cpp"
@@ -12,10 +15,24 @@
 
 namespace {
 std::vector<std::string> shapes;
+std::set<std::string> products;
+// The head of what a product's kernel is passed (crf_ortho.hip).
+struct ProductHead {
+    const void *left, *right, *add, *out, *out_t;
+    int k, stride, t_stride, across;
+};
 }
 
-extern "C" hipError_t hipLaunchKernel(const void *f, dim3 g, dim3 b, void **, size_t lds, hipStream_t) {
+extern "C" hipError_t hipLaunchKernel(const void *f, dim3 g, dim3 b, void **args, size_t lds, hipStream_t) {
     std::string name = names[f];
+    const size_t tile = name.find("ortho_tile_kernel<");
+    if (tile != std::string::npos) {   // (kind and tiles are its template's arguments, the kind perhaps with its type)
+        std::string of = name.substr(tile + 18, name.find('>', tile) - tile - 18);
+        const size_t kind = of.rfind(')', of.find(','));
+        if (kind != std::string::npos) of = of.substr(kind + 1);
+        of.erase(of.find(','), 1);
+        products.insert("T " + of + " " + std::to_string(static_cast<const ProductHead *>(args[0])->k));
+    }
     const size_t end = name.find('('), start = name.find("(anonymous namespace)::");
     name = start != std::string::npos && start < name.find("_kernel") ? name.substr(start + 23) : name.substr(0, end);
     name = name.substr(0, name.find_first_of("(<"));
@@ -122,7 +139,18 @@ int update(void *lib, int count, int rows, int cols) {
     if (crf_muon_step(f(0), f(1), f(2), count, rows, cols, cols, 0.9f, 1, 0.1f, 0.01f, kSteps[0], 2, 1e-7f, f(0), f(2), f(3), ow,
                       nullptr) != CRF_OK)
         return 3;
-    for (const std::string &s : shapes) std::printf("%s\n", s.c_str());
+    return 0;
+}
+
+int tile_products(void *lib, int sides, int counts) {
+    for (int p = 1; p <= sides; ++p)
+        for (int q = p; q <= sides; ++q)
+            for (int count = 1; count <= counts; ++count) {
+                // (a side's last rows of padding may be all there, or none)
+                const int rc = (count & 1) != 0 ? update(lib, count, 64 * p, 64 * q) : update(lib, count, 64 * q - 7, 64 * p - 9);
+                if (rc != 0) return rc;
+            }
+    for (const std::string &s : products) std::printf("%s\n", s.c_str());
     return 0;
 }
 
@@ -140,6 +168,11 @@ int main(int argc, char **argv) {
     std::vector<int> v;
     for (int k = 3; k < argc; ++k) v.push_back(std::atoi(argv[k]));
     if (mode == "grids" && v.size() > 2) return grids(lib, v[0], v[1], std::vector<int32_t>(v.begin() + 2, v.end()));
-    if (mode == "update" && v.size() == 3) return update(lib, v[0], v[1], v[2]);
+    if (mode == "update" && v.size() == 3) {
+        const int rc = update(lib, v[0], v[1], v[2]);
+        for (const std::string &s : shapes) std::printf("%s\n", s.c_str());
+        return rc;
+    }
+    if (mode == "products" && v.size() == 2) return tile_products(lib, v[0], v[1]);
     return 2;
 }

@@ -111,6 +111,29 @@ def test_orthogonalize(torch, shape):
         check(got[q, :, :cols], x[q, :, :cols], B.MUON_STEPS, float(np.float32(1e-7)))
 
 
+# Matrices of which there are enough for each of the tiles: pp (the shorter side, padded)
+# a multiple of 128 with qq an odd and an even number of 64s, and pp an odd one.
+MANY = [(138, 100, 300), (160, 128, 192), (64, 200, 300), (43, 256, 320), (22, 384, 448), (13, 512, 576),
+        (128, 300, 120), (42, 256, 320), (43, 250, 330), (13, 512, 640), (44, 320, 190), (130, 65, 515)]
+
+
+@pytest.mark.parametrize("shape", MANY)
+def test_many_matrices(torch, shape):
+    count, rows, cols = shape
+    x, w, m = (matrices(count, rows, cols, cols, k) for k in (rows, 1, 2))
+    dev = [torch.from_numpy(v).to("cuda:0") for v in (w, x, m)]
+    got = B.orthogonalize(dev[1]).cpu().numpy()
+    B.muon_step(*dev, lr=0.5, mu=0.5, nesterov=False, scale=1.0)
+    moved, momentum = dev[0].cpu().numpy(), dev[2].cpu().numpy()
+    for q in sorted({0, 1, count // 2, count - 1}):
+        check(got[q], x[q], B.MUON_STEPS, float(np.float32(1e-7)))
+        u = 0.5 * m[q].astype(np.float64) + x[q]
+        assert np.all(np.abs(momentum[q] - u) <= 2.0 ** -24 * np.abs(u))
+        new = w[q] - 0.5 * products(u, B.MUON_STEPS, 1e-7, np.float64)
+        # (U's own rounding is within the tolerance's 2^-22 of it; one more in the last addition)
+        assert np.linalg.norm(moved[q] - new) <= 0.5 * tolerance(u, B.MUON_STEPS, 1e-7) + 1.01 * 2.0 ** -24 * np.linalg.norm(new)
+
+
 @pytest.mark.parametrize("steps", [CUBIC, FIFTH, ((1.0, 0.0, 0.0),), ((3.4445, -4.775, 2.0315),), FIFTH + CUBIC + FIFTH])
 @pytest.mark.parametrize("shape", [(2, 50, 60, 60), (1, 200, 140, 144), (3, 12, 90, 90), (2, 24, 400, 400)])
 def test_coefficients(torch, steps, shape):

@@ -168,6 +168,18 @@ def test_update_launches_fit_the_device(harness, shape):
         assert int(threads) <= 1024 and int(lds) <= 160 * 1024, name
 
 
+def test_tiles_take_whole_rounds_of_k(harness):
+    # a product in tiles of 64 M x 64 M runs its K in rounds of 64 M: a rule that
+    # picks the tile by the result's sides alone repeats K's last blocks.  Every
+    # pair of padded sides up to 640, and counts past each threshold on the way
+    # from small tiles to large ones (128 tiles: 128, 43, 22, 13, 9 matrices).
+    rows = [tuple(map(int, r[1:])) for r in run(harness, "products", 10, 132)]
+    assert {(kind, tiles) for kind, tiles, _ in rows} == {(kind, tiles) for kind in range(4) for tiles in (1, 2)}
+    for kind, tiles, k in rows:
+        assert 64 <= k <= 640 and k % 64 == 0
+        assert k % (64 * tiles) == 0, (kind, tiles, k)
+
+
 def test_scratch_memory():
     with open(BLD.TRAIN_RESOURCES) as f:
         rows = list(csv.DictReader(f, delimiter="\t"))
