@@ -184,13 +184,16 @@ int check_coefficients(const float *coefficients, int32_t steps, float eps) {
         auto at = [&](double t) {
             if (t > 0.0 && t < top) grown = std::max(grown, value(t)), inner = std::max(inner, poly(t));
         };
-        if (c != 0.0) {   // where a + 3 b t + 5 c t^2 or b + 2 c t is 0
-            const double disc = 9.0 * b * b - 20.0 * a * c;
-            if (disc >= 0.0) at((-3.0 * b + std::sqrt(disc)) / (10.0 * c)), at((-3.0 * b - std::sqrt(disc)) / (10.0 * c));
-            at(-b / (2.0 * c));
-        } else if (b != 0.0) {
-            at(-a / (3.0 * b));
+        // where a + 3 b t + 5 c t^2 is 0 (the larger root's numerator without a
+        // difference, the other root from their product: c may be next to nothing
+        // beside b), or b + 2 c t
+        const double disc = 9.0 * b * b - 20.0 * a * c;
+        if (disc >= 0.0) {
+            const double sum = -0.5 * (3.0 * b + std::copysign(std::sqrt(disc), b));
+            if (c != 0.0) at(sum / (5.0 * c));
+            if (sum != 0.0) at(a / sum);
         }
+        if (c != 0.0) at(-b / (2.0 * c));
         if (inner > 60.0 || grown > 4.0)
             return fail(CRF_EINVAL, "step %d takes singular values to %g (at most 4) by a polynomial of %g (at most 60)", k,
                         grown, inner);

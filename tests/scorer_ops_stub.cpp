@@ -7,6 +7,7 @@
 //   products LIB SIDES COUNTS    "T kind tiles k" of each product in tiles of 64 x tiles that
 //                                the update launches for matrices of up to SIDES x 64 rows and
 //                                columns, 1 to COUNTS of them
+//   steps LIB STEPS A B C ...    the status of the update with each set of that many steps' coefficients
 #define main launch_main
 #define hipLaunchKernel plain_hipLaunchKernel
 #include "launch_host_stub.cpp"
@@ -154,6 +155,14 @@ int tile_products(void *lib, int sides, int counts) {
     return 0;
 }
 
+int steps(void *lib, int count, const std::vector<float> &all) {
+    ENTRY(crf_orthogonalize);
+    auto f = [](int k) { return reinterpret_cast<float *>((uintptr_t)(k + 1) << 44); };
+    for (size_t k = 0; k + 3 * count <= all.size(); k += 3 * count)
+        std::printf("%d\n", crf_orthogonalize(f(0), 1, 8, 8, 8, &all[k], count, 1e-7f, f(1), f(2), 1 << 20, nullptr));
+    return 0;
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
@@ -165,6 +174,11 @@ int main(int argc, char **argv) {
     }
     const std::string mode = argv[1];
     if (mode == "alias") return op_aliases(lib);
+    if (mode == "steps" && argc > 6) {
+        std::vector<float> all;
+        for (int k = 4; k < argc; ++k) all.push_back(std::strtof(argv[k], nullptr));
+        return steps(lib, std::atoi(argv[3]), all);
+    }
     std::vector<int> v;
     for (int k = 3; k < argc; ++k) v.push_back(std::atoi(argv[k]));
     if (mode == "grids" && v.size() > 2) return grids(lib, v[0], v[1], std::vector<int32_t>(v.begin() + 2, v.end()));

@@ -168,6 +168,38 @@ def test_update_launches_fit_the_device(harness, shape):
         assert int(threads) <= 1024 and int(lds) <= 160 * 1024, name
 
 
+def reach(co, most=1.0):
+    """(what singular values up to `most` grow to at most, the polynomial's largest value) by dense sampling."""
+    s = most * np.sqrt(np.linspace(0, 1, 200001))
+    a, b, c = np.asarray(co, np.float32).astype(np.float64)
+    poly = np.abs(a + b * s ** 2 + c * s ** 4)
+    return (s * poly).max(), poly.max()
+
+
+# (a, b, 0)'s largest value inside (0, 1), as c goes to 0 from either side; and c
+# that rules, with a root of the derivative near 0
+SMALL_C = [(50, -50, c) for c in (0, 1e-30, -1e-30, 1e-16, -1e-16, 1e-12, 1e-6, -1e-6)] + \
+    [(-20, 20, 1e-20), (30, -40, -1e-25), (10.5, -10.5, 1e-18), (10.3, -10.3, 1e-18), (1e-25, 10, -10), (-1e-25, 11, -11),
+     (1e-20, 30, -30), (0, 12, -12), (10, 0, -10), (3, 1e-20, -3)]
+
+
+def test_steps_are_judged_by_what_they_reach(harness):
+    # every set is refused exactly where sampling says so (none lies within 1e-3 of a bound)
+    rng = np.random.default_rng(0)
+    sets = list(SMALL_C)
+    for _ in range(400):
+        a, b = rng.uniform(-30, 30), rng.uniform(-60, 60)
+        sets.append((a, rng.choice([b, -a, -2 * a]), rng.choice([1.0, 0.0, 1e-7, 1e-15, 1e-24]) * rng.uniform(-40, 40)))
+    bounds = [(g / 4, q / 60) for g, q in map(reach, sets)]
+    sets, bounds = zip(*[(co, max(b)) for co, b in zip(sets, bounds) if all(abs(v - 1) > 1e-3 for v in b)])
+    flat = [repr(float(np.float32(v))) for co in sets for v in co]
+    got = [int(r[0]) for r in run(harness, "steps", 1, *flat)]
+    assert len(got) == len(sets) > 380
+    for co, bound, status in zip(sets, bounds, got):
+        assert status == (B.CRF_EINVAL if bound > 1 else B.CRF_OK), (co, bound)
+    assert 50 < sum(bound > 1 for bound in bounds) < len(sets) - 50
+
+
 def test_tiles_take_whole_rounds_of_k(harness):
     # a product in tiles of 64 M x 64 M runs its K in rounds of 64 M: a rule that
     # picks the tile by the result's sides alone repeats K's last blocks.  Every
