@@ -8,12 +8,16 @@
 //
 // Memory-bound: the rows are read once and written once.  A row lies in the
 // registers of G lanes, eight entries each, so that its mean, its variance (of
-// the deviations, not of squares: a large mean costs no digits) and the two
-// means of the backward pass are sums over lanes, in 32 bits; the backward pass
-// takes the statistics from x again, which it has to read anyway, and nothing is
-// kept for it.  G is the least of 16 .. 1024 whose lanes hold a row: several
-// rows to a wavefront, or several wavefronts to a row, which then meet in LDS.
-// The plan's lists of fence posts give the rows, so that padded ones cost nothing.
+// the deviations, not of squares) and the two means of the backward pass are sums
+// over lanes, in 32 bits.  A mean far past the deviations costs no digits: what its
+// rounding leaves in them is their own mean, which is summed beside their squares
+// and taken off both (without it, means of 1,000 deviations cost the gradients two
+// to three digits; it costs under 1% up to d = 4,096, and 4% at 8,192: 24 paragraphs
+// back 76 us for 72.5).  The backward pass takes the statistics from x again, which
+// it has to read anyway, and nothing is kept for it.  G is the least of 16 .. 1024
+// whose lanes hold a row: several rows to a wavefront, or several wavefronts to a
+// row, which then meet in LDS.  The plan's lists of fence posts give the rows, so
+// that padded ones cost nothing.
 //
 // 5,000 sentences of d = 500 in bf16: 53 us forward (5.1 TB/s, as a large copy), 88
 // back (4.6 TB/s) and 5 for joining the shares of dgamma and dbeta; 24 paragraphs of
@@ -144,20 +148,26 @@ __device__ __forceinline__ float reciprocal_root(float v) {
     return fmaf(0.5f * r, fmaf(-(v * r), r, 1.f), r);
 }
 
-// Deviations from the mean (0 past d) in place, and 1 / sqrt(variance + eps).
+// The normalised row is f r + c: f the deviations from the mean in place (0 past d),
+// r = 1 / sqrt(variance + eps).  The sum's mean is off by some 2^-20 of the
+// entries' size, in every deviation alike; so they have that for their mean, which
+// c takes off them.
 template <int G>
-__device__ __forceinline__ float statistics(float (&f)[8], int k, int d, float eps, float (*slots)[16]) {
+__device__ __forceinline__ void statistics(float (&f)[8], int k, int d, float eps, float (*slots)[16], float &r, float &c) {
     const float each = 1.f / (float)d;
     float s[1] = {((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]))};
     row_sums<G, 1>(s, slots[0]);
     const float m = s[0] * each, m0 = k < d ? m : 0.f, m1 = k + 4 < d ? m : 0.f;   // (entries past d are 0)
+    float two[2] = {0.f, 0.f};
 #pragma unroll
     for (int q = 0; q < 8; ++q) f[q] -= q < 4 ? m0 : m1;
-    s[0] = 0.f;
+    two[0] = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
 #pragma unroll
-    for (int q = 0; q < 8; ++q) s[0] = fmaf(f[q], f[q], s[0]);
-    row_sums<G, 1>(s, slots[1]);
-    return reciprocal_root(fmaf(s[0], each, eps));
+    for (int q = 0; q < 8; ++q) two[1] = fmaf(f[q], f[q], two[1]);
+    row_sums<G, 2>(two, slots[1]);
+    const float rest = two[0] * each, v = fmaf(-rest, rest, two[1] * each);
+    r = reciprocal_root((v < 0.f ? 0.f : v) + eps);   // (a NaN stays one)
+    c = -rest * r;
 }
 
 // A lane's entries of gamma or beta (`none` where there is no array).
@@ -195,7 +205,7 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_kernel(const int32_t *__
                                                                const T *__restrict__ x, const float *__restrict__ gamma,
                                                                const float *__restrict__ beta, float eps,
                                                                uint16_t *__restrict__ y) {
-    __shared__ float slots[2][16];
+    __shared__ float slots[3][16];
     const int k = 8 * (threadIdx.x & (G - 1));
     Ahead<G> rows(posts, chunks);
     Raw<T> raw;
@@ -213,9 +223,10 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_kernel(const int32_t *__
         rows.take();
         load();
         rows.id2 = rows.id_of(c + 2 * gridDim.x);
-        const float r = statistics<G>(f, k, d, eps, slots);
+        float r, rest;
+        statistics<G>(f, k, d, eps, slots, r, rest);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) f[q] = fmaf(f[q] * r, g[q], b[q]);
+        for (int q = 0; q < 8; ++q) f[q] = fmaf(fmaf(f[q], r, rest), g[q], b[q]);
         if (rows.id >= 0) store(y + (size_t)rows.id * d, k, d, f);
     }
 }
@@ -230,7 +241,7 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(const int32_t
                                                                    T *__restrict__ dx, float *__restrict__ parts,
                                                                    float *__restrict__ dgamma, float *__restrict__ dbeta) {
     constexpr int kRows = norm_threads(G) / G;
-    __shared__ float slots[2][16], slots2[2 * 16];
+    __shared__ float slots[3][16], slots2[2 * 16];
     __shared__ float sums[PARTS && kRows > 1 ? kRows * 16 * G : 1];
     const int k = 8 * (threadIdx.x & (G - 1));
     const float each = 1.f / (float)d;
@@ -257,10 +268,11 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(const int32_t
         rows.take();
         load();
         rows.id2 = rows.id_of(c + 2 * gridDim.x);
-        const float r = statistics<G>(f, k, d, eps, slots);
+        float r, rest;
+        statistics<G>(f, k, d, eps, slots, r, rest);
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            f[q] *= r;
+            f[q] = fmaf(f[q], r, rest);   // (past d the gradient is 0)
             if constexpr (PARTS) {   // (a row that is not there adds zeros)
                 sg[q] = fmaf(e[q], f[q], sg[q]);
                 sb[q] += e[q];

@@ -147,6 +147,47 @@ def test_large_offsets_and_constant_rows(torch):
     check(out, h, t + 3 * U * np.abs(h) + rounded(h, False))
 
 
+def corrected(x, eps):
+    """h, r and their errors as statistics(), where the deviations' own mean is
+    taken off them.  f0 = x - m^ is off by u |f0| from x - m less m^'s error e, and
+    |f0| <= |x - m| + e; its mean, e but for 27 u mean|f0|, is taken off with one
+    more rounding:
+      D = x - m   off by 2.01 u |D| + 28 u (mean|D| + e)
+      v           mean f0^2 (34 u of itself) less e^2, which has 2 e times 27 u
+                  mean|f0|: by 34 u v + 90 u e (mean|D| + e)
+    """
+    m = x.mean(-1, keepdims=True)
+    dev = np.abs(x - m)
+    r = 1.0 / np.sqrt((dev ** 2).mean(-1, keepdims=True) + eps)
+    e, size = 26 * U * np.abs(x).mean(-1, keepdims=True), dev.mean(-1, keepdims=True)
+    off = 24 * U + 45 * U * e * (size + e) * r ** 2
+    h = (x - m) * r
+    return h, r, np.abs(h) * off + (2.01 * U * dev + 28 * U * (size + e)) * r, off
+
+
+@pytest.mark.parametrize("d", [100, 128, 500, 1028, 8192])
+@pytest.mark.parametrize("offset", [30.0, 1e3, 1e5])
+def test_a_large_mean_costs_no_digits(torch, d, offset):
+    # means far past the deviations, which float32 outputs show: dx and dgamma
+    lengths, n1 = [9, 20], 22
+    rng = np.random.default_rng(d)
+    x = (rng.standard_normal((2, n1, d)) + offset * (1 + rng.random((2, n1, 1))) * rng.choice([-1, 1], (2, n1, 1))).astype(np.float32)
+    bits, dy = values(lengths, n1, d, d + 2, False)
+    gamma = (1 + 0.3 * rng.standard_normal(d)).astype(np.float32)
+    eps, ok = float(np.float32(1e-5)), there(lengths, n1)
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        dx, dg, _ = (v.cpu().numpy() for v in plan.layer_norm_bwd(device(torch, x), device(torch, gamma), device(torch, bits)))
+    h, r, t, off = corrected(x[ok].astype(np.float64), eps)
+    u = dy[ok] * gamma
+    mean = lambda v: v.mean(-1, keepdims=True)
+    s, q = mean(u), mean(u * h)
+    want = r * (u - s - h * q)
+    e1, e2 = 27 * U * mean(np.abs(u)), 27 * U * mean(np.abs(u * h)) + mean(np.abs(u) * t)
+    tol = r * (3 * U * np.abs(u) + e1 + np.abs(h) * e2 + t * np.abs(q) + 4 * U * (np.abs(s) + np.abs(h * q)))
+    check(dx[ok], want, tol + np.abs(want) * off + rounded(want, True))
+    check(dg, (dy[ok] * h).sum(0), (np.abs(dy[ok]) * t).sum(0) + int(ok.sum()) * U * np.abs(dy[ok] * h).sum(0))
+
+
 @pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
 @pytest.mark.parametrize("d", [100, 252, 500, 1500])
 def test_one_row_is_not_finite(torch, d, bad):
