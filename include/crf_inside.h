@@ -482,7 +482,7 @@ int crf_biaffine_bwd_packed(const crf_plan *plan, const uint8_t *rl_codes, const
  *           aligned) or float32 (CRF_F32); rows past n_b are not read.
  *   d       4 <= d <= CRF_MAX_ROW, a multiple of 4.
  *   gamma, beta  device float32[d], or NULL: 1 and 0.
- *   eps     positive.
+ *   eps     finite, 2^-126 (float32's least normal number) or more.
  *   y       device bf16 bit patterns [B][N1][d], 8-byte aligned; must not alias x.
  * A row with an infinity or NaN, or whose sum of squared deviations passes what
  * float32 holds, becomes NaN, other rows are as without it.  Rows past n_b are

@@ -139,11 +139,10 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float *slots) {
     }
 }
 
-// 1 / sqrt(v) for v > 0: the instruction's value (off by 2^-23 at most) and a
-// Newton step, 8 instructions where the library's root and division take 40.  (v
-// below the least normal number is taken as that: deviations are all 0 then.)
+// 1 / sqrt(v) for v of eps (a normal number) or more: the instruction's value (off by
+// 2^-23 at most) and a Newton step, 8 instructions where the library's root and
+// division take 40.
 __device__ __forceinline__ float reciprocal_root(float v) {
-    v = v < 1.17549435e-38f ? 1.17549435e-38f : v;   // (a NaN stays one)
     const float r = __builtin_amdgcn_rsqf(v);
     return fmaf(0.5f * r, fmaf(-(v * r), r, 1.f), r);
 }

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <initializer_list>
@@ -133,7 +134,9 @@ int check_norm(const void *x, int32_t x_type, int32_t d, float eps) {
         return fail(CRF_EINVAL, "x_type %d is neither CRF_BF16 nor CRF_F32", x_type);
     if (misaligned(x, x_type == CRF_BF16 ? 8 : 4))
         return fail(CRF_EINVAL, "x must be %d-byte aligned", x_type == CRF_BF16 ? 8 : 4);
-    if (!finite_positive(eps) || eps == 0.f) return fail(CRF_EINVAL, "eps %g is not positive and finite", (double)eps);
+    // (squares beside a smaller one would be of few digits)
+    if (!finite_positive(eps) || eps < FLT_MIN)
+        return fail(CRF_EINVAL, "eps %g is not a finite number of 2^-126 or more", (double)eps);
     return CRF_OK;
 }
 

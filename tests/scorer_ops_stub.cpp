@@ -8,6 +8,7 @@
 //                                the update launches for matrices of up to SIDES x 64 rows and
 //                                columns, 1 to COUNTS of them
 //   steps LIB STEPS A B C ...    the status of the update with each set of that many steps' coefficients
+//   eps LIB EPS ...              the statuses of layer norm and of its backward pass with each
 #define main launch_main
 #define hipLaunchKernel plain_hipLaunchKernel
 #include "launch_host_stub.cpp"
@@ -163,6 +164,23 @@ int steps(void *lib, int count, const std::vector<float> &all) {
     return 0;
 }
 
+int norm_eps(void *lib, const std::vector<float> &all) {
+    ENTRY(crf_plan_create); ENTRY(crf_plan_destroy); ENTRY(crf_layer_norm); ENTRY(crf_layer_norm_bwd);
+    ENTRY(crf_layer_norm_bwd_workspace);
+    const int32_t len[kB] = {8, 3, 5};
+    crf_plan *p = nullptr;
+    if (crf_plan_create(&p, len, kB, kN1, 1, 0) != CRF_OK) return 1;
+    int64_t nw = 0;
+    crf_layer_norm_bwd_workspace(p, kD, &nw);
+    auto f = [](int k) { return reinterpret_cast<float *>((uintptr_t)(k + 1) << 44); };
+    for (const float eps : all)
+        std::printf("%d %d\n", crf_layer_norm(p, f(0), CRF_F32, kD, nullptr, nullptr, eps, (uint16_t *)f(1), nullptr),
+                    crf_layer_norm_bwd(p, f(0), CRF_F32, kD, nullptr, (uint16_t *)f(1), eps, f(2), f(3), f(4), f(5), nw,
+                                       nullptr));
+    crf_plan_destroy(p);
+    return 0;
+}
+
 }  // namespace
 
 int main(int argc, char **argv) {
@@ -174,11 +192,10 @@ int main(int argc, char **argv) {
     }
     const std::string mode = argv[1];
     if (mode == "alias") return op_aliases(lib);
-    if (mode == "steps" && argc > 6) {
-        std::vector<float> all;
-        for (int k = 4; k < argc; ++k) all.push_back(std::strtof(argv[k], nullptr));
-        return steps(lib, std::atoi(argv[3]), all);
-    }
+    std::vector<float> all;
+    for (int k = 3; k < argc; ++k) all.push_back(std::strtof(argv[k], nullptr));
+    if (mode == "steps" && argc > 6) return steps(lib, std::atoi(argv[3]), std::vector<float>(all.begin() + 1, all.end()));
+    if (mode == "eps" && argc > 3) return norm_eps(lib, all);
     std::vector<int> v;
     for (int k = 3; k < argc; ++k) v.push_back(std::atoi(argv[k]));
     if (mode == "grids" && v.size() > 2) return grids(lib, v[0], v[1], std::vector<int32_t>(v.begin() + 2, v.end()));

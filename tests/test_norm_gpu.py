@@ -188,6 +188,20 @@ def test_a_large_mean_costs_no_digits(torch, d, offset):
     check(dg, (dy[ok] * h).sum(0), (np.abs(dy[ok]) * t).sum(0) + int(ok.sum()) * U * np.abs(dy[ok] * h).sum(0))
 
 
+@pytest.mark.parametrize("scale", [1e-20, 1e-19, 1e-18])
+def test_the_least_eps(torch, scale):
+    # squares about float32's least normal number, which eps is: each square, their
+    # mean and the square that is taken off it are off by 2^-150 at most, which is
+    # 3 u / 2 of 1 / sqrt(v + eps) at v + eps >= 2^-126
+    lengths, n1, d, eps = [9], 10, 500, 2.0 ** -126
+    raw, _ = values(lengths, n1, d, 19, True, offset=0.0)
+    raw = (raw * scale).astype(np.float32)
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        out = plan.layer_norm(device(torch, raw), eps=eps).float().cpu().numpy()
+    h, _, t, _ = statistics(raw.astype(np.float64), eps)
+    check(out, h, t + 5 * U * np.abs(h) + rounded(h, False))
+
+
 @pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
 @pytest.mark.parametrize("d", [100, 252, 500, 1500])
 def test_one_row_is_not_finite(torch, d, bad):

@@ -168,6 +168,18 @@ def test_update_launches_fit_the_device(harness, shape):
         assert int(threads) <= 1024 and int(lds) <= 160 * 1024, name
 
 
+def test_eps_of_a_norm(harness):
+    # a variance beside an eps below float32's least normal number, 2^-126, would be
+    # one of squares of few digits
+    least = 2.0 ** -126
+    bad = [0.0, -1.0, float("nan"), float("inf"), 2.0 ** -149, 1e-40, least * (1 - 2.0 ** -23)]
+    good = [least, 1.2e-38, 1e-12, 1e-5, 1.0]
+    for status in run(harness, "eps", *map(repr, bad)):
+        assert status == [str(B.CRF_EINVAL)] * 2
+    for status in run(harness, "eps", *map(repr, good)):
+        assert status == [str(B.CRF_OK)] * 2
+
+
 def reach(co, most=1.0):
     """(what singular values up to `most` grow to at most, the polynomial's largest value) by dense sampling."""
     s = most * np.sqrt(np.linspace(0, 1, 200001))
