@@ -90,6 +90,30 @@ def test_bias_and_gradient(torch, name, L):
     assert np.all(np.abs(gt.cpu().numpy() - sums) <= count * 2.0 ** -24 * size)
 
 
+@pytest.mark.parametrize("K", [1, 16, 64, 65, 1024])
+@pytest.mark.parametrize("L,lengths", [(1, [1000, 40, 7]), (1, [1023]), (1, [30, 12, 1] * 400), (3, [300, 17, 64]), (4, [255, 9]),
+                                       (15, [130, 61, 3]), (16, [130, 61, 3]), (26, [90, 90, 2])])
+def test_many_buckets(torch, L, lengths, K):
+    # sums by bucket (up to 64 of few labels) and by width, one label and more: small
+    # whole numbers, of which float32 holds every sum, so a cell that is lost or
+    # counted twice shows
+    n1 = max(lengths) + 1
+    rng = np.random.default_rng(K + L)
+    g = rng.integers(-8, 9, (len(lengths), n1, n1) + ((L,) if L > 1 else ())).astype(np.float32)
+    valid = W.valid_mask(np.asarray(lengths), n1)
+    g[~valid] = np.nan
+    buckets = rng.integers(-1, K + 1, n1).astype(np.int32)
+    buckets[1:4] = K - 1, 0, K
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        gs, gt = plan.width_bias_bwd(torch.from_numpy(g).to("cuda:0"), torch.from_numpy(buckets).to("cuda:0"), K)
+    w = np.broadcast_to((np.arange(n1)[None] - np.arange(n1)[:, None])[None], valid.shape)[valid]
+    want = np.zeros((K + 2, L), np.int64)
+    np.add.at(want, buckets[w], g[valid].reshape(-1, L).astype(np.int64))   # (-1 and K: the last two)
+    assert np.abs(g[valid]).sum() < 2 ** 24 * L
+    assert np.array_equal(gt.cpu().numpy(), want[:K])
+    assert np.array_equal(gs.cpu().numpy()[valid], g[valid]) and (gs.cpu().numpy()[~valid] == 0).all()
+
+
 @pytest.mark.parametrize("shift", [1, 2])
 def test_arrays_that_start_inside_a_vector(torch, shift):
     lengths, n1, L, K = [9, 4, 17], 18, 4, 3
