@@ -6,18 +6,17 @@
 //     dx = r (u - mean(u) - h mean(u h)),   u = dy gamma,
 //     dgamma = sum of dy h over the rows,   dbeta = sum of dy.
 //
-// Memory-bound: the rows are read once and written once.  A row lies in the
-// registers of G lanes, eight entries each, so that its mean, its variance (of
-// the deviations, not of squares) and the two means of the backward pass are sums
-// over lanes, in 32 bits.  A mean far past the deviations costs no digits: what its
-// rounding leaves in them is their own mean, which is summed beside their squares
-// and taken off both (without it, means of 1,000 deviations cost the gradients two
-// to three digits; it costs under 1% up to d = 4,096, and 4% at 8,192: 24 paragraphs
-// back 76 us for 72.5).  The backward pass takes the statistics from x again, which
-// it has to read anyway, and nothing is kept for it.  G is the least of 16 .. 1024
-// whose lanes hold a row: several rows to a wavefront, or several wavefronts to a
-// row, which then meet in LDS.  The plan's lists of fence posts give the rows, so
-// that padded ones cost nothing.
+// Memory-bound: the rows are read once and written once.  A row lies in the registers
+// of G lanes, eight entries each, so that its mean, its variance (of the deviations,
+// not of squares) and the two means of the backward pass are sums over lanes, in 32
+// bits.  A mean far past the deviations costs no digits: what its rounding leaves in
+// them is their own mean, which is summed beside their squares and taken off both
+// (means of 1,000 deviations: dgamma off by 1e-4 without it, by 1e-7 with it, for 0.3
+// us of 62 and no more of d = 8,192).  The backward pass takes the statistics from x
+// again, which it has to read anyway, and nothing is kept for it.  G is the least of
+// 16 .. 1024 whose lanes hold a row: several rows to a wavefront, or several
+// wavefronts to a row, which then meet in LDS.  The plan's lists of fence posts give
+// the rows, so that padded ones cost nothing.
 //
 // 5,000 sentences of d = 500 in bf16: 53 us forward (5.1 TB/s, as a large copy), 88
 // back (4.6 TB/s) and 5 for joining the shares of dgamma and dbeta; 24 paragraphs of
@@ -150,7 +149,8 @@ __device__ __forceinline__ float reciprocal_root(float v) {
 // The normalised row is f r + c: f the deviations from the mean in place (0 past d),
 // r = 1 / sqrt(variance + eps).  The sum's mean is off by some 2^-20 of the
 // entries' size, in every deviation alike; so they have that for their mean, which
-// c takes off them.
+// c takes off them.  (A variance of 2^-20 of that squared is no more than the
+// roundings of the two: what is less, for a row of one value, counts as that.)
 template <int G>
 __device__ __forceinline__ void statistics(float (&f)[8], int k, int d, float eps, float (*slots)[16], float &r, float &c) {
     const float each = 1.f / (float)d;
@@ -164,8 +164,8 @@ __device__ __forceinline__ void statistics(float (&f)[8], int k, int d, float ep
 #pragma unroll
     for (int q = 0; q < 8; ++q) two[1] = fmaf(f[q], f[q], two[1]);
     row_sums<G, 2>(two, slots[1]);
-    const float rest = two[0] * each, v = fmaf(-rest, rest, two[1] * each);
-    r = reciprocal_root((v < 0.f ? 0.f : v) + eps);   // (a NaN stays one)
+    const float rest = two[0] * each, v = fmaf(-rest, rest, two[1] * each), least = rest * rest * 0x1p-20f;
+    r = reciprocal_root((v < least ? least : v) + eps);   // (a NaN stays one)
     c = -rest * r;
 }
 

@@ -188,6 +188,27 @@ def test_a_large_mean_costs_no_digits(torch, d, offset):
     check(dg, (dy[ok] * h).sum(0), (np.abs(dy[ok]) * t).sum(0) + int(ok.sum()) * U * np.abs(dy[ok] * h).sum(0))
 
 
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("d", [4, 12, 100, 164, 500, 508, 1028, 4100, 6212, 7132, 7684, 8052, 8188, 8192])
+def test_rows_of_one_value(torch, d, wide):
+    # deviations of 0, whatever the value up to 2^76: what the mean's rounding e leaves
+    # of them is 27 u e once their mean is off, over the root of 2^-20 e^2 at least:
+    # 2^-9.  (A row of zeros is exact.  The first values: with these d, sums of their
+    # deviations over d are not their deviation.)
+    sizes = 2.0 ** 76 * 10.0 ** -np.linspace(0, 60, 59)
+    sizes[1:9:2] = 2.908594e16, 32087424000000.0, 2.4709912e20, 4.7043146e21
+    lengths, n1 = [29, 29], 30
+    x = np.zeros((2, n1, d), np.float32)
+    x.reshape(60, d)[:59] = (sizes * np.where(np.arange(59) % 2, 1, -0.97))[:, None]
+    raw = x if wide else W.to_bf16(x)
+    with B.Plan(lengths, n1=n1, device="cuda:0") as plan:
+        h = plan.layer_norm(device(torch, raw)).float().cpu().numpy()
+        dy = torch.ones((2, n1, d), dtype=torch.bfloat16, device="cuda:0")
+        dx, dg, db = (v.float().cpu().numpy() for v in plan.layer_norm_bwd(device(torch, raw), None, dy))
+    assert np.all(np.abs(h) <= 2.0 ** -9) and np.all(h[1, 29] == 0)
+    assert np.all(np.abs(dg) <= 60 * 2.0 ** -9) and np.all(db == 60) and np.isfinite(dx).all()
+
+
 @pytest.mark.parametrize("scale", [1e-20, 1e-19, 1e-18])
 def test_the_least_eps(torch, scale):
     # squares about float32's least normal number, which eps is: each square, their
