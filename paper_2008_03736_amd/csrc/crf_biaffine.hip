@@ -560,11 +560,12 @@ hipError_t scorer_attributes() {
 }  // namespace
 
 hipError_t set_biaffine_attributes() {
-    for (auto set : {scorer_attributes<4, false>, scorer_attributes<8, false>, scorer_attributes<4, true>, scorer_attributes<8, true>}) {
-        const hipError_t e = set();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    const hipError_t e = scorer_attributes<4, false>();
+    return e != hipSuccess ? e : scorer_attributes<8, false>();
+}
+hipError_t set_biaffine_biased_attributes() {
+    const hipError_t e = scorer_attributes<4, true>();
+    return e != hipSuccess ? e : scorer_attributes<8, true>();
 }
 
 int64_t biaffine_lds_bytes(int) {

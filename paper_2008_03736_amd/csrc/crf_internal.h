@@ -659,6 +659,7 @@ hipError_t set_biaffine_attributes();   // once per plan: the LDS of the largest
 hipError_t launch_biaffine(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
                            int ldw, int L, float *scores, hipStream_t stream);
 // The same with a bias by width (table [K][L], bucket [N1]) added.
+hipError_t set_biaffine_biased_attributes();   // (once per device)
 hipError_t launch_biaffine_biased(const KernelPlan &p, const uint16_t *rl, const uint16_t *rr, const uint16_t *w, int d,
                                   int ldw, int L, const float *table, const int32_t *bucket, int K, float *scores,
                                   hipStream_t stream);

@@ -437,6 +437,10 @@ int crf_biaffine_scores_biased(const crf_plan *plan, const uint16_t *rl, const u
                              {"buckets", buckets, 4 * (int64_t)plan->n1}})) != CRF_OK ||
         (rc = check_device(plan)) != CRF_OK)
         return rc;
+    static std::once_flag set[64];   // (see scorer_backward)
+    std::call_once(set[plan->device & 63], [] {
+        if (crf::set_biaffine_biased_attributes() != hipSuccess) (void)hipGetLastError();
+    });
     const hipError_t e = crf::launch_biaffine_biased(plan->kp, rl, rr, w, d, ldw, num_labels, table, buckets, num_buckets,
                                                      scores, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ok() : hip_fail(e, "crf_biaffine_scores_biased launch");

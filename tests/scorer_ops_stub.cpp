@@ -9,6 +9,9 @@
 //                                columns, 1 to COUNTS of them
 //   steps LIB STEPS A B C ...    the status of the update with each set of that many steps' coefficients
 //   eps LIB EPS ...              the statuses of layer norm and of its backward pass with each
+//   biased LIB                   "A name" of each scorer kernel whose attribute a plan's creation sets, then
+//                                of two threads' first calls of the scorer with a bias "EARLY name" of each
+//                                kernel launched before its attribute was set, and "launches N"
 #define main launch_main
 #define hipLaunchKernel plain_hipLaunchKernel
 #include "launch_host_stub.cpp"
@@ -26,6 +29,8 @@ struct ProductHead {
 }
 
 extern "C" hipError_t hipLaunchKernel(const void *f, dim3 g, dim3 b, void **args, size_t lds, hipStream_t) {
+    std::lock_guard<std::mutex> lock(mu);
+    if (watch_attributes && lds > 65536 && ready.count(f) == 0) early.push_back(names[f]);
     std::string name = names[f];
     const size_t tile = name.find("ortho_tile_kernel<");
     if (tile != std::string::npos) {   // (kind and tiles are its template's arguments, the kind perhaps with its type)
@@ -164,6 +169,34 @@ int steps(void *lib, int count, const std::vector<float> &all) {
     return 0;
 }
 
+int biased(void *lib) {
+    ENTRY(crf_plan_create); ENTRY(crf_plan_destroy); ENTRY(crf_biaffine_scores_biased);
+    const int32_t len[kB] = {8, 3, 100};
+    crf_plan *p[2] = {nullptr, nullptr};
+    for (auto &x : p)
+        if (crf_plan_create(&x, len, kB, 101, 1, 0) != CRF_OK) return 1;
+    for (const void *f : ready)
+        if (names[f].find("biaffine") != std::string::npos) std::printf("A %s\n", names[f].c_str());
+    shapes.clear();
+    slow_attributes = watch_attributes = true;
+    int rc[2] = {0, 0};
+    auto call = [&](int t) {
+        auto at = [&](int k) { return reinterpret_cast<char *>(((uintptr_t)1 << 40) + ((uintptr_t)(16 * t + k) << 28)); };
+        rc[t] = crf_biaffine_scores_biased(p[t], (uint16_t *)at(0), (uint16_t *)at(1), (uint16_t *)at(2), 500, 504, 1,
+                                           (float *)at(3), (int32_t *)at(4), 4, (float *)at(5), nullptr);
+    };
+    std::thread a(call, 0), b([&]() {
+        std::this_thread::sleep_for(std::chrono::milliseconds(5));   // the first thread is at its attributes
+        call(1);
+    });
+    a.join();
+    b.join();
+    for (const std::string &x : early) std::printf("EARLY %s\n", x.c_str());
+    std::printf("launches %d status %d %d\n", (int)shapes.size(), rc[0], rc[1]);
+    for (auto *x : p) crf_plan_destroy(x);
+    return 0;
+}
+
 int norm_eps(void *lib, const std::vector<float> &all) {
     ENTRY(crf_plan_create); ENTRY(crf_plan_destroy); ENTRY(crf_layer_norm); ENTRY(crf_layer_norm_bwd);
     ENTRY(crf_layer_norm_bwd_workspace);
@@ -192,6 +225,7 @@ int main(int argc, char **argv) {
     }
     const std::string mode = argv[1];
     if (mode == "alias") return op_aliases(lib);
+    if (mode == "biased") return biased(lib);
     std::vector<float> all;
     for (int k = 3; k < argc; ++k) all.push_back(std::strtof(argv[k], nullptr));
     if (mode == "steps" && argc > 6) return steps(lib, std::atoi(argv[3]), std::vector<float>(all.begin() + 1, all.end()));

@@ -6,6 +6,7 @@ import ctypes
 import csv
 import math
 import os
+import re
 import shutil
 import subprocess
 from fractions import Fraction
@@ -222,6 +223,16 @@ def test_tiles_take_whole_rounds_of_k(harness):
     for kind, tiles, k in rows:
         assert 64 <= k <= 640 and k % 64 == 0
         assert k % (64 * tiles) == 0, (kind, tiles, k)
+
+
+def test_attributes_of_the_scorer_with_a_bias(harness):
+    # set once a device, before any thread's first launch there; a plan sets those
+    # of the scorer without one alone
+    rows = run(harness, "biased")
+    plans = [" ".join(r[1:]) for r in rows if r[0] == "A"]
+    assert len(plans) == 10 and all(re.search(r"_kernel<[^>]*, false>", name) for name in plans)
+    assert rows[-1] == ["launches", "2", "status", "0", "0"]
+    assert not [r for r in rows if r[0] == "EARLY"]
 
 
 def test_scratch_memory():
