@@ -477,7 +477,8 @@ int crf_biaffine_bwd_packed(const crf_plan *plan, const uint8_t *rl_codes, const
  * crf_layer_norm -- layer norm of activation rows: with m and v the mean and the
  * variance of a row's d entries,
  *   y = (x - m) / sqrt(v + eps) * gamma + beta.
- * Sums in float32; the variance is that of the deviations from the mean.
+ * Sums in float32; the variance is that of the deviations from the mean, and what
+ * the mean's rounding leaves in them is taken off.
  *   x       device [B][N1][d], bf16 bit patterns (x_type CRF_BF16, 8-byte
  *           aligned) or float32 (CRF_F32); rows past n_b are not read.
  *   d       4 <= d <= CRF_MAX_ROW, a multiple of 4.
@@ -485,8 +486,9 @@ int crf_biaffine_bwd_packed(const crf_plan *plan, const uint8_t *rl_codes, const
  *   eps     finite, 2^-126 (float32's least normal number) or more.
  *   y       device bf16 bit patterns [B][N1][d], 8-byte aligned; must not alias x.
  * A row with an infinity or NaN, or whose sum of squared deviations passes what
- * float32 holds, becomes NaN, other rows are as without it.  Rows past n_b are
- * left as they were.  B, N1 and the lengths are the plan's.
+ * float32 holds, becomes NaN, as may one of entries past 2^76 in size, whose mean's
+ * rounding or sum can do so; other rows are as without it.  Rows past n_b are left
+ * as they were.  B, N1 and the lengths are the plan's.
  */
 int crf_layer_norm(const crf_plan *plan, const void *x, int32_t x_type, int32_t d, const float *gamma, const float *beta,
                    float eps, uint16_t *y, void *stream);
@@ -572,9 +574,10 @@ int crf_orthogonalize_workspace(int32_t count, int32_t rows, int32_t cols, int64
  *   coefficients  host float[steps][3], read during the call.  Singular values
  *                 from [0, 1] must stay in [0, 4] after every step, and
  *                 |a + b s^2 + c s^4| within 60 (CRF_EINVAL otherwise: the parts
- *                 of larger values would overflow).
+ *                 of larger values would overflow); none past 1,000 in size.
  *   steps         1 <= steps <= CRF_MAX_STEPS.
- *   eps           positive.
+ *   eps           positive.  The parts of x / (|x|_F + eps) are whole multiples of
+ *                 2^-36, so where |x|_F is far below eps they have few digits.
  * A matrix with an infinity or NaN gives NaN everywhere, the others are as
  * without it; a matrix of zeros gives zeros.
  */

@@ -213,6 +213,13 @@ def test_steps_are_judged_by_what_they_reach(harness):
     assert 50 < sum(bound > 1 for bound in bounds) < len(sets) - 50
 
 
+def test_coefficients_past_a_thousand(harness):
+    # refused whatever they reach: a first step to 0.01, where b s^2 is 0.15 at most
+    sets = [(0.01, 0, 0, 1, b, c) for b, c in ((999, 0), (1500, 0), (-1500, 0), (1000, 0), (0, 1000), (0, 2000), (1, -1001))]
+    got = [int(r[0]) for r in run(harness, "steps", 2, *(v for co in sets for v in co))]
+    assert got == [B.CRF_EINVAL if max(abs(v) for v in co) > 1000 else B.CRF_OK for co in sets]
+
+
 def test_tiles_take_whole_rounds_of_k(harness):
     # a product in tiles of 64 M x 64 M runs its K in rounds of 64 M: a rule that
     # picks the tile by the result's sides alone repeats K's last blocks.  Every
