@@ -18,7 +18,7 @@
 // wavefronts to a row, which then meet in LDS.  The plan's lists of fence posts give
 // the rows, so that padded ones cost nothing.
 //
-// 5,000 sentences of d = 500 in bf16: 53 us forward (5.1 TB/s, as a large copy), 88
+// 5,000 sentences of d = 500 in bf16: 54 us forward (5.0 TB/s, a large copy 5.1), 89
 // back (4.6 TB/s) and 5 for joining the shares of dgamma and dbeta; 24 paragraphs of
 // d = 4,096 in float32 46 and 5 back; a sentence alone 3, a launch.
 #include <hip/hip_runtime.h>

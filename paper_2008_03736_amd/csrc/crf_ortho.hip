@@ -20,7 +20,7 @@
 //
 // Three ways, by size (five steps): thin matrices whole in registers (one of 16 x
 // 1,000 in 26 us), small ones in a workgroup's LDS and registers (138 of 100 x 101
-// in 46 us, 300 of 32 x 500 in 77), others a launch a product, tile by tile (one of
+// in 46 us, 300 of 32 x 500 in 78), others a launch a product, tile by tile (one of
 // 500 x 501 in 92 us, of 2,048 x 2,048 in 707).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -701,7 +701,7 @@ void launch_thin(const OrthoIo &io, const Steps &steps, int count, hipStream_t s
 // shares the work evenly.  Bound by a step's three chains (products, LDS, barrier):
 // 6.6 us a step of 100 x 101 whether there is one matrix or 138, the matrix cores
 // 23% busy; 300 of 100 x 150 take 116 us, a launch a product 351, 300 of 32 x 500
-// 77 and 221.
+// 78 and 221.
 constexpr int kSmallRows = 128;
 __host__ __device__ constexpr int small_stride(int tiles) { return (tiles + 1) / 2 * 32 + 8; }   // of a row of 16 `tiles`
 inline int64_t small_lds(int p, int q) {

@@ -14,7 +14,8 @@
 //
 // 5,000 sentences, one label: 9.6 us forward; 15.4 back, and 4 to join the shares.
 // Their rows are 12 cells long on the average, at odd places: 25 MB of lines are
-// read for 7.9 MB of cells.  100 sentences of 138 labels: 12.3 us forward (3.7 TB/s
+// read for 7.9 MB of cells, both ways; back, a thread's 32 loads a block are all
+// issued, whatever the rows' lengths.  100 sentences of 138 labels: 12.3 us forward (3.7 TB/s
 // of the cells); 12.3 back and 4.2, as long as the few passes of a workgroup.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
